@@ -1,0 +1,38 @@
+// Launch descriptors of the shared-prefix attention and paged-cache kernels (flasheval_prefix.h).
+#pragma once
+
+#include "fe_common.h"
+#include "flasheval_prefix.h"
+
+constexpr int kPrefixMaxLen = 1 << 22;   // T and L: a tile's packed own rows (256 lists) stay in int32
+
+// One attention call as its kernels see it.  The query rows of a (request, key head) are numbered
+// r = (k S + s) G + hg < R with G = n_heads / n_kv_heads, so the rows that share keys are adjacent.
+struct PrefixArgs {
+  const void *q, *ctx_k, *ctx_v, *own_k, *own_v;
+  const int32_t *table, *ctx_len, *q_len, *own_len;
+  void* out; float* lse;
+  int B, K, S, Hq, Hkv, T, L, page_rows, n_pages, causal;
+  int q_ld, ctx_ld, own_ld, out_ld;
+  float scale;
+  int G, R;
+  int tiles, splits;                    // row tiles per (request, key head); key ranges per tile
+  float *part_o, *part_ml;              // splits > 1: [splits][B*K*S*Hq][dh] sums, [..][2] maximum and sum
+};
+
+// The gradient's further tensors.
+struct PrefixGradArgs {
+  PrefixArgs f;
+  const void* dout; int dout_ld;
+  void *dq, *dctx_k, *dctx_v, *down_k, *down_v;
+  int dq_ld, dctx_ld, down_ld;
+  float* delta;                         // [B*K*S*Hq] dout . out
+  int ctx_tiles, own_tiles;             // key tiles of the shared rows / of the own rows per (request, key head)
+};
+
+// Row tiles, key ranges and partial-sum bytes of a forward call: functions of the sizes alone.
+struct PrefixPlan { int rows, tiles, splits; size_t part_bytes; };
+PrefixPlan prefix_plan(const fe_prefix_args& a);
+hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixPlan& p, hipStream_t s);
+hipError_t launch_prefix_grad(PrefixGradArgs a, int dh, bool bf16_rows, hipStream_t s);
+hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s);

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libflasheval.so")
 FE_OK, FE_EINVAL, FE_EUNSUPPORTED, FE_ENOMEM, FE_EHIP = range(5)
 FE_F32, FE_BF16 = 0, 1
 FE_ATTN_SOFTMAX, FE_ATTN_LINEAR = 0, 1
-FE_DEV_BAD_INDEX, FE_DEV_BAD_TOKEN = 1, 2
+FE_DEV_BAD_INDEX, FE_DEV_BAD_TOKEN, FE_DEV_BAD_PAGE = 1, 2, 4
 FE_LOSS_MSE, FE_LOSS_BCE, FE_LOSS_CE = 0, 1, 2
 LOSS_KIND = {"mse": FE_LOSS_MSE, "bce": FE_LOSS_BCE, "ce": FE_LOSS_CE}
 
@@ -27,7 +27,8 @@ EXPORTED = ("fe_param_count", "fe_model_create", "fe_model_destroy", "fe_workspa
             "fe_read_device_status", "fe_encode_context", "fe_encode_items", "fe_assemble", "fe_cross_sequence",
             "fe_cross_sequence_noalloc", "fe_score_select", "fe_encode_sequences", "fe_score_objectives", "fe_naive_workspace_size", "fe_evaluate_naive", "fe_trace_enable", "fe_trace_read",
             "fe_trace_read_launches", "fe_trace_family", "fe_train_workspace_size", "fe_train_grads",
-            "fe_executor_create", "fe_executor_submit", "fe_executor_join", "fe_executor_destroy")
+            "fe_executor_create", "fe_executor_submit", "fe_executor_join", "fe_executor_destroy",
+            "fe_cache_append", "fe_prefix_workspace_size", "fe_prefix_attention", "fe_prefix_attention_grad")
 FE_EXECUTOR_MAX_STREAMS = 8
 FE_TRACE_FAMILIES = 12
 
@@ -51,6 +52,28 @@ class fe_pass_args(ctypes.Structure):
                 ("n_uniq", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("H", ctypes.c_void_p), ("seq", ctypes.c_void_p),
                 ("Cp", ctypes.c_void_p), ("scores", ctypes.c_void_p), ("best", ctypes.c_void_p), ("ws", ctypes.c_void_p),
                 ("ws_bytes", ctypes.c_size_t)]
+
+
+def _struct(name: str, ints: str, pointers: str, tail=()):
+    """A ctypes structure of int32 fields followed by pointer fields, in the order of the C header."""
+    fields = [(n, ctypes.c_float if n == "scale" else ctypes.c_int32) for n in ints.split()]
+    fields += [(n, ctypes.c_void_p) for n in pointers.split()]
+    return type(name, (ctypes.Structure,), {"_fields_": fields + list(tail)})
+
+
+fe_append_args = _struct(
+    "fe_append_args", "dtype N S n_heads n_kv_heads dh rot neighbours page_rows n_pages table_cols q_ld k_ld v_ld q_out_ld page_ld",
+    "q k v q_out freq table len new_len pos0 k_pages v_pages len_out status")
+fe_prefix_args = _struct(
+    "fe_prefix_args", "dtype B K S n_heads n_kv_heads dh T L page_rows n_pages causal scale q_ld ctx_ld own_ld out_ld",
+    "q ctx_k ctx_v own_k own_v table ctx_len q_len own_len out lse ws", [("ws_bytes", ctypes.c_size_t)])
+
+
+class fe_prefix_grads(ctypes.Structure):
+    _fields_ = [("dout", ctypes.c_void_p), ("dout_ld", ctypes.c_int32), ("dq_ld", ctypes.c_int32),
+                ("dctx_ld", ctypes.c_int32), ("down_ld", ctypes.c_int32), ("dq", ctypes.c_void_p),
+                ("dctx_k", ctypes.c_void_p), ("dctx_v", ctypes.c_void_p), ("down_k", ctypes.c_void_p),
+                ("down_v", ctypes.c_void_p)]
 
 
 _lib = None
@@ -95,6 +118,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fe_executor_submit": (S, [P, ctypes.POINTER(fe_pass_args), P]),
         "fe_executor_join": (S, [P, P]),
         "fe_executor_destroy": (None, [P]),
+        "fe_cache_append": (S, [ctypes.POINTER(fe_append_args), P]),
+        "fe_prefix_workspace_size": (S, [ctypes.POINTER(fe_prefix_args), I, ctypes.POINTER(Z)]),
+        "fe_prefix_attention": (S, [ctypes.POINTER(fe_prefix_args), P]),
+        "fe_prefix_attention_grad": (S, [ctypes.POINTER(fe_prefix_args), ctypes.POINTER(fe_prefix_grads), P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -316,6 +343,26 @@ def fe_train_grads(cfg: fe_config, params, B: int, T: int, M: int, K: int, L: in
            "fe_train_grads")
 
 
+def fe_cache_append(args: fe_append_args, stream=None) -> None:
+    _check(load_library().fe_cache_append(ctypes.byref(args), _stream(stream)), "fe_cache_append")
+
+
+def fe_prefix_workspace_size(args: fe_prefix_args, grad: bool = False) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().fe_prefix_workspace_size(ctypes.byref(args), 1 if grad else 0, ctypes.byref(n)),
+           "fe_prefix_workspace_size")
+    return n.value
+
+
+def fe_prefix_attention(args: fe_prefix_args, stream=None) -> None:
+    _check(load_library().fe_prefix_attention(ctypes.byref(args), _stream(stream)), "fe_prefix_attention")
+
+
+def fe_prefix_attention_grad(args: fe_prefix_args, grads: fe_prefix_grads, stream=None) -> None:
+    _check(load_library().fe_prefix_attention_grad(ctypes.byref(args), ctypes.byref(grads), _stream(stream)),
+           "fe_prefix_attention_grad")
+
+
 def fe_trace_enable(on: bool) -> None:
     _check(load_library().fe_trace_enable(1 if on else 0), "fe_trace_enable")
 
@@ -482,3 +529,205 @@ class Executor:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------------------------------------
+# Lists over a shared context: paged cache and attention (include/flasheval_prefix.h)
+# ---------------------------------------------------------------------------------------------
+
+def _act(dtype: str):
+    import torch
+    if dtype not in ("bf16", "f32"):
+        raise ValueError(f"dtype must be 'bf16' or 'f32', got {dtype!r}")
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def _row_stride(t, name: str, shape: Tuple[int, ...], dtype) -> int:
+    """Elements from one row to the next of a tensor [..][heads][dh] whose rows are evenly spaced and dense inside
+    (column blocks of a wider tensor qualify); raises ValueError for any other layout, shape or type."""
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected a {dtype} tensor {shape}, got {t.dtype} {tuple(t.shape)}")
+    st, width = t.stride(), shape[-1] * shape[-2]
+    if t.numel() == 0:
+        return width
+    ok = st[-1] == 1 and (shape[-2] == 1 or st[-2] == shape[-1])
+    ld, rows = None, 1                      # stride of the innermost row axis longer than 1; rows inside the axis at hand
+    for n, s in zip(reversed(shape[:-2]), reversed(st[:-2])):
+        if n > 1:
+            if ld is None:
+                ld = s
+            ok = ok and s == ld * rows
+            rows *= n
+    ld = width if ld is None else ld
+    if not ok or ld < width:
+        raise ValueError(f"{name}: rows of {width} elements must be dense and evenly spaced, got strides {tuple(st)} for shape "
+                         f"{shape}")
+    return ld
+
+
+def _on_device(tensors) -> None:
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (here is None or not t.is_cuda or t.device.index != here):
+            raise ValueError(f"every tensor must be on the current HIP device, got one on {t.device}")
+
+
+class PagedCache:
+    """Keys and values of N growing sequences in pages of a shared pool (fe_cache_append).
+
+    k_pages, v_pages [n_pages][page_rows][n_kv_heads][dh] and table [N][cols] int32 are the caller's:
+    table[s][c] names the page that holds rows c * page_rows .. of sequence s.  len [N] int32 counts the rows
+    of every sequence and is advanced by `append`."""
+
+    def __init__(self, k_pages, v_pages, table, length=None):
+        import torch
+        if k_pages.dim() != 4:
+            raise ValueError(f"k_pages: expected [pages][rows][heads][dh], got {tuple(k_pages.shape)}")
+        if k_pages.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"k_pages: bfloat16 or float32, got {k_pages.dtype}")
+        shape = tuple(k_pages.shape)
+        self.page_ld = _row_stride(k_pages, "k_pages", shape, k_pages.dtype)
+        if _row_stride(v_pages, "v_pages", shape, k_pages.dtype) != self.page_ld:
+            raise ValueError("k_pages and v_pages must have the same row stride")
+        if table.dim() != 2:
+            raise ValueError(f"table: expected [sequences][columns], got {tuple(table.shape)}")
+        self.N, self.cols = table.shape
+        _need(table, "table", torch.int32, self.N * self.cols)
+        self.len = torch.zeros(self.N, dtype=torch.int32, device=table.device) if length is None else length
+        _need(self.len, "length", torch.int32, self.N)
+        self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
+        self.status = torch.zeros(self.N, dtype=torch.int32, device=table.device)
+        _on_device((k_pages, v_pages, table, self.len))
+
+    def append(self, k, v, q=None, q_out=None, new_len=None, pos0=None, freq=None, neighbours=False, len_out=None,
+               stream=None):
+        """Append rows k, v [N][S][n_kv_heads][dh] (the first new_len[s] of sequence s); with `freq` (float64 [rot / 2])
+        keys and q [N][S][n_heads][dh] are turned by their positions pos0[s] + row.  q_out defaults to a new
+        tensor; it is returned.  The lengths advance in place, or into len_out when that is given.
+        `status` [N] holds FE_DEV_BAD_PAGE for a sequence with a row that found no page."""
+        import torch
+        pages, P, hkv, dh = self.k_pages.shape
+        dt = self.k_pages.dtype
+        if k.dim() != 4:
+            raise ValueError(f"k: expected [sequences][rows][heads][dh], got {tuple(k.shape)}")
+        S = k.shape[1]
+        a = fe_append_args()
+        a.dtype, a.N, a.S = FE_BF16 if dt == torch.bfloat16 else FE_F32, self.N, S
+        a.n_kv_heads, a.dh, a.page_rows, a.n_pages, a.table_cols, a.page_ld = hkv, dh, P, pages, self.cols, self.page_ld
+        a.k_ld = _row_stride(k, "k", (self.N, S, hkv, dh), dt)
+        a.v_ld = _row_stride(v, "v", (self.N, S, hkv, dh), dt)
+        if q is not None:
+            if q.dim() != 4:
+                raise ValueError(f"q: expected [sequences][rows][heads][dh], got {tuple(q.shape)}")
+            a.n_heads = q.shape[2]
+            a.q_ld = _row_stride(q, "q", (self.N, S, a.n_heads, dh), dt)
+            if q_out is None:
+                q_out = torch.empty((self.N, S, a.n_heads, dh), dtype=dt, device=q.device)
+            a.q_out_ld = _row_stride(q_out, "q_out", (self.N, S, a.n_heads, dh), dt)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if freq is not None:
+            a.rot, a.neighbours = 2 * freq.numel(), 1 if neighbours else 0
+            _need(freq, "freq", torch.float64, freq.numel())
+        length = self.len if len_out is None else len_out
+        for t, name in ((length, "len_out"), (new_len, "new_len"), (pos0, "pos0")):
+            _need(t, name, torch.int32, self.N)
+        _on_device((k, v, q, q_out, freq, length, new_len, pos0))
+        a.q, a.k, a.v, a.q_out, a.freq, a.table = _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(freq), _ptr(self.table)
+        a.len, a.new_len, a.pos0, a.len_out = _ptr(self.len), _ptr(new_len), _ptr(pos0), _ptr(length)
+        a.k_pages, a.v_pages, a.status = _ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.status)
+        fe_cache_append(a, stream)
+        return q_out
+
+
+class PrefixAttention:
+    """Attention of K lists per request over the request's shared rows and each list's own rows
+    (fe_prefix_attention), with its outputs and workspace for one batch shape; `train=True` also keeps lse and allows `grad`.
+
+    `run` takes q [B][K][S][n_heads][dh], ctx_k and ctx_v [B][T][n_kv_heads][dh] (a layer's slice of
+    fe_encode_context's cache, viewed with its heads, is one), and own_k and own_v [B][K][L][n_kv_heads][dh], or
+    with page_rows > 0 the pages of a PagedCache [n_pages][page_rows][n_kv_heads][dh] and `table`
+    [B][K][L / page_rows] int32.  ctx_len [B], q_len [B][K] and own_len [B][K] int32 give the rows in use.  The outputs
+    belong to this object and are overwritten by its next call, as is its workspace: one object per stream."""
+
+    def __init__(self, B: int, K: int, S: int, T: int, L: int, n_heads: int, n_kv_heads: int, dh: int, dtype: str,
+                 causal: bool = False, scale: Optional[float] = None, page_rows: int = 0, n_pages: int = 0,
+                 train: bool = False):
+        self.act, self.train = _act(dtype), train
+        a = self.args = fe_prefix_args()
+        a.dtype = FE_BF16 if dtype == "bf16" else FE_F32
+        a.B, a.K, a.S, a.T, a.L, a.n_heads, a.n_kv_heads, a.dh = B, K, S, T, L, n_heads, n_kv_heads, dh
+        a.page_rows, a.n_pages, a.causal = page_rows, n_pages, 1 if causal else 0
+        a.scale = dh ** -0.5 if scale is None else scale
+        self.ws_bytes = fe_prefix_workspace_size(a)
+        if train:
+            self.ws_bytes = max(self.ws_bytes, fe_prefix_workspace_size(a, True))
+        self.out = None
+        self.grads = None
+
+    def allocate(self):
+        """Outputs and workspace on the current device (done by the first `run`)."""
+        import torch
+        a, dev = self.args, torch.device("cuda", torch.cuda.current_device())
+        self.out = torch.empty((a.B, a.K, a.S, a.n_heads, a.dh), dtype=self.act, device=dev)
+        self.lse = torch.empty((a.B, a.K, a.S, a.n_heads), dtype=torch.float32, device=dev) if self.train else None
+        self.ws = torch.empty(max(16, self.ws_bytes), dtype=torch.uint8, device=dev)
+        a.out, a.lse, a.ws, a.ws_bytes = _ptr(self.out), _ptr(self.lse), _ptr(self.ws), self.ws_bytes
+        a.out_ld = a.n_heads * a.dh
+        if self.train:
+            self.grads = (torch.empty_like(self.out),
+                          *(torch.empty((a.B, a.T, a.n_kv_heads, a.dh), dtype=self.act, device=dev) for _ in range(2)),
+                          *(torch.empty((a.B, a.K, a.L, a.n_kv_heads, a.dh), dtype=self.act, device=dev) for _ in range(2)))
+
+    def _take(self, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len):
+        import torch
+        a = self.args
+        ctx = (a.B, a.T, a.n_kv_heads, a.dh)
+        own = (a.n_pages, a.page_rows) if a.page_rows else (a.B, a.K, a.L)
+        own += (a.n_kv_heads, a.dh)
+        a.q_ld = _row_stride(q, "q", (a.B, a.K, a.S, a.n_heads, a.dh), self.act)
+        if a.T:
+            a.ctx_ld = _row_stride(ctx_k, "ctx_k", ctx, self.act)
+            if _row_stride(ctx_v, "ctx_v", ctx, self.act) != a.ctx_ld:
+                raise ValueError("ctx_k and ctx_v must have the same row stride")
+        if a.L:
+            a.own_ld = _row_stride(own_k, "own_k", own, self.act)
+            if _row_stride(own_v, "own_v", own, self.act) != a.own_ld:
+                raise ValueError("own_k and own_v must have the same row stride")
+        if a.page_rows:
+            if table is None:
+                raise ValueError("paged own rows need a table")
+            _need(table, "table", torch.int32, a.B * a.K * (a.L // a.page_rows))
+        elif table is not None:
+            raise ValueError("a table needs page_rows > 0")
+        _need(ctx_len, "ctx_len", torch.int32, a.B)
+        _need(q_len, "q_len", torch.int32, a.B * a.K)
+        _need(own_len, "own_len", torch.int32, a.B * a.K)
+        _on_device((q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len, self.out))
+        if self.out is None:
+            self.allocate()
+        a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = _ptr(q), _ptr(ctx_k), _ptr(ctx_v), _ptr(own_k), _ptr(own_v)
+        a.table, a.ctx_len, a.own_len, a.q_len = _ptr(table), _ptr(ctx_len), _ptr(own_len), _ptr(q_len)
+
+    def run(self, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
+        """Enqueue the attention; returns out [B][K][S][n_heads][dh] (self.lse holds the log sums when training)."""
+        self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        fe_prefix_attention(self.args, stream)
+        return self.out
+
+    def grad(self, dout, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
+        """Gradients (dq, dctx_k, dctx_v, down_k, down_v) of the last `run`, which must have had the same tensors."""
+        if not self.train:
+            raise ValueError("grad needs train=True")
+        if self.out is None:
+            raise ValueError("grad follows run")
+        self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        a, g = self.args, fe_prefix_grads()
+        g.dout_ld = _row_stride(dout, "dout", (a.B, a.K, a.S, a.n_heads, a.dh), self.act)
+        _on_device((dout,))
+        g.dout = _ptr(dout)
+        g.dq_ld, g.dctx_ld, g.down_ld = a.n_heads * a.dh, a.n_kv_heads * a.dh, a.n_kv_heads * a.dh
+        g.dq, g.dctx_k, g.dctx_v, g.down_k, g.down_v = (_ptr(t) for t in self.grads)
+        fe_prefix_attention_grad(a, g, stream)
+        return self.grads
