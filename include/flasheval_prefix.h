@@ -128,6 +128,7 @@ typedef struct {
   const int32_t* own_len;               /* [B][K], or NULL: L */
   void* out;                            /* [B][K][S] rows of n_heads * dh */
   float* lse;                           /* [B][K][S][n_heads], or NULL (the gradient needs it) */
+  void* out_rest;                       /* FE_BF16: [B][K][S][n_heads * dh] what the rounding of out left, or NULL */
   void* ws;
   size_t ws_bytes;
 } fe_prefix_args;
@@ -136,7 +137,7 @@ fe_status fe_prefix_attention(const fe_prefix_args* a, void* stream);
 
 /*
  * Gradients of fe_prefix_attention for d loss / d out = dout.  `a` holds the forward's arguments with
- * its out and lse and a workspace of fe_prefix_workspace_size(a, 1) bytes; own rows must be dense
+ * its out and lse (and out_rest: without it FE_BF16 takes D from the rounded out) and a workspace of fe_prefix_workspace_size(a, 1) bytes; own rows must be dense
  * (FE_EUNSUPPORTED otherwise).  With D = dout.out, dp = dout.v and ds = p (dp - D):
  *   dq = scale sum ds k,   dk = scale sum ds q,   dv = sum p dout,
  * where a key's sums run over every list (shared rows), row and head that reads it.  Every row of dq, of the shared

@@ -60,7 +60,7 @@ fe_status check_forward(const fe_prefix_args* a) {
   if (a->L > 0 && (!a->own_k || !a->own_v)) return pfail(FE_EINVAL, "own_k or own_v is NULL");
   if (a->L > 0 && a->page_rows > 0 && !a->table) return pfail(FE_EINVAL, "page table is NULL");
   if (!aligned(a->q, 16) || !aligned(a->out, 16) || !aligned(a->ctx_k, 16) || !aligned(a->ctx_v, 16) ||
-      !aligned(a->own_k, 16) || !aligned(a->own_v, 16) || !aligned(a->ws, 16))
+      !aligned(a->own_k, 16) || !aligned(a->own_v, 16) || !aligned(a->out_rest, 16) || !aligned(a->ws, 16))
     return pfail(FE_EINVAL, "pointers must be 16-byte aligned");
   if (!aligned(a->table, 4) || !aligned(a->ctx_len, 4) || !aligned(a->q_len, 4) || !aligned(a->own_len, 4) || !aligned(a->lse, 4))
     return pfail(FE_EINVAL, "tables, lengths and lse must be 4-byte aligned");
@@ -70,14 +70,15 @@ fe_status check_forward(const fe_prefix_args* a) {
   return FE_OK;
 }
 
-size_t delta_bytes(const fe_prefix_args& a) { return ((size_t)a.B * a.K * a.S * a.n_heads * sizeof(float) + 255) & ~size_t(255); }
+size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+size_t grad_bytes(const PrefixGradPlan& p) { return up256(p.rows_bytes) + up256(p.dq_bytes) + up256(p.dkv_bytes); }
 
 PrefixArgs kernel_args(const fe_prefix_args& a) {
   PrefixArgs k{};
   k.q = a.q; k.ctx_k = a.ctx_k; k.ctx_v = a.ctx_v; k.own_k = a.own_k; k.own_v = a.own_v;
   k.table = a.table; k.ctx_len = a.ctx_len; k.q_len = a.q_len; k.own_len = a.own_len;
-  k.out = a.out; k.lse = a.lse;
-  k.B = a.B; k.K = a.K; k.S = a.S; k.Hq = a.n_heads; k.Hkv = a.n_kv_heads; k.T = a.T; k.L = a.L;
+  k.out = a.out; k.lse = a.lse; k.out_rest = a.dtype == FE_BF16 ? a.out_rest : nullptr;
+  k.B = a.B; k.K = a.K; k.S = a.S; k.Hq = a.n_heads; k.Hkv = a.n_kv_heads; k.dh = a.dh; k.T = a.T; k.L = a.L;
   k.page_rows = a.page_rows; k.n_pages = a.n_pages; k.causal = a.causal != 0;
   k.q_ld = a.q_ld; k.ctx_ld = a.ctx_ld; k.own_ld = a.own_ld; k.out_ld = a.out_ld;
   k.scale = a.scale;
@@ -96,7 +97,7 @@ fe_status fe_prefix_workspace_size(const fe_prefix_args* a, int grad, size_t* by
   if (st != FE_OK) return st;
   if (!bytes) return pfail(FE_EINVAL, "bytes is NULL");
   if (grad && a->page_rows > 0) return pfail(FE_EUNSUPPORTED, "the gradient takes dense own rows");
-  *bytes = grad ? delta_bytes(*a) : prefix_plan(*a).part_bytes;
+  *bytes = grad ? grad_bytes(prefix_grad_plan(*a)) : prefix_plan(*a).part_bytes;
   return FE_OK;
 }
 
@@ -130,15 +131,19 @@ fe_status fe_prefix_attention_grad(const fe_prefix_args* a, const fe_prefix_grad
   if (!stride_ok(g->dout_ld, wq, a->dtype) || !stride_ok(g->dq_ld, wq, a->dtype) ||
       (a->T > 0 && !stride_ok(g->dctx_ld, wk, a->dtype)) || (a->L > 0 && !stride_ok(g->down_ld, wk, a->dtype)))
     return pfail(FE_EINVAL, "a row stride is shorter than its row or not a multiple of 16 bytes");
-  const size_t need = delta_bytes(*a);
+  const PrefixGradPlan p = prefix_grad_plan(*a);
+  const size_t need = grad_bytes(p);
   if (!a->ws || a->ws_bytes < need) return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);
   PrefixGradArgs k{};
   k.f = kernel_args(*a);
   k.dout = g->dout; k.dout_ld = g->dout_ld;
   k.dq = g->dq; k.dctx_k = g->dctx_k; k.dctx_v = g->dctx_v; k.down_k = g->down_k; k.down_v = g->down_v;
   k.dq_ld = g->dq_ld; k.dctx_ld = g->dctx_ld; k.down_ld = g->down_ld;
-  k.delta = static_cast<float*>(a->ws);
-  const hipError_t e = launch_prefix_grad(k, a->dh, a->dtype == FE_BF16, static_cast<hipStream_t>(stream));
+  char* ws = static_cast<char*>(a->ws);
+  k.rows = reinterpret_cast<float4*>(ws);
+  k.f.part_o = reinterpret_cast<float*>(ws + up256(p.rows_bytes));
+  k.part_kv = reinterpret_cast<float*>(ws + up256(p.rows_bytes) + up256(p.dq_bytes));
+  const hipError_t e = launch_prefix_grad(k, a->dh, a->dtype == FE_BF16, p, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? FE_OK : pfail(FE_EHIP, "shared-prefix gradient launch failed: %s", hipGetErrorString(e));
 }
 

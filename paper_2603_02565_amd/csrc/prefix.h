@@ -12,7 +12,8 @@ struct PrefixArgs {
   const void *q, *ctx_k, *ctx_v, *own_k, *own_v;
   const int32_t *table, *ctx_len, *q_len, *own_len;
   void* out; float* lse;
-  int B, K, S, Hq, Hkv, T, L, page_rows, n_pages, causal;
+  void* out_rest;                       // bf16: what rounding left of out, dense rows (or nullptr)
+  int B, K, S, Hq, Hkv, dh, T, L, page_rows, n_pages, causal;
   int q_ld, ctx_ld, own_ld, out_ld;
   float scale;
   int G, R;
@@ -26,13 +27,17 @@ struct PrefixGradArgs {
   const void* dout; int dout_ld;
   void *dq, *dctx_k, *dctx_v, *down_k, *down_v;
   int dq_ld, dctx_ld, down_ld;
-  float* delta;                         // [B*K*S*Hq] dout . out
+  float4* rows;                         // [B][Hkv][R]: what the products need of every row
   int ctx_tiles, own_tiles;             // key tiles of the shared rows / of the own rows per (request, key head)
+  int row_splits; float* part_kv;       // row ranges per key tile; their partial sums [row_splits][keys][2][dh]
 };
 
 // Row tiles, key ranges and partial-sum bytes of a forward call: functions of the sizes alone.
 struct PrefixPlan { int rows, tiles, splits; size_t part_bytes; };
 PrefixPlan prefix_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixPlan& p, hipStream_t s);
-hipError_t launch_prefix_grad(PrefixGradArgs a, int dh, bool bf16_rows, hipStream_t s);
+// The same of a gradient call: dq's row tiles and key ranges, dk's and dv's key tiles and row ranges, scratch bytes.
+struct PrefixGradPlan { int rows, tiles, splits, ctx_tiles, own_tiles, row_splits; size_t rows_bytes, dq_bytes, dkv_bytes; };
+PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a);
+hipError_t launch_prefix_grad(const PrefixGradArgs& a, int dh, bool bf16_rows, const PrefixGradPlan& p, hipStream_t s);
 hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s);

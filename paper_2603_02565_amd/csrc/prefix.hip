@@ -32,6 +32,13 @@ FE_DEV f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
 
 template <typename T> FE_DEV V8<T> ld8(const T* p) { return *reinterpret_cast<const V8<T>*>(p); }
 template <typename T> FE_DEV void st8(T* p, V8<T> v) { *reinterpret_cast<V8<T>*>(p) = v; }
+FE_DEV void st4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+FE_DEV void st4(bf16* p, f32x4 v) {
+  bf16x4 w;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) w[q] = (bf16)v[q];
+  *reinterpret_cast<bf16x4*>(p) = w;
+}
 // LDS row padding: 16 bytes
 template <typename T> constexpr int kPad = 16 / sizeof(T);
 
@@ -61,6 +68,31 @@ FE_DEV int wave_max(int v) { return -wave_min(-v); }
 FE_DEV int q_rows(const PrefixArgs& a, int bk) { return a.q_len ? clampi(a.q_len[bk], 0, a.S) : a.S; }
 FE_DEV int own_rows(const PrefixArgs& a, int bk) { return a.own_len ? clampi(a.own_len[bk], 0, a.L) : a.L; }
 FE_DEV int ctx_rows(const PrefixArgs& a, int b) { return a.ctx_len ? clampi(a.ctx_len[b], 0, a.T) : a.T; }
+
+// Key of a 32-key step that element j of a lane in group g4 stands for.
+FE_DEV int key_of(int j, int g4) { return 16 * (j >> 2) + 4 * g4 + (j & 3); }
+
+// log2(e) |scale|, the exponent's factor of a score; positive, so that masked scores stay -infinity when scale is 0.
+FE_DEV float score_unit(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-37f); }
+
+// Four consecutive elements of an output row, and what their rounding left (bf16, when asked for).
+template <typename T>
+FE_DEV void store_out(const PrefixArgs& a, long long at, int col, f32x4 v);
+template <>
+FE_DEV void store_out<bf16>(const PrefixArgs& a, long long at, int col, f32x4 v) {
+  bf16x4 w, r;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    w[q] = (bf16)v[q];
+    r[q] = (bf16)(v[q] - (float)w[q]);
+  }
+  *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.out) + at * a.out_ld + col) = w;
+  if (a.out_rest) *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.out_rest) + at * a.Hq * a.dh + col) = r;
+}
+template <>
+FE_DEV void store_out<float>(const PrefixArgs& a, long long at, int col, f32x4 v) {
+  *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at * a.out_ld + col) = v;
+}
 
 // The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
 // their number; a list without query rows contributes none.  NT threads, nb <= NT; ends with a barrier.
@@ -104,6 +136,13 @@ FE_DEV long long own_row(const PrefixArgs& a, int bk, int j) {
   return page >= 0 && page < a.n_pages ? (long long)page * a.page_rows + j % a.page_rows : -1;
 }
 
+// Row of own_k / own_v for row c of the lists packed in off, -1 for a page outside the pool, -2 past the last row.
+FE_DEV long long find_own(const PrefixArgs& a, int b, int k0, int nb, const int* off, int c) {
+  if (c >= off[nb]) return -2;
+  const int i = packed_list(off, nb, c);
+  return own_row(a, b * a.K + k0 + i, c - off[i]);
+}
+
 // What a lane has to know about its query row r of (request b, key head g).
 struct Row {
   int k, s, h;                          // list, row, query head
@@ -125,23 +164,52 @@ FE_DEV Row row_of(const PrefixArgs& a, int b, int g, int r) {
   return w;
 }
 
+// Operand of a product whose summed axis runs over LDS rows base .. base + 31 and whose other axis is column col + l % 16
+// (what a transposed copy would give, without one).  Element 4 x + j of lane l is row base + 16 x + 4 (l / 16) + j, the
+// order in which a lane holds the results of two 16-row products.  bf16: each group of 16 lanes reads a 4 x 16 block
+// transposed (ds_read_b64_tr_b16); row strides of 8 words modulo 16 keep the half-waves free of bank conflicts.
+template <int LD>
+FE_DEV bf16x8 ld_cols(const bf16* X, int base, int col, int lane) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+  bf16* p = const_cast<bf16*>(X) + (base + 4 * (lane >> 4) + ((lane & 15) >> 2)) * LD + col + (lane & 3) * 4;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 16 * LD));
+  const bf16x4 u = __builtin_bit_cast(bf16x4, a), v = __builtin_bit_cast(bf16x4, b);
+  return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <int LD>
+FE_DEV f32x8 ld_cols(const float* X, int base, int col, int lane) {
+  const float* p = X + (base + 4 * (lane >> 4)) * LD + col + (lane & 15);
+  f32x8 v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = p[(16 * (j >> 2) + (j & 3)) * LD];
+  return v;
+}
+
+// Waves per SIMD that the register file is shared between (more hide more latency; these leave no spills).
+constexpr int fwd_waves(int bytes, int w) { return bytes == 2 && w <= 64 ? 4 : w <= 64 || (bytes == 2 && w <= 128) ? 3 : 2; }
+
 // ------------------------------------------------------------------------------------------
 // Forward.  NW waves of QT 16-row tiles; chunks of KC keys staged through registers (the next chunk's loads in
-// flight behind this one's products) into LDS, K by rows and V transposed.  Scores are formed transposed
-// (keys x rows): a lane then holds keys 8 g + j of one row, which is the operand layout of the product with
-// the values, so probabilities never leave the registers.
+// flight behind this one's products) into LDS.  Scores are formed transposed (keys x rows): a lane then holds
+// eight keys of one row, which is the operand layout of the product with the values, so probabilities never leave the
+// registers.
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int QT, int NW, int KC>
-__global__ __launch_bounds__(NW * 64) void k_prefix_fwd(PrefixArgs a) {
+__global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_prefix_fwd(PrefixArgs a) {
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
-  constexpr int KLD = DH + kPad<T>, VLD = KC + kPad<T>;
+  constexpr int KLD = DH + kPad<T>, VLD = DH + 2 * kPad<T>;
   constexpr int PER_T = KC * DH / 8 / NT;
-  static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Ks[KC * KLD];
-  __shared__ __attribute__((aligned(16))) T Vt[DH * VLD];
+  constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
+  static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0 && KC <= NT, "tile shape");
+  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * KLD];
+  __shared__ __attribute__((aligned(16))) T Vs_[NBUF][KC * VLD];
   __shared__ int s_off[ROWS + 1];
-  __shared__ int s_odd;                            // last chunk whose values are not all finite
-  __shared__ int s_holes, s_hole[KC];              // last chunk with keys of pages outside the pool, and those keys
+  // per buffer: the last chunk whose values are not all finite, the last chunk with keys of pages outside the
+  // pool, and those keys
+  __shared__ int s_odd[2], s_holes[2], s_hole[2][KC];
+  __shared__ long long s_at[2][KC];                // rows of the next own chunks
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
@@ -153,19 +221,56 @@ __global__ __launch_bounds__(NW * 64) void k_prefix_fwd(PrefixArgs a) {
   const int g = id % a.Hkv, b = id / a.Hkv;
   const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R), sg = a.S * a.G;
   const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
-  if (tid == 0) s_odd = s_holes = -1;
-  if (tid < KC) s_hole[tid] = -1;
+  if (tid < 2) s_odd[tid] = s_holes[tid] = -1;
+  if (tid < KC) s_hole[0][tid] = s_hole[1][tid] = -1;
   pack_own<NT>(a, b, k0, nb, s_off);
 
-  const int nctx = ctx_rows(a, b), nown = s_off[nb];
+  const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_off[nb]);
   const int cctx = (nctx + KC - 1) / KC, chunks = cctx + (nown + KC - 1) / KC;
   const int cb = (int)((long long)chunks * z / a.splits), ce = (int)((long long)chunks * (z + 1) / a.splits);
+
+  V8<T> kreg[PER_T], vreg[PER_T];
+  int gone = 0, hole = 0;                          // bit p: key of kreg[p] past the rows or without a page; without a page
+  // The loads are unconditional (rows that do not count read one that exists); `gone` says what to leave out.
+  auto load_chunk = [&](int c) __attribute__((always_inline)) {
+    const bool shared = c < cctx;                  // uniform
+    const int left = shared ? nctx - c * KC : KC, ld = shared ? a.ctx_ld : a.own_ld;
+    const long long base = (long long)b * a.T + c * KC;
+    const T *kb = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + g * DH;
+    const T *vb = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + g * DH;
+    gone = hole = 0;
+#pragma unroll
+    for (int p = 0; p < PER_T; ++p) {
+      const int e = p * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
+      long long x = base + min(key, left - 1);
+      if (!shared) {
+        x = s_at[c & 1][key];
+        gone |= (x < 0) << p;
+        hole |= (x == -1) << p;
+        x = max(x, 0LL);
+      } else {
+        gone |= (key >= left) << p;
+      }
+      kreg[p] = ld8(kb + x * ld + d0);
+      vreg[p] = ld8(vb + x * ld + d0);
+    }
+  };
+  // own rows are found one chunk before they are loaded, so that a page table's latency is hidden as well
+  long long found = -2;
+  auto find = [&](int c) __attribute__((always_inline)) {
+    if (c >= cctx && c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+  };
+  find(cb);
+  if (tid < KC) s_at[cb & 1][tid] = found;
+  __syncthreads();
+  if (cb < ce) load_chunk(cb);
+  find(cb + 1);
 
   Row row[QT];
   V8<T> qf[QT][ND];
   int lo[QT], hi[QT];                              // the packed own rows that the row sees
   int wlo[QT], whi[QT], alo[QT], ahi[QT];          // their union and intersection over the wave's tile
-  float m_run[QT], l_run[QT];                      // l_run: this lane's keys only, until the end
+  float m_run[QT], l_run[QT];                      // maximum of q.k; l_run: this lane's keys only, until the end
   f32x4 o[QT][NB];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
@@ -178,139 +283,154 @@ __global__ __launch_bounds__(NW * 64) void k_prefix_fwd(PrefixArgs a) {
     ahi[i] = wave_min(hi[i]);
     const T* Q = static_cast<const T*>(a.q) + row[i].at * a.q_ld + row[i].h * DH;
 #pragma unroll
-    for (int c = 0; c < ND; ++c) qf[i][c] = row[i].live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
+    for (int c = 0; c < ND; ++c) {
+      qf[i][c] = row[i].live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
+      if (a.scale < 0) qf[i][c] = -qf[i][c];       // exact; the largest score is then the largest product
+    }
     m_run[i] = -INFINITY;
     l_run[i] = 0.f;
 #pragma unroll
     for (int n = 0; n < NB; ++n) o[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float sl2 = a.scale * kLog2e;
+  const float sl2 = score_unit(a.scale);
 
-  V8<T> kreg[PER_T], vreg[PER_T];
-  int hole = 0;                                    // bit p: kreg[p] belongs to a page outside the pool
-  auto load_chunk = [&](int c) {
-    hole = 0;
+  // Scores and probabilities of tile i for the 32 keys x0 .. of a step (keys [l, h) of each row; `edge`: some are outside),
+  // with the running maximum and sum.  pb is the operand of the product with the values.
+  auto scores = [&](int i, const V8<T> (&kf)[2][ND], float (&s)[8]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < PER_T; ++p) {
-      const int e = p * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      const T *kp = nullptr, *vp = nullptr;
-      if (c < cctx) {
-        const int x = c * KC + key;
-        if (x < nctx) {
-          const long long at = ((long long)b * a.T + x) * a.ctx_ld + g * DH + d0;
-          kp = static_cast<const T*>(a.ctx_k) + at;
-          vp = static_cast<const T*>(a.ctx_v) + at;
-        }
-      } else {
-        const int x = (c - cctx) * KC + key;
-        if (x < nown) {
-          const int i = packed_list(s_off, nb, x);
-          const long long at = own_row(a, b * a.K + k0 + i, x - s_off[i]);
-          if (at >= 0) {
-            kp = static_cast<const T*>(a.own_k) + at * a.own_ld + g * DH + d0;
-            vp = static_cast<const T*>(a.own_v) + at * a.own_ld + g * DH + d0;
-          } else {
-            hole |= 1 << p;
-          }
-        }
-      }
-      kreg[p] = kp ? ld8(kp) : V8<T>{};
-      vreg[p] = vp ? ld8(vp) : V8<T>{};
+    for (int x = 0; x < 2; ++x) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc = mma(kf[x][d], qf[i][d], acc);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * x + j] = acc[j];
     }
   };
-  if (cb < ce) load_chunk(cb);
+  auto softmax = [&](int i, float (&s)[8], V8<T>& pb) __attribute__((always_inline)) {
+    float mx = s[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[j]);
+    if (__any(mx > m_run[i])) {                    // else every row's factor is 1
+      const float m_new = fmaxf(m_run[i], rows_max(mx));
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[i] - m_new) * sl2);
+      m_run[i] = m_new;
+      l_run[i] *= alpha;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) o[i][n] *= alpha;
+    }
+    const float ref = m_run[i] == -INFINITY ? 0.f : m_run[i] * sl2;   // a row without keys so far: exp2(-inf) = 0
+    float psum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -ref));
+      psum += e;
+      pb[j] = from_f32<T>(e);
+    }
+    l_run[i] += psum;
+  };
+  auto load_keys = [&](const T* Ks, int kb, V8<T> (&kf)[2][ND]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 0; d < ND; ++d) kf[x][d] = ld8(&Ks[(kb + 16 * x + c16) * KLD + d * 32 + g4 * 8]);
+  };
 
-  for (int c = cb; c < ce; ++c) {
-    __syncthreads();                               // the previous chunk is no longer read
+  const int tiles_here = clampi((a.R - r0 - wave * QT * 16 + 15) / 16, 0, QT);   // the wave's tiles that hold rows
+  int cur = 0;
+  for (int c = cb; c < ce; ++c, cur ^= NBUF - 1) {
+    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    if constexpr (NBUF == 1) lds_barrier();        // the previous chunk is no longer read
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
       const int e = p * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
+      if ((c >= cctx || (c + 1) * KC > nctx) && gone >> p & 1) kreg[p] = vreg[p] = V8<T>{};
       st8(&Ks[key * KLD + d0], kreg[p]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) Vt[(d0 + i) * VLD + key] = vreg[p][i];
-      if (c >= cctx && !finite8(vreg[p])) s_odd = c;
-      if (hole >> p & 1) s_hole[key] = s_holes = c;
+      st8(&Vs[key * VLD + d0], vreg[p]);
+      if (c >= cctx) {                             // uniform
+        if (!finite8(vreg[p])) s_odd[c & 1] = c;
+        if (hole >> p & 1) s_hole[c & 1][key] = s_holes[c & 1] = c;
+      }
     }
-    __syncthreads();
+    if (c + 1 >= cctx && tid < KC) s_at[(c + 1) & 1][tid] = found;
+    lds_barrier();   // two buffers: also the end of every wave's reads of the one written next
     if (c + 1 < ce) load_chunk(c + 1);
-    const bool shared = c < cctx;
-    const int base = shared ? c * KC : (c - cctx) * KC, top = shared ? nctx : nown;
-    const bool odd = !shared && s_odd == c;
+    find(c + 2);
+    if (tiles_here == 0) continue;
 
+    if (c < cctx) {
 #pragma unroll
+      for (int kb = 0; kb < KC; kb += 32) {
+        const int left = nctx - c * KC - kb;       // keys of the step
+        if (left <= 0) break;                      // uniform
+        V8<T> kf[2][ND], pb[QT];
+        load_keys(Ks, kb, kf);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          float s[8];
+          scores(i, kf, s);
+          if (left < 32) {                         // uniform
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (key_of(j, g4) >= left) s[j] = -INFINITY;
+          }
+          softmax(i, s, pb[i]);
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const V8<T> vf = ld_cols<VLD>(Vs, kb, n * 16, lane);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[i], o[i][n]);
+        }
+      }
+      continue;
+    }
+
+    const bool odd = __builtin_amdgcn_readfirstlane(s_odd[c & 1]) == c;
+    const bool holes = __builtin_amdgcn_readfirstlane(s_holes[c & 1]) == c;
+#pragma unroll 1
     for (int kb = 0; kb < KC; kb += 32) {
-      const int x0 = base + kb;
-      if (x0 >= top) break;                        // uniform
-      V8<T> kf[2][ND], vf[NB];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-          kf[x][d] = ld8(&Ks[(kb + (c16 >> 2) * 8 + (c16 & 3) + 4 * x) * KLD + d * 32 + g4 * 8]);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) vf[n] = ld8(&Vt[(n * 16 + c16) * VLD + kb + g4 * 8]);
+      const int x0 = (c - cctx) * KC + kb;
+      if (x0 >= nown) break;                       // uniform
+      V8<T> kf[2][ND];
+      load_keys(Ks, kb, kf);
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
-        if (!shared && (x0 >= whi[i] || x0 + 32 <= wlo[i])) continue;   // uniform: no row of the tile sees a key of the step
+        if (x0 >= whi[i] || x0 + 32 <= wlo[i]) continue;   // uniform: no row of the tile sees a key of the step
         float s[8];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int d = 0; d < ND; ++d) acc = mma(kf[x][d], qf[i][d], acc);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[4 * x + j] = acc[j] * sl2;
-        }
-        if (shared ? x0 + 32 > nctx : (x0 < alo[i] || x0 + 32 > ahi[i])) {   // uniform
-          const int l = shared ? 0 : lo[i], h = shared ? nctx : hi[i];
+        scores(i, kf, s);
+        if (x0 < alo[i] || x0 + 32 > ahi[i]) {     // uniform
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int x = x0 + g4 * 8 + j;
-            if (x < l || x >= h) s[j] = -INFINITY;
+            const int x = x0 + key_of(j, g4);
+            if (x < lo[i] || x >= hi[i]) s[j] = -INFINITY;
           }
         }
-        if (s_holes == c) {                        // uniform
+        if (holes) {                               // uniform
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (s_hole[kb + g4 * 8 + j] == c) s[j] = -INFINITY;
+            if (s_hole[c & 1][kb + key_of(j, g4)] == c) s[j] = -INFINITY;
         }
-        float mx = s[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[j]);
-        const float m_new = fmaxf(m_run[i], rows_max(mx));
-        const float ref = m_new == -INFINITY ? 0.f : m_new;       // a row without keys so far: every factor below is 0
-        const float alpha = __builtin_amdgcn_exp2f(m_run[i] - ref);
-        m_run[i] = m_new;
-        float psum = 0.f;
         V8<T> pb;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float e = __builtin_amdgcn_exp2f(s[j] - ref);
-          psum += e;
-          pb[j] = from_f32<T>(e);
-        }
-        l_run[i] = fmaf(l_run[i], alpha, psum);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[i][n] *= alpha;
+        softmax(i, s, pb);
         if (!odd) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) o[i][n] = mma(vf[n], pb, o[i][n]);
-        } else {
-          // A value of the chunk is not finite: in a product it would reach the rows that do not see its key, as 0
-          // times infinity.  The same sums key by key, over the keys that the row sees.
+          for (int n = 0; n < NB; ++n) o[i][n] = mma(ld_cols<VLD>(Vs, kb, n * 16, lane), pb, o[i][n]);
+          continue;
+        }
+        // A value of the chunk is not finite: in a product it would reach the rows that do not see its key, as 0
+        // times infinity.  The same sums key by key, over the keys that the row sees.
 #pragma unroll 1
-          for (int gg = 0; gg < 4; ++gg)
+        for (int key = 0; key < 32; ++key) {
+          float e = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float e = __shfl(to_f32((T)pb[j]), gg * 16 + c16);
-              const int x = x0 + gg * 8 + j;
-              if (x < lo[i] || x >= hi[i]) continue;
+          for (int j = 0; j < 8; ++j) e = key_of(j, key >> 2 & 3) == key ? to_f32((T)pb[j]) : e;
+          e = __shfl(e, (key >> 2 & 3) * 16 + c16);
+          if (x0 + key < lo[i] || x0 + key >= hi[i]) continue;
 #pragma unroll
-              for (int n = 0; n < NB; ++n)
+          for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                  o[i][n][q] = fmaf(e, to_f32(Vt[(n * 16 + g4 * 4 + q) * VLD + kb + gg * 8 + j]), o[i][n][q]);
-            }
+            for (int q = 0; q < 4; ++q)
+              o[i][n][q] = fmaf(e, to_f32(Vs[(kb + key) * VLD + n * 16 + g4 * 4 + q]), o[i][n][q]);
         }
       }
     }
@@ -320,6 +440,7 @@ __global__ __launch_bounds__(NW * 64) void k_prefix_fwd(PrefixArgs a) {
   for (int i = 0; i < QT; ++i) {
     const float l = rows_sum(l_run[i]);
     if (r0 + (wave * QT + i) * 16 + c16 >= a.R) continue;
+    const float m2 = m_run[i] * sl2;
     const long long ro = row[i].at * a.Hq + row[i].h;
     if (a.splits > 1) {
       const long long rows = (long long)a.B * a.K * a.S * a.Hq;
@@ -327,19 +448,21 @@ __global__ __launch_bounds__(NW * 64) void k_prefix_fwd(PrefixArgs a) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(po + n * 16 + g4 * 4) = o[i][n];
       if (g4 == 0) {
-        a.part_ml[(z * rows + ro) * 2] = m_run[i];
+        a.part_ml[(z * rows + ro) * 2] = m2;
         a.part_ml[(z * rows + ro) * 2 + 1] = l;
       }
       continue;
     }
     const bool none = !row[i].live || m_run[i] == -INFINITY;
     const float inv = none ? 0.f : 1.f / l;
-    T* O = static_cast<T*>(a.out) + row[i].at * a.out_ld + row[i].h * DH;
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
+    for (int n = 0; n < NB; ++n) {
+      f32x4 v;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) O[n * 16 + g4 * 4 + q] = from_f32<T>(none ? 0.f : o[i][n][q] * inv);
-    if (a.lse && g4 == 0) a.lse[ro] = none ? -INFINITY : (m_run[i] + log2f(l)) * kLn2;
+      for (int q = 0; q < 4; ++q) v[q] = none ? 0.f : o[i][n][q] * inv;
+      store_out<T>(a, row[i].at, row[i].h * DH + n * 16 + g4 * 4, v);
+    }
+    if (a.lse && g4 == 0) a.lse[ro] = none ? -INFINITY : (m2 + log2f(l)) * kLn2;
   }
 }
 
@@ -351,6 +474,7 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
   const int d0 = (int)(e % (DH / 4)) * 4;
   if (ro >= rows) return;
   float m = -INFINITY;
+#pragma unroll 8
   for (int z = 0; z < a.splits; ++z) m = fmaxf(m, a.part_ml[(z * rows + ro) * 2]);
   const long long at = ro / a.Hq;
   const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);
@@ -358,15 +482,16 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
   const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
   for (int z = 0; z < a.splits; ++z) {
     const float w = __builtin_amdgcn_exp2f(a.part_ml[(z * rows + ro) * 2] - ref);
     l = fmaf(a.part_ml[(z * rows + ro) * 2 + 1], w, l);
     o += w * *reinterpret_cast<const f32x4*>(a.part_o + (z * rows + ro) * DH + d0);
   }
   const float inv = none ? 0.f : 1.f / l;
-  T* O = static_cast<T*>(a.out) + at * a.out_ld + h * DH + d0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) O[q] = from_f32<T>(none ? 0.f : o[q] * inv);
+  for (int q = 0; q < 4; ++q) o[q] = none ? 0.f : o[q] * inv;
+  store_out<T>(a, at, h * DH + d0, o);
   if (a.lse && d0 == 0) a.lse[ro] = none ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
@@ -374,175 +499,231 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
 // Gradient.
 // ------------------------------------------------------------------------------------------
 
-// delta = dout . out per row and head: 16 lanes a row.
+// What the gradient's products need of every row, in the order of the rows of a (request, key head):
+//   x = log2(e) lse (+infinity for a row without keys or past q_len: its probabilities are then 0),
+//   y = dout . out,   z, w = the own rows that it sees, numbered k L + j  [z, w).
+// DH / 8 lanes a row.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_prefix_delta(PrefixGradArgs p) {
+__global__ __launch_bounds__(256) void k_prefix_rows(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
-  const long long rows = (long long)a.B * a.K * a.S * a.Hq;
-  const long long ro = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int x = threadIdx.x & 15;
-  if (ro >= rows) return;
-  const long long at = ro / a.Hq;
-  const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);
+  constexpr int W = DH / 8;
+  const long long e = (long long)blockIdx.x * (256 / W) + threadIdx.x / W;
+  const int d0 = threadIdx.x % W * 8;
+  if (e >= (long long)a.B * a.Hkv * a.R) return;
+  const int r = (int)(e % a.R), bg = (int)(e / a.R), b = bg / a.Hkv;
+  const Row w = row_of(a, b, bg % a.Hkv, r);
   float v = 0.f;
-  if (s < q_rows(a, bk)) {
-    const T* O = static_cast<const T*>(a.out) + at * a.out_ld + h * DH;
-    const T* D = static_cast<const T*>(p.dout) + at * p.dout_ld + h * DH;
+  if (w.live) {
+    const V8<T> o = ld8(static_cast<const T*>(a.out) + w.at * a.out_ld + w.h * DH + d0);
+    const V8<T> d = ld8(static_cast<const T*>(p.dout) + w.at * p.dout_ld + w.h * DH + d0);
+    V8<T> rest = {};
+    if (a.out_rest) rest = ld8(static_cast<const T*>(a.out_rest) + (w.at * a.Hq + w.h) * DH + d0);
 #pragma unroll
-    for (int d = 0; d < DH; d += 16) v = fmaf(to_f32(D[d + x]), to_f32(O[d + x]), v);
+    for (int j = 0; j < 8; ++j) v = fmaf(to_f32((T)d[j]), to_f32((T)o[j]) + to_f32((T)rest[j]), v);
   }
-  v += dpp<0x128>(v);
-  v += dpp<0x124>(v);
-  v += dpp<0x4e>(v);
-  v += dpp<0xb1>(v);
-  if (x == 0) p.delta[ro] = v;
+#pragma unroll
+  for (int m = 1; m < W; m <<= 1) v += __shfl_xor(v, m);
+  if (d0) return;
+  const float lse = w.live ? a.lse[w.at * a.Hq + w.h] : -INFINITY;
+  float4 x;
+  x.x = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  x.y = v;
+  x.z = __int_as_float(w.k * a.L);
+  x.w = __int_as_float(w.k * a.L + w.own);
+  p.rows[e] = x;
 }
 
 // dq: rows and chunks as in the forward, probabilities again from lse.
-template <typename T, int DH, int NW, int KC>
-__global__ __launch_bounds__(NW * 64) void k_prefix_dq(PrefixGradArgs p) {
+template <typename T, int DH, int QT, int NW, int KC>
+__global__ __launch_bounds__(NW * 64, 2) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
-  constexpr int NT = NW * 64, ROWS = NW * 16, NB = DH / 16, ND = DH / 32;
-  constexpr int KLD = DH + kPad<T>, VLD = KC + kPad<T>;
+  constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
+  constexpr int KLD = DH + 2 * kPad<T>, VLD = DH + kPad<T>;
   constexpr int PER_T = KC * DH / 8 / NT;
-  static_assert(KC * DH / 8 % NT == 0 && KC % 32 == 0, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Ks[KC * KLD];
-  __shared__ __attribute__((aligned(16))) T Vs[KC * KLD];
-  __shared__ __attribute__((aligned(16))) T Kt[DH * VLD];
+  constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
+  static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0, "tile shape");
+  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * KLD];
+  __shared__ __attribute__((aligned(16))) T Vs_[NBUF][KC * VLD];
   __shared__ int s_off[ROWS + 1];
+  __shared__ long long s_at[2][KC];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
   int id = xcd_tile(blockIdx.x, gridDim.x);
+  const int z = id % a.splits;
+  id /= a.splits;
   const int t = id % a.tiles;
   id /= a.tiles;
   const int g = id % a.Hkv, b = id / a.Hkv;
   const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R), sg = a.S * a.G;
   const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
   pack_own<NT>(a, b, k0, nb, s_off);
-  const int nctx = ctx_rows(a, b), nown = s_off[nb];
+  const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_off[nb]);
   const int cctx = (nctx + KC - 1) / KC, chunks = cctx + (nown + KC - 1) / KC;
+  const int cb = (int)((long long)chunks * z / a.splits), ce = (int)((long long)chunks * (z + 1) / a.splits);
 
-  const int r = r0 + wave * 16 + c16;
-  const Row row = row_of(a, b, g, r);
-  const int lo = s_off[row.k - k0], hi = lo + row.own;
-  const int wlo = wave_min(row.own ? lo : 0x7fffffff), whi = wave_max(hi * (row.own != 0));
-  const long long ro = row.at * a.Hq + row.h;
-  const float lse = row.live ? a.lse[ro] : -INFINITY;
-  const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;   // no keys: every probability 0
-  const float delta = row.live ? p.delta[ro] : 0.f;
-  V8<T> qf[ND], df[ND];
-  {
+  V8<T> kreg[PER_T], vreg[PER_T];
+  int gone = 0;
+  // The loads are unconditional (rows that do not count read one that exists); `gone` says what to leave out.
+  auto load_chunk = [&](int c) __attribute__((always_inline)) {
+    const bool shared = c < cctx;                  // uniform
+    const int left = shared ? nctx - c * KC : KC, ld = shared ? a.ctx_ld : a.own_ld;
+    const long long base = (long long)b * a.T + c * KC;
+    const T *kb = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + g * DH;
+    const T *vb = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + g * DH;
+    gone = 0;
+#pragma unroll
+    for (int q = 0; q < PER_T; ++q) {
+      const int e = q * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
+      long long x = base + min(key, left - 1);
+      if (!shared) {
+        x = s_at[c & 1][key];
+        gone |= (x < 0) << q;
+        x = max(x, 0LL);
+      } else {
+        gone |= (key >= left) << q;
+      }
+      kreg[q] = ld8(kb + x * ld + d0);
+      vreg[q] = ld8(vb + x * ld + d0);
+    }
+  };
+  long long found = -2;
+  auto find = [&](int c) __attribute__((always_inline)) {
+    if (c >= cctx && c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+  };
+  find(cb);
+  if (tid < KC) s_at[cb & 1][tid] = found;
+  __syncthreads();
+  if (cb < ce) load_chunk(cb);
+  find(cb + 1);
+
+  V8<T> qf[QT][ND], df[QT][ND];
+  int lo[QT], hi[QT], wlo[QT], whi[QT], alo[QT], ahi[QT];
+  float lse2[QT], delta[QT];
+  f32x4 o[QT][NB];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const int r = r0 + (wave * QT + i) * 16 + c16;
+    const Row row = row_of(a, b, g, r);
+    const float4 x = p.rows[((long long)b * a.Hkv + g) * a.R + min(r, a.R - 1)];
+    lse2[i] = row.live ? x.x : INFINITY;
+    delta[i] = row.live ? x.y : 0.f;
+    lo[i] = s_off[row.k - k0];
+    hi[i] = lo[i] + row.own;
+    wlo[i] = wave_min(row.own ? lo[i] : 0x7fffffff);
+    whi[i] = wave_max(hi[i] * (row.own != 0));
+    alo[i] = wave_max(lo[i]);
+    ahi[i] = wave_min(hi[i]);
     const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH;
     const T* D = static_cast<const T*>(p.dout) + row.at * p.dout_ld + row.h * DH;
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      qf[c] = row.live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
-      df[c] = row.live ? ld8(D + c * 32 + g4 * 8) : V8<T>{};
+      qf[i][c] = row.live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
+      df[i][c] = row.live ? ld8(D + c * 32 + g4 * 8) : V8<T>{};
     }
-  }
-  f32x4 o[NB];
 #pragma unroll
-  for (int n = 0; n < NB; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NB; ++n) o[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   const float sl2 = a.scale * kLog2e;
 
-  V8<T> kreg[PER_T], vreg[PER_T];
-  auto load_chunk = [&](int c) {
+  int cur = 0;
+  for (int c = cb; c < ce; ++c, cur ^= NBUF - 1) {
+    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    if constexpr (NBUF == 1) lds_barrier();
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
       const int e = q * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      const T *kp = nullptr, *vp = nullptr;
-      if (c < cctx) {
-        const int x = c * KC + key;
-        if (x < nctx) {
-          const long long at = ((long long)b * a.T + x) * a.ctx_ld + g * DH + d0;
-          kp = static_cast<const T*>(a.ctx_k) + at;
-          vp = static_cast<const T*>(a.ctx_v) + at;
-        }
-      } else {
-        const int x = (c - cctx) * KC + key;
-        if (x < nown) {
-          const int i = packed_list(s_off, nb, x);
-          const long long at = own_row(a, b * a.K + k0 + i, x - s_off[i]) * a.own_ld + g * DH + d0;
-          kp = static_cast<const T*>(a.own_k) + at;
-          vp = static_cast<const T*>(a.own_v) + at;
-        }
-      }
-      kreg[q] = kp ? ld8(kp) : V8<T>{};
-      vreg[q] = vp ? ld8(vp) : V8<T>{};
-    }
-  };
-  if (chunks) load_chunk(0);
-  for (int c = 0; c < chunks; ++c) {
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < PER_T; ++q) {
-      const int e = q * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
+      if ((c >= cctx || (c + 1) * KC > nctx) && gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
       st8(&Ks[key * KLD + d0], kreg[q]);
-      st8(&Vs[key * KLD + d0], vreg[q]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) Kt[(d0 + i) * VLD + key] = kreg[q][i];
+      st8(&Vs[key * VLD + d0], vreg[q]);
     }
-    __syncthreads();
-    if (c + 1 < chunks) load_chunk(c + 1);
+    if (c + 1 >= cctx && tid < KC) s_at[(c + 1) & 1][tid] = found;
+    lds_barrier();
+    if (c + 1 < ce) load_chunk(c + 1);
+    find(c + 2);
     const bool shared = c < cctx;
     const int base = shared ? c * KC : (c - cctx) * KC, top = shared ? nctx : nown;
-    const int l = shared ? 0 : lo, h = shared ? nctx : hi;
 #pragma unroll
     for (int kb = 0; kb < KC; kb += 32) {
       const int x0 = base + kb;
       if (x0 >= top) break;                                            // uniform
-      if (!shared && (x0 >= whi || x0 + 32 <= wlo)) continue;          // uniform
-      V8<T> ds;
+      V8<T> ds[QT];
+      unsigned sees = 0;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-        const int at = (kb + (c16 >> 2) * 8 + (c16 & 3) + 4 * x) * KLD + g4 * 8;
+      for (int i = 0; i < QT; ++i) {
+        if (!shared && (x0 >= whi[i] || x0 + 32 <= wlo[i])) continue;  // uniform
+        sees |= 1u << i;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          s = mma(ld8(&Ks[at + d * 32]), qf[d], s);
-          dp = mma(ld8(&Vs[at + d * 32]), df[d], dp);
-        }
+        for (int x = 0; x < 2; ++x) {
+          f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+          const int key = kb + 16 * x + c16;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int y = x0 + g4 * 8 + 4 * x + j;
-          const float e = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -lse2)) * (dp[j] - delta);
-          ds[4 * x + j] = from_f32<T>(y >= l && y < h ? e : 0.f);
+          for (int d = 0; d < ND; ++d) {
+            s = mma(ld8(&Ks[key * KLD + d * 32 + g4 * 8]), qf[i][d], s);
+            dp = mma(ld8(&Vs[key * VLD + d * 32 + g4 * 8]), df[i][d], dp);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -lse2[i])) * (dp[j] - delta[i]);
+          if (shared ? x0 + 32 > nctx : (x0 < alo[i] || x0 + 32 > ahi[i])) {   // uniform
+            const int l = shared ? 0 : lo[i], h = shared ? nctx : hi[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int y = x0 + 16 * x + 4 * g4 + j;
+              if (y < l || y >= h) s[j] = 0.f;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ds[i][4 * x + j] = from_f32<T>(s[j]);
         }
       }
 #pragma unroll
-      for (int n = 0; n < NB; ++n) o[n] = mma(ld8(&Kt[(n * 16 + c16) * VLD + kb + g4 * 8]), ds, o[n]);
+      for (int n = 0; n < NB; ++n) {
+        const V8<T> kt = ld_cols<KLD>(Ks, kb, n * 16, lane);
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+          if (sees >> i & 1) o[i][n] = mma(kt, ds[i], o[i][n]);
+      }
     }
   }
-  if (r >= a.R) return;
-  T* O = static_cast<T*>(p.dq) + row.at * p.dq_ld + row.h * DH;
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
+  for (int i = 0; i < QT; ++i) {
+    const int r = r0 + (wave * QT + i) * 16 + c16;
+    if (r >= a.R) continue;
+    const Row row = row_of(a, b, g, r);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) O[n * 16 + g4 * 4 + q] = from_f32<T>(row.live ? o[n][q] * a.scale : 0.f);
+    for (int n = 0; n < NB; ++n) {
+      const f32x4 v = o[i][n] * (row.live ? a.scale : 0.f);
+      if (a.splits > 1) {
+        const long long rows = (long long)a.B * a.K * a.S * a.Hq;
+        *reinterpret_cast<f32x4*>(a.part_o + (z * rows + row.at * a.Hq + row.h) * DH + n * 16 + g4 * 4) = v;
+      } else {
+        st4(static_cast<T*>(p.dq) + row.at * p.dq_ld + row.h * DH + n * 16 + g4 * 4, v);
+      }
+    }
+  }
 }
 
-// dk and dv of a tile of keys: the keys stay in registers, the rows stream through LDS in chunks of RC, by rows and
-// transposed.  Tiles 0 .. ctx_tiles - 1 of a (request, key head) hold shared rows and meet every row; the others hold
-// own rows (dense, list after list) and meet the rows of their lists.  In the tile's numbering -- shared row, or
-// k L + j -- the keys that a row sees are again one interval.
-template <typename T, int DH, int NW, int RC>
-__global__ __launch_bounds__(NW * 64) void k_prefix_dkv(PrefixGradArgs p) {
+// dk and dv of a tile of keys: NW waves of KT 16-key tiles whose keys and values stay in registers, the rows stream through
+// LDS in chunks of RC.  Tiles 0 .. ctx_tiles - 1 of a (request, key head) hold shared rows and meet every row; the others
+// hold own rows (dense, list after list) and meet the rows of their lists.  In the tile's numbering -- shared row, or
+// k L + j -- the keys that a row sees are again one interval.  Few tiles: `row_splits` workgroups share a tile's rows.
+template <typename T, int DH, int KT, int NW, int RC>
+__global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
-  constexpr int NT = NW * 64, COLS = NW * 16, NB = DH / 16, ND = DH / 32;
-  constexpr int KLD = DH + kPad<T>, VLD = RC + kPad<T>;
-  constexpr int PER_T = (RC * DH / 8 + NT - 1) / NT;
-  static_assert(RC % 32 == 0 && RC <= NT, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Qs[RC * KLD], Ds[RC * KLD];
-  __shared__ __attribute__((aligned(16))) T Qt[DH * VLD], Dt[DH * VLD];
-  __shared__ float s_lse[RC], s_delta[RC];
-  __shared__ int s_lo[RC], s_hi[RC];
+  constexpr int NT = NW * 64, COLS = NW * KT * 16, NB = DH / 16, ND = DH / 32;
+  constexpr int LD = DH + 2 * kPad<T>;
+  constexpr int PER_T = RC * DH / 8 / NT;
+  static_assert(RC * DH / 8 % NT == 0 && RC % 32 == 0 && RC <= NT, "tile shape");
+  __shared__ __attribute__((aligned(16))) T Qs_[2][RC * LD], Ds_[2][RC * LD];
+  __shared__ float4 s_row[2][RC];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
   int id = xcd_tile(blockIdx.x, gridDim.x);
-  const int t = id % (p.ctx_tiles + p.own_tiles);
-  id /= p.ctx_tiles + p.own_tiles;
+  const int z = id % p.row_splits;
+  id /= p.row_splits;
+  const int tiles = p.ctx_tiles + p.own_tiles, t = id % tiles;
+  id /= tiles;
   const int g = id % a.Hkv, b = id / a.Hkv;
   const bool shared = t < p.ctx_tiles;
   const int x0 = (shared ? t : t - p.ctx_tiles) * COLS, cols = shared ? a.T : a.K * a.L, sg = a.S * a.G;
@@ -554,108 +735,195 @@ __global__ __launch_bounds__(NW * 64) void k_prefix_dkv(PrefixGradArgs p) {
     rb = x0 / a.L * sg;
     re = ((min(x0 + COLS, cols) - 1) / a.L + 1) * sg;
   }
+  const int steps = (re - rb + RC - 1) / RC;
+  const int cb = (int)((long long)steps * z / p.row_splits), ce = (int)((long long)steps * (z + 1) / p.row_splits);
 
-  const int x = x0 + wave * 16 + c16;                                   // this lane's key
-  bool live = false;
-  long long at = 0;                                                     // its row of the tensors
-  if (x < cols) {
-    if (shared) {
-      live = x < nctx;
-      at = (long long)b * a.T + x;
-    } else {
-      const int bk = b * a.K + x / a.L;
-      live = x % a.L < own_rows(a, bk) && q_rows(a, bk) > 0;
-      at = (long long)b * cols + x;
-    }
-  }
-  V8<T> kf[ND], vf[ND];
-  {
-    const long long off = at * (shared ? a.ctx_ld : a.own_ld) + g * DH + g4 * 8;
-    const T *kp = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + off, *vp = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + off;
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      kf[d] = live ? ld8(kp + d * 32) : V8<T>{};
-      vf[d] = live ? ld8(vp + d * 32) : V8<T>{};
-    }
-  }
-  f32x4 dk[NB], dv[NB];
-#pragma unroll
-  for (int n = 0; n < NB; ++n) dk[n] = dv[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const float sl2 = a.scale * kLog2e;
-
-  for (int rc = rb; rc < re; rc += RC) {
-    __syncthreads();
+  V8<T> qreg[PER_T], dreg[PER_T];
+  float lreg[PER_T];
+  float4 rreg;
+  const float4* rows = p.rows + ((long long)b * a.Hkv + g) * a.R;
+  auto load_chunk = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
-      const int e = q * NT + tid, i = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      if (RC * DH / 8 % NT != 0 && i >= RC) continue;
-      const Row w = row_of(a, b, g, rc + i);
-      const bool in = w.live && rc + i < re;
-      const V8<T> qv = in ? ld8(static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + d0) : V8<T>{};
-      const V8<T> dv8 = in ? ld8(static_cast<const T*>(p.dout) + w.at * p.dout_ld + w.h * DH + d0) : V8<T>{};
-      st8(&Qs[i * KLD + d0], qv);
-      st8(&Ds[i * KLD + d0], dv8);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        Qt[(d0 + j) * VLD + i] = qv[j];
-        Dt[(d0 + j) * VLD + i] = dv8[j];
+      const int e = q * NT + tid, r = rb + c * RC + e / (DH / 8), d0 = (e % (DH / 8)) * 8;
+      lreg[q] = INFINITY;
+      qreg[q] = dreg[q] = V8<T>{};
+      if (r < re) {
+        const long long at = (long long)b * a.K * a.S + r / a.G;
+        const int h = g * a.G + r % a.G;
+        qreg[q] = ld8(static_cast<const T*>(a.q) + at * a.q_ld + h * DH + d0);
+        dreg[q] = ld8(static_cast<const T*>(p.dout) + at * p.dout_ld + h * DH + d0);
+        lreg[q] = rows[r].x;
       }
     }
     if (tid < RC) {
-      const Row w = row_of(a, b, g, rc + tid);
-      const bool in = w.live && rc + tid < re;
-      const float l = in ? a.lse[w.at * a.Hq + w.h] : -INFINITY;
-      s_lse[tid] = l == -INFINITY ? INFINITY : l * kLog2e;
-      s_delta[tid] = in ? p.delta[w.at * a.Hq + w.h] : 0.f;
-      s_lo[tid] = shared ? 0 : w.k * a.L;
-      s_hi[tid] = !in ? 0 : shared ? nctx : w.k * a.L + w.own;
+      const int r = rb + c * RC + tid;
+      rreg = r < re ? rows[r] : make_float4(INFINITY, 0.f, 0.f, 0.f);
     }
-    __syncthreads();
+  };
+  if (cb < ce) load_chunk(cb);
+
+  V8<T> kf[KT][ND], vf[KT][ND];
+  bool live[KT];
+  long long at[KT];                                                     // the key's row of the tensors
+  f32x4 dk[KT][NB], dv[KT][NB];
+#pragma unroll
+  for (int i = 0; i < KT; ++i) {
+    const int x = x0 + (wave * KT + i) * 16 + c16;                      // this lane's key
+    live[i] = false;
+    at[i] = 0;
+    if (x < cols) {
+      if (shared) {
+        live[i] = x < nctx;
+        at[i] = (long long)b * a.T + x;
+      } else {
+        const int bk = b * a.K + x / a.L;
+        live[i] = x % a.L < own_rows(a, bk) && q_rows(a, bk) > 0;
+        at[i] = (long long)b * cols + x;
+      }
+    }
+    const long long off = at[i] * (shared ? a.ctx_ld : a.own_ld) + g * DH + g4 * 8;
+    const T *kp = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + off, *vp = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + off;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      kf[i][d] = live[i] ? ld8(kp + d * 32) : V8<T>{};
+      vf[i][d] = live[i] ? ld8(vp + d * 32) : V8<T>{};
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) dk[i][n] = dv[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sl2 = a.scale * kLog2e;
+
+  int cur = 0;
+  for (int c = cb; c < ce; ++c, cur ^= 1) {
+    T *Qs = Qs_[cur], *Ds = Ds_[cur];
+#pragma unroll
+    for (int q = 0; q < PER_T; ++q) {
+      const int e = q * NT + tid, i = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
+      const bool in = lreg[q] != INFINITY;                              // a row that sees nothing may hold anything
+      st8(&Qs[i * LD + d0], in ? qreg[q] : V8<T>{});
+      st8(&Ds[i * LD + d0], in ? dreg[q] : V8<T>{});
+    }
+    if (tid < RC) s_row[cur][tid] = rreg;
+    lds_barrier();
+    if (c + 1 < ce) load_chunk(c + 1);
 #pragma unroll
     for (int kb = 0; kb < RC; kb += 32) {
-      V8<T> pb, ds;
+      if (rb + c * RC + kb >= re) break;                                // uniform
+      float4 w[8];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-        const int ar = (kb + (c16 >> 2) * 8 + (c16 & 3) + 4 * u) * KLD + g4 * 8;
+      for (int j = 0; j < 8; ++j) w[j] = s_row[cur][kb + key_of(j, g4)];
+      V8<T> pb[KT], ds[KT];
+      unsigned sees = 0;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          s = mma(ld8(&Qs[ar + d * 32]), kf[d], s);
-          dp = mma(ld8(&Ds[ar + d * 32]), vf[d], dp);
+      for (int i = 0; i < KT; ++i) {
+        const int x = x0 + (wave * KT + i) * 16 + c16;
+        bool any = false;
+        if (!shared) {                                                  // uniform
+#pragma unroll
+          for (int j = 0; j < 8; ++j) any |= x >= __float_as_int(w[j].z) && x < __float_as_int(w[j].w);
+          if (!__any(any)) continue;
         }
+        sees |= 1u << i;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = kb + g4 * 8 + 4 * u + j;
-          const bool sees = x >= s_lo[i] && x < s_hi[i];
-          const float e = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -s_lse[i]));
-          pb[4 * u + j] = from_f32<T>(sees ? e : 0.f);
-          ds[4 * u + j] = from_f32<T>(sees ? e * (dp[j] - s_delta[i]) : 0.f);
+        for (int u = 0; u < 2; ++u) {
+          f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+          const int ar = (kb + 16 * u + c16) * LD + g4 * 8;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            s = mma(ld8(&Qs[ar + d * 32]), kf[i][d], s);
+            dp = mma(ld8(&Ds[ar + d * 32]), vf[i][d], dp);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float4 y = w[4 * u + j];
+            const bool in = shared ? x < nctx : x >= __float_as_int(y.z) && x < __float_as_int(y.w);
+            const float e = in ? __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -y.x)) : 0.f;
+            pb[i][4 * u + j] = from_f32<T>(e);
+            ds[i][4 * u + j] = from_f32<T>(e * (dp[j] - y.y));
+          }
         }
       }
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        dv[n] = mma(ld8(&Dt[(n * 16 + c16) * VLD + kb + g4 * 8]), pb, dv[n]);
-        dk[n] = mma(ld8(&Qt[(n * 16 + c16) * VLD + kb + g4 * 8]), ds, dk[n]);
+        const V8<T> dt = ld_cols<LD>(Ds, kb, n * 16, lane), qt = ld_cols<LD>(Qs, kb, n * 16, lane);
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+          if (sees >> i & 1) {
+            dv[i][n] = mma(dt, pb[i], dv[i][n]);
+            dk[i][n] = mma(qt, ds[i], dk[i][n]);
+          }
       }
     }
   }
-  if (x >= cols) return;
-  const long long off = at * (shared ? p.dctx_ld : p.down_ld) + g * DH;
-  T *ko = static_cast<T*>(shared ? p.dctx_k : p.down_k) + off, *vo = static_cast<T*>(shared ? p.dctx_v : p.down_v) + off;
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
+  for (int i = 0; i < KT; ++i) {
+    const int x = x0 + (wave * KT + i) * 16 + c16;
+    if (x >= cols) continue;
+    const long long off = at[i] * (shared ? p.dctx_ld : p.down_ld) + g * DH + g4 * 4;
+    T *ko = static_cast<T*>(shared ? p.dctx_k : p.down_k) + off, *vo = static_cast<T*>(shared ? p.dctx_v : p.down_v) + off;
+    const long long n_keys = (long long)a.B * (a.T + a.K * a.L) * a.Hkv;
+    const long long key = ((shared ? 0 : (long long)a.B * a.T) + at[i]) * a.Hkv + g;
+    float* po = p.row_splits > 1 ? p.part_kv + ((long long)z * n_keys + key) * 2 * DH + g4 * 4 : nullptr;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      ko[n * 16 + g4 * 4 + q] = from_f32<T>(live ? dk[n][q] * a.scale : 0.f);
-      vo[n * 16 + g4 * 4 + q] = from_f32<T>(live ? dv[n][q] : 0.f);
+    for (int n = 0; n < NB; ++n) {
+      const f32x4 k4 = dk[i][n] * a.scale, v4 = dv[i][n];
+      if (po) {
+        *reinterpret_cast<f32x4*>(po + n * 16) = k4;
+        *reinterpret_cast<f32x4*>(po + DH + n * 16) = v4;
+      } else {
+        st4(ko + n * 16, k4);
+        st4(vo + n * 16, v4);
+      }
     }
+  }
+}
+
+// Adds the partial sums of dq (key ranges) and of dk, dv (row ranges) in ascending order.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_prefix_sum_dq(PrefixGradArgs p) {
+  const PrefixArgs& a = p.f;
+  const long long rows = (long long)a.B * a.K * a.S * a.Hq;
+  const long long e = (long long)blockIdx.x * 256 + threadIdx.x, ro = e / (DH / 4);
+  const int d0 = (int)(e % (DH / 4)) * 4;
+  if (ro >= rows) return;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int z = 0; z < a.splits; ++z) v += *reinterpret_cast<const f32x4*>(a.part_o + (z * rows + ro) * DH + d0);
+  st4(static_cast<T*>(p.dq) + ro / a.Hq * p.dq_ld + ro % a.Hq * DH + d0, v);
+}
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_prefix_sum_dkv(PrefixGradArgs p) {
+  const PrefixArgs& a = p.f;
+  const long long n_keys = (long long)a.B * (a.T + a.K * a.L) * a.Hkv;
+  const long long e = (long long)blockIdx.x * 256 + threadIdx.x, key = e / (DH / 2);
+  const int d0 = (int)(e % (DH / 2)) * 4;                               // dk, then dv
+  if (key >= n_keys) return;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int z = 0; z < p.row_splits; ++z) v += *reinterpret_cast<const f32x4*>(p.part_kv + (z * n_keys + key) * 2 * DH + d0);
+  const long long at = key / a.Hkv, ctx = (long long)a.B * a.T;
+  const int g = (int)(key % a.Hkv), d = d0 % DH;
+  const bool is_v = d0 >= DH;
+  T* dst = at < ctx ? static_cast<T*>(is_v ? p.dctx_v : p.dctx_k) + at * p.dctx_ld
+                    : static_cast<T*>(is_v ? p.down_v : p.down_k) + (at - ctx) * p.down_ld;
+  st4(dst + g * DH + d, v);
+}
+
+// Tile shapes.  Forward and dq: QT 16-row tiles a wave; dkv: KT 16-key tiles a wave and RC rows a chunk.
+template <typename T, int DH> constexpr int kKT = DH == 128 ? 1 : 2;
+template <typename T, int DH> constexpr int kRC = sizeof(T) * DH > 256 ? 32 : 64;
+
+template <typename T, int DH, int QT>
+hipError_t launch_fwd_qt(const PrefixArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.splits));
+  hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, 64>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 template <typename T, int DH>
 hipError_t fwd(const PrefixArgs& a, const PrefixPlan& p, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.splits));
-  hipLaunchKernelGGL((k_prefix_fwd<T, DH, 1, 4, 64>), grid, dim3(256), 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = p.rows == 128 ? launch_fwd_qt<T, DH, 2>(a, s) : launch_fwd_qt<T, DH, 1>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   const long long rows = (long long)a.B * a.K * a.S * a.Hq;
   hipLaunchKernelGGL((k_prefix_join<T, DH>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, s, a);
@@ -663,20 +931,36 @@ hipError_t fwd(const PrefixArgs& a, const PrefixPlan& p, hipStream_t s) {
 }
 
 template <typename T, int DH>
-hipError_t grad(PrefixGradArgs p, hipStream_t s) {
+hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   PrefixArgs& a = p.f;
   const long long rows = (long long)a.B * a.K * a.S * a.Hq, bg = (long long)a.B * a.Hkv;
-  hipLaunchKernelGGL((k_prefix_delta<T, DH>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_prefix_rows<T, DH>), dim3((unsigned)((rows * (DH / 8) + 255) / 256)), dim3(256), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  a.tiles = (a.R + 63) / 64;
-  hipLaunchKernelGGL((k_prefix_dq<T, DH, 4, 64>), dim3((unsigned)(bg * a.tiles)), dim3(256), 0, s, p);
+  a.tiles = pl.tiles;
+  a.splits = pl.splits;
+  const dim3 gq((unsigned)(bg * a.tiles * a.splits));
+  if (pl.rows == 128)
+    hipLaunchKernelGGL((k_prefix_dq<T, DH, 2, 4, 64>), gq, dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, 64>), gq, dim3(256), 0, s, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  p.ctx_tiles = (a.T + 63) / 64;
-  p.own_tiles = (int)(((long long)a.K * a.L + 63) / 64);
+  if (a.splits > 1) {
+    hipLaunchKernelGGL((k_prefix_sum_dq<T, DH>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, s, p);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  p.ctx_tiles = pl.ctx_tiles;
+  p.own_tiles = pl.own_tiles;
+  p.row_splits = pl.row_splits;
   if (p.ctx_tiles + p.own_tiles == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_prefix_dkv<T, DH, 4, 32>), dim3((unsigned)(bg * (p.ctx_tiles + p.own_tiles))), dim3(256), 0, s, p);
+  const dim3 gk((unsigned)(bg * (p.ctx_tiles + p.own_tiles) * p.row_splits));
+  hipLaunchKernelGGL((k_prefix_dkv<T, DH, kKT<T, DH>, 4, kRC<T, DH>>), gk, dim3(256), 0, s, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.row_splits == 1) return e;
+  const long long keys = (long long)a.B * (a.T + a.K * a.L) * a.Hkv;
+  hipLaunchKernelGGL((k_prefix_sum_dkv<T, DH>), dim3((unsigned)((keys * (DH / 2) + 255) / 256)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -684,16 +968,37 @@ hipError_t grad(PrefixGradArgs p, hipStream_t s) {
 
 PrefixPlan prefix_plan(const fe_prefix_args& a) {
   PrefixPlan p;
-  p.rows = 64;
-  const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G;
+  const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
+  // 128 rows a workgroup share the staged keys where that leaves two workgroups per compute unit
+  p.rows = bg * ((R + 127) / 128) >= 512 ? 128 : 64;
   p.tiles = (int)((R + p.rows - 1) / p.rows);
   // split the keys while the launch has fewer than four workgroups per compute unit and a range keeps two chunks
-  const long long wgs = (long long)a.B * a.n_kv_heads * p.tiles;
+  const long long wgs = bg * p.tiles;
   const long long lists = std::min<long long>(a.K, (p.rows - 1) / (a.S * G) + 2);
   const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
   p.splits = (int)std::max(1LL, std::min({1024 / std::max(1LL, wgs), chunks / 2, 64LL}));
   const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads;
   p.part_bytes = p.splits > 1 ? p.splits * rows * (a.dh + 2) * sizeof(float) : 0;
+  return p;
+}
+
+PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a) {
+  PrefixGradPlan p;
+  const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
+  p.rows = bg * ((R + 127) / 128) >= 512 ? 128 : 64;
+  p.tiles = (int)((R + p.rows - 1) / p.rows);
+  const long long lists = std::min<long long>(a.K, (p.rows - 1) / (a.S * G) + 2);
+  const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
+  p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 2, 16LL}));
+  const int cols = a.dh == 128 ? 64 : 128;
+  p.ctx_tiles = (a.T + cols - 1) / cols;
+  p.own_tiles = (int)(((long long)a.K * a.L + cols - 1) / cols);
+  const long long wgs = bg * (p.ctx_tiles + p.own_tiles);
+  p.row_splits = wgs ? (int)std::max(1LL, std::min({512 / wgs, (R + 63) / 64 / 2, 16LL})) : 1;
+  const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads, keys = (size_t)a.B * (a.T + (size_t)a.K * a.L) * a.n_kv_heads;
+  p.rows_bytes = rows * sizeof(float4);
+  p.dq_bytes = p.splits > 1 ? p.splits * rows * a.dh * sizeof(float) : 0;
+  p.dkv_bytes = p.row_splits > 1 ? p.row_splits * keys * 2 * a.dh * sizeof(float) : 0;
   return p;
 }
 
@@ -704,7 +1009,7 @@ hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixP
   return dh == 32 ? fwd<float, 32>(a, p, s) : dh == 64 ? fwd<float, 64>(a, p, s) : fwd<float, 128>(a, p, s);
 }
 
-hipError_t launch_prefix_grad(PrefixGradArgs a, int dh, bool bf16_rows, hipStream_t s) {
-  if (bf16_rows) return dh == 32 ? grad<bf16, 32>(a, s) : dh == 64 ? grad<bf16, 64>(a, s) : grad<bf16, 128>(a, s);
-  return dh == 32 ? grad<float, 32>(a, s) : dh == 64 ? grad<float, 64>(a, s) : grad<float, 128>(a, s);
+hipError_t launch_prefix_grad(const PrefixGradArgs& a, int dh, bool bf16_rows, const PrefixGradPlan& p, hipStream_t s) {
+  if (bf16_rows) return dh == 32 ? grad<bf16, 32>(a, p, s) : dh == 64 ? grad<bf16, 64>(a, p, s) : grad<bf16, 128>(a, p, s);
+  return dh == 32 ? grad<float, 32>(a, p, s) : dh == 64 ? grad<float, 64>(a, p, s) : grad<float, 128>(a, p, s);
 }

@@ -66,7 +66,7 @@ fe_append_args = _struct(
     "q k v q_out freq table len new_len pos0 k_pages v_pages len_out status")
 fe_prefix_args = _struct(
     "fe_prefix_args", "dtype B K S n_heads n_kv_heads dh T L page_rows n_pages causal scale q_ld ctx_ld own_ld out_ld",
-    "q ctx_k ctx_v own_k own_v table ctx_len q_len own_len out lse ws", [("ws_bytes", ctypes.c_size_t)])
+    "q ctx_k ctx_v own_k own_v table ctx_len q_len own_len out lse out_rest ws", [("ws_bytes", ctypes.c_size_t)])
 
 
 class fe_prefix_grads(ctypes.Structure):
@@ -672,8 +672,10 @@ class PrefixAttention:
         a, dev = self.args, torch.device("cuda", torch.cuda.current_device())
         self.out = torch.empty((a.B, a.K, a.S, a.n_heads, a.dh), dtype=self.act, device=dev)
         self.lse = torch.empty((a.B, a.K, a.S, a.n_heads), dtype=torch.float32, device=dev) if self.train else None
+        self.out_rest = torch.empty_like(self.out) if self.train and self.act == torch.bfloat16 else None
         self.ws = torch.empty(max(16, self.ws_bytes), dtype=torch.uint8, device=dev)
-        a.out, a.lse, a.ws, a.ws_bytes = _ptr(self.out), _ptr(self.lse), _ptr(self.ws), self.ws_bytes
+        a.out, a.lse, a.out_rest = _ptr(self.out), _ptr(self.lse), _ptr(self.out_rest)
+        a.ws, a.ws_bytes = _ptr(self.ws), self.ws_bytes
         a.out_ld = a.n_heads * a.dh
         if self.train:
             self.grads = (torch.empty_like(self.out),
