@@ -107,8 +107,8 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream);
  * Errors: FE_EINVAL for a NULL or misaligned pointer, B, K, S, heads below 1, T or L below 0, n_heads not a
  * multiple of n_kv_heads, strides too short or not multiples of 16 bytes, L not a multiple of page_rows, a
  * scale that is not finite, an unknown dtype, a workspace that is too small; FE_EUNSUPPORTED for dh outside
- * {32, 64, 128}, T or L above 4194304, B*K*S*n_heads, B*T or B*K*L above 1073741823, or more than 16777215
- * workgroups of 64 rows or keys of one request and key head.
+ * {32, 64, 128}, T or L above 4194304, B*K*S*n_heads, B*T or B*K*L above 1073741823, more than 16777215
+ * workgroups of 64 rows or keys of one request and key head, or ctx_ld above 16777216.
  */
 typedef struct {
   int32_t dtype;                        /* fe_dtype of q, keys, values and out */

@@ -24,6 +24,8 @@ constexpr long long kInt32 = 0x7fffffffLL, kMaxGrid = (1 << 24) - 1;
 
 // A row stride of `ld` elements holds `width` and keeps rows 16-byte aligned.
 bool stride_ok(int ld, long long width, int dtype) { return ld >= width && ld % (dtype == FE_BF16 ? 8 : 4) == 0; }
+// ... and a chunk of 64 rows keeps its offsets in 32 bits.
+constexpr int kMaxStride = 1 << 24;
 
 fe_status check_sizes(const fe_prefix_args* a) {
   if (!a) return pfail(FE_EINVAL, "arguments are NULL");
@@ -67,6 +69,7 @@ fe_status check_forward(const fe_prefix_args* a) {
   if (!stride_ok(a->q_ld, wq, a->dtype) || !stride_ok(a->out_ld, wq, a->dtype) ||
       (a->T > 0 && !stride_ok(a->ctx_ld, wk, a->dtype)) || (a->L > 0 && !stride_ok(a->own_ld, wk, a->dtype)))
     return pfail(FE_EINVAL, "a row stride is shorter than its row or not a multiple of 16 bytes");
+  if (a->T > 0 && a->ctx_ld > kMaxStride) return pfail(FE_EUNSUPPORTED, "ctx_ld=%d above %d", a->ctx_ld, kMaxStride);
   return FE_OK;
 }
 

@@ -42,6 +42,13 @@ FE_DEV void st4(bf16* p, f32x4 v) {
 // LDS row padding: 16 bytes
 template <typename T> constexpr int kPad = 16 / sizeof(T);
 
+// Eight floats rounded to T (round to nearest even).
+template <typename T> FE_DEV V8<T> pack8(const float (&s)[8]);
+template <> FE_DEV f32x8 pack8<float>(const float (&s)[8]) { return f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}; }
+template <> FE_DEV bf16x8 pack8<bf16>(const float (&s)[8]) {
+  return __builtin_convertvector((f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}), bf16x8);
+}
+
 FE_DEV bool finite8(bf16x8 v) {
   const u32x4 w = __builtin_bit_cast(u32x4, v);
   bool bad = false;
@@ -100,6 +107,12 @@ template <int NT>
 FE_DEV void pack_own(const PrefixArgs& a, int b, int k0, int nb, int* off) {
   __shared__ int s_tot[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (!a.q_len && !a.own_len) {                    // uniform: lists of one length
+    if (tid <= nb) off[tid] = tid * a.L;
+    if (tid == 0) off[nb] = nb * a.L;
+    __syncthreads();
+    return;
+  }
   int v = 0;
   if (tid < nb) {
     const int bk = b * a.K + k0 + tid;
@@ -200,16 +213,16 @@ template <typename T, int DH, int QT, int NW, int KC>
 __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_prefix_fwd(PrefixArgs a) {
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
   constexpr int KLD = DH + kPad<T>, VLD = DH + 2 * kPad<T>;
-  constexpr int PER_T = KC * DH / 8 / NT;
+  constexpr int PER_T = KC * DH / 8 / NT, STEP = NT / (DH / 8);
   constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
   static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0 && KC <= NT, "tile shape");
   __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * KLD];
   __shared__ __attribute__((aligned(16))) T Vs_[NBUF][KC * VLD];
   __shared__ int s_off[ROWS + 1];
-  // per buffer: the last chunk whose values are not all finite, the last chunk with keys of pages outside the
-  // pool, and those keys
+  // by chunk parity: the last chunk whose values are not all finite, the last chunk with keys of pages outside the
+  // pool, and those keys; rows of the next own chunks
   __shared__ int s_odd[2], s_holes[2], s_hole[2][KC];
-  __shared__ long long s_at[2][KC];                // rows of the next own chunks
+  __shared__ long long s_at[2][KC];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
@@ -228,48 +241,56 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
   const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_off[nb]);
   const int cctx = (nctx + KC - 1) / KC, chunks = cctx + (nown + KC - 1) / KC;
   const int cb = (int)((long long)chunks * z / a.splits), ce = (int)((long long)chunks * (z + 1) / a.splits);
+  const int cm = min(max(cctx, cb), ce);           // shared chunks [cb, cm), own chunks [cm, ce)
 
+  // The loads are unconditional: rows that do not count read one that exists and are cleared when they are staged.
   V8<T> kreg[PER_T], vreg[PER_T];
-  int gone = 0, hole = 0;                          // bit p: key of kreg[p] past the rows or without a page; without a page
-  // The loads are unconditional (rows that do not count read one that exists); `gone` says what to leave out.
-  auto load_chunk = [&](int c) __attribute__((always_inline)) {
-    const bool shared = c < cctx;                  // uniform
-    const int left = shared ? nctx - c * KC : KC, ld = shared ? a.ctx_ld : a.own_ld;
-    const long long base = (long long)b * a.T + c * KC;
-    const T *kb = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + g * DH;
-    const T *vb = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + g * DH;
+  const int key0 = tid / (DH / 8), d0 = tid % (DH / 8) * 8;            // this thread's part of a chunk: keys key0 + p STEP
+  auto load_ctx = [&](int c) __attribute__((always_inline)) {
+    const long long base = ((long long)b * a.T + c * KC) * a.ctx_ld + g * DH;
+    const T *kp = static_cast<const T*>(a.ctx_k) + base, *vp = static_cast<const T*>(a.ctx_v) + base;
+    const int last = min(nctx - c * KC, KC) - 1;
+#pragma unroll
+    for (int p = 0; p < PER_T; ++p) {
+      const unsigned off = (unsigned)(min(key0 + p * STEP, last) * a.ctx_ld + d0);
+      kreg[p] = ld8(kp + off);
+      vreg[p] = ld8(vp + off);
+    }
+  };
+  int gone = 0, hole = 0;                          // bit p: the key does not count; because its page is outside the pool
+  auto load_own = [&](int c) __attribute__((always_inline)) {
+    const T *kp = static_cast<const T*>(a.own_k) + g * DH + d0, *vp = static_cast<const T*>(a.own_v) + g * DH + d0;
     gone = hole = 0;
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
-      const int e = p * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      long long x = base + min(key, left - 1);
-      if (!shared) {
-        x = s_at[c & 1][key];
-        gone |= (x < 0) << p;
-        hole |= (x == -1) << p;
-        x = max(x, 0LL);
-      } else {
-        gone |= (key >= left) << p;
-      }
-      kreg[p] = ld8(kb + x * ld + d0);
-      vreg[p] = ld8(vb + x * ld + d0);
+      const long long x = s_at[c & 1][key0 + p * STEP], at = max(x, 0LL) * a.own_ld;
+      gone |= (x < 0) << p;
+      hole |= (x == -1) << p;
+      kreg[p] = ld8(kp + at);
+      vreg[p] = ld8(vp + at);
     }
   };
   // own rows are found one chunk before they are loaded, so that a page table's latency is hidden as well
   long long found = -2;
   auto find = [&](int c) __attribute__((always_inline)) {
-    if (c >= cctx && c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+    if (c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
   };
-  find(cb);
-  if (tid < KC) s_at[cb & 1][tid] = found;
-  __syncthreads();
-  if (cb < ce) load_chunk(cb);
-  find(cb + 1);
+  if (cb < cm) {
+    load_ctx(cb);
+  } else if (cm < ce) {
+    find(cm);
+    if (tid < KC) s_at[cm & 1][tid] = found;
+    lds_barrier();
+    load_own(cm);
+    find(cm + 1);
+  }
 
   Row row[QT];
   V8<T> qf[QT][ND];
   int lo[QT], hi[QT];                              // the packed own rows that the row sees
-  int wlo[QT], whi[QT], alo[QT], ahi[QT];          // their union and intersection over the wave's tile
+  // of the wave's tile, uniform: bounds of what its rows see, and (empty where they belong to several lists) what every
+  // row sees.  lo does not fall from row to row, nor hi within a list; rows past q_len may see anything.
+  int wlo[QT], whi[QT], alo[QT], ahi[QT];
   float m_run[QT], l_run[QT];                      // maximum of q.k; l_run: this lane's keys only, until the end
   f32x4 o[QT][NB];
 #pragma unroll
@@ -277,10 +298,10 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
     row[i] = row_of(a, b, g, r0 + (wave * QT + i) * 16 + c16);
     lo[i] = s_off[row[i].k - k0];
     hi[i] = lo[i] + row[i].own;
-    wlo[i] = wave_min(row[i].own ? lo[i] : 0x7fffffff);
-    whi[i] = wave_max(hi[i] * (row[i].own != 0));
-    alo[i] = wave_max(lo[i]);
-    ahi[i] = wave_min(hi[i]);
+    wlo[i] = __builtin_amdgcn_readlane(lo[i], 0);
+    alo[i] = __builtin_amdgcn_readlane(lo[i], 15);
+    whi[i] = __builtin_amdgcn_readlane(s_off[row[i].k - k0 + 1], 15);
+    ahi[i] = wlo[i] == alo[i] ? __builtin_amdgcn_readlane(hi[i], 0) : -1;
     const T* Q = static_cast<const T*>(a.q) + row[i].at * a.q_ld + row[i].h * DH;
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
@@ -294,8 +315,7 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
   }
   const float sl2 = score_unit(a.scale);
 
-  // Scores and probabilities of tile i for the 32 keys x0 .. of a step (keys [l, h) of each row; `edge`: some are outside),
-  // with the running maximum and sum.  pb is the operand of the product with the values.
+  // Products q.k of tile i with the 32 keys of a step.
   auto scores = [&](int i, const V8<T> (&kf)[2][ND], float (&s)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -306,10 +326,9 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       for (int j = 0; j < 4; ++j) s[4 * x + j] = acc[j];
     }
   };
-  auto softmax = [&](int i, float (&s)[8], V8<T>& pb) __attribute__((always_inline)) {
-    float mx = s[0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[j]);
+  // Their probabilities against the running maximum, as the operand of the product with the values.
+  auto softmax = [&](int i, float (&s)[8]) __attribute__((always_inline)) {
+    const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     if (__any(mx > m_run[i])) {                    // else every row's factor is 1
       const float m_new = fmaxf(m_run[i], rows_max(mx));
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[i] - m_new) * sl2);
@@ -319,14 +338,9 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       for (int n = 0; n < NB; ++n) o[i][n] *= alpha;
     }
     const float ref = m_run[i] == -INFINITY ? 0.f : m_run[i] * sl2;   // a row without keys so far: exp2(-inf) = 0
-    float psum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -ref));
-      psum += e;
-      pb[j] = from_f32<T>(e);
-    }
-    l_run[i] += psum;
+    for (int j = 0; j < 8; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -ref));
+    l_run[i] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
   };
   auto load_keys = [&](const T* Ks, int kb, V8<T> (&kf)[2][ND]) __attribute__((always_inline)) {
 #pragma unroll
@@ -334,57 +348,79 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
 #pragma unroll
       for (int d = 0; d < ND; ++d) kf[x][d] = ld8(&Ks[(kb + 16 * x + c16) * KLD + d * 32 + g4 * 8]);
   };
-
-  const int tiles_here = clampi((a.R - r0 - wave * QT * 16 + 15) / 16, 0, QT);   // the wave's tiles that hold rows
-  int cur = 0;
-  for (int c = cb; c < ce; ++c, cur ^= NBUF - 1) {
-    T *Ks = Ks_[cur], *Vs = Vs_[cur];
-    if constexpr (NBUF == 1) lds_barrier();        // the previous chunk is no longer read
+  auto stage = [&](T* Ks, T* Vs) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
-      const int e = p * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      if ((c >= cctx || (c + 1) * KC > nctx) && gone >> p & 1) kreg[p] = vreg[p] = V8<T>{};
-      st8(&Ks[key * KLD + d0], kreg[p]);
-      st8(&Vs[key * VLD + d0], vreg[p]);
-      if (c >= cctx) {                             // uniform
-        if (!finite8(vreg[p])) s_odd[c & 1] = c;
-        if (hole >> p & 1) s_hole[c & 1][key] = s_holes[c & 1] = c;
-      }
+      st8(&Ks[(key0 + p * STEP) * KLD + d0], kreg[p]);
+      st8(&Vs[(key0 + p * STEP) * VLD + d0], vreg[p]);
     }
-    if (c + 1 >= cctx && tid < KC) s_at[(c + 1) & 1][tid] = found;
+  };
+
+  const bool idle = r0 + wave * QT * 16 >= a.R;    // no row in the wave's tiles
+  int cur = 0;
+  for (int c = cb; c < cm; ++c, cur ^= NBUF - 1) {
+    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    if constexpr (NBUF == 1) lds_barrier();        // the previous chunk is no longer read
+    if ((c + 1) * KC > nctx) {                     // uniform
+#pragma unroll
+      for (int p = 0; p < PER_T; ++p)
+        if (c * KC + key0 + p * STEP >= nctx) kreg[p] = vreg[p] = V8<T>{};
+    }
+    stage(Ks, Vs);
+    if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
+      find(cm);
+      if (tid < KC) s_at[cm & 1][tid] = found;
+    }
     lds_barrier();   // two buffers: also the end of every wave's reads of the one written next
-    if (c + 1 < ce) load_chunk(c + 1);
-    find(c + 2);
-    if (tiles_here == 0) continue;
-
-    if (c < cctx) {
-#pragma unroll
-      for (int kb = 0; kb < KC; kb += 32) {
-        const int left = nctx - c * KC - kb;       // keys of the step
-        if (left <= 0) break;                      // uniform
-        V8<T> kf[2][ND], pb[QT];
-        load_keys(Ks, kb, kf);
-#pragma unroll
-        for (int i = 0; i < QT; ++i) {
-          float s[8];
-          scores(i, kf, s);
-          if (left < 32) {                         // uniform
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (key_of(j, g4) >= left) s[j] = -INFINITY;
-          }
-          softmax(i, s, pb[i]);
-        }
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const V8<T> vf = ld_cols<VLD>(Vs, kb, n * 16, lane);
-#pragma unroll
-          for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[i], o[i][n]);
-        }
-      }
-      continue;
+    if (c + 1 < cm) {
+      load_ctx(c + 1);
+    } else if (cm < ce) {
+      load_own(cm);
+      find(cm + 1);
     }
+    if (idle) continue;
+#pragma unroll
+    for (int kb = 0; kb < KC; kb += 32) {
+      const int left = nctx - c * KC - kb;         // keys of the step
+      if (left <= 0) break;                        // uniform
+      V8<T> kf[2][ND], pb[QT];
+      load_keys(Ks, kb, kf);
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        float s[8];
+        scores(i, kf, s);
+        if (left < 32) {                           // uniform
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (key_of(j, g4) >= left) s[j] = -INFINITY;
+        }
+        softmax(i, s);
+        pb[i] = pack8<T>(s);
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const V8<T> vf = ld_cols<VLD>(Vs, kb, n * 16, lane);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[i], o[i][n]);
+      }
+    }
+  }
 
+  for (int c = cm; c < ce; ++c, cur ^= NBUF - 1) {
+    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    if constexpr (NBUF == 1) lds_barrier();
+#pragma unroll
+    for (int p = 0; p < PER_T; ++p) {
+      if (gone >> p & 1) kreg[p] = vreg[p] = V8<T>{};
+      if (!finite8(vreg[p])) s_odd[c & 1] = c;
+      if (hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
+    }
+    stage(Ks, Vs);
+    if (tid < KC) s_at[(c + 1) & 1][tid] = found;
+    lds_barrier();
+    if (c + 1 < ce) load_own(c + 1);
+    find(c + 2);
+    if (idle) continue;
     const bool odd = __builtin_amdgcn_readfirstlane(s_odd[c & 1]) == c;
     const bool holes = __builtin_amdgcn_readfirstlane(s_holes[c & 1]) == c;
 #pragma unroll 1
@@ -410,8 +446,8 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
           for (int j = 0; j < 8; ++j)
             if (s_hole[c & 1][kb + key_of(j, g4)] == c) s[j] = -INFINITY;
         }
-        V8<T> pb;
-        softmax(i, s, pb);
+        softmax(i, s);
+        const V8<T> pb = pack8<T>(s);
         if (!odd) {
 #pragma unroll
           for (int n = 0; n < NB; ++n) o[i][n] = mma(ld_cols<VLD>(Vs, kb, n * 16, lane), pb, o[i][n]);
@@ -427,10 +463,12 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
           e = __shfl(e, (key >> 2 & 3) * 16 + c16);
           if (x0 + key < lo[i] || x0 + key >= hi[i]) continue;
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
+          for (int n = 0; n < NB; ++n) {
+            __builtin_amdgcn_sched_barrier(0);     // few values in registers at a time
 #pragma unroll
             for (int q = 0; q < 4; ++q)
               o[i][n][q] = fmaf(e, to_f32(Vs[(kb + key) * VLD + n * 16 + g4 * 4 + q]), o[i][n][q]);
+          }
         }
       }
     }
