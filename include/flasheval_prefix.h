@@ -108,7 +108,7 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream);
  * multiple of n_kv_heads, strides too short or not multiples of 16 bytes, L not a multiple of page_rows, a
  * scale that is not finite, an unknown dtype, a workspace that is too small; FE_EUNSUPPORTED for dh outside
  * {32, 64, 128}, T or L above 4194304, B*K*S*n_heads, B*T or B*K*L above 1073741823, more than 16777215
- * workgroups of 64 rows or keys of one request and key head, or ctx_ld above 16777216.
+ * workgroups of 64 rows or keys of one request and key head, or ctx_ld above 8388608.
  */
 typedef struct {
   int32_t dtype;                        /* fe_dtype of q, keys, values and out */

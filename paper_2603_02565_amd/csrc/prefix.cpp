@@ -24,8 +24,8 @@ constexpr long long kInt32 = 0x7fffffffLL, kMaxGrid = (1 << 24) - 1;
 
 // A row stride of `ld` elements holds `width` and keeps rows 16-byte aligned.
 bool stride_ok(int ld, long long width, int dtype) { return ld >= width && ld % (dtype == FE_BF16 ? 8 : 4) == 0; }
-// ... and a chunk of 64 rows keeps its offsets in 32 bits.
-constexpr int kMaxStride = 1 << 24;
+// A chunk of 64 shared rows keeps its byte offsets in 32 bits.
+constexpr int kMaxStride = 1 << 23;
 
 fe_status check_sizes(const fe_prefix_args* a) {
   if (!a) return pfail(FE_EINVAL, "arguments are NULL");

@@ -31,6 +31,10 @@ FE_DEV f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
 }
 
 template <typename T> FE_DEV V8<T> ld8(const T* p) { return *reinterpret_cast<const V8<T>*>(p); }
+// ... at a byte offset from a uniform base
+template <typename T> FE_DEV V8<T> ld8_at(const T* base, unsigned at) {
+  return *reinterpret_cast<const V8<T>*>(reinterpret_cast<const char*>(base) + at);
+}
 template <typename T> FE_DEV void st8(T* p, V8<T> v) { *reinterpret_cast<V8<T>*>(p) = v; }
 FE_DEV void st4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
 FE_DEV void st4(bf16* p, f32x4 v) {
@@ -215,7 +219,8 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
   constexpr int KLD = DH + kPad<T>, VLD = DH + 2 * kPad<T>;
   constexpr int PER_T = KC * DH / 8 / NT, STEP = NT / (DH / 8);
   constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
-  static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0 && KC <= NT, "tile shape");
+  constexpr int NS = sizeof(T) * DH * QT > 256 ? 1 : 2;
+  static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % (32 * NS) == 0 && KC <= NT, "tile shape");
   __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * KLD];
   __shared__ __attribute__((aligned(16))) T Vs_[NBUF][KC * VLD];
   __shared__ int s_off[ROWS + 1];
@@ -246,15 +251,24 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
   // The loads are unconditional: rows that do not count read one that exists and are cleared when they are staged.
   V8<T> kreg[PER_T], vreg[PER_T];
   const int key0 = tid / (DH / 8), d0 = tid % (DH / 8) * 8;            // this thread's part of a chunk: keys key0 + p STEP
+  const unsigned ctx_at = (key0 * a.ctx_ld + d0) * sizeof(T), ctx_step = STEP * a.ctx_ld * sizeof(T);   // bytes
   auto load_ctx = [&](int c) __attribute__((always_inline)) {
     const long long base = ((long long)b * a.T + c * KC) * a.ctx_ld + g * DH;
     const T *kp = static_cast<const T*>(a.ctx_k) + base, *vp = static_cast<const T*>(a.ctx_v) + base;
-    const int last = min(nctx - c * KC, KC) - 1;
+    if ((c + 1) * KC <= nctx) {                    // uniform
+#pragma unroll
+      for (int p = 0; p < PER_T; ++p) {
+        kreg[p] = ld8_at(kp, ctx_at + p * ctx_step);
+        vreg[p] = ld8_at(vp, ctx_at + p * ctx_step);
+      }
+      return;
+    }
+    const int last = nctx - c * KC - 1;
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
-      const unsigned off = (unsigned)(min(key0 + p * STEP, last) * a.ctx_ld + d0);
-      kreg[p] = ld8(kp + off);
-      vreg[p] = ld8(vp + off);
+      const unsigned at = (min(key0 + p * STEP, last) * a.ctx_ld + d0) * sizeof(T);
+      kreg[p] = ld8_at(kp, at);
+      vreg[p] = ld8_at(vp, at);
     }
   };
   int gone = 0, hole = 0;                          // bit p: the key does not count; because its page is outside the pool
@@ -313,9 +327,9 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
 #pragma unroll
     for (int n = 0; n < NB; ++n) o[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float sl2 = score_unit(a.scale);
+  const float sl2 = score_unit(a.scale), lag = fminf(8.f / sl2, 1e30f);
 
-  // Products q.k of tile i with the 32 keys of a step.
+  // Products q.k of tile i with 32 keys.
   auto scores = [&](int i, const V8<T> (&kf)[2][ND], float (&s)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -326,21 +340,30 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       for (int j = 0; j < 4; ++j) s[4 * x + j] = acc[j];
     }
   };
-  // Their probabilities against the running maximum, as the operand of the product with the values.
-  auto softmax = [&](int i, float (&s)[8]) __attribute__((always_inline)) {
-    const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    if (__any(mx > m_run[i])) {                    // else every row's factor is 1
-      const float m_new = fmaxf(m_run[i], rows_max(mx));
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[i] - m_new) * sl2);
-      m_run[i] = m_new;
+  auto max8 = [&](const float (&s)[8]) __attribute__((always_inline)) {
+    return fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+  };
+  // Moves the reference of tile i's rows to mx (this lane's largest product) where that is more than `lag` above it.  The reference is the running
+  // maximum, but it follows only once a score is 8 / log2(e) above it (a probability is then at most 2^8, of no
+  // consequence to fp32 sums or to bf16's relative rounding): with the exact maximum some row of a tile moves in most steps.
+  // Whether a row's reference moves depends on that row alone.
+  auto follow = [&](int i, float mx) __attribute__((always_inline)) {
+    const float top = rows_max(mx);
+    if (top > m_run[i] + lag) {
+      const float alpha = __builtin_amdgcn_exp2f((m_run[i] - top) * sl2);
+      m_run[i] = top;
       l_run[i] *= alpha;
 #pragma unroll
       for (int n = 0; n < NB; ++n) o[i][n] *= alpha;
     }
+  };
+  // Probabilities against the reference, added to the sum, as the operand of the product with the values.
+  auto probs = [&](int i, float (&s)[8]) __attribute__((always_inline)) {
     const float ref = m_run[i] == -INFINITY ? 0.f : m_run[i] * sl2;   // a row without keys so far: exp2(-inf) = 0
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -ref));
     l_run[i] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+    return pack8<T>(s);
   };
   auto load_keys = [&](const T* Ks, int kb, V8<T> (&kf)[2][ND]) __attribute__((always_inline)) {
 #pragma unroll
@@ -379,30 +402,56 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       find(cm + 1);
     }
     if (idle) continue;
+    // Steps of NS 32-key blocks: the products of every tile and block first, one branch for the references, then the
+    // probabilities and the products with the values, so that the tiles' and blocks' chains overlap.
 #pragma unroll
-    for (int kb = 0; kb < KC; kb += 32) {
+    for (int kb = 0; kb < KC; kb += 32 * NS) {
       const int left = nctx - c * KC - kb;         // keys of the step
       if (left <= 0) break;                        // uniform
-      V8<T> kf[2][ND], pb[QT];
-      load_keys(Ks, kb, kf);
+      float s[NS][QT][8];
 #pragma unroll
-      for (int i = 0; i < QT; ++i) {
-        float s[8];
-        scores(i, kf, s);
-        if (left < 32) {                           // uniform
+      for (int u = 0; u < NS; ++u) {
+        V8<T> kf[2][ND];
+        load_keys(Ks, kb + 32 * u, kf);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) scores(i, kf, s[u][i]);
+      }
+      if (left < 32 * NS) {                        // uniform
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (key_of(j, g4) >= left) s[j] = -INFINITY;
+            if (32 * u + key_of(j, g4) >= left) {
+#pragma unroll
+              for (int i = 0; i < QT; ++i) s[u][i][j] = -INFINITY;
+            }
+      }
+      float mx[QT];
+      bool move = false;
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        mx[i] = max8(s[0][i]);
+#pragma unroll
+        for (int u = 1; u < NS; ++u) mx[i] = fmaxf(mx[i], max8(s[u][i]));
+        move |= mx[i] > m_run[i] + lag;
+      }
+      if (__any(move)) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i) follow(i, mx[i]);
+      }
+      V8<T> pb[NS][QT];
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int i = 0; i < QT; ++i) pb[u][i] = probs(i, s[u][i]);
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const V8<T> vf = ld_cols<VLD>(Vs, kb + 32 * u, n * 16, lane);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[u][i], o[i][n]);
         }
-        softmax(i, s);
-        pb[i] = pack8<T>(s);
-      }
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const V8<T> vf = ld_cols<VLD>(Vs, kb, n * 16, lane);
-#pragma unroll
-        for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[i], o[i][n]);
-      }
     }
   }
 
@@ -446,8 +495,9 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
           for (int j = 0; j < 8; ++j)
             if (s_hole[c & 1][kb + key_of(j, g4)] == c) s[j] = -INFINITY;
         }
-        softmax(i, s);
-        const V8<T> pb = pack8<T>(s);
+        const float mx = max8(s);
+        if (__any(mx > m_run[i] + lag)) follow(i, mx);
+        const V8<T> pb = probs(i, s);
         if (!odd) {
 #pragma unroll
           for (int n = 0; n < NB; ++n) o[i][n] = mma(ld_cols<VLD>(Vs, kb, n * 16, lane), pb, o[i][n]);
@@ -1007,14 +1057,19 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
 PrefixPlan prefix_plan(const fe_prefix_args& a) {
   PrefixPlan p;
   const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
-  // 128 rows a workgroup share the staged keys where that leaves two workgroups per compute unit
-  p.rows = bg * ((R + 127) / 128) >= 512 ? 128 : 64;
+  // 128 rows a workgroup read a chunk's keys from memory and from LDS half as often, for half the waves and, in fp32 at head
+  // width 128, more registers than there are.  They pay where 64 rows would read every key twice and 128 read it once
+  // (4 x 128 rows of 32768 keys: 236 us -> 175), and over long contexts with workgroups to spare (64 x 1024 rows: of 4096
+  // keys 126 -> 112, of 1024 keys 38.2 -> 39.0; 256 x 550 rows of 256 keys 29.6 -> 33.9).
+  const bool fits = a.dtype == FE_BF16 || a.dh <= 64;
+  p.rows = fits && ((R > 64 && R <= 128) || (a.T >= 2048 && bg * ((R + 127) / 128) >= 512)) ? 128 : 64;
   p.tiles = (int)((R + p.rows - 1) / p.rows);
-  // split the keys while the launch has fewer than four workgroups per compute unit and a range keeps two chunks
-  const long long wgs = bg * p.tiles;
+  // Key ranges: up to two workgroups per compute unit, at least three chunks each (a range costs its partial sums and all
+  // of them a second launch).  64 tiles of 24 chunks: one range 28.6 us at two, 23.0 at four, 19.5 at eight, 20.5 at
+  // sixteen; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.
   const long long lists = std::min<long long>(a.K, (p.rows - 1) / (a.S * G) + 2);
   const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
-  p.splits = (int)std::max(1LL, std::min({1024 / std::max(1LL, wgs), chunks / 2, 64LL}));
+  p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 3, 64LL}));
   const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads;
   p.part_bytes = p.splits > 1 ? p.splits * rows * (a.dh + 2) * sizeof(float) : 0;
   return p;

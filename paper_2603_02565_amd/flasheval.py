@@ -148,7 +148,7 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 # ---------------------------------------------------------------------------------------------
@@ -565,11 +565,40 @@ def _row_stride(t, name: str, shape: Tuple[int, ...], dtype) -> int:
     return ld
 
 
-def _on_device(tensors) -> None:
+class _Layouts:
+    """The layout checks of one object's tensors, remembered by name, shape, strides and type: a serving loop
+    passes the same layouts again and again."""
+
+    def __init__(self):
+        self.known = {}
+
+    def rows(self, t, name: str, shape: Tuple[int, ...], dtype) -> int:
+        key = (name, t.shape, t.stride(), t.dtype)
+        ld = self.known.get(key)
+        if ld is None:
+            ld = self.known[key] = _row_stride(t, name, shape, dtype)
+        return ld
+
+    def vector(self, t, name: str, dtype, numel: int) -> Optional[int]:
+        """Address of a contiguous vector of numel elements (None stays None)."""
+        if t is None:
+            return None
+        key = (name, t.shape, t.stride(), t.dtype)
+        if key not in self.known:
+            _need(t, name, dtype, numel)
+            self.known[key] = numel
+        return t.data_ptr()
+
+
+def _here() -> int:
+    """Index of the current HIP device, -1 without one."""
     import torch
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    return torch.cuda.current_device() if torch.cuda.is_available() else -1
+
+
+def _on_device(tensors, index: int) -> None:
     for t in tensors:
-        if t is not None and (here is None or not t.is_cuda or t.device.index != here):
+        if t is not None and (t.get_device() != index or index < 0):
             raise ValueError(f"every tensor must be on the current HIP device, got one on {t.device}")
 
 
@@ -598,7 +627,14 @@ class PagedCache:
         _need(self.len, "length", torch.int32, self.N)
         self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
         self.status = torch.zeros(self.N, dtype=torch.int32, device=table.device)
-        _on_device((k_pages, v_pages, table, self.len))
+        _on_device((k_pages, v_pages, table, self.len), _here())
+        a = self.args = fe_append_args()
+        a.dtype = FE_BF16 if k_pages.dtype == torch.bfloat16 else FE_F32
+        a.n_pages, a.page_rows, a.n_kv_heads, a.dh = shape
+        a.N, a.table_cols, a.page_ld = self.N, self.cols, self.page_ld
+        a.k_pages, a.v_pages, a.table = _ptr(k_pages), _ptr(v_pages), _ptr(table)
+        a.len, a.status = _ptr(self.len), _ptr(self.status)
+        self._layouts = _Layouts()
 
     def append(self, k, v, q=None, q_out=None, new_len=None, pos0=None, freq=None, neighbours=False, len_out=None,
                stream=None):
@@ -607,36 +643,37 @@ class PagedCache:
         tensor; it is returned.  The lengths advance in place, or into len_out when that is given.
         `status` [N] holds FE_DEV_BAD_PAGE for a sequence with a row that found no page."""
         import torch
-        pages, P, hkv, dh = self.k_pages.shape
-        dt = self.k_pages.dtype
+        a, lay, dt, N = self.args, self._layouts, self.k_pages.dtype, self.N
+        hkv, dh = self.k_pages.shape[2:]
         if k.dim() != 4:
             raise ValueError(f"k: expected [sequences][rows][heads][dh], got {tuple(k.shape)}")
-        S = k.shape[1]
-        a = fe_append_args()
-        a.dtype, a.N, a.S = FE_BF16 if dt == torch.bfloat16 else FE_F32, self.N, S
-        a.n_kv_heads, a.dh, a.page_rows, a.n_pages, a.table_cols, a.page_ld = hkv, dh, P, pages, self.cols, self.page_ld
-        a.k_ld = _row_stride(k, "k", (self.N, S, hkv, dh), dt)
-        a.v_ld = _row_stride(v, "v", (self.N, S, hkv, dh), dt)
+        S = a.S = k.shape[1]
+        a.k_ld = lay.rows(k, "k", (N, S, hkv, dh), dt)
+        a.v_ld = lay.rows(v, "v", (N, S, hkv, dh), dt)
+        if v.shape != k.shape:
+            raise ValueError(f"v: expected {tuple(k.shape)}, got {tuple(v.shape)}")
         if q is not None:
             if q.dim() != 4:
                 raise ValueError(f"q: expected [sequences][rows][heads][dh], got {tuple(q.shape)}")
             a.n_heads = q.shape[2]
-            a.q_ld = _row_stride(q, "q", (self.N, S, a.n_heads, dh), dt)
+            a.q_ld = lay.rows(q, "q", (N, S, q.shape[2], dh), dt)
             if q_out is None:
-                q_out = torch.empty((self.N, S, a.n_heads, dh), dtype=dt, device=q.device)
-            a.q_out_ld = _row_stride(q_out, "q_out", (self.N, S, a.n_heads, dh), dt)
+                q_out = torch.empty(q.shape, dtype=dt, device=q.device)
+            if q_out.shape != q.shape or q.shape[1] != S:
+                raise ValueError(f"q, q_out: expected {S} rows and one shape, got {tuple(q.shape)} and {tuple(q_out.shape)}")
+            a.q_out_ld = lay.rows(q_out, "q_out", (N, S, q.shape[2], dh), dt)
+            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise ValueError("q_out without q")
-        if freq is not None:
-            a.rot, a.neighbours = 2 * freq.numel(), 1 if neighbours else 0
-            _need(freq, "freq", torch.float64, freq.numel())
-        length = self.len if len_out is None else len_out
-        for t, name in ((length, "len_out"), (new_len, "new_len"), (pos0, "pos0")):
-            _need(t, name, torch.int32, self.N)
-        _on_device((k, v, q, q_out, freq, length, new_len, pos0))
-        a.q, a.k, a.v, a.q_out, a.freq, a.table = _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(freq), _ptr(self.table)
-        a.len, a.new_len, a.pos0, a.len_out = _ptr(self.len), _ptr(new_len), _ptr(pos0), _ptr(length)
-        a.k_pages, a.v_pages, a.status = _ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.status)
+        else:
+            a.q = a.q_out = None
+        a.rot, a.neighbours = 0 if freq is None else 2 * freq.numel(), 1 if neighbours else 0
+        a.freq = None if freq is None else lay.vector(freq, "freq", torch.float64, freq.numel())
+        a.new_len = lay.vector(new_len, "new_len", torch.int32, N)
+        a.pos0 = lay.vector(pos0, "pos0", torch.int32, N)
+        a.len_out = a.len if len_out is None else lay.vector(len_out, "len_out", torch.int32, N)
+        _on_device((self.k_pages, k, v, q, q_out, freq, len_out, new_len, pos0), _here())
+        a.k, a.v = k.data_ptr(), v.data_ptr()
         fe_cache_append(a, stream)
         return q_out
 
@@ -665,6 +702,9 @@ class PrefixAttention:
             self.ws_bytes = max(self.ws_bytes, fe_prefix_workspace_size(a, True))
         self.out = None
         self.grads = None
+        self.q_shape, self.ctx_shape = (B, K, S, n_heads, dh), (B, T, n_kv_heads, dh)
+        self.own_shape = (n_pages, page_rows, n_kv_heads, dh) if page_rows else (B, K, L, n_kv_heads, dh)
+        self._layouts = _Layouts()
 
     def allocate(self):
         """Outputs and workspace on the current device (done by the first `run`)."""
@@ -684,33 +724,26 @@ class PrefixAttention:
 
     def _take(self, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len):
         import torch
-        a = self.args
-        ctx = (a.B, a.T, a.n_kv_heads, a.dh)
-        own = (a.n_pages, a.page_rows) if a.page_rows else (a.B, a.K, a.L)
-        own += (a.n_kv_heads, a.dh)
-        a.q_ld = _row_stride(q, "q", (a.B, a.K, a.S, a.n_heads, a.dh), self.act)
+        a, lay, act, i32 = self.args, self._layouts, self.act, torch.int32
+        a.q_ld = lay.rows(q, "q", self.q_shape, act)
         if a.T:
-            a.ctx_ld = _row_stride(ctx_k, "ctx_k", ctx, self.act)
-            if _row_stride(ctx_v, "ctx_v", ctx, self.act) != a.ctx_ld:
+            a.ctx_ld = lay.rows(ctx_k, "ctx_k", self.ctx_shape, act)
+            if lay.rows(ctx_v, "ctx_v", self.ctx_shape, act) != a.ctx_ld:
                 raise ValueError("ctx_k and ctx_v must have the same row stride")
         if a.L:
-            a.own_ld = _row_stride(own_k, "own_k", own, self.act)
-            if _row_stride(own_v, "own_v", own, self.act) != a.own_ld:
+            a.own_ld = lay.rows(own_k, "own_k", self.own_shape, act)
+            if lay.rows(own_v, "own_v", self.own_shape, act) != a.own_ld:
                 raise ValueError("own_k and own_v must have the same row stride")
-        if a.page_rows:
-            if table is None:
-                raise ValueError("paged own rows need a table")
-            _need(table, "table", torch.int32, a.B * a.K * (a.L // a.page_rows))
-        elif table is not None:
-            raise ValueError("a table needs page_rows > 0")
-        _need(ctx_len, "ctx_len", torch.int32, a.B)
-        _need(q_len, "q_len", torch.int32, a.B * a.K)
-        _need(own_len, "own_len", torch.int32, a.B * a.K)
-        _on_device((q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len, self.out))
+        if (table is None) != (a.page_rows == 0):
+            raise ValueError("a table and page_rows > 0 go together")
+        a.table = None if table is None else lay.vector(table, "table", i32, a.B * a.K * (a.L // a.page_rows))
+        a.ctx_len = lay.vector(ctx_len, "ctx_len", i32, a.B)
+        a.q_len = lay.vector(q_len, "q_len", i32, a.B * a.K)
+        a.own_len = lay.vector(own_len, "own_len", i32, a.B * a.K)
+        _on_device((q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len, self.out), _here())
         if self.out is None:
             self.allocate()
-        a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = _ptr(q), _ptr(ctx_k), _ptr(ctx_v), _ptr(own_k), _ptr(own_v)
-        a.table, a.ctx_len, a.own_len, a.q_len = _ptr(table), _ptr(ctx_len), _ptr(own_len), _ptr(q_len)
+        a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = (None if t is None else t.data_ptr() for t in (q, ctx_k, ctx_v, own_k, own_v))
 
     def run(self, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
         """Enqueue the attention; returns out [B][K][S][n_heads][dh] (self.lse holds the log sums when training)."""
@@ -726,8 +759,8 @@ class PrefixAttention:
             raise ValueError("grad follows run")
         self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
         a, g = self.args, fe_prefix_grads()
-        g.dout_ld = _row_stride(dout, "dout", (a.B, a.K, a.S, a.n_heads, a.dh), self.act)
-        _on_device((dout,))
+        g.dout_ld = self._layouts.rows(dout, "dout", self.q_shape, self.act)
+        _on_device((dout,), _here())
         g.dout = _ptr(dout)
         g.dq_ld, g.dctx_ld, g.down_ld = a.n_heads * a.dh, a.n_kv_heads * a.dh, a.n_kv_heads * a.dh
         g.dq, g.dctx_k, g.dctx_v, g.down_k, g.down_v = (_ptr(t) for t in self.grads)
