@@ -37,7 +37,7 @@ struct PrefixPlan { int rows, tiles, splits; size_t part_bytes; };
 PrefixPlan prefix_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixPlan& p, hipStream_t s);
 // The same of a gradient call: dq's row tiles and key ranges, dk's and dv's key tiles and row ranges, scratch bytes.
-struct PrefixGradPlan { int rows, tiles, splits, ctx_tiles, own_tiles, row_splits; size_t rows_bytes, dq_bytes, dkv_bytes; };
+struct PrefixGradPlan { int tiles, splits, ctx_tiles, own_tiles, row_splits; size_t rows_bytes, dq_bytes, dkv_bytes; };
 PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_grad(const PrefixGradArgs& a, int dh, bool bf16_rows, const PrefixGradPlan& p, hipStream_t s);
 hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s);

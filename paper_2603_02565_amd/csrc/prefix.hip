@@ -43,8 +43,6 @@ FE_DEV void st4(bf16* p, f32x4 v) {
   for (int q = 0; q < 4; ++q) w[q] = (bf16)v[q];
   *reinterpret_cast<bf16x4*>(p) = w;
 }
-// LDS row padding: 16 bytes
-template <typename T> constexpr int kPad = 16 / sizeof(T);
 
 // Eight floats rounded to T (round to nearest even).
 template <typename T> FE_DEV V8<T> pack8(const float (&s)[8]);
@@ -181,31 +179,58 @@ FE_DEV Row row_of(const PrefixArgs& a, int b, int g, int r) {
   return w;
 }
 
-// Operand of a product whose summed axis runs over LDS rows base .. base + 31 and whose other axis is column col + l % 16
-// (what a transposed copy would give, without one).  Element 4 x + j of lane l is row base + 16 x + 4 (l / 16) + j, the
-// order in which a lane holds the results of two 16-row products.  bf16: each group of 16 lanes reads a 4 x 16 block
-// transposed (ds_read_b64_tr_b16); row strides of 8 words modulo 16 keep the half-waves free of bank conflicts.
-template <int LD>
-FE_DEV bf16x8 ld_cols(const bf16* X, int base, int col, int lane) {
-  typedef short s16x4 __attribute__((ext_vector_type(4)));
-  typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-  bf16* p = const_cast<bf16*>(X) + (base + 4 * (lane >> 4) + ((lane & 15) >> 2)) * LD + col + (lane & 3) * 4;
-  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 16 * LD));
-  const bf16x4 u = __builtin_bit_cast(bf16x4, a), v = __builtin_bit_cast(bf16x4, b);
-  return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-template <int LD>
-FE_DEV f32x8 ld_cols(const float* X, int base, int col, int lane) {
-  const float* p = X + (base + 4 * (lane >> 4)) * LD + col + (lane & 15);
-  f32x8 v;
+// A tile of rows of DH elements in LDS, read as an operand along its rows (summed over columns) and along its columns (summed
+// over rows).  bf16: rows of DH without padding, their 16-byte units exchanged inside a row, so that 16 rows at one unit and
+// 8 rows at one pair of units both fall on all 64 banks; fp32: rows of DH + 4.
+//
+// Both reads start from a number that depends on the lane alone (row_lane, col_lane); what differs from read to read is a
+// constant xor and a row offset.
+template <typename T, int DH> struct Tile;
+template <int DH> struct Tile<bf16, DH> {
+  static constexpr int LD = DH, UNITS = DH / 8, PER = 128 / DH;        // PER rows span the banks; the exchange repeats every 16 rows
+  static FE_DEV int swap(int row) {
+    const int h = row / PER % UNITS;
+    return (h % (UNITS / 2)) << 1 | h / (UNITS / 2);
+  }
+  static FE_DEV int at(int row, int unit) { return row * DH + ((unit ^ swap(row)) << 3); }
+  // Operand along rows: lane l is row base + l % 16, its elements are columns 32 d + 8 (l / 16) + j (base a multiple of 16).
+  static FE_DEV int row_lane(int lane) { return at(lane & 15, lane >> 4); }
+  static FE_DEV bf16x8 rows(const bf16* X, int base, int d, int row_lane) { return ld8(X + base * DH + (row_lane ^ (d << 5))); }
+  // Operand along columns: lane l is column 16 n + l % 16; its elements 4 x + j are rows base + 16 x + 4 (l / 16) + j, the
+  // order in which a lane holds the results of two 16-row products.  Each group of 16 lanes reads a 4 x 16 block
+  // transposed (ds_read_b64_tr_b16).
+  static FE_DEV int col_lane(int lane) { return at(4 * (lane >> 4) + ((lane & 15) >> 2), (lane & 3) >> 1) + (lane & 1) * 4; }
+  static FE_DEV bf16x8 cols(const bf16* X, int base, int n, int col_lane) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    bf16* p = const_cast<bf16*>(X) + base * DH + (col_lane ^ (n << 4));
+    const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 16 * DH));
+    return __builtin_shufflevector(__builtin_bit_cast(bf16x4, u), __builtin_bit_cast(bf16x4, v), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
+template <int DH> struct Tile<float, DH> {
+  static constexpr int LD = DH + 4;
+  static FE_DEV int at(int row, int unit) { return row * LD + unit * 8; }
+  static FE_DEV int row_lane(int lane) { return at(lane & 15, lane >> 4); }
+  static FE_DEV f32x8 rows(const float* X, int base, int d, int row_lane) { return ld8(X + base * LD + row_lane + d * 32); }
+  static FE_DEV int col_lane(int lane) { return 4 * (lane >> 4) * LD + (lane & 15); }
+  static FE_DEV f32x8 cols(const float* X, int base, int n, int col_lane) {
+    const float* p = X + base * LD + col_lane + n * 16;
+    f32x8 v;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = p[(16 * (j >> 2) + (j & 3)) * LD];
-  return v;
+    for (int j = 0; j < 8; ++j) v[j] = p[(16 * (j >> 2) + (j & 3)) * LD];
+    return v;
+  }
+};
+// Keeps a lane's number in one register, instead of a register for every xor of it that a loop uses.
+FE_DEV int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
-// Waves per SIMD that the register file is shared between (more hide more latency; these leave no spills).
-constexpr int fwd_waves(int bytes, int w) { return bytes == 2 && w <= 64 ? 4 : w <= 64 || (bytes == 2 && w <= 128) ? 3 : 2; }
+// Waves per SIMD that the register file is shared between (more hide more latency; fewer would spill).
+constexpr int waves_of(int bytes, int dh, int qt) { return dh == 128 ? 2 : bytes == 2 && dh * qt <= 64 ? 4 : dh * qt <= 64 || bytes == 2 ? 3 : 2; }
 
 // ------------------------------------------------------------------------------------------
 // Forward.  NW waves of QT 16-row tiles; chunks of KC keys staged through registers (the next chunk's loads in
@@ -214,15 +239,14 @@ constexpr int fwd_waves(int bytes, int w) { return bytes == 2 && w <= 64 ? 4 : w
 // registers.
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int QT, int NW, int KC>
-__global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_prefix_fwd(PrefixArgs a) {
+__global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_fwd(PrefixArgs a) {
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
-  constexpr int KLD = DH + kPad<T>, VLD = DH + 2 * kPad<T>;
+  typedef Tile<T, DH> L;
   constexpr int PER_T = KC * DH / 8 / NT, STEP = NT / (DH / 8);
   constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
   constexpr int NS = sizeof(T) * DH * QT > 256 ? 1 : 2;
   static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % (32 * NS) == 0 && KC <= NT, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * KLD];
-  __shared__ __attribute__((aligned(16))) T Vs_[NBUF][KC * VLD];
+  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * L::LD], Vs_[NBUF][KC * L::LD];
   __shared__ int s_off[ROWS + 1];
   // by chunk parity: the last chunk whose values are not all finite, the last chunk with keys of pages outside the
   // pool, and those keys; rows of the next own chunks
@@ -329,15 +353,23 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
   }
   const float sl2 = score_unit(a.scale), lag = fminf(8.f / sl2, 1e30f);
 
-  // Products q.k of tile i with 32 keys.
-  auto scores = [&](int i, const V8<T> (&kf)[2][ND], float (&s)[8]) __attribute__((always_inline)) {
+  // Products q.k of tiles [i0, i1) with 32 keys.
+  auto scores = [&](const T* Ks, int kb, int rl, int i0, int i1, float (&s)[QT][8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      f32x4 acc[QT];
 #pragma unroll
-      for (int d = 0; d < ND; ++d) acc = mma(kf[x][d], qf[i][d], acc);
+      for (int i = 0; i < QT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[4 * x + j] = acc[j];
+      for (int d = 0; d < ND; ++d) {
+        const V8<T> kf = L::rows(Ks, kb + 16 * x, d, rl);
+#pragma unroll
+        for (int i = i0; i < i1; ++i) acc[i] = mma(kf, qf[i][d], acc[i]);
+      }
+#pragma unroll
+      for (int i = i0; i < i1; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][4 * x + j] = acc[i][j];
     }
   };
   auto max8 = [&](const float (&s)[8]) __attribute__((always_inline)) {
@@ -365,21 +397,16 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
     l_run[i] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
     return pack8<T>(s);
   };
-  auto load_keys = [&](const T* Ks, int kb, V8<T> (&kf)[2][ND]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int d = 0; d < ND; ++d) kf[x][d] = ld8(&Ks[(kb + 16 * x + c16) * KLD + d * 32 + g4 * 8]);
-  };
   auto stage = [&](T* Ks, T* Vs) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
-      st8(&Ks[(key0 + p * STEP) * KLD + d0], kreg[p]);
-      st8(&Vs[(key0 + p * STEP) * VLD + d0], vreg[p]);
+      st8(&Ks[L::at(key0 + p * STEP, d0 / 8)], kreg[p]);
+      st8(&Vs[L::at(key0 + p * STEP, d0 / 8)], vreg[p]);
     }
   };
 
   const bool idle = r0 + wave * QT * 16 >= a.R;    // no row in the wave's tiles
+  int rl = L::row_lane(lane), cl = L::col_lane(lane);
   int cur = 0;
   for (int c = cb; c < cm; ++c, cur ^= NBUF - 1) {
     T *Ks = Ks_[cur], *Vs = Vs_[cur];
@@ -402,6 +429,8 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       find(cm + 1);
     }
     if (idle) continue;
+    rl = fresh(rl);
+    cl = fresh(cl);
     // Steps of NS 32-key blocks: the products of every tile and block first, one branch for the references, then the
     // probabilities and the products with the values, so that the tiles' and blocks' chains overlap.
 #pragma unroll
@@ -410,12 +439,7 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       if (left <= 0) break;                        // uniform
       float s[NS][QT][8];
 #pragma unroll
-      for (int u = 0; u < NS; ++u) {
-        V8<T> kf[2][ND];
-        load_keys(Ks, kb + 32 * u, kf);
-#pragma unroll
-        for (int i = 0; i < QT; ++i) scores(i, kf, s[u][i]);
-      }
+      for (int u = 0; u < NS; ++u) scores(Ks, kb + 32 * u, rl, 0, QT, s[u]);
       if (left < 32 * NS) {                        // uniform
 #pragma unroll
         for (int u = 0; u < NS; ++u)
@@ -448,7 +472,7 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
       for (int u = 0; u < NS; ++u)
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          const V8<T> vf = ld_cols<VLD>(Vs, kb + 32 * u, n * 16, lane);
+          const V8<T> vf = L::cols(Vs, kb + 32 * u, n, cl);
 #pragma unroll
           for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[u][i], o[i][n]);
         }
@@ -470,19 +494,20 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
     if (c + 1 < ce) load_own(c + 1);
     find(c + 2);
     if (idle) continue;
+    rl = fresh(rl);
+    cl = fresh(cl);
     const bool odd = __builtin_amdgcn_readfirstlane(s_odd[c & 1]) == c;
     const bool holes = __builtin_amdgcn_readfirstlane(s_holes[c & 1]) == c;
 #pragma unroll 1
     for (int kb = 0; kb < KC; kb += 32) {
       const int x0 = (c - cctx) * KC + kb;
       if (x0 >= nown) break;                       // uniform
-      V8<T> kf[2][ND];
-      load_keys(Ks, kb, kf);
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
         if (x0 >= whi[i] || x0 + 32 <= wlo[i]) continue;   // uniform: no row of the tile sees a key of the step
-        float s[8];
-        scores(i, kf, s);
+        float all[QT][8];
+        scores(Ks, kb, rl, i, i + 1, all);
+        float (&s)[8] = all[i];
         if (x0 < alo[i] || x0 + 32 > ahi[i]) {     // uniform
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -500,7 +525,7 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
         const V8<T> pb = probs(i, s);
         if (!odd) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) o[i][n] = mma(ld_cols<VLD>(Vs, kb, n * 16, lane), pb, o[i][n]);
+          for (int n = 0; n < NB; ++n) o[i][n] = mma(L::cols(Vs, kb, n, cl), pb, o[i][n]);
           continue;
         }
         // A value of the chunk is not finite: in a product it would reach the rows that do not see its key, as 0
@@ -517,7 +542,7 @@ __global__ __launch_bounds__(NW * 64, fwd_waves(sizeof(T), DH * QT)) void k_pref
             __builtin_amdgcn_sched_barrier(0);     // few values in registers at a time
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              o[i][n][q] = fmaf(e, to_f32(Vs[(kb + key) * VLD + n * 16 + g4 * 4 + q]), o[i][n][q]);
+              o[i][n][q] = fmaf(e, to_f32(Vs[L::at(kb + key, n * 2 + (g4 >> 1)) + (g4 & 1) * 4 + q]), o[i][n][q]);
           }
         }
       }
@@ -623,15 +648,14 @@ __global__ __launch_bounds__(256) void k_prefix_rows(PrefixGradArgs p) {
 
 // dq: rows and chunks as in the forward, probabilities again from lse.
 template <typename T, int DH, int QT, int NW, int KC>
-__global__ __launch_bounds__(NW * 64, 2) void k_prefix_dq(PrefixGradArgs p) {
+__global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
-  constexpr int KLD = DH + 2 * kPad<T>, VLD = DH + kPad<T>;
-  constexpr int PER_T = KC * DH / 8 / NT;
+  typedef Tile<T, DH> L;
+  constexpr int PER_T = KC * DH / 8 / NT, STEP = NT / (DH / 8);
   constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
   static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * KLD];
-  __shared__ __attribute__((aligned(16))) T Vs_[NBUF][KC * VLD];
+  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * L::LD], Vs_[NBUF][KC * L::LD];
   __shared__ int s_off[ROWS + 1];
   __shared__ long long s_at[2][KC];
 
@@ -649,44 +673,58 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dq(PrefixGradArgs p) {
   const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_off[nb]);
   const int cctx = (nctx + KC - 1) / KC, chunks = cctx + (nown + KC - 1) / KC;
   const int cb = (int)((long long)chunks * z / a.splits), ce = (int)((long long)chunks * (z + 1) / a.splits);
+  const int cm = min(max(cctx, cb), ce);
 
   V8<T> kreg[PER_T], vreg[PER_T];
+  const int key0 = tid / (DH / 8), d0 = tid % (DH / 8) * 8;
+  const unsigned ctx_at = (key0 * a.ctx_ld + d0) * sizeof(T), ctx_step = STEP * a.ctx_ld * sizeof(T);   // bytes
+  auto load_ctx = [&](int c) __attribute__((always_inline)) {
+    const long long base = ((long long)b * a.T + c * KC) * a.ctx_ld + g * DH;
+    const T *kp = static_cast<const T*>(a.ctx_k) + base, *vp = static_cast<const T*>(a.ctx_v) + base;
+    if ((c + 1) * KC <= nctx) {                    // uniform
+#pragma unroll
+      for (int q = 0; q < PER_T; ++q) {
+        kreg[q] = ld8_at(kp, ctx_at + q * ctx_step);
+        vreg[q] = ld8_at(vp, ctx_at + q * ctx_step);
+      }
+      return;
+    }
+    const int last = nctx - c * KC - 1;
+#pragma unroll
+    for (int q = 0; q < PER_T; ++q) {
+      const unsigned at = (min(key0 + q * STEP, last) * a.ctx_ld + d0) * sizeof(T);
+      kreg[q] = ld8_at(kp, at);
+      vreg[q] = ld8_at(vp, at);
+    }
+  };
   int gone = 0;
-  // The loads are unconditional (rows that do not count read one that exists); `gone` says what to leave out.
-  auto load_chunk = [&](int c) __attribute__((always_inline)) {
-    const bool shared = c < cctx;                  // uniform
-    const int left = shared ? nctx - c * KC : KC, ld = shared ? a.ctx_ld : a.own_ld;
-    const long long base = (long long)b * a.T + c * KC;
-    const T *kb = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + g * DH;
-    const T *vb = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + g * DH;
+  auto load_own = [&](int c) __attribute__((always_inline)) {
+    const T *kp = static_cast<const T*>(a.own_k) + g * DH + d0, *vp = static_cast<const T*>(a.own_v) + g * DH + d0;
     gone = 0;
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
-      const int e = q * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      long long x = base + min(key, left - 1);
-      if (!shared) {
-        x = s_at[c & 1][key];
-        gone |= (x < 0) << q;
-        x = max(x, 0LL);
-      } else {
-        gone |= (key >= left) << q;
-      }
-      kreg[q] = ld8(kb + x * ld + d0);
-      vreg[q] = ld8(vb + x * ld + d0);
+      const long long x = s_at[c & 1][key0 + q * STEP], at = max(x, 0LL) * a.own_ld;
+      gone |= (x < 0) << q;
+      kreg[q] = ld8(kp + at);
+      vreg[q] = ld8(vp + at);
     }
   };
   long long found = -2;
   auto find = [&](int c) __attribute__((always_inline)) {
-    if (c >= cctx && c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+    if (c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
   };
-  find(cb);
-  if (tid < KC) s_at[cb & 1][tid] = found;
-  __syncthreads();
-  if (cb < ce) load_chunk(cb);
-  find(cb + 1);
+  if (cb < cm) {
+    load_ctx(cb);
+  } else if (cm < ce) {
+    find(cm);
+    if (tid < KC) s_at[cm & 1][tid] = found;
+    lds_barrier();
+    load_own(cm);
+    find(cm + 1);
+  }
 
   V8<T> qf[QT][ND], df[QT][ND];
-  int lo[QT], hi[QT], wlo[QT], whi[QT], alo[QT], ahi[QT];
+  int lo[QT], hi[QT], wlo[QT], whi[QT], alo[QT], ahi[QT];              // as in the forward
   float lse2[QT], delta[QT];
   f32x4 o[QT][NB];
 #pragma unroll
@@ -698,10 +736,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dq(PrefixGradArgs p) {
     delta[i] = row.live ? x.y : 0.f;
     lo[i] = s_off[row.k - k0];
     hi[i] = lo[i] + row.own;
-    wlo[i] = wave_min(row.own ? lo[i] : 0x7fffffff);
-    whi[i] = wave_max(hi[i] * (row.own != 0));
-    alo[i] = wave_max(lo[i]);
-    ahi[i] = wave_min(hi[i]);
+    wlo[i] = __builtin_amdgcn_readlane(lo[i], 0);
+    alo[i] = __builtin_amdgcn_readlane(lo[i], 15);
+    whi[i] = __builtin_amdgcn_readlane(s_off[row.k - k0 + 1], 15);
+    ahi[i] = wlo[i] == alo[i] ? __builtin_amdgcn_readlane(hi[i], 0) : -1;
     const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH;
     const T* D = static_cast<const T*>(p.dout) + row.at * p.dout_ld + row.h * DH;
 #pragma unroll
@@ -714,65 +752,116 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dq(PrefixGradArgs p) {
   }
   const float sl2 = a.scale * kLog2e;
 
-  int cur = 0;
-  for (int c = cb; c < ce; ++c, cur ^= NBUF - 1) {
-    T *Ks = Ks_[cur], *Vs = Vs_[cur];
-    if constexpr (NBUF == 1) lds_barrier();
+  auto stage = [&](T* Ks, T* Vs) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
-      const int e = q * NT + tid, key = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      if ((c >= cctx || (c + 1) * KC > nctx) && gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
-      st8(&Ks[key * KLD + d0], kreg[q]);
-      st8(&Vs[key * VLD + d0], vreg[q]);
+      st8(&Ks[L::at(key0 + q * STEP, d0 / 8)], kreg[q]);
+      st8(&Vs[L::at(key0 + q * STEP, d0 / 8)], vreg[q]);
     }
-    if (c + 1 >= cctx && tid < KC) s_at[(c + 1) & 1][tid] = found;
+  };
+  // p (dp - delta) of tile i for the 32 keys from kb on
+  auto dscores = [&](const T* Ks, const T* Vs, int kb, int rl, int i, float (&e)[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        s = mma(L::rows(Ks, kb + 16 * x, d, rl), qf[i][d], s);
+        dp = mma(L::rows(Vs, kb + 16 * x, d, rl), df[i][d], dp);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e[4 * x + j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -lse2[i])) * (dp[j] - delta[i]);
+    }
+  };
+
+  const bool idle = r0 + wave * QT * 16 >= a.R;
+  int rl = L::row_lane(lane), cl = L::col_lane(lane);
+  int cur = 0;
+  for (int c = cb; c < cm; ++c, cur ^= NBUF - 1) {
+    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    if constexpr (NBUF == 1) lds_barrier();
+    if ((c + 1) * KC > nctx) {                     // uniform
+#pragma unroll
+      for (int q = 0; q < PER_T; ++q)
+        if (c * KC + key0 + q * STEP >= nctx) kreg[q] = vreg[q] = V8<T>{};
+    }
+    stage(Ks, Vs);
+    if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
+      find(cm);
+      if (tid < KC) s_at[cm & 1][tid] = found;
+    }
     lds_barrier();
-    if (c + 1 < ce) load_chunk(c + 1);
-    find(c + 2);
-    const bool shared = c < cctx;
-    const int base = shared ? c * KC : (c - cctx) * KC, top = shared ? nctx : nown;
+    if (c + 1 < cm) {
+      load_ctx(c + 1);
+    } else if (cm < ce) {
+      load_own(cm);
+      find(cm + 1);
+    }
+    if (idle) continue;
+    rl = fresh(rl);
+    cl = fresh(cl);
 #pragma unroll
     for (int kb = 0; kb < KC; kb += 32) {
-      const int x0 = base + kb;
-      if (x0 >= top) break;                                            // uniform
+      const int left = nctx - c * KC - kb;
+      if (left <= 0) break;                                            // uniform
       V8<T> ds[QT];
-      unsigned sees = 0;
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
-        if (!shared && (x0 >= whi[i] || x0 + 32 <= wlo[i])) continue;  // uniform
-        sees |= 1u << i;
+        float e[8];
+        dscores(Ks, Vs, kb, rl, i, e);
+        if (left < 32) {                                               // uniform
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-          const int key = kb + 16 * x + c16;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            s = mma(ld8(&Ks[key * KLD + d * 32 + g4 * 8]), qf[i][d], s);
-            dp = mma(ld8(&Vs[key * VLD + d * 32 + g4 * 8]), df[i][d], dp);
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -lse2[i])) * (dp[j] - delta[i]);
-          if (shared ? x0 + 32 > nctx : (x0 < alo[i] || x0 + 32 > ahi[i])) {   // uniform
-            const int l = shared ? 0 : lo[i], h = shared ? nctx : hi[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int y = x0 + 16 * x + 4 * g4 + j;
-              if (y < l || y >= h) s[j] = 0.f;
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) ds[i][4 * x + j] = from_f32<T>(s[j]);
+          for (int j = 0; j < 8; ++j)
+            if (key_of(j, g4) >= left) e[j] = 0.f;
         }
+        ds[i] = pack8<T>(e);
       }
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        const V8<T> kt = ld_cols<KLD>(Ks, kb, n * 16, lane);
+        const V8<T> kt = L::cols(Ks, kb, n, cl);
 #pragma unroll
-        for (int i = 0; i < QT; ++i)
-          if (sees >> i & 1) o[i][n] = mma(kt, ds[i], o[i][n]);
+        for (int i = 0; i < QT; ++i) o[i][n] = mma(kt, ds[i], o[i][n]);
       }
     }
   }
+
+  for (int c = cm; c < ce; ++c, cur ^= NBUF - 1) {
+    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    if constexpr (NBUF == 1) lds_barrier();
+#pragma unroll
+    for (int q = 0; q < PER_T; ++q)
+      if (gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
+    stage(Ks, Vs);
+    if (tid < KC) s_at[(c + 1) & 1][tid] = found;
+    lds_barrier();
+    if (c + 1 < ce) load_own(c + 1);
+    find(c + 2);
+    if (idle) continue;
+    rl = fresh(rl);
+    cl = fresh(cl);
+#pragma unroll 1
+    for (int kb = 0; kb < KC; kb += 32) {
+      const int x0 = (c - cctx) * KC + kb;
+      if (x0 >= nown) break;                                           // uniform
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        if (x0 >= whi[i] || x0 + 32 <= wlo[i]) continue;               // uniform
+        float e[8];
+        dscores(Ks, Vs, kb, rl, i, e);
+        if (x0 < alo[i] || x0 + 32 > ahi[i]) {                         // uniform
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int x = x0 + key_of(j, g4);
+            if (x < lo[i] || x >= hi[i]) e[j] = 0.f;
+          }
+        }
+        const V8<T> ds = pack8<T>(e);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[i][n] = mma(L::cols(Ks, kb, n, cl), ds, o[i][n]);
+      }
+    }
+  }
+
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const int r = r0 + (wave * QT + i) * 16 + c16;
@@ -780,7 +869,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dq(PrefixGradArgs p) {
     const Row row = row_of(a, b, g, r);
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      const f32x4 v = o[i][n] * (row.live ? a.scale : 0.f);
+      const f32x4 v = row.live ? o[i][n] * a.scale : f32x4{0.f, 0.f, 0.f, 0.f};
       if (a.splits > 1) {
         const long long rows = (long long)a.B * a.K * a.S * a.Hq;
         *reinterpret_cast<f32x4*>(a.part_o + (z * rows + row.at * a.Hq + row.h) * DH + n * 16 + g4 * 4) = v;
@@ -799,11 +888,12 @@ template <typename T, int DH, int KT, int NW, int RC>
 __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, COLS = NW * KT * 16, NB = DH / 16, ND = DH / 32;
-  constexpr int LD = DH + 2 * kPad<T>;
-  constexpr int PER_T = RC * DH / 8 / NT;
+  typedef Tile<T, DH> L;
+  constexpr int PER_T = RC * DH / 8 / NT, STEP = NT / (DH / 8);
   static_assert(RC * DH / 8 % NT == 0 && RC % 32 == 0 && RC <= NT, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Qs_[2][RC * LD], Ds_[2][RC * LD];
-  __shared__ float4 s_row[2][RC];
+  __shared__ __attribute__((aligned(16))) T Qs_[2][RC * L::LD], Ds_[2][RC * L::LD];
+  __shared__ __attribute__((aligned(16))) float s_lse[2][RC], s_delta[2][RC];
+  __shared__ __attribute__((aligned(16))) int s_lo[2][RC], s_hi[2][RC];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
@@ -829,24 +919,22 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
   V8<T> qreg[PER_T], dreg[PER_T];
   float lreg[PER_T];
   float4 rreg;
+  const int i0 = tid / (DH / 8), d0 = tid % (DH / 8) * 8;              // this thread's part of a chunk: rows i0 + q STEP
   const float4* rows = p.rows + ((long long)b * a.Hkv + g) * a.R;
   auto load_chunk = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
-      const int e = q * NT + tid, r = rb + c * RC + e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      lreg[q] = INFINITY;
-      qreg[q] = dreg[q] = V8<T>{};
-      if (r < re) {
-        const long long at = (long long)b * a.K * a.S + r / a.G;
-        const int h = g * a.G + r % a.G;
-        qreg[q] = ld8(static_cast<const T*>(a.q) + at * a.q_ld + h * DH + d0);
-        dreg[q] = ld8(static_cast<const T*>(p.dout) + at * p.dout_ld + h * DH + d0);
-        lreg[q] = rows[r].x;
-      }
+      const int r = min(rb + c * RC + i0 + q * STEP, re - 1);          // a row past the end repeats the last one, with lse = infinity
+      const long long at = (long long)b * a.K * a.S + (a.G == 1 ? r : r / a.G);
+      const int h = g * a.G + (a.G == 1 ? 0 : r % a.G);
+      qreg[q] = ld8(static_cast<const T*>(a.q) + at * a.q_ld + h * DH + d0);
+      dreg[q] = ld8(static_cast<const T*>(p.dout) + at * p.dout_ld + h * DH + d0);
+      if (a.q_len) lreg[q] = rows[r].x;                                // uniform
     }
     if (tid < RC) {
       const int r = rb + c * RC + tid;
-      rreg = r < re ? rows[r] : make_float4(INFINITY, 0.f, 0.f, 0.f);
+      rreg = rows[min(r, re - 1)];
+      if (r >= re) rreg.x = INFINITY, rreg.w = rreg.z;
     }
   };
   if (cb < ce) load_chunk(cb);
@@ -882,65 +970,85 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
   }
   const float sl2 = a.scale * kLog2e;
 
+  int rl = L::row_lane(lane), cl = L::col_lane(lane);
   int cur = 0;
   for (int c = cb; c < ce; ++c, cur ^= 1) {
     T *Qs = Qs_[cur], *Ds = Ds_[cur];
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
-      const int e = q * NT + tid, i = e / (DH / 8), d0 = (e % (DH / 8)) * 8;
-      const bool in = lreg[q] != INFINITY;                              // a row that sees nothing may hold anything
-      st8(&Qs[i * LD + d0], in ? qreg[q] : V8<T>{});
-      st8(&Ds[i * LD + d0], in ? dreg[q] : V8<T>{});
+      if (a.q_len && lreg[q] == INFINITY) qreg[q] = dreg[q] = V8<T>{};  // a row that sees nothing may hold anything
+      st8(&Qs[L::at(i0 + q * STEP, d0 / 8)], qreg[q]);
+      st8(&Ds[L::at(i0 + q * STEP, d0 / 8)], dreg[q]);
     }
-    if (tid < RC) s_row[cur][tid] = rreg;
+    if (tid < RC) {
+      s_lse[cur][tid] = rreg.x;
+      s_delta[cur][tid] = rreg.y;
+      s_lo[cur][tid] = __float_as_int(rreg.z);
+      s_hi[cur][tid] = __float_as_int(rreg.w);
+    }
     lds_barrier();
     if (c + 1 < ce) load_chunk(c + 1);
+    rl = fresh(rl);
+    cl = fresh(cl);
 #pragma unroll
     for (int kb = 0; kb < RC; kb += 32) {
       if (rb + c * RC + kb >= re) break;                                // uniform
-      float4 w[8];
+      if (!shared) {                                                    // uniform: lists of the step's rows, keys of the wave
+        const int first = __builtin_amdgcn_readfirstlane(s_lo[cur][kb]), last = __builtin_amdgcn_readfirstlane(s_lo[cur][kb + 31]);
+        const int xa = x0 + wave * KT * 16;
+        if (first >= xa + KT * 16 || last + a.L <= xa) continue;
+      }
+      float pe[KT][8], de[KT][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = s_row[cur][kb + key_of(j, g4)];
-      V8<T> pb[KT], ds[KT];
-      unsigned sees = 0;
+      for (int u = 0; u < 2; ++u) {
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(&s_lse[cur][kb + 16 * u + 4 * g4]);
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(&s_delta[cur][kb + 16 * u + 4 * g4]);
+        f32x4 s[KT], dp[KT];
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        const int x = x0 + (wave * KT + i) * 16 + c16;
-        bool any = false;
-        if (!shared) {                                                  // uniform
+        for (int i = 0; i < KT; ++i) s[i] = dp[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 8; ++j) any |= x >= __float_as_int(w[j].z) && x < __float_as_int(w[j].w);
-          if (!__any(any)) continue;
-        }
-        sees |= 1u << i;
+        for (int d = 0; d < ND; ++d) {
+          const V8<T> qv = L::rows(Qs, kb + 16 * u, d, rl), dv8 = L::rows(Ds, kb + 16 * u, d, rl);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
-          const int ar = (kb + 16 * u + c16) * LD + g4 * 8;
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            s = mma(ld8(&Qs[ar + d * 32]), kf[i][d], s);
-            dp = mma(ld8(&Ds[ar + d * 32]), vf[i][d], dp);
+          for (int i = 0; i < KT; ++i) {
+            s[i] = mma(qv, kf[i][d], s[i]);
+            dp[i] = mma(dv8, vf[i][d], dp[i]);
           }
+        }
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float4 y = w[4 * u + j];
-            const bool in = shared ? x < nctx : x >= __float_as_int(y.z) && x < __float_as_int(y.w);
-            const float e = in ? __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -y.x)) : 0.f;
-            pb[i][4 * u + j] = from_f32<T>(e);
-            ds[i][4 * u + j] = from_f32<T>(e * (dp[j] - y.y));
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[i][j], sl2, -lse[j]));
+            pe[i][4 * u + j] = e;
+            de[i][4 * u + j] = e * (dp[i][j] - delta[j]);
+          }
+        if (!shared) {                                                  // uniform
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int l = s_lo[cur][kb + 16 * u + 4 * g4 + j], h = s_hi[cur][kb + 16 * u + 4 * g4 + j];
+#pragma unroll
+            for (int i = 0; i < KT; ++i) {
+              const int x = x0 + (wave * KT + i) * 16 + c16;
+              if (x < l || x >= h) pe[i][4 * u + j] = de[i][4 * u + j] = 0.f;
+            }
           }
         }
       }
+      V8<T> pb[KT], ds[KT];
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        pb[i] = pack8<T>(pe[i]);
+        ds[i] = pack8<T>(de[i]);
+      }
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        const V8<T> dt = ld_cols<LD>(Ds, kb, n * 16, lane), qt = ld_cols<LD>(Qs, kb, n * 16, lane);
+        const V8<T> dt = L::cols(Ds, kb, n, cl), qt = L::cols(Qs, kb, n, cl);
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-          if (sees >> i & 1) {
-            dv[i][n] = mma(dt, pb[i], dv[i][n]);
-            dk[i][n] = mma(qt, ds[i], dk[i][n]);
-          }
+        for (int i = 0; i < KT; ++i) {
+          dv[i][n] = mma(dt, pb[i], dv[i][n]);
+          dk[i][n] = mma(qt, ds[i], dk[i][n]);
+        }
       }
     }
   }
@@ -955,7 +1063,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
     float* po = p.row_splits > 1 ? p.part_kv + ((long long)z * n_keys + key) * 2 * DH + g4 * 4 : nullptr;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      const f32x4 k4 = dk[i][n] * a.scale, v4 = dv[i][n];
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};                          // a key past its length: its sums mean nothing
+      const f32x4 k4 = live[i] ? dk[i][n] * a.scale : zero, v4 = live[i] ? dv[i][n] : zero;
       if (po) {
         *reinterpret_cast<f32x4*>(po + n * 16) = k4;
         *reinterpret_cast<f32x4*>(po + DH + n * 16) = v4;
@@ -1028,10 +1137,7 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   a.tiles = pl.tiles;
   a.splits = pl.splits;
   const dim3 gq((unsigned)(bg * a.tiles * a.splits));
-  if (pl.rows == 128)
-    hipLaunchKernelGGL((k_prefix_dq<T, DH, 2, 4, 64>), gq, dim3(256), 0, s, p);
-  else
-    hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, 64>), gq, dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, 64>), gq, dim3(256), 0, s, p);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.splits > 1) {
@@ -1078,16 +1184,17 @@ PrefixPlan prefix_plan(const fe_prefix_args& a) {
 PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a) {
   PrefixGradPlan p;
   const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
-  p.rows = bg * ((R + 127) / 128) >= 512 ? 128 : 64;
-  p.tiles = (int)((R + p.rows - 1) / p.rows);
-  const long long lists = std::min<long long>(a.K, (p.rows - 1) / (a.S * G) + 2);
+  // dq: 64 rows a workgroup (128: 64 x 1024 rows of 1088 keys at head width 64 the same, 256 x 550 fp32 rows 100 us -> 123).
+  // Key and row ranges as in the forward: up to two workgroups per compute unit, three chunks each.
+  p.tiles = (int)((R + 63) / 64);
+  const long long lists = std::min<long long>(a.K, 63 / (a.S * G) + 2);
   const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
-  p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 2, 16LL}));
+  p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 3, 16LL}));
   const int cols = a.dh == 128 ? 64 : 128;
   p.ctx_tiles = (a.T + cols - 1) / cols;
   p.own_tiles = (int)(((long long)a.K * a.L + cols - 1) / cols);
   const long long wgs = bg * (p.ctx_tiles + p.own_tiles);
-  p.row_splits = wgs ? (int)std::max(1LL, std::min({512 / wgs, (R + 63) / 64 / 2, 16LL})) : 1;
+  p.row_splits = wgs ? (int)std::max(1LL, std::min({512 / wgs, (R + 63) / 64 / 3, 16LL})) : 1;
   const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads, keys = (size_t)a.B * (a.T + (size_t)a.K * a.L) * a.n_kv_heads;
   p.rows_bytes = rows * sizeof(float4);
   p.dq_bytes = p.splits > 1 ? p.splits * rows * a.dh * sizeof(float) : 0;
