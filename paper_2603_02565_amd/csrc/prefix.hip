@@ -144,18 +144,30 @@ FE_DEV int packed_list(const int* off, int nb, int c) {
   return lo;
 }
 
-// Row of own_k / own_v that holds logical own row j of list bk, or -1 (a page outside the pool).
-FE_DEV long long own_row(const PrefixArgs& a, int bk, int j) {
-  if (a.page_rows == 0) return (long long)bk * a.L + j;
-  const int page = a.table[(long long)bk * (a.L / a.page_rows) + j / a.page_rows];
-  return page >= 0 && page < a.n_pages ? (long long)page * a.page_rows + j % a.page_rows : -1;
+// Where row c of the lists packed in off lies in own_k / own_v.  A page is only requested here and turned into a row when it
+// is needed, a chunk later, so that nothing waits for the table.
+struct OwnAt {
+  long long row;                        // dense: the row; paged: its place in the page; -2 past the last row
+  int page;
+};
+FE_DEV OwnAt find_own(const PrefixArgs& a, int b, int k0, int nb, const int* off, int c) {
+  OwnAt w{-2, 0};
+  if (c >= off[nb]) return w;
+  const int i = packed_list(off, nb, c), j = c - off[i];
+  const long long bk = (long long)b * a.K + k0 + i;
+  if (a.page_rows == 0) {
+    w.row = bk * a.L + j;
+  } else {
+    const int p = j / a.page_rows;
+    w.page = a.table[bk * (a.L / a.page_rows) + p];
+    w.row = j - p * a.page_rows;
+  }
+  return w;
 }
-
-// Row of own_k / own_v for row c of the lists packed in off, -1 for a page outside the pool, -2 past the last row.
-FE_DEV long long find_own(const PrefixArgs& a, int b, int k0, int nb, const int* off, int c) {
-  if (c >= off[nb]) return -2;
-  const int i = packed_list(off, nb, c);
-  return own_row(a, b * a.K + k0 + i, c - off[i]);
+// The row; -1 for a page outside the pool.
+FE_DEV long long own_row(const PrefixArgs& a, const OwnAt& w) {
+  if (a.page_rows == 0 || w.row < 0) return w.row;
+  return w.page >= 0 && w.page < a.n_pages ? (long long)w.page * a.page_rows + w.row : -1;
 }
 
 // What a lane has to know about its query row r of (request b, key head g).
@@ -232,6 +244,7 @@ FE_DEV int fresh(int x) {
 // Waves per SIMD that the register file is shared between (more hide more latency; fewer would spill).
 constexpr int waves_of(int bytes, int dh, int qt) { return dh == 128 ? 2 : bytes == 2 && dh * qt <= 64 ? 4 : dh * qt <= 64 || bytes == 2 ? 3 : 2; }
 
+constexpr int dkv_waves(int bytes, int dh) { return dh == 32 ? 3 : 2; }
 // ------------------------------------------------------------------------------------------
 // Forward.  NW waves of QT 16-row tiles; chunks of KC keys staged through registers (the next chunk's loads in
 // flight behind this one's products) into LDS.  Scores are formed transposed (keys x rows): a lane then holds
@@ -309,7 +322,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     }
   };
   // own rows are found one chunk before they are loaded, so that a page table's latency is hidden as well
-  long long found = -2;
+  OwnAt found{-2, 0};
   auto find = [&](int c) __attribute__((always_inline)) {
     if (c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
   };
@@ -317,7 +330,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     load_ctx(cb);
   } else if (cm < ce) {
     find(cm);
-    if (tid < KC) s_at[cm & 1][tid] = found;
+    if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
     lds_barrier();
     load_own(cm);
     find(cm + 1);
@@ -419,7 +432,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     stage(Ks, Vs);
     if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
       find(cm);
-      if (tid < KC) s_at[cm & 1][tid] = found;
+      if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
     }
     lds_barrier();   // two buffers: also the end of every wave's reads of the one written next
     if (c + 1 < cm) {
@@ -489,7 +502,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       if (hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
     }
     stage(Ks, Vs);
-    if (tid < KC) s_at[(c + 1) & 1][tid] = found;
+    if (tid < KC) s_at[(c + 1) & 1][tid] = own_row(a, found);
     lds_barrier();
     if (c + 1 < ce) load_own(c + 1);
     find(c + 2);
@@ -709,7 +722,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       vreg[q] = ld8(vp + at);
     }
   };
-  long long found = -2;
+  OwnAt found{-2, 0};
   auto find = [&](int c) __attribute__((always_inline)) {
     if (c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
   };
@@ -717,7 +730,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     load_ctx(cb);
   } else if (cm < ce) {
     find(cm);
-    if (tid < KC) s_at[cm & 1][tid] = found;
+    if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
     lds_barrier();
     load_own(cm);
     find(cm + 1);
@@ -788,7 +801,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     stage(Ks, Vs);
     if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
       find(cm);
-      if (tid < KC) s_at[cm & 1][tid] = found;
+      if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
     }
     lds_barrier();
     if (c + 1 < cm) {
@@ -800,29 +813,29 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     if (idle) continue;
     rl = fresh(rl);
     cl = fresh(cl);
+    const int left = nctx - c * KC;                // keys of the chunk
+    V8<T> ds[KC / 32][QT];
 #pragma unroll
-    for (int kb = 0; kb < KC; kb += 32) {
-      const int left = nctx - c * KC - kb;
-      if (left <= 0) break;                                            // uniform
-      V8<T> ds[QT];
+    for (int u = 0; u < KC / 32; ++u)
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
         float e[8];
-        dscores(Ks, Vs, kb, rl, i, e);
-        if (left < 32) {                                               // uniform
+        dscores(Ks, Vs, 32 * u, rl, i, e);
+        if (left < KC) {                           // uniform; keys past the length are zeros, but their probability may be anything
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (key_of(j, g4) >= left) e[j] = 0.f;
+            if (32 * u + key_of(j, g4) >= left) e[j] = 0.f;
         }
-        ds[i] = pack8<T>(e);
+        ds[u][i] = pack8<T>(e);
       }
+#pragma unroll
+    for (int u = 0; u < KC / 32; ++u)
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        const V8<T> kt = L::cols(Ks, kb, n, cl);
+        const V8<T> kt = L::cols(Ks, 32 * u, n, cl);
 #pragma unroll
-        for (int i = 0; i < QT; ++i) o[i][n] = mma(kt, ds[i], o[i][n]);
+        for (int i = 0; i < QT; ++i) o[i][n] = mma(kt, ds[u][i], o[i][n]);
       }
-    }
   }
 
   for (int c = cm; c < ce; ++c, cur ^= NBUF - 1) {
@@ -832,7 +845,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     for (int q = 0; q < PER_T; ++q)
       if (gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
     stage(Ks, Vs);
-    if (tid < KC) s_at[(c + 1) & 1][tid] = found;
+    if (tid < KC) s_at[(c + 1) & 1][tid] = own_row(a, found);
     lds_barrier();
     if (c + 1 < ce) load_own(c + 1);
     find(c + 2);
@@ -885,26 +898,28 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 // hold own rows (dense, list after list) and meet the rows of their lists.  In the tile's numbering -- shared row, or
 // k L + j -- the keys that a row sees are again one interval.  Few tiles: `row_splits` workgroups share a tile's rows.
 template <typename T, int DH, int KT, int NW, int RC>
-__global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
+__global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, COLS = NW * KT * 16, NB = DH / 16, ND = DH / 32;
   typedef Tile<T, DH> L;
-  constexpr int PER_T = RC * DH / 8 / NT, STEP = NT / (DH / 8);
-  static_assert(RC * DH / 8 % NT == 0 && RC % 32 == 0 && RC <= NT, "tile shape");
+  constexpr int PER_T = (RC * DH / 8 + NT - 1) / NT, STEP = NT / (DH / 8);
+  static_assert(RC % 32 == 0 && RC <= NT && (RC * DH / 8 % NT == 0 || RC * DH / 8 < NT), "tile shape");
   __shared__ __attribute__((aligned(16))) T Qs_[2][RC * L::LD], Ds_[2][RC * L::LD];
   __shared__ __attribute__((aligned(16))) float s_lse[2][RC], s_delta[2][RC];
   __shared__ __attribute__((aligned(16))) int s_lo[2][RC], s_hi[2][RC];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
-  int id = xcd_tile(blockIdx.x, gridDim.x);
+  // Shared tiles meet every row and come first; the own tiles, a few rows each, fill in behind them.
+  const int n_ctx = a.B * a.Hkv * p.ctx_tiles * p.row_splits;
+  const bool shared = (int)blockIdx.x < n_ctx;
+  int id = shared ? xcd_tile(blockIdx.x, n_ctx) : xcd_tile(blockIdx.x - n_ctx, gridDim.x - n_ctx);
   const int z = id % p.row_splits;
   id /= p.row_splits;
-  const int tiles = p.ctx_tiles + p.own_tiles, t = id % tiles;
+  const int tiles = shared ? p.ctx_tiles : p.own_tiles, t = id % tiles;
   id /= tiles;
   const int g = id % a.Hkv, b = id / a.Hkv;
-  const bool shared = t < p.ctx_tiles;
-  const int x0 = (shared ? t : t - p.ctx_tiles) * COLS, cols = shared ? a.T : a.K * a.L, sg = a.S * a.G;
+  const int x0 = t * COLS, cols = shared ? a.T : a.K * a.L, sg = a.S * a.G;
   const int nctx = ctx_rows(a, b);
   int rb = 0, re = a.R;
   if (shared) {
@@ -921,21 +936,42 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
   float4 rreg;
   const int i0 = tid / (DH / 8), d0 = tid % (DH / 8) * 8;              // this thread's part of a chunk: rows i0 + q STEP
   const float4* rows = p.rows + ((long long)b * a.Hkv + g) * a.R;
-  auto load_chunk = [&](int c) __attribute__((always_inline)) {
+  // Rows past the end repeat the last one, with lse = infinity.
+  const T *q_base = static_cast<const T*>(a.q), *d_base = static_cast<const T*>(p.dout);
+  const bool even = RC % a.G == 0 && a.q_ld <= (1 << 23) && p.dout_ld <= (1 << 23);   // uniform: a chunk's rows lie as the first one's do
+  unsigned q_at[PER_T], d_at[PER_T];               // ... and these are their byte offsets
 #pragma unroll
-    for (int q = 0; q < PER_T; ++q) {
-      const int r = min(rb + c * RC + i0 + q * STEP, re - 1);          // a row past the end repeats the last one, with lse = infinity
-      const long long at = (long long)b * a.K * a.S + (a.G == 1 ? r : r / a.G);
-      const int h = g * a.G + (a.G == 1 ? 0 : r % a.G);
-      qreg[q] = ld8(static_cast<const T*>(a.q) + at * a.q_ld + h * DH + d0);
-      dreg[q] = ld8(static_cast<const T*>(p.dout) + at * p.dout_ld + h * DH + d0);
-      if (a.q_len) lreg[q] = rows[r].x;                                // uniform
+  for (int q = 0; q < PER_T; ++q) {
+    const int i = i0 + q * STEP;
+    q_at[q] = (i / a.G * a.q_ld + (i % a.G) * DH + d0) * sizeof(T);
+    d_at[q] = (i / a.G * p.dout_ld + (i % a.G) * DH + d0) * sizeof(T);
+  }
+  auto load_chunk = [&](int c) __attribute__((always_inline)) {
+    const int r0 = rb + c * RC;                    // a multiple of G
+    if (even && r0 + RC <= re) {                   // uniform
+      const long long at = (long long)b * a.K * a.S + r0 / a.G;
+      const T *qp = q_base + at * a.q_ld + g * a.G * DH, *dp = d_base + at * p.dout_ld + g * a.G * DH;
+#pragma unroll
+      for (int q = 0; q < PER_T; ++q) {
+        if (RC * DH / 8 < NT && i0 >= RC) continue;
+        qreg[q] = ld8_at(qp, q_at[q]);
+        dreg[q] = ld8_at(dp, d_at[q]);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < PER_T; ++q) {
+        const int r = min(r0 + i0 + q * STEP, re - 1);
+        const long long at = (long long)b * a.K * a.S + r / a.G;
+        const int h = g * a.G + r % a.G;
+        qreg[q] = ld8(q_base + at * a.q_ld + h * DH + d0);
+        dreg[q] = ld8(d_base + at * p.dout_ld + h * DH + d0);
+      }
     }
-    if (tid < RC) {
-      const int r = rb + c * RC + tid;
-      rreg = rows[min(r, re - 1)];
-      if (r >= re) rreg.x = INFINITY, rreg.w = rreg.z;
+    if (a.q_len) {                                 // uniform
+#pragma unroll
+      for (int q = 0; q < PER_T; ++q) lreg[q] = rows[min(r0 + i0 + q * STEP, re - 1)].x;
     }
+    if (tid < RC) rreg = rows[min(r0 + tid, re - 1)];
   };
   if (cb < ce) load_chunk(cb);
 
@@ -971,84 +1007,114 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prefix_dkv(PrefixGradArgs p) {
   const float sl2 = a.scale * kLog2e;
 
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
+
+  // q.k and dout.v of 32 rows from kb on with the wave's keys
+  auto products = [&](const T* Qs, const T* Ds, int kb, f32x4 (&s)[2][KT], f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < KT; ++i) s[u][i] = dp[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const V8<T> qv = L::rows(Qs, kb + 16 * u, d, rl), dv8 = L::rows(Ds, kb + 16 * u, d, rl);
+#pragma unroll
+        for (int i = 0; i < KT; ++i) {
+          s[u][i] = mma(qv, kf[i][d], s[u][i]);
+          dp[u][i] = mma(dv8, vf[i][d], dp[u][i]);
+        }
+      }
+    }
+  };
+  // ... and with them the rows' part of dk and dv; own: rows see the keys [lo, hi)
+  auto add = [&](const T* Qs, const T* Ds, int cur, int kb, bool own, const f32x4 (&s)[2][KT], const f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
+    float pe[KT][8], de[KT][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f32x4 lse = *reinterpret_cast<const f32x4*>(&s_lse[cur][kb + 16 * u + 4 * g4]);
+      const f32x4 delta = *reinterpret_cast<const f32x4*>(&s_delta[cur][kb + 16 * u + 4 * g4]);
+#pragma unroll
+      for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[u][i][j], sl2, -lse[j]));
+          pe[i][4 * u + j] = e;
+          de[i][4 * u + j] = e * (dp[u][i][j] - delta[j]);
+        }
+      if (own) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int l = s_lo[cur][kb + 16 * u + 4 * g4 + j], h = s_hi[cur][kb + 16 * u + 4 * g4 + j];
+#pragma unroll
+          for (int i = 0; i < KT; ++i) {
+            const int x = x0 + (wave * KT + i) * 16 + c16;
+            if (x < l || x >= h) pe[i][4 * u + j] = de[i][4 * u + j] = 0.f;
+          }
+        }
+      }
+    }
+    V8<T> pb[KT], ds[KT];
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      pb[i] = pack8<T>(pe[i]);
+      ds[i] = pack8<T>(de[i]);
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const V8<T> dt = L::cols(Ds, kb, n, cl), qt = L::cols(Qs, kb, n, cl);
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        dv[i][n] = mma(dt, pb[i], dv[i][n]);
+        dk[i][n] = mma(qt, ds[i], dk[i][n]);
+      }
+    }
+  };
+
+  // Two loops, so that each keeps the sums in place.
   int cur = 0;
-  for (int c = cb; c < ce; ++c, cur ^= 1) {
+  auto stage = [&](int c) __attribute__((always_inline)) {
     T *Qs = Qs_[cur], *Ds = Ds_[cur];
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
       if (a.q_len && lreg[q] == INFINITY) qreg[q] = dreg[q] = V8<T>{};  // a row that sees nothing may hold anything
+      if (RC * DH / 8 < NT && i0 >= RC) continue;
       st8(&Qs[L::at(i0 + q * STEP, d0 / 8)], qreg[q]);
       st8(&Ds[L::at(i0 + q * STEP, d0 / 8)], dreg[q]);
     }
     if (tid < RC) {
-      s_lse[cur][tid] = rreg.x;
+      const bool past = rb + c * RC + tid >= re;
+      s_lse[cur][tid] = past ? INFINITY : rreg.x;
       s_delta[cur][tid] = rreg.y;
       s_lo[cur][tid] = __float_as_int(rreg.z);
-      s_hi[cur][tid] = __float_as_int(rreg.w);
+      s_hi[cur][tid] = __float_as_int(past ? rreg.z : rreg.w);
     }
     lds_barrier();
     if (c + 1 < ce) load_chunk(c + 1);
     rl = fresh(rl);
     cl = fresh(cl);
+  };
+  if (shared) {
+    for (int c = cb; c < ce; ++c, cur ^= 1) {
+      stage(c);
 #pragma unroll
-    for (int kb = 0; kb < RC; kb += 32) {
-      if (rb + c * RC + kb >= re) break;                                // uniform
-      if (!shared) {                                                    // uniform: lists of the step's rows, keys of the wave
+      for (int kb = 0; kb < RC; kb += 32) {                             // rows past the end have probability 0
+        f32x4 s[2][KT], dp[2][KT];
+        products(Qs_[cur], Ds_[cur], kb, s, dp);
+        add(Qs_[cur], Ds_[cur], cur, kb, false, s, dp);
+      }
+    }
+  } else {
+    for (int c = cb; c < ce; ++c, cur ^= 1) {
+      stage(c);
+#pragma unroll 1
+      for (int kb = 0; kb < RC; kb += 32) {
+        if (rb + c * RC + kb >= re) break;                              // uniform
+        // uniform: lists of the block's rows, keys of the wave
         const int first = __builtin_amdgcn_readfirstlane(s_lo[cur][kb]), last = __builtin_amdgcn_readfirstlane(s_lo[cur][kb + 31]);
         const int xa = x0 + wave * KT * 16;
         if (first >= xa + KT * 16 || last + a.L <= xa) continue;
-      }
-      float pe[KT][8], de[KT][8];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(&s_lse[cur][kb + 16 * u + 4 * g4]);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(&s_delta[cur][kb + 16 * u + 4 * g4]);
-        f32x4 s[KT], dp[KT];
-#pragma unroll
-        for (int i = 0; i < KT; ++i) s[i] = dp[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const V8<T> qv = L::rows(Qs, kb + 16 * u, d, rl), dv8 = L::rows(Ds, kb + 16 * u, d, rl);
-#pragma unroll
-          for (int i = 0; i < KT; ++i) {
-            s[i] = mma(qv, kf[i][d], s[i]);
-            dp[i] = mma(dv8, vf[i][d], dp[i]);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < KT; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[i][j], sl2, -lse[j]));
-            pe[i][4 * u + j] = e;
-            de[i][4 * u + j] = e * (dp[i][j] - delta[j]);
-          }
-        if (!shared) {                                                  // uniform
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int l = s_lo[cur][kb + 16 * u + 4 * g4 + j], h = s_hi[cur][kb + 16 * u + 4 * g4 + j];
-#pragma unroll
-            for (int i = 0; i < KT; ++i) {
-              const int x = x0 + (wave * KT + i) * 16 + c16;
-              if (x < l || x >= h) pe[i][4 * u + j] = de[i][4 * u + j] = 0.f;
-            }
-          }
-        }
-      }
-      V8<T> pb[KT], ds[KT];
-#pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        pb[i] = pack8<T>(pe[i]);
-        ds[i] = pack8<T>(de[i]);
-      }
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const V8<T> dt = L::cols(Ds, kb, n, cl), qt = L::cols(Qs, kb, n, cl);
-#pragma unroll
-        for (int i = 0; i < KT; ++i) {
-          dv[i][n] = mma(dt, pb[i], dv[i][n]);
-          dk[i][n] = mma(qt, ds[i], dk[i][n]);
-        }
+        f32x4 s[2][KT], dp[2][KT];
+        products(Qs_[cur], Ds_[cur], kb, s, dp);
+        add(Qs_[cur], Ds_[cur], cur, kb, true, s, dp);
       }
     }
   }
@@ -1108,7 +1174,7 @@ __global__ __launch_bounds__(256) void k_prefix_sum_dkv(PrefixGradArgs p) {
 }
 
 // Tile shapes.  Forward and dq: QT 16-row tiles a wave; dkv: KT 16-key tiles a wave and RC rows a chunk.
-template <typename T, int DH> constexpr int kKT = DH == 128 ? 1 : 2;
+template <typename T, int DH> constexpr int kKT = sizeof(T) == 2 && DH <= 64 ? 2 : 1;
 template <typename T, int DH> constexpr int kRC = sizeof(T) * DH > 256 ? 32 : 64;
 
 template <typename T, int DH, int QT>
@@ -1190,7 +1256,7 @@ PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a) {
   const long long lists = std::min<long long>(a.K, 63 / (a.S * G) + 2);
   const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
   p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 3, 16LL}));
-  const int cols = a.dh == 128 ? 64 : 128;
+  const int cols = a.dtype == FE_BF16 && a.dh <= 64 ? 128 : 64;
   p.ctx_tiles = (a.T + cols - 1) / cols;
   p.own_tiles = (int)(((long long)a.K * a.L + cols - 1) / cols);
   const long long wgs = bg * (p.ctx_tiles + p.own_tiles);
