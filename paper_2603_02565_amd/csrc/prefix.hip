@@ -144,31 +144,33 @@ FE_DEV int packed_list(const int* off, int nb, int c) {
   return lo;
 }
 
-// Where row c of the lists packed in off lies in own_k / own_v.  A page is only requested here and turned into a row when it
-// is needed, a chunk later, so that nothing waits for the table.
-struct OwnAt {
-  long long row;                        // dense: the row; paged: its place in the page; -2 past the last row
-  int page;
-};
-FE_DEV OwnAt find_own(const PrefixArgs& a, int b, int k0, int nb, const int* off, int c) {
-  OwnAt w{-2, 0};
-  if (c >= off[nb]) return w;
-  const int i = packed_list(off, nb, c), j = c - off[i];
-  const long long bk = (long long)b * a.K + k0 + i;
-  if (a.page_rows == 0) {
-    w.row = bk * a.L + j;
-  } else {
-    const int p = j / a.page_rows;
-    w.page = a.table[bk * (a.L / a.page_rows) + p];
-    w.row = j - p * a.page_rows;
+// Where row c of the lists packed in off lies in own_k / own_v: find() says it, row() turns it into the row's number, -2 past
+// the last row, -1 for a page outside the pool.  A page is requested by find() and looked at by row(), a chunk later, so that
+// nothing waits for the table.
+template <bool PAGED> struct OwnAt;
+template <> struct OwnAt<false> {
+  long long at = -2;
+  FE_DEV void find(const PrefixArgs& a, int b, int k0, int nb, const int* off, int c) {
+    at = -2;
+    if (c >= off[nb]) return;
+    const int i = packed_list(off, nb, c);
+    at = ((long long)b * a.K + k0 + i) * a.L + c - off[i];
   }
-  return w;
-}
-// The row; -1 for a page outside the pool.
-FE_DEV long long own_row(const PrefixArgs& a, const OwnAt& w) {
-  if (a.page_rows == 0 || w.row < 0) return w.row;
-  return w.page >= 0 && w.page < a.n_pages ? (long long)w.page * a.page_rows + w.row : -1;
-}
+  FE_DEV long long row(const PrefixArgs&) const { return at; }
+};
+template <> struct OwnAt<true> {
+  int page = 0, rest = -1;
+  FE_DEV void find(const PrefixArgs& a, int b, int k0, int nb, const int* off, int c) {
+    rest = -1;
+    if (c >= off[nb]) return;
+    const int i = packed_list(off, nb, c), j = c - off[i], p = j / a.page_rows;
+    page = a.table[((long long)b * a.K + k0 + i) * (a.L / a.page_rows) + p];
+    rest = j - p * a.page_rows;
+  }
+  FE_DEV long long row(const PrefixArgs& a) const {
+    return rest < 0 ? -2 : page >= 0 && page < a.n_pages ? (long long)page * a.page_rows + rest : -1;
+  }
+};
 
 // What a lane has to know about its query row r of (request b, key head g).
 struct Row {
@@ -251,7 +253,7 @@ constexpr int dkv_waves(int bytes, int dh) { return dh == 32 ? 3 : 2; }
 // eight keys of one row, which is the operand layout of the product with the values, so probabilities never leave the
 // registers.
 // ------------------------------------------------------------------------------------------
-template <typename T, int DH, int QT, int NW, int KC>
+template <typename T, int DH, int QT, int NW, int KC, bool PAGED>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_fwd(PrefixArgs a) {
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
   typedef Tile<T, DH> L;
@@ -316,21 +318,21 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     for (int p = 0; p < PER_T; ++p) {
       const long long x = s_at[c & 1][key0 + p * STEP], at = max(x, 0LL) * a.own_ld;
       gone |= (x < 0) << p;
-      hole |= (x == -1) << p;
+      if (PAGED) hole |= (x == -1) << p;
       kreg[p] = ld8(kp + at);
       vreg[p] = ld8(vp + at);
     }
   };
   // own rows are found one chunk before they are loaded, so that a page table's latency is hidden as well
-  OwnAt found{-2, 0};
+  OwnAt<PAGED> found;
   auto find = [&](int c) __attribute__((always_inline)) {
-    if (c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+    if (c < ce && tid < KC) found.find(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
   };
   if (cb < cm) {
     load_ctx(cb);
   } else if (cm < ce) {
     find(cm);
-    if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
+    if (tid < KC) s_at[cm & 1][tid] = found.row(a);
     lds_barrier();
     load_own(cm);
     find(cm + 1);
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     stage(Ks, Vs);
     if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
       find(cm);
-      if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
+      if (tid < KC) s_at[cm & 1][tid] = found.row(a);
     }
     lds_barrier();   // two buffers: also the end of every wave's reads of the one written next
     if (c + 1 < cm) {
@@ -499,10 +501,10 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     for (int p = 0; p < PER_T; ++p) {
       if (gone >> p & 1) kreg[p] = vreg[p] = V8<T>{};
       if (!finite8(vreg[p])) s_odd[c & 1] = c;
-      if (hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
+      if (PAGED && hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
     }
     stage(Ks, Vs);
-    if (tid < KC) s_at[(c + 1) & 1][tid] = own_row(a, found);
+    if (tid < KC) s_at[(c + 1) & 1][tid] = found.row(a);
     lds_barrier();
     if (c + 1 < ce) load_own(c + 1);
     find(c + 2);
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     rl = fresh(rl);
     cl = fresh(cl);
     const bool odd = __builtin_amdgcn_readfirstlane(s_odd[c & 1]) == c;
-    const bool holes = __builtin_amdgcn_readfirstlane(s_holes[c & 1]) == c;
+    const bool holes = PAGED && __builtin_amdgcn_readfirstlane(s_holes[c & 1]) == c;
 #pragma unroll 1
     for (int kb = 0; kb < KC; kb += 32) {
       const int x0 = (c - cctx) * KC + kb;
@@ -722,15 +724,15 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       vreg[q] = ld8(vp + at);
     }
   };
-  OwnAt found{-2, 0};
+  OwnAt<false> found;
   auto find = [&](int c) __attribute__((always_inline)) {
-    if (c < ce && tid < KC) found = find_own(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+    if (c < ce && tid < KC) found.find(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
   };
   if (cb < cm) {
     load_ctx(cb);
   } else if (cm < ce) {
     find(cm);
-    if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
+    if (tid < KC) s_at[cm & 1][tid] = found.row(a);
     lds_barrier();
     load_own(cm);
     find(cm + 1);
@@ -801,7 +803,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     stage(Ks, Vs);
     if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
       find(cm);
-      if (tid < KC) s_at[cm & 1][tid] = own_row(a, found);
+      if (tid < KC) s_at[cm & 1][tid] = found.row(a);
     }
     lds_barrier();
     if (c + 1 < cm) {
@@ -845,7 +847,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     for (int q = 0; q < PER_T; ++q)
       if (gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
     stage(Ks, Vs);
-    if (tid < KC) s_at[(c + 1) & 1][tid] = own_row(a, found);
+    if (tid < KC) s_at[(c + 1) & 1][tid] = found.row(a);
     lds_barrier();
     if (c + 1 < ce) load_own(c + 1);
     find(c + 2);
@@ -1180,13 +1182,20 @@ template <typename T, int DH> constexpr int kRC = sizeof(T) * DH > 256 ? 32 : 64
 template <typename T, int DH, int QT>
 hipError_t launch_fwd_qt(const PrefixArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.splits));
-  hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, 64>), grid, dim3(256), 0, s, a);
+  if (a.page_rows > 0)
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, 64, true>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, 64, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int DH>
 hipError_t fwd(const PrefixArgs& a, const PrefixPlan& p, hipStream_t s) {
-  hipError_t e = p.rows == 128 ? launch_fwd_qt<T, DH, 2>(a, s) : launch_fwd_qt<T, DH, 1>(a, s);
+  hipError_t e;
+  if constexpr (sizeof(T) * DH <= 256)
+    e = p.rows == 128 ? launch_fwd_qt<T, DH, 2>(a, s) : launch_fwd_qt<T, DH, 1>(a, s);
+  else
+    e = launch_fwd_qt<T, DH, 1>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   const long long rows = (long long)a.B * a.K * a.S * a.Hq;
   hipLaunchKernelGGL((k_prefix_join<T, DH>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, s, a);
