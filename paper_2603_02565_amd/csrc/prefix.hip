@@ -280,12 +280,10 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
   if (tid < 2) s_odd[tid] = s_holes[tid] = -1;
   if (tid < KC) s_hole[0][tid] = s_hole[1][tid] = -1;
-  pack_own<NT>(a, b, k0, nb, s_off);
-
-  const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_off[nb]);
-  const int cctx = (nctx + KC - 1) / KC, chunks = cctx + (nown + KC - 1) / KC;
-  const int cb = (int)((long long)chunks * z / a.splits), ce = (int)((long long)chunks * (z + 1) / a.splits);
-  const int cm = min(max(cctx, cb), ce);           // shared chunks [cb, cm), own chunks [cm, ce)
+  // This workgroup's share of the shared chunks and, below, of the own chunks.  The shared ones need no more than ctx_len,
+  // so they are under way while the lists' lengths, packing and pages are found.
+  const int nctx = ctx_rows(a, b), cctx = (nctx + KC - 1) / KC;
+  const int cb = (int)((long long)cctx * z / a.splits), cm = (int)((long long)cctx * (z + 1) / a.splits);
 
   // The loads are unconditional: rows that do not count read one that exists and are cleared when they are staged.
   V8<T> kreg[PER_T], vreg[PER_T];
@@ -310,6 +308,20 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       vreg[p] = ld8_at(vp, at);
     }
   };
+  if (cb < cm) load_ctx(cb);
+  Row row[QT];
+  V8<T> qf[QT][ND];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    row[i] = row_of(a, b, g, r0 + (wave * QT + i) * 16 + c16);
+    const T* Q = static_cast<const T*>(a.q) + row[i].at * a.q_ld + row[i].h * DH;
+#pragma unroll
+    for (int c = 0; c < ND; ++c) qf[i][c] = ld8(Q + c * 32 + g4 * 8);
+  }
+
+  pack_own<NT>(a, b, k0, nb, s_off);
+  const int nown = __builtin_amdgcn_readfirstlane(s_off[nb]), cown = (nown + KC - 1) / KC;
+  const int ob = (int)((long long)cown * z / a.splits), oe = (int)((long long)cown * (z + 1) / a.splits);
   int gone = 0, hole = 0;                          // bit p: the key does not count; because its page is outside the pool
   auto load_own = [&](int c) __attribute__((always_inline)) {
     const T *kp = static_cast<const T*>(a.own_k) + g * DH + d0, *vp = static_cast<const T*>(a.own_v) + g * DH + d0;
@@ -326,20 +338,19 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   // own rows are found one chunk before they are loaded, so that a page table's latency is hidden as well
   OwnAt<PAGED> found;
   auto find = [&](int c) __attribute__((always_inline)) {
-    if (c < ce && tid < KC) found.find(a, b, k0, nb, s_off, (c - cctx) * KC + tid);
+    if (c < oe && tid < KC) found.find(a, b, k0, nb, s_off, c * KC + tid);
   };
-  if (cb < cm) {
-    load_ctx(cb);
-  } else if (cm < ce) {
-    find(cm);
-    if (tid < KC) s_at[cm & 1][tid] = found.row(a);
+  auto first_own = [&]() __attribute__((always_inline)) {
+    find(ob);
+    if (tid < KC) s_at[ob & 1][tid] = found.row(a);
+  };
+  if (cb >= cm && ob < oe) {                       // uniform
+    first_own();
     lds_barrier();
-    load_own(cm);
-    find(cm + 1);
+    load_own(ob);
+    find(ob + 1);
   }
 
-  Row row[QT];
-  V8<T> qf[QT][ND];
   int lo[QT], hi[QT];                              // the packed own rows that the row sees
   // of the wave's tile, uniform: bounds of what its rows see, and (empty where they belong to several lists) what every
   // row sees.  lo does not fall from row to row, nor hi within a list; rows past q_len may see anything.
@@ -348,17 +359,15 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   f32x4 o[QT][NB];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
-    row[i] = row_of(a, b, g, r0 + (wave * QT + i) * 16 + c16);
     lo[i] = s_off[row[i].k - k0];
     hi[i] = lo[i] + row[i].own;
     wlo[i] = __builtin_amdgcn_readlane(lo[i], 0);
     alo[i] = __builtin_amdgcn_readlane(lo[i], 15);
     whi[i] = __builtin_amdgcn_readlane(s_off[row[i].k - k0 + 1], 15);
     ahi[i] = wlo[i] == alo[i] ? __builtin_amdgcn_readlane(hi[i], 0) : -1;
-    const T* Q = static_cast<const T*>(a.q) + row[i].at * a.q_ld + row[i].h * DH;
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      qf[i][c] = row[i].live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
+      if (!row[i].live) qf[i][c] = V8<T>{};
       if (a.scale < 0) qf[i][c] = -qf[i][c];       // exact; the largest score is then the largest product
     }
     m_run[i] = -INFINITY;
@@ -432,16 +441,13 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         if (c * KC + key0 + p * STEP >= nctx) kreg[p] = vreg[p] = V8<T>{};
     }
     stage(Ks, Vs);
-    if (c + 1 == cm && cm < ce) {                  // uniform; the first own chunk follows
-      find(cm);
-      if (tid < KC) s_at[cm & 1][tid] = found.row(a);
-    }
+    if (c + 1 == cm && ob < oe) first_own();       // uniform; the first own chunk follows
     lds_barrier();   // two buffers: also the end of every wave's reads of the one written next
     if (c + 1 < cm) {
       load_ctx(c + 1);
-    } else if (cm < ce) {
-      load_own(cm);
-      find(cm + 1);
+    } else if (ob < oe) {
+      load_own(ob);
+      find(ob + 1);
     }
     if (idle) continue;
     rl = fresh(rl);
@@ -494,7 +500,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     }
   }
 
-  for (int c = cm; c < ce; ++c, cur ^= NBUF - 1) {
+  for (int c = ob; c < oe; ++c, cur ^= NBUF - 1) {
     T *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();
 #pragma unroll
@@ -506,7 +512,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     stage(Ks, Vs);
     if (tid < KC) s_at[(c + 1) & 1][tid] = found.row(a);
     lds_barrier();
-    if (c + 1 < ce) load_own(c + 1);
+    if (c + 1 < oe) load_own(c + 1);
     find(c + 2);
     if (idle) continue;
     rl = fresh(rl);
@@ -515,7 +521,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     const bool holes = PAGED && __builtin_amdgcn_readfirstlane(s_holes[c & 1]) == c;
 #pragma unroll 1
     for (int kb = 0; kb < KC; kb += 32) {
-      const int x0 = (c - cctx) * KC + kb;
+      const int x0 = c * KC + kb;
       if (x0 >= nown) break;                       // uniform
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
@@ -601,21 +607,36 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
   const long long e = (long long)blockIdx.x * 256 + threadIdx.x, ro = e / (DH / 4);
   const int d0 = (int)(e % (DH / 4)) * 4;
   if (ro >= rows) return;
-  float m = -INFINITY;
-#pragma unroll 8
-  for (int z = 0; z < a.splits; ++z) m = fmaxf(m, a.part_ml[(z * rows + ro) * 2]);
   const long long at = ro / a.Hq;
   const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);
-  const bool none = m == -INFINITY || s >= q_rows(a, bk);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
+  const bool dead = s >= q_rows(a, bk);
+  float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int z = 0; z < a.splits; ++z) {
-    const float w = __builtin_amdgcn_exp2f(a.part_ml[(z * rows + ro) * 2] - ref);
-    l = fmaf(a.part_ml[(z * rows + ro) * 2 + 1], w, l);
-    o += w * *reinterpret_cast<const f32x4*>(a.part_o + (z * rows + ro) * DH + d0);
+  for (int z0 = 0; z0 < a.splits; z0 += 8) {       // eight ranges requested at once
+    float2 ml[8];
+    f32x4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const long long e = min(z0 + u, a.splits - 1) * rows + ro;
+      ml[u] = reinterpret_cast<const float2*>(a.part_ml)[e];
+      v[u] = *reinterpret_cast<const f32x4*>(a.part_o + e * DH + d0);
+      if (z0 + u >= a.splits) ml[u].x = -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) top = fmaxf(top, ml[u].x);
+    const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(m - ref);
+    m = top;
+    l *= old;
+    o *= old;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = __builtin_amdgcn_exp2f(ml[u].x - ref);
+      l = fmaf(ml[u].y, w, l);
+      if (ml[u].x != -INFINITY) o += w * v[u];     // a range without keys for the row says nothing
+    }
   }
+  const bool none = dead || m == -INFINITY;
   const float inv = none ? 0.f : 1.f / l;
 #pragma unroll
   for (int q = 0; q < 4; ++q) o[q] = none ? 0.f : o[q] * inv;
