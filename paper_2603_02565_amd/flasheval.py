@@ -344,7 +344,9 @@ def fe_train_grads(cfg: fe_config, params, B: int, T: int, M: int, K: int, L: in
 
 
 def fe_cache_append(args: fe_append_args, stream=None) -> None:
-    _check(load_library().fe_cache_append(ctypes.byref(args), _stream(stream)), "fe_cache_append")
+    st = load_library().fe_cache_append(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_cache_append")
 
 
 def fe_prefix_workspace_size(args: fe_prefix_args, grad: bool = False) -> int:
@@ -355,7 +357,9 @@ def fe_prefix_workspace_size(args: fe_prefix_args, grad: bool = False) -> int:
 
 
 def fe_prefix_attention(args: fe_prefix_args, stream=None) -> None:
-    _check(load_library().fe_prefix_attention(ctypes.byref(args), _stream(stream)), "fe_prefix_attention")
+    st = load_library().fe_prefix_attention(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_prefix_attention")
 
 
 def fe_prefix_attention_grad(args: fe_prefix_args, grads: fe_prefix_grads, stream=None) -> None:
@@ -566,40 +570,42 @@ def _row_stride(t, name: str, shape: Tuple[int, ...], dtype) -> int:
 
 
 class _Layouts:
-    """The layout checks of one object's tensors, remembered by name, shape, strides and type: a serving loop
-    passes the same layouts again and again."""
+    """The layout checks of one object's tensors, remembered by shapes, strides and types: a serving loop passes the same
+    layouts again and again."""
 
     def __init__(self):
         self.known = {}
 
-    def rows(self, t, name: str, shape: Tuple[int, ...], dtype) -> int:
-        key = (name, t.shape, t.stride(), t.dtype)
-        ld = self.known.get(key)
-        if ld is None:
-            ld = self.known[key] = _row_stride(t, name, shape, dtype)
-        return ld
-
-    def vector(self, t, name: str, dtype, numel: int) -> Optional[int]:
-        """Address of a contiguous vector of numel elements (None stays None)."""
-        if t is None:
-            return None
-        key = (name, t.shape, t.stride(), t.dtype)
-        if key not in self.known:
-            _need(t, name, dtype, numel)
-            self.known[key] = numel
-        return t.data_ptr()
+    def of(self, check, *tensors):
+        """What check(*tensors) returned for tensors of these layouts (it raises for those that do not fit)."""
+        key = tuple([None if t is None else (t.shape, t.stride(), t.dtype) for t in tensors])
+        got = self.known.get(key)
+        if got is None:
+            got = self.known[key] = check(*tensors)
+        return got
 
 
-def _here() -> int:
-    """Index of the current HIP device, -1 without one."""
+def _on_device(tensors) -> int:
+    """Index of the current HIP device, on which all the tensors have to be."""
     import torch
-    return torch.cuda.current_device() if torch.cuda.is_available() else -1
-
-
-def _on_device(tensors, index: int) -> None:
+    index = tensors[0].get_device()
     for t in tensors:
         if t is not None and (t.get_device() != index or index < 0):
             raise ValueError(f"every tensor must be on the current HIP device, got one on {t.device}")
+    if torch.cuda.current_device() != index:
+        raise ValueError(f"the tensors are on device {index}, the current HIP device is {torch.cuda.current_device()}")
+    return index
+
+
+def _stream_on(index: int, stream) -> int:
+    if stream is not None:
+        return _stream(stream)
+    import torch
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _addr(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 class PagedCache:
@@ -627,7 +633,7 @@ class PagedCache:
         _need(self.len, "length", torch.int32, self.N)
         self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
         self.status = torch.zeros(self.N, dtype=torch.int32, device=table.device)
-        _on_device((k_pages, v_pages, table, self.len), _here())
+        _on_device((k_pages, v_pages, table, self.len))
         a = self.args = fe_append_args()
         a.dtype = FE_BF16 if k_pages.dtype == torch.bfloat16 else FE_F32
         a.n_pages, a.page_rows, a.n_kv_heads, a.dh = shape
@@ -636,45 +642,44 @@ class PagedCache:
         a.len, a.status = _ptr(self.len), _ptr(self.status)
         self._layouts = _Layouts()
 
+    def _check(self, k, v, q, q_out, freq, new_len, pos0, len_out):
+        """(rows, n_heads, k_ld, v_ld, q_ld, q_out_ld, rot) of an append's tensors."""
+        import torch
+        hkv, dh, dt, N = self.k_pages.shape[2], self.k_pages.shape[3], self.k_pages.dtype, self.N
+        if k.dim() != 4:
+            raise ValueError(f"k: expected [sequences][rows][heads][dh], got {tuple(k.shape)}")
+        S = k.shape[1]
+        k_ld, v_ld = (_row_stride(t, n, (N, S, hkv, dh), dt) for t, n in ((k, "k"), (v, "v")))
+        H = q_ld = q_out_ld = 0
+        if q is not None:
+            if q.dim() != 4:
+                raise ValueError(f"q: expected [sequences][rows][heads][dh], got {tuple(q.shape)}")
+            H = q.shape[2]
+            q_ld, q_out_ld = (_row_stride(t, n, (N, S, H, dh), dt) for t, n in ((q, "q"), (q_out, "q_out")))
+        if freq is not None:
+            _need(freq, "freq", torch.float64, freq.numel())
+        for t, name in ((new_len, "new_len"), (pos0, "pos0"), (len_out, "len_out")):
+            _need(t, name, torch.int32, N)
+        return S, H, k_ld, v_ld, q_ld, q_out_ld, 0 if freq is None else 2 * freq.numel()
+
     def append(self, k, v, q=None, q_out=None, new_len=None, pos0=None, freq=None, neighbours=False, len_out=None,
                stream=None):
         """Append rows k, v [N][S][n_kv_heads][dh] (the first new_len[s] of sequence s); with `freq` (float64 [rot / 2])
         keys and q [N][S][n_heads][dh] are turned by their positions pos0[s] + row.  q_out defaults to a new
         tensor; it is returned.  The lengths advance in place, or into len_out when that is given.
         `status` [N] holds FE_DEV_BAD_PAGE for a sequence with a row that found no page."""
-        import torch
-        a, lay, dt, N = self.args, self._layouts, self.k_pages.dtype, self.N
-        hkv, dh = self.k_pages.shape[2:]
-        if k.dim() != 4:
-            raise ValueError(f"k: expected [sequences][rows][heads][dh], got {tuple(k.shape)}")
-        S = a.S = k.shape[1]
-        a.k_ld = lay.rows(k, "k", (N, S, hkv, dh), dt)
-        a.v_ld = lay.rows(v, "v", (N, S, hkv, dh), dt)
-        if v.shape != k.shape:
-            raise ValueError(f"v: expected {tuple(k.shape)}, got {tuple(v.shape)}")
-        if q is not None:
-            if q.dim() != 4:
-                raise ValueError(f"q: expected [sequences][rows][heads][dh], got {tuple(q.shape)}")
-            a.n_heads = q.shape[2]
-            a.q_ld = lay.rows(q, "q", (N, S, q.shape[2], dh), dt)
-            if q_out is None:
-                q_out = torch.empty(q.shape, dtype=dt, device=q.device)
-            if q_out.shape != q.shape or q.shape[1] != S:
-                raise ValueError(f"q, q_out: expected {S} rows and one shape, got {tuple(q.shape)} and {tuple(q_out.shape)}")
-            a.q_out_ld = lay.rows(q_out, "q_out", (N, S, q.shape[2], dh), dt)
-            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
-        elif q_out is not None:
-            raise ValueError("q_out without q")
-        else:
-            a.q = a.q_out = None
-        a.rot, a.neighbours = 0 if freq is None else 2 * freq.numel(), 1 if neighbours else 0
-        a.freq = None if freq is None else lay.vector(freq, "freq", torch.float64, freq.numel())
-        a.new_len = lay.vector(new_len, "new_len", torch.int32, N)
-        a.pos0 = lay.vector(pos0, "pos0", torch.int32, N)
-        a.len_out = a.len if len_out is None else lay.vector(len_out, "len_out", torch.int32, N)
-        _on_device((self.k_pages, k, v, q, q_out, freq, len_out, new_len, pos0), _here())
-        a.k, a.v = k.data_ptr(), v.data_ptr()
-        fe_cache_append(a, stream)
+        a = self.args
+        if (q is None) != (q_out is None):
+            if q is None:
+                raise ValueError("q_out without q")
+            q_out = q.new_empty(q.shape)
+        a.S, a.n_heads, a.k_ld, a.v_ld, a.q_ld, a.q_out_ld, a.rot = self._layouts.of(
+            self._check, k, v, q, q_out, freq, new_len, pos0, len_out)
+        index = _on_device((k, v, q, q_out, freq, new_len, pos0, len_out, self.k_pages))
+        a.neighbours = 1 if neighbours else 0
+        a.q, a.k, a.v, a.q_out, a.freq = _addr(q), k.data_ptr(), v.data_ptr(), _addr(q_out), _addr(freq)
+        a.new_len, a.pos0, a.len_out = _addr(new_len), _addr(pos0), a.len if len_out is None else len_out.data_ptr()
+        fe_cache_append(a, _stream_on(index, stream))
         return q_out
 
 
@@ -722,33 +727,44 @@ class PrefixAttention:
                           *(torch.empty((a.B, a.T, a.n_kv_heads, a.dh), dtype=self.act, device=dev) for _ in range(2)),
                           *(torch.empty((a.B, a.K, a.L, a.n_kv_heads, a.dh), dtype=self.act, device=dev) for _ in range(2)))
 
-    def _take(self, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len):
+    def _check(self, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len):
+        """(q_ld, ctx_ld, own_ld) of a call's tensors."""
         import torch
-        a, lay, act, i32 = self.args, self._layouts, self.act, torch.int32
-        a.q_ld = lay.rows(q, "q", self.q_shape, act)
-        if a.T:
-            a.ctx_ld = lay.rows(ctx_k, "ctx_k", self.ctx_shape, act)
-            if lay.rows(ctx_v, "ctx_v", self.ctx_shape, act) != a.ctx_ld:
-                raise ValueError("ctx_k and ctx_v must have the same row stride")
-        if a.L:
-            a.own_ld = lay.rows(own_k, "own_k", self.own_shape, act)
-            if lay.rows(own_v, "own_v", self.own_shape, act) != a.own_ld:
-                raise ValueError("own_k and own_v must have the same row stride")
+        a, act, i32 = self.args, self.act, torch.int32
+        q_ld, lds = _row_stride(q, "q", self.q_shape, act), []
+        for k, v, name, shape, n in ((ctx_k, ctx_v, "ctx", self.ctx_shape, a.T), (own_k, own_v, "own", self.own_shape, a.L)):
+            if n and (k is None or v is None):
+                raise ValueError(f"{name}_k, {name}_v: missing")
+            ld = [_row_stride(t, f"{name}_{x}", shape, act) if n else 0 for t, x in ((k, "k"), (v, "v"))]
+            if ld[0] != ld[1]:
+                raise ValueError(f"{name}_k and {name}_v must have the same row stride")
+            lds.append(ld[0])
         if (table is None) != (a.page_rows == 0):
             raise ValueError("a table and page_rows > 0 go together")
-        a.table = None if table is None else lay.vector(table, "table", i32, a.B * a.K * (a.L // a.page_rows))
-        a.ctx_len = lay.vector(ctx_len, "ctx_len", i32, a.B)
-        a.q_len = lay.vector(q_len, "q_len", i32, a.B * a.K)
-        a.own_len = lay.vector(own_len, "own_len", i32, a.B * a.K)
-        _on_device((q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len, self.out), _here())
+        if table is not None:
+            _need(table, "table", i32, a.B * a.K * (a.L // a.page_rows))
+        _need(ctx_len, "ctx_len", i32, a.B)
+        _need(q_len, "q_len", i32, a.B * a.K)
+        _need(own_len, "own_len", i32, a.B * a.K)
+        return q_ld, lds[0], lds[1]
+
+    def _take(self, *tensors):
+        a = self.args
+        q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len = tensors
+        a.q_ld, a.ctx_ld, a.own_ld = self._layouts.of(self._check, *tensors)
+        index = _on_device(tensors)
         if self.out is None:
             self.allocate()
-        a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = (None if t is None else t.data_ptr() for t in (q, ctx_k, ctx_v, own_k, own_v))
+        elif self.out.get_device() != index:
+            raise ValueError(f"the outputs are on {self.out.device}, the tensors on device {index}")
+        a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = q.data_ptr(), _addr(ctx_k), _addr(ctx_v), _addr(own_k), _addr(own_v)
+        a.table, a.ctx_len, a.own_len, a.q_len = _addr(table), _addr(ctx_len), _addr(own_len), _addr(q_len)
+        return index
 
     def run(self, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
         """Enqueue the attention; returns out [B][K][S][n_heads][dh] (self.lse holds the log sums when training)."""
-        self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
-        fe_prefix_attention(self.args, stream)
+        index = self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        fe_prefix_attention(self.args, _stream_on(index, stream))
         return self.out
 
     def grad(self, dout, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
@@ -757,12 +773,12 @@ class PrefixAttention:
             raise ValueError("grad needs train=True")
         if self.out is None:
             raise ValueError("grad follows run")
-        self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        index = self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
         a, g = self.args, fe_prefix_grads()
-        g.dout_ld = self._layouts.rows(dout, "dout", self.q_shape, self.act)
-        _on_device((dout,), _here())
-        g.dout = _ptr(dout)
+        g.dout_ld = self._layouts.of(lambda t: _row_stride(t, "dout", self.q_shape, self.act), dout)
+        _on_device((dout, q))
+        g.dout = dout.data_ptr()
         g.dq_ld, g.dctx_ld, g.down_ld = a.n_heads * a.dh, a.n_kv_heads * a.dh, a.n_kv_heads * a.dh
-        g.dq, g.dctx_k, g.dctx_v, g.down_k, g.down_v = (_ptr(t) for t in self.grads)
-        fe_prefix_attention_grad(a, g, stream)
+        g.dq, g.dctx_k, g.dctx_v, g.down_k, g.down_v = (t.data_ptr() for t in self.grads)
+        fe_prefix_attention_grad(a, g, _stream_on(index, stream))
         return self.grads
