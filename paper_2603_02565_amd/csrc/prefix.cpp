@@ -74,7 +74,7 @@ fe_status check_forward(const fe_prefix_args* a) {
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
-size_t grad_bytes(const PrefixGradPlan& p) { return up256(p.rows_bytes) + up256(p.dq_bytes) + up256(p.dkv_bytes); }
+size_t grad_bytes(const PrefixGradPlan& p) { return up256(p.rows_bytes) + up256(p.dq_bytes) + up256(p.ctx_bytes) + up256(p.own_bytes); }
 
 PrefixArgs kernel_args(const fe_prefix_args& a) {
   PrefixArgs k{};
@@ -143,9 +143,15 @@ fe_status fe_prefix_attention_grad(const fe_prefix_args* a, const fe_prefix_grad
   k.dq = g->dq; k.dctx_k = g->dctx_k; k.dctx_v = g->dctx_v; k.down_k = g->down_k; k.down_v = g->down_v;
   k.dq_ld = g->dq_ld; k.dctx_ld = g->dctx_ld; k.down_ld = g->down_ld;
   char* ws = static_cast<char*>(a->ws);
-  k.rows = reinterpret_cast<float4*>(ws);
-  k.f.part_o = reinterpret_cast<float*>(ws + up256(p.rows_bytes));
-  k.part_kv = reinterpret_cast<float*>(ws + up256(p.rows_bytes) + up256(p.dq_bytes));
+  auto take = [&](size_t bytes) {
+    char* at = ws;
+    ws += up256(bytes);
+    return reinterpret_cast<float*>(at);
+  };
+  k.rows = reinterpret_cast<float4*>(take(p.rows_bytes));
+  k.f.part_o = take(p.dq_bytes);
+  k.part_ctx = take(p.ctx_bytes);
+  k.part_own = take(p.own_bytes);
   const hipError_t e = launch_prefix_grad(k, a->dh, a->dtype == FE_BF16, p, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? FE_OK : pfail(FE_EHIP, "shared-prefix gradient launch failed: %s", hipGetErrorString(e));
 }

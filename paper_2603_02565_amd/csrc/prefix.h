@@ -29,7 +29,8 @@ struct PrefixGradArgs {
   int dq_ld, dctx_ld, down_ld;
   float4* rows;                         // [B][Hkv][R]: what the products need of every row
   int ctx_tiles, own_tiles;             // key tiles of the shared rows / of the own rows per (request, key head)
-  int row_splits; float* part_kv;       // row ranges per key tile; their partial sums [row_splits][keys][2][dh]
+  int ctx_splits, own_splits;           // row ranges per shared / own key tile
+  float *part_ctx, *part_own;           // their partial sums [splits][keys][2][dh]
 };
 
 // Row tiles, key ranges and partial-sum bytes of a forward call: functions of the sizes alone.
@@ -37,7 +38,10 @@ struct PrefixPlan { int rows, tiles, splits; size_t part_bytes; };
 PrefixPlan prefix_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixPlan& p, hipStream_t s);
 // The same of a gradient call: dq's row tiles and key ranges, dk's and dv's key tiles and row ranges, scratch bytes.
-struct PrefixGradPlan { int tiles, splits, ctx_tiles, own_tiles, row_splits; size_t rows_bytes, dq_bytes, dkv_bytes; };
+struct PrefixGradPlan {
+  int tiles, splits, ctx_tiles, own_tiles, ctx_splits, own_splits;
+  size_t rows_bytes, dq_bytes, ctx_bytes, own_bytes;
+};
 PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_grad(const PrefixGradArgs& a, int dh, bool bf16_rows, const PrefixGradPlan& p, hipStream_t s);
 hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s);

@@ -919,7 +919,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 // dk and dv of a tile of keys: NW waves of KT 16-key tiles whose keys and values stay in registers, the rows stream through
 // LDS in chunks of RC.  Tiles 0 .. ctx_tiles - 1 of a (request, key head) hold shared rows and meet every row; the others
 // hold own rows (dense, list after list) and meet the rows of their lists.  In the tile's numbering -- shared row, or
-// k L + j -- the keys that a row sees are again one interval.  Few tiles: `row_splits` workgroups share a tile's rows.
+// k L + j -- the keys that a row sees are again one interval.  Few tiles: several workgroups share a tile's rows.
 template <typename T, int DH, int KT, int NW, int RC>
 __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -934,11 +934,11 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
   // Shared tiles meet every row and come first; the own tiles, a few rows each, fill in behind them.
-  const int n_ctx = a.B * a.Hkv * p.ctx_tiles * p.row_splits;
+  const int n_ctx = a.B * a.Hkv * p.ctx_tiles * p.ctx_splits;
   const bool shared = (int)blockIdx.x < n_ctx;
   int id = shared ? xcd_tile(blockIdx.x, n_ctx) : xcd_tile(blockIdx.x - n_ctx, gridDim.x - n_ctx);
-  const int z = id % p.row_splits;
-  id /= p.row_splits;
+  const int splits = shared ? p.ctx_splits : p.own_splits, z = id % splits;
+  id /= splits;
   const int tiles = shared ? p.ctx_tiles : p.own_tiles, t = id % tiles;
   id /= tiles;
   const int g = id % a.Hkv, b = id / a.Hkv;
@@ -952,7 +952,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
     re = ((min(x0 + COLS, cols) - 1) / a.L + 1) * sg;
   }
   const int steps = (re - rb + RC - 1) / RC;
-  const int cb = (int)((long long)steps * z / p.row_splits), ce = (int)((long long)steps * (z + 1) / p.row_splits);
+  const int cb = (int)((long long)steps * z / splits), ce = (int)((long long)steps * (z + 1) / splits);
 
   V8<T> qreg[PER_T], dreg[PER_T];
   float lreg[PER_T];
@@ -1147,9 +1147,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
     if (x >= cols) continue;
     const long long off = at[i] * (shared ? p.dctx_ld : p.down_ld) + g * DH + g4 * 4;
     T *ko = static_cast<T*>(shared ? p.dctx_k : p.down_k) + off, *vo = static_cast<T*>(shared ? p.dctx_v : p.down_v) + off;
-    const long long n_keys = (long long)a.B * (a.T + a.K * a.L) * a.Hkv;
-    const long long key = ((shared ? 0 : (long long)a.B * a.T) + at[i]) * a.Hkv + g;
-    float* po = p.row_splits > 1 ? p.part_kv + ((long long)z * n_keys + key) * 2 * DH + g4 * 4 : nullptr;
+    const long long n_keys = (long long)a.B * cols * a.Hkv;
+    float* po = splits > 1 ? (shared ? p.part_ctx : p.part_own) + (z * n_keys + at[i] * a.Hkv + g) * 2 * DH + g4 * 4 : nullptr;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const f32x4 zero = {0.f, 0.f, 0.f, 0.f};                          // a key past its length: its sums mean nothing
@@ -1178,22 +1177,16 @@ __global__ __launch_bounds__(256) void k_prefix_sum_dq(PrefixGradArgs p) {
   for (int z = 0; z < a.splits; ++z) v += *reinterpret_cast<const f32x4*>(a.part_o + (z * rows + ro) * DH + d0);
   st4(static_cast<T*>(p.dq) + ro / a.Hq * p.dq_ld + ro % a.Hq * DH + d0, v);
 }
+// n_keys keys of dk, dv with row stride ld; part [splits][n_keys][2][DH]
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_prefix_sum_dkv(PrefixGradArgs p) {
-  const PrefixArgs& a = p.f;
-  const long long n_keys = (long long)a.B * (a.T + a.K * a.L) * a.Hkv;
+__global__ __launch_bounds__(256) void k_prefix_sum_dkv(const float* part, long long n_keys, int splits, int Hkv, int ld, T* dk, T* dv) {
   const long long e = (long long)blockIdx.x * 256 + threadIdx.x, key = e / (DH / 2);
   const int d0 = (int)(e % (DH / 2)) * 4;                               // dk, then dv
   if (key >= n_keys) return;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int z = 0; z < p.row_splits; ++z) v += *reinterpret_cast<const f32x4*>(p.part_kv + (z * n_keys + key) * 2 * DH + d0);
-  const long long at = key / a.Hkv, ctx = (long long)a.B * a.T;
-  const int g = (int)(key % a.Hkv), d = d0 % DH;
-  const bool is_v = d0 >= DH;
-  T* dst = at < ctx ? static_cast<T*>(is_v ? p.dctx_v : p.dctx_k) + at * p.dctx_ld
-                    : static_cast<T*>(is_v ? p.down_v : p.down_k) + (at - ctx) * p.down_ld;
-  st4(dst + g * DH + d, v);
+  for (int z = 0; z < splits; ++z) v += *reinterpret_cast<const f32x4*>(part + (z * n_keys + key) * 2 * DH + d0);
+  st4((d0 >= DH ? dv : dk) + key / Hkv * ld + key % Hkv * DH + d0 % DH, v);
 }
 
 // Tile shapes.  Forward and dq: QT 16-row tiles a wave; dkv: KT 16-key tiles a wave and RC rows a chunk.
@@ -1243,17 +1236,39 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   }
   p.ctx_tiles = pl.ctx_tiles;
   p.own_tiles = pl.own_tiles;
-  p.row_splits = pl.row_splits;
+  p.ctx_splits = pl.ctx_splits;
+  p.own_splits = pl.own_splits;
   if (p.ctx_tiles + p.own_tiles == 0) return hipSuccess;
-  const dim3 gk((unsigned)(bg * (p.ctx_tiles + p.own_tiles) * p.row_splits));
+  const dim3 gk((unsigned)(bg * (p.ctx_tiles * p.ctx_splits + p.own_tiles * p.own_splits)));
   hipLaunchKernelGGL((k_prefix_dkv<T, DH, kKT<T, DH>, 4, kRC<T, DH>>), gk, dim3(256), 0, s, p);
   e = hipGetLastError();
-  if (e != hipSuccess || p.row_splits == 1) return e;
-  const long long keys = (long long)a.B * (a.T + a.K * a.L) * a.Hkv;
-  hipLaunchKernelGGL((k_prefix_sum_dkv<T, DH>), dim3((unsigned)((keys * (DH / 2) + 255) / 256)), dim3(256), 0, s, p);
-  return hipGetLastError();
+  auto sum = [&](const float* part, long long keys, int splits, int ld, void* dk, void* dv) {
+    if (e != hipSuccess || splits == 1 || keys == 0) return;
+    hipLaunchKernelGGL((k_prefix_sum_dkv<T, DH>), dim3((unsigned)((keys * (DH / 2) + 255) / 256)), dim3(256), 0, s, part, keys, splits,
+                       a.Hkv, ld, static_cast<T*>(dk), static_cast<T*>(dv));
+    e = hipGetLastError();
+  };
+  sum(p.part_ctx, (long long)a.B * a.T * a.Hkv, p.ctx_splits, p.dctx_ld, p.dctx_k, p.dctx_v);
+  sum(p.part_own, (long long)a.B * a.K * a.L * a.Hkv, p.own_splits, p.down_ld, p.down_k, p.down_v);
+  return e;
 }
 
+}  // namespace
+
+namespace {
+// Ranges that `items` chunks of 64 are split into, for each of `wgs` tiles: up to two workgroups per compute unit, at least three chunks a range
+// (a range costs its partial sums, and all of them a launch).  64 tiles of 24 chunks: one range 28.6 us, two 23.0 at four,
+// 19.5 at eight, 20.5 at sixteen; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.  In fp32 also as many as keep a range at
+// 2048: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8) of its result, 1.1e-6 at 6400.
+int ranges(long long wgs, long long items, int most, bool f32) {
+  const long long by_size = std::min({512 / std::max(1LL, wgs), items / 3, (long long)most});
+  return (int)std::min(std::max({1LL, by_size, f32 ? (items + 31) / 32 : 1LL}), 256LL);
+}
+// 64-key chunks that a tile of `rows` rows meets: the shared ones and those of the lists it touches.
+long long chunks_of(const fe_prefix_args& a, long long rows) {
+  const long long sg = (long long)a.S * (a.n_heads / a.n_kv_heads);
+  return (a.T + 63) / 64 + (std::min<long long>(a.K, (rows - 1) / sg + 2) * a.L + 63) / 64;
+}
 }  // namespace
 
 PrefixPlan prefix_plan(const fe_prefix_args& a) {
@@ -1266,12 +1281,7 @@ PrefixPlan prefix_plan(const fe_prefix_args& a) {
   const bool fits = a.dtype == FE_BF16 || a.dh <= 64;
   p.rows = fits && ((R > 64 && R <= 128) || (a.T >= 2048 && bg * ((R + 127) / 128) >= 512)) ? 128 : 64;
   p.tiles = (int)((R + p.rows - 1) / p.rows);
-  // Key ranges: up to two workgroups per compute unit, at least three chunks each (a range costs its partial sums and all
-  // of them a second launch).  64 tiles of 24 chunks: one range 28.6 us at two, 23.0 at four, 19.5 at eight, 20.5 at
-  // sixteen; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.
-  const long long lists = std::min<long long>(a.K, (p.rows - 1) / (a.S * G) + 2);
-  const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
-  p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 3, 64LL}));
+  p.splits = ranges(bg * p.tiles, chunks_of(a, p.rows), 64, a.dtype == FE_F32);
   const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads;
   p.part_bytes = p.splits > 1 ? p.splits * rows * (a.dh + 2) * sizeof(float) : 0;
   return p;
@@ -1280,21 +1290,22 @@ PrefixPlan prefix_plan(const fe_prefix_args& a) {
 PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a) {
   PrefixGradPlan p;
   const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
-  // dq: 64 rows a workgroup (128: 64 x 1024 rows of 1088 keys at head width 64 the same, 256 x 550 fp32 rows 100 us -> 123).
-  // Key and row ranges as in the forward: up to two workgroups per compute unit, three chunks each.
+  const bool f32 = a.dtype == FE_F32;
+  // dq: 64 rows a workgroup (128: 64 x 1024 rows of 1088 keys at head width 64 the same, 256 x 550 fp32 rows 100 us -> 123)
   p.tiles = (int)((R + 63) / 64);
-  const long long lists = std::min<long long>(a.K, 63 / (a.S * G) + 2);
-  const long long chunks = (a.T + 63) / 64 + (lists * a.L + 63) / 64;
-  p.splits = (int)std::max(1LL, std::min({512 / std::max(1LL, bg * p.tiles), chunks / 3, 16LL}));
-  const int cols = a.dtype == FE_BF16 && a.dh <= 64 ? 128 : 64;
-  p.ctx_tiles = (a.T + cols - 1) / cols;
+  p.splits = ranges(bg * p.tiles, chunks_of(a, 64), 16, f32);
+  // dk, dv: a shared tile meets every row, an own tile those of its lists
+  const long long cols = a.dtype == FE_BF16 && a.dh <= 64 ? 128 : 64;
+  p.ctx_tiles = (int)((a.T + cols - 1) / cols);
   p.own_tiles = (int)(((long long)a.K * a.L + cols - 1) / cols);
-  const long long wgs = bg * (p.ctx_tiles + p.own_tiles);
-  p.row_splits = wgs ? (int)std::max(1LL, std::min({512 / wgs, (R + 63) / 64 / 3, 16LL})) : 1;
-  const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads, keys = (size_t)a.B * (a.T + (size_t)a.K * a.L) * a.n_kv_heads;
+  const long long lists = a.L ? std::min<long long>(a.K, (cols - 1) / a.L + 2) : 0;
+  p.ctx_splits = a.T ? ranges(bg * p.ctx_tiles, (R + 63) / 64, 16, f32) : 1;
+  p.own_splits = a.L ? ranges(bg * p.own_tiles, (lists * a.S * G + 63) / 64, 16, f32) : 1;
+  const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads, row_bytes = 2 * a.dh * sizeof(float);
   p.rows_bytes = rows * sizeof(float4);
   p.dq_bytes = p.splits > 1 ? p.splits * rows * a.dh * sizeof(float) : 0;
-  p.dkv_bytes = p.row_splits > 1 ? p.row_splits * keys * 2 * a.dh * sizeof(float) : 0;
+  p.ctx_bytes = p.ctx_splits > 1 ? p.ctx_splits * (size_t)a.B * a.T * a.n_kv_heads * row_bytes : 0;
+  p.own_bytes = p.own_splits > 1 ? p.own_splits * (size_t)a.B * a.K * a.L * a.n_kv_heads * row_bytes : 0;
   return p;
 }
 
