@@ -1275,11 +1275,16 @@ PrefixPlan prefix_plan(const fe_prefix_args& a) {
   PrefixPlan p;
   const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
   // 128 rows a workgroup read a chunk's keys from memory and from LDS half as often, for half the waves and, in fp32 at head
-  // width 128, more registers than there are.  They pay where 64 rows would read every key twice and 128 read it once
-  // (4 x 128 rows of 32768 keys: 236 us -> 175), and over long contexts with workgroups to spare (64 x 1024 rows: of 4096
-  // keys 126 -> 112, of 1024 keys 38.2 -> 39.0; 256 x 550 rows of 256 keys 29.6 -> 33.9).
+  // width 128, more registers than there are.  They pay
+  //  - where 64 rows would read every key twice and 128 read it once (4 x 128 rows of 32768 keys: 236 us -> 175);
+  //  - with workgroups to spare, unless they leave more rows of the last tile empty (72 x 3168 rows, heads of 128: of 81 keys
+  //    65 -> 56 us, of 1500 339 -> 249; 64 x 2048 rows, heads of 64, of 364 keys 35 -> 31; 256 x 550 rows, whose 640 are 11%
+  //    more than 576, of 267 keys 28.5 -> 33.4; 32 x 576 rows of 1064 keys 25 -> 29);
+  //  - over long contexts with fewer to spare (64 x 1024 rows: of 4096 keys 126 -> 112, of 1088 38.2 -> 39.0).
   const bool fits = a.dtype == FE_BF16 || a.dh <= 64;
-  p.rows = fits && ((R > 64 && R <= 128) || (a.T >= 2048 && bg * ((R + 127) / 128) >= 512)) ? 128 : 64;
+  const long long t128 = (R + 127) / 128, t64 = (R + 63) / 64;
+  const bool spare = bg * t128 >= (a.T >= 2048 ? 512 : 1024) && 100 * 2 * t128 <= 108 * t64;
+  p.rows = fits && ((R > 64 && R <= 128) || spare) ? 128 : 64;
   p.tiles = (int)((R + p.rows - 1) / p.rows);
   p.splits = ranges(bg * p.tiles, chunks_of(a, p.rows), 64, a.dtype == FE_F32);
   const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads;
