@@ -128,7 +128,7 @@ typedef struct {
   const int32_t* own_len;               /* [B][K], or NULL: L */
   void* out;                            /* [B][K][S] rows of n_heads * dh */
   float* lse;                           /* [B][K][S][n_heads], or NULL (the gradient needs it) */
-  void* out_rest;                       /* FE_BF16: [B][K][S][n_heads * dh] what the rounding of out left, or NULL */
+  void* out_rest;                       /* FE_BF16: [B][K][S][n_heads * dh] bytes, the bits that the rounding of out cut, or NULL */
   void* ws;
   size_t ws_bytes;
 } fe_prefix_args;

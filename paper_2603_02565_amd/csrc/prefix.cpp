@@ -80,7 +80,7 @@ PrefixArgs kernel_args(const fe_prefix_args& a) {
   PrefixArgs k{};
   k.q = a.q; k.ctx_k = a.ctx_k; k.ctx_v = a.ctx_v; k.own_k = a.own_k; k.own_v = a.own_v;
   k.table = a.table; k.ctx_len = a.ctx_len; k.q_len = a.q_len; k.own_len = a.own_len;
-  k.out = a.out; k.lse = a.lse; k.out_rest = a.dtype == FE_BF16 ? a.out_rest : nullptr;
+  k.out = a.out; k.lse = a.lse; k.out_rest = a.dtype == FE_BF16 ? static_cast<signed char*>(a.out_rest) : nullptr;
   k.B = a.B; k.K = a.K; k.S = a.S; k.Hq = a.n_heads; k.Hkv = a.n_kv_heads; k.dh = a.dh; k.T = a.T; k.L = a.L;
   k.page_rows = a.page_rows; k.n_pages = a.n_pages; k.causal = a.causal != 0;
   k.q_ld = a.q_ld; k.ctx_ld = a.ctx_ld; k.own_ld = a.own_ld; k.out_ld = a.out_ld;

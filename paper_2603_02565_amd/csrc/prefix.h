@@ -12,7 +12,7 @@ struct PrefixArgs {
   const void *q, *ctx_k, *ctx_v, *own_k, *own_v;
   const int32_t *table, *ctx_len, *q_len, *own_len;
   void* out; float* lse;
-  void* out_rest;                       // bf16: what rounding left of out, dense rows (or nullptr)
+  signed char* out_rest;                // bf16: the eight bits below out's, dense rows (or nullptr)
   int B, K, S, Hq, Hkv, dh, T, L, page_rows, n_pages, causal;
   int q_ld, ctx_ld, own_ld, out_ld;
   float scale;

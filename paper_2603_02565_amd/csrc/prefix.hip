@@ -89,15 +89,21 @@ template <typename T>
 FE_DEV void store_out(const PrefixArgs& a, long long at, int col, f32x4 v);
 template <>
 FE_DEV void store_out<bf16>(const PrefixArgs& a, long long at, int col, f32x4 v) {
-  bf16x4 w, r;
+  bf16x4 w;
+  unsigned rest = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     w[q] = (bf16)v[q];
-    r[q] = (bf16)(v[q] - (float)w[q]);
+    // the next eight bits below the rounded value's, as a signed step of its bit pattern
+    const int step = ((int)__float_as_uint(v[q]) - (int)__float_as_uint((float)w[q])) >> 8;
+    rest |= (unsigned)(min(step, 127) & 255) << (8 * q);
   }
   *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.out) + at * a.out_ld + col) = w;
-  if (a.out_rest) *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.out_rest) + at * a.Hq * a.dh + col) = r;
+  if (a.out_rest) *reinterpret_cast<unsigned*>(a.out_rest + at * a.Hq * a.dh + col) = rest;
 }
+// ... and back: out with its rest, to 2^-17.
+FE_DEV float with_rest(bf16 v, int step) { return __uint_as_float(__float_as_uint((float)v) + (step << 8)); }
+FE_DEV float with_rest(float v, int) { return v; }
 template <>
 FE_DEV void store_out<float>(const PrefixArgs& a, long long at, int col, f32x4 v) {
   *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at * a.out_ld + col) = v;
@@ -648,41 +654,10 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
 // Gradient.
 // ------------------------------------------------------------------------------------------
 
-// What the gradient's products need of every row, in the order of the rows of a (request, key head):
+// dq: rows and chunks as in the forward, probabilities again from lse.  Before that it forms what the gradient's products need of
+// every row and leaves it for dk and dv, in the order of the rows of a (request, key head):
 //   x = log2(e) lse (+infinity for a row without keys or past q_len: its probabilities are then 0),
 //   y = dout . out,   z, w = the own rows that it sees, numbered k L + j  [z, w).
-// DH / 8 lanes a row.
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_prefix_rows(PrefixGradArgs p) {
-  const PrefixArgs& a = p.f;
-  constexpr int W = DH / 8;
-  const long long e = (long long)blockIdx.x * (256 / W) + threadIdx.x / W;
-  const int d0 = threadIdx.x % W * 8;
-  if (e >= (long long)a.B * a.Hkv * a.R) return;
-  const int r = (int)(e % a.R), bg = (int)(e / a.R), b = bg / a.Hkv;
-  const Row w = row_of(a, b, bg % a.Hkv, r);
-  float v = 0.f;
-  if (w.live) {
-    const V8<T> o = ld8(static_cast<const T*>(a.out) + w.at * a.out_ld + w.h * DH + d0);
-    const V8<T> d = ld8(static_cast<const T*>(p.dout) + w.at * p.dout_ld + w.h * DH + d0);
-    V8<T> rest = {};
-    if (a.out_rest) rest = ld8(static_cast<const T*>(a.out_rest) + (w.at * a.Hq + w.h) * DH + d0);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v = fmaf(to_f32((T)d[j]), to_f32((T)o[j]) + to_f32((T)rest[j]), v);
-  }
-#pragma unroll
-  for (int m = 1; m < W; m <<= 1) v += __shfl_xor(v, m);
-  if (d0) return;
-  const float lse = w.live ? a.lse[w.at * a.Hq + w.h] : -INFINITY;
-  float4 x;
-  x.x = lse == -INFINITY ? INFINITY : lse * kLog2e;
-  x.y = v;
-  x.z = __int_as_float(w.k * a.L);
-  x.w = __int_as_float(w.k * a.L + w.own);
-  p.rows[e] = x;
-}
-
-// dq: rows and chunks as in the forward, probabilities again from lse.
 template <typename T, int DH, int QT, int NW, int KC>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -767,22 +742,36 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   for (int i = 0; i < QT; ++i) {
     const int r = r0 + (wave * QT + i) * 16 + c16;
     const Row row = row_of(a, b, g, r);
-    const float4 x = p.rows[((long long)b * a.Hkv + g) * a.R + min(r, a.R - 1)];
-    lse2[i] = row.live ? x.x : INFINITY;
-    delta[i] = row.live ? x.y : 0.f;
+    const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH;
+    const T* D = static_cast<const T*>(p.dout) + row.at * p.dout_ld + row.h * DH;
+    const T* O = static_cast<const T*>(a.out) + row.at * a.out_ld + row.h * DH;
+    const signed char* rest = a.out_rest ? a.out_rest + (row.at * a.Hq + row.h) * DH : nullptr;
+    float v = 0.f;
+#pragma unroll
+    for (int c = 0; c < ND; ++c) {
+      qf[i][c] = row.live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
+      df[i][c] = row.live ? ld8(D + c * 32 + g4 * 8) : V8<T>{};
+      const V8<T> out = row.live ? ld8(O + c * 32 + g4 * 8) : V8<T>{};
+      uint2 step = make_uint2(0, 0);
+      if (sizeof(T) == 2 && rest) step = *reinterpret_cast<const uint2*>(rest + c * 32 + g4 * 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int w = (int)((j < 4 ? step.x : step.y) << (24 - 8 * (j & 3))) >> 24;
+        v = fmaf(to_f32((T)df[i][c][j]), with_rest((T)out[j], row.live ? w : 0), v);
+      }
+    }
+    delta[i] = rows_sum(v);
+    const float lse = row.live ? a.lse[row.at * a.Hq + row.h] : -INFINITY;
+    lse2[i] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (z == 0 && g4 == 0 && r < a.R)
+      p.rows[((long long)b * a.Hkv + g) * a.R + r] =
+          make_float4(lse2[i], delta[i], __int_as_float(row.k * a.L), __int_as_float(row.k * a.L + row.own));
     lo[i] = s_off[row.k - k0];
     hi[i] = lo[i] + row.own;
     wlo[i] = __builtin_amdgcn_readlane(lo[i], 0);
     alo[i] = __builtin_amdgcn_readlane(lo[i], 15);
     whi[i] = __builtin_amdgcn_readlane(s_off[row.k - k0 + 1], 15);
     ahi[i] = wlo[i] == alo[i] ? __builtin_amdgcn_readlane(hi[i], 0) : -1;
-    const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH;
-    const T* D = static_cast<const T*>(p.dout) + row.at * p.dout_ld + row.h * DH;
-#pragma unroll
-    for (int c = 0; c < ND; ++c) {
-      qf[i][c] = row.live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
-      df[i][c] = row.live ? ld8(D + c * 32 + g4 * 8) : V8<T>{};
-    }
 #pragma unroll
     for (int n = 0; n < NB; ++n) o[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -1220,14 +1209,11 @@ template <typename T, int DH>
 hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   PrefixArgs& a = p.f;
   const long long rows = (long long)a.B * a.K * a.S * a.Hq, bg = (long long)a.B * a.Hkv;
-  hipLaunchKernelGGL((k_prefix_rows<T, DH>), dim3((unsigned)((rows * (DH / 8) + 255) / 256)), dim3(256), 0, s, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
   a.tiles = pl.tiles;
   a.splits = pl.splits;
   const dim3 gq((unsigned)(bg * a.tiles * a.splits));
   hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, 64>), gq, dim3(256), 0, s, p);
-  e = hipGetLastError();
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.splits > 1) {
     hipLaunchKernelGGL((k_prefix_sum_dq<T, DH>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, s, p);

@@ -717,7 +717,7 @@ class PrefixAttention:
         a, dev = self.args, torch.device("cuda", torch.cuda.current_device())
         self.out = torch.empty((a.B, a.K, a.S, a.n_heads, a.dh), dtype=self.act, device=dev)
         self.lse = torch.empty((a.B, a.K, a.S, a.n_heads), dtype=torch.float32, device=dev) if self.train else None
-        self.out_rest = torch.empty_like(self.out) if self.train and self.act == torch.bfloat16 else None
+        self.out_rest = torch.empty(self.q_shape, dtype=torch.int8, device=dev) if self.train and self.act == torch.bfloat16 else None
         self.ws = torch.empty(max(16, self.ws_bytes), dtype=torch.uint8, device=dev)
         a.out, a.lse, a.out_rest = _ptr(self.out), _ptr(self.lse), _ptr(self.out_rest)
         a.ws, a.ws_bytes = _ptr(self.ws), self.ws_bytes
