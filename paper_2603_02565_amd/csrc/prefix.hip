@@ -1248,7 +1248,8 @@ namespace {
 // 2048: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8) of its result, 1.1e-6 at 6400.
 int ranges(long long wgs, long long items, int most, bool f32) {
   const long long by_size = std::min({512 / std::max(1LL, wgs), items / 3, (long long)most});
-  return (int)std::min(std::max({1LL, by_size, f32 ? (items + 31) / 32 : 1LL}), 256LL);
+  const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);           // a launch holds 2^24 - 1 workgroups of 256
+  return (int)std::max(1LL, std::min({std::max({1LL, by_size, f32 ? (items + 31) / 32 : 1LL}), 256LL, grid}));
 }
 // 64-key chunks that a tile of `rows` rows meets: the shared ones and those of the lists it touches.
 long long chunks_of(const fe_prefix_args& a, long long rows) {

@@ -118,6 +118,23 @@ FORWARD = [
     dict(dtype="bf16", B=1, K=4, S=6, H=2, Hkv=2, dh=64, T=150, L=20, amp=6.0),
     dict(dtype="f32", B=1, K=4, S=6, H=2, Hkv=2, dh=64, T=150, L=20, amp=6.0, scale=0.3),
     dict(dtype="f32", B=1, K=4, S=6, H=2, Hkv=2, dh=32, T=50, L=20, scale=-0.4),
+    # 65 to 128 rows of a key head, in one tile
+    dict(dtype="bf16", B=2, K=25, S=1, H=8, Hkv=2, dh=128, T=150, L=40, P=8),
+    dict(dtype="bf16", B=1, K=5, S=10, H=6, Hkv=3, dh=128, T=90, L=10, lens="own"),
+    dict(dtype="bf16", B=2, K=11, S=2, H=8, Hkv=2, dh=64, T=70, L=33, P=4),
+    dict(dtype="f32", B=2, K=7, S=5, H=6, Hkv=2, dh=32, T=70, L=21),
+    dict(dtype="f32", B=1, K=16, S=1, H=8, Hkv=1, dh=64, T=200, L=30, P=30, lens="edge"),
+    # many tiles of 128 rows
+    dict(dtype="bf16", B=128, K=2, S=64, H=8, Hkv=4, dh=32, T=5, L=64, lens="own"),
+    # one long list, causal, over several tiles and chunks; lists of different lengths in one tile
+    dict(dtype="bf16", B=1, K=1, S=333, H=1, Hkv=1, dh=64, T=0, L=333, lens="full"),
+    dict(dtype="f32", B=1, K=2, S=200, H=3, Hkv=1, dh=32, T=33, L=260),
+    # groups of heads that no power of two divides
+    dict(dtype="bf16", B=1, K=3, S=9, H=5, Hkv=1, dh=32, T=20, L=9, lens="own"),
+    # equal weights
+    dict(dtype="bf16", B=1, K=3, S=4, H=2, Hkv=2, dh=32, T=45, L=9, scale=0.0),
+    # fp32 sums longer than one chain, with workgroups to spare
+    dict(dtype="f32", B=8, K=1, S=1, H=8, Hkv=8, dh=32, T=4500, L=2, lens="full"),
     # few rows over many keys
     dict(dtype="bf16", B=1, K=2, S=1, H=2, Hkv=1, dh=64, T=5000, L=300, P=16),
     dict(dtype="f32", B=1, K=1, S=2, H=1, Hkv=1, dh=128, T=3001, L=3, lens="full"),
@@ -154,6 +171,15 @@ GRAD = [
     dict(dtype="f32", B=6, K=7, S=4, H=2, Hkv=1, dh=32, T=33, L=20, lens="edge"),
     dict(dtype="bf16", B=1, K=2, S=1, H=2, Hkv=2, dh=64, T=700, L=90, causal=False),
     dict(dtype="bf16", B=1, K=40, S=5, H=4, Hkv=1, dh=32, T=65, L=5, causal=False, lens="own"),
+    # one long list; own rows longer than the query rows; groups of 3 and 5; a negative scale; equal weights
+    dict(dtype="bf16", B=1, K=1, S=200, H=2, Hkv=1, dh=64, T=10, L=200, lens="full"),
+    dict(dtype="f32", B=1, K=2, S=30, H=3, Hkv=1, dh=32, T=20, L=150),
+    dict(dtype="bf16", B=1, K=4, S=13, H=10, Hkv=2, dh=32, T=50, L=13, lens="own"),
+    dict(dtype="f32", B=2, K=3, S=5, H=2, Hkv=2, dh=64, T=40, L=9, scale=-0.3),
+    dict(dtype="f32", B=1, K=2, S=5, H=2, Hkv=2, dh=32, T=30, L=9, scale=0.0),
+    # more rows than one fp32 chain
+    dict(dtype="f32", B=1, K=60, S=20, H=2, Hkv=1, dh=32, T=70, L=20, causal=False, lens="own"),
+    dict(dtype="bf16", B=2, K=30, S=20, H=4, Hkv=1, dh=128, T=20, L=20, lens="own"),
 ]
 NAMES = ("dq", "dck", "dcv", "dok", "dov")
 
@@ -174,6 +200,51 @@ def test_grad(i):
     first = [g.clone() for g in grads]
     for g in p.grad(dout, *c.keys, **c.more), :
         assert all(torch.equal(a, b) for a, b in zip(first, g))
+
+
+def test_grad_without_the_rest_of_out():
+    """Without out_rest the gradient takes dout . out from the rounded out (the bound covers both)."""
+    c = Case(dtype="bf16", B=2, K=3, S=9, H=4, Hkv=2, dh=64, T=40, L=9, lens="own", seed=77).device()
+    p = fe.PrefixAttention(train=True, **c.dims)
+    p.run(*c.keys, **c.more)
+    dout = torch.tensor(c.do).bfloat16().cuda()
+    kept = [g.clone() for g in p.grad(dout, *c.keys, **c.more)]
+    p.args.out_rest = None
+    want = c.reference(grad=True)
+    differs = False
+    for name, g, k in zip(NAMES, p.grad(dout, *c.keys, **c.more), kept):
+        _near(g, want[name], name)
+        differs |= not torch.equal(g, k)
+    assert differs
+
+
+def test_two_calls_at_once():
+    """Two objects on two streams, many calls in flight: each keeps its own outputs and workspace."""
+    cases = [Case(dtype="bf16", B=1, K=4, S=1, H=4, Hkv=2, dh=64, T=3000, L=48, P=16, seed=s).device() for s in (41, 42)]
+    plans = [fe.PrefixAttention(**c.dims) for c in cases]
+    want = [p.run(*c.keys, **c.more).clone() for p, c in zip(plans, cases)]
+    streams = [torch.cuda.Stream() for _ in plans]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for p, c, s in zip(plans, cases, streams):
+            p.run(*c.keys, stream=s, **c.more)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p.out, w) for p, w in zip(plans, want))
+
+
+def test_lists_do_not_depend_on_each_other():
+    """The same list beside other lists of the same lengths: the same bits."""
+    c = Case(dtype="bf16", B=1, K=12, S=7, H=4, Hkv=2, dh=64, T=100, L=15, seed=61).device()
+    p = fe.PrefixAttention(**c.dims)
+    want = p.run(*c.keys, **c.more).clone()
+    other = [t.clone() for t in c.keys]
+    keep = [0, 5, 11]
+    for i in (0, 3, 4):                                  # queries, own keys, own values of the other lists
+        new = torch.randn(other[i].shape, device="cuda").bfloat16() * 3
+        new[:, keep] = other[i][:, keep]
+        other[i] = new
+    got = p.run(*other, **c.more)
+    assert torch.equal(got[:, keep], want[:, keep])
 
 
 def test_grad_matches_differences():
