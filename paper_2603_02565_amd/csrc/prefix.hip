@@ -1153,29 +1153,35 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
   }
 }
 
-// Adds the partial sums of dq (key ranges) and of dk, dv (row ranges) in ascending order.
+// Adds the partial sums of dq (key ranges) and of dk and dv (row ranges) in ascending order, in one launch: the first
+// blocks[0] workgroups dq, the next blocks[1] the shared keys, the rest the own keys.
+struct SumBlocks { unsigned dq, ctx; };
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_prefix_sum_dq(PrefixGradArgs p) {
+__global__ __launch_bounds__(256) void k_prefix_sum(PrefixGradArgs p, SumBlocks blocks) {
   const PrefixArgs& a = p.f;
-  const long long rows = (long long)a.B * a.K * a.S * a.Hq;
-  const long long e = (long long)blockIdx.x * 256 + threadIdx.x, ro = e / (DH / 4);
-  const int d0 = (int)(e % (DH / 4)) * 4;
-  if (ro >= rows) return;
+  unsigned blk = blockIdx.x;
+  const float* part;
+  long long n;                          // rows, or keys with dk and dv side by side
+  int splits, heads, ld, width = 2 * DH;
+  T *dst, *dst_v = nullptr;
+  if (blk < blocks.dq) {                // uniform
+    part = a.part_o; n = (long long)a.B * a.K * a.S * a.Hq; splits = a.splits; heads = a.Hq; ld = p.dq_ld; width = DH;
+    dst = static_cast<T*>(p.dq);
+  } else if ((blk -= blocks.dq) < blocks.ctx) {
+    part = p.part_ctx; n = (long long)a.B * a.T * a.Hkv; splits = p.ctx_splits; heads = a.Hkv; ld = p.dctx_ld;
+    dst = static_cast<T*>(p.dctx_k); dst_v = static_cast<T*>(p.dctx_v);
+  } else {
+    blk -= blocks.ctx;
+    part = p.part_own; n = (long long)a.B * a.K * a.L * a.Hkv; splits = p.own_splits; heads = a.Hkv; ld = p.down_ld;
+    dst = static_cast<T*>(p.down_k); dst_v = static_cast<T*>(p.down_v);
+  }
+  const long long e = (long long)blk * 256 + threadIdx.x, row = e / (width / 4);
+  const int d0 = (int)(e % (width / 4)) * 4;
+  if (row >= n) return;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int z = 0; z < a.splits; ++z) v += *reinterpret_cast<const f32x4*>(a.part_o + (z * rows + ro) * DH + d0);
-  st4(static_cast<T*>(p.dq) + ro / a.Hq * p.dq_ld + ro % a.Hq * DH + d0, v);
-}
-// n_keys keys of dk, dv with row stride ld; part [splits][n_keys][2][DH]
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_prefix_sum_dkv(const float* part, long long n_keys, int splits, int Hkv, int ld, T* dk, T* dv) {
-  const long long e = (long long)blockIdx.x * 256 + threadIdx.x, key = e / (DH / 2);
-  const int d0 = (int)(e % (DH / 2)) * 4;                               // dk, then dv
-  if (key >= n_keys) return;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int z = 0; z < splits; ++z) v += *reinterpret_cast<const f32x4*>(part + (z * n_keys + key) * 2 * DH + d0);
-  st4((d0 >= DH ? dv : dk) + key / Hkv * ld + key % Hkv * DH + d0 % DH, v);
+  for (int z = 0; z < splits; ++z) v += *reinterpret_cast<const f32x4*>(part + (z * n + row) * width + d0);
+  st4((d0 >= DH ? dst_v : dst) + row / heads * ld + row % heads * DH + d0 % DH, v);
 }
 
 // Tile shapes.  Forward and dq: QT 16-row tiles a wave; dkv: KT 16-key tiles a wave and RC rows a chunk.
@@ -1215,28 +1221,22 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, 64>), gq, dim3(256), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.splits > 1) {
-    hipLaunchKernelGGL((k_prefix_sum_dq<T, DH>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, s, p);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   p.ctx_tiles = pl.ctx_tiles;
   p.own_tiles = pl.own_tiles;
   p.ctx_splits = pl.ctx_splits;
   p.own_splits = pl.own_splits;
-  if (p.ctx_tiles + p.own_tiles == 0) return hipSuccess;
-  const dim3 gk((unsigned)(bg * (p.ctx_tiles * p.ctx_splits + p.own_tiles * p.own_splits)));
-  hipLaunchKernelGGL((k_prefix_dkv<T, DH, kKT<T, DH>, 4, kRC<T, DH>>), gk, dim3(256), 0, s, p);
-  e = hipGetLastError();
-  auto sum = [&](const float* part, long long keys, int splits, int ld, void* dk, void* dv) {
-    if (e != hipSuccess || splits == 1 || keys == 0) return;
-    hipLaunchKernelGGL((k_prefix_sum_dkv<T, DH>), dim3((unsigned)((keys * (DH / 2) + 255) / 256)), dim3(256), 0, s, part, keys, splits,
-                       a.Hkv, ld, static_cast<T*>(dk), static_cast<T*>(dv));
+  if (p.ctx_tiles + p.own_tiles > 0) {
+    const dim3 gk((unsigned)(bg * (p.ctx_tiles * p.ctx_splits + p.own_tiles * p.own_splits)));
+    hipLaunchKernelGGL((k_prefix_dkv<T, DH, kKT<T, DH>, 4, kRC<T, DH>>), gk, dim3(256), 0, s, p);
     e = hipGetLastError();
-  };
-  sum(p.part_ctx, (long long)a.B * a.T * a.Hkv, p.ctx_splits, p.dctx_ld, p.dctx_k, p.dctx_v);
-  sum(p.part_own, (long long)a.B * a.K * a.L * a.Hkv, p.own_splits, p.down_ld, p.down_k, p.down_v);
-  return e;
+    if (e != hipSuccess) return e;
+  }
+  auto blocks_of = [](int splits, long long n, int width) { return splits > 1 ? (unsigned)((n * (width / 4) + 255) / 256) : 0u; };
+  const SumBlocks blocks{blocks_of(a.splits, rows, DH), blocks_of(p.ctx_splits, (long long)a.B * a.T * a.Hkv, 2 * DH)};
+  const unsigned all = blocks.dq + blocks.ctx + blocks_of(p.own_splits, (long long)a.B * a.K * a.L * a.Hkv, 2 * DH);
+  if (all == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_prefix_sum<T, DH>), dim3(all), dim3(256), 0, s, p, blocks);
+  return hipGetLastError();
 }
 
 }  // namespace
