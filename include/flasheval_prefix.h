@@ -15,8 +15,8 @@
  *   fe_prefix_workspace_size  workspace bytes of the two attention calls
  *
  * Conventions are those of flasheval.h: device pointers owned by the caller, nothing allocated and
- * nothing waited for, asynchronous on `stream`, host-side validation before any launch, one
- * workspace not used by two streams (or two captured graphs that may run at once) at a time.  The calls hold no state: they can be
+ * nothing waited for, asynchronous on `stream`, host-side validation before any launch, one workspace not used
+ * by two streams (or two captured graphs that may run at once) at a time.  The calls hold no state: they can be
  * captured into a graph and replayed.  Tensors, workspace and stream belong to the current device.
  * Pointers are 16-byte aligned (int32 and double arrays as their type) and row strides are multiples
  * of 16 bytes.  Offsets into the caches are 64-bit.
@@ -128,7 +128,8 @@ typedef struct {
   const int32_t* own_len;               /* [B][K], or NULL: L */
   void* out;                            /* [B][K][S] rows of n_heads * dh */
   float* lse;                           /* [B][K][S][n_heads], or NULL (the gradient needs it) */
-  void* out_rest;                       /* FE_BF16: [B][K][S][n_heads * dh] bytes, the bits that the rounding of out cut, or NULL */
+  void* out_rest;                       /* FE_BF16: [B][K][S][n_heads * dh] bytes, the eight bits that the rounding of
+                                           out cut (16-byte aligned), or NULL */
   void* ws;
   size_t ws_bytes;
 } fe_prefix_args;
@@ -136,15 +137,15 @@ fe_status fe_prefix_workspace_size(const fe_prefix_args* a, int grad, size_t* by
 fe_status fe_prefix_attention(const fe_prefix_args* a, void* stream);
 
 /*
- * Gradients of fe_prefix_attention for d loss / d out = dout.  `a` holds the forward's arguments with
- * its out and lse (and out_rest: without it FE_BF16 takes D from the rounded out) and a workspace of fe_prefix_workspace_size(a, 1) bytes; own rows must be dense
- * (FE_EUNSUPPORTED otherwise).  With D = dout.out, dp = dout.v and ds = p (dp - D):
+ * Gradients of fe_prefix_attention for d loss / d out = dout.  `a` holds the forward's arguments with its out and
+ * lse (and out_rest: without it FE_BF16 takes D from the rounded out) and a workspace of
+ * fe_prefix_workspace_size(a, 1) bytes; own rows must be dense (FE_EUNSUPPORTED otherwise).  With D = dout.out, dp = dout.v and ds = p (dp - D):
  *   dq = scale sum ds k,   dk = scale sum ds q,   dv = sum p dout,
  * where a key's sums run over every list (shared rows), row and head that reads it.  Every row of dq, of the shared
  * gradients [B][T] and of the own gradients [B][K][L] is written; rows outside the lengths are zero.  dout
  * rows i >= q_len are not read into anything.  Sums are fp32, in a fixed order without atomics, rounded
- * once; FE_BF16 rounds p and ds to bf16 for the products.  Values inside the lengths have to be finite: one that is not may
- * reach the gradients of the other lists of its request.
+ * once; FE_BF16 rounds p and ds to bf16 for the products.  Values inside the lengths have to be finite: one that is
+ * not may reach the gradients of the other lists of its request.
  * dctx_k, dctx_v (own: down_k, down_v) may be NULL only when T (L) is 0.
  */
 typedef struct {

@@ -35,10 +35,13 @@ fe_status check_sizes(const fe_prefix_args* a) {
   if (a->T < 0 || a->L < 0) return pfail(FE_EINVAL, "T and L must be >= 0");
   if (a->n_heads % a->n_kv_heads)
     return pfail(FE_EINVAL, "n_heads=%d is not a multiple of n_kv_heads=%d", a->n_heads, a->n_kv_heads);
-  if (a->page_rows < 0 || (a->page_rows > 0 && a->n_pages < 1)) return pfail(FE_EINVAL, "page_rows=%d, n_pages=%d", a->page_rows, a->n_pages);
-  if (a->page_rows > 0 && a->L % a->page_rows) return pfail(FE_EINVAL, "L=%d is not a multiple of page_rows=%d", a->L, a->page_rows);
+  if (a->page_rows < 0 || (a->page_rows > 0 && a->n_pages < 1))
+    return pfail(FE_EINVAL, "page_rows=%d, n_pages=%d", a->page_rows, a->n_pages);
+  if (a->page_rows > 0 && a->L % a->page_rows)
+    return pfail(FE_EINVAL, "L=%d is not a multiple of page_rows=%d", a->L, a->page_rows);
   if (a->dh != 32 && a->dh != 64 && a->dh != 128) return pfail(FE_EUNSUPPORTED, "head width %d not in {32,64,128}", a->dh);
-  if (a->T > kPrefixMaxLen || a->L > kPrefixMaxLen) return pfail(FE_EUNSUPPORTED, "T=%d or L=%d above %d", a->T, a->L, kPrefixMaxLen);
+  if (a->T > kPrefixMaxLen || a->L > kPrefixMaxLen)
+    return pfail(FE_EUNSUPPORTED, "T=%d or L=%d above %d", a->T, a->L, kPrefixMaxLen);
   const double most = 1073741823., lists = (double)a->B * a->K;
   if (lists * a->S * a->n_heads > most || (double)a->B * a->T > most || lists * a->L > most)
     return pfail(FE_EUNSUPPORTED, "batch too large: more than %.0f rows", most);
@@ -64,7 +67,8 @@ fe_status check_forward(const fe_prefix_args* a) {
   if (!aligned(a->q, 16) || !aligned(a->out, 16) || !aligned(a->ctx_k, 16) || !aligned(a->ctx_v, 16) ||
       !aligned(a->own_k, 16) || !aligned(a->own_v, 16) || !aligned(a->out_rest, 16) || !aligned(a->ws, 16))
     return pfail(FE_EINVAL, "pointers must be 16-byte aligned");
-  if (!aligned(a->table, 4) || !aligned(a->ctx_len, 4) || !aligned(a->q_len, 4) || !aligned(a->own_len, 4) || !aligned(a->lse, 4))
+  if (!aligned(a->table, 4) || !aligned(a->ctx_len, 4) || !aligned(a->q_len, 4) || !aligned(a->own_len, 4) ||
+      !aligned(a->lse, 4))
     return pfail(FE_EINVAL, "tables, lengths and lse must be 4-byte aligned");
   if (!stride_ok(a->q_ld, wq, a->dtype) || !stride_ok(a->out_ld, wq, a->dtype) ||
       (a->T > 0 && !stride_ok(a->ctx_ld, wk, a->dtype)) || (a->L > 0 && !stride_ok(a->own_ld, wk, a->dtype)))
@@ -74,7 +78,9 @@ fe_status check_forward(const fe_prefix_args* a) {
 }
 
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
-size_t grad_bytes(const PrefixGradPlan& p) { return up256(p.rows_bytes) + up256(p.dq_bytes) + up256(p.ctx_bytes) + up256(p.own_bytes); }
+size_t grad_bytes(const PrefixGradPlan& p) {
+  return up256(p.rows_bytes) + up256(p.dq_bytes) + up256(p.ctx_bytes) + up256(p.own_bytes);
+}
 
 PrefixArgs kernel_args(const fe_prefix_args& a) {
   PrefixArgs k{};
@@ -136,7 +142,8 @@ fe_status fe_prefix_attention_grad(const fe_prefix_args* a, const fe_prefix_grad
     return pfail(FE_EINVAL, "a row stride is shorter than its row or not a multiple of 16 bytes");
   const PrefixGradPlan p = prefix_grad_plan(*a);
   const size_t need = grad_bytes(p);
-  if (!a->ws || a->ws_bytes < need) return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);
+  if (!a->ws || a->ws_bytes < need)
+    return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);
   PrefixGradArgs k{};
   k.f = kernel_args(*a);
   k.dout = g->dout; k.dout_ld = g->dout_ld;
@@ -159,19 +166,21 @@ fe_status fe_prefix_attention_grad(const fe_prefix_args* a, const fe_prefix_grad
 fe_status fe_cache_append(const fe_append_args* a, void* stream) {
   if (!a) return pfail(FE_EINVAL, "arguments are NULL");
   if (a->dtype != FE_F32 && a->dtype != FE_BF16) return pfail(FE_EINVAL, "dtype %d is not FE_F32 or FE_BF16", a->dtype);
-  if (a->N < 1 || a->S < 1 || a->n_kv_heads < 1 || a->page_rows < 1 || a->n_pages < 1 || a->table_cols < 1 || (a->q && a->n_heads < 1))
+  if (a->N < 1 || a->S < 1 || a->n_kv_heads < 1 || a->page_rows < 1 || a->n_pages < 1 || a->table_cols < 1 ||
+      (a->q && a->n_heads < 1))
     return pfail(FE_EINVAL, "N, S, heads, page_rows, n_pages and table_cols must be >= 1");
   if (a->dh != 32 && a->dh != 64 && a->dh != 128) return pfail(FE_EUNSUPPORTED, "head width %d not in {32,64,128}", a->dh);
-  if (a->rot < 0 || a->rot > a->dh || a->rot % 2) return pfail(FE_EINVAL, "rot=%d is not an even number in [0, %d]", a->rot, a->dh);
+  if (a->rot < 0 || a->rot > a->dh || a->rot % 2)
+    return pfail(FE_EINVAL, "rot=%d is not an even number in [0, %d]", a->rot, a->dh);
   if (a->rot % 16) return pfail(FE_EUNSUPPORTED, "rot=%d is not a multiple of 16", a->rot);
   if (!a->k || !a->v || !a->k_pages || !a->v_pages || !a->table || !a->len) return pfail(FE_EINVAL, "NULL pointer argument");
   if ((a->q == nullptr) != (a->q_out == nullptr)) return pfail(FE_EINVAL, "q and q_out go together");
   if (a->rot > 0 && !a->freq) return pfail(FE_EINVAL, "rot=%d without freq", a->rot);
-  if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->k_pages, 16) || !aligned(a->v_pages, 16) || !aligned(a->q, 16) ||
-      !aligned(a->q_out, 16))
+  if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->k_pages, 16) || !aligned(a->v_pages, 16) ||
+      !aligned(a->q, 16) || !aligned(a->q_out, 16))
     return pfail(FE_EINVAL, "pointers must be 16-byte aligned");
-  if (!aligned(a->freq, 8) || !aligned(a->table, 4) || !aligned(a->len, 4) || !aligned(a->new_len, 4) || !aligned(a->pos0, 4) ||
-      !aligned(a->len_out, 4) || !aligned(a->status, 4))
+  if (!aligned(a->freq, 8) || !aligned(a->table, 4) || !aligned(a->len, 4) || !aligned(a->new_len, 4) ||
+      !aligned(a->pos0, 4) || !aligned(a->len_out, 4) || !aligned(a->status, 4))
     return pfail(FE_EINVAL, "freq must be 8-byte aligned, tables, lengths and status 4-byte aligned");
   const long long wk = (long long)a->n_kv_heads * a->dh, wq = a->q ? (long long)a->n_heads * a->dh : 0;
   if (!stride_ok(a->k_ld, wk, a->dtype) || !stride_ok(a->v_ld, wk, a->dtype) || !stride_ok(a->page_ld, wk, a->dtype) ||
@@ -179,7 +188,8 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream) {
     return pfail(FE_EINVAL, "a row stride is shorter than its row or not a multiple of 16 bytes");
   if ((long long)a->N * a->S > kInt32 || (long long)a->table_cols * a->page_rows > kInt32 || wq + 2 * wk > kInt32 / 4)
     return pfail(FE_EINVAL, "sizes overflow int32");
-  if ((long long)a->N * a->S > kMaxGrid) return pfail(FE_EUNSUPPORTED, "N*S=%lld rows above %lld", (long long)a->N * a->S, kMaxGrid);
+  if ((long long)a->N * a->S > kMaxGrid)
+    return pfail(FE_EUNSUPPORTED, "N*S=%lld rows above %lld", (long long)a->N * a->S, kMaxGrid);
   const hipError_t e = launch_cache_append(*a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? FE_OK : pfail(FE_EHIP, "cache append launch failed: %s", hipGetErrorString(e));
 }

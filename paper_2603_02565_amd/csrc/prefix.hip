@@ -14,9 +14,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Eight consecutive elements along the summed axis: one operand of the 16 x 16 x 32 bf16 product, or
-// of eight 16 x 16 x 4 fp32 ones.  Lane l holds row (or column) l % 16 and elements 8 (l / 16) + j; product j
-// of the fp32 form sums over {8 g + j}, so both types use one layout.
+// Eight elements along the summed axis: one operand of the 16 x 16 x 32 bf16 product, or of eight 16 x 16 x 4 fp32 ones.
+// Lane l holds row (or column) l % 16 and the eight elements of its group l / 16; product j of the fp32 form sums over
+// element j of the four groups, so both types use one layout, and which element is which is free as long as both operands agree.
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> { typedef bf16x8 type; };
@@ -46,7 +46,9 @@ FE_DEV void st4(bf16* p, f32x4 v) {
 
 // Eight floats rounded to T (round to nearest even).
 template <typename T> FE_DEV V8<T> pack8(const float (&s)[8]);
-template <> FE_DEV f32x8 pack8<float>(const float (&s)[8]) { return f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}; }
+template <> FE_DEV f32x8 pack8<float>(const float (&s)[8]) {
+  return f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]};
+}
 template <> FE_DEV bf16x8 pack8<bf16>(const float (&s)[8]) {
   return __builtin_convertvector((f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}), bf16x8);
 }
@@ -67,12 +69,6 @@ FE_DEV bool finite8(f32x8 v) {
 }
 
 FE_DEV int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
-FE_DEV int wave_min(int v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = min(v, __shfl_xor(v, m));
-  return __builtin_amdgcn_readfirstlane(v);
-}
-FE_DEV int wave_max(int v) { return -wave_min(-v); }
 
 FE_DEV int q_rows(const PrefixArgs& a, int bk) { return a.q_len ? clampi(a.q_len[bk], 0, a.S) : a.S; }
 FE_DEV int own_rows(const PrefixArgs& a, int bk) { return a.own_len ? clampi(a.own_len[bk], 0, a.L) : a.L; }
@@ -94,15 +90,15 @@ FE_DEV void store_out<bf16>(const PrefixArgs& a, long long at, int col, f32x4 v)
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     w[q] = (bf16)v[q];
-    // the next eight bits below the rounded value's, as a signed step of its bit pattern
+    // the eight bits below the rounded value's, as a signed step of its bit pattern
     const int step = ((int)__float_as_uint(v[q]) - (int)__float_as_uint((float)w[q])) >> 8;
     rest |= (unsigned)(min(step, 127) & 255) << (8 * q);
   }
   *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.out) + at * a.out_ld + col) = w;
   if (a.out_rest) *reinterpret_cast<unsigned*>(a.out_rest + at * a.Hq * a.dh + col) = rest;
 }
-// ... and back: out with its rest, to 2^-17.
-FE_DEV float with_rest(bf16 v, int step) { return __uint_as_float(__float_as_uint((float)v) + (step << 8)); }
+// ... and back: out with its rest, to 2^-16.
+FE_DEV float with_rest(bf16 v, int step) { return __uint_as_float(__float_as_uint((float)v) + step * 256); }
 FE_DEV float with_rest(float v, int) { return v; }
 template <>
 FE_DEV void store_out<float>(const PrefixArgs& a, long long at, int col, f32x4 v) {
@@ -150,9 +146,9 @@ FE_DEV int packed_list(const int* off, int nb, int c) {
   return lo;
 }
 
-// Where row c of the lists packed in off lies in own_k / own_v: find() says it, row() turns it into the row's number, -2 past
-// the last row, -1 for a page outside the pool.  A page is requested by find() and looked at by row(), a chunk later, so that
-// nothing waits for the table.
+// Where row c of the lists packed in off lies in own_k / own_v: find() says it, row() turns it into the row's number,
+// -2 past the last row, -1 for a page outside the pool.  A page is requested by find() and looked at by row(), a chunk
+// later, so that nothing waits for the table.
 template <bool PAGED> struct OwnAt;
 template <> struct OwnAt<false> {
   long long at = -2;
@@ -199,27 +195,33 @@ FE_DEV Row row_of(const PrefixArgs& a, int b, int g, int r) {
   return w;
 }
 
-// A tile of rows of DH elements in LDS, read as an operand along its rows (summed over columns) and along its columns (summed
-// over rows).  bf16: rows of DH without padding, their 16-byte units exchanged inside a row, so that 16 rows at one unit and
-// 8 rows at one pair of units both fall on all 64 banks; fp32: rows of DH + 4.
+// A tile of rows of DH elements in LDS, read as an operand along its rows (summed over columns) and along its columns
+// (summed over rows).  bf16: rows of DH without padding, their 16-byte units exchanged inside a row, so that 16 rows at
+// one unit and 8 rows at one pair of units both fall on all 64 banks (measured: a row read 8.4 cycles, 7.9 at best; a
+// transposed one 10.1, the same at every stride); fp32: rows of DH + 4.
 //
 // Both reads start from a number that depends on the lane alone (row_lane, col_lane); what differs from read to read is a
 // constant xor and a row offset.
 template <typename T, int DH> struct Tile;
 template <int DH> struct Tile<bf16, DH> {
-  static constexpr int LD = DH, UNITS = DH / 8, PER = 128 / DH;        // PER rows span the banks; the exchange repeats every 16 rows
-  static FE_DEV int swap(int row) {
+  static constexpr int LD = DH, UNITS = DH / 8, PER = 128 / DH;   // PER rows span the banks
+  static FE_DEV int swap(int row) {                // repeats every 16 rows
     const int h = row / PER % UNITS;
     return (h % (UNITS / 2)) << 1 | h / (UNITS / 2);
   }
   static FE_DEV int at(int row, int unit) { return row * DH + ((unit ^ swap(row)) << 3); }
-  // Operand along rows: lane l is row base + l % 16, its elements are columns 32 d + 8 (l / 16) + j (base a multiple of 16).
+  // Operand along rows: lane l is row base + l % 16, its elements are columns 32 d + 8 (l / 16) + j (base a multiple
+  // of 16).
   static FE_DEV int row_lane(int lane) { return at(lane & 15, lane >> 4); }
-  static FE_DEV bf16x8 rows(const bf16* X, int base, int d, int row_lane) { return ld8(X + base * DH + (row_lane ^ (d << 5))); }
+  static FE_DEV bf16x8 rows(const bf16* X, int base, int d, int row_lane) {
+    return ld8(X + base * DH + (row_lane ^ (d << 5)));
+  }
   // Operand along columns: lane l is column 16 n + l % 16; its elements 4 x + j are rows base + 16 x + 4 (l / 16) + j, the
   // order in which a lane holds the results of two 16-row products.  Each group of 16 lanes reads a 4 x 16 block
   // transposed (ds_read_b64_tr_b16).
-  static FE_DEV int col_lane(int lane) { return at(4 * (lane >> 4) + ((lane & 15) >> 2), (lane & 3) >> 1) + (lane & 1) * 4; }
+  static FE_DEV int col_lane(int lane) {
+    return at(4 * (lane >> 4) + ((lane & 15) >> 2), (lane & 3) >> 1) + (lane & 1) * 4;
+  }
   static FE_DEV bf16x8 cols(const bf16* X, int base, int n, int col_lane) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
@@ -233,7 +235,9 @@ template <int DH> struct Tile<float, DH> {
   static constexpr int LD = DH + 4;
   static FE_DEV int at(int row, int unit) { return row * LD + unit * 8; }
   static FE_DEV int row_lane(int lane) { return at(lane & 15, lane >> 4); }
-  static FE_DEV f32x8 rows(const float* X, int base, int d, int row_lane) { return ld8(X + base * LD + row_lane + d * 32); }
+  static FE_DEV f32x8 rows(const float* X, int base, int d, int row_lane) {
+    return ld8(X + base * LD + row_lane + d * 32);
+  }
   static FE_DEV int col_lane(int lane) { return 4 * (lane >> 4) * LD + (lane & 15); }
   static FE_DEV f32x8 cols(const float* X, int base, int n, int col_lane) {
     const float* p = X + base * LD + col_lane + n * 16;
@@ -250,9 +254,11 @@ FE_DEV int fresh(int x) {
 }
 
 // Waves per SIMD that the register file is shared between (more hide more latency; fewer would spill).
-constexpr int waves_of(int bytes, int dh, int qt) { return dh == 128 ? 2 : bytes == 2 && dh * qt <= 64 ? 4 : dh * qt <= 64 || bytes == 2 ? 3 : 2; }
+constexpr int waves_of(int bytes, int dh, int qt) {
+  return dh == 128 ? 2 : bytes == 2 && dh * qt <= 64 ? 4 : dh * qt <= 64 || bytes == 2 ? 3 : 2;
+}
+constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 
-constexpr int dkv_waves(int bytes, int dh) { return dh == 32 ? 3 : 2; }
 // ------------------------------------------------------------------------------------------
 // Forward.  NW waves of QT 16-row tiles; chunks of KC keys staged through registers (the next chunk's loads in
 // flight behind this one's products) into LDS.  Scores are formed transposed (keys x rows): a lane then holds
@@ -405,10 +411,11 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   auto max8 = [&](const float (&s)[8]) __attribute__((always_inline)) {
     return fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
   };
-  // Moves the reference of tile i's rows to mx (this lane's largest product) where that is more than `lag` above it.  The reference is the running
-  // maximum, but it follows only once a score is 8 / log2(e) above it (a probability is then at most 2^8, of no
-  // consequence to fp32 sums or to bf16's relative rounding): with the exact maximum some row of a tile moves in most steps.
-  // Whether a row's reference moves depends on that row alone.
+  // Moves the reference of tile i's rows to the largest product (mx: this lane's) where that is more than `lag` above
+  // it.  The reference is the running maximum, but it follows only once a score is 8 / log2(e) above it: a probability
+  // is then at most 2^8, of no consequence to fp32 sums or to bf16's relative rounding, while with the exact maximum
+  // some row of a tile moves in most steps (32 x 64 x 1024 rows: 40.6 us, 39.2 so).  Whether a row's reference moves
+  // depends on that row alone.
   auto follow = [&](int i, float mx) __attribute__((always_inline)) {
     const float top = rows_max(mx);
     if (top > m_run[i] + lag) {
@@ -593,7 +600,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       }
       continue;
     }
-    const bool none = !row[i].live || m_run[i] == -INFINITY;
+    const bool none = !row[i].live || l == 0.f;    // no key; a NaN score leaves a NaN sum
     const float inv = none ? 0.f : 1.f / l;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -642,7 +649,7 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
       if (ml[u].x != -INFINITY) o += w * v[u];     // a range without keys for the row says nothing
     }
   }
-  const bool none = dead || m == -INFINITY;
+  const bool none = dead || l == 0.f;
   const float inv = none ? 0.f : 1.f / l;
 #pragma unroll
   for (int q = 0; q < 4; ++q) o[q] = none ? 0.f : o[q] * inv;
@@ -654,8 +661,8 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
 // Gradient.
 // ------------------------------------------------------------------------------------------
 
-// dq: rows and chunks as in the forward, probabilities again from lse.  Before that it forms what the gradient's products need of
-// every row and leaves it for dk and dv, in the order of the rows of a (request, key head):
+// dq: rows and chunks as in the forward, probabilities again from lse.  Before that it forms what the gradient's
+// products need of every row and leaves it for dk and dv, in the order of the rows of a (request, key head):
 //   x = log2(e) lse (+infinity for a row without keys or past q_len: its probabilities are then 0),
 //   y = dout . out,   z, w = the own rows that it sees, numbered k L + j  [z, w).
 template <typename T, int DH, int QT, int NW, int KC>
@@ -833,7 +840,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       for (int i = 0; i < QT; ++i) {
         float e[8];
         dscores(Ks, Vs, 32 * u, rl, i, e);
-        if (left < KC) {                           // uniform; keys past the length are zeros, but their probability may be anything
+        if (left < KC) {                           // uniform; a key past the length is zero, its probability may be anything
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             if (32 * u + key_of(j, g4) >= left) e[j] = 0.f;
@@ -910,7 +917,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 // hold own rows (dense, list after list) and meet the rows of their lists.  In the tile's numbering -- shared row, or
 // k L + j -- the keys that a row sees are again one interval.  Few tiles: several workgroups share a tile's rows.
 template <typename T, int DH, int KT, int NW, int RC>
-__global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dkv(PrefixGradArgs p) {
+__global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, COLS = NW * KT * 16, NB = DH / 16, ND = DH / 32;
   typedef Tile<T, DH> L;
@@ -950,8 +957,9 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
   const float4* rows = p.rows + ((long long)b * a.Hkv + g) * a.R;
   // Rows past the end repeat the last one, with lse = infinity.
   const T *q_base = static_cast<const T*>(a.q), *d_base = static_cast<const T*>(p.dout);
-  const bool even = RC % a.G == 0 && a.q_ld <= (1 << 23) && p.dout_ld <= (1 << 23);   // uniform: a chunk's rows lie as the first one's do
-  unsigned q_at[PER_T], d_at[PER_T];               // ... and these are their byte offsets
+  // uniform: every chunk's rows lie as the first one's do, and q_at, d_at are their byte offsets
+  const bool even = RC % a.G == 0 && a.q_ld <= (1 << 23) && p.dout_ld <= (1 << 23);
+  unsigned q_at[PER_T], d_at[PER_T];
 #pragma unroll
   for (int q = 0; q < PER_T; ++q) {
     const int i = i0 + q * STEP;
@@ -1007,7 +1015,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
       }
     }
     const long long off = at[i] * (shared ? a.ctx_ld : a.own_ld) + g * DH + g4 * 8;
-    const T *kp = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + off, *vp = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + off;
+    const T* kp = static_cast<const T*>(shared ? a.ctx_k : a.own_k) + off;
+    const T* vp = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + off;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       kf[i][d] = live[i] ? ld8(kp + d * 32) : V8<T>{};
@@ -1021,7 +1030,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
 
   // q.k and dout.v of 32 rows from kb on with the wave's keys
-  auto products = [&](const T* Qs, const T* Ds, int kb, f32x4 (&s)[2][KT], f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
+  auto products = [&](const T* Qs, const T* Ds, int kb, f32x4 (&s)[2][KT],
+                      f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -1038,7 +1048,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
     }
   };
   // ... and with them the rows' part of dk and dv; own: rows see the keys [lo, hi)
-  auto add = [&](const T* Qs, const T* Ds, int cur, int kb, bool own, const f32x4 (&s)[2][KT], const f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
+  auto add = [&](const T* Qs, const T* Ds, int cur, int kb, bool own, const f32x4 (&s)[2][KT],
+                 const f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
     float pe[KT][8], de[KT][8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -1121,7 +1132,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
       for (int kb = 0; kb < RC; kb += 32) {
         if (rb + c * RC + kb >= re) break;                              // uniform
         // uniform: lists of the block's rows, keys of the wave
-        const int first = __builtin_amdgcn_readfirstlane(s_lo[cur][kb]), last = __builtin_amdgcn_readfirstlane(s_lo[cur][kb + 31]);
+        const int first = __builtin_amdgcn_readfirstlane(s_lo[cur][kb]);
+        const int last = __builtin_amdgcn_readfirstlane(s_lo[cur][kb + 31]);
         const int xa = x0 + wave * KT * 16;
         if (first >= xa + KT * 16 || last + a.L <= xa) continue;
         f32x4 s[2][KT], dp[2][KT];
@@ -1135,9 +1147,11 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(sizeof(T), DH)) void k_prefix_dk
     const int x = x0 + (wave * KT + i) * 16 + c16;
     if (x >= cols) continue;
     const long long off = at[i] * (shared ? p.dctx_ld : p.down_ld) + g * DH + g4 * 4;
-    T *ko = static_cast<T*>(shared ? p.dctx_k : p.down_k) + off, *vo = static_cast<T*>(shared ? p.dctx_v : p.down_v) + off;
+    T* ko = static_cast<T*>(shared ? p.dctx_k : p.down_k) + off;
+    T* vo = static_cast<T*>(shared ? p.dctx_v : p.down_v) + off;
     const long long n_keys = (long long)a.B * cols * a.Hkv;
-    float* po = splits > 1 ? (shared ? p.part_ctx : p.part_own) + (z * n_keys + at[i] * a.Hkv + g) * 2 * DH + g4 * 4 : nullptr;
+    float* po = nullptr;
+    if (splits > 1) po = (shared ? p.part_ctx : p.part_own) + (z * n_keys + at[i] * a.Hkv + g) * 2 * DH + g4 * 4;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const f32x4 zero = {0.f, 0.f, 0.f, 0.f};                          // a key past its length: its sums mean nothing
@@ -1231,7 +1245,9 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  auto blocks_of = [](int splits, long long n, int width) { return splits > 1 ? (unsigned)((n * (width / 4) + 255) / 256) : 0u; };
+  auto blocks_of = [](int splits, long long n, int width) {
+    return splits > 1 ? (unsigned)((n * (width / 4) + 255) / 256) : 0u;
+  };
   const SumBlocks blocks{blocks_of(a.splits, rows, DH), blocks_of(p.ctx_splits, (long long)a.B * a.T * a.Hkv, 2 * DH)};
   const unsigned all = blocks.dq + blocks.ctx + blocks_of(p.own_splits, (long long)a.B * a.K * a.L * a.Hkv, 2 * DH);
   if (all == 0) return hipSuccess;
@@ -1242,10 +1258,11 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
 }  // namespace
 
 namespace {
-// Ranges that `items` chunks of 64 are split into, for each of `wgs` tiles: up to two workgroups per compute unit, at least three chunks a range
-// (a range costs its partial sums, and all of them a launch).  64 tiles of 24 chunks: one range 28.6 us, two 23.0 at four,
-// 19.5 at eight, 20.5 at sixteen; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.  In fp32 also as many as keep a range at
-// 2048: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8) of its result, 1.1e-6 at 6400.
+// Ranges that `items` chunks of 64 are split into, for each of `wgs` tiles: up to two workgroups per compute unit, at
+// least three chunks a range (a range costs its partial sums, and all of them a launch).  64 tiles of 24 chunks: one range
+// 28.6 us, four 23.0, eight 19.5, sixteen 20.5; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.  In fp32 also as many as
+// keep a range at 2048 keys or rows: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8) of its
+// result, 1.1e-6 at 6400.
 int ranges(long long wgs, long long items, int most, bool f32) {
   const long long by_size = std::min({512 / std::max(1LL, wgs), items / 3, (long long)most});
   const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);           // a launch holds 2^24 - 1 workgroups of 256

@@ -62,7 +62,8 @@ def _struct(name: str, ints: str, pointers: str, tail=()):
 
 
 fe_append_args = _struct(
-    "fe_append_args", "dtype N S n_heads n_kv_heads dh rot neighbours page_rows n_pages table_cols q_ld k_ld v_ld q_out_ld page_ld",
+    "fe_append_args",
+    "dtype N S n_heads n_kv_heads dh rot neighbours page_rows n_pages table_cols q_ld k_ld v_ld q_out_ld page_ld",
     "q k v q_out freq table len new_len pos0 k_pages v_pages len_out status")
 fe_prefix_args = _struct(
     "fe_prefix_args", "dtype B K S n_heads n_kv_heads dh T L page_rows n_pages causal scale q_ld ctx_ld own_ld out_ld",
@@ -717,7 +718,8 @@ class PrefixAttention:
         a, dev = self.args, torch.device("cuda", torch.cuda.current_device())
         self.out = torch.empty((a.B, a.K, a.S, a.n_heads, a.dh), dtype=self.act, device=dev)
         self.lse = torch.empty((a.B, a.K, a.S, a.n_heads), dtype=torch.float32, device=dev) if self.train else None
-        self.out_rest = torch.empty(self.q_shape, dtype=torch.int8, device=dev) if self.train and self.act == torch.bfloat16 else None
+        rest = self.train and self.act == torch.bfloat16
+        self.out_rest = torch.empty(self.q_shape, dtype=torch.int8, device=dev) if rest else None
         self.ws = torch.empty(max(16, self.ws_bytes), dtype=torch.uint8, device=dev)
         a.out, a.lse, a.out_rest = _ptr(self.out), _ptr(self.lse), _ptr(self.out_rest)
         a.ws, a.ws_bytes = _ptr(self.ws), self.ws_bytes

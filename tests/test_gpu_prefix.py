@@ -327,6 +327,20 @@ def test_a_list_keeps_its_infinities_to_itself(dtype):
     assert (((got - want).abs().float() <= tol) | hit).all()
 
 
+@pytest.mark.parametrize("T", [40, 3000])                # whole, and in ranges that are joined
+def test_a_nan_query_gives_nan(T):
+    """A row whose scores are all NaN is not a row without keys; the other rows keep their bits."""
+    c = Case(dtype="bf16", B=1, K=3, S=2, H=2, Hkv=2, dh=32, T=T, L=6, lens="full", seed=13).device()
+    p = fe.PrefixAttention(train=True, **c.dims)
+    want, lse = p.run(*c.keys, **c.more).clone(), p.lse.clone()
+    c.keys[0][0, 1, 0, 1, 3] = NAN
+    got = p.run(*c.keys, **c.more)
+    hit = torch.zeros(want.shape[:4], dtype=torch.bool)
+    hit[0, 1, 0, 1] = True
+    assert torch.isnan(got[hit.cuda()]).all() and torch.isnan(p.lse[hit.cuda()]).all()
+    assert torch.equal(got[~hit.cuda()], want[~hit.cuda()]) and torch.equal(p.lse[~hit.cuda()], lse[~hit.cuda()])
+
+
 def test_streams_and_graphs():
     """On a stream of its own; captured once and replayed with other lengths, queries and pages, eager work in between."""
     cases = [Case(dtype="bf16", B=2, K=4, S=1, H=4, Hkv=2, dh=64, T=900, L=48, P=16, seed=s).device() for s in (21, 22, 23)]
