@@ -108,7 +108,8 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream);
  * multiple of n_kv_heads, strides too short or not multiples of 16 bytes, L not a multiple of page_rows, a
  * scale that is not finite, an unknown dtype, a workspace that is too small; FE_EUNSUPPORTED for dh outside
  * {32, 64, 128}, T or L above 4194304, B*K*S*n_heads, B*T or B*K*L above 1073741823, more than 16777215
- * workgroups of 64 rows or keys of one request and key head, or ctx_ld above 8388608.
+ * workgroups of 64 rows or keys of one request and key head (the gradient: of partial sums, 1024 each, too), or
+ * ctx_ld above 8388608.
  */
 typedef struct {
   int32_t dtype;                        /* fe_dtype of q, keys, values and out */
@@ -139,7 +140,8 @@ fe_status fe_prefix_attention(const fe_prefix_args* a, void* stream);
 /*
  * Gradients of fe_prefix_attention for d loss / d out = dout.  `a` holds the forward's arguments with its out and
  * lse (and out_rest: without it FE_BF16 takes D from the rounded out) and a workspace of
- * fe_prefix_workspace_size(a, 1) bytes; own rows must be dense (FE_EUNSUPPORTED otherwise).  With D = dout.out, dp = dout.v and ds = p (dp - D):
+ * fe_prefix_workspace_size(a, 1) bytes; own rows must be dense (FE_EUNSUPPORTED otherwise).
+ * With D = dout.out, dp = dout.v and ds = p (dp - D):
  *   dq = scale sum ds k,   dk = scale sum ds q,   dv = sum p dout,
  * where a key's sums run over every list (shared rows), row and head that reads it.  Every row of dq, of the shared
  * gradients [B][T] and of the own gradients [B][K][L] is written; rows outside the lengths are zero.  dout

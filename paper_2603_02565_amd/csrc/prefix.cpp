@@ -45,8 +45,7 @@ fe_status check_sizes(const fe_prefix_args* a) {
   const double most = 1073741823., lists = (double)a->B * a->K;
   if (lists * a->S * a->n_heads > most || (double)a->B * a->T > most || lists * a->L > most)
     return pfail(FE_EUNSUPPORTED, "batch too large: more than %.0f rows", most);
-  // every launch of the forward and the gradient, at 64 rows or keys a workgroup (16 for dout . out): a grid of 256
-  // threads a workgroup holds 2^24 - 1 of them
+  // every launch of the forward, and the gradient's unsplit: a grid of 256 threads a workgroup holds 2^24 - 1 of them
   const double pairs = (double)a->B * a->n_kv_heads, G = a->n_heads / a->n_kv_heads;
   const double tiles = std::floor(((double)a->K * a->S * G + 63) / 64);
   const double keys = std::floor((a->T + 63) / 64.) + std::floor(((double)a->K * a->L + 63) / 64);
@@ -74,6 +73,13 @@ fe_status check_forward(const fe_prefix_args* a) {
       (a->T > 0 && !stride_ok(a->ctx_ld, wk, a->dtype)) || (a->L > 0 && !stride_ok(a->own_ld, wk, a->dtype)))
     return pfail(FE_EINVAL, "a row stride is shorter than its row or not a multiple of 16 bytes");
   if (a->T > 0 && a->ctx_ld > kMaxStride) return pfail(FE_EUNSUPPORTED, "ctx_ld=%d above %d", a->ctx_ld, kMaxStride);
+  return FE_OK;
+}
+
+// The gradient's launches, split.
+fe_status check_grid(const PrefixGradPlan& p) {
+  if (p.dkv_blocks > kMaxGrid || p.sum_blocks > kMaxGrid)
+    return pfail(FE_EUNSUPPORTED, "batch too large for the gradient: more than %lld workgroups", kMaxGrid);
   return FE_OK;
 }
 
@@ -106,8 +112,13 @@ fe_status fe_prefix_workspace_size(const fe_prefix_args* a, int grad, size_t* by
   if (st != FE_OK) return st;
   if (!bytes) return pfail(FE_EINVAL, "bytes is NULL");
   if (grad && a->page_rows > 0) return pfail(FE_EUNSUPPORTED, "the gradient takes dense own rows");
-  *bytes = grad ? grad_bytes(prefix_grad_plan(*a)) : prefix_plan(*a).part_bytes;
-  return FE_OK;
+  if (!grad) {
+    *bytes = prefix_plan(*a).part_bytes;
+    return FE_OK;
+  }
+  const PrefixGradPlan p = prefix_grad_plan(*a);
+  *bytes = grad_bytes(p);
+  return check_grid(p);
 }
 
 fe_status fe_prefix_attention(const fe_prefix_args* a, void* stream) {
@@ -141,6 +152,7 @@ fe_status fe_prefix_attention_grad(const fe_prefix_args* a, const fe_prefix_grad
       (a->T > 0 && !stride_ok(g->dctx_ld, wk, a->dtype)) || (a->L > 0 && !stride_ok(g->down_ld, wk, a->dtype)))
     return pfail(FE_EINVAL, "a row stride is shorter than its row or not a multiple of 16 bytes");
   const PrefixGradPlan p = prefix_grad_plan(*a);
+  if (check_grid(p) != FE_OK) return FE_EUNSUPPORTED;
   const size_t need = grad_bytes(p);
   if (!a->ws || a->ws_bytes < need)
     return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);

@@ -41,6 +41,7 @@ hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixP
 struct PrefixGradPlan {
   int tiles, splits, ctx_tiles, own_tiles, ctx_splits, own_splits;
   size_t rows_bytes, dq_bytes, ctx_bytes, own_bytes;
+  long long dkv_blocks, sum_blocks;     // workgroups
 };
 PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_grad(const PrefixGradArgs& a, int dh, bool bf16_rows, const PrefixGradPlan& p, hipStream_t s);

@@ -921,8 +921,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, COLS = NW * KT * 16, NB = DH / 16, ND = DH / 32;
   typedef Tile<T, DH> L;
-  constexpr int PER_T = (RC * DH / 8 + NT - 1) / NT, STEP = NT / (DH / 8);
-  static_assert(RC % 32 == 0 && RC <= NT && (RC * DH / 8 % NT == 0 || RC * DH / 8 < NT), "tile shape");
+  constexpr int PER_T = RC * DH / 8 / NT, STEP = NT / (DH / 8);
+  static_assert(RC % 32 == 0 && RC <= NT && RC * DH / 8 % NT == 0, "tile shape");
   __shared__ __attribute__((aligned(16))) T Qs_[2][RC * L::LD], Ds_[2][RC * L::LD];
   __shared__ __attribute__((aligned(16))) float s_lse[2][RC], s_delta[2][RC];
   __shared__ __attribute__((aligned(16))) int s_lo[2][RC], s_hi[2][RC];
@@ -973,7 +973,6 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
       const T *qp = q_base + at * a.q_ld + g * a.G * DH, *dp = d_base + at * p.dout_ld + g * a.G * DH;
 #pragma unroll
       for (int q = 0; q < PER_T; ++q) {
-        if (RC * DH / 8 < NT && i0 >= RC) continue;
         qreg[q] = ld8_at(qp, q_at[q]);
         dreg[q] = ld8_at(dp, d_at[q]);
       }
@@ -1099,7 +1098,6 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
       if (a.q_len && lreg[q] == INFINITY) qreg[q] = dreg[q] = V8<T>{};  // a row that sees nothing may hold anything
-      if (RC * DH / 8 < NT && i0 >= RC) continue;
       st8(&Qs[L::at(i0 + q * STEP, d0 / 8)], qreg[q]);
       st8(&Ds[L::at(i0 + q * STEP, d0 / 8)], dreg[q]);
     }
@@ -1170,6 +1168,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
 // Adds the partial sums of dq (key ranges) and of dk and dv (row ranges) in ascending order, in one launch: the first
 // blocks[0] workgroups dq, the next blocks[1] the shared keys, the rest the own keys.
 struct SumBlocks { unsigned dq, ctx; };
+// workgroups that add `bytes` of partial sums in `splits` parts, four sums a thread
+long long sum_blocks(size_t bytes, int splits) { return (long long)((bytes / splits + 4095) / 4096); }
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_prefix_sum(PrefixGradArgs p, SumBlocks blocks) {
   const PrefixArgs& a = p.f;
@@ -1228,7 +1228,7 @@ hipError_t fwd(const PrefixArgs& a, const PrefixPlan& p, hipStream_t s) {
 template <typename T, int DH>
 hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   PrefixArgs& a = p.f;
-  const long long rows = (long long)a.B * a.K * a.S * a.Hq, bg = (long long)a.B * a.Hkv;
+  const long long bg = (long long)a.B * a.Hkv;
   a.tiles = pl.tiles;
   a.splits = pl.splits;
   const dim3 gq((unsigned)(bg * a.tiles * a.splits));
@@ -1239,25 +1239,18 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   p.own_tiles = pl.own_tiles;
   p.ctx_splits = pl.ctx_splits;
   p.own_splits = pl.own_splits;
-  if (p.ctx_tiles + p.own_tiles > 0) {
-    const dim3 gk((unsigned)(bg * (p.ctx_tiles * p.ctx_splits + p.own_tiles * p.own_splits)));
+  if (pl.dkv_blocks > 0) {
+    const dim3 gk((unsigned)pl.dkv_blocks);
     hipLaunchKernelGGL((k_prefix_dkv<T, DH, kKT<T, DH>, 4, kRC<T, DH>>), gk, dim3(256), 0, s, p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  auto blocks_of = [](int splits, long long n, int width) {
-    return splits > 1 ? (unsigned)((n * (width / 4) + 255) / 256) : 0u;
-  };
-  const SumBlocks blocks{blocks_of(a.splits, rows, DH), blocks_of(p.ctx_splits, (long long)a.B * a.T * a.Hkv, 2 * DH)};
-  const unsigned all = blocks.dq + blocks.ctx + blocks_of(p.own_splits, (long long)a.B * a.K * a.L * a.Hkv, 2 * DH);
-  if (all == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_prefix_sum<T, DH>), dim3(all), dim3(256), 0, s, p, blocks);
+  if (pl.sum_blocks == 0) return hipSuccess;
+  const SumBlocks blocks{(unsigned)sum_blocks(pl.dq_bytes, pl.splits), (unsigned)sum_blocks(pl.ctx_bytes, pl.ctx_splits)};
+  hipLaunchKernelGGL((k_prefix_sum<T, DH>), dim3((unsigned)pl.sum_blocks), dim3(256), 0, s, p, blocks);
   return hipGetLastError();
 }
 
-}  // namespace
-
-namespace {
 // Ranges that `items` chunks of 64 are split into, for each of `wgs` tiles: up to two workgroups per compute unit, at
 // least three chunks a range (a range costs its partial sums, and all of them a launch).  64 tiles of 24 chunks: one range
 // 28.6 us, four 23.0, eight 19.5, sixteen 20.5; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.  In fp32 also as many as
@@ -1315,6 +1308,9 @@ PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a) {
   p.dq_bytes = p.splits > 1 ? p.splits * rows * a.dh * sizeof(float) : 0;
   p.ctx_bytes = p.ctx_splits > 1 ? p.ctx_splits * (size_t)a.B * a.T * a.n_kv_heads * row_bytes : 0;
   p.own_bytes = p.own_splits > 1 ? p.own_splits * (size_t)a.B * a.K * a.L * a.n_kv_heads * row_bytes : 0;
+  p.dkv_blocks = bg * ((long long)p.ctx_tiles * p.ctx_splits + (long long)p.own_tiles * p.own_splits);
+  p.sum_blocks = sum_blocks(p.dq_bytes, p.splits) + sum_blocks(p.ctx_bytes, p.ctx_splits) +
+                 sum_blocks(p.own_bytes, p.own_splits);
   return p;
 }
 

@@ -567,6 +567,8 @@ def _row_stride(t, name: str, shape: Tuple[int, ...], dtype) -> int:
     if not ok or ld < width:
         raise ValueError(f"{name}: rows of {width} elements must be dense and evenly spaced, got strides {tuple(st)} for shape "
                          f"{shape}")
+    if ld > 2 ** 31 - 1:
+        raise ValueError(f"{name}: a row stride of {ld} elements does not fit int32")
     return ld
 
 
@@ -603,6 +605,19 @@ def _stream_on(index: int, stream) -> int:
         return _stream(stream)
     import torch
     return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _allocated_for(stream, *tensors) -> None:
+    """Tensors just allocated that `stream`, not the current one, is about to use: it waits for what the current stream still
+    does in their memory, and the memory is not given out again before its own work there has ended."""
+    import torch
+    if stream is None or _stream(stream) == torch.cuda.current_stream().cuda_stream:
+        return
+    other = torch.cuda.ExternalStream(_stream(stream))
+    other.wait_stream(torch.cuda.current_stream())
+    for t in tensors:
+        if t is not None:
+            t.record_stream(other)
 
 
 def _addr(t) -> Optional[int]:
@@ -674,6 +689,7 @@ class PagedCache:
             if q is None:
                 raise ValueError("q_out without q")
             q_out = q.new_empty(q.shape)
+            _allocated_for(stream, q_out)
         a.S, a.n_heads, a.k_ld, a.v_ld, a.q_ld, a.q_out_ld, a.rot = self._layouts.of(
             self._check, k, v, q, q_out, freq, new_len, pos0, len_out)
         index = _on_device((k, v, q, q_out, freq, new_len, pos0, len_out, self.k_pages))
@@ -750,13 +766,14 @@ class PrefixAttention:
         _need(own_len, "own_len", i32, a.B * a.K)
         return q_ld, lds[0], lds[1]
 
-    def _take(self, *tensors):
+    def _take(self, stream, *tensors):
         a = self.args
         q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len = tensors
         a.q_ld, a.ctx_ld, a.own_ld = self._layouts.of(self._check, *tensors)
         index = _on_device(tensors)
         if self.out is None:
             self.allocate()
+            _allocated_for(stream, self.out, self.lse, self.out_rest, self.ws, *(self.grads or ()))
         elif self.out.get_device() != index:
             raise ValueError(f"the outputs are on {self.out.device}, the tensors on device {index}")
         a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = q.data_ptr(), _addr(ctx_k), _addr(ctx_v), _addr(own_k), _addr(own_v)
@@ -765,7 +782,7 @@ class PrefixAttention:
 
     def run(self, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
         """Enqueue the attention; returns out [B][K][S][n_heads][dh] (self.lse holds the log sums when training)."""
-        index = self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        index = self._take(stream, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
         fe_prefix_attention(self.args, _stream_on(index, stream))
         return self.out
 
@@ -775,7 +792,7 @@ class PrefixAttention:
             raise ValueError("grad needs train=True")
         if self.out is None:
             raise ValueError("grad follows run")
-        index = self._take(q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        index = self._take(stream, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
         a, g = self.args, fe_prefix_grads()
         g.dout_ld = self._layouts.of(lambda t: _row_stride(t, "dout", self.q_shape, self.act), dout)
         _on_device((dout, q))

@@ -232,6 +232,24 @@ def test_two_calls_at_once():
     assert all(torch.equal(p.out, w) for p, w in zip(plans, want))
 
 
+def test_first_call_on_a_given_stream():
+    """Outputs, workspace and q_out that a call allocates itself are good for the stream that it is given."""
+    c = Case(dtype="bf16", B=1, K=4, S=1, H=4, Hkv=2, dh=64, T=3000, L=48, P=16, seed=43).device()
+    want = fe.PrefixAttention(**c.dims).run(*c.keys, **c.more).clone()
+    ac = AppendCase(seed=44, **APPEND[0])
+    (k, v), kw = ac.device()
+    for side in (torch.cuda.Stream(), torch.cuda.default_stream()):
+        p = fe.PrefixAttention(**c.dims)
+        torch.cuda.synchronize()
+        got = p.run(*c.keys, stream=side, **c.more)
+        side.synchronize()
+        assert torch.equal(got, want)
+    side = torch.cuda.Stream()
+    q_out = ac.cache.append(k, v, stream=side, **kw)
+    side.synchronize()
+    ac.check(q_out)
+
+
 def test_lists_do_not_depend_on_each_other():
     """The same list beside other lists of the same lengths: the same bits."""
     c = Case(dtype="bf16", B=1, K=12, S=7, H=4, Hkv=2, dh=64, T=100, L=15, seed=61).device()

@@ -98,6 +98,20 @@ def test_prefix_workspace():
         fe.fe_prefix_workspace_size(_args(page_rows=4, n_pages=2), True)
 
 
+def test_gradient_grid():
+    """2^28 shared keys of 4096 rows in two ranges: 2^26 workgroups of partial sums, more than a launch holds."""
+    a = _args(dtype=fe.FE_F32, B=1, K=1, S=4096, n_heads=64, n_kv_heads=64, dh=128, T=1 << 22, L=0)
+    fe.fe_prefix_workspace_size(a)
+    with pytest.raises(fe.FeError, match="too large for the gradient"):
+        fe.fe_prefix_workspace_size(a, True)
+
+
+def test_row_stride_above_int32():
+    t = torch.empty_strided((1, 2, 1, 32), (1 << 33, 1 << 32, 32, 1), dtype=torch.float32, device="meta")
+    with pytest.raises(ValueError, match="int32"):
+        fe._row_stride(t, "k", (1, 2, 1, 32), torch.float32)
+
+
 def _append_args(**kw):
     a = fe.fe_append_args()
     base = dict(dtype=fe.FE_F32, N=3, S=2, n_heads=4, n_kv_heads=2, dh=32, rot=32, neighbours=0, page_rows=4, n_pages=9, table_cols=3,
