@@ -18,7 +18,10 @@ struct PrefixArgs {
   float scale;
   int G, R;
   int tiles, splits;                    // row tiles per (request, key head); key ranges per tile
-  float *part_o, *part_ml;              // splits > 1: [splits][B*K*S*Hq][dh] sums, [..][2] maximum and sum
+  // Forward, splits > 1: B * splits ranges in all; by_length: a request has as many of them as its share of the keys
+  // says, its own rows taken as own_chunks chunks of 64.
+  int by_length, own_chunks;
+  float *part_o, *part_ml;              // splits > 1: [B*splits][K*S*Hq][dh] sums, [..][2] maximum and sum; dq: its sums
 };
 
 // The gradient's further tensors.
@@ -34,7 +37,7 @@ struct PrefixGradArgs {
 };
 
 // Row tiles, key ranges and partial-sum bytes of a forward call: functions of the sizes alone.
-struct PrefixPlan { int rows, tiles, splits; size_t part_bytes; };
+struct PrefixPlan { int rows, tiles, splits, by_length, own_chunks; size_t part_bytes; };
 PrefixPlan prefix_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixPlan& p, hipStream_t s);
 // The same of a gradient call: dq's row tiles and key ranges, dk's and dv's key tiles and row ranges, scratch bytes.

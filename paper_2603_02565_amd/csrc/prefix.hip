@@ -80,6 +80,26 @@ FE_DEV int key_of(int j, int g4) { return 16 * (j >> 2) + 4 * g4 + (j & 3); }
 // log2(e) |scale|, the exponent's factor of a score; positive, so that masked scores stay -infinity when scale is 0.
 FE_DEV float score_unit(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-37f); }
 
+// The key ranges of the forward are numbered request after request: request b has `n` of them, from `first` on.
+struct Ranges { int first, n; };
+// by_length (B <= 64): lane b finds those of request b.  Every request has one; the others are shared out in proportion
+// to the chunks of keys, rounded down, so they may leave a few unused.
+FE_DEV Ranges ranges_of_lane(const PrefixArgs& a) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < a.B ? (ctx_rows(a, lane) + 63) / 64 + a.own_chunks + 1 : 0;
+  int all = mine;                                  // at most 2^25
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) all += __shfl_xor(all, x);
+  const int n = lane < a.B ? 1 + (int)((float)(a.B * (a.splits - 1)) * (float)mine / (float)all) : 0;
+  int end = n;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    const int before = __shfl_up(end, x);
+    if (lane >= x) end += before;
+  }
+  return {end - n, n};
+}
+
 // Four consecutive elements of an output row, and what their rounding left (bf16, when asked for).
 template <typename T>
 FE_DEV void store_out(const PrefixArgs& a, long long at, int col, f32x4 v);
@@ -282,12 +302,20 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g4 = lane >> 4, c16 = lane & 15;
-  int id = xcd_tile(blockIdx.x, gridDim.x);        // a (request, key head)'s workgroups share an XCD's L2
-  const int z = id % a.splits;
-  id /= a.splits;
+  // Workgroups that read the same keys, or the same lines of them, share an XCD's L2; where there are none, the ranges
+  // of a request are spread over the XCDs.
+  int id = a.tiles == 1 && sizeof(T) * DH >= 128 ? (int)blockIdx.x : xcd_tile(blockIdx.x, gridDim.x);
   const int t = id % a.tiles;
   id /= a.tiles;
-  const int g = id % a.Hkv, b = id / a.Hkv;
+  const int g = id % a.Hkv, range = id / a.Hkv;
+  int b = range / a.splits, z = range % a.splits, splits = a.splits;
+  if (a.by_length) {                               // uniform
+    const Ranges mine = ranges_of_lane(a);
+    b = __popcll(__ballot(lane < a.B && mine.first + mine.n <= range));
+    if (b >= a.B) return;                          // left over
+    z = range - __builtin_amdgcn_readlane(mine.first, b);
+    splits = __builtin_amdgcn_readlane(mine.n, b);
+  }
   const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R), sg = a.S * a.G;
   const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
   if (tid < 2) s_odd[tid] = s_holes[tid] = -1;
@@ -295,7 +323,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   // This workgroup's share of the shared chunks and, below, of the own chunks.  The shared ones need no more than ctx_len,
   // so they are under way while the lists' lengths, packing and pages are found.
   const int nctx = ctx_rows(a, b), cctx = (nctx + KC - 1) / KC;
-  const int cb = (int)((long long)cctx * z / a.splits), cm = (int)((long long)cctx * (z + 1) / a.splits);
+  const int cb = (int)((long long)cctx * z / splits), cm = (int)((long long)cctx * (z + 1) / splits);
 
   // The loads are unconditional: rows that do not count read one that exists and are cleared when they are staged.
   V8<T> kreg[PER_T], vreg[PER_T];
@@ -333,7 +361,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 
   pack_own<NT>(a, b, k0, nb, s_off);
   const int nown = __builtin_amdgcn_readfirstlane(s_off[nb]), cown = (nown + KC - 1) / KC;
-  const int ob = (int)((long long)cown * z / a.splits), oe = (int)((long long)cown * (z + 1) / a.splits);
+  const int ob = (int)((long long)cown * z / splits), oe = (int)((long long)cown * (z + 1) / splits);
   int gone = 0, hole = 0;                          // bit p: the key does not count; because its page is outside the pool
   auto load_own = [&](int c) __attribute__((always_inline)) {
     const T *kp = static_cast<const T*>(a.own_k) + g * DH + d0, *vp = static_cast<const T*>(a.own_v) + g * DH + d0;
@@ -590,13 +618,13 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     const float m2 = m_run[i] * sl2;
     const long long ro = row[i].at * a.Hq + row[i].h;
     if (a.splits > 1) {
-      const long long rows = (long long)a.B * a.K * a.S * a.Hq;
-      float* po = a.part_o + (z * rows + ro) * DH;
+      const long long at = ro + (long long)(range - b) * a.K * a.S * a.Hq;   // [range][row of the request]
+      float* po = a.part_o + at * DH;
 #pragma unroll
       for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(po + n * 16 + g4 * 4) = o[i][n];
       if (g4 == 0) {
-        a.part_ml[(z * rows + ro) * 2] = m2;
-        a.part_ml[(z * rows + ro) * 2 + 1] = l;
+        a.part_ml[at * 2] = m2;
+        a.part_ml[at * 2 + 1] = l;
       }
       continue;
     }
@@ -619,21 +647,27 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
   const long long rows = (long long)a.B * a.K * a.S * a.Hq;
   const long long e = (long long)blockIdx.x * 256 + threadIdx.x, ro = e / (DH / 4);
   const int d0 = (int)(e % (DH / 4)) * 4;
+  int b = (int)(min(ro, rows - 1) / (rows / a.B)), first = b * a.splits, splits = a.splits;
+  if (a.by_length) {                               // uniform
+    const Ranges mine = ranges_of_lane(a);
+    first = __shfl(mine.first, b);
+    splits = __shfl(mine.n, b);
+  }
   if (ro >= rows) return;
-  const long long at = ro / a.Hq;
+  const long long at = ro / a.Hq, step = rows / a.B, from = (first - b) * step + ro;
   const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);
   const bool dead = s >= q_rows(a, bk);
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int z0 = 0; z0 < a.splits; z0 += 8) {       // eight ranges requested at once
+  for (int z0 = 0; z0 < splits; z0 += 8) {         // eight ranges requested at once
     float2 ml[8];
     f32x4 v[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const long long e = min(z0 + u, a.splits - 1) * rows + ro;
+      const long long e = min(z0 + u, splits - 1) * step + from;
       ml[u] = reinterpret_cast<const float2*>(a.part_ml)[e];
       v[u] = *reinterpret_cast<const f32x4*>(a.part_o + e * DH + d0);
-      if (z0 + u >= a.splits) ml[u].x = -INFINITY;
+      if (z0 + u >= splits) ml[u].x = -INFINITY;
     }
     float top = m;
 #pragma unroll
@@ -1256,8 +1290,13 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
 // 28.6 us, four 23.0, eight 19.5, sixteen 20.5; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.  In fp32 also as many as
 // keep a range at 2048 keys or rows: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8) of its
 // result, 1.1e-6 at 6400.
-int ranges(long long wgs, long long items, int most, bool f32) {
-  const long long by_size = std::min({512 / std::max(1LL, wgs), items / 3, (long long)most});
+// narrow (forward, bf16 heads of at most 64, three of whose workgroups a compute unit holds): up to three as long as a
+// range keeps eight chunks (heads of 64, 128 tiles of 512 + 16 chunks: 237 us -> 181, of 32 + 16: 33 -> 30; heads of 32,
+// 32 tiles of 32 + 32 chunks: two 16.1, three 18.0).
+int ranges(long long wgs, long long items, int most, bool f32, bool narrow = false) {
+  const long long two = std::min(512 / std::max(1LL, wgs), items / 3);
+  const long long three = narrow ? std::min(768 / std::max(1LL, wgs), items / 8) : 0;
+  const long long by_size = std::min(std::max(two, three), (long long)most);
   const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);           // a launch holds 2^24 - 1 workgroups of 256
   return (int)std::max(1LL, std::min({std::max({1LL, by_size, f32 ? (items + 31) / 32 : 1LL}), 256LL, grid}));
 }
@@ -1283,7 +1322,14 @@ PrefixPlan prefix_plan(const fe_prefix_args& a) {
   const bool spare = bg * t128 >= (a.T >= 2048 ? 512 : 1024) && 100 * 2 * t128 <= 108 * t64;
   p.rows = fits && ((R > 64 && R <= 128) || spare) ? 128 : 64;
   p.tiles = (int)((R + p.rows - 1) / p.rows);
-  p.splits = ranges(bg * p.tiles, chunks_of(a, p.rows), 64, a.dtype == FE_F32);
+  p.splits = ranges(bg * p.tiles, chunks_of(a, p.rows), 64, a.dtype == FE_F32, a.dtype == FE_BF16 && a.dh <= 64);
+  // Ranges by the requests' lengths: with enough of them for the rounding and long enough for the arithmetic that shares
+  // them out (4 requests, lengths from half of T to T, 32 lists, heads of 128: T = 32768 in 16 ranges 133 us -> 115, 8192
+  // 51.4 -> 50.0; heads of 64, 16 lists: 56 -> 52, 27.0 -> 29.4; 16 requests of 8192 in 4 ranges 68 -> 72; 8 of 1024 in 8
+  // 15.4 -> 18.0).  fp32 keeps equal numbers, for the length of its chains of sums.
+  p.by_length = p.splits > 1 && a.dtype == FE_BF16 && a.ctx_len && a.B > 1 && a.B <= 64 &&
+                p.splits >= 8 && a.T >= 1024 * p.splits;
+  p.own_chunks = (int)((chunks_of(a, p.rows) - (a.T + 63) / 64) / 2);    // lists half full
   const size_t rows = (size_t)a.B * a.K * a.S * a.n_heads;
   p.part_bytes = p.splits > 1 ? p.splits * rows * (a.dh + 2) * sizeof(float) : 0;
   return p;
@@ -1317,6 +1363,8 @@ PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a) {
 hipError_t launch_prefix_fwd(PrefixArgs a, int dh, bool bf16_rows, const PrefixPlan& p, hipStream_t s) {
   a.tiles = p.tiles;
   a.splits = p.splits;
+  a.by_length = p.by_length;
+  a.own_chunks = p.own_chunks;
   if (bf16_rows) return dh == 32 ? fwd<bf16, 32>(a, p, s) : dh == 64 ? fwd<bf16, 64>(a, p, s) : fwd<bf16, 128>(a, p, s);
   return dh == 32 ? fwd<float, 32>(a, p, s) : dh == 64 ? fwd<float, 64>(a, p, s) : fwd<float, 128>(a, p, s);
 }

@@ -158,6 +158,26 @@ def test_forward(i):
     assert torch.equal(again, out)                     # the same bits from call to call
 
 
+# Long contexts whose key ranges follow the requests' lengths: eight requests, some of none and of all the rows; as many
+# requests as share ranges that way, and one more
+BY_LENGTH = [
+    dict(dtype="bf16", B=8, K=3, S=2, H=8, Hkv=8, dh=32, T=12288, L=20, lens="edge", seed=3),
+    dict(dtype="bf16", B=64, K=2, S=1, H=2, Hkv=1, dh=32, T=12288, L=70, P=16, seed=4),
+    dict(dtype="bf16", B=65, K=2, S=1, H=1, Hkv=1, dh=32, T=12288, L=7, seed=5),
+    dict(dtype="bf16", B=2, K=40, S=1, H=32, Hkv=16, dh=128, T=16384, L=30, seed=6),
+]
+
+
+@pytest.mark.parametrize("i", range(len(BY_LENGTH)))
+def test_ranges_by_length(i):
+    _say("by length", i, BY_LENGTH[i])
+    c = Case(**BY_LENGTH[i]).device()
+    p = fe.PrefixAttention(**c.dims)
+    out = p.run(*c.keys, **c.more)
+    _near(out, c.reference()["out"], "out")
+    assert torch.equal(p.run(*c.keys, **c.more).clone(), out)
+
+
 GRAD = [
     dict(dtype="f32", B=1, K=1, S=1, H=1, Hkv=1, dh=32, T=1, L=1, lens="full"),
     dict(dtype="f32", B=1, K=2, S=3, H=2, Hkv=1, dh=32, T=0, L=3, lens="own"),
