@@ -74,8 +74,10 @@ FE_DEV int q_rows(const PrefixArgs& a, int bk) { return a.q_len ? clampi(a.q_len
 FE_DEV int own_rows(const PrefixArgs& a, int bk) { return a.own_len ? clampi(a.own_len[bk], 0, a.L) : a.L; }
 FE_DEV int ctx_rows(const PrefixArgs& a, int b) { return a.ctx_len ? clampi(a.ctx_len[b], 0, a.T) : a.T; }
 
-// Key of a 32-key step that element j of a lane in group g4 stands for.
-FE_DEV int key_of(int j, int g4) { return 16 * (j >> 2) + 4 * g4 + (j & 3); }
+// Key of a 32-key step that element j of a lane in group g4 stands for: 4 g4 and a part that is the same for all lanes
+// (compared with a limit from which 4 g4 has been taken, it needs no register).
+FE_DEV int key_of(int j) { return 16 * (j >> 2) + (j & 3); }
+FE_DEV int key_of(int j, int g4) { return key_of(j) + 4 * g4; }
 
 // log2(e) |scale|, the exponent's factor of a score; positive, so that masked scores stay -infinity when scale is 0.
 FE_DEV float score_unit(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-37f); }
@@ -436,8 +438,11 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         for (int j = 0; j < 4; ++j) s[i][4 * x + j] = acc[i][j];
     }
   };
-  auto max8 = [&](const float (&s)[8]) __attribute__((always_inline)) {
-    return fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+  // one chain: two values an instruction
+  auto max8 = [&](float m, const float (&s)[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) m = fmaxf(fmaxf(m, s[j]), s[j + 1]);
+    return m;
   };
   // Moves the reference of tile i's rows to the largest product (mx: this lane's) where that is more than `lag` above
   // it.  The reference is the running maximum, but it follows only once a score is 8 / log2(e) above it: a probability
@@ -503,11 +508,12 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 #pragma unroll
       for (int u = 0; u < NS; ++u) scores(Ks, kb + 32 * u, rl, 0, QT, s[u]);
       if (left < 32 * NS) {                        // uniform
+        const int end = left - 4 * g4;
 #pragma unroll
         for (int u = 0; u < NS; ++u)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (32 * u + key_of(j, g4) >= left) {
+            if (32 * u + key_of(j) >= end) {
 #pragma unroll
               for (int i = 0; i < QT; ++i) s[u][i][j] = -INFINITY;
             }
@@ -516,9 +522,9 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       bool move = false;
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
-        mx[i] = max8(s[0][i]);
+        mx[i] = m_run[i];
 #pragma unroll
-        for (int u = 1; u < NS; ++u) mx[i] = fmaxf(mx[i], max8(s[u][i]));
+        for (int u = 0; u < NS; ++u) mx[i] = max8(mx[i], s[u][i]);
         move |= mx[i] > m_run[i] + lag;
       }
       if (__any(move)) {
@@ -571,18 +577,17 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         scores(Ks, kb, rl, i, i + 1, all);
         float (&s)[8] = all[i];
         if (x0 < alo[i] || x0 + 32 > ahi[i]) {     // uniform
+          const int from = lo[i] - x0 - 4 * g4, to = hi[i] - x0 - 4 * g4;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int x = x0 + key_of(j, g4);
-            if (x < lo[i] || x >= hi[i]) s[j] = -INFINITY;
-          }
+          for (int j = 0; j < 8; ++j)
+            if (key_of(j) < from || key_of(j) >= to) s[j] = -INFINITY;
         }
         if (holes) {                               // uniform
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             if (s_hole[c & 1][kb + key_of(j, g4)] == c) s[j] = -INFINITY;
         }
-        const float mx = max8(s);
+        const float mx = max8(m_run[i], s);
         if (__any(mx > m_run[i] + lag)) follow(i, mx);
         const V8<T> pb = probs(i, s);
         if (!odd) {
@@ -875,9 +880,10 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         float e[8];
         dscores(Ks, Vs, 32 * u, rl, i, e);
         if (left < KC) {                           // uniform; a key past the length is zero, its probability may be anything
+          const int end = left - 4 * g4;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (32 * u + key_of(j, g4) >= left) e[j] = 0.f;
+            if (32 * u + key_of(j) >= end) e[j] = 0.f;
         }
         ds[u][i] = pack8<T>(e);
       }
@@ -915,11 +921,10 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         float e[8];
         dscores(Ks, Vs, kb, rl, i, e);
         if (x0 < alo[i] || x0 + 32 > ahi[i]) {                         // uniform
+          const int from = lo[i] - x0 - 4 * g4, to = hi[i] - x0 - 4 * g4;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int x = x0 + key_of(j, g4);
-            if (x < lo[i] || x >= hi[i]) e[j] = 0.f;
-          }
+          for (int j = 0; j < 8; ++j)
+            if (key_of(j) < from || key_of(j) >= to) e[j] = 0.f;
         }
         const V8<T> ds = pack8<T>(e);
 #pragma unroll
