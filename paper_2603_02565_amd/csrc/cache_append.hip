@@ -28,7 +28,7 @@ FE_DEV void turn(long long pos, double freq, float* c, float* s) {
 
 // One workgroup takes `rows` consecutive new rows of one sequence: the sines and cosines of a row are formed
 // once, in LDS, for all its heads, then every thread moves units of 16 columns (8 pairs).
-// Bound: HBM, every row read and written once (32768 rows of 24 heads of 32, bf16, 101 MB: 18.8 us, 5.4 TB/s); small
+// Bound: HBM, every row read and written once (32768 rows of 24 heads of 32, bf16, 101 MB: 18.2 us, 5.5 TB/s); small
 // calls launch latency (128 rows of 24 heads of 64: 4.1 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_cache_append(fe_append_args a, int rows, int blocks) {
@@ -132,8 +132,8 @@ __global__ void k_advance(int32_t* len, const int32_t* new_len, int N, int S) {
 }  // namespace
 
 hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s) {
-  // rows per workgroup: about 512 units of 16 columns, two a thread (ragged prompts, 37 x 129 rows: 256 units 11.7 us, 512 11.2,
-  // 1024 12.6, 2048 13.8; 16 x 2048 rows: 18.6, 18.8, 19.3, 20.2), and no more sines than the LDS tables hold
+  // rows per workgroup: about 512 units of 16 columns, two a thread (ragged prompts, 37 x 129 rows: 256 units 11.7 us,
+  // 512 11.2, 1024 12.6, 2048 13.8; 16 x 2048 rows: 18.6, 18.8, 19.3, 20.2), and no more sines than the LDS tables hold
   const int units = ((a.q ? a.n_heads : 0) + 2 * a.n_kv_heads) * (a.dh / 16);
   const int fit = a.rot ? std::min(kMaxRows, kMaxRows * 16 / (a.rot / 2)) : kMaxRows;
   const int rows = std::max(1, std::min({a.S, fit, 512 / std::max(1, units)}));

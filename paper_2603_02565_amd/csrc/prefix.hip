@@ -16,7 +16,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Eight elements along the summed axis: one operand of the 16 x 16 x 32 bf16 product, or of eight 16 x 16 x 4 fp32 ones.
 // Lane l holds row (or column) l % 16 and the eight elements of its group l / 16; product j of the fp32 form sums over
-// element j of the four groups, so both types use one layout, and which element is which is free as long as both operands agree.
+// element j of the four groups, so both types use one layout; which element is which is free as long as both operands
+// agree.
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> { typedef bf16x8 type; };
@@ -286,6 +287,12 @@ constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 // flight behind this one's products) into LDS.  Scores are formed transposed (keys x rows): a lane then holds
 // eight keys of one row, which is the operand layout of the product with the values, so probabilities never leave the
 // registers.
+// Bound: with many rows a key the vector unit (a product-sum, an exponential, a sum, half a maximum and half a rounding a
+// score beside its 4 dh matrix operations; 64 x 1024 rows of 1088 keys, heads of 64: 36.6 us, 480 TFLOP/s, vector unit 60%
+// of the time, LDS 44%, matrix cores 22%; 256 x 550 rows of 267 keys, heads of 32: 26.6 us, 180 TFLOP/s); with few rows
+// HBM (4 x 32 lists of 4 rows a key head, heads of 128, 539 MB: 129 us, 4.2 TB/s); fp32 the matrix cores' fp32 form
+// (256 x 550 rows, heads of 32: 76 us, 63 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
+// keys: 7.3 us).
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int QT, int NW, int KC, bool PAGED>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_fwd(PrefixArgs a) {
@@ -647,6 +654,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 }
 
 // Joins the key ranges of a row: DH / 4 threads a row, ranges in ascending order.
+// Bound: the partial sums, from HBM or L2 (4096 rows of 128 in 16 ranges, 34 MB: 9.9 us); one trip for a few (3.9 us).
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
   const long long rows = (long long)a.B * a.K * a.S * a.Hq;
@@ -704,6 +712,10 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
 // products need of every row and leaves it for dk and dv, in the order of the rows of a (request, key head):
 //   x = log2(e) lse (+infinity for a row without keys or past q_len: its probabilities are then 0),
 //   y = dout . out,   z, w = the own rows that it sees, numbered k L + j  [z, w).
+// ds goes into the product with the keys as it lies in the registers, as the probabilities do in the forward.
+// Bound: LDS (55% of the time: every wave reads keys twice and values once for its 16 rows) and the vector unit (48%)
+// beside 27% of matrix cores (64 x 1024 rows of 1088 keys, heads of 64: 46 us, 576 TFLOP/s); fp32 the matrix cores
+// (256 x 550 rows, heads of 32: 102 us, 70 TFLOP/s).
 template <typename T, int DH, int QT, int NW, int KC>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -955,6 +967,10 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 // LDS in chunks of RC.  Tiles 0 .. ctx_tiles - 1 of a (request, key head) hold shared rows and meet every row; the others
 // hold own rows (dense, list after list) and meet the rows of their lists.  In the tile's numbering -- shared row, or
 // k L + j -- the keys that a row sees are again one interval.  Few tiles: several workgroups share a tile's rows.
+// Scores are formed a second time: sums of dq by key tiles would be B K S n_heads dh floats for every tile of 128 keys,
+// more traffic than the two products cost.
+// Bound: vector unit (43% of the time), LDS and matrix cores (30% each) with two waves a SIMD (64 x 1024 rows of 1088
+// keys, heads of 64: 57 us, 625 TFLOP/s); fp32 the matrix cores (256 x 550 rows, heads of 32: 130 us, 74 TFLOP/s).
 template <typename T, int DH, int KT, int NW, int RC>
 __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -1206,6 +1222,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
 
 // Adds the partial sums of dq (key ranges) and of dk and dv (row ranges) in ascending order, in one launch: the first
 // blocks[0] workgroups dq, the next blocks[1] the shared keys, the rest the own keys.
+// Bound: one trip to memory (5328 rows of 128 in 2 parts, 1332 keys in 7 and 1332 in 2, 18 MB: 5.0 us).
 struct SumBlocks { unsigned dq, ctx; };
 // workgroups that add `bytes` of partial sums in `splits` parts, four sums a thread
 long long sum_blocks(size_t bytes, int splits) { return (long long)((bytes / splits + 4095) / 4096); }
