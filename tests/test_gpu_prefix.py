@@ -178,6 +178,27 @@ def test_ranges_by_length(i):
     assert torch.equal(p.run(*c.keys, **c.more).clone(), out)
 
 
+def test_ranges_by_length_in_a_graph():
+    """A captured call replayed with other lengths: the ranges follow them, and every replay has the eager call's bits."""
+    c = Case(**dict(BY_LENGTH[0], lens="full")).device()
+    B, T = c.dims["B"], c.dims["T"]
+    g = torch.Generator().manual_seed(9)
+    lens = [torch.full((B,), T), torch.tensor([T] + [0] * (B - 1)), torch.randint(0, T + 1, (B,), generator=g)]
+    lens = [n.to(torch.int32).cuda() for n in lens]
+    more = dict(c.more, ctx_len=lens[0].clone())
+    plan, other = fe.PrefixAttention(**c.dims), fe.PrefixAttention(**c.dims)
+    eager = [plan.run(*c.keys, **dict(c.more, ctx_len=n)).clone() for n in lens]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = plan.run(*c.keys, **more)
+    for i in (0, 1, 2, 1, 0):
+        more["ctx_len"].copy_(lens[i])
+        graph.replay()
+        again = other.run(*c.keys, **dict(c.more, ctx_len=lens[i]))
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[i]) and torch.equal(again, eager[i]), i
+
+
 GRAD = [
     dict(dtype="f32", B=1, K=1, S=1, H=1, Hkv=1, dh=32, T=1, L=1, lens="full"),
     dict(dtype="f32", B=1, K=2, S=3, H=2, Hkv=1, dh=32, T=0, L=3, lens="own"),
