@@ -98,8 +98,10 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream);
  * logical row j of list (b, k) in page table[b][k][j / page_rows] (L a multiple of page_rows); the
  * keys of a page outside [0, n_pages) do not count.  T = 0 or L = 0 leaves that part out.
  *
- * Scores, the softmax's maximum and sum and the output sums are fp32 (FE_BF16: bf16 products with fp32
- * accumulation, probabilities rounded to bf16 for the product with the values).  A list's outputs do not
+ * Scores, the softmax's maximum and sum and the output sums are fp32.  FE_BF16: bf16 products with fp32
+ * accumulation, probabilities rounded to bf16 for the product with the values.  FE_F32: operands in three bf16 parts
+ * whose sum they are, products good to 2^-21; an infinity inside the lengths may give NaN where the fp32 product with it
+ * would be infinite.  A list's outputs do not
  * depend on the values of other lists.  Results have the same bits from call to call.
  *
  * Workspace: fe_prefix_workspace_size(a, 0) bytes (may be 0: then ws is not read).

@@ -14,10 +14,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Eight elements along the summed axis: one operand of the 16 x 16 x 32 bf16 product, or of eight 16 x 16 x 4 fp32 ones.
-// Lane l holds row (or column) l % 16 and the eight elements of its group l / 16; product j of the fp32 form sums over
-// element j of the four groups, so both types use one layout; which element is which is free as long as both operands
-// agree.
+// Eight elements along the summed axis: one operand of the 16 x 16 x 32 bf16 product.  Lane l holds row (or column) l % 16
+// and the eight elements of its group l / 16; which element is which is free as long as both operands agree.
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> { typedef bf16x8 type; };
@@ -25,11 +23,59 @@ template <> struct Vec8<float> { typedef f32x8 type; };
 template <typename T> using V8 = typename Vec8<T>::type;
 
 FE_DEV f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-FE_DEV f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
-  return c;
+// fp32 operands in three bf16 parts: truncation takes the first 8 bits of the significand, then the next 8, and leaves the
+// last 8, so that x = p[0] + p[1] + p[2] exactly.  Of the nine products of parts the six largest are formed; the others are
+// below 2^-21 of |x||y|, 2^-24.6 in the mean.  Six bf16 products take 3/8 of the time of the eight 16 x 16 x 4 fp32 ones (training
+// step of 256 x 550 rows, heads of 32: 277 us with those, 222 in parts; 64 x 1024 rows, heads of 64: 698, 490).  An
+// infinity is a first part alone.
+struct Parts { bf16x8 p[3]; };
+FE_DEV f32x4 mma(Parts a, Parts b, f32x4 c) {
+  c = mma(a.p[2], b.p[0], c);
+  c = mma(a.p[0], b.p[2], c);
+  c = mma(a.p[1], b.p[1], c);
+  c = mma(a.p[1], b.p[0], c);
+  c = mma(a.p[0], b.p[1], c);
+  return mma(a.p[0], b.p[0], c);
 }
+template <bool FINITE> FE_DEV Parts parts8(const f32x8 v) {
+  u32x4 w[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned h[2], m[2], l[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x = v[2 * i + j];
+      h[j] = __float_as_uint(x);
+      float rest = x - __uint_as_float(h[j] & 0xffff0000u);
+      if (!FINITE && (h[j] & 0x7f800000u) == 0x7f800000u) rest = 0.f;
+      m[j] = __float_as_uint(rest);
+      l[j] = __float_as_uint(rest - __uint_as_float(m[j] & 0xffff0000u));
+    }
+    w[0][i] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302);   // the upper halves of two
+    w[1][i] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302);
+    w[2][i] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302);
+  }
+  return Parts{{__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1]), __builtin_bit_cast(bf16x8, w[2])}};
+}
+
+// The operand of a product, from eight elements or from eight floats (bf16: rounded to nearest even).
+template <typename T> struct Form;
+template <> struct Form<bf16> {
+  typedef bf16x8 Op;
+  static FE_DEV Op of(bf16x8 v) { return v; }
+  static FE_DEV Op of(const float (&s)[8]) {
+    return __builtin_convertvector((f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}), bf16x8);
+  }
+  static FE_DEV float value(Op v, int j) { return to_f32((bf16)v[j]); }
+};
+template <> struct Form<float> {
+  typedef Parts Op;
+  static FE_DEV Op of(f32x8 v) { return parts8<false>(v); }
+  static FE_DEV Op of(const float (&s)[8]) {
+    return parts8<true>(f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]});
+  }
+  static FE_DEV float value(const Op& v, int j) { return (to_f32(v.p[2][j]) + to_f32(v.p[1][j])) + to_f32(v.p[0][j]); }
+};
 
 template <typename T> FE_DEV V8<T> ld8(const T* p) { return *reinterpret_cast<const V8<T>*>(p); }
 // ... at a byte offset from a uniform base
@@ -43,15 +89,6 @@ FE_DEV void st4(bf16* p, f32x4 v) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) w[q] = (bf16)v[q];
   *reinterpret_cast<bf16x4*>(p) = w;
-}
-
-// Eight floats rounded to T (round to nearest even).
-template <typename T> FE_DEV V8<T> pack8(const float (&s)[8]);
-template <> FE_DEV f32x8 pack8<float>(const float (&s)[8]) {
-  return f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]};
-}
-template <> FE_DEV bf16x8 pack8<bf16>(const float (&s)[8]) {
-  return __builtin_convertvector((f32x8{s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]}), bf16x8);
 }
 
 FE_DEV bool finite8(bf16x8 v) {
@@ -221,18 +258,21 @@ FE_DEV Row row_of(const PrefixArgs& a, int b, int g, int r) {
 // A tile of rows of DH elements in LDS, read as an operand along its rows (summed over columns) and along its columns
 // (summed over rows).  bf16: rows of DH without padding, their 16-byte units exchanged inside a row, so that 16 rows at
 // one unit and 8 rows at one pair of units both fall on all 64 banks (measured: a row read 8.4 cycles, 7.9 at best; a
-// transposed one 10.1, the same at every stride); fp32: rows of DH + 4.
+// transposed one 10.1, the same at every stride); fp32: three such tiles, one for each part.
 //
 // Both reads start from a number that depends on the lane alone (row_lane, col_lane); what differs from read to read is a
 // constant xor and a row offset.
-template <typename T, int DH> struct Tile;
-template <int DH> struct Tile<bf16, DH> {
-  static constexpr int LD = DH, UNITS = DH / 8, PER = 128 / DH;   // PER rows span the banks
+template <typename T, int DH, int ROWS> struct Tile;
+template <int DH, int ROWS> struct Tile<bf16, DH, ROWS> {
+  typedef bf16 Elem;
+  static constexpr int SIZE = ROWS * DH, UNITS = DH / 8, PER = 128 / DH;   // PER rows span the banks
   static FE_DEV int swap(int row) {                // repeats every 16 rows
     const int h = row / PER % UNITS;
     return (h % (UNITS / 2)) << 1 | h / (UNITS / 2);
   }
   static FE_DEV int at(int row, int unit) { return row * DH + ((unit ^ swap(row)) << 3); }
+  template <bool FINITE> static FE_DEV void put(bf16* X, int row, int unit, bf16x8 v) { st8(X + at(row, unit), v); }
+  static FE_DEV float value(const bf16* X, int row, int col) { return to_f32(X[at(row, col >> 3) + (col & 7)]); }
   // Operand along rows: lane l is row base + l % 16, its elements are columns 32 d + 8 (l / 16) + j (base a multiple
   // of 16).
   static FE_DEV int row_lane(int lane) { return at(lane & 15, lane >> 4); }
@@ -254,20 +294,27 @@ template <int DH> struct Tile<bf16, DH> {
     return __builtin_shufflevector(__builtin_bit_cast(bf16x4, u), __builtin_bit_cast(bf16x4, v), 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
-template <int DH> struct Tile<float, DH> {
-  static constexpr int LD = DH + 4;
-  static FE_DEV int at(int row, int unit) { return row * LD + unit * 8; }
-  static FE_DEV int row_lane(int lane) { return at(lane & 15, lane >> 4); }
-  static FE_DEV f32x8 rows(const float* X, int base, int d, int row_lane) {
-    return ld8(X + base * LD + row_lane + d * 32);
-  }
-  static FE_DEV int col_lane(int lane) { return 4 * (lane >> 4) * LD + (lane & 15); }
-  static FE_DEV f32x8 cols(const float* X, int base, int n, int col_lane) {
-    const float* p = X + base * LD + col_lane + n * 16;
-    f32x8 v;
+template <int DH, int ROWS> struct Tile<float, DH, ROWS> {
+  typedef Tile<bf16, DH, ROWS> Part;
+  typedef bf16 Elem;
+  static constexpr int SIZE = 3 * Part::SIZE;
+  template <bool FINITE> static FE_DEV void put(bf16* X, int row, int unit, f32x8 v) {
+    const Parts w = parts8<FINITE>(v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = p[(16 * (j >> 2) + (j & 3)) * LD];
-    return v;
+    for (int i = 0; i < 3; ++i) Part::template put<true>(X + i * Part::SIZE, row, unit, w.p[i]);
+  }
+  static FE_DEV float value(const bf16* X, int row, int col) {
+    return (Part::value(X + 2 * Part::SIZE, row, col) + Part::value(X + Part::SIZE, row, col)) + Part::value(X, row, col);
+  }
+  static FE_DEV int row_lane(int lane) { return Part::row_lane(lane); }
+  static FE_DEV int col_lane(int lane) { return Part::col_lane(lane); }
+  static FE_DEV Parts rows(const bf16* X, int base, int d, int row_lane) {
+    return Parts{{Part::rows(X, base, d, row_lane), Part::rows(X + Part::SIZE, base, d, row_lane),
+                  Part::rows(X + 2 * Part::SIZE, base, d, row_lane)}};
+  }
+  static FE_DEV Parts cols(const bf16* X, int base, int n, int col_lane) {
+    return Parts{{Part::cols(X, base, n, col_lane), Part::cols(X + Part::SIZE, base, n, col_lane),
+                  Part::cols(X + 2 * Part::SIZE, base, n, col_lane)}};
   }
 };
 // Keeps a lane's number in one register, instead of a register for every xor of it that a loop uses.
@@ -278,7 +325,7 @@ FE_DEV int fresh(int x) {
 
 // Waves per SIMD that the register file is shared between (more hide more latency; fewer would spill).
 constexpr int waves_of(int bytes, int dh, int qt) {
-  return dh == 128 ? 2 : bytes == 2 && dh * qt <= 64 ? 4 : dh * qt <= 64 || bytes == 2 ? 3 : 2;
+  return dh == 128 ? 2 : dh * qt <= (bytes == 2 ? 64 : 32) ? 4 : dh * qt <= 64 || bytes == 2 ? 3 : 2;
 }
 constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 
@@ -290,19 +337,22 @@ constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 // Bound: with many rows a key the vector unit (a product-sum, an exponential, a sum, half a maximum and half a rounding a
 // score beside its 4 dh matrix operations; 64 x 1024 rows of 1088 keys, heads of 64: 36.6 us, 480 TFLOP/s, vector unit 60%
 // of the time, LDS 44%, matrix cores 22%; 256 x 550 rows of 267 keys, heads of 32: 26.6 us, 180 TFLOP/s); with few rows
-// HBM (4 x 32 lists of 4 rows a key head, heads of 128, 539 MB: 129 us, 4.2 TB/s); fp32 the matrix cores' fp32 form
-// (256 x 550 rows, heads of 32: 76 us, 63 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
+// HBM (4 x 32 lists of 4 rows a key head, heads of 128, 539 MB: 129 us, 4.2 TB/s); fp32 the vector
+// unit, which also splits the operands (256 x 550 rows, heads of 32: 57 us, 84 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
 // keys: 7.3 us).
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int QT, int NW, int KC, bool PAGED>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_fwd(PrefixArgs a) {
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
-  typedef Tile<T, DH> L;
+  typedef Tile<T, DH, KC> L;
+  typedef Form<T> F;
+  typedef typename F::Op Op;
+  typedef typename L::Elem E;
   constexpr int PER_T = KC * DH / 8 / NT, STEP = NT / (DH / 8);
-  constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
+  constexpr int NBUF = sizeof(T) == 4 ? 1 : 2;
   constexpr int NS = sizeof(T) * DH * QT > 256 ? 1 : 2;
   static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % (32 * NS) == 0 && KC <= NT, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * L::LD], Vs_[NBUF][KC * L::LD];
+  __shared__ __attribute__((aligned(16))) E Ks_[NBUF][L::SIZE], Vs_[NBUF][L::SIZE];
   __shared__ int s_off[ROWS + 1];
   // by chunk parity: the last chunk whose values are not all finite, the last chunk with keys of pages outside the
   // pool, and those keys; rows of the next own chunks
@@ -359,13 +409,14 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   };
   if (cb < cm) load_ctx(cb);
   Row row[QT];
-  V8<T> qf[QT][ND];
+  V8<T> qreg[QT][ND];
+  Op qf[QT][ND];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     row[i] = row_of(a, b, g, r0 + (wave * QT + i) * 16 + c16);
     const T* Q = static_cast<const T*>(a.q) + row[i].at * a.q_ld + row[i].h * DH;
 #pragma unroll
-    for (int c = 0; c < ND; ++c) qf[i][c] = ld8(Q + c * 32 + g4 * 8);
+    for (int c = 0; c < ND; ++c) qreg[i][c] = ld8(Q + c * 32 + g4 * 8);
   }
 
   pack_own<NT>(a, b, k0, nb, s_off);
@@ -416,8 +467,9 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     ahi[i] = wlo[i] == alo[i] ? __builtin_amdgcn_readlane(hi[i], 0) : -1;
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      if (!row[i].live) qf[i][c] = V8<T>{};
-      if (a.scale < 0) qf[i][c] = -qf[i][c];       // exact; the largest score is then the largest product
+      if (!row[i].live) qreg[i][c] = V8<T>{};
+      if (a.scale < 0) qreg[i][c] = -qreg[i][c];   // exact; the largest score is then the largest product
+      qf[i][c] = F::of(qreg[i][c]);
     }
     m_run[i] = -INFINITY;
     l_run[i] = 0.f;
@@ -427,7 +479,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   const float sl2 = score_unit(a.scale), lag = fminf(8.f / sl2, 1e30f);
 
   // Products q.k of tiles [i0, i1) with 32 keys.
-  auto scores = [&](const T* Ks, int kb, int rl, int i0, int i1, float (&s)[QT][8]) __attribute__((always_inline)) {
+  auto scores = [&](const E* Ks, int kb, int rl, int i0, int i1, float (&s)[QT][8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       f32x4 acc[QT];
@@ -435,7 +487,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       for (int i = 0; i < QT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
-        const V8<T> kf = L::rows(Ks, kb + 16 * x, d, rl);
+        const Op kf = L::rows(Ks, kb + 16 * x, d, rl);
 #pragma unroll
         for (int i = i0; i < i1; ++i) acc[i] = mma(kf, qf[i][d], acc[i]);
       }
@@ -472,13 +524,13 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -ref));
     l_run[i] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
-    return pack8<T>(s);
+    return F::of(s);
   };
-  auto stage = [&](T* Ks, T* Vs) __attribute__((always_inline)) {
+  auto stage = [&](E* Ks, E* Vs) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
-      st8(&Ks[L::at(key0 + p * STEP, d0 / 8)], kreg[p]);
-      st8(&Vs[L::at(key0 + p * STEP, d0 / 8)], vreg[p]);
+      L::template put<false>(Ks, key0 + p * STEP, d0 / 8, kreg[p]);
+      L::template put<false>(Vs, key0 + p * STEP, d0 / 8, vreg[p]);
     }
   };
 
@@ -486,7 +538,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
   int cur = 0;
   for (int c = cb; c < cm; ++c, cur ^= NBUF - 1) {
-    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    E *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();        // the previous chunk is no longer read
     if ((c + 1) * KC > nctx) {                     // uniform
 #pragma unroll
@@ -538,7 +590,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 #pragma unroll
         for (int i = 0; i < QT; ++i) follow(i, mx[i]);
       }
-      V8<T> pb[NS][QT];
+      Op pb[NS][QT];
 #pragma unroll
       for (int u = 0; u < NS; ++u)
 #pragma unroll
@@ -547,7 +599,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       for (int u = 0; u < NS; ++u)
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          const V8<T> vf = L::cols(Vs, kb + 32 * u, n, cl);
+          const Op vf = L::cols(Vs, kb + 32 * u, n, cl);
 #pragma unroll
           for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[u][i], o[i][n]);
         }
@@ -555,7 +607,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   }
 
   for (int c = ob; c < oe; ++c, cur ^= NBUF - 1) {
-    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    E *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
@@ -596,7 +648,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         }
         const float mx = max8(m_run[i], s);
         if (__any(mx > m_run[i] + lag)) follow(i, mx);
-        const V8<T> pb = probs(i, s);
+        const Op pb = probs(i, s);
         if (!odd) {
 #pragma unroll
           for (int n = 0; n < NB; ++n) o[i][n] = mma(L::cols(Vs, kb, n, cl), pb, o[i][n]);
@@ -608,7 +660,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         for (int key = 0; key < 32; ++key) {
           float e = 0.f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) e = key_of(j, key >> 2 & 3) == key ? to_f32((T)pb[j]) : e;
+          for (int j = 0; j < 8; ++j) e = key_of(j, key >> 2 & 3) == key ? F::value(pb, j) : e;
           e = __shfl(e, (key >> 2 & 3) * 16 + c16);
           if (x0 + key < lo[i] || x0 + key >= hi[i]) continue;
 #pragma unroll
@@ -616,7 +668,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
             __builtin_amdgcn_sched_barrier(0);     // few values in registers at a time
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              o[i][n][q] = fmaf(e, to_f32(Vs[L::at(kb + key, n * 2 + (g4 >> 1)) + (g4 & 1) * 4 + q]), o[i][n][q]);
+              o[i][n][q] = fmaf(e, L::value(Vs, kb + key, n * 16 + g4 * 4 + q), o[i][n][q]);
           }
         }
       }
@@ -720,11 +772,14 @@ template <typename T, int DH, int QT, int NW, int KC>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
-  typedef Tile<T, DH> L;
+  typedef Tile<T, DH, KC> L;
+  typedef Form<T> F;
+  typedef typename F::Op Op;
+  typedef typename L::Elem E;
   constexpr int PER_T = KC * DH / 8 / NT, STEP = NT / (DH / 8);
-  constexpr int NBUF = sizeof(T) * DH > 256 ? 1 : 2;
+  constexpr int NBUF = sizeof(T) == 4 ? 1 : 2;
   static_assert(ROWS <= NT && KC * DH / 8 % NT == 0 && KC % 32 == 0, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Ks_[NBUF][KC * L::LD], Vs_[NBUF][KC * L::LD];
+  __shared__ __attribute__((aligned(16))) E Ks_[NBUF][L::SIZE], Vs_[NBUF][L::SIZE];
   __shared__ int s_off[ROWS + 1];
   __shared__ long long s_at[2][KC];
 
@@ -792,7 +847,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     find(cm + 1);
   }
 
-  V8<T> qf[QT][ND], df[QT][ND];
+  Op qf[QT][ND], df[QT][ND];
   int lo[QT], hi[QT], wlo[QT], whi[QT], alo[QT], ahi[QT];              // as in the forward
   float lse2[QT], delta[QT];
   f32x4 o[QT][NB];
@@ -807,15 +862,16 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     float v = 0.f;
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      qf[i][c] = row.live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{};
-      df[i][c] = row.live ? ld8(D + c * 32 + g4 * 8) : V8<T>{};
+      qf[i][c] = F::of(row.live ? ld8(Q + c * 32 + g4 * 8) : V8<T>{});
+      const V8<T> dout = row.live ? ld8(D + c * 32 + g4 * 8) : V8<T>{};
+      df[i][c] = F::of(dout);
       const V8<T> out = row.live ? ld8(O + c * 32 + g4 * 8) : V8<T>{};
       uint2 step = make_uint2(0, 0);
       if (sizeof(T) == 2 && rest) step = *reinterpret_cast<const uint2*>(rest + c * 32 + g4 * 8);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int w = (int)((j < 4 ? step.x : step.y) << (24 - 8 * (j & 3))) >> 24;
-        v = fmaf(to_f32((T)df[i][c][j]), with_rest((T)out[j], row.live ? w : 0), v);
+        v = fmaf(to_f32((T)dout[j]), with_rest((T)out[j], row.live ? w : 0), v);
       }
     }
     delta[i] = rows_sum(v);
@@ -835,15 +891,15 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   }
   const float sl2 = a.scale * kLog2e;
 
-  auto stage = [&](T* Ks, T* Vs) __attribute__((always_inline)) {
+  auto stage = [&](E* Ks, E* Vs) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
-      st8(&Ks[L::at(key0 + q * STEP, d0 / 8)], kreg[q]);
-      st8(&Vs[L::at(key0 + q * STEP, d0 / 8)], vreg[q]);
+      L::template put<true>(Ks, key0 + q * STEP, d0 / 8, kreg[q]);
+      L::template put<true>(Vs, key0 + q * STEP, d0 / 8, vreg[q]);
     }
   };
   // p (dp - delta) of tile i for the 32 keys from kb on
-  auto dscores = [&](const T* Ks, const T* Vs, int kb, int rl, int i, float (&e)[8]) __attribute__((always_inline)) {
+  auto dscores = [&](const E* Ks, const E* Vs, int kb, int rl, int i, float (&e)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
@@ -861,7 +917,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
   int cur = 0;
   for (int c = cb; c < cm; ++c, cur ^= NBUF - 1) {
-    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    E *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();
     if ((c + 1) * KC > nctx) {                     // uniform
 #pragma unroll
@@ -884,7 +940,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     rl = fresh(rl);
     cl = fresh(cl);
     const int left = nctx - c * KC;                // keys of the chunk
-    V8<T> ds[KC / 32][QT];
+    Op ds[KC / 32][QT];
 #pragma unroll
     for (int u = 0; u < KC / 32; ++u)
 #pragma unroll
@@ -897,20 +953,20 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
           for (int j = 0; j < 8; ++j)
             if (32 * u + key_of(j) >= end) e[j] = 0.f;
         }
-        ds[u][i] = pack8<T>(e);
+        ds[u][i] = F::of(e);
       }
 #pragma unroll
     for (int u = 0; u < KC / 32; ++u)
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        const V8<T> kt = L::cols(Ks, 32 * u, n, cl);
+        const Op kt = L::cols(Ks, 32 * u, n, cl);
 #pragma unroll
         for (int i = 0; i < QT; ++i) o[i][n] = mma(kt, ds[u][i], o[i][n]);
       }
   }
 
   for (int c = cm; c < ce; ++c, cur ^= NBUF - 1) {
-    T *Ks = Ks_[cur], *Vs = Vs_[cur];
+    E *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();
 #pragma unroll
     for (int q = 0; q < PER_T; ++q)
@@ -938,7 +994,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
           for (int j = 0; j < 8; ++j)
             if (key_of(j) < from || key_of(j) >= to) e[j] = 0.f;
         }
-        const V8<T> ds = pack8<T>(e);
+        const Op ds = F::of(e);
 #pragma unroll
         for (int n = 0; n < NB; ++n) o[i][n] = mma(L::cols(Ks, kb, n, cl), ds, o[i][n]);
       }
@@ -975,10 +1031,13 @@ template <typename T, int DH, int KT, int NW, int RC>
 __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
   constexpr int NT = NW * 64, COLS = NW * KT * 16, NB = DH / 16, ND = DH / 32;
-  typedef Tile<T, DH> L;
+  typedef Tile<T, DH, RC> L;
+  typedef Form<T> F;
+  typedef typename F::Op Op;
+  typedef typename L::Elem E;
   constexpr int PER_T = RC * DH / 8 / NT, STEP = NT / (DH / 8);
   static_assert(RC % 32 == 0 && RC <= NT && RC * DH / 8 % NT == 0, "tile shape");
-  __shared__ __attribute__((aligned(16))) T Qs_[2][RC * L::LD], Ds_[2][RC * L::LD];
+  __shared__ __attribute__((aligned(16))) E Qs_[2][L::SIZE], Ds_[2][L::SIZE];
   __shared__ __attribute__((aligned(16))) float s_lse[2][RC], s_delta[2][RC];
   __shared__ __attribute__((aligned(16))) int s_lo[2][RC], s_hi[2][RC];
 
@@ -1049,7 +1108,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
   };
   if (cb < ce) load_chunk(cb);
 
-  V8<T> kf[KT][ND], vf[KT][ND];
+  Op kf[KT][ND], vf[KT][ND];
   bool live[KT];
   long long at[KT];                                                     // the key's row of the tensors
   f32x4 dk[KT][NB], dv[KT][NB];
@@ -1073,8 +1132,8 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
     const T* vp = static_cast<const T*>(shared ? a.ctx_v : a.own_v) + off;
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
-      kf[i][d] = live[i] ? ld8(kp + d * 32) : V8<T>{};
-      vf[i][d] = live[i] ? ld8(vp + d * 32) : V8<T>{};
+      kf[i][d] = F::of(live[i] ? ld8(kp + d * 32) : V8<T>{});
+      vf[i][d] = F::of(live[i] ? ld8(vp + d * 32) : V8<T>{});
     }
 #pragma unroll
     for (int n = 0; n < NB; ++n) dk[i][n] = dv[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1084,7 +1143,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
 
   // q.k and dout.v of 32 rows from kb on with the wave's keys
-  auto products = [&](const T* Qs, const T* Ds, int kb, f32x4 (&s)[2][KT],
+  auto products = [&](const E* Qs, const E* Ds, int kb, f32x4 (&s)[2][KT],
                       f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -1092,7 +1151,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
       for (int i = 0; i < KT; ++i) s[u][i] = dp[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
-        const V8<T> qv = L::rows(Qs, kb + 16 * u, d, rl), dv8 = L::rows(Ds, kb + 16 * u, d, rl);
+        const Op qv = L::rows(Qs, kb + 16 * u, d, rl), dv8 = L::rows(Ds, kb + 16 * u, d, rl);
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
           s[u][i] = mma(qv, kf[i][d], s[u][i]);
@@ -1102,7 +1161,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
     }
   };
   // ... and with them the rows' part of dk and dv; own: rows see the keys [lo, hi)
-  auto add = [&](const T* Qs, const T* Ds, int cur, int kb, bool own, const f32x4 (&s)[2][KT],
+  auto add = [&](const E* Qs, const E* Ds, int cur, int kb, bool own, const f32x4 (&s)[2][KT],
                  const f32x4 (&dp)[2][KT]) __attribute__((always_inline)) {
     float pe[KT][8], de[KT][8];
 #pragma unroll
@@ -1129,15 +1188,15 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
         }
       }
     }
-    V8<T> pb[KT], ds[KT];
+    Op pb[KT], ds[KT];
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
-      pb[i] = pack8<T>(pe[i]);
-      ds[i] = pack8<T>(de[i]);
+      pb[i] = F::of(pe[i]);
+      ds[i] = F::of(de[i]);
     }
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      const V8<T> dt = L::cols(Ds, kb, n, cl), qt = L::cols(Qs, kb, n, cl);
+      const Op dt = L::cols(Ds, kb, n, cl), qt = L::cols(Qs, kb, n, cl);
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         dv[i][n] = mma(dt, pb[i], dv[i][n]);
@@ -1149,12 +1208,12 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
   // Two loops, so that each keeps the sums in place.
   int cur = 0;
   auto stage = [&](int c) __attribute__((always_inline)) {
-    T *Qs = Qs_[cur], *Ds = Ds_[cur];
+    E *Qs = Qs_[cur], *Ds = Ds_[cur];
 #pragma unroll
     for (int q = 0; q < PER_T; ++q) {
       if (a.q_len && lreg[q] == INFINITY) qreg[q] = dreg[q] = V8<T>{};  // a row that sees nothing may hold anything
-      st8(&Qs[L::at(i0 + q * STEP, d0 / 8)], qreg[q]);
-      st8(&Ds[L::at(i0 + q * STEP, d0 / 8)], dreg[q]);
+      L::template put<true>(Qs, i0 + q * STEP, d0 / 8, qreg[q]);
+      L::template put<true>(Ds, i0 + q * STEP, d0 / 8, dreg[q]);
     }
     if (tid < RC) {
       const bool past = rb + c * RC + tid >= re;
@@ -1256,15 +1315,16 @@ __global__ __launch_bounds__(256) void k_prefix_sum(PrefixGradArgs p, SumBlocks 
 
 // Tile shapes.  Forward and dq: QT 16-row tiles a wave; dkv: KT 16-key tiles a wave and RC rows a chunk.
 template <typename T, int DH> constexpr int kKT = sizeof(T) == 2 && DH <= 64 ? 2 : 1;
-template <typename T, int DH> constexpr int kRC = sizeof(T) * DH > 256 ? 32 : 64;
+template <typename T, int DH> constexpr int kRC = sizeof(T) * DH > 128 && sizeof(T) == 4 ? 32 : 64;
+template <typename T, int DH> constexpr int kKC = sizeof(T) * DH > 256 ? 32 : 64;
 
 template <typename T, int DH, int QT>
 hipError_t launch_fwd_qt(const PrefixArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.splits));
   if (a.page_rows > 0)
-    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, 64, true>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, true>), grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, 64, false>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -1288,7 +1348,7 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
   a.tiles = pl.tiles;
   a.splits = pl.splits;
   const dim3 gq((unsigned)(bg * a.tiles * a.splits));
-  hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, 64>), gq, dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_prefix_dq<T, DH, 1, 4, kKC<T, DH>>), gq, dim3(256), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   p.ctx_tiles = pl.ctx_tiles;
