@@ -338,7 +338,7 @@ constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 // score beside its 4 dh matrix operations; 64 x 1024 rows of 1088 keys, heads of 64: 36.6 us, 480 TFLOP/s, vector unit 60%
 // of the time, LDS 44%, matrix cores 22%; 256 x 550 rows of 267 keys, heads of 32: 26.6 us, 180 TFLOP/s); with few rows
 // HBM (4 x 32 lists of 4 rows a key head, heads of 128, 539 MB: 129 us, 4.2 TB/s); fp32 the vector
-// unit, which also splits the operands (256 x 550 rows, heads of 32: 57 us, 84 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
+// unit, which also splits the operands (75% of the time; 256 x 550 rows, heads of 32: 60 us, 80 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
 // keys: 7.3 us).
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int QT, int NW, int KC, bool PAGED>
@@ -766,8 +766,8 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
 //   y = dout . out,   z, w = the own rows that it sees, numbered k L + j  [z, w).
 // ds goes into the product with the keys as it lies in the registers, as the probabilities do in the forward.
 // Bound: LDS (55% of the time: every wave reads keys twice and values once for its 16 rows) and the vector unit (48%)
-// beside 27% of matrix cores (64 x 1024 rows of 1088 keys, heads of 64: 46 us, 576 TFLOP/s); fp32 the matrix cores
-// (256 x 550 rows, heads of 32: 102 us, 70 TFLOP/s).
+// beside 27% of matrix cores (64 x 1024 rows of 1088 keys, heads of 64: 46 us, 576 TFLOP/s); fp32 the vector unit (63%;
+// 256 x 550 rows, heads of 32: 71 us, 101 TFLOP/s).
 template <typename T, int DH, int QT, int NW, int KC>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -1026,7 +1026,8 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 // Scores are formed a second time: sums of dq by key tiles would be B K S n_heads dh floats for every tile of 128 keys,
 // more traffic than the two products cost.
 // Bound: vector unit (43% of the time), LDS and matrix cores (30% each) with two waves a SIMD (64 x 1024 rows of 1088
-// keys, heads of 64: 57 us, 625 TFLOP/s); fp32 the matrix cores (256 x 550 rows, heads of 32: 130 us, 74 TFLOP/s).
+// keys, heads of 64: 57 us, 625 TFLOP/s); fp32 the vector unit (66%; 256 x 550 rows, heads of 32: 93 us, 103
+// TFLOP/s).  fp32 heads of 128 take a whole compute unit's LDS and one wave a SIMD, whose registers hold everything.
 template <typename T, int DH, int KT, int NW, int RC>
 __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
