@@ -1231,6 +1231,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
   if (shared) {
     for (int c = cb; c < ce; ++c, cur ^= 1) {
       stage(c);
+      if (x0 + wave * KT * 16 >= nctx) continue;                        // uniform: the wave's keys are past the length
 #pragma unroll
       for (int kb = 0; kb < RC; kb += 32) {                             // rows past the end have probability 0
         f32x4 s[2][KT], dp[2][KT];
