@@ -91,19 +91,23 @@ FE_DEV void st4(bf16* p, f32x4 v) {
   *reinterpret_cast<bf16x4*>(p) = w;
 }
 
-FE_DEV bool finite8(bf16x8 v) {
+// The largest magnitudes among several vectors, as bit patterns (bf16: of the even and of the odd elements), and
+// whether they are all finite.
+FE_DEV unsigned peak(unsigned m, bf16x8 v) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   const u32x4 w = __builtin_bit_cast(u32x4, v);
-  bool bad = false;
+  u16x2 top = __builtin_bit_cast(u16x2, m);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  return !bad;
+  for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+  return __builtin_bit_cast(unsigned, top);
 }
-FE_DEV bool finite8(f32x8 v) {
-  bool bad = false;
+FE_DEV unsigned peak(unsigned m, f32x8 v) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) bad |= (__float_as_uint(v[i]) & 0x7f800000u) == 0x7f800000u;
-  return !bad;
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+template <typename T> FE_DEV bool finite(unsigned m) {
+  return sizeof(T) == 4 ? m < 0x7f800000u : max(m & 0xffffu, m >> 16) < 0x7f80u;
 }
 
 FE_DEV int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
@@ -146,16 +150,16 @@ FE_DEV void store_out(const PrefixArgs& a, long long at, int col, f32x4 v);
 template <>
 FE_DEV void store_out<bf16>(const PrefixArgs& a, long long at, int col, f32x4 v) {
   bf16x4 w;
-  unsigned rest = 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    w[q] = (bf16)v[q];
-    // the eight bits below the rounded value's, as a signed step of its bit pattern
-    const int step = ((int)__float_as_uint(v[q]) - (int)__float_as_uint((float)w[q])) >> 8;
-    rest |= (unsigned)(min(step, 127) & 255) << (8 * q);
-  }
+  for (int q = 0; q < 4; ++q) w[q] = (bf16)v[q];
   *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.out) + at * a.out_ld + col) = w;
-  if (a.out_rest) *reinterpret_cast<unsigned*>(a.out_rest + at * a.Hq * a.dh + col) = rest;
+  if (!a.out_rest) return;                         // uniform
+  // the eight bits below the rounded value's, as a signed step of its bit pattern: the second byte of the difference
+  int d[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) d[q] = min((int)__float_as_uint(v[q]) - (int)__float_as_uint((float)w[q]), 0x7fff);
+  *reinterpret_cast<unsigned*>(a.out_rest + at * a.Hq * a.dh + col) =
+      __builtin_amdgcn_perm(d[1], d[0], 0x0c0c0501) | __builtin_amdgcn_perm(d[3], d[2], 0x05010c0c);
 }
 // ... and back: out with its rest, to 2^-16.
 FE_DEV float with_rest(bf16 v, int step) { return __uint_as_float(__float_as_uint((float)v) + step * 256); }
@@ -465,9 +469,13 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     alo[i] = __builtin_amdgcn_readlane(lo[i], 15);
     whi[i] = __builtin_amdgcn_readlane(s_off[row[i].k - k0 + 1], 15);
     ahi[i] = wlo[i] == alo[i] ? __builtin_amdgcn_readlane(hi[i], 0) : -1;
+    if (__any(!row[i].live)) {
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+        if (!row[i].live) qreg[i][c] = V8<T>{};
+    }
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      if (!row[i].live) qreg[i][c] = V8<T>{};
       if (a.scale < 0) qreg[i][c] = -qreg[i][c];   // exact; the largest score is then the largest product
       qf[i][c] = F::of(qreg[i][c]);
     }
@@ -609,12 +617,17 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   for (int c = ob; c < oe; ++c, cur ^= NBUF - 1) {
     E *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();
+    if (__any(gone)) {
 #pragma unroll
-    for (int p = 0; p < PER_T; ++p) {
-      if (gone >> p & 1) kreg[p] = vreg[p] = V8<T>{};
-      if (!finite8(vreg[p])) s_odd[c & 1] = c;
-      if (PAGED && hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
+      for (int p = 0; p < PER_T; ++p) {
+        if (gone >> p & 1) kreg[p] = vreg[p] = V8<T>{};
+        if (PAGED && hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
+      }
     }
+    unsigned top = 0;
+#pragma unroll
+    for (int p = 0; p < PER_T; ++p) top = peak(top, vreg[p]);
+    if (!finite<T>(top)) s_odd[c & 1] = c;
     stage(Ks, Vs);
     if (tid < KC) s_at[(c + 1) & 1][tid] = found.row(a);
     lds_barrier();
@@ -694,13 +707,13 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     }
     const bool none = !row[i].live || l == 0.f;    // no key; a NaN score leaves a NaN sum
     const float inv = none ? 0.f : 1.f / l;
+    if (__any(none)) {
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      f32x4 v;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = none ? 0.f : o[i][n][q] * inv;
-      store_out<T>(a, row[i].at, row[i].h * DH + n * 16 + g4 * 4, v);
+      for (int n = 0; n < NB; ++n)
+        if (none) o[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) store_out<T>(a, row[i].at, row[i].h * DH + n * 16 + g4 * 4, o[i][n] * inv);
     if (a.lse && g4 == 0) a.lse[ro] = none ? -INFINITY : (m2 + log2f(l)) * kLn2;
   }
 }
@@ -968,9 +981,11 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   for (int c = cm; c < ce; ++c, cur ^= NBUF - 1) {
     E *Ks = Ks_[cur], *Vs = Vs_[cur];
     if constexpr (NBUF == 1) lds_barrier();
+    if (__any(gone)) {
 #pragma unroll
-    for (int q = 0; q < PER_T; ++q)
-      if (gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
+      for (int q = 0; q < PER_T; ++q)
+        if (gone >> q & 1) kreg[q] = vreg[q] = V8<T>{};
+    }
     stage(Ks, Vs);
     if (tid < KC) s_at[(c + 1) & 1][tid] = found.row(a);
     lds_barrier();
