@@ -25,7 +25,9 @@ def attend(q, ck, cv, ok, ov, *, dtype, causal, scale=None, ctx_len=None, q_len=
       delta = dout.out takes that error times |dout|, plus dh e sum |dout||out|;
       dp    is off by dh e sum |dout||v|;
       ds = p (dp - delta) is off by p (err dp + err delta) + (rp + u_p + 2 e) |ds|, and dq, dk sum it times |k|, |q|;
-      dv sums (rp + u_p) p |dout|; the sums of N terms add N e times the sum of the terms' sizes."""
+      dv sums (rp + u_p) p |dout|; the sums of N terms add N e times the sum of the terms' sizes.
+    FE_F32's products in three parts are good to 2^-21 = 8 e each and add a part's six sums every 32 terms: both lie inside
+    (dh + 2) e for a score and dh e for dp (dh >= 32), and inside rp >= 32 e in the sums over keys and rows."""
     B, K, S, H, dh = q.shape
     T, Hkv, L = ck.shape[1], ck.shape[2] if ck.shape[1] else ok.shape[3], ok.shape[2]
     G, scale = H // Hkv, dh ** -0.5 if scale is None else scale
