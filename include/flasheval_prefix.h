@@ -99,10 +99,10 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream);
  * keys of a page outside [0, n_pages) do not count.  T = 0 or L = 0 leaves that part out.
  *
  * Scores, the softmax's maximum and sum and the output sums are fp32.  FE_BF16: bf16 products with fp32
- * accumulation, probabilities rounded to bf16 for the product with the values.  FE_F32: operands in three bf16 parts
- * whose sum they are, products good to 2^-21; an infinity inside the lengths may give NaN where the fp32 product with it
- * would be infinite.  A list's outputs do not
- * depend on the values of other lists.  Results have the same bits from call to call.
+ * accumulation, probabilities rounded to bf16 for the product with the values (with out_rest, dense own rows and
+ * T + L <= 256: to two bf16, 16 bits).  FE_F32: operands in three bf16 parts whose sum they are, products good to
+ * 2^-21; an infinity inside the lengths may give NaN where the fp32 product with it would be infinite.
+ * A list's outputs do not depend on the values of other lists.  Results have the same bits from call to call.
  *
  * Workspace: fe_prefix_workspace_size(a, 0) bytes (may be 0: then ws is not read).
  *
@@ -148,8 +148,9 @@ fe_status fe_prefix_attention(const fe_prefix_args* a, void* stream);
  * where a key's sums run over every list (shared rows), row and head that reads it.  Every row of dq, of the shared
  * gradients [B][T] and of the own gradients [B][K][L] is written; rows outside the lengths are zero.  dout
  * rows i >= q_len are not read into anything.  Sums are fp32, in a fixed order without atomics, rounded
- * once; FE_BF16 rounds p and ds to bf16 for the products.  Values inside the lengths have to be finite: one that is
- * not may reach the gradients of the other lists of its request.
+ * once; FE_BF16 rounds p and ds to bf16 for the products (own keys' gradients:
+ * to two bf16, 16 bits).  Values inside the lengths have to be finite: one that is not may reach the gradients
+ * of the other lists of its request.
  * dctx_k, dctx_v (own: down_k, down_v) may be NULL only when T (L) is 0.
  */
 typedef struct {

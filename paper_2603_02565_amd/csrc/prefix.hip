@@ -345,7 +345,7 @@ constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 // unit, which also splits the operands (75% of the time; 256 x 550 rows, heads of 32: 60 us, 80 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
 // keys: 7.3 us).
 // ------------------------------------------------------------------------------------------
-template <typename T, int DH, int QT, int NW, int KC, bool PAGED>
+template <typename T, int DH, int QT, int NW, int KC, bool PAGED, bool FINE>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_fwd(PrefixArgs a) {
   constexpr int NT = NW * 64, ROWS = NW * QT * 16, NB = DH / 16, ND = DH / 32;
   typedef Tile<T, DH, KC> L;
@@ -526,13 +526,22 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       for (int n = 0; n < NB; ++n) o[i][n] *= alpha;
     }
   };
-  // Probabilities against the reference, added to the sum, as the operand of the product with the values.
-  auto probs = [&](int i, float (&s)[8]) __attribute__((always_inline)) {
+  // Probabilities against the reference, added to the sum, as the operand of the product with the values.  FINE: what its
+  // rounding cut is a second one.  A training step over few keys needs it, as its gradient takes D = dout . out from out and
+  // ds = p (dp - D) may be small beside D: keys 1 + 2, dq off by 3.1e-3 of its norm without, 2.3e-3 with; 4 + 11 2.6e-3,
+  // 2.3e-3; 130 + 44 2.40e-3, 2.36e-3; 1024 + 64 the same, at 142 us a step for 155.
+  auto probs = [&](int i, float (&s)[8], Op& fine) __attribute__((always_inline)) {
     const float ref = m_run[i] == -INFINITY ? 0.f : m_run[i] * sl2;   // a row without keys so far: exp2(-inf) = 0
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], sl2, -ref));
     l_run[i] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
-    return F::of(s);
+    const Op p = F::of(s);
+    if constexpr (FINE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] -= F::value(p, j);
+      fine = F::of(s);
+    }
+    return p;
   };
   auto stage = [&](E* Ks, E* Vs) __attribute__((always_inline)) {
 #pragma unroll
@@ -598,18 +607,21 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 #pragma unroll
         for (int i = 0; i < QT; ++i) follow(i, mx[i]);
       }
-      Op pb[NS][QT];
+      Op pb[NS][QT], pf[NS][QT];
 #pragma unroll
       for (int u = 0; u < NS; ++u)
 #pragma unroll
-        for (int i = 0; i < QT; ++i) pb[u][i] = probs(i, s[u][i]);
+        for (int i = 0; i < QT; ++i) pb[u][i] = probs(i, s[u][i], pf[u][i]);
 #pragma unroll
       for (int u = 0; u < NS; ++u)
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const Op vf = L::cols(Vs, kb + 32 * u, n, cl);
 #pragma unroll
-          for (int i = 0; i < QT; ++i) o[i][n] = mma(vf, pb[u][i], o[i][n]);
+          for (int i = 0; i < QT; ++i) {
+            if (FINE) o[i][n] = mma(vf, pf[u][i], o[i][n]);
+            o[i][n] = mma(vf, pb[u][i], o[i][n]);
+          }
         }
     }
   }
@@ -661,10 +673,15 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         }
         const float mx = max8(m_run[i], s);
         if (__any(mx > m_run[i] + lag)) follow(i, mx);
-        const Op pb = probs(i, s);
+        Op pf;
+        const Op pb = probs(i, s, pf);
         if (!odd) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) o[i][n] = mma(L::cols(Vs, kb, n, cl), pb, o[i][n]);
+          for (int n = 0; n < NB; ++n) {
+            const Op vf = L::cols(Vs, kb, n, cl);
+            if (FINE) o[i][n] = mma(vf, pf, o[i][n]);
+            o[i][n] = mma(vf, pb, o[i][n]);
+          }
           continue;
         }
         // A value of the chunk is not finite: in a product it would reach the rows that do not see its key, as 0
@@ -1052,6 +1069,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
   typedef typename F::Op Op;
   typedef typename L::Elem E;
   constexpr int PER_T = RC * DH / 8 / NT, STEP = NT / (DH / 8);
+  constexpr bool FINE = sizeof(T) == 2;
   static_assert(RC % 32 == 0 && RC <= NT && RC * DH / 8 % NT == 0, "tile shape");
   __shared__ __attribute__((aligned(16))) E Qs_[2][L::SIZE], Ds_[2][L::SIZE];
   __shared__ __attribute__((aligned(16))) float s_lse[2][RC], s_delta[2][RC];
@@ -1210,11 +1228,31 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
       pb[i] = F::of(pe[i]);
       ds[i] = F::of(de[i]);
     }
+    // An own key meets few rows, and one may make most of its sums: bf16 adds what the roundings cut (dk off by 2.4e-3
+    // to 3.3e-3 of its norm without, 1.7e-3 with, which is its own rounding; training step of 256 x 550 rows, heads of 32,
+    // 87 us without, 93 with, of 64 x 1024 rows, heads of 64, the same).
+    Op pf[KT], df[KT];
+    if (FINE && own) {
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          pe[i][j] -= F::value(pb[i], j);
+          de[i][j] -= F::value(ds[i], j);
+        }
+        pf[i] = F::of(pe[i]);
+        df[i] = F::of(de[i]);
+      }
+    }
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const Op dt = L::cols(Ds, kb, n, cl), qt = L::cols(Qs, kb, n, cl);
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
+        if (FINE && own) {
+          dv[i][n] = mma(dt, pf[i], dv[i][n]);
+          dk[i][n] = mma(qt, df[i], dk[i][n]);
+        }
         dv[i][n] = mma(dt, pb[i], dv[i][n]);
         dk[i][n] = mma(qt, ds[i], dk[i][n]);
       }
@@ -1339,9 +1377,11 @@ template <typename T, int DH, int QT>
 hipError_t launch_fwd_qt(const PrefixArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.splits));
   if (a.page_rows > 0)
-    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, true>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, true, false>), grid, dim3(256), 0, s, a);
+  else if (sizeof(T) == 2 && a.out_rest && a.T + a.L <= 256)             // few keys: see the probabilities there
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, false, sizeof(T) == 2>), grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, false>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, false, false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
