@@ -607,17 +607,38 @@ def _stream_on(index: int, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _allocated_for(stream, *tensors) -> None:
-    """Tensors just allocated that `stream`, not the current one, is about to use: it waits for what the current stream still
-    does in their memory, and the memory is not given out again before its own work there has ended."""
+def _allocated_for(stream, *tensors, home=None) -> None:
+    """Tensors allocated on the stream `home` (the current one) that `stream`, another one, is about to use: it waits for what
+    `home` still does in their memory, and the memory is not given out again before its own work there has ended."""
     import torch
-    if stream is None or _stream(stream) == torch.cuda.current_stream().cuda_stream:
+    home = torch.cuda.current_stream() if home is None else home
+    if stream is None or _stream(stream) == home.cuda_stream:
         return
-    other = torch.cuda.ExternalStream(_stream(stream))
-    other.wait_stream(torch.cuda.current_stream())
+    other = torch.cuda.ExternalStream(_stream(stream)) if _stream(stream) else torch.cuda.default_stream()
+    other.wait_stream(home)
     for t in tensors:
         if t is not None:
             t.record_stream(other)
+
+
+class _Kept:
+    """Tensors that an object allocates for itself, on the current stream, and keeps: handed once to every other stream that
+    uses them."""
+
+    def __init__(self, *tensors):
+        import torch
+        self.tensors, self.home = tensors, torch.cuda.current_stream()
+        self.known = {self.home.cuda_stream}
+
+    def use_on(self, handle: int) -> None:
+        if handle in self.known:
+            return
+        import torch
+        if not torch.cuda.is_current_stream_capturing():
+            self.known.add(handle)
+        elif torch.cuda.current_stream().cuda_stream != self.home.cuda_stream:
+            return                           # a capture cannot wait for work outside it; it begins after that
+        _allocated_for(handle, *self.tensors, home=self.home)
 
 
 def _addr(t) -> Optional[int]:
@@ -650,6 +671,7 @@ class PagedCache:
         self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
         self.status = torch.zeros(self.N, dtype=torch.int32, device=table.device)
         _on_device((k_pages, v_pages, table, self.len))
+        self._kept = _Kept(self.status, self.len if length is None else None)
         a = self.args = fe_append_args()
         a.dtype = FE_BF16 if k_pages.dtype == torch.bfloat16 else FE_F32
         a.n_pages, a.page_rows, a.n_kv_heads, a.dh = shape
@@ -692,11 +714,12 @@ class PagedCache:
             _allocated_for(stream, q_out)
         a.S, a.n_heads, a.k_ld, a.v_ld, a.q_ld, a.q_out_ld, a.rot = self._layouts.of(
             self._check, k, v, q, q_out, freq, new_len, pos0, len_out)
-        index = _on_device((k, v, q, q_out, freq, new_len, pos0, len_out, self.k_pages))
+        handle = _stream_on(_on_device((k, v, q, q_out, freq, new_len, pos0, len_out, self.k_pages)), stream)
+        self._kept.use_on(handle)
         a.neighbours = 1 if neighbours else 0
         a.q, a.k, a.v, a.q_out, a.freq = _addr(q), k.data_ptr(), v.data_ptr(), _addr(q_out), _addr(freq)
         a.new_len, a.pos0, a.len_out = _addr(new_len), _addr(pos0), a.len if len_out is None else len_out.data_ptr()
-        fe_cache_append(a, _stream_on(index, stream))
+        fe_cache_append(a, handle)
         return q_out
 
 
@@ -729,7 +752,7 @@ class PrefixAttention:
         self._layouts = _Layouts()
 
     def allocate(self):
-        """Outputs and workspace on the current device (done by the first `run`)."""
+        """Outputs and workspace on the current device and stream (done by the first `run`)."""
         import torch
         a, dev = self.args, torch.device("cuda", torch.cuda.current_device())
         self.out = torch.empty((a.B, a.K, a.S, a.n_heads, a.dh), dtype=self.act, device=dev)
@@ -744,6 +767,7 @@ class PrefixAttention:
             self.grads = (torch.empty_like(self.out),
                           *(torch.empty((a.B, a.T, a.n_kv_heads, a.dh), dtype=self.act, device=dev) for _ in range(2)),
                           *(torch.empty((a.B, a.K, a.L, a.n_kv_heads, a.dh), dtype=self.act, device=dev) for _ in range(2)))
+        self._kept = _Kept(self.out, self.lse, self.out_rest, self.ws, *(self.grads or ()))
 
     def _check(self, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len):
         """(q_ld, ctx_ld, own_ld) of a call's tensors."""
@@ -773,17 +797,18 @@ class PrefixAttention:
         index = _on_device(tensors)
         if self.out is None:
             self.allocate()
-            _allocated_for(stream, self.out, self.lse, self.out_rest, self.ws, *(self.grads or ()))
         elif self.out.get_device() != index:
             raise ValueError(f"the outputs are on {self.out.device}, the tensors on device {index}")
         a.q, a.ctx_k, a.ctx_v, a.own_k, a.own_v = q.data_ptr(), _addr(ctx_k), _addr(ctx_v), _addr(own_k), _addr(own_v)
         a.table, a.ctx_len, a.own_len, a.q_len = _addr(table), _addr(ctx_len), _addr(own_len), _addr(q_len)
-        return index
+        handle = _stream_on(index, stream)
+        self._kept.use_on(handle)
+        return handle
 
     def run(self, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
         """Enqueue the attention; returns out [B][K][S][n_heads][dh] (self.lse holds the log sums when training)."""
-        index = self._take(stream, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
-        fe_prefix_attention(self.args, _stream_on(index, stream))
+        handle = self._take(stream, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        fe_prefix_attention(self.args, handle)
         return self.out
 
     def grad(self, dout, q, ctx_k, ctx_v, own_k, own_v, table=None, ctx_len=None, own_len=None, q_len=None, stream=None):
@@ -792,12 +817,12 @@ class PrefixAttention:
             raise ValueError("grad needs train=True")
         if self.out is None:
             raise ValueError("grad follows run")
-        index = self._take(stream, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
+        handle = self._take(stream, q, ctx_k, ctx_v, own_k, own_v, table, ctx_len, own_len, q_len)
         a, g = self.args, fe_prefix_grads()
         g.dout_ld = self._layouts.of(lambda t: _row_stride(t, "dout", self.q_shape, self.act), dout)
         _on_device((dout, q))
         g.dout = dout.data_ptr()
         g.dq_ld, g.dctx_ld, g.down_ld = a.n_heads * a.dh, a.n_kv_heads * a.dh, a.n_kv_heads * a.dh
         g.dq, g.dctx_k, g.dctx_v, g.down_k, g.down_v = (t.data_ptr() for t in self.grads)
-        fe_prefix_attention_grad(a, g, _stream_on(index, stream))
+        fe_prefix_attention_grad(a, g, handle)
         return self.grads

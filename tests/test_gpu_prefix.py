@@ -291,6 +291,40 @@ def test_first_call_on_a_given_stream():
     ac.check(q_out)
 
 
+def _busy():
+    """Some milliseconds of work on the current stream."""
+    a = torch.ones(4096, 4096, device="cuda")
+    for _ in range(10):
+        a = a @ a * 2.0 ** -12
+    return a
+
+
+def test_own_tensors_on_a_given_stream():
+    """Lengths that the cache starts at zero itself, and outputs allocated ahead, while their own stream is still busy with what
+    their memory held before."""
+    ac = AppendCase(seed=45, **APPEND[0])
+    (k, v), kw = ac.device()
+    ac.len[:] = 0
+    c = Case(dtype="bf16", B=1, K=4, S=1, H=4, Hkv=2, dh=64, T=3000, L=48, P=16, seed=46).device()
+    want = fe.PrefixAttention(**c.dims).run(*c.keys, **c.more).clone()
+    p = fe.PrefixAttention(**c.dims)
+    before = [torch.empty(ac.len.shape, dtype=torch.int32, device="cuda") for _ in range(2)]
+    old = [torch.empty_like(want), torch.empty(p.ws_bytes, dtype=torch.uint8, device="cuda")]
+    torch.cuda.synchronize()
+    kept = _busy()
+    for t in before + old:
+        t.fill_(77)
+    del before, old
+    ac.cache = fe.PagedCache(ac.cache.k_pages, ac.cache.v_pages, ac.cache.table)
+    p.allocate()
+    side = torch.cuda.Stream()
+    q_out = ac.cache.append(k, v, stream=side, **kw)
+    got = p.run(*c.keys, stream=side, **c.more)
+    torch.cuda.synchronize()
+    ac.check(q_out)
+    assert torch.equal(got, want) and bool(torch.isfinite(kept).all())
+
+
 def test_lists_do_not_depend_on_each_other():
     """The same list beside other lists of the same lengths: the same bits."""
     c = Case(dtype="bf16", B=1, K=12, S=7, H=4, Hkv=2, dh=64, T=100, L=15, seed=61).device()

@@ -172,6 +172,71 @@ def test_binding_checks_layouts():
         fe.PagedCache(pages, pages, table)
 
 
+class _Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+def _without_a_gpu(monkeypatch):
+    """The binding on CPU tensors, current stream 7, no library call; returns the list of (stream, tensors) handed over."""
+    handed = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream(7))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(fe, "_on_device", lambda tensors: 0)
+    monkeypatch.setattr(fe, "_allocated_for", lambda stream, *t, **kw: handed.append((stream, t)))
+    for name in ("fe_cache_append", "fe_prefix_attention", "fe_prefix_attention_grad"):
+        monkeypatch.setattr(fe, name, lambda *a: None)
+    return handed
+
+
+def _same(got, want):
+    return any(g is want for g in got)
+
+
+def test_a_caches_own_tensors_are_handed_to_a_given_stream(monkeypatch):
+    """The first append on a stream waits for the zeros of the lengths and of status that the cache made itself."""
+    handed = _without_a_gpu(monkeypatch)
+    pages, table, k = torch.zeros(4, 8, 2, 32), torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, 1, 2, 32)
+    cache = fe.PagedCache(pages, pages, table)
+    for stream in (7, 11, 11, 13):
+        cache.append(k, k, stream=stream)
+    streams = [s for s, t in handed if _same(t, cache.len) and _same(t, cache.status)]
+    assert streams == [11, 13]
+    del handed[:]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    cache.append(k, k, stream=17)                             # captured on the tensors' own stream: the wait is captured too
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream(19))
+    cache.append(k, k, stream=19)                             # on another: it cannot wait for what is outside the capture
+    assert [s for s, _ in handed] == [17]
+    del handed[:]
+    monkeypatch.undo()
+    handed = _without_a_gpu(monkeypatch)
+    cache.append(k, k, stream=17)                             # a capture says nothing about later calls
+    assert [s for s, _ in handed] == [17]
+    del handed[:]
+    mine = torch.zeros(3, dtype=torch.int32)                  # lengths of the caller's are the caller's to order
+    cache = fe.PagedCache(pages, pages, table, mine)
+    cache.append(k, k, stream=11)
+    assert [s for s, t in handed if _same(t, cache.status)] == [11] and not any(_same(t, mine) for _, t in handed)
+
+
+def test_outputs_are_handed_to_every_stream(monkeypatch):
+    """Outputs and workspace of an explicit allocate(), or of a call on another stream, as well."""
+    handed = _without_a_gpu(monkeypatch)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    p = fe.PrefixAttention(B=1, K=2, S=3, T=4, L=3, n_heads=2, n_kv_heads=1, dh=32, dtype="f32", train=True)
+    with monkeypatch.context() as m:
+        m.setattr(torch, "device", lambda *a: "cpu")
+        p.allocate()
+    p.out.get_device = lambda: 0
+    q, c, o = torch.zeros(1, 2, 3, 2, 32), torch.zeros(1, 4, 1, 32), torch.zeros(1, 2, 3, 1, 32)
+    for stream in (7, 11, 11):
+        p.run(q, c, c, o, o, stream=stream)
+    p.grad(q, q, c, c, o, o, stream=13)
+    streams = [s for s, t in handed if all(_same(t, x) for x in (p.out, p.lse, p.ws, *p.grads))]
+    assert streams == [11, 13]
+
+
 @pytest.mark.parametrize("shape,view,ld", [
     ((2, 3, 4, 32), lambda: torch.zeros(2, 3, 4, 32), 128),
     ((2, 3, 4, 32), lambda: torch.zeros(2, 3, 12, 32)[:, :, 4:8], 384),           # a column block of a fused projection
