@@ -102,7 +102,8 @@ fe_status fe_cache_append(const fe_append_args* a, void* stream);
  * accumulation, probabilities rounded to bf16 for the product with the values (with out_rest, dense own rows and
  * T + L <= 256: to two bf16, 16 bits).  FE_F32: operands in three bf16 parts whose sum they are, products good to
  * 2^-21; an infinity inside the lengths may give NaN where the fp32 product with it would be infinite.
- * A list's outputs do not depend on the values of other lists.  Results have the same bits from call to call.
+ * A list's outputs do not depend on the values of other lists, finite or not: they have the same bits.  Results have the
+ * same bits from call to call.
  *
  * Workspace: fe_prefix_workspace_size(a, 0) bytes (may be 0: then ws is not read).
  *

@@ -110,6 +110,14 @@ template <typename T> FE_DEV bool finite(unsigned m) {
   return sizeof(T) == 4 ? m < 0x7f800000u : max(m & 0xffffu, m >> 16) < 0x7f80u;
 }
 
+// v with zeros for its infinities and NaNs.
+FE_DEV bf16x8 finite_of(bf16x8 v) {
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  const u16x8 w = __builtin_bit_cast(u16x8, v);
+  return __builtin_bit_cast(bf16x8, (u16x8)((w & 0x7f80) == 0x7f80 ? (u16x8)0 : w));
+}
+FE_DEV Parts finite_of(const Parts& v) { return Parts{{finite_of(v.p[0]), finite_of(v.p[1]), finite_of(v.p[2])}}; }
+
 FE_DEV int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 FE_DEV int q_rows(const PrefixArgs& a, int bk) { return a.q_len ? clampi(a.q_len[bk], 0, a.S) : a.S; }
@@ -551,6 +559,33 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     }
   };
 
+  // A value of the chunk that is not finite would reach, in a product, the rows that do not see its key, as 0 times infinity.
+  // The products take a zero in its place, so that the other rows' results have the bits that they have beside finite
+  // values, and this adds it to tile i's rows that see it: those with from <= key < to, of the 32 keys from kb on.
+  auto add_odd = [&](const E* Vs, int kb, int i, int from, int to, const Op& pb, const Op& pf) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int key = 0; key < 32; ++key) {
+      float e = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float p = F::value(pb, j);
+        if (FINE) p += F::value(pf, j);
+        e = key_of(j, key >> 2 & 3) == key ? p : e;
+      }
+      e = __shfl(e, (key >> 2 & 3) * 16 + c16);
+      if (key < from || key >= to) continue;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        __builtin_amdgcn_sched_barrier(0);         // few values in registers at a time
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float v = L::value(Vs, kb + key, n * 16 + g4 * 4 + q);
+          o[i][n][q] = fmaf(e, __builtin_isfinite(v) ? 0.f : v, o[i][n][q]);
+        }
+      }
+    }
+  };
+
   const bool idle = r0 + wave * QT * 16 >= a.R;    // no row in the wave's tiles
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
   int cur = 0;
@@ -675,32 +710,14 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         if (__any(mx > m_run[i] + lag)) follow(i, mx);
         Op pf;
         const Op pb = probs(i, s, pf);
-        if (!odd) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            const Op vf = L::cols(Vs, kb, n, cl);
-            if (FINE) o[i][n] = mma(vf, pf, o[i][n]);
-            o[i][n] = mma(vf, pb, o[i][n]);
-          }
-          continue;
+        for (int n = 0; n < NB; ++n) {
+          Op vf = L::cols(Vs, kb, n, cl);
+          if (odd) vf = finite_of(vf);             // uniform
+          if (FINE) o[i][n] = mma(vf, pf, o[i][n]);
+          o[i][n] = mma(vf, pb, o[i][n]);
         }
-        // A value of the chunk is not finite: in a product it would reach the rows that do not see its key, as 0
-        // times infinity.  The same sums key by key, over the keys that the row sees.
-#pragma unroll 1
-        for (int key = 0; key < 32; ++key) {
-          float e = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) e = key_of(j, key >> 2 & 3) == key ? F::value(pb, j) : e;
-          e = __shfl(e, (key >> 2 & 3) * 16 + c16);
-          if (x0 + key < lo[i] || x0 + key >= hi[i]) continue;
-#pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            __builtin_amdgcn_sched_barrier(0);     // few values in registers at a time
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              o[i][n][q] = fmaf(e, L::value(Vs, kb + key, n * 16 + g4 * 4 + q), o[i][n][q]);
-          }
-        }
+        if (odd) add_odd(Vs, kb, i, lo[i] - x0, hi[i] - x0, pb, pf);
       }
     }
   }

@@ -12,7 +12,7 @@ from tests.gpu_harness import make_evaluator, upload
 pytestmark = pytest.mark.gpu
 
 ACT = {"bf16": torch.bfloat16, "f32": torch.float32}
-NAN = float("nan")
+NAN, INF = float("nan"), float("inf")
 
 
 def _say(*what):
@@ -418,6 +418,32 @@ def test_a_list_keeps_its_infinities_to_itself(dtype):
     # the same rows summed in another order: two roundings of the type and of a sum of 35 fp32 terms of size at most 4
     tol = 2 * ref.HALF_STEP[dtype] * want.abs().float() + 35 * 2.0 ** -24 * 4
     assert (((got - want).abs().float() <= tol) | hit).all()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype="bf16"), dict(dtype="bf16", train=True), dict(dtype="bf16", T=300, train=True), dict(dtype="bf16", P=2, dh=64),
+    dict(dtype="f32"), dict(dtype="f32", dh=64, P=2), dict(dtype="bf16", dh=128, train=True)])
+def test_infinities_leave_the_neighbours_bits(kw):
+    """Infinite and NaN own values of some lists: every output that sees none of them keeps its bits, and what out's rounding
+    cut as well."""
+    kw = dict(dict(T=30, dh=32, train=False), **kw)
+    train = kw.pop("train")
+    c = Case(B=1, K=9, S=5, H=2, Hkv=1, L=6, lens="full", seed=14, **kw).device()
+    p = fe.PrefixAttention(train=train, **c.dims)
+    want = p.run(*c.keys, **c.more).clone()
+    rest = p.out_rest.clone() if p.out_rest is not None else None
+    hit = torch.zeros(want.shape, dtype=torch.bool, device="cuda")
+    for k, j, col, value in ((2, 3, 7, INF), (4, 2, 0, NAN), (6, 0, 31, -INF), (6, 5, 8, INF)):
+        if c.P:
+            c.keys[4][int(c.table[0, k, j // c.P]), j % c.P, 0, col] = value
+        else:
+            c.keys[4][0, k, j, 0, col] = value
+        hit[0, k, max(0, j - 1):, :, col] = True            # causal: row i sees j <= i + 1
+    got = p.run(*c.keys, **c.more)
+    assert (got[0, 2, 2:, :, 7] == INF).all() and torch.isnan(got[0, 4, 1:, :, 0]).all()
+    assert (got[0, 6, :, :, 31] == -INF).all() and (got[0, 6, 4:, :, 8] == INF).all()
+    assert torch.equal(got[~hit], want[~hit])
+    assert rest is None or torch.equal(p.out_rest[~hit], rest[~hit])
 
 
 @pytest.mark.parametrize("T", [40, 3000])                # whole, and in ranges that are joined
