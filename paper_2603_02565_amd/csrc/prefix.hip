@@ -369,6 +369,8 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   // by chunk parity: the last chunk whose values are not all finite, the last chunk with keys of pages outside the
   // pool, and those keys; rows of the next own chunks
   __shared__ int s_odd[2], s_holes[2], s_hole[2][KC];
+  // FINE: the infinities (1, 2: -infinity) and NaNs (4) of every column of the shared values; whether there are any
+  __shared__ int s_wild[FINE ? DH : 1], s_any_wild;
   __shared__ long long s_at[2][KC];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -391,6 +393,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
   const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
   if (tid < 2) s_odd[tid] = s_holes[tid] = -1;
   if (tid < KC) s_hole[0][tid] = s_hole[1][tid] = -1;
+  if (FINE && tid < DH) s_wild[tid] = s_any_wild = 0;
   // This workgroup's share of the shared chunks and, below, of the own chunks.  The shared ones need no more than ctx_len,
   // so they are under way while the lists' lengths, packing and pages are found.
   const int nctx = ctx_rows(a, b), cctx = (nctx + KC - 1) / KC;
@@ -551,6 +554,12 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
     }
     return p;
   };
+  auto all_finite = [&]() __attribute__((always_inline)) {             // this thread's values
+    unsigned top = 0;
+#pragma unroll
+    for (int p = 0; p < PER_T; ++p) top = peak(top, vreg[p]);
+    return finite<T>(top);
+  };
   auto stage = [&](E* Ks, E* Vs) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PER_T; ++p) {
@@ -596,6 +605,22 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 #pragma unroll
       for (int p = 0; p < PER_T; ++p)
         if (c * KC + key0 + p * STEP >= nctx) kreg[p] = vreg[p] = V8<T>{};
+    }
+    if constexpr (FINE) {
+      // Infinity times a probability's second part, which may be zero or negative, is not the infinity that it has to be.
+      // Every row sees every shared key: such a value makes its column infinite, or NaN, in all of them, at the end.
+      if (!all_finite()) {
+#pragma unroll
+        for (int p = 0; p < PER_T; ++p) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float v = to_f32((T)vreg[p][j]);
+            if (!__builtin_isfinite(v)) atomicOr(&s_wild[d0 + j], v != v ? 4 : v > 0 ? 1 : 2);
+          }
+          vreg[p] = finite_of(vreg[p]);
+        }
+        s_any_wild = 1;
+      }
     }
     stage(Ks, Vs);
     if (c + 1 == cm && ob < oe) first_own();       // uniform; the first own chunk follows
@@ -671,10 +696,7 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         if (PAGED && hole >> p & 1) s_hole[c & 1][key0 + p * STEP] = s_holes[c & 1] = c;
       }
     }
-    unsigned top = 0;
-#pragma unroll
-    for (int p = 0; p < PER_T; ++p) top = peak(top, vreg[p]);
-    if (!finite<T>(top)) s_odd[c & 1] = c;
+    if (!all_finite()) s_odd[c & 1] = c;
     stage(Ks, Vs);
     if (tid < KC) s_at[(c + 1) & 1][tid] = found.row(a);
     lds_barrier();
@@ -720,6 +742,18 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
         if (odd) add_odd(Vs, kb, i, lo[i] - x0, hi[i] - x0, pb, pf);
       }
     }
+  }
+
+  if (FINE && __builtin_amdgcn_readfirstlane(s_any_wild)) {   // uniform
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int w = s_wild[n * 16 + g4 * 4 + q];
+        const float v = w == 0 ? 0.f : w == 1 ? INFINITY : w == 2 ? -INFINITY : NAN;
+#pragma unroll
+        for (int i = 0; i < QT; ++i) o[i][n][q] += v;
+      }
   }
 
 #pragma unroll

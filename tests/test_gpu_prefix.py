@@ -446,6 +446,38 @@ def test_infinities_leave_the_neighbours_bits(kw):
     assert rest is None or torch.equal(p.out_rest[~hit], rest[~hit])
 
 
+@pytest.mark.parametrize("dh,T,train", [(32, 70, False), (32, 70, True), (64, 70, True), (128, 200, True), (32, 400, True)])
+def test_infinite_shared_values(dh, T, train):
+    """bf16: an infinite shared value makes its column infinite in every row of its request, and nothing else."""
+    c = Case(dtype="bf16", B=2, K=4, S=6, H=2, Hkv=2, dh=dh, T=T, L=6, lens="full", seed=15).device()
+    p = fe.PrefixAttention(train=train, **c.dims)
+    want = p.run(*c.keys, **c.more).clone()
+    c.keys[2][1, T - 4, 1, 5] = INF
+    c.keys[2][1, 3, 0, 9] = -INF
+    c.keys[2][1, 35, 0, 31] = NAN
+    got = p.run(*c.keys, **c.more)
+    hit = torch.zeros(want.shape, dtype=torch.bool, device="cuda")
+    hit[1, :, :, 1, 5] = hit[1, :, :, 0, 9] = hit[1, :, :, 0, 31] = True
+    assert (got[1, :, :, 1, 5] == INF).all() and (got[1, :, :, 0, 9] == -INF).all() and torch.isnan(got[1, :, :, 0, 31]).all()
+    assert torch.equal(got[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("dh,T,train", [(32, 70, False), (32, 70, True), (64, 70, True), (128, 200, True), (32, 400, True)])
+def test_infinite_shared_values(dh, T, train):
+    """bf16: an infinite shared value makes its column infinite in every row of its request, and nothing else."""
+    c = Case(dtype="bf16", B=2, K=4, S=6, H=2, Hkv=2, dh=dh, T=T, L=6, lens="full", seed=15).device()
+    p = fe.PrefixAttention(train=train, **c.dims)
+    want = p.run(*c.keys, **c.more).clone()
+    c.keys[2][1, T - 4, 1, 5] = INF
+    c.keys[2][1, 3, 0, 9] = -INF
+    c.keys[2][1, 35, 0, 31] = NAN
+    got = p.run(*c.keys, **c.more)
+    hit = torch.zeros(want.shape, dtype=torch.bool, device="cuda")
+    hit[1, :, :, 1, 5] = hit[1, :, :, 0, 9] = hit[1, :, :, 0, 31] = True
+    assert (got[1, :, :, 1, 5] == INF).all() and (got[1, :, :, 0, 9] == -INF).all() and torch.isnan(got[1, :, :, 0, 31]).all()
+    assert torch.equal(got[~hit], want[~hit])
+
+
 @pytest.mark.parametrize("T", [40, 3000])                # whole, and in ranges that are joined
 def test_a_nan_query_gives_nan(T):
     """A row whose scores are all NaN is not a row without keys; the other rows keep their bits."""
