@@ -27,7 +27,7 @@ FE_DEV f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32
 // last 8, so that x = p[0] + p[1] + p[2] exactly.  Of the nine products of parts the six largest are formed; the others are
 // below 2^-21 of |x||y|, 2^-24.6 in the mean.  Six bf16 products take 3/8 of the time of the eight 16 x 16 x 4 fp32 ones (training
 // step of 256 x 550 rows, heads of 32: 277 us with those, 222 in parts; 64 x 1024 rows, heads of 64: 698, 490).  An
-// infinity is a first part alone.
+// infinity is a first part alone; a NaN is one in its later parts, whatever the first 16 bits alone would be.
 struct Parts { bf16x8 p[3]; };
 FE_DEV f32x4 mma(Parts a, Parts b, f32x4 c) {
   c = mma(a.p[2], b.p[0], c);
@@ -47,7 +47,7 @@ template <bool FINITE> FE_DEV Parts parts8(const f32x8 v) {
       const float x = v[2 * i + j];
       h[j] = __float_as_uint(x);
       float rest = x - __uint_as_float(h[j] & 0xffff0000u);
-      if (!FINITE && (h[j] & 0x7f800000u) == 0x7f800000u) rest = 0.f;
+      if (!FINITE && __builtin_isinf(x)) rest = 0.f;
       m[j] = __float_as_uint(rest);
       l[j] = __float_as_uint(rest - __uint_as_float(m[j] & 0xffff0000u));
     }

@@ -478,6 +478,24 @@ def test_infinite_shared_values(dh, T, train):
     assert torch.equal(got[~hit], want[~hit])
 
 
+@pytest.mark.parametrize("payload", [0x7f800001, -0x7fffff, 0x7fc00000])
+@pytest.mark.parametrize("which", range(5))
+def test_a_nan_of_any_payload_gives_nan(which, payload):
+    """fp32: a NaN whose first sixteen bits are those of an infinity is a NaN in every output that sees it."""
+    c = Case(dtype="f32", B=1, K=3, S=4, H=2, Hkv=2, dh=32, T=40, L=6, lens="full", causal=False, seed=16).device()
+    p = fe.PrefixAttention(train=True, **c.dims)
+    want = p.run(*c.keys, **c.more).clone()
+    at = ((0, 1, 2, 1, 3), (0, 17, 1, 3), (0, 17, 1, 3), (0, 1, 5, 1, 3), (0, 1, 5, 1, 3))[which]
+    c.keys[which].view(torch.int32)[at] = payload
+    assert torch.isnan(c.keys[which][at])
+    got = p.run(*c.keys, **c.more)
+    hit = torch.zeros(want.shape, dtype=torch.bool, device="cuda")
+    hit[((0, 1, 2, 1), (0, slice(None), slice(None), 1), (0, slice(None), slice(None), 1, 3), (0, 1, slice(None), 1),
+         (0, 1, slice(None), 1, 3))[which]] = True
+    assert torch.isnan(got[hit]).all()
+    assert torch.equal(got[~hit], want[~hit])
+
+
 @pytest.mark.parametrize("T", [40, 3000])                # whole, and in ranges that are joined
 def test_a_nan_query_gives_nan(T):
     """A row whose scores are all NaN is not a row without keys; the other rows keep their bits."""
