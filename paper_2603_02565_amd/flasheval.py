@@ -574,7 +574,9 @@ def _row_stride(t, name: str, shape: Tuple[int, ...], dtype) -> int:
 
 class _Layouts:
     """The layout checks of one object's tensors, remembered by shapes, strides and types: a serving loop passes the same
-    layouts again and again."""
+    layouts again and again.  Prompts of ever new lengths do not: the MOST last learnt are kept."""
+
+    MOST = 256
 
     def __init__(self):
         self.known = {}
@@ -584,7 +586,10 @@ class _Layouts:
         key = tuple([None if t is None else (t.shape, t.stride(), t.dtype) for t in tensors])
         got = self.known.get(key)
         if got is None:
-            got = self.known[key] = check(*tensors)
+            got = check(*tensors)
+            if len(self.known) >= self.MOST:
+                del self.known[next(iter(self.known))]
+            self.known[key] = got
         return got
 
 

@@ -172,6 +172,19 @@ def test_binding_checks_layouts():
         fe.PagedCache(pages, pages, table)
 
 
+def test_remembered_layouts_are_few():
+    """Ever new lengths: what is remembered of them stays bounded, and what is asked again is right all the same."""
+    known, asked = fe._Layouts(), []
+    wide = lambda t: asked.append(1) or t.shape[1]                                      # noqa: E731
+    for n in list(range(1, 2001)) + [2000, 1, 1, 2000]:
+        assert known.of(wide, torch.empty(1, n, device="meta")) == n
+    assert len(known.known) <= 256 and len(asked) == 2001
+    bad = lambda t: (_ for _ in ()).throw(ValueError("no"))                             # noqa: E731
+    for _ in range(2):                                                                  # a refusal is not remembered
+        with pytest.raises(ValueError):
+            known.of(bad, torch.empty(5, 5, device="meta"))
+
+
 class _Stream:
     def __init__(self, handle):
         self.cuda_stream = handle
