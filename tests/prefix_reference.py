@@ -4,6 +4,8 @@ derives how far a kernel that rounds as the header says may be off."""
 import numpy as np
 
 HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}     # a rounding is off by at most this, relative
+TWO_PARTS = 2.0 ** -16     # a number as two bf16: the second is off by a half step of what the first left, 2^-8 of it
+REST = 2.0 ** -15          # out with its rest: 16 bits of the significand, the others cut
 
 
 def clamp_lengths(B, K, S, T, L, ctx_len, q_len, own_len):
@@ -11,7 +13,8 @@ def clamp_lengths(B, K, S, T, L, ctx_len, q_len, own_len):
     return full(ctx_len, T, (B,)), full(q_len, S, (B, K)), full(own_len, L, (B, K))
 
 
-def attend(q, ck, cv, ok, ov, *, dtype, causal, scale=None, ctx_len=None, q_len=None, own_len=None, dout=None, seen=None):
+def attend(q, ck, cv, ok, ov, *, dtype, causal, scale=None, ctx_len=None, q_len=None, own_len=None, dout=None, seen=None,
+           up_out=None, up_own=None, u_rest=None):
     """q [B][K][S][H][dh], ck/cv [B][T][Hkv][dh], ok/ov [B][K][L][Hkv][dh] (float64; anything outside the lengths).
     `seen` [B][K][L]: own keys that count at all (pages inside the pool).  Returns {name: (value, bound)} of out and
     lse, and with dout of dq, dck, dcv, dok, dov.
@@ -26,6 +29,8 @@ def attend(q, ck, cv, ok, ov, *, dtype, causal, scale=None, ctx_len=None, q_len=
       dp    is off by dh e sum |dout||v|;
       ds = p (dp - delta) is off by p (err dp + err delta) + (rp + u_p + 2 e) |ds|, and dq, dk sum it times |k|, |q|;
       dv sums (rp + u_p) p |dout|; the sums of N terms add N e times the sum of the terms' sizes.
+    up_out, up_own: another u for the p of out, and for the p and ds of own keys' gradients; u_rest: D = dout.out is taken
+    from an out that is off by this, relative, in place of its rounding (dq, dk and dv of shared keys keep u for p and ds).
     FE_F32's products in three parts are good to 2^-21 = 8 e each and add a part's six sums every 32 terms: both lie inside
     (dh + 2) e for a score and dh e for dp (dh >= 32), and inside rp >= 32 e in the sums over keys and rows."""
     B, K, S, H, dh = q.shape
@@ -33,6 +38,7 @@ def attend(q, ck, cv, ok, ov, *, dtype, causal, scale=None, ctx_len=None, q_len=
     G, scale = H // Hkv, dh ** -0.5 if scale is None else scale
     u, e = HALF_STEP[dtype], 2.0 ** -24
     up = u if dtype == "bf16" else 0.0
+    up_out, up_own = up if up_out is None else up_out, up if up_own is None else up_own
     nc, nq, no = clamp_lengths(B, K, S, T, L, ctx_len, q_len, own_len)
     zero = lambda *shape: (np.zeros(shape), np.zeros(shape))     # noqa: E731
     out, dq = zero(B, K, S, H, dh), zero(B, K, S, H, dh)
@@ -72,22 +78,26 @@ def attend(q, ck, cv, ok, ov, *, dtype, causal, scale=None, ctx_len=None, q_len=
                 smax = np.where(see, np.abs(qq) @ np.abs(kk).T * abs(scale), 0.0).max(1)
                 rp = 2 * e * ((dh + 8) * smax + np.abs(ls) + t + m + 16)
                 oa = p @ np.abs(vv)
-                eo = (rp + up + (t + m) * e)[:, None] * oa
+                eo = (rp + up_out + (t + m) * e)[:, None] * oa
                 out[1][b, k, :n, h] = eo + u * (np.abs(o) + eo)
                 lse[1][b, k, :n, h] = rp + 4 * e * (np.abs(ls) + 1)
                 if dout is None:
                     continue
                 do = dout[b, k, :n, h]
                 delta = (do * o).sum(1)
-                ed = (np.abs(do) * out[1][b, k, :n, h]).sum(1) + dh * e * (np.abs(do) * np.abs(o)).sum(1)
+                ed = out[1][b, k, :n, h] if u_rest is None else eo + u_rest * (np.abs(o) + eo)
+                ed = (np.abs(do) * ed).sum(1) + dh * e * (np.abs(do) * np.abs(o)).sum(1)
                 dp = do @ vv.T
                 dpa = np.abs(do) @ np.abs(vv).T
                 ds = p * (dp - delta[:, None])
-                es = p * (dh * e * dpa + ed[:, None] + 2 * e * (dpa + np.abs(delta)[:, None])) + (rp + up + 4 * e)[:, None] * np.abs(ds)
-                ep = (rp + up)[:, None] * p
+                ups = np.where(np.arange(t + m) < t, up, up_own)
+                es = p * (dh * e * dpa + ed[:, None] + 2 * e * (dpa + np.abs(delta)[:, None]))
+                eq = es + (rp + up + 4 * e)[:, None] * np.abs(ds)
+                es = es + (rp[:, None] + ups + 4 * e) * np.abs(ds)
+                ep = (rp[:, None] + ups) * p
                 nk, nr = t + m, K * S * G
                 d = ds @ kk * scale
-                err = scale * (es @ np.abs(kk) + nk * e * (np.abs(ds) + es) @ np.abs(kk))
+                err = scale * (eq @ np.abs(kk) + nk * e * (np.abs(ds) + eq) @ np.abs(kk))
                 dq[0][b, k, :n, h] = d
                 dq[1][b, k, :n, h] = abs(err) + u * (np.abs(d) + abs(err))
                 dk, dv = ds.T @ qq * scale, p.T @ do

@@ -556,6 +556,75 @@ def test_grad_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(want, grads))
 
 
+def _forward_cases():
+    return [dict(seed=i, **kw) for i, kw in enumerate(FORWARD)] + BY_LENGTH
+
+
+@pytest.mark.parametrize("i", range(len(FORWARD) + len(BY_LENGTH)))
+def test_forward_repeats_itself(i):
+    """The same bits from a second call, whatever the outputs and the workspace held before it."""
+    kw = _forward_cases()[i]
+    _say("repeats", i, kw)
+    c = Case(**kw).device()
+    p = fe.PrefixAttention(train=not c.P, **c.dims)
+    first = p.run(*c.keys, **c.more).clone()
+    lse = None if c.P else p.lse.clone()
+    p.ws.fill_(255)                                     # as floats: NaN
+    p.out.fill_(NAN)
+    if lse is not None:
+        p.lse.fill_(NAN)
+    p.run(*c.keys, **c.more)
+    assert torch.equal(p.out, first)
+    assert lse is None or torch.equal(p.lse, lse)
+
+
+def test_two_calls_at_once_write_their_outputs():
+    """Two objects on two streams, many calls in flight, over outputs that hold something else before."""
+    cases = [Case(dtype="bf16", B=1, K=4, S=1, H=4, Hkv=2, dh=64, T=3000, L=48, P=16, seed=s).device() for s in (41, 42)]
+    plans = [fe.PrefixAttention(**c.dims) for c in cases]
+    want = [p.run(*c.keys, **c.more).clone() for p, c in zip(plans, cases)]
+    streams = [torch.cuda.Stream() for _ in plans]
+    for p in plans:
+        p.out.fill_(NAN)
+        p.ws.fill_(255)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for p, c, s in zip(plans, cases, streams):
+            p.run(*c.keys, stream=s, **c.more)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p.out, w) for p, w in zip(plans, want))
+
+
+# Where the header says 16 bits: up to 256 keys, and the own keys' gradients over more
+PRECISE = [
+    dict(dtype="bf16", B=2, K=3, S=11, H=4, Hkv=2, dh=64, T=60, L=20, amp=0.5),
+    dict(dtype="bf16", B=1, K=7, S=5, H=4, Hkv=4, dh=32, T=200, L=56, causal=False),
+    dict(dtype="bf16", B=1, K=2, S=40, H=2, Hkv=1, dh=128, T=9, L=40, lens="own"),
+    dict(dtype="bf16", B=1, K=3, S=30, H=2, Hkv=2, dh=64, T=400, L=30, lens="own"),
+    dict(dtype="bf16", B=1, K=64, S=1, H=1, Hkv=1, dh=32, T=0, L=3, causal=False, lens="full"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(PRECISE)))
+def test_second_products(i):
+    """bf16 with out_rest: over at most 256 keys the probabilities of out have 16 bits, D is that of out with its rest, and
+    own keys' gradients take p and ds at 16 bits.  The plain roundings lie outside these bounds
+    (tests/test_prefix_host.py: test_precise_bounds_tell_the_roundings_apart)."""
+    kw = PRECISE[i]
+    _say("precise", i, kw)
+    c = Case(seed=200 + i, **kw).device()
+    p = fe.PrefixAttention(train=True, **c.dims)
+    out = p.run(*c.keys, **c.more)
+    dout = torch.tensor(c.do).bfloat16().cuda()
+    grads = p.grad(dout, *c.keys, **c.more)
+    want = ref.attend(c.q, c.ck, c.cv, c.ok, c.ov, dtype="bf16", causal=c.dims["causal"], ctx_len=c.nc, q_len=c.nq,
+                      own_len=c.no, dout=c.do, up_out=ref.TWO_PARTS if c.dims["T"] + c.L <= 256 else None,
+                      up_own=ref.TWO_PARTS, u_rest=ref.REST)
+    _near(out, want["out"], "out")
+    for name, g in zip(NAMES, grads):
+        _near(g, want[name], name)
+
+
 # -- the cache -----------------------------------------------------------------------------------
 
 APPEND = [

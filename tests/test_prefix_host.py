@@ -340,3 +340,46 @@ def test_reference_turn_keeps_differences_of_positions():
         dots = [float((ref.turned(a, np.array(p + 5.0), f, near) * ref.turned(b, np.array(p * 1.0), f, near)).sum()) for p in (0, 7, 1000)]
         assert max(dots) - min(dots) < 1e-10
         assert abs(np.linalg.norm(ref.turned(a, np.array(3.0), f, near)) - np.linalg.norm(a)) < 1e-12
+
+
+def _bf16(v):
+    return torch.tensor(v).bfloat16().double().numpy()
+
+
+def _two(v):
+    return _bf16(v) + _bf16(v - _bf16(v))
+
+
+def _cut(v):
+    """The first 16 bits of the significand."""
+    step = 2.0 ** (np.floor(np.log2(np.abs(v))) - 15)
+    return np.trunc(v / step) * step
+
+
+@pytest.mark.parametrize("K,S,L,dh", [(1, 40, 120, 64), (64, 1, 3, 32)])     # long sums; few terms, where D matters
+def test_precise_bounds_tell_the_roundings_apart(K, S, L, dh):
+    """The kernel's sums in float64, with p and ds rounded to one bf16 or as two, D from the rounded out or from out with its
+    rest: the bounds at 16 bits hold what has 16 bits, and not the others."""
+    r = np.random.default_rng(12)
+    q, k, v, do = (_bf16(r.standard_normal((1, K, n, 1, dh))) for n in (S, L, L, S))
+    none = np.zeros((1, 0, 1, dh))
+    fine = ref.attend(q, none, none, k, v, dtype="bf16", causal=False, dout=do, up_out=ref.TWO_PARTS, up_own=ref.TWO_PARTS,
+                      u_rest=ref.REST)
+
+    def inside(name, got):
+        val, bound = (x[0, :, :, 0] for x in fine[name])
+        return bool((np.abs(_bf16(got) - val) <= bound).all())
+
+    Q, K_, V, D = (x[0, :, :, 0] for x in (q, k, v, do))
+    T = lambda x: x.transpose(0, 2, 1)                                                  # noqa: E731
+    s = Q @ T(K_) * dh ** -0.5
+    e = np.exp(s - s.max(-1, keepdims=True))
+    l = e.sum(-1, keepdims=True)
+    out = _two(e) @ V / l
+    assert inside("out", out) and not inside("out", _bf16(e) @ V / l)
+    p, dp = e / l, D @ T(V)
+    dk = lambda f, o: T(f(p * (dp - (D * o).sum(-1, keepdims=True)))) @ Q * dh ** -0.5  # noqa: E731
+    assert inside("dok", dk(_two, _cut(out))) and inside("dov", T(_two(p)) @ D)
+    assert not inside("dok", dk(_bf16, _cut(out))) and not inside("dov", T(_bf16(p)) @ D)
+    if L < 8:
+        assert not inside("dok", dk(_two, _bf16(out)))
