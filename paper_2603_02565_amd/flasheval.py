@@ -149,7 +149,15 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _current_stream(torch.cuda.current_device())
+
+
+def _current_stream(index: int) -> int:
+    """Handle of device `index`'s current stream; without torch's own short way to it, where a build of torch has none, by a stream
+    object (about a microsecond more)."""
+    import torch
+    short = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return short(index) if short else torch.cuda.current_stream(index).cuda_stream
 
 
 # ---------------------------------------------------------------------------------------------
@@ -606,10 +614,7 @@ def _on_device(tensors) -> int:
 
 
 def _stream_on(index: int, stream) -> int:
-    if stream is not None:
-        return _stream(stream)
-    import torch
-    return torch._C._cuda_getCurrentRawStream(index)
+    return _current_stream(index) if stream is None else _stream(stream)
 
 
 def _allocated_for(stream, *tensors, home=None) -> None:

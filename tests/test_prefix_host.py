@@ -190,6 +190,15 @@ class _Stream:
         self.cuda_stream = handle
 
 
+def test_current_stream_without_the_short_way(monkeypatch):
+    """A torch without the private function that names a device's current stream serves every call all the same."""
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream(70 + a[0]))
+    assert fe._stream(None) == 73 and fe._stream_on(2, None) == 72
+    assert fe._stream(5) == fe._stream_on(2, 5) == fe._stream_on(2, _Stream(5)) == 5
+
+
 def _without_a_gpu(monkeypatch):
     """The binding on CPU tensors, current stream 7, no library call; returns the list of (stream, tensors) handed over."""
     handed = []
