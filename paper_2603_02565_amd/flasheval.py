@@ -741,7 +741,9 @@ class PrefixAttention:
     fe_encode_context's cache, viewed with its heads, is one), and own_k and own_v [B][K][L][n_kv_heads][dh], or
     with page_rows > 0 the pages of a PagedCache [n_pages][page_rows][n_kv_heads][dh] and `table`
     [B][K][L / page_rows] int32.  ctx_len [B], q_len [B][K] and own_len [B][K] int32 give the rows in use.  The outputs
-    belong to this object and are overwritten by its next call, as is its workspace: one object per stream."""
+    belong to this object and are overwritten by its next call, as is its workspace: one object per stream.  The calls work outside
+    torch's autograd, whatever their tensors require: `run` returns no history, and what `grad` returns is handed on with
+    torch.autograd.backward((q, ctx_k, ctx_v, own_k, own_v), grads)."""
 
     def __init__(self, B: int, K: int, S: int, T: int, L: int, n_heads: int, n_kv_heads: int, dh: int, dtype: str,
                  causal: bool = False, scale: Optional[float] = None, page_rows: int = 0, n_pages: int = 0,

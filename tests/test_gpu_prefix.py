@@ -365,6 +365,22 @@ def test_grad_matches_differences():
         assert abs(diff - want) <= 2e-3 * max(1.0, abs(want)), (NAMES[i], diff, want)
 
 
+def test_gradients_handed_to_autograd():
+    """Queries, keys and values that a model computed: run() returns no history, and the gradients go on into the model."""
+    c = Case(dtype="f32", B=2, K=3, S=4, H=4, Hkv=2, dh=32, T=21, L=4, lens="full", seed=8).device()
+    weights = [torch.full((32,), 0.5 + i, device="cuda", requires_grad=True) for i in range(5)]
+    made = [x * w for x, w in zip(c.keys, weights)]
+    p = fe.PrefixAttention(train=True, **c.dims)
+    dout = torch.tensor(c.do).float().cuda()
+    assert not p.run(*made, **c.more).requires_grad
+    grads = p.grad(dout, *made, **c.more)
+    torch.autograd.backward(made, grads)
+    for w, x, g in zip(weights, c.keys, grads):
+        want, size = ((x * g).double().flatten(0, -2).sum(0), (x * g).double().abs().flatten(0, -2).sum(0))
+        n = x.numel() // 32                              # fp32 sums of n products, in an order of torch's
+        assert ((w.grad.double() - want).abs() <= (n + 1) * 2.0 ** -24 * size).all()
+
+
 def test_strided_inputs():
     """Queries as a column block of a fused projection, the shared rows as one layer of a context cache."""
     c = Case(dtype="bf16", B=2, K=3, S=4, H=4, Hkv=2, dh=32, T=50, L=10, seed=7).device()
