@@ -169,7 +169,7 @@ FE_DEV void store_out<bf16>(const PrefixArgs& a, long long at, int col, f32x4 v)
   *reinterpret_cast<unsigned*>(a.out_rest + at * a.Hq * a.dh + col) =
       __builtin_amdgcn_perm(d[1], d[0], 0x0c0c0501) | __builtin_amdgcn_perm(d[3], d[2], 0x05010c0c);
 }
-// ... and back: out with its rest, to 2^-16.
+// ... and back: out with its rest, 16 bits of the significand, the others cut.
 FE_DEV float with_rest(bf16 v, int step) { return __uint_as_float(__float_as_uint((float)v) + step * 256); }
 FE_DEV float with_rest(float v, int) { return v; }
 template <>
@@ -346,12 +346,13 @@ constexpr int dkv_waves(int dh) { return dh == 32 ? 3 : 2; }
 // flight behind this one's products) into LDS.  Scores are formed transposed (keys x rows): a lane then holds
 // eight keys of one row, which is the operand layout of the product with the values, so probabilities never leave the
 // registers.
-// Bound: with many rows a key the vector unit (a product-sum, an exponential, a sum, half a maximum and half a rounding a
-// score beside its 4 dh matrix operations; 64 x 1024 rows of 1088 keys, heads of 64: 36.6 us, 480 TFLOP/s, vector unit 60%
-// of the time, LDS 44%, matrix cores 22%; 256 x 550 rows of 267 keys, heads of 32: 26.6 us, 180 TFLOP/s); with few rows
-// HBM (4 x 32 lists of 4 rows a key head, heads of 128, 539 MB: 129 us, 4.2 TB/s); fp32 the vector
-// unit, which also splits the operands (75% of the time; 256 x 550 rows, heads of 32: 60 us, 80 TFLOP/s); a short context its few dependent trips to memory (20 rows of 181 + 12
-// keys: 7.3 us).
+// Bound: with many rows a key the vector unit: a product-sum, an exponential, a sum, half a maximum and half a rounding a
+// score beside its 4 dh matrix operations, and the staging, the masks and the prologue (64 x 1024 rows of 1088 keys, heads
+// of 64: 33.5 us, 529 TFLOP/s, 8.8 vector instructions a score; vector unit 57% of the time, LDS 49%, matrix cores 24%, one
+// after another within a step; 256 x 550 rows of 267 keys, heads of 32: 24.2 us, 199 TFLOP/s, 13.8 a score, vector unit 66%);
+// with few rows HBM (4 x 32 lists of 4 rows a key head, heads of 128, 539 MB: 129 us, 4.2 TB/s); fp32 the vector unit, which
+// also splits the operands (72% of the time; 256 x 550 rows, heads of 32: 62 us, 77 TFLOP/s); a short context its few
+// dependent trips to memory (20 rows of 181 + 12 keys: 7.1 us).
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int QT, int NW, int KC, bool PAGED, bool FINE>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_fwd(PrefixArgs a) {
@@ -537,7 +538,8 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
       for (int n = 0; n < NB; ++n) o[i][n] *= alpha;
     }
   };
-  // Probabilities against the reference, added to the sum, as the operand of the product with the values.  FINE: what its
+  // Probabilities against the reference, added to the sum, as the operand of the product with the values.  bf16 rounds them,
+  // for one product in place of two (out off by 2.0e-3 to 2.2e-3 of its norm, its own rounding 1.66e-3).  FINE: what that
   // rounding cut is a second one.  A training step over few keys needs it, as its gradient takes D = dout . out from out and
   // ds = p (dp - D) may be small beside D: keys 1 + 2, dq off by 3.1e-3 of its norm without, 2.3e-3 with; 4 + 11 2.6e-3,
   // 2.3e-3; 130 + 44 2.40e-3, 2.36e-3; 1024 + 64 the same, at 142 us a step for 155.
@@ -845,10 +847,11 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixArgs a) {
 // products need of every row and leaves it for dk and dv, in the order of the rows of a (request, key head):
 //   x = log2(e) lse (+infinity for a row without keys or past q_len: its probabilities are then 0),
 //   y = dout . out,   z, w = the own rows that it sees, numbered k L + j  [z, w).
-// ds goes into the product with the keys as it lies in the registers, as the probabilities do in the forward.
-// Bound: LDS (55% of the time: every wave reads keys twice and values once for its 16 rows) and the vector unit (48%)
-// beside 27% of matrix cores (64 x 1024 rows of 1088 keys, heads of 64: 46 us, 576 TFLOP/s); fp32 the vector unit (63%;
-// 256 x 550 rows, heads of 32: 71 us, 101 TFLOP/s).
+// ds goes into the product with the keys as it lies in the registers, as the probabilities do in the forward: bf16 rounds it
+// there, for one product in place of two (dq off by 2.4e-3 of its norm, of which its own rounding makes 1.66e-3).
+// Bound: LDS (58% of the time: every wave reads keys twice and values once for its 16 rows) and the vector unit (50%)
+// beside 29% of matrix cores (64 x 1024 rows of 1088 keys, heads of 64: 47 us, 564 TFLOP/s); fp32 the vector unit (63%;
+// 256 x 550 rows, heads of 32: 72 us, 100 TFLOP/s; at heads of 64 8 registers, 36 bytes a lane, are spilled).
 template <typename T, int DH, int QT, int NW, int KC>
 __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix_dq(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -1108,9 +1111,11 @@ __global__ __launch_bounds__(NW * 64, waves_of(sizeof(T), DH, QT)) void k_prefix
 // k L + j -- the keys that a row sees are again one interval.  Few tiles: several workgroups share a tile's rows.
 // Scores are formed a second time: sums of dq by key tiles would be B K S n_heads dh floats for every tile of 128 keys,
 // more traffic than the two products cost.
-// Bound: vector unit (43% of the time), LDS and matrix cores (30% each) with two waves a SIMD (64 x 1024 rows of 1088
-// keys, heads of 64: 57 us, 625 TFLOP/s); fp32 the vector unit (66%; 256 x 550 rows, heads of 32: 93 us, 103
+// Bound: vector unit (44% of the time), LDS and matrix cores (30% each) with two waves a SIMD (64 x 1024 rows of 1088
+// keys, heads of 64: 59 us, 602 TFLOP/s); fp32 the vector unit (66%; 256 x 550 rows, heads of 32: 94 us, 102
 // TFLOP/s).  fp32 heads of 128 take a whole compute unit's LDS and one wave a SIMD, whose registers hold everything.
+// The own tiles' second products spill in bf16, 14 registers at heads of 32 (60 bytes a lane) and 8 at heads of 128 (36 bytes;
+// 4 x 1332 rows, 333 + 37 keys: 17.5 us without these products, 20.5 with them).
 template <typename T, int DH, int KT, int NW, int RC>
 __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGradArgs p) {
   const PrefixArgs& a = p.f;
@@ -1279,6 +1284,7 @@ __global__ __launch_bounds__(NW * 64, dkv_waves(DH)) void k_prefix_dkv(PrefixGra
       pb[i] = F::of(pe[i]);
       ds[i] = F::of(de[i]);
     }
+    // bf16 rounds p and ds of shared keys for the products, whose sums have many rows' terms (dk off by 2.35e-3 of its norm).
     // An own key meets few rows, and one may make most of its sums: bf16 adds what the roundings cut (dk off by 2.4e-3
     // to 3.3e-3 of its norm without, 1.7e-3 with, which is its own rounding; training step of 256 x 550 rows, heads of 32,
     // 87 us without, 93 with, of 64 x 1024 rows, heads of 64, the same).
@@ -1427,9 +1433,14 @@ template <typename T, int DH> constexpr int kKC = sizeof(T) * DH > 256 ? 32 : 64
 template <typename T, int DH, int QT>
 hipError_t launch_fwd_qt(const PrefixArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.splits));
+  // FINE, for a training step over few keys: out is off by its own rounding alone, 1.66e-3 of its norm, at 2 to 20% of the step.
+  // Without it, over 16, 64 and 256 keys, out is off by 2.0e-3, 2.1e-3, 2.2e-3, and dq by 2.47e-3, 2.40e-3, 2.43e-3 for 2.36e-3,
+  // 2.37e-3, 2.42e-3 (heads of 32): the gradients' gain ends there.  A step of 256 x 550 rows takes 73, 73, 96 us without
+  // and 79, 81, 109 with it (heads of 32), 106, 107, 137 and 111, 117, 154 (of 64).  The lengths are on the device, so
+  // the capacities decide.
   if (a.page_rows > 0)
     hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, true, false>), grid, dim3(256), 0, s, a);
-  else if (sizeof(T) == 2 && a.out_rest && a.T + a.L <= 256)             // few keys: see the probabilities there
+  else if (sizeof(T) == 2 && a.out_rest && a.T + a.L <= 256)
     hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, false, sizeof(T) == 2>), grid, dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((k_prefix_fwd<T, DH, QT, 4, kKC<T, DH>, false, false>), grid, dim3(256), 0, s, a);
@@ -1478,8 +1489,8 @@ hipError_t grad(PrefixGradArgs p, const PrefixGradPlan& pl, hipStream_t s) {
 // Ranges that `items` chunks of 64 are split into, for each of `wgs` tiles: up to two workgroups per compute unit, at
 // least three chunks a range (a range costs its partial sums, and all of them a launch).  64 tiles of 24 chunks: one range
 // 28.6 us, four 23.0, eight 19.5, sixteen 20.5; 8 tiles of 4 chunks: 7.4 us whole, 8.9 in two.  In fp32 also as many as
-// keep a range at 2048 keys or rows: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8) of its
-// result, 1.1e-6 at 6400.
+// keep a range at 2048 keys or rows, up to 256 of them: one chain of fp32 sums over n of them is off by about 2^-25 sqrt(n / 8)
+// of its result, 1.1e-6 at 6400 and, by this, 1.3e-6 at 4194304 keys in 256 ranges.
 // narrow (forward, bf16 heads of at most 64, three of whose workgroups a compute unit holds): up to three as long as a
 // range keeps eight chunks (heads of 64, 128 tiles of 512 + 16 chunks: 237 us -> 181, of 32 + 16: 33 -> 30; heads of 32,
 // 32 tiles of 32 + 32 chunks: two 16.1, three 18.0).
