@@ -1,0 +1,53 @@
+// Launch descriptors of the 4-bit cache's kernels (flasheval_packed.h), and how a cached row is found.
+#pragma once
+
+#include "fe_common.h"
+#include "flasheval_packed.h"
+
+constexpr int kPackedMaxRows = 1 << 22;  // a sequence's capacity
+
+// A cache as the kernels see it.  Row j's page is the quotient j / page_rows, by a multiplication: j magic >> shift, exact for
+// j < 2^31.
+struct PackedCache {
+  char* pages;
+  long long page_ld;
+  const int32_t *table, *len;
+  int cols, page_rows, n_pages, cap, head_bytes;
+  unsigned magic;
+  int shift;
+};
+PackedCache packed_cache(const fe_packed_cache& c, int dh);
+
+FE_DEV int packed_page(const PackedCache& c, int j) {
+  return (int)((unsigned long long)(unsigned)j * c.magic >> c.shift);
+}
+FE_DEV int packed_len(const PackedCache& c, int s) { return min(max(c.len[s], 0), c.cap); }
+
+// The attention's and the weights' arguments.  The query rows of a (request, key head) are numbered r = (k S + s) G + hg < R
+// with G = Hq / Hkv: rows that share keys are adjacent.
+struct PackedArgs {
+  PackedCache ctx, own;                  // cap = 0: none
+  const void* q;
+  const int32_t* q_len;
+  void* out;
+  float* lse;
+  int B, K, S, Hq, Hkv, G, R, causal, q_ld, out_ld;
+  float scale;
+  int tiles, splits;                     // row tiles per (request, key head); key ranges per tile
+  float *part_o, *part_ml;               // splits > 1: [splits][B K S Hq][dh] sums, [..][2] maximum and sum
+  const float *ctx_w, *own_w;            // weights
+  float *ctx_w_out, *own_w_out;
+  int ctx_tiles, own_tiles, ctx_splits, own_splits;   // key tiles per sequence, row ranges per key tile
+  float *part_ctx, *part_own;            // [splits][N][Hkv][cap]
+};
+
+struct PackedPlan { int waves, tiles, splits; size_t part_bytes; };   // waves: those that a chunk of keys is shared by
+PackedPlan packed_plan(const fe_packed_args& a);
+struct PackedWeighPlan { int ctx_tiles, own_tiles, ctx_splits, own_splits; size_t ctx_bytes, own_bytes; long long blocks, sum_blocks; };
+PackedWeighPlan packed_weigh_plan(const fe_packed_args& a);
+
+hipError_t launch_packed_attention(const PackedArgs& a, int dh, bool bf16_rows, const PackedPlan& p, hipStream_t s);
+hipError_t launch_packed_weights(const PackedArgs& a, int dh, bool bf16_rows, hipStream_t s);
+hipError_t launch_packed_append(const fe_packed_append_args& a, hipStream_t s);
+hipError_t launch_packed_read(const fe_packed_read_args& a, hipStream_t s);
+hipError_t launch_packed_evict(const fe_packed_evict_args& a, hipStream_t s);

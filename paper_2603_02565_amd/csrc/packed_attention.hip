@@ -1,0 +1,776 @@
+// Attention of a request's lists over rows held in 4 bits (fe_packed_attention), and the weight that every cached row
+// received (fe_packed_weights).
+#include <algorithm>
+
+#include "packed.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+FE_DEV f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// The side of a product that is not held in 4 bits: eight bf16 values, or eight floats in three bf16 parts whose sum they are
+// (each truncation takes the next 8 bits of the significand; an infinity is a first part alone).
+struct Parts { bf16x8 p[3]; };
+FE_DEV Parts parts8(f32x8 v) {
+  u32x4 w[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned h[2], m[2], l[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x = v[2 * i + j];
+      h[j] = __float_as_uint(x);
+      float rest = x - __uint_as_float(h[j] & 0xffff0000u);
+      if (__builtin_isinf(x)) rest = 0.f;
+      m[j] = __float_as_uint(rest);
+      l[j] = __float_as_uint(rest - __uint_as_float(m[j] & 0xffff0000u));
+    }
+    w[0][i] = __builtin_amdgcn_perm(h[1], h[0], 0x07060302);
+    w[1][i] = __builtin_amdgcn_perm(m[1], m[0], 0x07060302);
+    w[2][i] = __builtin_amdgcn_perm(l[1], l[0], 0x07060302);
+  }
+  return Parts{{__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1]), __builtin_bit_cast(bf16x8, w[2])}};
+}
+template <typename T> struct Form;
+template <> struct Form<bf16> {
+  typedef bf16x8 Op;
+  typedef bf16x8 V;
+  static FE_DEV Op of(V v) { return v; }
+  static FE_DEV Op rounded(f32x8 v) { return __builtin_convertvector(v, bf16x8); }
+};
+template <> struct Form<float> {
+  typedef Parts Op;
+  typedef f32x8 V;
+  static FE_DEV Op of(V v) { return parts8(v); }
+  static FE_DEV Op rounded(f32x8 v) { return parts8(v); }
+};
+// held x other, the held values exact in bf16: one product, or one a part, the smallest first.
+FE_DEV f32x16 mma_held(bf16x8 held, bf16x8 x, f32x16 c) { return mma(held, x, c); }
+FE_DEV f32x16 mma_held(bf16x8 held, const Parts& x, f32x16 c) {
+  return mma(held, x.p[0], mma(held, x.p[1], mma(held, x.p[2], c)));
+}
+FE_DEV f32x16 mma_held_right(bf16x8 x, bf16x8 held, f32x16 c) { return mma(x, held, c); }
+FE_DEV f32x16 mma_held_right(const Parts& x, bf16x8 held, f32x16 c) {
+  return mma(x.p[0], held, mma(x.p[1], held, mma(x.p[2], held, c)));
+}
+
+template <typename V, typename T> FE_DEV V ldv(const T* p) { return *reinterpret_cast<const V*>(p); }
+
+// Eight columns from four bytes of codes and the block's power of two.
+FE_DEV bf16x8 values8(unsigned w, float unit) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+FE_DEV float unit_of(unsigned scale) { return __uint_as_float(scale << 23); }   // 255: NaN from the conversion
+
+FE_DEV int q_rows(const PackedArgs& a, int bk) { return a.q_len ? min(max(a.q_len[bk], 0), a.S) : a.S; }
+FE_DEV int own_rows(const PackedArgs& a, int bk) { return a.own.cap ? packed_len(a.own, bk) : 0; }
+FE_DEV int ctx_rows(const PackedArgs& a, int b) { return a.ctx.cap ? packed_len(a.ctx, b) : 0; }
+
+// log2(e) |scale|; positive, so that masked scores stay -infinity when scale is 0.
+FE_DEV float score_unit(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-37f); }
+
+// The two halves of a wave hold the same rows.
+FE_DEV float halves_max(float v) {
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+FE_DEV float halves_sum(float v) {
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Query row r of (request b, key head g).
+struct Row {
+  int k, s, h;                           // list, row, query head
+  bool live;                             // r < R and s < q_len
+  long long at;                          // (b K + k) S + s
+  int own;                               // own keys it sees: j < own
+};
+FE_DEV Row row_of(const PackedArgs& a, int b, int g, int r) {
+  Row w;
+  const int rr = min(r, a.R - 1), sg = a.S * a.G;
+  w.k = rr / sg;
+  const int rem = rr - w.k * sg;
+  w.s = rem / a.G;
+  w.h = g * a.G + rem - w.s * a.G;
+  const int bk = b * a.K + w.k, n = q_rows(a, bk), m = own_rows(a, bk);
+  w.live = r < a.R && w.s < n;
+  w.at = (long long)bk * a.S + w.s;
+  w.own = !w.live ? 0 : a.causal ? min(max(m - n + w.s + 1, 0), m) : m;
+  return w;
+}
+
+// The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
+// their number; a list without query rows contributes none.  nb <= 128; 256 threads; ends with a barrier.
+FE_DEV void pack_own(const PackedArgs& a, int b, int k0, int nb, int* off) {
+  __shared__ int s_half;
+  const int tid = threadIdx.x, lane = tid & 63;
+  int v = 0;
+  if (tid < nb) {
+    const int bk = b * a.K + k0 + tid;
+    v = q_rows(a, bk) > 0 ? own_rows(a, bk) : 0;
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int u = __shfl_up(v, m);
+    if (lane >= m) v += u;
+  }
+  if (tid == 63) s_half = v;
+  __syncthreads();
+  if (tid >= 64 && tid < 128) v += s_half;
+  if (tid < nb) off[tid + 1] = v;
+  if (tid == 0) off[0] = 0;
+  __syncthreads();
+}
+
+// A tile of keys or values in LDS as bf16, rows of DH without padding, their units of 8 columns exchanged inside a row so that
+// 16 rows at one unit and 4 rows at 4 neighbouring units both fall on all 64 banks.
+template <int DH> struct Tile {
+  static FE_DEV int swap(int row) {
+    if (DH == 128) return (row & 3) << 2 | (row >> 2 & 3);
+    if (DH == 64) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    return row >> 2 & 3;
+  }
+  static FE_DEV int at(int row, int unit) { return row * DH + ((unit ^ swap(row)) << 3); }
+  // Operand along rows: lane l is row base + l % 32, its elements columns 16 c + 8 (l / 32) + j (base a multiple of 32).
+  static FE_DEV int row_lane(int lane) { return at(lane & 31, lane >> 5); }
+  static FE_DEV bf16x8 rows(const bf16* X, int base, int c, int row_lane) {
+    return ldv<bf16x8>(X + base * DH + (row_lane ^ (c << 4)));
+  }
+  // Operand along columns: lane l is column 32 n + l % 32, its elements 4 x + j are rows base + 8 x + 4 (l / 32) + j: the
+  // order in which a lane holds the scores of a 32-row product.  Every 16 lanes read a 4 x 16 block transposed.
+  static FE_DEV int col_lane(int lane) {
+    const int row = 4 * (lane >> 5) + (lane >> 2 & 3);
+    return at(row, 2 * (lane >> 4 & 1) + (lane >> 1 & 1)) + (lane & 1) * 4;
+  }
+  static FE_DEV bf16x8 cols(const bf16* X, int base, int n, int col_lane) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    bf16* p = const_cast<bf16*>(X) + base * DH + (col_lane ^ (n << 5) ^ step(base));
+    bf16* q = const_cast<bf16*>(X) + (base + 8) * DH + (col_lane ^ (n << 5) ^ step(base + 8));
+    const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)q);
+    return __builtin_shufflevector(__builtin_bit_cast(bf16x4, u), __builtin_bit_cast(bf16x4, v), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  // What a base that is a multiple of 8 changes in the exchange.
+  static FE_DEV constexpr int step(int base) { return (base >> 2 & 3) << 3; }
+};
+
+FE_DEV int fresh(int x) {                // keeps a lane's number in one register, not one for every xor of it
+  asm volatile("" : "+v"(x));
+  return x;
+}
+FE_DEV void order() { asm volatile("" ::: "memory"); }   // LDS operations of one wave stay in order
+
+// ------------------------------------------------------------------------------------------
+// Forward.  The rows of a (request, key head) are one matrix of R rows; four waves are WK groups of WR waves with 32
+// rows each.  A group takes every WK-th chunk of KC keys (first the shared rows, then the own rows of the lists that the
+// tile touches, packed without gaps); a thread loads PER units of UE codes of the keys and of the values, the next
+// chunk's in flight behind this one's products, turns them into bf16, which holds them exactly, and puts them into LDS.
+// Scores are formed transposed (keys x rows), so that a lane holds 16 keys of one row in the operand layout of the
+// product with the values.  With WK > 1 the groups' sums are joined in LDS at the end.
+// ------------------------------------------------------------------------------------------
+template <typename T, int DH, int WR, int UE> struct Shape {
+  static constexpr int WK = 4 / WR, GT = 64 * WR, ROWS = 32 * WR, UPR = DH / UE;
+  static constexpr int PER = 32 * UPR > GT ? 32 * UPR / GT : 1, KC = GT * PER / UPR;
+  static constexpr int NBUF = WR > 1 ? 2 : 1, ND = DH / 16, NB = DH / 32;
+};
+constexpr int fwd_waves(int bytes, int dh, int wr) {
+  return dh == 128 ? (bytes == 4 ? 1 : 2) : dh == 64 ? (bytes == 4 ? 2 : 3) : bytes == 4 ? 3 : 4;
+}
+
+template <typename T, int DH, int WR, int UE>
+__global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fwd(PackedArgs a) {
+  typedef Shape<T, DH, WR, UE> C;
+  typedef Form<T> F;
+  typedef typename F::Op Op;
+  typedef Tile<DH> L;
+  constexpr int WK = C::WK, GT = C::GT, ROWS = C::ROWS, UPR = C::UPR, PER = C::PER, KC = C::KC, NBUF = C::NBUF;
+  constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH;
+  static_assert(KC % 32 == 0 && 4 * 32 * DH * 4 - WR * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2, "the join fits the tiles");
+  __shared__ __attribute__((aligned(16))) bf16 s_kv[WK][NBUF][2][TILE];
+  __shared__ int s_off[ROWS + 1], s_hi;
+  // of a chunk (by its parity in the group): the last one with rows of no page, those rows; the last one with own values
+  // of NaN, those units
+  __shared__ int s_holes[WK][2], s_hole[WK][2][KC], s_odds[WK][2], s_odd[WK][2][KC * UPR];
+  __shared__ float s_ml[4][32][2];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave / WR, wr = wave % WR, gt = tid % GT, half = lane >> 5, c32 = lane & 31;
+  int id = xcd_tile(blockIdx.x, gridDim.x);
+  const int t = id % a.tiles;
+  id /= a.tiles;
+  const int z = id % a.splits;
+  id /= a.splits;
+  const int g = id % a.Hkv, b = id / a.Hkv;
+  const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R), sg = a.S * a.G;
+  const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
+  for (int i = tid; i < WK * 2 * KC; i += 256) (&s_hole[0][0][0])[i] = -1;
+  for (int i = tid; i < WK * 2 * KC * UPR; i += 256) (&s_odd[0][0][0])[i] = -1;
+  if (tid < WK * 2) (&s_holes[0][0])[tid] = (&s_odds[0][0])[tid] = -1;
+  if (tid == 0) s_hi = 0;
+
+  // this wave's rows
+  const Row row = row_of(a, b, g, r0 + wr * 32 + c32);
+  typename F::V qreg[ND];
+  {
+    const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH + 8 * half;
+#pragma unroll
+    for (int c = 0; c < ND; ++c) qreg[c] = ldv<typename F::V>(Q + 16 * c);
+  }
+  pack_own(a, b, k0, nb, s_off);
+  const int lo = s_off[row.k - k0], hi = lo + row.own;   // the packed own rows that the row sees
+  int whi = row.live ? hi : 0, ahi = row.live ? hi : 0x7fffffff;
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) {
+    whi = max(whi, __shfl_xor(whi, x));
+    ahi = min(ahi, __shfl_xor(ahi, x));
+  }
+  // of the wave, uniform: bounds of what its rows see, and what all of them see
+  const int wlo = __builtin_amdgcn_readlane(lo, 0), alo = __builtin_amdgcn_readlane(lo, 31);
+  whi = __builtin_amdgcn_readfirstlane(whi);
+  ahi = wlo == alo ? __builtin_amdgcn_readfirstlane(ahi) : -1;
+  if (lane == 0 && grp == 0) atomicMax(&s_hi, whi);
+  __syncthreads();
+
+  const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_hi);
+  const int cctx = (nctx + KC - 1) / KC, call = cctx + (nown + KC - 1) / KC;
+  const int zb = (int)((long long)call * z / a.splits), ze = (int)((long long)call * (z + 1) / a.splits);
+
+  Op qf[ND];
+#pragma unroll
+  for (int c = 0; c < ND; ++c) {
+    if (!row.live) qreg[c] = typename F::V{};
+    if (a.scale < 0) qreg[c] = -qreg[c];   // exact; the largest score is then the largest product
+    qf[c] = F::of(qreg[c]);
+  }
+  const float sl2 = score_unit(a.scale), lag = fminf(8.f / sl2, 1e30f);
+  float m_run = -INFINITY, l_run = 0.f;    // maximum of q.k; l_run: this lane's keys only, until the end
+  f32x16 o[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) o[n] = f32x16{};
+
+  // This thread's units of a chunk.  Their pages are looked up a chunk before they are loaded.
+  unsigned kc[PER][UE / 8], vc[PER][UE / 8], ks[PER], vs[PER];
+  int entry[PER], rest[PER], list[PER];    // rest: row inside the page, -1 past the rows
+  int gone = 0, hole = 0;                  // bit p: does not count; as its page is none
+#pragma unroll
+  for (int p = 0; p < PER; ++p) list[p] = 0;
+  auto find = [&](int c) __attribute__((always_inline)) {
+    if (c >= ze) return;                   // uniform
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int key = (gt + p * GT) / UPR;
+      rest[p] = -1;
+      if (c < cctx) {                      // uniform
+        const int j = c * KC + key;
+        if (j < nctx) {
+          const int pg = packed_page(a.ctx, j);
+          rest[p] = j - pg * a.ctx.page_rows;
+          entry[p] = a.ctx.table[(long long)b * a.ctx.cols + pg];
+        }
+      } else {
+        const int x = (c - cctx) * KC + key;
+        if (x < nown) {
+          int i = list[p];
+          while (s_off[i + 1] <= x) ++i;
+          list[p] = i;
+          const int j = x - s_off[i], pg = packed_page(a.own, j);
+          rest[p] = j - pg * a.own.page_rows;
+          entry[p] = a.own.table[((long long)b * a.K + k0 + i) * a.own.cols + pg];
+        }
+      }
+    }
+  };
+  auto load = [&](int c) __attribute__((always_inline)) {
+    if (c >= ze) return;                   // uniform
+    const PackedCache& x = c < cctx ? a.ctx : a.own;
+    gone = hole = 0;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const bool none = rest[p] >= 0 && (entry[p] < 0 || entry[p] >= x.n_pages), skip = rest[p] < 0 || none;
+      gone |= skip << p;
+      hole |= none << p;
+      const int u = (gt + p * GT) % UPR, at = (skip ? 0 : rest[p]) * UPR + u;   // what does not count reads row 0 of page 0
+      const char* head = x.pages + (skip ? 0 : entry[p]) * x.page_ld + (long long)g * x.head_bytes;
+      const long long all = (long long)x.page_rows * UPR;
+      const char* k = head + (long long)at * (UE / 2);
+      const char* v = k + all * (UE / 2);
+      const unsigned char* s = reinterpret_cast<const unsigned char*>(head + all * UE) + (UE == 32 ? at : at >> 1);
+      if constexpr (UE == 32) {
+        const u32x4 kk = ldv<u32x4>(k), vv = ldv<u32x4>(v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kc[p][i] = kk[i], vc[p][i] = vv[i];
+      } else {
+        const uint2 kk = ldv<uint2>(k), vv = ldv<uint2>(v);
+        kc[p][0] = kk.x, kc[p][1] = kk.y, vc[p][0] = vv.x, vc[p][1] = vv.y;
+      }
+      ks[p] = s[0];
+      vs[p] = s[UE == 32 ? all : all >> 1];
+    }
+  };
+  // The units of a quad of lanes lie in one row: every lane starts with another one, so that the writes meet all banks.
+  const int key_of_thread = gt / UPR;
+  const int turn = DH == 128 ? key_of_thread & (UE == 32 ? 3 : 1) : DH == 64 ? (key_of_thread >> 1 & 1) << (UE == 32) : 0;
+  auto stage = [&](bf16* K, bf16* V, int c, int par) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int key = (gt + p * GT) / UPR, u = (gt + p * GT) % UPR;
+      unsigned kk[UE / 8], vv[UE / 8];
+#pragma unroll
+      for (int i = 0; i < UE / 8; ++i) kk[i] = kc[p][i], vv[i] = vc[p][i];
+      float ku = unit_of(ks[p]), vu = unit_of(vs[p]);
+      if (gone >> p & 1) {
+#pragma unroll
+        for (int i = 0; i < UE / 8; ++i) kk[i] = vv[i] = 0;
+        ku = vu = 1.f;
+        if (hole >> p & 1) s_hole[grp][par][key] = s_holes[grp][par] = c;
+      } else if (c >= cctx && vs[p] == 255) {
+        // NaN would reach the rows of other lists, as 0 times NaN: they get zeros, the rows that see it get it at the end
+#pragma unroll
+        for (int i = 0; i < UE / 8; ++i) vv[i] = 0;
+        vu = 1.f;
+        s_odd[grp][par][key * UPR + u] = s_odds[grp][par] = c;
+      }
+      auto exchange = [&](unsigned (&w)[UE / 8]) __attribute__((always_inline)) {
+        if (UE / 8 >= 2 && DH > 32) {
+          if (turn & 1) {
+#pragma unroll
+            for (int i = 0; i < UE / 8; i += 2) { const unsigned y = w[i]; w[i] = w[i + 1]; w[i + 1] = y; }
+          }
+          if (UE == 32 && (turn & 2)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { const unsigned y = w[i]; w[i] = w[(i + 2) % (UE / 8)]; w[(i + 2) % (UE / 8)] = y; }
+          }
+        }
+      };
+      exchange(kk);
+      exchange(vv);
+#pragma unroll
+      for (int i = 0; i < UE / 8; ++i) {
+        const int at = L::at(key, u * (UE / 8) + (i ^ turn));
+        *reinterpret_cast<bf16x8*>(K + at) = values8(kk[i], ku);
+        *reinterpret_cast<bf16x8*>(V + at) = values8(vv[i], vu);
+      }
+    }
+  };
+
+  int rl = L::row_lane(lane), cl = L::col_lane(lane);
+  const bool idle = r0 + wr * 32 >= a.R;
+  find(zb + grp);
+  load(zb + grp);
+  find(zb + grp + WK);
+  const int trips = (ze - zb + WK - 1) / WK;
+  for (int it = 0; it < trips; ++it) {
+    const int c = zb + grp + it * WK, par = it & 1;
+    bf16 *K = s_kv[grp][it % NBUF][0], *V = s_kv[grp][it % NBUF][1];
+    if (c < ze) stage(K, V, c, par);
+    load(c + WK);
+    find(c + 2 * WK);
+    if constexpr (WR > 1) lds_barrier();   // also the end of every wave's reads of the buffer written next
+    else order();
+    if (c >= ze || idle) continue;         // uniform
+    rl = fresh(rl);
+    cl = fresh(cl);
+    const bool own = c >= cctx;
+    const bool holes = __builtin_amdgcn_readfirstlane(s_holes[grp][par]) == c;
+    const bool odds = __builtin_amdgcn_readfirstlane(s_odds[grp][par]) == c;
+#pragma unroll 1
+    for (int kb = 0; kb < KC; kb += 32) {
+      const int x0 = (own ? c - cctx : c) * KC + kb;     // first key: of the shared rows, or packed
+      if (own ? x0 >= whi : x0 >= nctx) break;           // uniform
+      if (own && x0 + 32 <= wlo) continue;
+      f32x16 s{};
+#pragma unroll
+      for (int d = 0; d < ND; ++d) s = mma_held(L::rows(K, kb, d, rl), qf[d], s);
+      // element i of a lane is key 8 (i / 4) + 4 half + i % 4 of the step
+      if (own ? x0 < alo || x0 + 32 > ahi : x0 + 32 > nctx) {   // uniform
+        const int from = (own ? lo : 0) - x0 - 4 * half, to = (own ? hi : nctx) - x0 - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (8 * (i >> 2) + (i & 3) < from || 8 * (i >> 2) + (i & 3) >= to) s[i] = -INFINITY;
+      }
+      if (holes) {                         // uniform
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (s_hole[grp][par][kb + 8 * (i >> 2) + 4 * half + (i & 3)] == c) s[i] = -INFINITY;
+      }
+      float mx = m_run;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
+      // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
+      if (__any(mx > m_run + lag)) {
+        const float top = halves_max(mx);
+        if (top > m_run + lag) {
+          const float alpha = __builtin_amdgcn_exp2f((m_run - top) * sl2);
+          m_run = top;
+          l_run *= alpha;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) o[n] *= alpha;
+        }
+      }
+      const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -ref));
+        sum[i & 3] += s[i];
+      }
+      l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        f32x8 w;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = s[8 * m + j];
+        const Op p = F::rounded(w);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 16 * m, n, cl), p, o[n]);
+      }
+      if (odds) {                          // uniform: the columns of a NaN block, in the rows that see its key
+#pragma unroll 1
+        for (int e = 0; e < 32 * UPR; ++e) {
+          const int x = x0 + e / UPR, n = e % UPR * UE / 32;
+          if (__builtin_amdgcn_readfirstlane(s_odd[grp][par][kb * UPR + e]) != c || x < lo || x >= hi) continue;
+#pragma unroll
+          for (int q = 0; q < NB; ++q)
+            if (q == n) o[q] += f32x16{} + NAN;
+        }
+      }
+    }
+    if constexpr (WR == 1) order();        // this chunk's reads before the next one's writes
+  }
+
+  float l = halves_sum(l_run);
+  if constexpr (WK > 1) {                  // joins the groups in their order: group 0's waves hold the sums
+    __syncthreads();
+    float* X = reinterpret_cast<float*>(s_kv);
+    constexpr int LANE = 16 * NB;          // floats of a lane
+    if (grp > 0) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(X + ((wave - WR) * LANE + 16 * n + 4 * q) * 64 + 4 * lane) =
+              f32x4{o[n][4 * q], o[n][4 * q + 1], o[n][4 * q + 2], o[n][4 * q + 3]};
+      if (half == 0) {
+        s_ml[wave][c32][0] = m_run;
+        s_ml[wave][c32][1] = l;
+      }
+    }
+    __syncthreads();
+    if (grp > 0) return;
+    float top = m_run;
+#pragma unroll
+    for (int w = 1; w < WK; ++w) top = fmaxf(top, s_ml[w * WR + wr][c32][0]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float f = __builtin_amdgcn_exp2f((m_run - ref) * sl2);
+    l *= f;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) o[n] *= f;
+#pragma unroll
+    for (int w = 1; w < WK; ++w) {
+      const int other = w * WR + wr;
+      f = __builtin_amdgcn_exp2f((s_ml[other][c32][0] - ref) * sl2);
+      l = fmaf(s_ml[other][c32][1], f, l);
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = ldv<f32x4>(X + ((other - WR) * LANE + 16 * n + 4 * q) * 64 + 4 * lane);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][4 * q + i] = fmaf(v[i], f, o[n][4 * q + i]);
+        }
+    }
+    m_run = top;
+  }
+
+  if (r0 + wr * 32 + c32 >= a.R) return;
+  const float m2 = m_run * sl2;
+  const long long ro = row.at * a.Hq + row.h;
+  if (a.splits > 1) {
+    const long long at = (long long)z * a.B * a.K * a.S * a.Hq + ro;
+    float* po = a.part_o + at * DH;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(po + 32 * n + 8 * q + 4 * half) =
+            f32x4{o[n][4 * q], o[n][4 * q + 1], o[n][4 * q + 2], o[n][4 * q + 3]};
+    if (half == 0) {
+      a.part_ml[at * 2] = m2;
+      a.part_ml[at * 2 + 1] = l;
+    }
+    return;
+  }
+  const bool none = !row.live || l == 0.f;   // no key; a NaN score leaves a NaN sum
+  const float inv = none ? 0.f : 1.f / l;
+  T* out = static_cast<T*>(a.out) + row.at * a.out_ld + row.h * DH + 4 * half;
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      T4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(none ? 0.f : o[n][4 * q + i] * inv);
+      *reinterpret_cast<T4*>(out + 32 * n + 8 * q) = v;
+    }
+  if (a.lse && half == 0) a.lse[ro] = none ? -INFINITY : (m2 + log2f(l)) * kLn2;
+}
+
+// Joins the key ranges of a row in ascending order: DH / 4 threads a row.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
+  const long long rows = (long long)a.B * a.K * a.S * a.Hq;
+  const long long e = (long long)blockIdx.x * 256 + threadIdx.x, ro = e / (DH / 4);
+  const int d0 = (int)(e % (DH / 4)) * 4;
+  if (ro >= rows) return;
+  float top = -INFINITY;
+  for (int z = 0; z < a.splits; ++z) top = fmaxf(top, a.part_ml[(z * rows + ro) * 2]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float l = 0.f;
+  f32x4 o{};
+#pragma unroll 4
+  for (int z = 0; z < a.splits; ++z) {
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[(z * rows + ro) * 2] - ref);
+    const f32x4 v = ldv<f32x4>(a.part_o + (z * rows + ro) * DH + d0);
+    l = fmaf(a.part_ml[(z * rows + ro) * 2 + 1], f, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
+  }
+  const long long at = ro / a.Hq;
+  const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);
+  const bool none = s >= q_rows(a, bk) || l == 0.f;
+  const float inv = none ? 0.f : 1.f / l;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(none ? 0.f : o[i] * inv);
+  *reinterpret_cast<T4*>(static_cast<T*>(a.out) + at * a.out_ld + h * DH + d0) = v;
+  if (a.lse && d0 == 0) a.lse[ro] = none ? -INFINITY : (top + log2f(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------------------
+// Weights.  A wave takes 32 NK keys of a sequence's head, as operands in registers from the codes themselves (which
+// column a summed element is does not matter: lane l has the half l / 32 of its key's columns), and walks the query rows that
+// see them, 32 at a time: a lane then holds 16 rows' scores of its key, and their exponentials are added up in it.  Shared keys
+// meet every list's rows, own keys their list's.
+// ------------------------------------------------------------------------------------------
+template <typename T, int DH, int NK>
+__global__ __launch_bounds__(256, sizeof(T) * DH >= 256 ? 2 : 3) void k_packed_weigh(PackedArgs a) {
+  typedef Form<T> F;
+  constexpr int ND = DH / 16;              // products of 16 columns
+  __shared__ float s_lse[4][32];
+  __shared__ int s_seen[4][32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, c32 = lane & 31;
+  // one task a wave: (request, key head, key tile, row range) of the shared rows, then (list, ...) of the own rows
+  const long long n_ctx = (long long)a.B * a.Hkv * a.ctx_tiles * a.ctx_splits;
+  long long id = (long long)xcd_tile(blockIdx.x, gridDim.x) * 4 + wave;
+  const bool own = id >= n_ctx;
+  if (own) id -= n_ctx;
+  const int tiles = own ? a.own_tiles : a.ctx_tiles, splits = own ? a.own_splits : a.ctx_splits;
+  if (own && id >= (long long)a.B * a.K * a.Hkv * a.own_tiles * a.own_splits) return;
+  const int t = (int)(id % tiles);
+  id /= tiles;
+  const int z = (int)(id % splits);
+  id /= splits;
+  const int g = (int)(id % a.Hkv), sq = (int)(id / a.Hkv), b = own ? sq / a.K : sq;
+  const PackedCache& x = own ? a.own : a.ctx;
+  const int n = packed_len(x, sq), j0 = t * 32 * NK;
+  if (j0 >= n) return;
+  const int sg = a.S * a.G, first = own ? (sq - b * a.K) * sg : 0;     // rows of the request that may see the keys
+  const int all_rows = own ? q_rows(a, sq) * a.G : a.R;
+  const int steps = (all_rows + 31) / 32, ib = (int)((long long)steps * z / splits), ie = (int)((long long)steps * (z + 1) / splits);
+
+  bf16x8 kf[NK][ND];
+  bool counts[NK];
+#pragma unroll
+  for (int u = 0; u < NK; ++u) {
+    const int j = j0 + 32 * u + c32;
+    int page = -1, r = 0;
+    if (j < n) {
+      const int p = packed_page(x, j);
+      r = j - p * x.page_rows;
+      page = x.table[(long long)sq * x.cols + p];
+    }
+    counts[u] = page >= 0 && page < x.n_pages;
+    const char* head = x.pages + (counts[u] ? page : 0) * x.page_ld + (long long)g * x.head_bytes;
+    const int row = counts[u] ? r : 0;
+    const unsigned* code = reinterpret_cast<const unsigned*>(head + (long long)row * (DH / 2)) + half * (DH / 16);
+    const unsigned char* scale = reinterpret_cast<const unsigned char*>(head + (long long)x.page_rows * DH) + row * (DH / 32);
+#pragma unroll
+    for (int c = 0; c < ND; ++c) kf[u][c] = values8(code[c], unit_of(scale[DH == 32 ? 0 : (half * (DH / 2) + 8 * c) / 32]));
+  }
+  const float scale = a.scale;
+  float sum[NK];
+#pragma unroll
+  for (int u = 0; u < NK; ++u) sum[u] = 0.f;
+
+  const int m = own ? n : 0, nq = own ? q_rows(a, sq) : 0;
+  bool any = false;                        // a row that counts
+  for (int i = ib; i < ie; ++i) {
+    const int rr = i * 32 + c32;
+    const bool inside = rr < all_rows;
+    const Row w = row_of(a, b, g, first + min(rr, all_rows - 1));
+    const float lse = a.lse[w.at * a.Hq + w.h];
+    const bool live = inside && w.live && lse != -INFINITY;
+    any |= __any(live);
+    const T* Q = static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + half * (DH / 2);
+    if (half == 0) {
+      s_lse[wave][c32] = live ? lse : INFINITY;
+      s_seen[wave][c32] = !live ? 0 : a.causal ? m - nq + w.s + 1 : m;   // own keys that it sees
+    }
+    f32x16 s[NK];
+#pragma unroll
+    for (int u = 0; u < NK; ++u) s[u] = f32x16{};
+#pragma unroll
+    for (int c = 0; c < ND; ++c) {
+      typename F::V v = ldv<typename F::V>(Q + 8 * c);
+      if (!live) v = typename F::V{};
+      const typename F::Op q = F::of(v);
+#pragma unroll
+      for (int u = 0; u < NK; ++u) s[u] = mma_held_right(q, kf[u][c], s[u]);
+    }
+    order();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {          // rows 8 e + 4 half + 0 .. 3
+      const f32x4 ls = ldv<f32x4>(&s_lse[wave][8 * e + 4 * half]);
+      const int4 seen = ldv<int4>(&s_seen[wave][8 * e + 4 * half]);
+#pragma unroll
+      for (int u = 0; u < NK; ++u) {
+        const int j = j0 + 32 * u + c32;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float d = fmaf(s[u][4 * e + q], scale, -ls[q]);
+          const float p = __builtin_amdgcn_exp2f(d * kLog2e);
+          const int to = q == 0 ? seen.x : q == 1 ? seen.y : q == 2 ? seen.z : seen.w;
+          sum[u] += !own || j < to ? p : 0.f;
+        }
+      }
+    }
+    order();
+  }
+  const float* wi = own ? a.own_w : a.ctx_w;
+  float* wo = own ? a.own_w_out : a.ctx_w_out;
+  float* part = own ? a.part_own : a.part_ctx;
+  const long long N = own ? (long long)a.B * a.K : a.B;
+#pragma unroll
+  for (int u = 0; u < NK; ++u) {
+    const float total = halves_sum(sum[u]);
+    const int j = j0 + 32 * u + c32;
+    if (j >= n || half) continue;
+    const long long at = ((long long)sq * a.Hkv + g) * x.cap + j;
+    const float got = counts[u] && any ? total : 0.f;   // rows that do not count may have met NaN
+    if (splits > 1) part[(z * N * a.Hkv) * x.cap + at] = got;
+    else wo[at] = wi[at] + got;
+  }
+}
+
+// Adds the row ranges of every key in ascending order.
+__global__ __launch_bounds__(256) void k_packed_weigh_sum(PackedCache x, int Hkv, int splits, long long keys, const float* part,
+                                                          const float* w, float* out) {
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (at >= keys) return;
+  const int s = (int)(at / x.cap / Hkv);
+  if (at % x.cap >= packed_len(x, s)) return;
+  float v = 0.f;
+  for (int z = 0; z < splits; ++z) v += part[z * keys + at];
+  out[at] = w[at] + v;
+}
+
+template <typename T, int DH, int UE>
+void fwd_tiles(const PackedArgs& a, const PackedPlan& p, dim3 grid, hipStream_t s) {
+  if (p.waves == 1) hipLaunchKernelGGL((k_packed_fwd<T, DH, 1, UE>), grid, dim3(256), 0, s, a);
+  else if (p.waves == 2) hipLaunchKernelGGL((k_packed_fwd<T, DH, 2, UE>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_packed_fwd<T, DH, 4, UE>), grid, dim3(256), 0, s, a);
+}
+template <typename T, int DH, int UE>
+hipError_t fwd(const PackedArgs& a, const PackedPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.splits * a.tiles));
+  fwd_tiles<T, DH, UE>(a, p, grid, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  const long long n = (long long)a.B * a.K * a.S * a.Hq * (DH / 4);
+  hipLaunchKernelGGL((k_packed_join<T, DH>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+constexpr int kWeighKeys = 2;              // 32-key operands of a wave
+
+template <typename T, int DH>
+hipError_t weigh(const PackedArgs& a, hipStream_t s) {
+  const long long tasks = (long long)a.B * a.Hkv * ((long long)a.ctx_tiles * a.ctx_splits + (long long)a.K * a.own_tiles * a.own_splits);
+  if (tasks > 0) hipLaunchKernelGGL((k_packed_weigh<T, DH, kWeighKeys>), dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, s, a);
+  hipError_t e = hipGetLastError();
+  auto sum = [&](const PackedCache& x, long long n, int splits, const float* part, const float* w, float* out) {
+    if (e != hipSuccess || splits <= 1) return;
+    const long long keys = n * a.Hkv * x.cap;
+    hipLaunchKernelGGL(k_packed_weigh_sum, dim3((unsigned)((keys + 255) / 256)), dim3(256), 0, s, x, a.Hkv, splits, keys, part, w, out);
+    e = hipGetLastError();
+  };
+  if (a.ctx_tiles) sum(a.ctx, a.B, a.ctx_splits, a.part_ctx, a.ctx_w, a.ctx_w_out);
+  if (a.own_tiles) sum(a.own, (long long)a.B * a.K, a.own_splits, a.part_own, a.own_w, a.own_w_out);
+  return e;
+}
+
+}  // namespace
+
+PackedPlan packed_plan(const fe_packed_args& a) {
+  PackedPlan p;
+  const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, bg = (long long)a.B * a.n_kv_heads;
+  p.waves = R <= 32 ? 1 : R <= 64 ? 2 : 4;
+  const long long rows = 32 * p.waves, sg = (long long)a.S * G;
+  p.tiles = (int)((R + rows - 1) / rows);
+  const long long T = a.ctx.N > 0 ? (long long)a.ctx.cols * a.ctx.page_rows : 0;
+  const long long L = a.own.N > 0 ? (long long)a.own.cols * a.own.page_rows : 0;
+  const long long keys = T + std::min<long long>(a.K, (rows - 1) / sg + 2) * L, wgs = bg * p.tiles;
+  const long long items = (keys + 63) / 64;
+  long long want = (512 + wgs - 1) / wgs;                       // two workgroups a compute unit
+  want = std::min(want, std::max(1LL, items / 4));
+  if (a.dtype == FE_F32) want = std::max(want, (items + 31) / 32);   // fp32 sums over at most 2048 keys
+  const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);
+  p.splits = (int)std::max(1LL, std::min({want, 256LL, grid}));
+  const size_t out_rows = (size_t)a.B * a.K * a.S * a.n_heads;
+  p.part_bytes = p.splits > 1 ? p.splits * out_rows * (a.dh + 2) * sizeof(float) : 0;
+  return p;
+}
+
+PackedWeighPlan packed_weigh_plan(const fe_packed_args& a) {
+  PackedWeighPlan p{};
+  const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, sg = (long long)a.S * G;
+  const long long T = a.ctx.N > 0 && a.ctx_w ? (long long)a.ctx.cols * a.ctx.page_rows : 0;
+  const long long L = a.own.N > 0 && a.own_w ? (long long)a.own.cols * a.own.page_rows : 0;
+  const int tile = 32 * kWeighKeys;
+  p.ctx_tiles = (int)((T + tile - 1) / tile);
+  p.own_tiles = (int)((L + tile - 1) / tile);
+  // waves enough for the chip, each with 128 rows at least
+  auto ranges = [](long long waves, long long rows) {
+    return (int)std::max(1LL, std::min({(2048 + waves - 1) / std::max(1LL, waves), rows / 128, 64LL}));
+  };
+  const long long bg = (long long)a.B * a.n_kv_heads;
+  p.ctx_splits = p.ctx_tiles ? ranges(bg * p.ctx_tiles, R) : 1;
+  p.own_splits = p.own_tiles ? ranges(bg * a.K * p.own_tiles, sg) : 1;
+  p.ctx_bytes = p.ctx_splits > 1 ? (size_t)p.ctx_splits * bg * T * sizeof(float) : 0;
+  p.own_bytes = p.own_splits > 1 ? (size_t)p.own_splits * bg * a.K * L * sizeof(float) : 0;
+  p.blocks = (bg * ((long long)p.ctx_tiles * p.ctx_splits + (long long)a.K * p.own_tiles * p.own_splits) + 3) / 4;
+  p.sum_blocks = std::max(p.ctx_splits > 1 ? (bg * T + 255) / 256 : 0, p.own_splits > 1 ? (bg * a.K * L + 255) / 256 : 0);
+  return p;
+}
+
+hipError_t launch_packed_attention(const PackedArgs& a, int dh, bool bf16_rows, const PackedPlan& p, hipStream_t s) {
+  if (bf16_rows) return dh == 32 ? fwd<bf16, 32, 32>(a, p, s) : dh == 64 ? fwd<bf16, 64, 32>(a, p, s) : fwd<bf16, 128, 32>(a, p, s);
+  return dh == 32 ? fwd<float, 32, 32>(a, p, s) : dh == 64 ? fwd<float, 64, 32>(a, p, s) : fwd<float, 128, 32>(a, p, s);
+}
+
+hipError_t launch_packed_weights(const PackedArgs& a, int dh, bool bf16_rows, hipStream_t s) {
+  if (bf16_rows) return dh == 32 ? weigh<bf16, 32>(a, s) : dh == 64 ? weigh<bf16, 64>(a, s) : weigh<bf16, 128>(a, s);
+  return dh == 32 ? weigh<float, 32>(a, s) : dh == 64 ? weigh<float, 64>(a, s) : weigh<float, 128>(a, s);
+}

@@ -28,7 +28,9 @@ EXPORTED = ("fe_param_count", "fe_model_create", "fe_model_destroy", "fe_workspa
             "fe_cross_sequence_noalloc", "fe_score_select", "fe_encode_sequences", "fe_score_objectives", "fe_naive_workspace_size", "fe_evaluate_naive", "fe_trace_enable", "fe_trace_read",
             "fe_trace_read_launches", "fe_trace_family", "fe_train_workspace_size", "fe_train_grads",
             "fe_executor_create", "fe_executor_submit", "fe_executor_join", "fe_executor_destroy",
-            "fe_cache_append", "fe_prefix_workspace_size", "fe_prefix_attention", "fe_prefix_attention_grad")
+            "fe_cache_append", "fe_prefix_workspace_size", "fe_prefix_attention", "fe_prefix_attention_grad",
+            "fe_packed_page_bytes", "fe_packed_append", "fe_packed_read", "fe_packed_attention", "fe_packed_weights",
+            "fe_packed_evict", "fe_packed_workspace_size")
 FE_EXECUTOR_MAX_STREAMS = 8
 FE_TRACE_FAMILIES = 12
 
@@ -77,6 +79,27 @@ class fe_prefix_grads(ctypes.Structure):
                 ("down_v", ctypes.c_void_p)]
 
 
+class fe_packed_cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("page_ld", ctypes.c_int64), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("N", ctypes.c_int32), ("cols", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32)]
+
+
+def _packed(name: str, caches: str, ints: str, pointers: str, tail=()):
+    """A ctypes structure of fe_packed_cache fields, then as _struct."""
+    plain = _struct(name, ints, pointers, tail)
+    return type(name, (ctypes.Structure,), {"_fields_": [(n, fe_packed_cache) for n in caches.split()] + plain._fields_})
+
+
+fe_packed_append_args = _packed(
+    "fe_packed_append_args", "cache", "dtype S n_heads n_kv_heads dh rot neighbours q_ld k_ld v_ld q_out_ld",
+    "q k v q_out freq new_len pos0 len_out status")
+fe_packed_read_args = _packed("fe_packed_read_args", "cache", "dtype S n_kv_heads dh k_ld v_ld", "start count k v")
+fe_packed_args = _packed(
+    "fe_packed_args", "ctx own", "dtype B K S n_heads n_kv_heads dh causal scale q_ld out_ld",
+    "q q_len out lse ctx_w own_w ctx_w_out own_w_out ws", [("ws_bytes", ctypes.c_size_t)])
+fe_packed_evict_args = _packed(
+    "fe_packed_evict_args", "from_ to", "n_kv_heads dh keep first recent", "weight weight_out kept status")
+
 _lib = None
 
 
@@ -123,6 +146,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fe_prefix_workspace_size": (S, [ctypes.POINTER(fe_prefix_args), I, ctypes.POINTER(Z)]),
         "fe_prefix_attention": (S, [ctypes.POINTER(fe_prefix_args), P]),
         "fe_prefix_attention_grad": (S, [ctypes.POINTER(fe_prefix_args), ctypes.POINTER(fe_prefix_grads), P]),
+        "fe_packed_page_bytes": (S, [I, I, I, ctypes.POINTER(Z)]),
+        "fe_packed_append": (S, [ctypes.POINTER(fe_packed_append_args), P]),
+        "fe_packed_read": (S, [ctypes.POINTER(fe_packed_read_args), P]),
+        "fe_packed_workspace_size": (S, [ctypes.POINTER(fe_packed_args), I, ctypes.POINTER(Z)]),
+        "fe_packed_attention": (S, [ctypes.POINTER(fe_packed_args), P]),
+        "fe_packed_weights": (S, [ctypes.POINTER(fe_packed_args), P]),
+        "fe_packed_evict": (S, [ctypes.POINTER(fe_packed_evict_args), P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -374,6 +404,49 @@ def fe_prefix_attention(args: fe_prefix_args, stream=None) -> None:
 def fe_prefix_attention_grad(args: fe_prefix_args, grads: fe_prefix_grads, stream=None) -> None:
     _check(load_library().fe_prefix_attention_grad(ctypes.byref(args), ctypes.byref(grads), _stream(stream)),
            "fe_prefix_attention_grad")
+
+
+def fe_packed_page_bytes(page_rows: int, n_kv_heads: int, dh: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().fe_packed_page_bytes(page_rows, n_kv_heads, dh, ctypes.byref(n)), "fe_packed_page_bytes")
+    return n.value
+
+
+def fe_packed_append(args: fe_packed_append_args, stream=None) -> None:
+    st = load_library().fe_packed_append(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_packed_append")
+
+
+def fe_packed_read(args: fe_packed_read_args, stream=None) -> None:
+    st = load_library().fe_packed_read(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_packed_read")
+
+
+def fe_packed_workspace_size(args: fe_packed_args, weights: bool = False) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().fe_packed_workspace_size(ctypes.byref(args), 1 if weights else 0, ctypes.byref(n)),
+           "fe_packed_workspace_size")
+    return n.value
+
+
+def fe_packed_attention(args: fe_packed_args, stream=None) -> None:
+    st = load_library().fe_packed_attention(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_packed_attention")
+
+
+def fe_packed_weights(args: fe_packed_args, stream=None) -> None:
+    st = load_library().fe_packed_weights(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_packed_weights")
+
+
+def fe_packed_evict(args: fe_packed_evict_args, stream=None) -> None:
+    st = load_library().fe_packed_evict(args, _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_packed_evict")
 
 
 def fe_trace_enable(on: bool) -> None:
@@ -838,3 +911,250 @@ class PrefixAttention:
         g.dq, g.dctx_k, g.dctx_v, g.down_k, g.down_v = (t.data_ptr() for t in self.grads)
         fe_prefix_attention_grad(a, g, handle)
         return self.grads
+
+
+# ---------------------------------------------------------------------------------------------
+# A cache in 4 bits (include/flasheval_packed.h)
+# ---------------------------------------------------------------------------------------------
+
+class PagedCache4:
+    """Keys and values of N growing sequences in 4 bits, in pages of a shared pool (fe_packed_append and its kin).
+
+    pages [n_pages][page_bytes(page_rows, n_kv_heads, dh)] uint8 and table [N][cols] int32 are the caller's:
+    table[s][c] names the page that holds rows c * page_rows .. of sequence s.  len [N] int32 counts the rows
+    of every sequence; `append` advances it, `evict` sets that of the cache it fills.  A shared context is such a cache of B
+    sequences, the lists' own rows one of B * K; both may use one pool."""
+
+    def __init__(self, pages, table, page_rows: int, n_kv_heads: int, dh: int, length=None):
+        import torch
+        width = self.page_bytes(page_rows, n_kv_heads, dh)
+        if pages.dtype != torch.uint8 or pages.dim() != 2 or pages.shape[1] != width or pages.stride(1) != 1:
+            raise ValueError(f"pages: expected a uint8 tensor [pages][{width}] with dense rows, got {pages.dtype} "
+                             f"{tuple(pages.shape)}")
+        if table.dim() != 2:
+            raise ValueError(f"table: expected [sequences][columns], got {tuple(table.shape)}")
+        self.N, self.cols = table.shape
+        _need(table, "table", torch.int32, self.N * self.cols)
+        self.len = torch.zeros(self.N, dtype=torch.int32, device=table.device) if length is None else length
+        _need(self.len, "length", torch.int32, self.N)
+        self.pages, self.table, self.page_rows, self.n_kv_heads, self.dh = pages, table, page_rows, n_kv_heads, dh
+        self.capacity = self.cols * page_rows
+        self.status = torch.zeros(self.N, dtype=torch.int32, device=table.device)
+        _on_device((pages, table, self.len))
+        self._kept = _Kept(self.status, self.len if length is None else None)
+        c = self.cache = fe_packed_cache(_ptr(pages), pages.stride(0) if pages.shape[0] > 1 else width, _ptr(table),
+                                         _ptr(self.len), self.N, self.cols, page_rows, pages.shape[0])
+        self.args, self.read_args, self.evict_args = (t() for t in (fe_packed_append_args, fe_packed_read_args,
+                                                                    fe_packed_evict_args))
+        self.args.cache = self.read_args.cache = self.evict_args.from_ = c
+        for a in (self.args, self.read_args, self.evict_args):
+            a.n_kv_heads, a.dh = n_kv_heads, dh
+        self.args.status = self.evict_args.status = _ptr(self.status)
+        self._layouts, self._read_layouts = _Layouts(), _Layouts()
+
+    @staticmethod
+    def page_bytes(page_rows: int, n_kv_heads: int, dh: int) -> int:
+        """Bytes of a page: 17/32 of a byte for a column of keys and one of values, heads rounded up to 16 bytes."""
+        return fe_packed_page_bytes(page_rows, n_kv_heads, dh)
+
+    def _type(self, t, name: str):
+        import torch
+        if t.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"{name}: bfloat16 or float32, got {t.dtype}")
+        return FE_BF16 if t.dtype == torch.bfloat16 else FE_F32
+
+    def _check(self, k, v, q, q_out, freq, new_len, pos0, len_out):
+        """(dtype, rows, n_heads, k_ld, v_ld, q_ld, q_out_ld, rot) of an append's tensors."""
+        import torch
+        act, N = self._type(k, "k"), self.N
+        if k.dim() != 4:
+            raise ValueError(f"k: expected [sequences][rows][heads][dh], got {tuple(k.shape)}")
+        S, dt = k.shape[1], k.dtype
+        k_ld, v_ld = (_row_stride(t, n, (N, S, self.n_kv_heads, self.dh), dt) for t, n in ((k, "k"), (v, "v")))
+        H = q_ld = q_out_ld = 0
+        if q is not None:
+            if q.dim() != 4:
+                raise ValueError(f"q: expected [sequences][rows][heads][dh], got {tuple(q.shape)}")
+            H = q.shape[2]
+            q_ld, q_out_ld = (_row_stride(t, n, (N, S, H, self.dh), dt) for t, n in ((q, "q"), (q_out, "q_out")))
+        if freq is not None:
+            _need(freq, "freq", torch.float64, freq.numel())
+        for t, name in ((new_len, "new_len"), (pos0, "pos0"), (len_out, "len_out")):
+            _need(t, name, torch.int32, N)
+        return act, S, H, k_ld, v_ld, q_ld, q_out_ld, 0 if freq is None else 2 * freq.numel()
+
+    def append(self, k, v, q=None, q_out=None, new_len=None, pos0=None, freq=None, neighbours=False, len_out=None,
+               stream=None):
+        """Append rows k, v [N][S][n_kv_heads][dh], bf16 or fp32 (the first new_len[s] of sequence s); with `freq` (float64
+        [rot / 2]) keys and q [N][S][n_heads][dh] are turned by their positions pos0[s] + row.  q_out defaults to a new
+        tensor and may not be q; it is returned.  The lengths advance in place, or into len_out when that is given.
+        `status` [N] holds FE_DEV_BAD_PAGE for a sequence with a row that found no page."""
+        a = self.args
+        if (q is None) != (q_out is None):
+            if q is None:
+                raise ValueError("q_out without q")
+            q_out = q.new_empty(q.shape)
+            _allocated_for(stream, q_out)
+        a.dtype, a.S, a.n_heads, a.k_ld, a.v_ld, a.q_ld, a.q_out_ld, a.rot = self._layouts.of(
+            self._check, k, v, q, q_out, freq, new_len, pos0, len_out)
+        handle = _stream_on(_on_device((k, v, q, q_out, freq, new_len, pos0, len_out, self.pages)), stream)
+        self._kept.use_on(handle)
+        a.neighbours = 1 if neighbours else 0
+        a.q, a.k, a.v, a.q_out, a.freq = _addr(q), k.data_ptr(), v.data_ptr(), _addr(q_out), _addr(freq)
+        a.new_len, a.pos0, a.len_out = _addr(new_len), _addr(pos0), a.cache.len if len_out is None else len_out.data_ptr()
+        fe_packed_append(a, handle)
+        return q_out
+
+    def _check_read(self, k, v, start, count):
+        """(dtype, rows, k_ld, v_ld) of a read's tensors."""
+        import torch
+        t = v if k is None else k
+        act = self._type(t, "k")
+        if t.dim() != 4:
+            raise ValueError(f"k, v: expected [sequences][rows][heads][dh], got {tuple(t.shape)}")
+        shape = (self.N, t.shape[1], self.n_kv_heads, self.dh)
+        lds = [0 if x is None else _row_stride(x, n, shape, t.dtype) for x, n in ((k, "k"), (v, "v"))]
+        _need(start, "start", torch.int32, self.N)
+        _need(count, "count", torch.int32, self.N)
+        return act, t.shape[1], lds[0], lds[1]
+
+    def read(self, k=None, v=None, start=None, count=None, stream=None):
+        """The values that rows start[s] .. start[s] + count[s] stand for, into k and v [N][S][n_kv_heads][dh], bf16 or
+        fp32 (exact in both); either may be None.  Without `start` from row 0, without `count` up to the length; other
+        rows of k and v are left as they were.  Without k and v: new bf16 tensors of the cache's capacity, zeros past the
+        length.  Returns (k, v)."""
+        import torch
+        a = self.read_args
+        if k is None and v is None:
+            k, v = (torch.zeros((self.N, self.capacity, self.n_kv_heads, self.dh), dtype=torch.bfloat16,
+                                device=self.pages.device) for _ in range(2))
+            _allocated_for(stream, k, v)
+        a.dtype, a.S, a.k_ld, a.v_ld = self._read_layouts.of(self._check_read, k, v, start, count)
+        handle = _stream_on(_on_device((v if k is None else k, v, start, count, self.pages)), stream)
+        self._kept.use_on(handle)
+        a.k, a.v, a.start, a.count = _addr(k), _addr(v), _addr(start), _addr(count)
+        fe_packed_read(a, handle)
+        return k, v
+
+    def evict(self, weights, to: "PagedCache4", keep: int, first: int = 0, recent: int = 0, weights_out=None, kept=None,
+              stream=None):
+        """Fill `to`, a cache of as many sequences in pages that none of this one's sequences use, with the `keep` rows of
+        every sequence and key head that matter: the `first` and the `recent` ones, and of the others those of
+        greatest weights [N][n_kv_heads][capacity] (fp32; of equal ones the lower index).  Sets to.len; rows keep their
+        order and their bits.  Their weights go to weights_out [N][n_kv_heads][to.capacity] when given, their indices
+        here to kept [N][n_kv_heads][keep] int32 (-1 where there are fewer), which is returned.  `status` holds
+        FE_DEV_BAD_PAGE for a sequence with rows of no page."""
+        import torch
+        a = self.evict_args
+        if (to.N, to.n_kv_heads, to.dh) != (self.N, self.n_kv_heads, self.dh):
+            raise ValueError(f"to: expected {self.N} sequences of {self.n_kv_heads} heads of {self.dh}, got "
+                             f"{(to.N, to.n_kv_heads, to.dh)}")
+        if kept is None:
+            kept = torch.empty((self.N, self.n_kv_heads, keep), dtype=torch.int32, device=self.pages.device)
+            _allocated_for(stream, kept)
+        _need(weights, "weights", torch.float32, self.N * self.n_kv_heads * self.capacity)
+        _need(weights_out, "weights_out", torch.float32, self.N * self.n_kv_heads * to.capacity)
+        _need(kept, "kept", torch.int32, self.N * self.n_kv_heads * keep)
+        handle = _stream_on(_on_device((weights, weights_out, kept, self.pages, to.pages)), stream)
+        self._kept.use_on(handle)
+        to._kept.use_on(handle)
+        a.to, a.keep, a.first, a.recent = to.cache, keep, first, recent
+        a.weight, a.weight_out, a.kept = weights.data_ptr(), _addr(weights_out), kept.data_ptr()
+        fe_packed_evict(a, handle)
+        return kept
+
+
+class PrefixAttention4:
+    """Attention of K lists per request over shared rows and each list's own rows, both held in 4 bits (fe_packed_attention),
+    and the weight that every cached row received (fe_packed_weights), with outputs and workspace for one batch shape.
+
+    `run` takes q [B][K][S][n_heads][dh], `ctx`, a PagedCache4 of B sequences with a capacity of T rows, and `own`, one of
+    B * K sequences with a capacity of L rows (T = 0 or L = 0: None); their lengths are the rows in use, q_len [B][K]
+    int32 the query rows in use, with `causal` the last own rows.  out and lse [B][K][S][n_heads] belong to this
+    object and are overwritten by its next call, as is its workspace: one object per stream."""
+
+    def __init__(self, B: int, K: int, S: int, T: int, L: int, n_heads: int, n_kv_heads: int, dh: int, dtype: str,
+                 causal: bool = False, scale: Optional[float] = None):
+        self.act, self.B, self.K, self.T, self.L = _act(dtype), B, K, T, L
+        a = self.args = fe_packed_args()
+        a.dtype = FE_BF16 if dtype == "bf16" else FE_F32
+        a.B, a.K, a.S, a.n_heads, a.n_kv_heads, a.dh = B, K, S, n_heads, n_kv_heads, dh
+        a.causal = 1 if causal else 0
+        a.scale = dh ** -0.5 if scale is None else scale
+        if T < 0 or L < 0:
+            raise ValueError(f"T and L must be >= 0, got {T} and {L}")
+        # workspaces go by the capacity, however it is cut into pages
+        a.ctx = fe_packed_cache(None, 0, None, None, B if T else 0, 1, T, 1)
+        a.own = fe_packed_cache(None, 0, None, None, B * K if L else 0, 1, L, 1)
+        a.ctx_w, a.own_w = (1 if T else None), (1 if L else None)      # sizes only: the largest workspace
+        self.ws_bytes = max(fe_packed_workspace_size(a), fe_packed_workspace_size(a, True))
+        a.ctx_w = a.own_w = None
+        self.q_shape, self.heads = (B, K, S, n_heads, dh), (n_kv_heads, dh)
+        self.out = self.lse = None
+        self._layouts = _Layouts()
+
+    def allocate(self):
+        """Outputs and workspace on the current device and stream (done by the first `run` or `weigh`)."""
+        import torch
+        a, dev = self.args, torch.device("cuda", torch.cuda.current_device())
+        self.out = torch.empty(self.q_shape, dtype=self.act, device=dev)
+        self.lse = torch.empty(self.q_shape[:-1], dtype=torch.float32, device=dev)
+        self.ws = torch.empty(max(16, self.ws_bytes), dtype=torch.uint8, device=dev)
+        a.ws, a.ws_bytes = _ptr(self.ws), self.ws_bytes
+        a.out, a.out_ld = _ptr(self.out), a.n_heads * a.dh
+        self._kept = _Kept(self.out, self.lse, self.ws)
+
+    def _check(self, q, q_len):
+        import torch
+        _need(q_len, "q_len", torch.int32, self.B * self.K)
+        return _row_stride(q, "q", self.q_shape, self.act)
+
+    def _take(self, stream, q, ctx, own, q_len, *tensors):
+        a = self.args
+        a.q_ld = self._layouts.of(self._check, q, q_len)
+        for cache, name, n, capacity in ((ctx, "ctx", self.B, self.T), (own, "own", self.B * self.K, self.L)):
+            if (cache is None) != (capacity == 0):
+                raise ValueError(f"{name}: a cache and a capacity above 0 go together")
+            if cache is not None and ((cache.N, cache.capacity) != (n, capacity) or (cache.n_kv_heads, cache.dh) != self.heads):
+                raise ValueError(f"{name}: expected {n} sequences of {capacity} rows with {self.heads[0]} heads of {self.heads[1]}, got "
+                                 f"{cache.N} of {cache.capacity} with {cache.n_kv_heads} of {cache.dh}")
+        index = _on_device((q, q_len, *tensors, None if ctx is None else ctx.pages, None if own is None else own.pages))
+        if self.out is None:
+            self.allocate()
+        elif self.out.get_device() != index:
+            raise ValueError(f"the outputs are on {self.out.device}, the tensors on device {index}")
+        if ctx is not None:
+            a.ctx = ctx.cache
+        if own is not None:
+            a.own = own.cache
+        a.q, a.q_len = q.data_ptr(), _addr(q_len)
+        handle = _stream_on(index, stream)
+        for kept in (self, ctx, own):
+            if kept is not None:
+                kept._kept.use_on(handle)
+        return handle
+
+    def run(self, q, ctx: Optional[PagedCache4], own: Optional[PagedCache4], q_len=None, stream=None):
+        """Enqueue the attention; returns out [B][K][S][n_heads][dh] (self.lse holds the log sums)."""
+        handle = self._take(stream, q, ctx, own, q_len)
+        self.args.lse = self.lse.data_ptr()
+        fe_packed_attention(self.args, handle)
+        return self.out
+
+    def weigh(self, q, lse, ctx: Optional[PagedCache4], own: Optional[PagedCache4], ctx_w=None, own_w=None, q_len=None,
+              ctx_w_out=None, own_w_out=None, stream=None):
+        """Add the attention weight that every cached row received from the query rows (lse: `run`'s) to ctx_w
+        [B][n_kv_heads][T] and own_w [B * K][n_kv_heads][L] fp32 (either may be None), in place or into the outputs.
+        Returns the two tensors written."""
+        import torch
+        a, Hkv = self.args, self.heads[0]
+        ctx_w_out, own_w_out = (w if o is None else o for w, o in ((ctx_w, ctx_w_out), (own_w, own_w_out)))
+        for t, name, n in ((ctx_w, "ctx_w", self.B * self.T), (ctx_w_out, "ctx_w_out", self.B * self.T),
+                           (own_w, "own_w", self.B * self.K * self.L), (own_w_out, "own_w_out", self.B * self.K * self.L)):
+            _need(t, name, torch.float32, n * Hkv)
+        _need(lse, "lse", torch.float32, self.B * self.K * self.q_shape[2] * self.q_shape[3])
+        handle = self._take(stream, q, ctx, own, q_len, lse, ctx_w, own_w, ctx_w_out, own_w_out)
+        a.lse = lse.data_ptr()
+        a.ctx_w, a.own_w, a.ctx_w_out, a.own_w_out = _addr(ctx_w), _addr(own_w), _addr(ctx_w_out), _addr(own_w_out)
+        fe_packed_weights(a, handle)
+        return ctx_w_out, own_w_out
