@@ -43,7 +43,7 @@ extern "C" {
  * table entry outside [0, n_pages) names no page.  cols * page_rows is a sequence's capacity. */
 typedef struct {
   void* pages;                          /* 16-byte aligned */
-  int64_t page_ld;                      /* bytes from one page to the next: a multiple of 16, >= n_kv_heads * head_bytes */
+  int64_t page_ld;                      /* bytes from one page to the next: a multiple of 16, >= n_kv_heads * head_bytes, < 2^31 */
   const int32_t* table;                 /* [N][cols] */
   int32_t* len;                         /* [N] rows in the cache; written by fe_packed_evict's `to` alone */
   int32_t N, cols, page_rows, n_pages;

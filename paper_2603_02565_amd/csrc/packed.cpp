@@ -48,6 +48,7 @@ fe_status check_cache(const fe_packed_cache& c, int dh, int n_kv_heads, const ch
   if (!c.pages || !c.table || !c.len) return pfail(FE_EINVAL, "%s: pages, table or len is NULL", name);
   if (!aligned(c.pages, 16) || !aligned(c.table, 4) || !aligned(c.len, 4))
     return pfail(FE_EINVAL, "%s: pages must be 16-byte aligned, table and lengths 4-byte aligned", name);
+  if (c.page_ld > kInt32) return pfail(FE_EUNSUPPORTED, "%s: pages of more than %lld bytes", name, kInt32);
   if (c.page_ld % 16 || c.page_ld < n_kv_heads * head_bytes(c.page_rows, dh))
     return pfail(FE_EINVAL, "%s: a page stride of %lld bytes is shorter than the page or not a multiple of 16", name,
                  (long long)c.page_ld);
@@ -206,6 +207,8 @@ fe_status fe_packed_attention(const fe_packed_args* a, void* stream) {
   PackedArgs k = kernel_args(*a);
   k.tiles = p.tiles;
   k.splits = p.splits;
+  k.by_length = p.by_length;
+  k.own_chunks = p.own_chunks;
   if (p.part_bytes) {
     k.part_o = static_cast<float*>(a->ws);
     k.part_ml = k.part_o + (size_t)p.splits * a->B * a->K * a->S * a->n_heads * a->dh;

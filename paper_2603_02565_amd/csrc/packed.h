@@ -34,14 +34,17 @@ struct PackedArgs {
   int B, K, S, Hq, Hkv, G, R, causal, q_ld, out_ld;
   float scale;
   int tiles, splits;                     // row tiles per (request, key head); key ranges per tile
-  float *part_o, *part_ml;               // splits > 1: [splits][B K S Hq][dh] sums, [..][2] maximum and sum
+  // splits > 1: B * splits ranges in all; by_length: a request has as many of them as its share of the keys says, its own
+  // rows taken as own_chunks chunks of 64
+  int by_length, own_chunks;
+  float *part_o, *part_ml;               // splits > 1: [B * splits][K S Hq][dh] sums, [..][2] maximum and sum
   const float *ctx_w, *own_w;            // weights
   float *ctx_w_out, *own_w_out;
   int ctx_tiles, own_tiles, ctx_splits, own_splits;   // key tiles per sequence, row ranges per key tile
   float *part_ctx, *part_own;            // [splits][N][Hkv][cap]
 };
 
-struct PackedPlan { int waves, tiles, splits; size_t part_bytes; };   // waves: those that a chunk of keys is shared by
+struct PackedPlan { int waves, tiles, splits, by_length, own_chunks; size_t part_bytes; };   // waves: those that share a chunk
 PackedPlan packed_plan(const fe_packed_args& a);
 struct PackedWeighPlan { int ctx_tiles, own_tiles, ctx_splits, own_splits; size_t ctx_bytes, own_bytes; long long blocks, sum_blocks; };
 PackedWeighPlan packed_weigh_plan(const fe_packed_args& a);

@@ -1,6 +1,7 @@
 // Attention of a request's lists over rows held in 4 bits (fe_packed_attention), and the weight that every cached row
 // received (fe_packed_weights).
 #include <algorithm>
+#include <type_traits>
 
 #include "packed.h"
 
@@ -107,6 +108,26 @@ FE_DEV Row row_of(const PackedArgs& a, int b, int g, int r) {
   return w;
 }
 
+// The key ranges are numbered request after request: request b has `n` of them, from `first` on.  by_length (B <= 64): lane b
+// finds those of request b.  Every request has one; the others are shared out in proportion to the chunks of 64 keys,
+// rounded down, so they may leave a few unused.
+struct Ranges { int first, n; };
+FE_DEV Ranges ranges_of_lane(const PackedArgs& a) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < a.B ? (ctx_rows(a, lane) + 63) / 64 + a.own_chunks + 1 : 0;
+  int all = mine;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) all += __shfl_xor(all, x);
+  const int n = lane < a.B ? 1 + (int)((float)(a.B * (a.splits - 1)) * (float)mine / (float)all) : 0;
+  int end = n;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    const int before = __shfl_up(end, x);
+    if (lane >= x) end += before;
+  }
+  return {end - n, n};
+}
+
 // The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
 // their number; a list without query rows contributes none.  nb <= 128; 256 threads; ends with a barrier.
 FE_DEV void pack_own(const PackedArgs& a, int b, int k0, int nb, int* off) {
@@ -131,12 +152,14 @@ FE_DEV void pack_own(const PackedArgs& a, int b, int k0, int nb, int* off) {
 }
 
 // A tile of keys or values in LDS as bf16, rows of DH without padding, their units of 8 columns exchanged inside a row so that
-// 16 rows at one unit and 4 rows at 4 neighbouring units both fall on all 64 banks.
+// 16 rows at one unit, 4 rows at 4 neighbouring units, and what 16 neighbouring threads write at a time (a unit of each of
+// their blocks of 32 columns) all fall on all 64 banks.
 template <int DH> struct Tile {
-  static FE_DEV int swap(int row) {
-    if (DH == 128) return (row & 3) << 2 | (row >> 2 & 3);
-    if (DH == 64) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
-    return row >> 2 & 3;
+  static FE_DEV int swap(int row) {        // a bijection of the rows that share a unit's banks
+    const int r0 = row & 3, r1 = row >> 2 & 3;
+    if (DH == 128) return r0 << 2 | (r1 ^ r0);
+    if (DH == 64) return ((r0 & 2) << 1) | ((r1 & 2) ^ (r0 & 2)) | (r1 & 1);
+    return r1;
   }
   static FE_DEV int at(int row, int unit) { return row * DH + ((unit ^ swap(row)) << 3); }
   // Operand along rows: lane l is row base + l % 32, its elements columns 16 c + 8 (l / 32) + j (base a multiple of 32).
@@ -167,6 +190,14 @@ FE_DEV int fresh(int x) {                // keeps a lane's number in one registe
   asm volatile("" : "+v"(x));
   return x;
 }
+// The kernel's arguments, to be read again where they are used: what only the own rows need does not take registers from the
+// loop over the shared ones.
+typedef const __attribute__((address_space(4))) PackedArgs* ArgsAgain;
+FE_DEV ArgsAgain args_again() {
+  ArgsAgain p = (ArgsAgain)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
 FE_DEV void order() { asm volatile("" ::: "memory"); }   // LDS operations of one wave stay in order
 
 // ------------------------------------------------------------------------------------------
@@ -181,6 +212,7 @@ template <typename T, int DH, int WR, int UE> struct Shape {
   static constexpr int WK = 4 / WR, GT = 64 * WR, ROWS = 32 * WR, UPR = DH / UE;
   static constexpr int PER = 32 * UPR > GT ? 32 * UPR / GT : 1, KC = GT * PER / UPR;
   static constexpr int NBUF = WR > 1 ? 2 : 1, ND = DH / 16, NB = DH / 32;
+  static constexpr int NS = KC >= 64 && sizeof(T) == 2 ? 2 : 1;   // 32-key blocks at a time
 };
 constexpr int fwd_waves(int bytes, int dh, int wr) {
   return dh == 128 ? (bytes == 4 ? 1 : 2) : dh == 64 ? (bytes == 4 ? 2 : 3) : bytes == 4 ? 3 : 4;
@@ -193,8 +225,8 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   typedef typename F::Op Op;
   typedef Tile<DH> L;
   constexpr int WK = C::WK, GT = C::GT, ROWS = C::ROWS, UPR = C::UPR, PER = C::PER, KC = C::KC, NBUF = C::NBUF;
-  constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH;
-  static_assert(KC % 32 == 0 && 4 * 32 * DH * 4 - WR * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2, "the join fits the tiles");
+  constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH, NS = C::NS;
+  static_assert(KC % (32 * NS) == 0 && 4 * 32 * DH * 4 - WR * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2, "the join fits the tiles");
   __shared__ __attribute__((aligned(16))) bf16 s_kv[WK][NBUF][2][TILE];
   __shared__ int s_off[ROWS + 1], s_hi;
   // of a chunk (by its parity in the group): the last one with rows of no page, those rows; the last one with own values
@@ -207,15 +239,83 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   int id = xcd_tile(blockIdx.x, gridDim.x);
   const int t = id % a.tiles;
   id /= a.tiles;
-  const int z = id % a.splits;
-  id /= a.splits;
-  const int g = id % a.Hkv, b = id / a.Hkv;
+  const int g = id % a.Hkv, range = id / a.Hkv;
+  int b = range / a.splits, z = range % a.splits, splits = a.splits;
+  if (a.by_length) {                       // uniform
+    const Ranges mine = ranges_of_lane(a);
+    b = __popcll(__ballot(lane < a.B && mine.first + mine.n <= range));
+    if (b >= a.B) return;                  // left over
+    z = range - __builtin_amdgcn_readlane(mine.first, b);
+    splits = __builtin_amdgcn_readlane(mine.n, b);
+  }
   const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R), sg = a.S * a.G;
   const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
   for (int i = tid; i < WK * 2 * KC; i += 256) (&s_hole[0][0][0])[i] = -1;
   for (int i = tid; i < WK * 2 * KC * UPR; i += 256) (&s_odd[0][0][0])[i] = -1;
   if (tid < WK * 2) (&s_holes[0][0])[tid] = (&s_odds[0][0])[tid] = -1;
   if (tid == 0) s_hi = 0;
+
+  // This group's chunks: numbers q = grp + WK i of the range's share of the shared ones (from cb on) and, after these nc, of
+  // the own ones (from ob on).  A thread's units of a chunk: their pages are looked up a chunk before they are loaded.
+  const int nctx = ctx_rows(a, b), cctx = (nctx + KC - 1) / KC;
+  const int cb = (int)((long long)cctx * z / splits), nc = (int)((long long)cctx * (z + 1) / splits) - cb;
+  u32x4 kc[PER], vc[PER];
+  unsigned ks[PER], vs[PER];
+  int entry[PER], rest[PER], list[PER];    // rest: row inside the page, -1 past the rows
+  int page[PER], row_in[PER];              // of the next shared chunk
+  int gone = 0, hole = 0;                  // bit p: does not count; as its page is none
+  const int jump = a.ctx.cap ? packed_page(a.ctx, WK * KC) : 0, jump_rows = WK * KC - jump * a.ctx.page_rows;
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    list[p] = 0;
+    const int j = (cb + grp) * KC + (gt + p * GT) / UPR;
+    page[p] = a.ctx.cap ? packed_page(a.ctx, j) : 0;
+    row_in[p] = j - page[p] * a.ctx.page_rows;
+  }
+  const int32_t* ctx_table = a.ctx.cap ? a.ctx.table + (long long)b * a.ctx.cols : nullptr;
+  auto find_ctx = [&](int q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      rest[p] = -1;
+      if ((cb + q) * KC + (gt + p * GT) / UPR < nctx) {
+        rest[p] = row_in[p];
+        entry[p] = ctx_table[(unsigned)page[p]];
+      }
+      page[p] += jump;
+      row_in[p] += jump_rows;
+      if (row_in[p] >= a.ctx.page_rows) {
+        row_in[p] -= a.ctx.page_rows;
+        ++page[p];
+      }
+    }
+  };
+  auto load_from = [&](const auto& x) __attribute__((always_inline)) {
+    gone = hole = 0;
+    const unsigned all = (unsigned)x.page_rows * UPR;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const bool none = rest[p] >= 0 && (unsigned)entry[p] >= (unsigned)x.n_pages, skip = rest[p] < 0 || none;
+      gone |= skip << p;
+      hole |= none << p;
+      const unsigned u = (gt + p * GT) % UPR, at = (skip ? 0 : rest[p]) * UPR + u;   // what does not count reads row 0 of page 0
+      const char* head = x.pages + (unsigned long long)(skip ? 0u : (unsigned)entry[p]) * (unsigned)x.page_ld;
+      const unsigned k = (unsigned)g * x.head_bytes + at * (UE / 2), s = (unsigned)g * x.head_bytes + all * UE + (UE == 32 ? at : at >> 1);
+      if constexpr (UE == 32) {
+        kc[p] = ldv<u32x4>(head + k);
+        vc[p] = ldv<u32x4>(head + (k + all * (UE / 2)));
+      } else {
+        const uint2 kk = ldv<uint2>(head + k), vv = ldv<uint2>(head + (k + all * (UE / 2)));
+        kc[p] = u32x4{kk.x, kk.y, 0, 0};
+        vc[p] = u32x4{vv.x, vv.y, 0, 0};
+      }
+      ks[p] = *reinterpret_cast<const unsigned char*>(head + s);
+      vs[p] = *reinterpret_cast<const unsigned char*>(head + (s + (UE == 32 ? all : all >> 1)));
+    }
+  };
+  if (grp < nc) {                          // under way while the lists' lengths and packing are found
+    find_ctx(grp);
+    load_from(a.ctx);
+  }
 
   // this wave's rows
   const Row row = row_of(a, b, g, r0 + wr * 32 + c32);
@@ -239,10 +339,8 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   ahi = wlo == alo ? __builtin_amdgcn_readfirstlane(ahi) : -1;
   if (lane == 0 && grp == 0) atomicMax(&s_hi, whi);
   __syncthreads();
-
-  const int nctx = ctx_rows(a, b), nown = __builtin_amdgcn_readfirstlane(s_hi);
-  const int cctx = (nctx + KC - 1) / KC, call = cctx + (nown + KC - 1) / KC;
-  const int zb = (int)((long long)call * z / a.splits), ze = (int)((long long)call * (z + 1) / a.splits);
+  const int nown = __builtin_amdgcn_readfirstlane(s_hi), cown = (nown + KC - 1) / KC;
+  const int ob = (int)((long long)cown * z / splits), nq = nc + (int)((long long)cown * (z + 1) / splits) - ob;
 
   Op qf[ND];
 #pragma unroll
@@ -257,190 +355,162 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
 #pragma unroll
   for (int n = 0; n < NB; ++n) o[n] = f32x16{};
 
-  // This thread's units of a chunk.  Their pages are looked up a chunk before they are loaded.
-  unsigned kc[PER][UE / 8], vc[PER][UE / 8], ks[PER], vs[PER];
-  int entry[PER], rest[PER], list[PER];    // rest: row inside the page, -1 past the rows
-  int gone = 0, hole = 0;                  // bit p: does not count; as its page is none
-#pragma unroll
-  for (int p = 0; p < PER; ++p) list[p] = 0;
-  auto find = [&](int c) __attribute__((always_inline)) {
-    if (c >= ze) return;                   // uniform
+  auto find_own = [&](int q) __attribute__((always_inline)) {
+    const ArgsAgain A = args_again();
+    const unsigned rows = A->own.page_rows;
+    const int32_t* table = A->own.table + ((long long)b * A->K + k0) * A->own.cols;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-      const int key = (gt + p * GT) / UPR;
+      const int x = (ob + q - nc) * KC + (gt + p * GT) / UPR;
       rest[p] = -1;
-      if (c < cctx) {                      // uniform
-        const int j = c * KC + key;
-        if (j < nctx) {
-          const int pg = packed_page(a.ctx, j);
-          rest[p] = j - pg * a.ctx.page_rows;
-          entry[p] = a.ctx.table[(long long)b * a.ctx.cols + pg];
-        }
-      } else {
-        const int x = (c - cctx) * KC + key;
-        if (x < nown) {
-          int i = list[p];
-          while (s_off[i + 1] <= x) ++i;
-          list[p] = i;
-          const int j = x - s_off[i], pg = packed_page(a.own, j);
-          rest[p] = j - pg * a.own.page_rows;
-          entry[p] = a.own.table[((long long)b * a.K + k0 + i) * a.own.cols + pg];
-        }
+      if (x < nown) {
+        int i = list[p];
+        while (s_off[i + 1] <= x) ++i;
+        list[p] = i;
+        const int j = x - s_off[i], pg = (int)((unsigned long long)(unsigned)j * A->own.magic >> A->own.shift);
+        rest[p] = j - pg * rows;
+        entry[p] = table[(long long)i * A->own.cols + pg];
       }
     }
   };
-  auto load = [&](int c) __attribute__((always_inline)) {
-    if (c >= ze) return;                   // uniform
-    const PackedCache& x = c < cctx ? a.ctx : a.own;
-    gone = hole = 0;
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const bool none = rest[p] >= 0 && (entry[p] < 0 || entry[p] >= x.n_pages), skip = rest[p] < 0 || none;
-      gone |= skip << p;
-      hole |= none << p;
-      const int u = (gt + p * GT) % UPR, at = (skip ? 0 : rest[p]) * UPR + u;   // what does not count reads row 0 of page 0
-      const char* head = x.pages + (skip ? 0 : entry[p]) * x.page_ld + (long long)g * x.head_bytes;
-      const long long all = (long long)x.page_rows * UPR;
-      const char* k = head + (long long)at * (UE / 2);
-      const char* v = k + all * (UE / 2);
-      const unsigned char* s = reinterpret_cast<const unsigned char*>(head + all * UE) + (UE == 32 ? at : at >> 1);
-      if constexpr (UE == 32) {
-        const u32x4 kk = ldv<u32x4>(k), vv = ldv<u32x4>(v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kc[p][i] = kk[i], vc[p][i] = vv[i];
-      } else {
-        const uint2 kk = ldv<uint2>(k), vv = ldv<uint2>(v);
-        kc[p][0] = kk.x, kc[p][1] = kk.y, vc[p][0] = vv.x, vc[p][1] = vv.y;
-      }
-      ks[p] = s[0];
-      vs[p] = s[UE == 32 ? all : all >> 1];
-    }
+  auto find = [&](int q) __attribute__((always_inline)) {
+    if (q < nc) find_ctx(q);               // uniform
+    else if (q < nq) find_own(q);
   };
-  // The units of a quad of lanes lie in one row: every lane starts with another one, so that the writes meet all banks.
-  const int key_of_thread = gt / UPR;
-  const int turn = DH == 128 ? key_of_thread & (UE == 32 ? 3 : 1) : DH == 64 ? (key_of_thread >> 1 & 1) << (UE == 32) : 0;
-  auto stage = [&](bf16* K, bf16* V, int c, int par) __attribute__((always_inline)) {
+  auto load = [&](int q) __attribute__((always_inline)) {
+    if (q < nc) load_from(a.ctx);          // uniform
+    else if (q < nq) load_from(args_again()->own);
+  };
+  auto stage = [&](bf16* K, bf16* V, int q, int par) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int key = (gt + p * GT) / UPR, u = (gt + p * GT) % UPR;
-      unsigned kk[UE / 8], vv[UE / 8];
-#pragma unroll
-      for (int i = 0; i < UE / 8; ++i) kk[i] = kc[p][i], vv[i] = vc[p][i];
       float ku = unit_of(ks[p]), vu = unit_of(vs[p]);
       if (gone >> p & 1) {
-#pragma unroll
-        for (int i = 0; i < UE / 8; ++i) kk[i] = vv[i] = 0;
+        kc[p] = vc[p] = u32x4{0, 0, 0, 0};
         ku = vu = 1.f;
-        if (hole >> p & 1) s_hole[grp][par][key] = s_holes[grp][par] = c;
-      } else if (c >= cctx && vs[p] == 255) {
+        if (hole >> p & 1) s_hole[grp][par][key] = s_holes[grp][par] = q;
+      } else if (q >= nc && vs[p] == 255) {
         // NaN would reach the rows of other lists, as 0 times NaN: they get zeros, the rows that see it get it at the end
-#pragma unroll
-        for (int i = 0; i < UE / 8; ++i) vv[i] = 0;
+        vc[p] = u32x4{0, 0, 0, 0};
         vu = 1.f;
-        s_odd[grp][par][key * UPR + u] = s_odds[grp][par] = c;
+        s_odd[grp][par][key * UPR + u] = s_odds[grp][par] = q;
       }
-      auto exchange = [&](unsigned (&w)[UE / 8]) __attribute__((always_inline)) {
-        if (UE / 8 >= 2 && DH > 32) {
-          if (turn & 1) {
-#pragma unroll
-            for (int i = 0; i < UE / 8; i += 2) { const unsigned y = w[i]; w[i] = w[i + 1]; w[i + 1] = y; }
-          }
-          if (UE == 32 && (turn & 2)) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) { const unsigned y = w[i]; w[i] = w[(i + 2) % (UE / 8)]; w[(i + 2) % (UE / 8)] = y; }
-          }
-        }
-      };
-      exchange(kk);
-      exchange(vv);
+      const int base = L::at(key, u * (UE / 8));
 #pragma unroll
       for (int i = 0; i < UE / 8; ++i) {
-        const int at = L::at(key, u * (UE / 8) + (i ^ turn));
-        *reinterpret_cast<bf16x8*>(K + at) = values8(kk[i], ku);
-        *reinterpret_cast<bf16x8*>(V + at) = values8(vv[i], vu);
+        *reinterpret_cast<bf16x8*>(K + (base ^ i << 3)) = values8(kc[p][i], ku);
+        *reinterpret_cast<bf16x8*>(V + (base ^ i << 3)) = values8(vc[p][i], vu);
       }
     }
   };
 
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
-  const bool idle = r0 + wr * 32 >= a.R;
-  find(zb + grp);
-  load(zb + grp);
-  find(zb + grp + WK);
-  const int trips = (ze - zb + WK - 1) / WK;
-  for (int it = 0; it < trips; ++it) {
-    const int c = zb + grp + it * WK, par = it & 1;
-    bf16 *K = s_kv[grp][it % NBUF][0], *V = s_kv[grp][it % NBUF][1];
-    if (c < ze) stage(K, V, c, par);
-    load(c + WK);
-    find(c + 2 * WK);
-    if constexpr (WR > 1) lds_barrier();   // also the end of every wave's reads of the buffer written next
-    else order();
-    if (c >= ze || idle) continue;         // uniform
-    rl = fresh(rl);
-    cl = fresh(cl);
-    const bool own = c >= cctx;
-    const bool holes = __builtin_amdgcn_readfirstlane(s_holes[grp][par]) == c;
-    const bool odds = __builtin_amdgcn_readfirstlane(s_odds[grp][par]) == c;
-#pragma unroll 1
-    for (int kb = 0; kb < KC; kb += 32) {
-      const int x0 = (own ? c - cctx : c) * KC + kb;     // first key: of the shared rows, or packed
-      if (own ? x0 >= whi : x0 >= nctx) break;           // uniform
-      if (own && x0 + 32 <= wlo) continue;
-      f32x16 s{};
+  // N 32-key blocks from row kb of the tiles on; element i of a lane is key 8 (i / 4) + 4 half + i % 4 of a block.  Products of
+  // all blocks first, one branch for the reference, then probabilities and products with the values: the chains overlap.
+  // mask(s) sets what the rows do not see to -infinity.
+  auto blocks = [&](auto count, const bf16* K, const bf16* V, int kb, auto mask) __attribute__((always_inline)) {
+    constexpr int N = decltype(count)::value;
+    f32x16 s[N];
 #pragma unroll
-      for (int d = 0; d < ND; ++d) s = mma_held(L::rows(K, kb, d, rl), qf[d], s);
-      // element i of a lane is key 8 (i / 4) + 4 half + i % 4 of the step
-      if (own ? x0 < alo || x0 + 32 > ahi : x0 + 32 > nctx) {   // uniform
-        const int from = (own ? lo : 0) - x0 - 4 * half, to = (own ? hi : nctx) - x0 - 4 * half;
+    for (int u = 0; u < N; ++u) s[u] = f32x16{};
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (8 * (i >> 2) + (i & 3) < from || 8 * (i >> 2) + (i & 3) >= to) s[i] = -INFINITY;
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int u = 0; u < N; ++u) s[u] = mma_held(L::rows(K, kb + 32 * u, d, rl), qf[d], s[u]);
+    mask(s);
+    float mx = m_run;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[u][i]), s[u][i + 1]);
+    // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
+    if (__any(mx > m_run + lag)) {
+      const float top = halves_max(mx);
+      if (top > m_run + lag) {
+        const float alpha = __builtin_amdgcn_exp2f((m_run - top) * sl2);
+        m_run = top;
+        l_run *= alpha;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n] *= alpha;
       }
-      if (holes) {                         // uniform
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (s_hole[grp][par][kb + 8 * (i >> 2) + 4 * half + (i & 3)] == c) s[i] = -INFINITY;
-      }
-      float mx = m_run;
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
-      // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
-      if (__any(mx > m_run + lag)) {
-        const float top = halves_max(mx);
-        if (top > m_run + lag) {
-          const float alpha = __builtin_amdgcn_exp2f((m_run - top) * sl2);
-          m_run = top;
-          l_run *= alpha;
-#pragma unroll
-          for (int n = 0; n < NB; ++n) o[n] *= alpha;
-        }
-      }
-      const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
+    for (int u = 0; u < N; ++u) {
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -ref));
-        sum[i & 3] += s[i];
+        s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], sl2, -ref));
+        sum[i & 3] += s[u][i];
       }
       l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         f32x8 w;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = s[8 * m + j];
+        for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
         const Op p = F::rounded(w);
 #pragma unroll
-        for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 16 * m, n, cl), p, o[n]);
+        for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 32 * u + 16 * m, n, cl), p, o[n]);
       }
-      if (odds) {                          // uniform: the columns of a NaN block, in the rows that see its key
+    }
+  };
+  const bool idle = r0 + wr * 32 >= a.R;
+  if (grp >= nc) {                         // uniform: no shared chunk was under way
+    find(grp);
+    load(grp);
+  }
+  find(grp + WK);
+  const int trips = (nq + WK - 1) / WK;
+  for (int it = 0; it < trips; ++it) {
+    const int q = grp + it * WK, par = it & 1;
+    bf16 *K = s_kv[grp][it % NBUF][0], *V = s_kv[grp][it % NBUF][1];
+    if (q < nq) stage(K, V, q, par);
+    load(q + WK);
+    find(q + 2 * WK);
+    if constexpr (WR > 1) lds_barrier();   // also the end of every wave's reads of the buffer written next
+    else order();
+    if (q >= nq || idle) continue;         // uniform
+    rl = fresh(rl);
+    cl = fresh(cl);
+    const bool own = q >= nc;
+    const bool any_hole = __builtin_amdgcn_readfirstlane(s_holes[grp][par]) == q;
+    const int x1 = own ? (ob + q - nc) * KC : (cb + q) * KC;   // first key: packed own rows, or shared ones
+    if (!own && !any_hole && x1 + KC <= nctx) {          // uniform: every row sees every key
 #pragma unroll 1
-        for (int e = 0; e < 32 * UPR; ++e) {
-          const int x = x0 + e / UPR, n = e % UPR * UE / 32;
-          if (__builtin_amdgcn_readfirstlane(s_odd[grp][par][kb * UPR + e]) != c || x < lo || x >= hi) continue;
+      for (int kb = 0; kb < KC; kb += 32 * NS)
+        blocks(std::integral_constant<int, NS>{}, K, V, kb, [](f32x16 (&)[NS]) {});
+    } else {
+      const bool odds = __builtin_amdgcn_readfirstlane(s_odds[grp][par]) == q;
+      const int first = own ? wlo : 0, end = own ? whi : nctx, all_from = own ? alo : 0, all_to = own ? ahi : nctx;
+#pragma unroll 1
+      for (int kb = 0; kb < KC; kb += 32) {
+        const int x0 = x1 + kb;
+        if (x0 >= end) break;              // uniform
+        if (x0 + 32 <= first) continue;
+        blocks(std::integral_constant<int, 1>{}, K, V, kb, [&](f32x16 (&s)[1]) __attribute__((always_inline)) {
+          if (x0 < all_from || x0 + 32 > all_to) {       // uniform
+            const int from = (own ? lo : 0) - x0 - 4 * half, to = (own ? hi : nctx) - x0 - 4 * half;
 #pragma unroll
-          for (int q = 0; q < NB; ++q)
-            if (q == n) o[q] += f32x16{} + NAN;
+            for (int i = 0; i < 16; ++i)
+              if (8 * (i >> 2) + (i & 3) < from || 8 * (i >> 2) + (i & 3) >= to) s[0][i] = -INFINITY;
+          }
+          if (any_hole) {                  // uniform
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (s_hole[grp][par][kb + 8 * (i >> 2) + 4 * half + (i & 3)] == q) s[0][i] = -INFINITY;
+          }
+        });
+        if (odds) {                        // uniform: the columns of a NaN block, in the rows that see its key
+#pragma unroll 1
+          for (int e = 0; e < 32 * UPR; ++e) {
+            const int x = x0 + e / UPR, n = e % UPR * UE / 32;
+            if (__builtin_amdgcn_readfirstlane(s_odd[grp][par][kb * UPR + e]) != q || x < lo || x >= hi) continue;
+#pragma unroll
+            for (int y = 0; y < NB; ++y)
+              if (y == n) o[y] += f32x16{} + NAN;
+          }
         }
       }
     }
@@ -495,7 +565,7 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   const float m2 = m_run * sl2;
   const long long ro = row.at * a.Hq + row.h;
   if (a.splits > 1) {
-    const long long at = (long long)z * a.B * a.K * a.S * a.Hq + ro;
+    const long long at = ro + (long long)(range - b) * a.K * a.S * a.Hq;   // [range][row of the request]
     float* po = a.part_o + at * DH;
 #pragma unroll
     for (int n = 0; n < NB; ++n)
@@ -528,20 +598,28 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
 // Joins the key ranges of a row in ascending order: DH / 4 threads a row.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
-  const long long rows = (long long)a.B * a.K * a.S * a.Hq;
+  const long long per = (long long)a.K * a.S * a.Hq, rows = a.B * per;
   const long long e = (long long)blockIdx.x * 256 + threadIdx.x, ro = e / (DH / 4);
   const int d0 = (int)(e % (DH / 4)) * 4;
+  const int b = (int)(min(ro, rows - 1) / per);
+  int first = b * a.splits, splits = a.splits;
+  if (a.by_length) {                       // uniform
+    const Ranges mine = ranges_of_lane(a);
+    first = __shfl(mine.first, b);
+    splits = __shfl(mine.n, b);
+  }
   if (ro >= rows) return;
+  const long long at0 = (first - b) * per + ro;
   float top = -INFINITY;
-  for (int z = 0; z < a.splits; ++z) top = fmaxf(top, a.part_ml[(z * rows + ro) * 2]);
+  for (int z = 0; z < splits; ++z) top = fmaxf(top, a.part_ml[(z * per + at0) * 2]);
   const float ref = top == -INFINITY ? 0.f : top;
   float l = 0.f;
   f32x4 o{};
 #pragma unroll 4
-  for (int z = 0; z < a.splits; ++z) {
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[(z * rows + ro) * 2] - ref);
-    const f32x4 v = ldv<f32x4>(a.part_o + (z * rows + ro) * DH + d0);
-    l = fmaf(a.part_ml[(z * rows + ro) * 2 + 1], f, l);
+  for (int z = 0; z < splits; ++z) {
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[(z * per + at0) * 2] - ref);
+    const f32x4 v = ldv<f32x4>(a.part_o + (z * per + at0) * DH + d0);
+    l = fmaf(a.part_ml[(z * per + at0) * 2 + 1], f, l);
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
   }
@@ -731,13 +809,15 @@ PackedPlan packed_plan(const fe_packed_args& a) {
   p.tiles = (int)((R + rows - 1) / rows);
   const long long T = a.ctx.N > 0 ? (long long)a.ctx.cols * a.ctx.page_rows : 0;
   const long long L = a.own.N > 0 ? (long long)a.own.cols * a.own.page_rows : 0;
-  const long long keys = T + std::min<long long>(a.K, (rows - 1) / sg + 2) * L, wgs = bg * p.tiles;
-  const long long items = (keys + 63) / 64;
+  const long long own = std::min<long long>(a.K, (rows - 1) / sg + 2) * L, wgs = bg * p.tiles;
+  const long long items = (T + 63) / 64 + (own + 63) / 64;
   long long want = (512 + wgs - 1) / wgs;                       // two workgroups a compute unit
   want = std::min(want, std::max(1LL, items / 4));
   if (a.dtype == FE_F32) want = std::max(want, (items + 31) / 32);   // fp32 sums over at most 2048 keys
   const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);
   p.splits = (int)std::max(1LL, std::min({want, 256LL, grid}));
+  p.by_length = a.dtype == FE_BF16 && p.splits >= 8 && a.B > 1 && a.B <= 64 && T >= 1024 * p.splits;
+  p.own_chunks = (int)((own + 63) / 64 / 2);                    // lists half full
   const size_t out_rows = (size_t)a.B * a.K * a.S * a.n_heads;
   p.part_bytes = p.splits > 1 ? p.splits * out_rows * (a.dh + 2) * sizeof(float) : 0;
   return p;
@@ -766,8 +846,8 @@ PackedWeighPlan packed_weigh_plan(const fe_packed_args& a) {
 }
 
 hipError_t launch_packed_attention(const PackedArgs& a, int dh, bool bf16_rows, const PackedPlan& p, hipStream_t s) {
-  if (bf16_rows) return dh == 32 ? fwd<bf16, 32, 32>(a, p, s) : dh == 64 ? fwd<bf16, 64, 32>(a, p, s) : fwd<bf16, 128, 32>(a, p, s);
-  return dh == 32 ? fwd<float, 32, 32>(a, p, s) : dh == 64 ? fwd<float, 64, 32>(a, p, s) : fwd<float, 128, 32>(a, p, s);
+  if (bf16_rows) return dh == 32 ? fwd<bf16, 32, 16>(a, p, s) : dh == 64 ? fwd<bf16, 64, 16>(a, p, s) : fwd<bf16, 128, 32>(a, p, s);
+  return dh == 32 ? fwd<float, 32, 16>(a, p, s) : dh == 64 ? fwd<float, 64, 16>(a, p, s) : fwd<float, 128, 32>(a, p, s);
 }
 
 hipError_t launch_packed_weights(const PackedArgs& a, int dh, bool bf16_rows, hipStream_t s) {

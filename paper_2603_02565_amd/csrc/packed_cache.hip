@@ -247,13 +247,112 @@ FE_DEV unsigned order_of(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+// What a sequence's first head writes for it: its length in `to`, whether rows in use have no page.  Uniform over NW waves.
+template <int NW>
+FE_DEV void evict_state(const fe_packed_evict_args& a, const PackedCache& from, const PackedCache& to, int s, int n, int m) {
+  const int tid = threadIdx.x;
+  if (tid == 0) const_cast<int32_t*>(to.len)[s] = m;
+  if (!a.status) return;
+  int bad = 0;
+  if (n > 0)
+    for (int p = tid; p <= packed_page(from, n - 1); p += NW * 64) {
+      const int page = from.table[(long long)s * from.cols + p];
+      bad |= page < 0 || page >= from.n_pages;
+    }
+  if (m > 0)
+    for (int p = tid; p <= packed_page(to, m - 1); p += NW * 64) {
+      const int page = to.table[(long long)s * to.cols + p];
+      bad |= page < 0 || page >= to.n_pages;
+    }
+  bad = block_any<NW>(bad);
+  if (tid == 0) a.status[s] = bad ? FE_DEV_BAD_PAGE : 0;
+}
+
+// Block x of kept row i of (sequence, head), row j of `from`: its keys and its values.
+FE_DEV void move_block(const PackedCache& from, const PackedCache& to, int s, int h, int log_blocks, int i, int j, int x) {
+  const int p = packed_page(from, j), t = packed_page(to, i);
+  const int page = from.table[(long long)s * from.cols + p], to_page = to.table[(long long)s * to.cols + t];
+  if (page < 0 || page >= from.n_pages || to_page < 0 || to_page >= to.n_pages) return;
+  const char* src = from.pages + page * from.page_ld + (long long)h * from.head_bytes;
+  char* dst = to.pages + to_page * to.page_ld + (long long)h * to.head_bytes;
+  const long long b = ((long long)(j - p * from.page_rows) << log_blocks) + x, d = ((long long)(i - t * to.page_rows) << log_blocks) + x;
+  const long long sn = (long long)from.page_rows << log_blocks, dn = (long long)to.page_rows << log_blocks;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(src + 16 * b), v = *reinterpret_cast<const u32x4*>(src + 16 * (sn + b));
+  const char ks = src[32 * sn + b], vs = src[33 * sn + b];
+  *reinterpret_cast<u32x4*>(dst + 16 * d) = k;
+  *reinterpret_cast<u32x4*>(dst + 16 * (dn + d)) = v;
+  dst[32 * dn + d] = ks;
+  dst[33 * dn + d] = vs;
+}
+
+// Short sequences (64 E rows at most): one wave selects, all four move.  The m-th greatest order is found bit by bit: a ballot
+// counts the candidates at or above a trial.
+template <int E>
+__global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args a, PackedCache from, PackedCache to) {
+  __shared__ int s_kept[64 * E];
+  const int tid = threadIdx.x, lane = tid & 63, s = blockIdx.x / a.n_kv_heads, h = blockIdx.x % a.n_kv_heads;
+  const int n = packed_len(from, s), m = min(a.keep, n);
+  const int first = min(a.first, m), recent = min(a.recent, m - first), lo = first, hi = n - recent;
+  int32_t* kept = a.kept + (long long)blockIdx.x * a.keep;
+  if (h == 0) evict_state<4>(a, from, to, s, n, m);
+  for (int i = m + tid; i < a.keep; i += 256) kept[i] = -1;
+  if (tid < 64) {
+    const float* w = a.weight + (long long)blockIdx.x * from.cap;
+    float v[E];
+    unsigned o[E];                         // 0: a NaN, or no candidate
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = e * 64 + lane < n ? w[e * 64 + lane] : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = e * 64 + lane >= lo && e * 64 + lane < hi ? order_of(v[e]) : 0;
+    int left = m - first - recent;
+    unsigned cut = 0xffffffffu;            // no order is as great
+    const bool all = m == n;
+    if (!all && left > 0) {
+      cut = 0;
+      for (int bit = 31; bit >= 0; --bit) {
+        const unsigned trial = cut | 1u << bit;
+        int c = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) c += __popcll(__ballot(o[e] >= trial));
+        if (c >= left) cut = trial;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) left -= __popcll(__ballot(o[e] > cut));
+    }
+    const unsigned long long below = (1ull << lane) - 1;
+    float* out = a.weight_out ? a.weight_out + (long long)blockIdx.x * to.cap : nullptr;
+    int at = 0, equal = 0;                 // kept, and candidates equal to the cut, so far: the first `left` of these are kept
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = e * 64 + lane;
+      const bool inside = i >= lo && i < hi, same = !all && inside && o[e] == cut;
+      const unsigned long long eq = __ballot(same);
+      const bool take = i < n && (all || !inside || o[e] > cut || (same && equal + __popcll(eq & below) < left));
+      const unsigned long long got = __ballot(take);
+      if (take) {
+        const int d = at + __popcll(got & below);
+        s_kept[d] = i;
+        kept[d] = i;
+        if (out) out[d] = v[e];
+      }
+      at += __popcll(got);
+      equal += __popcll(eq);
+    }
+  }
+  __syncthreads();
+  const int log_blocks = a.dh == 32 ? 0 : a.dh == 64 ? 1 : 2;
+#pragma unroll 2
+  for (int e = tid; e < m << log_blocks; e += 256)
+    move_block(from, to, s, h, log_blocks, e >> log_blocks, s_kept[e >> log_blocks], e & ((1 << log_blocks) - 1));
+}
+
 // Selects a (sequence, key head)'s rows.  Four passes over 8 bits each find the m-th greatest order among the candidates:
 // a histogram in LDS, in 32 copies by lane so that equal digits, the rule among weights, do not meet in one word.  Then
 // every wave walks its rows in order and numbers what is kept.  Rows (NW * 64 * E a segment) stay in registers
 // where one segment holds the sequence.
-template <int NW, int E>
-__global__ __launch_bounds__(NW * 64) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
-  constexpr int NT = NW * 64, SEG = NT * E;
+template <int E>
+__global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
+  constexpr int NW = 16, NT = NW * 64, SEG = NT * E;
   __shared__ int s_hist[256 * 32];
   __shared__ int s_sum[256], s_kept[NW + 1], s_equal[NW + 1], s_digit, s_left;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -265,24 +364,7 @@ __global__ __launch_bounds__(NW * 64) void k_packed_select(fe_packed_evict_args 
   int32_t* kept = a.kept + (long long)blockIdx.x * a.keep;
   float* out = a.weight_out ? a.weight_out + (long long)blockIdx.x * to.cap : nullptr;
 
-  if (h == 0) {
-    if (tid == 0) const_cast<int32_t*>(to.len)[s] = m;
-    if (a.status) {                        // uniform
-      int bad = 0;
-      if (n > 0)
-        for (int p = tid; p <= packed_page(from, n - 1); p += NT) {
-          const int page = from.table[(long long)s * from.cols + p];
-          bad |= page < 0 || page >= from.n_pages;
-        }
-      if (m > 0)
-        for (int p = tid; p <= packed_page(to, m - 1); p += NT) {
-          const int page = to.table[(long long)s * to.cols + p];
-          bad |= page < 0 || page >= to.n_pages;
-        }
-      bad = block_any<NW>(bad);
-      if (tid == 0) a.status[s] = bad ? FE_DEV_BAD_PAGE : 0;
-    }
-  }
+  if (h == 0) evict_state<NW>(a, from, to, s, n, m);
   for (int i = m + tid; i < a.keep; i += NT) kept[i] = -1;
 
   float v[E];
@@ -313,12 +395,14 @@ __global__ __launch_bounds__(NW * 64) void k_packed_select(fe_packed_evict_args 
         }
       }
       __syncthreads();
-      for (int b = wave; b < 256; b += 2 * NW) {   // two digits a wave at a time
-        const int bin = b + (lane >> 5) * NW;
-        int c = s_hist[bin * 32 + (lane & 31)];
+      {                                    // four threads a digit, each from another bank
+        const int bin = tid >> 2, at = bin * 32 + (tid & 3) * 8;
+        int c = 0;
 #pragma unroll
-        for (int x = 1; x < 32; x *= 2) c += __shfl_xor(c, x);
-        if ((lane & 31) == 0) s_sum[bin] = c;
+        for (int i = 0; i < 8; ++i) c += s_hist[at + ((i + (bin >> 1)) & 7)];
+        c += __builtin_amdgcn_update_dpp(0, c, 0xb1, 0xf, 0xf, true);
+        c += __builtin_amdgcn_update_dpp(0, c, 0x4e, 0xf, 0xf, true);
+        if ((tid & 3) == 0) s_sum[bin] = c;
       }
       __syncthreads();
       if (wave == 0) {                     // digits from the greatest: lane l has 255 - 4 l and the three below
@@ -404,21 +488,7 @@ __global__ __launch_bounds__(256) void k_packed_move(fe_packed_evict_args a, Pac
   const int log_blocks = a.dh == 32 ? 0 : a.dh == 64 ? 1 : 2;
   const int m = min(a.keep, packed_len(from, s));
   const int e = blk * 256 + threadIdx.x, i = e >> log_blocks, x = e & ((1 << log_blocks) - 1);
-  if (i >= m) return;
-  const int j = a.kept[(long long)sh * a.keep + i];
-  const int p = packed_page(from, j), t = packed_page(to, i);
-  const int page = from.table[(long long)s * from.cols + p], to_page = to.table[(long long)s * to.cols + t];
-  if (page < 0 || page >= from.n_pages || to_page < 0 || to_page >= to.n_pages) return;
-  const char* src = from.pages + page * from.page_ld + (long long)h * from.head_bytes;
-  char* dst = to.pages + to_page * to.page_ld + (long long)h * to.head_bytes;
-  const long long b = ((long long)(j - p * from.page_rows) << log_blocks) + x, d = ((long long)(i - t * to.page_rows) << log_blocks) + x;
-  const long long sn = (long long)from.page_rows << log_blocks, dn = (long long)to.page_rows << log_blocks;
-  const u32x4 k = *reinterpret_cast<const u32x4*>(src + 16 * b), v = *reinterpret_cast<const u32x4*>(src + 16 * (sn + b));
-  const char ks = src[32 * sn + b], vs = src[33 * sn + b];
-  *reinterpret_cast<u32x4*>(dst + 16 * d) = k;
-  *reinterpret_cast<u32x4*>(dst + 16 * (dn + d)) = v;
-  dst[32 * dn + d] = ks;
-  dst[33 * dn + d] = vs;
+  if (i < m) move_block(from, to, s, h, log_blocks, i, a.kept[(long long)sh * a.keep + i], x);
 }
 
 }  // namespace
@@ -478,13 +548,20 @@ hipError_t launch_packed_read(const fe_packed_read_args& a, hipStream_t s) {
 hipError_t launch_packed_evict(const fe_packed_evict_args& a, hipStream_t s) {
   const PackedCache from = packed_cache(a.from, a.dh), to = packed_cache(a.to, a.dh);
   const unsigned heads = (unsigned)a.from.N * a.n_kv_heads;
-  if (from.cap <= 1024)
-    hipLaunchKernelGGL((k_packed_select<4, 4>), dim3(heads), dim3(256), 0, s, a, from, to);
-  else if (from.cap <= 8192)
-    hipLaunchKernelGGL((k_packed_select<16, 8>), dim3(heads), dim3(1024), 0, s, a, from, to);
+  if (from.cap <= 1024) {
+    if (from.cap <= 64)
+      hipLaunchKernelGGL(k_packed_evict_short<1>, dim3(heads), dim3(256), 0, s, a, from, to);
+    else if (from.cap <= 256)
+      hipLaunchKernelGGL(k_packed_evict_short<4>, dim3(heads), dim3(256), 0, s, a, from, to);
+    else
+      hipLaunchKernelGGL(k_packed_evict_short<16>, dim3(heads), dim3(256), 0, s, a, from, to);
+    return hipGetLastError();
+  }
+  if (from.cap <= 8192)
+    hipLaunchKernelGGL(k_packed_select<8>, dim3(heads), dim3(1024), 0, s, a, from, to);
   else
-    hipLaunchKernelGGL((k_packed_select<16, 32>), dim3(heads), dim3(1024), 0, s, a, from, to);
-  hipError_t e = hipGetLastError();
+    hipLaunchKernelGGL(k_packed_select<32>, dim3(heads), dim3(1024), 0, s, a, from, to);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int blocks = (int)(((long long)std::min(a.keep, from.cap) * (a.dh / 32) + 255) / 256);
   hipLaunchKernelGGL(k_packed_move, dim3((unsigned)((long long)heads * blocks)), dim3(256), 0, s, a, from, to, blocks);
