@@ -109,6 +109,8 @@ PackedArgs kernel_args(const fe_packed_args& a) {
   k.B = a.B; k.K = a.K; k.S = a.S; k.Hq = a.n_heads; k.Hkv = a.n_kv_heads;
   k.G = a.n_heads / a.n_kv_heads;
   k.R = a.K * a.S * k.G;
+  k.by_sg = divisor((long long)a.S * k.G);
+  k.by_g = divisor(k.G);
   k.causal = a.causal != 0;
   k.q_ld = a.q_ld; k.out_ld = a.out_ld; k.scale = a.scale;
   k.ctx_w = a.ctx_w; k.own_w = a.own_w; k.ctx_w_out = a.ctx_w_out; k.own_w_out = a.own_w_out;

@@ -6,21 +6,26 @@
 
 constexpr int kPackedMaxRows = 1 << 22;  // a sequence's capacity
 
-// A cache as the kernels see it.  Row j's page is the quotient j / page_rows, by a multiplication: j magic >> shift, exact for
-// j < 2^31.
+// Division by a number that a launch does not change, as a multiplication: n magic >> shift, exact for 0 <= n < 2^31.
+struct Divisor { unsigned magic; int shift; };
+inline Divisor divisor(long long d) {
+  int s = 0;
+  while ((1LL << s) < d) ++s;
+  return {(unsigned)((1ULL << (31 + s)) / d + 1), 31 + s};
+}
+FE_DEV int quotient(const Divisor& d, int n) { return (int)((unsigned long long)(unsigned)n * d.magic >> d.shift); }
+
+// A cache as the kernels see it.
 struct PackedCache {
   char* pages;
   long long page_ld;
   const int32_t *table, *len;
   int cols, page_rows, n_pages, cap, head_bytes;
-  unsigned magic;
-  int shift;
+  Divisor by_rows;                       // by page_rows
 };
 PackedCache packed_cache(const fe_packed_cache& c, int dh);
 
-FE_DEV int packed_page(const PackedCache& c, int j) {
-  return (int)((unsigned long long)(unsigned)j * c.magic >> c.shift);
-}
+FE_DEV int packed_page(const PackedCache& c, int j) { return quotient(c.by_rows, j); }
 FE_DEV int packed_len(const PackedCache& c, int s) { return min(max(c.len[s], 0), c.cap); }
 
 // The attention's and the weights' arguments.  The query rows of a (request, key head) are numbered r = (k S + s) G + hg < R
@@ -33,6 +38,7 @@ struct PackedArgs {
   float* lse;
   int B, K, S, Hq, Hkv, G, R, causal, q_ld, out_ld;
   float scale;
+  Divisor by_sg, by_g;                   // by S G and by G
   int tiles, splits;                     // row tiles per (request, key head); key ranges per tile
   // splits > 1: B * splits ranges in all; by_length: a request has as many of them as its share of the keys says, its own
   // rows taken as own_chunks chunks of 64

@@ -97,9 +97,9 @@ struct Row {
 FE_DEV Row row_of(const PackedArgs& a, int b, int g, int r) {
   Row w;
   const int rr = min(r, a.R - 1), sg = a.S * a.G;
-  w.k = rr / sg;
+  w.k = quotient(a.by_sg, rr);
   const int rem = rr - w.k * sg;
-  w.s = rem / a.G;
+  w.s = quotient(a.by_g, rem);
   w.h = g * a.G + rem - w.s * a.G;
   const int bk = b * a.K + w.k, n = q_rows(a, bk), m = own_rows(a, bk);
   w.live = r < a.R && w.s < n;
@@ -129,26 +129,28 @@ FE_DEV Ranges ranges_of_lane(const PackedArgs& a) {
 }
 
 // The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
-// their number; a list without query rows contributes none.  nb <= 128; 256 threads; ends with a barrier.
+// their number; a list without query rows contributes none.  nb <= 128.  Every wave writes the same; a barrier follows.
 FE_DEV void pack_own(const PackedArgs& a, int b, int k0, int nb, int* off) {
-  __shared__ int s_half;
-  const int tid = threadIdx.x, lane = tid & 63;
-  int v = 0;
-  if (tid < nb) {
-    const int bk = b * a.K + k0 + tid;
-    v = q_rows(a, bk) > 0 ? own_rows(a, bk) : 0;
-  }
+  const int lane = threadIdx.x & 63;
+  auto own = [&](int i) { return i < nb && q_rows(a, b * a.K + k0 + i) > 0 ? own_rows(a, b * a.K + k0 + i) : 0; };
+  const int u = own(2 * lane);
+  int v = u + own(2 * lane + 1);
+  const int both = v;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    const int u = __shfl_up(v, m);
-    if (lane >= m) v += u;
+    const int x = __shfl_up(v, m);
+    if (lane >= m) v += x;
   }
-  if (tid == 63) s_half = v;
-  __syncthreads();
-  if (tid >= 64 && tid < 128) v += s_half;
-  if (tid < nb) off[tid + 1] = v;
-  if (tid == 0) off[0] = 0;
-  __syncthreads();
+  if (lane == 0) off[0] = 0;
+  if (2 * lane < nb) off[2 * lane + 1] = v - both + u;
+  if (2 * lane + 1 < nb) off[2 * lane + 2] = v;
+}
+
+// Share z of `splits` of n things: the first n % splits shares have one more.
+FE_DEV int share(int n, int z, int splits) {
+  if (splits == 1) return z ? n : 0;
+  const int each = n / splits;
+  return z * each + min(z, n - each * splits);
 }
 
 // A tile of keys or values in LDS as bf16, rows of DH without padding, their units of 8 columns exchanged inside a row so that
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH, NS = C::NS;
   static_assert(KC % (32 * NS) == 0 && 4 * 32 * DH * 4 - WR * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2, "the join fits the tiles");
   __shared__ __attribute__((aligned(16))) bf16 s_kv[WK][NBUF][2][TILE];
-  __shared__ int s_off[ROWS + 1], s_hi;
+  __shared__ int s_off[ROWS + 1];
   // of a chunk (by its parity in the group): the last one with rows of no page, those rows; the last one with own values
   // of NaN, those units
   __shared__ int s_holes[WK][2], s_hole[WK][2][KC], s_odds[WK][2], s_odd[WK][2][KC * UPR];
@@ -248,17 +250,16 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     z = range - __builtin_amdgcn_readlane(mine.first, b);
     splits = __builtin_amdgcn_readlane(mine.n, b);
   }
-  const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R), sg = a.S * a.G;
-  const int k0 = r0 / sg, nb = (r1 - 1) / sg - k0 + 1;
+  const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R);
+  const int k0 = quotient(a.by_sg, r0), nb = quotient(a.by_sg, r1 - 1) - k0 + 1;
   for (int i = tid; i < WK * 2 * KC; i += 256) (&s_hole[0][0][0])[i] = -1;
   for (int i = tid; i < WK * 2 * KC * UPR; i += 256) (&s_odd[0][0][0])[i] = -1;
   if (tid < WK * 2) (&s_holes[0][0])[tid] = (&s_odds[0][0])[tid] = -1;
-  if (tid == 0) s_hi = 0;
 
   // This group's chunks: numbers q = grp + WK i of the range's share of the shared ones (from cb on) and, after these nc, of
   // the own ones (from ob on).  A thread's units of a chunk: their pages are looked up a chunk before they are loaded.
   const int nctx = ctx_rows(a, b), cctx = (nctx + KC - 1) / KC;
-  const int cb = (int)((long long)cctx * z / splits), nc = (int)((long long)cctx * (z + 1) / splits) - cb;
+  const int cb = share(cctx, z, splits), nc = share(cctx, z + 1, splits) - cb;
   u32x4 kc[PER], vc[PER];
   unsigned ks[PER], vs[PER];
   int entry[PER], rest[PER], list[PER];    // rest: row inside the page, -1 past the rows
@@ -326,21 +327,23 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     for (int c = 0; c < ND; ++c) qreg[c] = ldv<typename F::V>(Q + 16 * c);
   }
   pack_own(a, b, k0, nb, s_off);
-  const int lo = s_off[row.k - k0], hi = lo + row.own;   // the packed own rows that the row sees
-  int whi = row.live ? hi : 0, ahi = row.live ? hi : 0x7fffffff;
-#pragma unroll
-  for (int x = 1; x < 32; x *= 2) {
-    whi = max(whi, __shfl_xor(whi, x));
-    ahi = min(ahi, __shfl_xor(ahi, x));
-  }
-  // of the wave, uniform: bounds of what its rows see, and what all of them see
-  const int wlo = __builtin_amdgcn_readlane(lo, 0), alo = __builtin_amdgcn_readlane(lo, 31);
-  whi = __builtin_amdgcn_readfirstlane(whi);
-  ahi = wlo == alo ? __builtin_amdgcn_readfirstlane(ahi) : -1;
-  if (lane == 0 && grp == 0) atomicMax(&s_hi, whi);
   __syncthreads();
-  const int nown = __builtin_amdgcn_readfirstlane(s_hi), cown = (nown + KC - 1) / KC;
-  const int ob = (int)((long long)cown * z / splits), nq = nc + (int)((long long)cown * (z + 1) / splits) - ob;
+  const int lo = s_off[row.k - k0], hi = lo + row.own;   // the packed own rows that the row sees
+  // Of the wave, uniform: bounds of what its rows see, and (empty where they belong to several lists) what all of them see.
+  // Neither lo nor the live rows' hi falls from row to row.
+  const unsigned live = (unsigned)__ballot(row.live);
+  const int wlo = __builtin_amdgcn_readlane(lo, 0), alo = __builtin_amdgcn_readlane(lo, 31);
+  const int whi = live ? __builtin_amdgcn_readlane(hi, 31 - __builtin_clz(live)) : 0;
+  const int ahi = !live ? 0x7fffffff : wlo == alo ? __builtin_amdgcn_readlane(hi, __builtin_ctz(live)) : -1;
+  // the tile's packed rows end with what the last list's last live row in it sees
+  int nown = s_off[nb - 1];
+  {
+    const int bk = b * a.K + k0 + nb - 1, n = q_rows(a, bk), m = own_rows(a, bk);
+    const int s = min(quotient(a.by_g, r1 - 1 - (k0 + nb - 1) * a.S * a.G), n - 1);
+    if (s >= 0) nown += a.causal ? min(max(m - n + s + 1, 0), m) : m;
+    nown = __builtin_amdgcn_readfirstlane(nown);
+  }
+  const int cown = (nown + KC - 1) / KC, ob = share(cown, z, splits), nq = nc + share(cown, z + 1, splits) - ob;
 
   Op qf[ND];
 #pragma unroll
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
         int i = list[p];
         while (s_off[i + 1] <= x) ++i;
         list[p] = i;
-        const int j = x - s_off[i], pg = (int)((unsigned long long)(unsigned)j * A->own.magic >> A->own.shift);
+        const int j = x - s_off[i], pg = (int)((unsigned long long)(unsigned)j * A->own.by_rows.magic >> A->own.by_rows.shift);
         rest[p] = j - pg * rows;
         entry[p] = table[(long long)i * A->own.cols + pg];
       }
@@ -610,18 +613,35 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
   }
   if (ro >= rows) return;
   const long long at0 = (first - b) * per + ro;
-  float top = -INFINITY;
-  for (int z = 0; z < splits; ++z) top = fmaxf(top, a.part_ml[(z * per + at0) * 2]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float l = 0.f;
+  // ranges in batches, their loads together
+  constexpr int N = 8;
+  float top = -INFINITY, l = 0.f;
   f32x4 o{};
-#pragma unroll 4
-  for (int z = 0; z < splits; ++z) {
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[(z * per + at0) * 2] - ref);
-    const f32x4 v = ldv<f32x4>(a.part_o + (z * per + at0) * DH + d0);
-    l = fmaf(a.part_ml[(z * per + at0) * 2 + 1], f, l);
+  for (int z0 = 0; z0 < splits; z0 += N) {
+    float2 ml[N];
+    f32x4 v[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
+    for (int i = 0; i < N; ++i) {
+      const long long at = min(z0 + i, splits - 1) * per + at0;
+      ml[i] = ldv<float2>(a.part_ml + at * 2);
+      v[i] = ldv<f32x4>(a.part_o + at * DH + d0);
+    }
+    float next = top;
+#pragma unroll
+    for (int i = 0; i < N; ++i) next = fmaxf(next, ml[i].x);
+    const float ref = next == -INFINITY ? 0.f : next;
+    float f = __builtin_amdgcn_exp2f(top - ref);
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (z0 + i >= splits) break;         // uniform in a request
+      f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+      l = fmaf(ml[i].y, f, l);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] = fmaf(v[i][x], f, o[x]);
+    }
+    top = next;
   }
   const long long at = ro / a.Hq;
   const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);

@@ -505,10 +505,7 @@ PackedCache packed_cache(const fe_packed_cache& c, int dh) {
   k.cap = c.N > 0 ? c.cols * c.page_rows : 0;
   if (c.N > 0) {
     k.head_bytes = (c.page_rows * (dh + dh / 16) + 15) / 16 * 16;
-    int s = 0;
-    while ((1LL << s) < c.page_rows) ++s;
-    k.shift = 31 + s;
-    k.magic = (unsigned)((1ULL << (31 + s)) / c.page_rows + 1);
+    k.by_rows = divisor(c.page_rows);
   }
   return k;
 }
