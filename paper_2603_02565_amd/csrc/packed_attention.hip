@@ -657,119 +657,240 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
 
 // ------------------------------------------------------------------------------------------
 // Weights.  A wave takes 32 NK keys of a sequence's head, as operands in registers from the codes themselves (which
-// column a summed element is does not matter: lane l has the half l / 32 of its key's columns), and walks the query rows that
+// column a summed element is does not matter: lane l has the half l / 32 of its key's columns), and meets the query rows that
 // see them, 32 at a time: a lane then holds 16 rows' scores of its key, and their exponentials are added up in it.  Shared keys
-// meet every list's rows, own keys their list's.
+// meet every list's rows: four waves with keys of one head read them from LDS, 64 rows at a time, the next ones' loads in flight
+// behind this one's products.  Own keys meet their list's rows, each wave by itself.
 // ------------------------------------------------------------------------------------------
-template <typename T, int DH, int NK>
-__global__ __launch_bounds__(256, sizeof(T) * DH >= 256 ? 2 : 3) void k_packed_weigh(PackedArgs a) {
+template <typename T, int DH, int NK> struct Weigh {
   typedef Form<T> F;
-  constexpr int ND = DH / 16;              // products of 16 columns
-  __shared__ float s_lse[4][32];
-  __shared__ int s_seen[4][32];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, c32 = lane & 31;
-  // one task a wave: (request, key head, key tile, row range) of the shared rows, then (list, ...) of the own rows
-  const long long n_ctx = (long long)a.B * a.Hkv * a.ctx_tiles * a.ctx_splits;
-  long long id = (long long)xcd_tile(blockIdx.x, gridDim.x) * 4 + wave;
-  const bool own = id >= n_ctx;
-  if (own) id -= n_ctx;
-  const int tiles = own ? a.own_tiles : a.ctx_tiles, splits = own ? a.own_splits : a.ctx_splits;
-  if (own && id >= (long long)a.B * a.K * a.Hkv * a.own_tiles * a.own_splits) return;
-  const int t = (int)(id % tiles);
-  id /= tiles;
-  const int z = (int)(id % splits);
-  id /= splits;
-  const int g = (int)(id % a.Hkv), sq = (int)(id / a.Hkv), b = own ? sq / a.K : sq;
-  const PackedCache& x = own ? a.own : a.ctx;
-  const int n = packed_len(x, sq), j0 = t * 32 * NK;
-  if (j0 >= n) return;
-  const int sg = a.S * a.G, first = own ? (sq - b * a.K) * sg : 0;     // rows of the request that may see the keys
-  const int all_rows = own ? q_rows(a, sq) * a.G : a.R;
-  const int steps = (all_rows + 31) / 32, ib = (int)((long long)steps * z / splits), ie = (int)((long long)steps * (z + 1) / splits);
+  static constexpr int ND = DH / 16, ROWS = 64, PARTS = sizeof(T) == 4 ? 3 : 1, NBUF = sizeof(T) == 4 ? 1 : 2;
+  static constexpr int PER = ROWS * DH / 8 / 256;        // units of 8 columns that a thread stages
 
-  bf16x8 kf[NK][ND];
-  bool counts[NK];
-#pragma unroll
-  for (int u = 0; u < NK; ++u) {
-    const int j = j0 + 32 * u + c32;
-    int page = -1, r = 0;
-    if (j < n) {
-      const int p = packed_page(x, j);
-      r = j - p * x.page_rows;
-      page = x.table[(long long)sq * x.cols + p];
-    }
-    counts[u] = page >= 0 && page < x.n_pages;
-    const char* head = x.pages + (counts[u] ? page : 0) * x.page_ld + (long long)g * x.head_bytes;
-    const int row = counts[u] ? r : 0;
-    const unsigned* code = reinterpret_cast<const unsigned*>(head + (long long)row * (DH / 2)) + half * (DH / 16);
-    const unsigned char* scale = reinterpret_cast<const unsigned char*>(head + (long long)x.page_rows * DH) + row * (DH / 32);
-#pragma unroll
-    for (int c = 0; c < ND; ++c) kf[u][c] = values8(code[c], unit_of(scale[DH == 32 ? 0 : (half * (DH / 2) + 8 * c) / 32]));
-  }
-  const float scale = a.scale;
-  float sum[NK];
-#pragma unroll
-  for (int u = 0; u < NK; ++u) sum[u] = 0.f;
-
-  const int m = own ? n : 0, nq = own ? q_rows(a, sq) : 0;
-  bool any = false;                        // a row that counts
-  for (int i = ib; i < ie; ++i) {
-    const int rr = i * 32 + c32;
-    const bool inside = rr < all_rows;
-    const Row w = row_of(a, b, g, first + min(rr, all_rows - 1));
-    const float lse = a.lse[w.at * a.Hq + w.h];
-    const bool live = inside && w.live && lse != -INFINITY;
-    any |= __any(live);
-    const T* Q = static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + half * (DH / 2);
-    if (half == 0) {
-      s_lse[wave][c32] = live ? lse : INFINITY;
-      s_seen[wave][c32] = !live ? 0 : a.causal ? m - nq + w.s + 1 : m;   // own keys that it sees
-    }
-    f32x16 s[NK];
-#pragma unroll
-    for (int u = 0; u < NK; ++u) s[u] = f32x16{};
-#pragma unroll
-    for (int c = 0; c < ND; ++c) {
-      typename F::V v = ldv<typename F::V>(Q + 8 * c);
-      if (!live) v = typename F::V{};
-      const typename F::Op q = F::of(v);
-#pragma unroll
-      for (int u = 0; u < NK; ++u) s[u] = mma_held_right(q, kf[u][c], s[u]);
-    }
-    order();
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {          // rows 8 e + 4 half + 0 .. 3
-      const f32x4 ls = ldv<f32x4>(&s_lse[wave][8 * e + 4 * half]);
-      const int4 seen = ldv<int4>(&s_seen[wave][8 * e + 4 * half]);
+  // The keys j0 + 32 u + lane % 32 of sequence sq.
+  struct Keys {
+    bf16x8 f[NK][ND];
+    bool counts[NK];
+    FE_DEV void load(const PackedCache& x, int sq, int g, int j0, int n) {
+      const int lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
       for (int u = 0; u < NK; ++u) {
-        const int j = j0 + 32 * u + c32;
+        const int j = j0 + 32 * u + (lane & 31);
+        int page = -1, r = 0;
+        if (j < n) {
+          const int p = packed_page(x, j);
+          r = j - p * x.page_rows;
+          page = x.table[(long long)sq * x.cols + p];
+        }
+        counts[u] = page >= 0 && page < x.n_pages;
+        const char* head = x.pages + (counts[u] ? page : 0) * x.page_ld + (long long)g * x.head_bytes;
+        const int row = counts[u] ? r : 0;
+        const unsigned* code = reinterpret_cast<const unsigned*>(head + (long long)row * (DH / 2)) + half * (DH / 16);
+        const unsigned char* scale = reinterpret_cast<const unsigned char*>(head + (long long)x.page_rows * DH) + row * (DH / 32);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float d = fmaf(s[u][4 * e + q], scale, -ls[q]);
-          const float p = __builtin_amdgcn_exp2f(d * kLog2e);
-          const int to = q == 0 ? seen.x : q == 1 ? seen.y : q == 2 ? seen.z : seen.w;
-          sum[u] += !own || j < to ? p : 0.f;
+        for (int c = 0; c < ND; ++c) f[u][c] = values8(code[c], unit_of(scale[DH == 32 ? 0 : (half * (DH / 2) + 8 * c) / 32]));
+      }
+    }
+  };
+
+  // ... and what they received: `any`: some row counted (rows that do not may have met NaN).
+  static FE_DEV void store(const PackedArgs& a, const PackedCache& x, const Keys& k, const float (&sum)[NK], bool any, int sq, int g,
+                           int j0, int n, int z, int splits, long long sequences, const float* w, float* out, float* part) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int u = 0; u < NK; ++u) {
+      const float total = halves_sum(sum[u]);
+      const int j = j0 + 32 * u + (lane & 31);
+      if (j >= n || lane >= 32) continue;
+      const long long at = ((long long)sq * a.Hkv + g) * x.cap + j;
+      const float got = k.counts[u] && any ? total : 0.f;
+      if (splits > 1) part[(z * sequences * a.Hkv) * x.cap + at] = got;
+      else out[at] = w[at] + got;
+    }
+  }
+
+  // Four waves, 4 * 32 NK shared keys, rows [ib, ie) of 64.
+  static FE_DEV void shared(const PackedArgs& a, int id, bf16 (*s_q)[PARTS][ROWS * DH], float (*s_lse)[ROWS], int* s_any) {
+    typedef Tile<DH> L;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const int tiles = (a.ctx_tiles + 3) / 4, t = id % tiles;
+    id /= tiles;
+    const int g = id % a.Hkv;
+    id /= a.Hkv;
+    const int z = id % a.ctx_splits, b = id / a.ctx_splits;
+    const int n = packed_len(a.ctx, b), j0 = (4 * t + wave) * 32 * NK;
+    if (4 * t * 32 * NK >= n) return;      // uniform over the workgroup
+    const int steps = (a.R + ROWS - 1) / ROWS, ib = share(steps, z, a.ctx_splits), ie = share(steps, z + 1, a.ctx_splits);
+    if (tid == 0) *s_any = 0;
+    typename F::V q[PER];
+    float lse = -INFINITY;                 // of row tid of the step
+    unsigned live = 0;                     // bit p: the thread's unit p counts
+    auto load = [&](int i) __attribute__((always_inline)) {
+      live = 0;
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int u = tid + 256 * p;
+        const Row w = row_of(a, b, g, i * ROWS + u / (DH / 8));
+        q[p] = ldv<typename F::V>(static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + u % (DH / 8) * 8);
+        if (w.live && a.lse[w.at * a.Hq + w.h] != -INFINITY) live |= 1u << p;
+      }
+      if (tid < ROWS) {
+        const Row w = row_of(a, b, g, i * ROWS + tid);
+        lse = w.live ? a.lse[w.at * a.Hq + w.h] : -INFINITY;
+      }
+    };
+    if (ib < ie) load(ib);
+    Keys k;
+    k.load(a.ctx, b, g, j0, n);
+    const float sl2 = a.scale * kLog2e;
+    float sum[NK];
+#pragma unroll
+    for (int u = 0; u < NK; ++u) sum[u] = 0.f;
+    const int from = L::at(lane & 31, half * (DH / 16));
+    __syncthreads();                       // s_any
+    for (int i = ib; i < ie; ++i) {
+      const int buf = NBUF == 2 ? i & 1 : 0;
+      if constexpr (NBUF == 1) lds_barrier();
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int u = tid + 256 * p, at = L::at(u / (DH / 8), u % (DH / 8));
+        const typename F::V v = live >> p & 1 ? q[p] : typename F::V{};
+        if constexpr (PARTS == 1) {
+          *reinterpret_cast<bf16x8*>(s_q[buf][0] + at) = v;
+        } else {
+          const Parts w = parts8(v);
+#pragma unroll
+          for (int x = 0; x < 3; ++x) *reinterpret_cast<bf16x8*>(s_q[buf][x] + at) = w.p[x];
+        }
+      }
+      if (tid < ROWS) {
+        s_lse[buf][tid] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+        if (lse != -INFINITY) *s_any = 1;
+      }
+      lds_barrier();                       // two buffers: also the end of every wave's reads of the one written next
+      if (i + 1 < ie) load(i + 1);         // uniform
+      if (j0 >= n) continue;               // uniform in the wave
+#pragma unroll
+      for (int r = 0; r < ROWS; r += 32) {
+        const int left = a.R - i * ROWS - r;             // rows from here on
+        if (left <= 0) break;              // uniform
+        f32x16 s[NK];
+#pragma unroll
+        for (int u = 0; u < NK; ++u) s[u] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < ND; ++c) {
+          const int at = r * DH + (from ^ c << 3);
+          typename F::Op x;
+          if constexpr (PARTS == 1) x = ldv<bf16x8>(s_q[buf][0] + at);
+          else x = Parts{{ldv<bf16x8>(s_q[buf][0] + at), ldv<bf16x8>(s_q[buf][1] + at), ldv<bf16x8>(s_q[buf][2] + at)}};
+#pragma unroll
+          for (int u = 0; u < NK; ++u) s[u] = mma_held_right(x, k.f[u][c], s[u]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {      // rows 8 e + 4 half + 0 .. 3
+          if (8 * e >= left) break;        // uniform
+          const f32x4 ls = ldv<f32x4>(&s_lse[buf][r + 8 * e + 4 * half]);
+#pragma unroll
+          for (int u = 0; u < NK; ++u) {
+            float p[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + x], sl2, -ls[x]));
+            sum[u] += (p[0] + p[1]) + (p[2] + p[3]);
+          }
         }
       }
     }
-    order();
+    store(a, a.ctx, k, sum, *s_any != 0, b, g, j0, n, z, a.ctx_splits, a.B, a.ctx_w, a.ctx_w_out, a.part_ctx);
   }
-  const float* wi = own ? a.own_w : a.ctx_w;
-  float* wo = own ? a.own_w_out : a.ctx_w_out;
-  float* part = own ? a.part_own : a.part_ctx;
-  const long long N = own ? (long long)a.B * a.K : a.B;
+
+  // One wave, 32 NK own keys of a list, rows [ib, ie) of 32 of that list.
+  static FE_DEV void own(const PackedArgs& a, long long id, float* s_lse, int* s_seen) {
+    const int lane = threadIdx.x & 63, half = lane >> 5, c32 = lane & 31;
+    const int t = (int)(id % a.own_tiles);
+    id /= a.own_tiles;
+    const int z = (int)(id % a.own_splits);
+    id /= a.own_splits;
+    const int g = (int)(id % a.Hkv), sq = (int)(id / a.Hkv), b = sq / a.K;
+    const int n = packed_len(a.own, sq), j0 = t * 32 * NK;
+    if (j0 >= n) return;
+    const int nq = q_rows(a, sq), rows = nq * a.G, first = (sq - b * a.K) * a.S * a.G;
+    const int steps = (rows + 31) / 32, ib = share(steps, z, a.own_splits), ie = share(steps, z + 1, a.own_splits);
+    bool live = false;
+    int seen = 0;
+    float lse = 0.f;
+    typename F::V q[ND];
+    auto load = [&](int i) __attribute__((always_inline)) {
+      const int r = i * 32 + c32;
+      const Row w = row_of(a, b, g, first + min(r, rows - 1));
+      lse = a.lse[w.at * a.Hq + w.h];
+      live = r < rows;
+      seen = a.causal ? n - nq + w.s + 1 : n;
+      const T* Q = static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + half * (DH / 2);
 #pragma unroll
-  for (int u = 0; u < NK; ++u) {
-    const float total = halves_sum(sum[u]);
-    const int j = j0 + 32 * u + c32;
-    if (j >= n || half) continue;
-    const long long at = ((long long)sq * a.Hkv + g) * x.cap + j;
-    const float got = counts[u] && any ? total : 0.f;   // rows that do not count may have met NaN
-    if (splits > 1) part[(z * N * a.Hkv) * x.cap + at] = got;
-    else wo[at] = wi[at] + got;
+      for (int c = 0; c < ND; ++c) q[c] = ldv<typename F::V>(Q + 8 * c);
+    };
+    if (ib < ie) load(ib);
+    Keys k;
+    k.load(a.own, sq, g, j0, n);
+    const float sl2 = a.scale * kLog2e;
+    float sum[NK];
+#pragma unroll
+    for (int u = 0; u < NK; ++u) sum[u] = 0.f;
+    bool any = false;
+    for (int i = ib; i < ie; ++i) {
+      const bool counts = live && lse != -INFINITY;
+      any |= __any(counts);
+      if (half == 0) {
+        s_lse[c32] = counts ? lse * kLog2e : INFINITY;
+        s_seen[c32] = counts ? seen : 0;
+      }
+      f32x16 s[NK];
+#pragma unroll
+      for (int u = 0; u < NK; ++u) s[u] = f32x16{};
+#pragma unroll
+      for (int c = 0; c < ND; ++c) {
+        const typename F::Op x = F::of(counts ? q[c] : typename F::V{});
+#pragma unroll
+        for (int u = 0; u < NK; ++u) s[u] = mma_held_right(x, k.f[u][c], s[u]);
+      }
+      if (i + 1 < ie) load(i + 1);         // uniform
+      order();
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (8 * e >= rows - 32 * i) break; // uniform
+        const f32x4 ls = ldv<f32x4>(s_lse + 8 * e + 4 * half);
+        const int4 to = ldv<int4>(s_seen + 8 * e + 4 * half);
+#pragma unroll
+        for (int u = 0; u < NK; ++u) {
+          const int j = j0 + 32 * u + c32;
+          sum[u] += j < to.x ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e], sl2, -ls[0])) : 0.f;
+          sum[u] += j < to.y ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + 1], sl2, -ls[1])) : 0.f;
+          sum[u] += j < to.z ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + 2], sl2, -ls[2])) : 0.f;
+          sum[u] += j < to.w ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + 3], sl2, -ls[3])) : 0.f;
+        }
+      }
+      order();
+    }
+    store(a, a.own, k, sum, any, sq, g, j0, n, z, a.own_splits, (long long)a.B * a.K, a.own_w, a.own_w_out, a.part_own);
   }
+};
+
+template <typename T, int DH, int NK>
+__global__ __launch_bounds__(256, sizeof(T) * DH >= 256 ? 2 : 3) void k_packed_weigh(PackedArgs a) {
+  typedef Weigh<T, DH, NK> W;
+  __shared__ __attribute__((aligned(16))) bf16 s_q[W::NBUF][W::PARTS][W::ROWS * DH];
+  __shared__ __attribute__((aligned(16))) float s_lse[W::NBUF][W::ROWS];
+  __shared__ __attribute__((aligned(16))) float s_own_lse[4][32];
+  __shared__ __attribute__((aligned(16))) int s_seen[4][32];
+  __shared__ int s_any;
+  const int id = xcd_tile(blockIdx.x, gridDim.x), n_ctx = a.B * a.Hkv * a.ctx_splits * ((a.ctx_tiles + 3) / 4);
+  if (id < n_ctx) {                        // uniform
+    W::shared(a, id, s_q, s_lse, &s_any);
+    return;
+  }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long task = (long long)(id - n_ctx) * 4 + wave;
+  if (task < (long long)a.B * a.K * a.Hkv * a.own_tiles * a.own_splits) W::own(a, task, s_own_lse[wave], s_seen[wave]);
 }
 
 // Adds the row ranges of every key in ascending order.
@@ -805,8 +926,9 @@ constexpr int kWeighKeys = 2;              // 32-key operands of a wave
 
 template <typename T, int DH>
 hipError_t weigh(const PackedArgs& a, hipStream_t s) {
-  const long long tasks = (long long)a.B * a.Hkv * ((long long)a.ctx_tiles * a.ctx_splits + (long long)a.K * a.own_tiles * a.own_splits);
-  if (tasks > 0) hipLaunchKernelGGL((k_packed_weigh<T, DH, kWeighKeys>), dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, s, a);
+  const long long bg = (long long)a.B * a.Hkv, blocks = bg * a.ctx_splits * ((a.ctx_tiles + 3) / 4) +
+                                                        (bg * a.K * a.own_tiles * a.own_splits + 3) / 4;
+  if (blocks > 0) hipLaunchKernelGGL((k_packed_weigh<T, DH, kWeighKeys>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   auto sum = [&](const PackedCache& x, long long n, int splits, const float* part, const float* w, float* out) {
     if (e != hipSuccess || splits <= 1) return;
@@ -860,7 +982,7 @@ PackedWeighPlan packed_weigh_plan(const fe_packed_args& a) {
   p.own_splits = p.own_tiles ? ranges(bg * a.K * p.own_tiles, sg) : 1;
   p.ctx_bytes = p.ctx_splits > 1 ? (size_t)p.ctx_splits * bg * T * sizeof(float) : 0;
   p.own_bytes = p.own_splits > 1 ? (size_t)p.own_splits * bg * a.K * L * sizeof(float) : 0;
-  p.blocks = (bg * ((long long)p.ctx_tiles * p.ctx_splits + (long long)a.K * p.own_tiles * p.own_splits) + 3) / 4;
+  p.blocks = bg * p.ctx_splits * ((p.ctx_tiles + 3) / 4) + (bg * a.K * p.own_tiles * p.own_splits + 3) / 4;
   p.sum_blocks = std::max(p.ctx_splits > 1 ? (bg * T + 255) / 256 : 0, p.own_splits > 1 ? (bg * a.K * L + 255) / 256 : 0);
   return p;
 }
