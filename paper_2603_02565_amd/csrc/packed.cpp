@@ -234,8 +234,9 @@ fe_status fe_packed_weights(const fe_packed_args* a, void* stream) {
   if (need && (!a->ws || a->ws_bytes < need))
     return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);
   PackedArgs k = kernel_args(*a);
-  k.ctx_tiles = p.ctx_tiles; k.own_tiles = p.own_tiles;
+  k.ctx_keys = p.ctx_keys; k.own_keys = p.own_keys;
   k.ctx_splits = p.ctx_splits; k.own_splits = p.own_splits;
+  k.keys_by_length = p.keys_by_length;
   k.part_ctx = static_cast<float*>(a->ws);
   k.part_own = reinterpret_cast<float*>(static_cast<char*>(a->ws) + up256(p.ctx_bytes));
   const hipError_t e = launch_packed_weights(k, a->dh, a->dtype == FE_BF16, static_cast<hipStream_t>(stream));

@@ -46,13 +46,18 @@ struct PackedArgs {
   float *part_o, *part_ml;               // splits > 1: [B * splits][K S Hq][dh] sums, [..][2] maximum and sum
   const float *ctx_w, *own_w;            // weights
   float *ctx_w_out, *own_w_out;
-  int ctx_tiles, own_tiles, ctx_splits, own_splits;   // key tiles per sequence, row ranges per key tile
+  int ctx_keys, own_keys, ctx_splits, own_splits;     // key ranges, and row ranges, per (sequence, key head)
+  int keys_by_length;                    // the shared keys' ranges, as above
   float *part_ctx, *part_own;            // [splits][N][Hkv][cap]
 };
 
 struct PackedPlan { int waves, tiles, splits, by_length, own_chunks; size_t part_bytes; };   // waves: those that share a chunk
 PackedPlan packed_plan(const fe_packed_args& a);
-struct PackedWeighPlan { int ctx_tiles, own_tiles, ctx_splits, own_splits; size_t ctx_bytes, own_bytes; long long blocks, sum_blocks; };
+struct PackedWeighPlan {
+  int ctx_keys, own_keys, ctx_splits, own_splits, keys_by_length;
+  size_t ctx_bytes, own_bytes;
+  long long blocks, sum_blocks;
+};
 PackedWeighPlan packed_weigh_plan(const fe_packed_args& a);
 
 hipError_t launch_packed_attention(const PackedArgs& a, int dh, bool bf16_rows, const PackedPlan& p, hipStream_t s);

@@ -108,17 +108,17 @@ FE_DEV Row row_of(const PackedArgs& a, int b, int g, int r) {
   return w;
 }
 
-// The key ranges are numbered request after request: request b has `n` of them, from `first` on.  by_length (B <= 64): lane b
-// finds those of request b.  Every request has one; the others are shared out in proportion to the chunks of 64 keys,
-// rounded down, so they may leave a few unused.
+// Key ranges by length are numbered request after request: request b has `n` of them, from `first` on; B <= 64, lane b finds
+// those of request b.  Every request has one; the others of B * splits are shared out in proportion to the chunks of 64 keys,
+// `more` beside the shared ones, rounded down, so they may leave a few unused.
 struct Ranges { int first, n; };
-FE_DEV Ranges ranges_of_lane(const PackedArgs& a) {
+FE_DEV Ranges ranges_of_lane(const PackedArgs& a, int splits, int more) {
   const int lane = threadIdx.x & 63;
-  const int mine = lane < a.B ? (ctx_rows(a, lane) + 63) / 64 + a.own_chunks + 1 : 0;
+  const int mine = lane < a.B ? (ctx_rows(a, lane) + 63) / 64 + more + 1 : 0;
   int all = mine;
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) all += __shfl_xor(all, x);
-  const int n = lane < a.B ? 1 + (int)((float)(a.B * (a.splits - 1)) * (float)mine / (float)all) : 0;
+  const int n = lane < a.B ? 1 + (int)((float)(a.B * (splits - 1)) * (float)mine / (float)all) : 0;
   int end = n;
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) {
@@ -126,6 +126,16 @@ FE_DEV Ranges ranges_of_lane(const PackedArgs& a) {
     if (lane >= x) end += before;
   }
   return {end - n, n};
+}
+// Turns number `range` into request b's range z of `splits`; false: left over.
+FE_DEV bool range_of(const PackedArgs& a, int range, int more, int& b, int& z, int& splits) {
+  const int lane = threadIdx.x & 63;
+  const Ranges mine = ranges_of_lane(a, splits, more);
+  b = __popcll(__ballot(lane < a.B && mine.first + mine.n <= range));
+  if (b >= a.B) return false;
+  z = range - __builtin_amdgcn_readlane(mine.first, b);
+  splits = __builtin_amdgcn_readlane(mine.n, b);
+  return true;
 }
 
 // The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
@@ -243,13 +253,7 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   id /= a.tiles;
   const int g = id % a.Hkv, range = id / a.Hkv;
   int b = range / a.splits, z = range % a.splits, splits = a.splits;
-  if (a.by_length) {                       // uniform
-    const Ranges mine = ranges_of_lane(a);
-    b = __popcll(__ballot(lane < a.B && mine.first + mine.n <= range));
-    if (b >= a.B) return;                  // left over
-    z = range - __builtin_amdgcn_readlane(mine.first, b);
-    splits = __builtin_amdgcn_readlane(mine.n, b);
-  }
+  if (a.by_length && !range_of(a, range, a.own_chunks, b, z, splits)) return;   // uniform
   const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R);
   const int k0 = quotient(a.by_sg, r0), nb = quotient(a.by_sg, r1 - 1) - k0 + 1;
   for (int i = tid; i < WK * 2 * KC; i += 256) (&s_hole[0][0][0])[i] = -1;
@@ -607,7 +611,7 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
   const int b = (int)(min(ro, rows - 1) / per);
   int first = b * a.splits, splits = a.splits;
   if (a.by_length) {                       // uniform
-    const Ranges mine = ranges_of_lane(a);
+    const Ranges mine = ranges_of_lane(a, a.splits, a.own_chunks);
     first = __shfl(mine.first, b);
     splits = __shfl(mine.n, b);
   }
@@ -656,241 +660,210 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Weights.  A wave takes 32 NK keys of a sequence's head, as operands in registers from the codes themselves (which
-// column a summed element is does not matter: lane l has the half l / 32 of its key's columns), and meets the query rows that
-// see them, 32 at a time: a lane then holds 16 rows' scores of its key, and their exponentials are added up in it.  Shared keys
-// meet every list's rows: four waves with keys of one head read them from LDS, 64 rows at a time, the next ones' loads in flight
-// behind this one's products.  Own keys meet their list's rows, each wave by itself.
+// Weights.  A workgroup takes a range of a sequence's keys of one head, and a range of the query rows that see them: every
+// list's for shared keys, the list's for own keys.  The rows lie in LDS, as many as fit; each wave walks tiles of 32 NK keys
+// without meeting the others, its operands made in registers from the codes, whose loads run a tile ahead and their pages two.
+// Which column a summed element is does not matter: lane l has the half l / 32 of its key's columns.  A lane then holds 16
+// rows' scores of its key, and their exponentials are added up in it.
 // ------------------------------------------------------------------------------------------
-template <typename T, int DH, int NK> struct Weigh {
+template <typename T, int DH> struct Weigh {
   typedef Form<T> F;
-  static constexpr int ND = DH / 16, ROWS = 64, PARTS = sizeof(T) == 4 ? 3 : 1, NBUF = sizeof(T) == 4 ? 1 : 2;
-  static constexpr int PER = ROWS * DH / 8 / 256;        // units of 8 columns that a thread stages
-
-  // The keys j0 + 32 u + lane % 32 of sequence sq.
-  struct Keys {
-    bf16x8 f[NK][ND];
-    bool counts[NK];
-    FE_DEV void load(const PackedCache& x, int sq, int g, int j0, int n) {
-      const int lane = threadIdx.x & 63, half = lane >> 5;
-#pragma unroll
-      for (int u = 0; u < NK; ++u) {
-        const int j = j0 + 32 * u + (lane & 31);
-        int page = -1, r = 0;
-        if (j < n) {
-          const int p = packed_page(x, j);
-          r = j - p * x.page_rows;
-          page = x.table[(long long)sq * x.cols + p];
-        }
-        counts[u] = page >= 0 && page < x.n_pages;
-        const char* head = x.pages + (counts[u] ? page : 0) * x.page_ld + (long long)g * x.head_bytes;
-        const int row = counts[u] ? r : 0;
-        const unsigned* code = reinterpret_cast<const unsigned*>(head + (long long)row * (DH / 2)) + half * (DH / 16);
-        const unsigned char* scale = reinterpret_cast<const unsigned char*>(head + (long long)x.page_rows * DH) + row * (DH / 32);
-#pragma unroll
-        for (int c = 0; c < ND; ++c) f[u][c] = values8(code[c], unit_of(scale[DH == 32 ? 0 : (half * (DH / 2) + 8 * c) / 32]));
-      }
-    }
+  typedef Tile<DH> L;
+  static constexpr int ND = DH / 16, PARTS = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int ROWS = (sizeof(T) == 4 ? 8192 : 16384) / DH;    // rows in LDS at a time
+  struct Lds {
+    __attribute__((aligned(16))) bf16 q[PARTS][ROWS * DH];
+    __attribute__((aligned(16))) float lse[ROWS];
+    __attribute__((aligned(16))) int seen[ROWS];                       // own keys that the row sees
+    int any;
   };
 
-  // ... and what they received: `any`: some row counted (rows that do not may have met NaN).
-  static FE_DEV void store(const PackedArgs& a, const PackedCache& x, const Keys& k, const float (&sum)[NK], bool any, int sq, int g,
-                           int j0, int n, int z, int splits, long long sequences, const float* w, float* out, float* part) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int u = 0; u < NK; ++u) {
-      const float total = halves_sum(sum[u]);
-      const int j = j0 + 32 * u + (lane & 31);
-      if (j >= n || lane >= 32) continue;
-      const long long at = ((long long)sq * a.Hkv + g) * x.cap + j;
-      const float got = k.counts[u] && any ? total : 0.f;
-      if (splits > 1) part[(z * sequences * a.Hkv) * x.cap + at] = got;
-      else out[at] = w[at] + got;
-    }
-  }
-
-  // Four waves, 4 * 32 NK shared keys, rows [ib, ie) of 64.
-  static FE_DEV void shared(const PackedArgs& a, int id, bf16 (*s_q)[PARTS][ROWS * DH], float (*s_lse)[ROWS], int* s_any) {
-    typedef Tile<DH> L;
+  template <bool OWN, int NK> static FE_DEV void run(const PackedArgs& a, int id, Lds& S) {
+    constexpr int WORDS = DH / 16, SCALES = DH == 128 ? 2 : 1;         // of a lane: half a key's codes, and their blocks' scales
+    const PackedCache& x = OWN ? a.own : a.ctx;
+    const int key_splits = OWN ? a.own_keys : a.ctx_keys, row_splits = OWN ? a.own_splits : a.ctx_splits;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-    const int tiles = (a.ctx_tiles + 3) / 4, t = id % tiles;
-    id /= tiles;
+    const int z = id % row_splits;
+    id /= row_splits;
     const int g = id % a.Hkv;
     id /= a.Hkv;
-    const int z = id % a.ctx_splits, b = id / a.ctx_splits;
-    const int n = packed_len(a.ctx, b), j0 = (4 * t + wave) * 32 * NK;
-    if (4 * t * 32 * NK >= n) return;      // uniform over the workgroup
-    const int steps = (a.R + ROWS - 1) / ROWS, ib = share(steps, z, a.ctx_splits), ie = share(steps, z + 1, a.ctx_splits);
-    if (tid == 0) *s_any = 0;
-    typename F::V q[PER];
-    float lse = -INFINITY;                 // of row tid of the step
-    unsigned live = 0;                     // bit p: the thread's unit p counts
-    auto load = [&](int i) __attribute__((always_inline)) {
-      live = 0;
+    int sq = id / key_splits, zk = id % key_splits, ranges = key_splits;
+    if (!OWN && a.keys_by_length && !range_of(a, id, 0, sq, zk, ranges)) return;   // uniform over the workgroup
+    const int b = OWN ? sq / a.K : sq;
+    const int n = packed_len(x, sq), tiles = (n + 32 * NK - 1) / (32 * NK);
+    const int tb = share(tiles, zk, ranges), te = share(tiles, zk + 1, ranges);
+    if (tb == te) return;                  // uniform over the workgroup
+    const int nq = OWN ? q_rows(a, sq) : 0, rows = OWN ? nq * a.G : a.R, first = OWN ? (sq - b * a.K) * a.S * a.G : 0;
+    const int rb = share(rows, z, row_splits), re = share(rows, z + 1, row_splits);
+
+    int page[NK], row[NK];                 // of the tile after the next: row -1 past the length
+    unsigned code[NK][WORDS], scale[NK][SCALES];
+    bool counts[NK];                       // of the tile whose codes are under way
+    const int32_t* table = x.table + (long long)sq * x.cols;
+    auto find = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int p = 0; p < PER; ++p) {
-        const int u = tid + 256 * p;
-        const Row w = row_of(a, b, g, i * ROWS + u / (DH / 8));
-        q[p] = ldv<typename F::V>(static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + u % (DH / 8) * 8);
-        if (w.live && a.lse[w.at * a.Hq + w.h] != -INFINITY) live |= 1u << p;
-      }
-      if (tid < ROWS) {
-        const Row w = row_of(a, b, g, i * ROWS + tid);
-        lse = w.live ? a.lse[w.at * a.Hq + w.h] : -INFINITY;
+      for (int u = 0; u < NK; ++u) {
+        const int j = (t * NK + u) * 32 + (lane & 31);
+        row[u] = -1;
+        if (t < te && j < n) {
+          const int p = packed_page(x, j);
+          row[u] = j - p * x.page_rows;
+          page[u] = table[(unsigned)p];
+        }
       }
     };
-    if (ib < ie) load(ib);
-    Keys k;
-    k.load(a.ctx, b, g, j0, n);
+    auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < NK; ++u) {
+        counts[u] = row[u] >= 0 && (unsigned)page[u] < (unsigned)x.n_pages;
+        const unsigned r = counts[u] ? row[u] : 0;                     // what does not count reads row 0 of page 0
+        const char* head = x.pages + (unsigned long long)(counts[u] ? (unsigned)page[u] : 0u) * (unsigned)x.page_ld;
+        const unsigned at = (unsigned)g * x.head_bytes;
+        const unsigned* w = reinterpret_cast<const unsigned*>(head + (at + r * (DH / 2) + half * (DH / 4)));
+        const unsigned char* s = reinterpret_cast<const unsigned char*>(head + (at + (unsigned)x.page_rows * DH + r * (DH / 32)));
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) code[u][i] = w[i];
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) scale[u][i] = s[DH == 32 ? 0 : half * SCALES + i];
+      }
+    };
+    const int t0 = tb + wave;
+    find(t0);
+
     const float sl2 = a.scale * kLog2e;
-    float sum[NK];
-#pragma unroll
-    for (int u = 0; u < NK; ++u) sum[u] = 0.f;
     const int from = L::at(lane & 31, half * (DH / 16));
-    __syncthreads();                       // s_any
-    for (int i = ib; i < ie; ++i) {
-      const int buf = NBUF == 2 ? i & 1 : 0;
-      if constexpr (NBUF == 1) lds_barrier();
-#pragma unroll
-      for (int p = 0; p < PER; ++p) {
-        const int u = tid + 256 * p, at = L::at(u / (DH / 8), u % (DH / 8));
-        const typename F::V v = live >> p & 1 ? q[p] : typename F::V{};
-        if constexpr (PARTS == 1) {
-          *reinterpret_cast<bf16x8*>(s_q[buf][0] + at) = v;
-        } else {
-          const Parts w = parts8(v);
-#pragma unroll
-          for (int x = 0; x < 3; ++x) *reinterpret_cast<bf16x8*>(s_q[buf][x] + at) = w.p[x];
-        }
+    const float* w_in = OWN ? a.own_w : a.ctx_w;
+    float* out = OWN ? a.own_w_out : a.ctx_w_out;
+    if (row_splits > 1) out = (OWN ? a.part_own : a.part_ctx) + z * ((long long)(OWN ? a.B * a.K : a.B) * a.Hkv) * x.cap;
+    const long long base = ((long long)sq * a.Hkv + g) * x.cap;
+    // at least one trip, so that every key gets its entry
+    for (int rc = rb; rc == rb || rc < re; rc += ROWS) {
+      const int here = min(ROWS, re - rc);               // rows of this trip, 0 where there are none
+      if (rc > rb) {
+        find(t0);
+        __syncthreads();                   // the rows before are no longer read
       }
-      if (tid < ROWS) {
-        s_lse[buf][tid] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-        if (lse != -INFINITY) *s_any = 1;
-      }
-      lds_barrier();                       // two buffers: also the end of every wave's reads of the one written next
-      if (i + 1 < ie) load(i + 1);         // uniform
-      if (j0 >= n) continue;               // uniform in the wave
+      // the rows' loads four units of a thread at a time, the first ones' and the keys' together
+      constexpr int BATCH = 2;
+      const int units = (here + 31) / 32 * 32 * (DH / 8);
+      typename F::V v[BATCH];
+      float lse[BATCH];
+      int sees[BATCH];
+      auto rows_load = [&](int u0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < ROWS; r += 32) {
-        const int left = a.R - i * ROWS - r;             // rows from here on
-        if (left <= 0) break;              // uniform
-        f32x16 s[NK];
-#pragma unroll
-        for (int u = 0; u < NK; ++u) s[u] = f32x16{};
-#pragma unroll
-        for (int c = 0; c < ND; ++c) {
-          const int at = r * DH + (from ^ c << 3);
-          typename F::Op x;
-          if constexpr (PARTS == 1) x = ldv<bf16x8>(s_q[buf][0] + at);
-          else x = Parts{{ldv<bf16x8>(s_q[buf][0] + at), ldv<bf16x8>(s_q[buf][1] + at), ldv<bf16x8>(s_q[buf][2] + at)}};
-#pragma unroll
-          for (int u = 0; u < NK; ++u) s[u] = mma_held_right(x, k.f[u][c], s[u]);
+        for (int i = 0; i < BATCH; ++i) {
+          const int u = u0 + 256 * i, r = u / (DH / 8);
+          if (u >= units) break;
+          const Row q = row_of(a, b, g, first + rc + min(r, here - 1));
+          v[i] = ldv<typename F::V>(static_cast<const T*>(a.q) + q.at * a.q_ld + q.h * DH + u % (DH / 8) * 8);
+          lse[i] = a.lse[q.at * a.Hq + q.h];
+          sees[i] = r < here && q.live ? (a.causal ? n - nq + q.s + 1 : n) : -0x7fffffff;
         }
+      };
+      auto rows_store = [&](int u0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {      // rows 8 e + 4 half + 0 .. 3
-          if (8 * e >= left) break;        // uniform
-          const f32x4 ls = ldv<f32x4>(&s_lse[buf][r + 8 * e + 4 * half]);
+        for (int i = 0; i < BATCH; ++i) {
+          const int u = u0 + 256 * i, r = u / (DH / 8), at = L::at(r, u % (DH / 8));
+          if (u >= units) break;
+          const bool live = sees[i] != -0x7fffffff && lse[i] != -INFINITY;
+          if (!live) v[i] = typename F::V{};
+          if constexpr (PARTS == 1) {
+            *reinterpret_cast<bf16x8*>(S.q[0] + at) = v[i];
+          } else {
+            const Parts w = parts8(v[i]);
 #pragma unroll
-          for (int u = 0; u < NK; ++u) {
-            float p[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) p[x] = __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + x], sl2, -ls[x]));
-            sum[u] += (p[0] + p[1]) + (p[2] + p[3]);
+            for (int x = 0; x < 3; ++x) *reinterpret_cast<bf16x8*>(S.q[x] + at) = w.p[x];
+          }
+          if (u % (DH / 8) == 0) {
+            S.lse[r] = live ? lse[i] * kLog2e : INFINITY;
+            if (OWN) S.seen[r] = live ? sees[i] : 0;
+            if (live) S.any = 1;
           }
         }
+      };
+      rows_load(tid);
+      load();
+      find(t0 + 4);
+      if (tid == 0) S.any = 0;
+      __syncthreads();
+      for (int u = tid; u < units; u += 256 * BATCH) {
+        if (u != tid) rows_load(u);
+        rows_store(u);
       }
-    }
-    store(a, a.ctx, k, sum, *s_any != 0, b, g, j0, n, z, a.ctx_splits, a.B, a.ctx_w, a.ctx_w_out, a.part_ctx);
-  }
-
-  // One wave, 32 NK own keys of a list, rows [ib, ie) of 32 of that list.
-  static FE_DEV void own(const PackedArgs& a, long long id, float* s_lse, int* s_seen) {
-    const int lane = threadIdx.x & 63, half = lane >> 5, c32 = lane & 31;
-    const int t = (int)(id % a.own_tiles);
-    id /= a.own_tiles;
-    const int z = (int)(id % a.own_splits);
-    id /= a.own_splits;
-    const int g = (int)(id % a.Hkv), sq = (int)(id / a.Hkv), b = sq / a.K;
-    const int n = packed_len(a.own, sq), j0 = t * 32 * NK;
-    if (j0 >= n) return;
-    const int nq = q_rows(a, sq), rows = nq * a.G, first = (sq - b * a.K) * a.S * a.G;
-    const int steps = (rows + 31) / 32, ib = share(steps, z, a.own_splits), ie = share(steps, z + 1, a.own_splits);
-    bool live = false;
-    int seen = 0;
-    float lse = 0.f;
-    typename F::V q[ND];
-    auto load = [&](int i) __attribute__((always_inline)) {
-      const int r = i * 32 + c32;
-      const Row w = row_of(a, b, g, first + min(r, rows - 1));
-      lse = a.lse[w.at * a.Hq + w.h];
-      live = r < rows;
-      seen = a.causal ? n - nq + w.s + 1 : n;
-      const T* Q = static_cast<const T*>(a.q) + w.at * a.q_ld + w.h * DH + half * (DH / 2);
-#pragma unroll
-      for (int c = 0; c < ND; ++c) q[c] = ldv<typename F::V>(Q + 8 * c);
-    };
-    if (ib < ie) load(ib);
-    Keys k;
-    k.load(a.own, sq, g, j0, n);
-    const float sl2 = a.scale * kLog2e;
-    float sum[NK];
-#pragma unroll
-    for (int u = 0; u < NK; ++u) sum[u] = 0.f;
-    bool any = false;
-    for (int i = ib; i < ie; ++i) {
-      const bool counts = live && lse != -INFINITY;
-      any |= __any(counts);
-      if (half == 0) {
-        s_lse[c32] = counts ? lse * kLog2e : INFINITY;
-        s_seen[c32] = counts ? seen : 0;
-      }
-      f32x16 s[NK];
-#pragma unroll
-      for (int u = 0; u < NK; ++u) s[u] = f32x16{};
-#pragma unroll
-      for (int c = 0; c < ND; ++c) {
-        const typename F::Op x = F::of(counts ? q[c] : typename F::V{});
-#pragma unroll
-        for (int u = 0; u < NK; ++u) s[u] = mma_held_right(x, k.f[u][c], s[u]);
-      }
-      if (i + 1 < ie) load(i + 1);         // uniform
-      order();
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (8 * e >= rows - 32 * i) break; // uniform
-        const f32x4 ls = ldv<f32x4>(s_lse + 8 * e + 4 * half);
-        const int4 to = ldv<int4>(s_seen + 8 * e + 4 * half);
+      __syncthreads();
+      const bool any = S.any;              // a row that counts: those that do not may have met NaN
+      for (int t = t0; t < te; t += 4) {
+        bf16x8 k[NK][ND];
+        bool got[NK];
 #pragma unroll
         for (int u = 0; u < NK; ++u) {
-          const int j = j0 + 32 * u + c32;
-          sum[u] += j < to.x ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e], sl2, -ls[0])) : 0.f;
-          sum[u] += j < to.y ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + 1], sl2, -ls[1])) : 0.f;
-          sum[u] += j < to.z ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + 2], sl2, -ls[2])) : 0.f;
-          sum[u] += j < to.w ? __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + 3], sl2, -ls[3])) : 0.f;
+          got[u] = counts[u];
+#pragma unroll
+          for (int c = 0; c < ND; ++c) k[u][c] = values8(code[u][c], unit_of(scale[u][c * SCALES / ND]));
+        }
+        if (t + 4 < te) {                  // uniform
+          load();
+          find(t + 8);
+        }
+        float sum[NK];
+#pragma unroll
+        for (int u = 0; u < NK; ++u) sum[u] = 0.f;
+#pragma unroll 1
+        for (int r = 0; r < here; r += 32) {
+          f32x16 s[NK];
+#pragma unroll
+          for (int u = 0; u < NK; ++u) s[u] = f32x16{};
+#pragma unroll
+          for (int c = 0; c < ND; ++c) {
+            const int at = r * DH + (from ^ c << 3);
+            typename F::Op q;
+            if constexpr (PARTS == 1) q = ldv<bf16x8>(S.q[0] + at);
+            else q = Parts{{ldv<bf16x8>(S.q[0] + at), ldv<bf16x8>(S.q[1] + at), ldv<bf16x8>(S.q[2] + at)}};
+#pragma unroll
+            for (int u = 0; u < NK; ++u) s[u] = mma_held_right(q, k[u][c], s[u]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {    // rows 8 e + 4 half + 0 .. 3
+            if (r + 8 * e >= here) break;  // uniform
+            const f32x4 ls = ldv<f32x4>(S.lse + r + 8 * e + 4 * half);
+            int4 seen;
+            if (OWN) seen = ldv<int4>(S.seen + r + 8 * e + 4 * half);
+#pragma unroll
+            for (int u = 0; u < NK; ++u) {
+              float p[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + i], sl2, -ls[i]));
+              if (OWN) {
+                const int j = (t * NK + u) * 32 + (lane & 31);
+                p[0] = j < seen.x ? p[0] : 0.f;
+                p[1] = j < seen.y ? p[1] : 0.f;
+                p[2] = j < seen.z ? p[2] : 0.f;
+                p[3] = j < seen.w ? p[3] : 0.f;
+              }
+              sum[u] += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < NK; ++u) {
+          const float total = halves_sum(sum[u]), add = got[u] && any ? total : 0.f;
+          const int j = (t * NK + u) * 32 + (lane & 31);
+          if (j >= n || half) continue;
+          const float had = rc > rb ? out[base + j] : row_splits > 1 ? 0.f : w_in[base + j];
+          out[base + j] = had + add;
         }
       }
-      order();
     }
-    store(a, a.own, k, sum, any, sq, g, j0, n, z, a.own_splits, (long long)a.B * a.K, a.own_w, a.own_w_out, a.part_own);
   }
 };
 
-template <typename T, int DH, int NK>
-__global__ __launch_bounds__(256, sizeof(T) * DH >= 256 ? 2 : 3) void k_packed_weigh(PackedArgs a) {
-  typedef Weigh<T, DH, NK> W;
-  __shared__ __attribute__((aligned(16))) bf16 s_q[W::NBUF][W::PARTS][W::ROWS * DH];
-  __shared__ __attribute__((aligned(16))) float s_lse[W::NBUF][W::ROWS];
-  __shared__ __attribute__((aligned(16))) float s_own_lse[4][32];
-  __shared__ __attribute__((aligned(16))) int s_seen[4][32];
-  __shared__ int s_any;
-  const int id = xcd_tile(blockIdx.x, gridDim.x), n_ctx = a.B * a.Hkv * a.ctx_splits * ((a.ctx_tiles + 3) / 4);
-  if (id < n_ctx) {                        // uniform
-    W::shared(a, id, s_q, s_lse, &s_any);
-    return;
-  }
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long task = (long long)(id - n_ctx) * 4 + wave;
-  if (task < (long long)a.B * a.K * a.Hkv * a.own_tiles * a.own_splits) W::own(a, task, s_own_lse[wave], s_seen[wave]);
+template <typename T, int DH>
+__global__ __launch_bounds__(256, sizeof(T) * DH > 256 ? 2 : 4) void k_packed_weigh(PackedArgs a) {
+  typedef Weigh<T, DH> W;
+  __shared__ typename W::Lds S;
+  const int id = blockIdx.x, n_ctx = a.ctx_w ? a.B * a.Hkv * a.ctx_splits * a.ctx_keys : 0;
+  if (id < n_ctx) W::template run<false, 1>(a, xcd_tile(id, n_ctx), S);   // uniform
+  else W::template run<true, 1>(a, id - n_ctx, S);
 }
 
 // Adds the row ranges of every key in ascending order.
@@ -922,13 +895,11 @@ hipError_t fwd(const PackedArgs& a, const PackedPlan& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-constexpr int kWeighKeys = 2;              // 32-key operands of a wave
-
 template <typename T, int DH>
 hipError_t weigh(const PackedArgs& a, hipStream_t s) {
-  const long long bg = (long long)a.B * a.Hkv, blocks = bg * a.ctx_splits * ((a.ctx_tiles + 3) / 4) +
-                                                        (bg * a.K * a.own_tiles * a.own_splits + 3) / 4;
-  if (blocks > 0) hipLaunchKernelGGL((k_packed_weigh<T, DH, kWeighKeys>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  const long long bg = (long long)a.B * a.Hkv;
+  const long long blocks = (a.ctx_w ? bg * a.ctx_splits * a.ctx_keys : 0) + (a.own_w ? bg * a.K * a.own_splits * a.own_keys : 0);
+  if (blocks > 0) hipLaunchKernelGGL((k_packed_weigh<T, DH>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   auto sum = [&](const PackedCache& x, long long n, int splits, const float* part, const float* w, float* out) {
     if (e != hipSuccess || splits <= 1) return;
@@ -936,8 +907,8 @@ hipError_t weigh(const PackedArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(k_packed_weigh_sum, dim3((unsigned)((keys + 255) / 256)), dim3(256), 0, s, x, a.Hkv, splits, keys, part, w, out);
     e = hipGetLastError();
   };
-  if (a.ctx_tiles) sum(a.ctx, a.B, a.ctx_splits, a.part_ctx, a.ctx_w, a.ctx_w_out);
-  if (a.own_tiles) sum(a.own, (long long)a.B * a.K, a.own_splits, a.part_own, a.own_w, a.own_w_out);
+  if (a.ctx_w) sum(a.ctx, a.B, a.ctx_splits, a.part_ctx, a.ctx_w, a.ctx_w_out);
+  if (a.own_w) sum(a.own, (long long)a.B * a.K, a.own_splits, a.part_own, a.own_w, a.own_w_out);
   return e;
 }
 
@@ -970,19 +941,21 @@ PackedWeighPlan packed_weigh_plan(const fe_packed_args& a) {
   const long long G = a.n_heads / a.n_kv_heads, R = (long long)a.K * a.S * G, sg = (long long)a.S * G;
   const long long T = a.ctx.N > 0 && a.ctx_w ? (long long)a.ctx.cols * a.ctx.page_rows : 0;
   const long long L = a.own.N > 0 && a.own_w ? (long long)a.own.cols * a.own.page_rows : 0;
-  const int tile = 32 * kWeighKeys;
-  p.ctx_tiles = (int)((T + tile - 1) / tile);
-  p.own_tiles = (int)((L + tile - 1) / tile);
-  // waves enough for the chip, each with 128 rows at least
-  auto ranges = [](long long waves, long long rows) {
-    return (int)std::max(1LL, std::min({(2048 + waves - 1) / std::max(1LL, waves), rows / 128, 64LL}));
+  const long long bg = (long long)a.B * a.n_kv_heads, most = (1 << 24) - 1;
+  // Workgroups: key ranges until there are some for every compute unit, each of a tile a wave at least; then row ranges, of 128
+  // rows at least.
+  auto ranges = [&](long long sequences, long long keys, int tile, long long rows, int* by_key, int* by_row) {
+    const long long want = (1024 + sequences - 1) / sequences;
+    *by_key = (int)std::max(1LL, std::min({want, (keys + 4 * tile - 1) / (4 * tile), most / std::max(1LL, sequences)}));
+    *by_row = (int)std::max(1LL, std::min({want / *by_key, rows / 128, 64LL, most / std::max(1LL, sequences * *by_key)}));
   };
-  const long long bg = (long long)a.B * a.n_kv_heads;
-  p.ctx_splits = p.ctx_tiles ? ranges(bg * p.ctx_tiles, R) : 1;
-  p.own_splits = p.own_tiles ? ranges(bg * a.K * p.own_tiles, sg) : 1;
+  p.ctx_keys = p.ctx_splits = p.own_keys = p.own_splits = 1;
+  if (T) ranges(bg, T, 32, R, &p.ctx_keys, &p.ctx_splits);
+  if (L) ranges(bg * a.K, L, 32, sg, &p.own_keys, &p.own_splits);
+  p.keys_by_length = p.ctx_keys >= 8 && a.B > 1 && a.B <= 64 && T >= 512 * p.ctx_keys;
   p.ctx_bytes = p.ctx_splits > 1 ? (size_t)p.ctx_splits * bg * T * sizeof(float) : 0;
   p.own_bytes = p.own_splits > 1 ? (size_t)p.own_splits * bg * a.K * L * sizeof(float) : 0;
-  p.blocks = bg * p.ctx_splits * ((p.ctx_tiles + 3) / 4) + (bg * a.K * p.own_tiles * p.own_splits + 3) / 4;
+  p.blocks = (T ? bg * p.ctx_splits * p.ctx_keys : 0) + (L ? bg * a.K * p.own_splits * p.own_keys : 0);
   p.sum_blocks = std::max(p.ctx_splits > 1 ? (bg * T + 255) / 256 : 0, p.own_splits > 1 ? (bg * a.K * L + 255) / 256 : 0);
   return p;
 }
