@@ -1,7 +1,6 @@
 // Attention of a request's lists over rows held in 4 bits (fe_packed_attention), and the weight that every cached row
 // received (fe_packed_weights).
 #include <algorithm>
-#include <type_traits>
 
 #include "packed.h"
 
@@ -413,56 +412,6 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   };
 
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
-  // N 32-key blocks from row kb of the tiles on; element i of a lane is key 8 (i / 4) + 4 half + i % 4 of a block.  Products of
-  // all blocks first, one branch for the reference, then probabilities and products with the values: the chains overlap.
-  // mask(s) sets what the rows do not see to -infinity.
-  auto blocks = [&](auto count, const bf16* K, const bf16* V, int kb, auto mask) __attribute__((always_inline)) {
-    constexpr int N = decltype(count)::value;
-    f32x16 s[N];
-#pragma unroll
-    for (int u = 0; u < N; ++u) s[u] = f32x16{};
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int u = 0; u < N; ++u) s[u] = mma_held(L::rows(K, kb + 32 * u, d, rl), qf[d], s[u]);
-    mask(s);
-    float mx = m_run;
-#pragma unroll
-    for (int u = 0; u < N; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[u][i]), s[u][i + 1]);
-    // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
-    if (__any(mx > m_run + lag)) {
-      const float top = halves_max(mx);
-      if (top > m_run + lag) {
-        const float alpha = __builtin_amdgcn_exp2f((m_run - top) * sl2);
-        m_run = top;
-        l_run *= alpha;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[n] *= alpha;
-      }
-    }
-    const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], sl2, -ref));
-        sum[i & 3] += s[u][i];
-      }
-      l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        f32x8 w;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
-        const Op p = F::rounded(w);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 32 * u + 16 * m, n, cl), p, o[n]);
-      }
-    }
-  };
   const bool idle = r0 + wr * 32 >= a.R;
   if (grp >= nc) {                         // uniform: no shared chunk was under way
     find(grp);
@@ -481,43 +430,83 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     if (q >= nq || idle) continue;         // uniform
     rl = fresh(rl);
     cl = fresh(cl);
+    // NS blocks of 32 keys at a time, whose chains of products overlap; element i of a lane is key 8 (i / 4) + 4 half + i % 4 of
+    // a block.
     const bool own = q >= nc;
-    const bool any_hole = __builtin_amdgcn_readfirstlane(s_holes[grp][par]) == q;
     const int x1 = own ? (ob + q - nc) * KC : (cb + q) * KC;   // first key: packed own rows, or shared ones
-    if (!own && !any_hole && x1 + KC <= nctx) {          // uniform: every row sees every key
+    const int first = own ? wlo : 0, end = own ? whi : nctx, all_from = own ? alo : 0, all_to = own ? ahi : nctx;
+    const int holes = s_holes[grp][par], odds = s_odds[grp][par];
 #pragma unroll 1
-      for (int kb = 0; kb < KC; kb += 32 * NS)
-        blocks(std::integral_constant<int, NS>{}, K, V, kb, [](f32x16 (&)[NS]) {});
-    } else {
-      const bool odds = __builtin_amdgcn_readfirstlane(s_odds[grp][par]) == q;
-      const int first = own ? wlo : 0, end = own ? whi : nctx, all_from = own ? alo : 0, all_to = own ? ahi : nctx;
+    for (int kb = 0; kb < KC; kb += 32 * NS) {
+      const int x0 = x1 + kb;
+      if (x0 >= end) break;                // uniform
+      if (x0 + 32 * NS <= first) continue;
+      f32x16 s[NS];
+#pragma unroll
+      for (int u = 0; u < NS; ++u) s[u] = f32x16{};
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int u = 0; u < NS; ++u) s[u] = mma_held(L::rows(K, kb + 32 * u, d, rl), qf[d], s[u]);
+      if (x0 < all_from || x0 + 32 * NS > all_to) {      // uniform
+        const int from = (own ? lo : 0) - x0 - 4 * half, to = (own ? hi : nctx) - x0 - 4 * half;
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (32 * u + 8 * (i >> 2) + (i & 3) < from || 32 * u + 8 * (i >> 2) + (i & 3) >= to) s[u][i] = -INFINITY;
+      }
+      if (__builtin_amdgcn_readfirstlane(holes) == q) {  // uniform
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (s_hole[grp][par][kb + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3)] == q) s[u][i] = -INFINITY;
+      }
+      float mx = m_run;
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[u][i]), s[u][i + 1]);
+      // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
+      // Whether a row's moves depends on that row alone; the others are multiplied by 1.
+      if (__any(mx > m_run + lag)) {
+        const float top = halves_max(mx), next = top > m_run + lag ? top : m_run;
+        const float alpha = next == m_run ? 1.f : __builtin_amdgcn_exp2f((m_run - next) * sl2);
+        m_run = next;
+        l_run *= alpha;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n] *= alpha;
+      }
+      const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
+#pragma unroll
+      for (int u = 0; u < NS; ++u) {
+        float sum[4];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], sl2, -ref));
+          sum[i & 3] = i < 4 ? s[u][i] : sum[i & 3] + s[u][i];
+        }
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          f32x8 w;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
+          const Op p = F::rounded(w);
+#pragma unroll
+          for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 32 * u + 16 * m, n, cl), p, o[n]);
+        }
+      }
+      if (own && __builtin_amdgcn_readfirstlane(odds) == q) {
+        // uniform: the columns of a NaN block, in the rows that see its key
 #pragma unroll 1
-      for (int kb = 0; kb < KC; kb += 32) {
-        const int x0 = x1 + kb;
-        if (x0 >= end) break;              // uniform
-        if (x0 + 32 <= first) continue;
-        blocks(std::integral_constant<int, 1>{}, K, V, kb, [&](f32x16 (&s)[1]) __attribute__((always_inline)) {
-          if (x0 < all_from || x0 + 32 > all_to) {       // uniform
-            const int from = (own ? lo : 0) - x0 - 4 * half, to = (own ? hi : nctx) - x0 - 4 * half;
+        for (int e = 0; e < 32 * NS * UPR; ++e) {
+          const int x = x0 + e / UPR, n = e % UPR * UE / 32;
+          if (__builtin_amdgcn_readfirstlane(s_odd[grp][par][kb * UPR + e]) != q) continue;
+          const float nan = x < lo || x >= hi ? 0.f : NAN;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (8 * (i >> 2) + (i & 3) < from || 8 * (i >> 2) + (i & 3) >= to) s[0][i] = -INFINITY;
-          }
-          if (any_hole) {                  // uniform
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (s_hole[grp][par][kb + 8 * (i >> 2) + 4 * half + (i & 3)] == q) s[0][i] = -INFINITY;
-          }
-        });
-        if (odds) {                        // uniform: the columns of a NaN block, in the rows that see its key
-#pragma unroll 1
-          for (int e = 0; e < 32 * UPR; ++e) {
-            const int x = x0 + e / UPR, n = e % UPR * UE / 32;
-            if (__builtin_amdgcn_readfirstlane(s_odd[grp][par][kb * UPR + e]) != q || x < lo || x >= hi) continue;
-#pragma unroll
-            for (int y = 0; y < NB; ++y)
-              if (y == n) o[y] += f32x16{} + NAN;
-          }
+          for (int y = 0; y < NB; ++y) o[y] += y == n ? nan : 0.f;
         }
       }
     }
