@@ -1,6 +1,7 @@
 // Attention of a request's lists over rows held in 4 bits (fe_packed_attention), and the weight that every cached row
 // received (fe_packed_weights).
 #include <algorithm>
+#include <type_traits>
 
 #include "packed.h"
 
@@ -237,12 +238,14 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   typedef Tile<DH> L;
   constexpr int WK = C::WK, GT = C::GT, ROWS = C::ROWS, UPR = C::UPR, PER = C::PER, KC = C::KC, NBUF = C::NBUF;
   constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH, NS = C::NS;
+  static_assert(WR == 1 || (WK * 2 * KC >= 128 && WK * NBUF * 2 * TILE >= 4 * 64 * DH), "own rows by wave fit the tiles");
   static_assert(KC % (32 * NS) == 0 && 4 * 32 * DH * 4 - WR * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2, "the join fits the tiles");
   __shared__ __attribute__((aligned(16))) bf16 s_kv[WK][NBUF][2][TILE];
   __shared__ int s_off[ROWS + 1];
   // of a chunk (by its parity in the group): the last one with rows of no page, those rows; the last one with own values
   // of NaN, those units
   __shared__ int s_holes[WK][2], s_hole[WK][2][KC], s_odds[WK][2], s_odd[WK][2][KC * UPR];
+  __shared__ int s_wave_hole[4], s_wave_odd[4];         // ... of a wave's own rows
   __shared__ float s_ml[4][32][2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -258,20 +261,23 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   for (int i = tid; i < WK * 2 * KC; i += 256) (&s_hole[0][0][0])[i] = -1;
   for (int i = tid; i < WK * 2 * KC * UPR; i += 256) (&s_odd[0][0][0])[i] = -1;
   if (tid < WK * 2) (&s_holes[0][0])[tid] = (&s_odds[0][0])[tid] = -1;
+  if (tid < 4) s_wave_hole[tid] = s_wave_odd[tid] = -1;
 
   // This group's chunks: numbers q = grp + WK i of the range's share of the shared ones (from cb on) and, after these nc, of
   // the own ones (from ob on).  A thread's units of a chunk: their pages are looked up a chunk before they are loaded.
   const int nctx = ctx_rows(a, b), cctx = (nctx + KC - 1) / KC;
   const int cb = share(cctx, z, splits), nc = share(cctx, z + 1, splits) - cb;
-  u32x4 kc[PER], vc[PER];
-  unsigned ks[PER], vs[PER];
-  int entry[PER], rest[PER], list[PER];    // rest: row inside the page, -1 past the rows
+  constexpr int MOST = DH == 128 && PER < 2 ? 2 : PER;   // units of a thread, here or in own rows by wave
+  u32x4 kc[MOST], vc[MOST];
+  unsigned ks[MOST], vs[MOST];
+  int entry[MOST], rest[MOST], list[MOST]; // rest: row inside the page, -1 past the rows
   int page[PER], row_in[PER];              // of the next shared chunk
   int gone = 0, hole = 0;                  // bit p: does not count; as its page is none
   const int jump = a.ctx.cap ? packed_page(a.ctx, WK * KC) : 0, jump_rows = WK * KC - jump * a.ctx.page_rows;
 #pragma unroll
+  for (int p = 0; p < MOST; ++p) list[p] = 0;
+#pragma unroll
   for (int p = 0; p < PER; ++p) {
-    list[p] = 0;
     const int j = (cb + grp) * KC + (gt + p * GT) / UPR;
     page[p] = a.ctx.cap ? packed_page(a.ctx, j) : 0;
     row_in[p] = j - page[p] * a.ctx.page_rows;
@@ -293,32 +299,36 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
       }
     }
   };
-  auto load_from = [&](const auto& x) __attribute__((always_inline)) {
+  // Units of U codes, `threads` apart: a group's share of a chunk, or (own rows by wave) a lane's of a wave's 32 keys.
+  auto load_units = [&](const auto& x, auto width, auto count, int first, int threads) __attribute__((always_inline)) {
+    constexpr int U = decltype(width)::value, N = decltype(count)::value, ROW = DH / U;
     gone = hole = 0;
-    const unsigned all = (unsigned)x.page_rows * UPR;
+    const unsigned all = (unsigned)x.page_rows * ROW;
 #pragma unroll
-    for (int p = 0; p < PER; ++p) {
+    for (int p = 0; p < N; ++p) {
       const bool none = rest[p] >= 0 && (unsigned)entry[p] >= (unsigned)x.n_pages, skip = rest[p] < 0 || none;
       gone |= skip << p;
       hole |= none << p;
-      const unsigned u = (gt + p * GT) % UPR, at = (skip ? 0 : rest[p]) * UPR + u;   // what does not count reads row 0 of page 0
+      const unsigned u = (first + p * threads) % ROW, at = (skip ? 0 : rest[p]) * ROW + u;   // what does not count reads row 0 of page 0
       const char* head = x.pages + (unsigned long long)(skip ? 0u : (unsigned)entry[p]) * (unsigned)x.page_ld;
-      const unsigned k = (unsigned)g * x.head_bytes + at * (UE / 2), s = (unsigned)g * x.head_bytes + all * UE + (UE == 32 ? at : at >> 1);
-      if constexpr (UE == 32) {
+      const unsigned k = (unsigned)g * x.head_bytes + at * (U / 2), s = (unsigned)g * x.head_bytes + all * U + (U == 32 ? at : at >> 1);
+      if constexpr (U == 32) {
         kc[p] = ldv<u32x4>(head + k);
-        vc[p] = ldv<u32x4>(head + (k + all * (UE / 2)));
+        vc[p] = ldv<u32x4>(head + (k + all * (U / 2)));
       } else {
-        const uint2 kk = ldv<uint2>(head + k), vv = ldv<uint2>(head + (k + all * (UE / 2)));
+        const uint2 kk = ldv<uint2>(head + k), vv = ldv<uint2>(head + (k + all * (U / 2)));
         kc[p] = u32x4{kk.x, kk.y, 0, 0};
         vc[p] = u32x4{vv.x, vv.y, 0, 0};
       }
       ks[p] = *reinterpret_cast<const unsigned char*>(head + s);
-      vs[p] = *reinterpret_cast<const unsigned char*>(head + (s + (UE == 32 ? all : all >> 1)));
+      vs[p] = *reinterpret_cast<const unsigned char*>(head + (s + (U == 32 ? all : all >> 1)));
     }
   };
+  constexpr std::integral_constant<int, UE> kUnit{};
+  constexpr std::integral_constant<int, PER> kPer{};
   if (grp < nc) {                          // under way while the lists' lengths and packing are found
     find_ctx(grp);
-    load_from(a.ctx);
+    load_units(a.ctx, kUnit, kPer, gt, GT);
   }
 
   // this wave's rows
@@ -346,7 +356,10 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     if (s >= 0) nown += a.causal ? min(max(m - n + s + 1, 0), m) : m;
     nown = __builtin_amdgcn_readfirstlane(nown);
   }
-  const int cown = (nown + KC - 1) / KC, ob = share(cown, z, splits), nq = nc + share(cown, z + 1, splits) - ob;
+  // Own rows of long lists are taken as the shared ones are; of short ones, which few of the tile's rows see, every wave takes
+  // those of its rows' lists by itself, after the shared ones.
+  const bool by_wave = WR > 1 && 2 * a.S * a.G <= ROWS;
+  const int cown = by_wave ? 0 : (nown + KC - 1) / KC, ob = share(cown, z, splits), nq = nc + share(cown, z + 1, splits) - ob;
 
   Op qf[ND];
 #pragma unroll
@@ -361,15 +374,17 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
 #pragma unroll
   for (int n = 0; n < NB; ++n) o[n] = f32x16{};
 
-  auto find_own = [&](int q) __attribute__((always_inline)) {
+  // packed rows x0 + key of the units, below `to`
+  auto find_own = [&](int x0, int to, auto width, auto count, int first, int threads) __attribute__((always_inline)) {
+    constexpr int U = decltype(width)::value, N = decltype(count)::value, ROW = DH / U;
     const ArgsAgain A = args_again();
     const unsigned rows = A->own.page_rows;
     const int32_t* table = A->own.table + ((long long)b * A->K + k0) * A->own.cols;
 #pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const int x = (ob + q - nc) * KC + (gt + p * GT) / UPR;
+    for (int p = 0; p < N; ++p) {
+      const int x = x0 + (first + p * threads) / ROW;
       rest[p] = -1;
-      if (x < nown) {
+      if (x < to) {
         int i = list[p];
         while (s_off[i + 1] <= x) ++i;
         list[p] = i;
@@ -381,30 +396,34 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   };
   auto find = [&](int q) __attribute__((always_inline)) {
     if (q < nc) find_ctx(q);               // uniform
-    else if (q < nq) find_own(q);
+    else if (q < nq) find_own((ob + q - nc) * KC, nown, kUnit, kPer, gt, GT);
   };
   auto load = [&](int q) __attribute__((always_inline)) {
-    if (q < nc) load_from(a.ctx);          // uniform
-    else if (q < nq) load_from(args_again()->own);
+    if (q < nc) load_units(a.ctx, kUnit, kPer, gt, GT);          // uniform
+    else if (q < nq) load_units(args_again()->own, kUnit, kPer, gt, GT);
   };
-  auto stage = [&](bf16* K, bf16* V, int q, int par) __attribute__((always_inline)) {
+  // Puts the units into tiles K and V; marks rows of no page with `tag` in holes[key] and any_hole, and (own rows) values of
+  // NaN in odds[unit] and any_odd: NaN would reach the rows of other lists, as 0 times NaN, so they get zeros and the rows that
+  // see it get it at the end.
+  auto stage = [&](bf16* K, bf16* V, auto width, auto count, int first, int threads, bool own, int tag, int* holes, int* any_hole,
+                   int* odds, int* any_odd) __attribute__((always_inline)) {
+    constexpr int U = decltype(width)::value, N = decltype(count)::value, ROW = DH / U;
 #pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const int key = (gt + p * GT) / UPR, u = (gt + p * GT) % UPR;
+    for (int p = 0; p < N; ++p) {
+      const int key = (first + p * threads) / ROW, u = (first + p * threads) % ROW;
       float ku = unit_of(ks[p]), vu = unit_of(vs[p]);
       if (gone >> p & 1) {
         kc[p] = vc[p] = u32x4{0, 0, 0, 0};
         ku = vu = 1.f;
-        if (hole >> p & 1) s_hole[grp][par][key] = s_holes[grp][par] = q;
-      } else if (q >= nc && vs[p] == 255) {
-        // NaN would reach the rows of other lists, as 0 times NaN: they get zeros, the rows that see it get it at the end
+        if (hole >> p & 1) holes[key] = *any_hole = tag;
+      } else if (own && vs[p] == 255) {
         vc[p] = u32x4{0, 0, 0, 0};
         vu = 1.f;
-        s_odd[grp][par][key * UPR + u] = s_odds[grp][par] = q;
+        odds[key * ROW + u] = *any_odd = tag;
       }
-      const int base = L::at(key, u * (UE / 8));
+      const int base = L::at(key, u * (U / 8));
 #pragma unroll
-      for (int i = 0; i < UE / 8; ++i) {
+      for (int i = 0; i < U / 8; ++i) {
         *reinterpret_cast<bf16x8*>(K + (base ^ i << 3)) = values8(kc[p][i], ku);
         *reinterpret_cast<bf16x8*>(V + (base ^ i << 3)) = values8(vc[p][i], vu);
       }
@@ -412,6 +431,82 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   };
 
   int rl = L::row_lane(lane), cl = L::col_lane(lane);
+  // N blocks of 32 keys from row kb of the tiles on, key x0 the first of them, whose chains of products overlap; element i of a lane
+  // is key 8 (i / 4) + 4 half + i % 4 of a block.  The lane's row sees keys [from0, to0), all rows [all_from, all_to).
+  auto blocks = [&](auto number, auto width, const bf16* K, const bf16* V, int kb, int x0, bool own, int from0, int to0, int all_from,
+                    int all_to, int tag, const int* holes, int any_hole, const int* odds, int any_odd) __attribute__((always_inline)) {
+    constexpr int N = decltype(number)::value, U = decltype(width)::value, ROW = DH / U;
+    f32x16 s[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) s[u] = f32x16{};
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int u = 0; u < N; ++u) s[u] = mma_held(L::rows(K, kb + 32 * u, d, rl), qf[d], s[u]);
+    __builtin_amdgcn_s_setprio(0);
+    if (x0 < all_from || x0 + 32 * N > all_to) {      // uniform
+      const int from = from0 - x0 - 4 * half, to = to0 - x0 - 4 * half;
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * u + 8 * (i >> 2) + (i & 3) < from || 32 * u + 8 * (i >> 2) + (i & 3) >= to) s[u][i] = -INFINITY;
+    }
+    if (__builtin_amdgcn_readfirstlane(any_hole) == tag) {  // uniform
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (holes[kb + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3)] == tag) s[u][i] = -INFINITY;
+    }
+    float mx = m_run;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[u][i]), s[u][i + 1]);
+    // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
+    // Whether a row's moves depends on that row alone; the others are multiplied by 1.
+    if (__any(mx > m_run + lag)) {
+      const float top = halves_max(mx), next = top > m_run + lag ? top : m_run;
+      const float alpha = next == m_run ? 1.f : __builtin_amdgcn_exp2f((m_run - next) * sl2);
+      m_run = next;
+      l_run *= alpha;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) o[n] *= alpha;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      float sum[4];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], sl2, -ref));
+        sum[i & 3] = i < 4 ? s[u][i] : sum[i & 3] + s[u][i];
+      }
+      l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        f32x8 w;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
+        const Op p = F::rounded(w);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 32 * u + 16 * m, n, cl), p, o[n]);
+      }
+    }
+    if (own && __builtin_amdgcn_readfirstlane(any_odd) == tag) {
+      // uniform: the columns of a NaN block, in the rows that see its key
+#pragma unroll 1
+      for (int e = 0; e < 32 * N * ROW; ++e) {
+        const int x = x0 + e / ROW, n = e % ROW * U / 32;
+        if (__builtin_amdgcn_readfirstlane(odds[kb * ROW + e]) != tag) continue;
+        const float nan = x < lo || x >= hi ? 0.f : NAN;
+#pragma unroll
+        for (int y = 0; y < NB; ++y) o[y] += y == n ? nan : 0.f;
+      }
+    }
+  };
   const bool idle = r0 + wr * 32 >= a.R;
   if (grp >= nc) {                         // uniform: no shared chunk was under way
     find(grp);
@@ -422,7 +517,8 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   for (int it = 0; it < trips; ++it) {
     const int q = grp + it * WK, par = it & 1;
     bf16 *K = s_kv[grp][it % NBUF][0], *V = s_kv[grp][it % NBUF][1];
-    if (q < nq) stage(K, V, q, par);
+    const bool own = q >= nc;
+    if (q < nq) stage(K, V, kUnit, kPer, gt, GT, own, q, s_hole[grp][par], &s_holes[grp][par], s_odd[grp][par], &s_odds[grp][par]);
     load(q + WK);
     find(q + 2 * WK);
     if constexpr (WR > 1) lds_barrier();   // also the end of every wave's reads of the buffer written next
@@ -430,87 +526,46 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     if (q >= nq || idle) continue;         // uniform
     rl = fresh(rl);
     cl = fresh(cl);
-    // NS blocks of 32 keys at a time, whose chains of products overlap; element i of a lane is key 8 (i / 4) + 4 half + i % 4 of
-    // a block.
-    const bool own = q >= nc;
     const int x1 = own ? (ob + q - nc) * KC : (cb + q) * KC;   // first key: packed own rows, or shared ones
-    const int first = own ? wlo : 0, end = own ? whi : nctx, all_from = own ? alo : 0, all_to = own ? ahi : nctx;
-    const int holes = s_holes[grp][par], odds = s_odds[grp][par];
+    const int first = own ? wlo : 0, end = own ? whi : nctx;
+    const int any_hole = s_holes[grp][par], any_odd = s_odds[grp][par];
 #pragma unroll 1
     for (int kb = 0; kb < KC; kb += 32 * NS) {
       const int x0 = x1 + kb;
       if (x0 >= end) break;                // uniform
       if (x0 + 32 * NS <= first) continue;
-      f32x16 s[NS];
-#pragma unroll
-      for (int u = 0; u < NS; ++u) s[u] = f32x16{};
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int u = 0; u < NS; ++u) s[u] = mma_held(L::rows(K, kb + 32 * u, d, rl), qf[d], s[u]);
-      if (x0 < all_from || x0 + 32 * NS > all_to) {      // uniform
-        const int from = (own ? lo : 0) - x0 - 4 * half, to = (own ? hi : nctx) - x0 - 4 * half;
-#pragma unroll
-        for (int u = 0; u < NS; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (32 * u + 8 * (i >> 2) + (i & 3) < from || 32 * u + 8 * (i >> 2) + (i & 3) >= to) s[u][i] = -INFINITY;
-      }
-      if (__builtin_amdgcn_readfirstlane(holes) == q) {  // uniform
-#pragma unroll
-        for (int u = 0; u < NS; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (s_hole[grp][par][kb + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3)] == q) s[u][i] = -INFINITY;
-      }
-      float mx = m_run;
-#pragma unroll
-      for (int u = 0; u < NS; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[u][i]), s[u][i + 1]);
-      // The reference follows the running maximum once a score is 8 / log2(e) above it: a probability is at most 2^8 then.
-      // Whether a row's moves depends on that row alone; the others are multiplied by 1.
-      if (__any(mx > m_run + lag)) {
-        const float top = halves_max(mx), next = top > m_run + lag ? top : m_run;
-        const float alpha = next == m_run ? 1.f : __builtin_amdgcn_exp2f((m_run - next) * sl2);
-        m_run = next;
-        l_run *= alpha;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[n] *= alpha;
-      }
-      const float ref = m_run == -INFINITY ? 0.f : m_run * sl2;   // a row without keys so far: exp2(-inf) = 0
-#pragma unroll
-      for (int u = 0; u < NS; ++u) {
-        float sum[4];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], sl2, -ref));
-          sum[i & 3] = i < 4 ? s[u][i] : sum[i & 3] + s[u][i];
-        }
-        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          f32x8 w;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
-          const Op p = F::rounded(w);
-#pragma unroll
-          for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 32 * u + 16 * m, n, cl), p, o[n]);
-        }
-      }
-      if (own && __builtin_amdgcn_readfirstlane(odds) == q) {
-        // uniform: the columns of a NaN block, in the rows that see its key
-#pragma unroll 1
-        for (int e = 0; e < 32 * NS * UPR; ++e) {
-          const int x = x0 + e / UPR, n = e % UPR * UE / 32;
-          if (__builtin_amdgcn_readfirstlane(s_odd[grp][par][kb * UPR + e]) != q) continue;
-          const float nan = x < lo || x >= hi ? 0.f : NAN;
-#pragma unroll
-          for (int y = 0; y < NB; ++y) o[y] += y == n ? nan : 0.f;
-        }
-      }
+      blocks(std::integral_constant<int, NS>{}, kUnit, K, V, kb, x0, own, own ? lo : 0, own ? hi : nctx, own ? alo : 0,
+             own ? ahi : nctx, q, s_hole[grp][par], any_hole, s_odd[grp][par], any_odd);
     }
     if constexpr (WR == 1) order();        // this chunk's reads before the next one's writes
+  }
+  if (WR > 1 && by_wave) {                 // uniform
+    // the wave's packed rows [wlo, whi) in chunks of 32, in tiles of its own; rows of the tile's other waves do not matter here
+    constexpr std::integral_constant<int, DH == 32 ? 16 : 32> width{};
+    constexpr std::integral_constant<int, DH == 128 ? 2 : 1> count{};
+    const int chunks = max(whi - wlo + 31, 0) / 32, c1 = share(chunks, z + 1, splits);
+    int c = share(chunks, z, splits) + grp;
+    bf16 *K = &s_kv[0][0][0][0] + wave * 64 * DH, *V = K + 32 * DH;
+    int *holes = &s_hole[0][0][0] + wave * 32, *odds = &s_odd[0][0][0] + wave * (32 * (DH / width.value));
+    int *any_hole = &s_wave_hole[wave], *any_odd = &s_wave_odd[wave];
+#pragma unroll
+    for (int p = 0; p < count.value; ++p) list[p] = __builtin_amdgcn_readlane(row.k - k0, 0);
+    if (c < c1) find_own(wlo + 32 * c, whi, width, count, lane, 64);
+    if (c < c1) load_units(args_again()->own, width, count, lane, 64);
+    if (c + WK < c1) find_own(wlo + 32 * (c + WK), whi, width, count, lane, 64);
+    __syncthreads();                       // the shared chunks are no longer read, nor their marks
+    for (int i = lane; i < 32 * (1 + DH / width.value); i += 64) (i < 32 ? holes[i] : odds[i - 32]) = -1;
+    order();
+    for (; c < c1; c += WK) {
+      stage(K, V, width, count, lane, 64, true, c, holes, any_hole, odds, any_odd);
+      if (c + WK < c1) load_units(args_again()->own, width, count, lane, 64);
+      if (c + 2 * WK < c1) find_own(wlo + 32 * (c + 2 * WK), whi, width, count, lane, 64);
+      order();
+      rl = fresh(rl);
+      cl = fresh(cl);
+      blocks(std::integral_constant<int, 1>{}, width, K, V, 0, wlo + 32 * c, true, lo, hi, alo, ahi, c, holes, *any_hole, odds, *any_odd);
+      order();
+    }
   }
 
   float l = halves_sum(l_run);
