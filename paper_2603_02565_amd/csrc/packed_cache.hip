@@ -240,9 +240,9 @@ __global__ __launch_bounds__(256) void k_packed_read(fe_packed_read_args a, Pack
   if (a.v) put8(static_cast<T*>(a.v) + row * a.v_ld + h * a.dh + 8 * x, v);
 }
 
-// The order of weights as that of integers, the greatest first; NaN below every number; both zeros are equal.
+// The order of weights as that of integers; NaN (1) below every number, both zeros equal.  0 is left for what is no candidate.
 FE_DEV unsigned order_of(float w) {
-  if (w != w) return 0;
+  if (w != w) return 1;
   const unsigned b = __float_as_uint(w == 0.f ? 0.f : w);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args
   if (tid < 64) {
     const float* w = a.weight + (long long)blockIdx.x * from.cap;
     float v[E];
-    unsigned o[E];                         // 0: a NaN, or no candidate
+    unsigned o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = e * 64 + lane < n ? w[e * 64 + lane] : 0.f;
 #pragma unroll
@@ -348,8 +348,8 @@ __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args
 
 // Selects a (sequence, key head)'s rows.  Four passes over 8 bits each find the m-th greatest order among the candidates:
 // a histogram in LDS, in 32 copies by lane so that equal digits, the rule among weights, do not meet in one word.  Then
-// every wave walks its rows in order and numbers what is kept.  Rows (NW * 64 * E a segment) stay in registers
-// where one segment holds the sequence.
+// every wave walks its rows in order and numbers what is kept.  The orders of 1024 E rows stay in registers where they are
+// all.  What is no candidate has order 0, below all of them, and is counted with them to no effect.
 template <int E>
 __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
   constexpr int NW = 16, NT = NW * 64, SEG = NT * E;
@@ -362,37 +362,38 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
   const int lo = first, hi = n - recent, segments = (n + SEG - 1) / SEG;
   const float* w = a.weight + (long long)blockIdx.x * from.cap;
   int32_t* kept = a.kept + (long long)blockIdx.x * a.keep;
-  float* out = a.weight_out ? a.weight_out + (long long)blockIdx.x * to.cap : nullptr;
 
   if (h == 0) evict_state<NW>(a, from, to, s, n, m);
   for (int i = m + tid; i < a.keep; i += NT) kept[i] = -1;
 
-  float v[E];
+  const bool all = m == n;                 // uniform
+  unsigned o[E];
   auto index = [&](int seg, int e) { return seg * SEG + (wave * E + e) * 64 + lane; };
   auto load = [&](int seg) __attribute__((always_inline)) {
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = w[min(index(seg, e), n - 1)];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int i = index(seg, e);
-      v[e] = i < n ? w[i] : 0.f;
+      o[e] = i >= lo && i < hi ? order_of(v[e]) : 0;
     }
   };
-  unsigned cut = 0;                        // orders above it are kept, and `left` of those equal to it
+  unsigned cut = 0xffffffffu;              // orders above it are kept, and `left` of those equal to it; none is as great
   int left = m - first - recent;
-  const bool all = m == n;                 // uniform
   if (segments == 1) load(0);
   if (!all && left > 0) {
+    cut = 0;
+#pragma unroll 1
     for (int shift = 24; shift >= 0; shift -= 8) {
       for (int i = tid; i < 256 * 32; i += NT) s_hist[i] = 0;
       __syncthreads();
       for (int seg = 0; seg < segments; ++seg) {
         if (segments > 1) load(seg);
+        const unsigned differ = shift == 24 ? 0xffffffffu : (1u << (shift + 8)) - 1;   // a digit counts below the cut's
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int i = index(seg, e);
-          const unsigned o = order_of(v[e]);
-          if (i >= lo && i < hi && (shift == 24 || o >> (shift + 8) == cut >> (shift + 8)))
-            atomicAdd(&s_hist[(o >> shift & 255) * 32 + (lane & 31)], 1);
-        }
+        for (int e = 0; e < E; ++e)
+          if ((o[e] ^ cut) <= differ) atomicAdd(&s_hist[(o[e] >> shift & 255) * 32 + (lane & 31)], 1);
       }
       __syncthreads();
       {                                    // four threads a digit, each from another bank
@@ -429,25 +430,19 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
       cut |= (unsigned)s_digit << shift;
       left = s_left;
     }
-  } else if (!all) {
-    cut = 0xffffffffu;                     // no order is as great
   }
 
+  // certain: rows outside the candidates, and candidates above the cut; all of them where nothing is left out
+  const int sure_lo = all ? n : lo, sure_hi = all ? 0 : hi;
   int kept_before = 0, equal_before = 0;   // in the segments before
   for (int seg = 0; seg < segments; ++seg) {
     if (segments > 1) load(seg);
     int n_kept = 0, n_equal = 0;           // the wave's: certain ones, and candidates equal to the cut
-    unsigned certain = 0, equal = 0;       // bit e
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int i = index(seg, e);
-      const unsigned o = order_of(v[e]);
-      const bool inside = i >= lo && i < hi;
-      const bool sure = i < n && (all || !inside || o > cut), same = !all && inside && o == cut;
-      certain |= (unsigned)sure << e;
-      equal |= (unsigned)same << e;
-      n_kept += __popcll(__ballot(sure));
-      n_equal += __popcll(__ballot(same));
+      n_kept += __popcll(__ballot((i < sure_lo || i >= sure_hi) && i < n) | __ballot(o[e] > cut));
+      n_equal += __popcll(__ballot(o[e] == cut));
     }
     if (lane == 0) {
       s_kept[wave] = n_kept;
@@ -460,18 +455,18 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
       ks += s_kept[x];
       es += s_equal[x];
     }
-    const unsigned long long below = (1ull << lane) - 1;
     int at = k0 + min(e0, left);           // of the equal ones the first `left` are kept
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const bool same = equal >> e & 1;
-      const unsigned long long eq = __ballot(same);
-      const bool take = certain >> e & 1 || (same && e0 + __popcll(eq & below) < left);
-      const unsigned long long got = __ballot(take);
-      if (take) {
-        const int d = at + __popcll(got & below);
-        kept[d] = index(seg, e);
-        if (out) out[d] = v[e];
+      int i = index(seg, e);
+      asm volatile("" : "+v"(o[e]), "+v"(i));            // ballots are made again: kept, they would not fit the scalar registers
+      const unsigned long long eq = __ballot(o[e] == cut);
+      unsigned long long got = __ballot((i < sure_lo || i >= sure_hi) && i < n) | __ballot(o[e] > cut);
+      if (eq)                              // uniform
+        got |= __ballot((eq >> lane & 1) && e0 + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(eq >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)eq, 0)) < left);
+      if (got >> lane & 1) {
+        const int d = at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(got >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)got, 0));
+        kept[d] = i;
       }
       at += __popcll(got);
       e0 += __popcll(eq);
@@ -482,13 +477,16 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
   }
 }
 
-// The kept rows: a thread takes one block, of keys and of values.
+// The kept rows: a thread takes one block, of keys and of values, the first of a row its weight as well.
 __global__ __launch_bounds__(256) void k_packed_move(fe_packed_evict_args a, PackedCache from, PackedCache to, int blocks) {
   const int sh = blockIdx.x / blocks, blk = blockIdx.x % blocks, s = sh / a.n_kv_heads, h = sh - s * a.n_kv_heads;
   const int log_blocks = a.dh == 32 ? 0 : a.dh == 64 ? 1 : 2;
   const int m = min(a.keep, packed_len(from, s));
   const int e = blk * 256 + threadIdx.x, i = e >> log_blocks, x = e & ((1 << log_blocks) - 1);
-  if (i < m) move_block(from, to, s, h, log_blocks, i, a.kept[(long long)sh * a.keep + i], x);
+  if (i >= m) return;
+  const int j = a.kept[(long long)sh * a.keep + i];
+  if (x == 0 && a.weight_out) a.weight_out[(long long)sh * to.cap + i] = a.weight[(long long)sh * from.cap + j];
+  move_block(from, to, s, h, log_blocks, i, j, x);
 }
 
 }  // namespace
