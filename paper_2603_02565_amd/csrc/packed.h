@@ -51,7 +51,7 @@ struct PackedArgs {
   float *part_ctx, *part_own;            // [splits][N][Hkv][cap]
 };
 
-struct PackedPlan { int waves, tiles, splits, by_length, own_chunks; size_t part_bytes; };   // waves: those that share a chunk
+struct PackedPlan { int waves, wide, tiles, splits, by_length, own_chunks; size_t part_bytes; };   // waves: those that share a chunk
 PackedPlan packed_plan(const fe_packed_args& a);
 struct PackedWeighPlan {
   int ctx_keys, own_keys, ctx_splits, own_splits, keys_by_length;

@@ -2,6 +2,8 @@
 // received (fe_packed_weights).
 #include <algorithm>
 #include <type_traits>
+#include <cstdlib>
+static int env(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 
 #include "packed.h"
 
@@ -140,21 +142,31 @@ FE_DEV bool range_of(const PackedArgs& a, int range, int more, int& b, int& z, i
 
 // The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
 // their number; a list without query rows contributes none.  nb <= 128.  Every wave writes the same; a barrier follows.
-FE_DEV void pack_own(const PackedArgs& a, int b, int k0, int nb, int* off) {
-  const int lane = threadIdx.x & 63;
-  auto own = [&](int i) { return i < nb && q_rows(a, b * a.K + k0 + i) > 0 ? own_rows(a, b * a.K + k0 + i) : 0; };
-  const int u = own(2 * lane);
-  int v = u + own(2 * lane + 1);
-  const int both = v;
+struct Packing {
+  int n[2];                                // own rows of lists 2 lane and 2 lane + 1
+  FE_DEV void load(const PackedArgs& a, int b, int k0, int nb) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int x = __shfl_up(v, m);
-    if (lane >= m) v += x;
+    for (int x = 0; x < 2; ++x) {
+      const int bk = b * a.K + k0 + min(2 * lane + x, nb - 1);
+      const int q = q_rows(a, bk), m = own_rows(a, bk);
+      n[x] = 2 * lane + x < nb && q > 0 ? m : 0;
+    }
   }
-  if (lane == 0) off[0] = 0;
-  if (2 * lane < nb) off[2 * lane + 1] = v - both + u;
-  if (2 * lane + 1 < nb) off[2 * lane + 2] = v;
-}
+  FE_DEV void store(int nb, int* off) const {
+    const int lane = threadIdx.x & 63;
+    int v = n[0] + n[1];
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      if (m >= nb) break;                  // uniform
+      const int x = __shfl_up(v, m);
+      if (lane >= m) v += x;
+    }
+    if (lane == 0) off[0] = 0;
+    if (2 * lane < nb) off[2 * lane + 1] = v - n[1];
+    if (2 * lane + 1 < nb) off[2 * lane + 2] = v;
+  }
+};
 
 // Share z of `splits` of n things: the first n % splits shares have one more.
 FE_DEV int share(int n, int z, int splits) {
@@ -220,8 +232,8 @@ FE_DEV void order() { asm volatile("" ::: "memory"); }   // LDS operations of on
 // Scores are formed transposed (keys x rows), so that a lane holds 16 keys of one row in the operand layout of the
 // product with the values.  With WK > 1 the groups' sums are joined in LDS at the end.
 // ------------------------------------------------------------------------------------------
-template <typename T, int DH, int WR, int UE> struct Shape {
-  static constexpr int WK = 4 / WR, GT = 64 * WR, ROWS = 32 * WR, UPR = DH / UE;
+template <typename T, int DH, int WR, int UE, int W> struct Shape {
+  static constexpr int WK = W / WR, GT = 64 * WR, ROWS = 32 * WR, UPR = DH / UE;
   static constexpr int PER = 32 * UPR > GT ? 32 * UPR / GT : 1, KC = GT * PER / UPR;
   static constexpr int NBUF = WR > 1 ? 2 : 1, ND = DH / 16, NB = DH / 32;
   static constexpr int NS = KC >= 64 && sizeof(T) == 2 ? 2 : 1;   // 32-key blocks at a time
@@ -230,23 +242,23 @@ constexpr int fwd_waves(int bytes, int dh, int wr) {
   return dh == 128 ? (bytes == 4 ? 1 : 2) : dh == 64 ? (bytes == 4 ? 2 : 3) : bytes == 4 ? 3 : 4;
 }
 
-template <typename T, int DH, int WR, int UE>
-__global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fwd(PackedArgs a) {
-  typedef Shape<T, DH, WR, UE> C;
+template <typename T, int DH, int WR, int UE, int W>
+__global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR)) void k_packed_fwd(PackedArgs a) {
+  typedef Shape<T, DH, WR, UE, W> C;
   typedef Form<T> F;
   typedef typename F::Op Op;
   typedef Tile<DH> L;
   constexpr int WK = C::WK, GT = C::GT, ROWS = C::ROWS, UPR = C::UPR, PER = C::PER, KC = C::KC, NBUF = C::NBUF;
   constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH, NS = C::NS;
   static_assert(WR == 1 || (WK * 2 * KC >= 128 && WK * NBUF * 2 * TILE >= 4 * 64 * DH), "own rows by wave fit the tiles");
-  static_assert(KC % (32 * NS) == 0 && 4 * 32 * DH * 4 - WR * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2, "the join fits the tiles");
+  static_assert(KC % (32 * NS) == 0 && (WK == 1 || W * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2), "the join fits the tiles");
   __shared__ __attribute__((aligned(16))) bf16 s_kv[WK][NBUF][2][TILE];
   __shared__ int s_off[ROWS + 1];
   // of a chunk (by its parity in the group): the last one with rows of no page, those rows; the last one with own values
   // of NaN, those units
   __shared__ int s_holes[WK][2], s_hole[WK][2][KC], s_odds[WK][2], s_odd[WK][2][KC * UPR];
   __shared__ int s_wave_hole[4], s_wave_odd[4];         // ... of a wave's own rows
-  __shared__ float s_ml[4][32][2];
+  __shared__ float s_ml[W][32][2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave / WR, wr = wave % WR, gt = tid % GT, half = lane >> 5, c32 = lane & 31;
@@ -258,8 +270,19 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   if (a.by_length && !range_of(a, range, a.own_chunks, b, z, splits)) return;   // uniform
   const int r0 = t * ROWS, r1 = min(r0 + ROWS, a.R);
   const int k0 = quotient(a.by_sg, r0), nb = quotient(a.by_sg, r1 - 1) - k0 + 1;
-  for (int i = tid; i < WK * 2 * KC; i += 256) (&s_hole[0][0][0])[i] = -1;
-  for (int i = tid; i < WK * 2 * KC * UPR; i += 256) (&s_odd[0][0][0])[i] = -1;
+  // what needs only the sizes to be found is under way first: the lists' lengths, this wave's rows
+  Packing packing;
+  packing.load(a, b, k0, nb);
+  const Row row = row_of(a, b, g, r0 + wr * 32 + c32);
+  typename F::V qreg[ND];
+  {
+    const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH + 8 * half;
+#pragma unroll
+    for (int c = 0; c < ND; ++c) qreg[c] = ldv<typename F::V>(Q + 16 * c);
+  }
+  const int last_q = q_rows(a, b * a.K + k0 + nb - 1), last_own = own_rows(a, b * a.K + k0 + nb - 1);
+  for (int i = tid; i < WK * 2 * KC; i += 64 * W) (&s_hole[0][0][0])[i] = -1;
+  for (int i = tid; i < WK * 2 * KC * UPR; i += 64 * W) (&s_odd[0][0][0])[i] = -1;
   if (tid < WK * 2) (&s_holes[0][0])[tid] = (&s_odds[0][0])[tid] = -1;
   if (tid < 4) s_wave_hole[tid] = s_wave_odd[tid] = -1;
 
@@ -331,15 +354,7 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     load_units(a.ctx, kUnit, kPer, gt, GT);
   }
 
-  // this wave's rows
-  const Row row = row_of(a, b, g, r0 + wr * 32 + c32);
-  typename F::V qreg[ND];
-  {
-    const T* Q = static_cast<const T*>(a.q) + row.at * a.q_ld + row.h * DH + 8 * half;
-#pragma unroll
-    for (int c = 0; c < ND; ++c) qreg[c] = ldv<typename F::V>(Q + 16 * c);
-  }
-  pack_own(a, b, k0, nb, s_off);
+  packing.store(nb, s_off);
   __syncthreads();
   const int lo = s_off[row.k - k0], hi = lo + row.own;   // the packed own rows that the row sees
   // Of the wave, uniform: bounds of what its rows see, and (empty where they belong to several lists) what all of them see.
@@ -351,9 +366,8 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
   // the tile's packed rows end with what the last list's last live row in it sees
   int nown = s_off[nb - 1];
   {
-    const int bk = b * a.K + k0 + nb - 1, n = q_rows(a, bk), m = own_rows(a, bk);
-    const int s = min(quotient(a.by_g, r1 - 1 - (k0 + nb - 1) * a.S * a.G), n - 1);
-    if (s >= 0) nown += a.causal ? min(max(m - n + s + 1, 0), m) : m;
+    const int s = min(quotient(a.by_g, r1 - 1 - (k0 + nb - 1) * a.S * a.G), last_q - 1);
+    if (s >= 0) nown += a.causal ? min(max(last_own - last_q + s + 1, 0), last_own) : last_own;
     nown = __builtin_amdgcn_readfirstlane(nown);
   }
   // Own rows of long lists are taken as the shared ones are; of short ones, which few of the tile's rows see, every wave takes
@@ -568,82 +582,67 @@ __global__ __launch_bounds__(256, fwd_waves(sizeof(T), DH, WR)) void k_packed_fw
     }
   }
 
-  float l = halves_sum(l_run);
-  if constexpr (WK > 1) {                  // joins the groups in their order: group 0's waves hold the sums
+  const float l_all = halves_sum(l_run);
+  const bool in = r0 + wr * 32 + c32 < a.R;
+  const long long ro = row.at * a.Hq + row.h;
+  // Slice i of a lane: columns 8 i + 4 half .. + 3, v its sums against reference m (in units of 1 / sl2).
+  auto store = [&](int i, f32x4 v, float m, float l) __attribute__((always_inline)) {
+    const float m2 = m * sl2;
+    if (a.splits > 1) {
+      const long long at = ro + (long long)(range - b) * a.K * a.S * a.Hq;   // [range][row of the request]
+      *reinterpret_cast<f32x4*>(a.part_o + at * DH + 8 * i + 4 * half) = v;
+      if (i == 0 && half == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = float2{m2, l};
+      return;
+    }
+    const bool none = !row.live || l == 0.f;   // no key; a NaN score leaves a NaN sum
+    const float inv = none ? 0.f : 1.f / l;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 w;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) w[x] = from_f32<T>(none ? 0.f : v[x] * inv);
+    *reinterpret_cast<T4*>(static_cast<T*>(a.out) + row.at * a.out_ld + row.h * DH + 8 * i + 4 * half) = w;
+    if (a.lse && i == 0 && half == 0) a.lse[ro] = none ? -INFINITY : (m2 + log2f(l)) * kLn2;
+  };
+  auto slice = [&](int i) __attribute__((always_inline)) {
+    const f32x16 v = o[i >> 2];
+    return f32x4{v[4 * (i & 3)], v[4 * (i & 3) + 1], v[4 * (i & 3) + 2], v[4 * (i & 3) + 3]};
+  };
+  if constexpr (WK == 1) {
+    if (!in) return;
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i) store(i, slice(i), m_run, l_all);
+  } else {                                 // joins the groups in their order, every group some of the slices
     __syncthreads();
     float* X = reinterpret_cast<float*>(s_kv);
-    constexpr int LANE = 16 * NB;          // floats of a lane
-    if (grp > 0) {
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<f32x4*>(X + ((wave - WR) * LANE + 16 * n + 4 * q) * 64 + 4 * lane) =
-              f32x4{o[n][4 * q], o[n][4 * q + 1], o[n][4 * q + 2], o[n][4 * q + 3]};
-      if (half == 0) {
-        s_ml[wave][c32][0] = m_run;
-        s_ml[wave][c32][1] = l;
-      }
+    for (int i = 0; i < 4 * NB; ++i) *reinterpret_cast<f32x4*>(X + ((wave * 4 * NB + i) * 64 + lane) * 4) = slice(i);
+    if (half == 0) {
+      s_ml[wave][c32][0] = m_run;
+      s_ml[wave][c32][1] = l_all;
     }
     __syncthreads();
-    if (grp > 0) return;
-    float top = m_run;
+    if (!in) return;
+    float top = -INFINITY, l = 0.f, f[WK];
 #pragma unroll
-    for (int w = 1; w < WK; ++w) top = fmaxf(top, s_ml[w * WR + wr][c32][0]);
+    for (int w = 0; w < WK; ++w) top = fmaxf(top, s_ml[w * WR + wr][c32][0]);
     const float ref = top == -INFINITY ? 0.f : top;
-    float f = __builtin_amdgcn_exp2f((m_run - ref) * sl2);
-    l *= f;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) o[n] *= f;
-#pragma unroll
-    for (int w = 1; w < WK; ++w) {
-      const int other = w * WR + wr;
-      f = __builtin_amdgcn_exp2f((s_ml[other][c32][0] - ref) * sl2);
-      l = fmaf(s_ml[other][c32][1], f, l);
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 v = ldv<f32x4>(X + ((other - WR) * LANE + 16 * n + 4 * q) * 64 + 4 * lane);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[n][4 * q + i] = fmaf(v[i], f, o[n][4 * q + i]);
-        }
+    for (int w = 0; w < WK; ++w) {
+      f[w] = __builtin_amdgcn_exp2f((s_ml[w * WR + wr][c32][0] - ref) * sl2);
+      l = fmaf(s_ml[w * WR + wr][c32][1], f[w], l);
     }
-    m_run = top;
+#pragma unroll 1
+    for (int i = grp; i < 4 * NB; i += WK) {
+      f32x4 v{};
+#pragma unroll
+      for (int w = 0; w < WK; ++w) {
+        const f32x4 x = ldv<f32x4>(X + (((w * WR + wr) * 4 * NB + i) * 64 + lane) * 4);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) v[y] = fmaf(x[y], f[w], v[y]);
+      }
+      store(i, v, top, l);
+    }
   }
-
-  if (r0 + wr * 32 + c32 >= a.R) return;
-  const float m2 = m_run * sl2;
-  const long long ro = row.at * a.Hq + row.h;
-  if (a.splits > 1) {
-    const long long at = ro + (long long)(range - b) * a.K * a.S * a.Hq;   // [range][row of the request]
-    float* po = a.part_o + at * DH;
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(po + 32 * n + 8 * q + 4 * half) =
-            f32x4{o[n][4 * q], o[n][4 * q + 1], o[n][4 * q + 2], o[n][4 * q + 3]};
-    if (half == 0) {
-      a.part_ml[at * 2] = m2;
-      a.part_ml[at * 2 + 1] = l;
-    }
-    return;
-  }
-  const bool none = !row.live || l == 0.f;   // no key; a NaN score leaves a NaN sum
-  const float inv = none ? 0.f : 1.f / l;
-  T* out = static_cast<T*>(a.out) + row.at * a.out_ld + row.h * DH + 4 * half;
-#pragma unroll
-  for (int n = 0; n < NB; ++n)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      typedef T T4 __attribute__((ext_vector_type(4)));
-      T4 v;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(none ? 0.f : o[n][4 * q + i] * inv);
-      *reinterpret_cast<T4*>(out + 32 * n + 8 * q) = v;
-    }
-  if (a.lse && half == 0) a.lse[ro] = none ? -INFINITY : (m2 + log2f(l)) * kLn2;
 }
 
 // Joins the key ranges of a row in ascending order: DH / 4 threads a row.
@@ -922,16 +921,14 @@ __global__ __launch_bounds__(256) void k_packed_weigh_sum(PackedCache x, int Hkv
   out[at] = w[at] + v;
 }
 
-template <typename T, int DH, int UE>
-void fwd_tiles(const PackedArgs& a, const PackedPlan& p, dim3 grid, hipStream_t s) {
-  if (p.waves == 1) hipLaunchKernelGGL((k_packed_fwd<T, DH, 1, UE>), grid, dim3(256), 0, s, a);
-  else if (p.waves == 2) hipLaunchKernelGGL((k_packed_fwd<T, DH, 2, UE>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_packed_fwd<T, DH, 4, UE>), grid, dim3(256), 0, s, a);
-}
-template <typename T, int DH, int UE>
+template <typename T, int DH>
 hipError_t fwd(const PackedArgs& a, const PackedPlan& p, hipStream_t s) {
+  constexpr int UE = DH == 128 ? 32 : 16, U1 = DH == 32 ? 16 : 32, W1 = DH == 128 || sizeof(T) == 4 ? 8 : 16;
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.splits * a.tiles));
-  fwd_tiles<T, DH, UE>(a, p, grid, s);
+  if (p.waves == 1 && p.wide) hipLaunchKernelGGL((k_packed_fwd<T, DH, 1, U1, W1>), grid, dim3(64 * W1), 0, s, a);
+  else if (p.waves == 1) hipLaunchKernelGGL((k_packed_fwd<T, DH, 1, U1, 4>), grid, dim3(256), 0, s, a);
+  else if (p.waves == 2) hipLaunchKernelGGL((k_packed_fwd<T, DH, 2, UE, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_packed_fwd<T, DH, 4, UE, 4>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const long long n = (long long)a.B * a.K * a.S * a.Hq * (DH / 4);
@@ -968,8 +965,10 @@ PackedPlan packed_plan(const fe_packed_args& a) {
   const long long L = a.own.N > 0 ? (long long)a.own.cols * a.own.page_rows : 0;
   const long long own = std::min<long long>(a.K, (rows - 1) / sg + 2) * L, wgs = bg * p.tiles;
   const long long items = (T + 63) / 64 + (own + 63) / 64;
-  long long want = (512 + wgs - 1) / wgs;                       // two workgroups a compute unit
-  want = std::min(want, std::max(1LL, items / 4));
+  p.wide = p.waves == 1 && wgs < env("WIDE", 512) && (a.dtype == FE_BF16 || a.dh < 128);
+  long long want = (env("WANT", 512) + wgs - 1) / wgs;                       // two workgroups a compute unit
+  if (p.wide) want = (env("WANTW", 256) + wgs - 1) / wgs;
+  want = std::min(want, std::max(1LL, items / (p.wide ? env("IT", 32) : env("ITN", 4))));
   if (a.dtype == FE_F32) want = std::max(want, (items + 31) / 32);   // fp32 sums over at most 2048 keys
   const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);
   p.splits = (int)std::max(1LL, std::min({want, 256LL, grid}));
@@ -1005,8 +1004,8 @@ PackedWeighPlan packed_weigh_plan(const fe_packed_args& a) {
 }
 
 hipError_t launch_packed_attention(const PackedArgs& a, int dh, bool bf16_rows, const PackedPlan& p, hipStream_t s) {
-  if (bf16_rows) return dh == 32 ? fwd<bf16, 32, 16>(a, p, s) : dh == 64 ? fwd<bf16, 64, 16>(a, p, s) : fwd<bf16, 128, 32>(a, p, s);
-  return dh == 32 ? fwd<float, 32, 16>(a, p, s) : dh == 64 ? fwd<float, 64, 16>(a, p, s) : fwd<float, 128, 32>(a, p, s);
+  if (bf16_rows) return dh == 32 ? fwd<bf16, 32>(a, p, s) : dh == 64 ? fwd<bf16, 64>(a, p, s) : fwd<bf16, 128>(a, p, s);
+  return dh == 32 ? fwd<float, 32>(a, p, s) : dh == 64 ? fwd<float, 64>(a, p, s) : fwd<float, 128>(a, p, s);
 }
 
 hipError_t launch_packed_weights(const PackedArgs& a, int dh, bool bf16_rows, hipStream_t s) {
