@@ -143,7 +143,7 @@ FE_DEV bool range_of(const PackedArgs& a, int range, int more, int& b, int& z, i
 // The packed own rows of lists k0 .. k0 + nb - 1 of request b: off[i] = first packed row of list k0 + i, off[nb] =
 // their number; a list without query rows contributes none.  nb <= 128.  Every wave writes the same; a barrier follows.
 struct Packing {
-  int n[2];                                // own rows of lists 2 lane and 2 lane + 1
+  int n[2], end[2];                        // own rows of lists 2 lane and 2 lane + 1; their ends, past the last list out of reach
   FE_DEV void load(const PackedArgs& a, int b, int k0, int nb) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -153,7 +153,7 @@ struct Packing {
       n[x] = 2 * lane + x < nb && q > 0 ? m : 0;
     }
   }
-  FE_DEV void store(int nb, int* off) const {
+  FE_DEV void store(int nb, int* off) {
     const int lane = threadIdx.x & 63;
     int v = n[0] + n[1];
 #pragma unroll
@@ -165,6 +165,11 @@ struct Packing {
     if (lane == 0) off[0] = 0;
     if (2 * lane < nb) off[2 * lane + 1] = v - n[1];
     if (2 * lane + 1 < nb) off[2 * lane + 2] = v;
+    end[0] = 2 * lane < nb ? v - n[1] : 0x7fffffff;
+    end[1] = 2 * lane + 1 < nb ? v : 0x7fffffff;
+  }
+  FE_DEV int list(int x) const {           // that packed row x, the same in all lanes, lies in
+    return __popcll(__ballot(end[0] <= x)) + __popcll(__ballot(end[1] <= x));
   }
 };
 
@@ -293,12 +298,10 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
   constexpr int MOST = DH == 128 && PER < 2 ? 2 : PER;   // units of a thread, here or in own rows by wave
   u32x4 kc[MOST], vc[MOST];
   unsigned ks[MOST], vs[MOST];
-  int entry[MOST], rest[MOST], list[MOST]; // rest: row inside the page, -1 past the rows
+  int entry[MOST], rest[MOST];             // rest: row inside the page, -1 past the rows
   int page[PER], row_in[PER];              // of the next shared chunk
   int gone = 0, hole = 0;                  // bit p: does not count; as its page is none
   const int jump = a.ctx.cap ? packed_page(a.ctx, WK * KC) : 0, jump_rows = WK * KC - jump * a.ctx.page_rows;
-#pragma unroll
-  for (int p = 0; p < MOST; ++p) list[p] = 0;
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int j = (cb + grp) * KC + (gt + p * GT) / UPR;
@@ -394,14 +397,14 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
     const ArgsAgain A = args_again();
     const unsigned rows = A->own.page_rows;
     const int32_t* table = A->own.table + ((long long)b * A->K + k0) * A->own.cols;
+    const int list = packing.list(x0);
 #pragma unroll
     for (int p = 0; p < N; ++p) {
       const int x = x0 + (first + p * threads) / ROW;
       rest[p] = -1;
       if (x < to) {
-        int i = list[p];
+        int i = list;
         while (s_off[i + 1] <= x) ++i;
-        list[p] = i;
         const int j = x - s_off[i], pg = (int)((unsigned long long)(unsigned)j * A->own.by_rows.magic >> A->own.by_rows.shift);
         rest[p] = j - pg * rows;
         entry[p] = table[(long long)i * A->own.cols + pg];
@@ -562,8 +565,6 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
     bf16 *K = &s_kv[0][0][0][0] + wave * 64 * DH, *V = K + 32 * DH;
     int *holes = &s_hole[0][0][0] + wave * 32, *odds = &s_odd[0][0][0] + wave * (32 * (DH / width.value));
     int *any_hole = &s_wave_hole[wave], *any_odd = &s_wave_odd[wave];
-#pragma unroll
-    for (int p = 0; p < count.value; ++p) list[p] = __builtin_amdgcn_readlane(row.k - k0, 0);
     if (c < c1) find_own(wlo + 32 * c, whi, width, count, lane, 64);
     if (c < c1) load_units(args_again()->own, width, count, lane, 64);
     if (c + WK < c1) find_own(wlo + 32 * (c + WK), whi, width, count, lane, 64);
