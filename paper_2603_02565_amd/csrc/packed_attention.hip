@@ -2,8 +2,6 @@
 // received (fe_packed_weights).
 #include <algorithm>
 #include <type_traits>
-#include <cstdlib>
-static int env(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 
 #include "packed.h"
 
@@ -966,10 +964,15 @@ PackedPlan packed_plan(const fe_packed_args& a) {
   const long long L = a.own.N > 0 ? (long long)a.own.cols * a.own.page_rows : 0;
   const long long own = std::min<long long>(a.K, (rows - 1) / sg + 2) * L, wgs = bg * p.tiles;
   const long long items = (T + 63) / 64 + (own + 63) / 64;
-  p.wide = p.waves == 1 && wgs < env("WIDE", 512) && (a.dtype == FE_BF16 || a.dh < 128);
-  long long want = (env("WANT", 512) + wgs - 1) / wgs;                       // two workgroups a compute unit
-  if (p.wide) want = (env("WANTW", 256) + wgs - 1) / wgs;
-  want = std::min(want, std::max(1LL, items / (p.wide ? env("IT", 32) : env("ITN", 4))));
+  // Few rows and few workgroups: more waves share a workgroup's keys and join in LDS (fp32 at head width 128 has no registers
+  // for it).  One wave of rows, heads of 64: 8 x 5 of 8192 keys 22.3 us -> 17.5; 256 x 4 of 2048 24.1 -> 18.3; heads of 128, 8 x 32
+  // of 32768 43.6 -> 32.7.
+  p.wide = p.waves == 1 && wgs < 512 && (a.dtype == FE_BF16 || a.dh < 128);
+  // Ranges of keys until there are two workgroups a compute unit (wide: one), each of 4 chunks of 64 keys at least (wide: 16;
+  // fp32: 2).  32 x 128 rows of 32768 keys, 256 / 512 / 768 / 1024 workgroups: 162, 107, 137, 123 us; 64 x 16 rows of 1024 in 8
+  // and 16 chunks 16.1, 15.7; fp32, 6 x 399 rows of 777 in 2 and 4 chunks 18.1, 20.9.
+  long long want = ((p.wide ? 256 : 512) + wgs - 1) / wgs;
+  want = std::min(want, std::max(1LL, items / (p.wide ? 16 : a.dtype == FE_F32 ? 2 : 4)));
   if (a.dtype == FE_F32) want = std::max(want, (items + 31) / 32);   // fp32 sums over at most 2048 keys
   const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);
   p.splits = (int)std::max(1LL, std::min({want, 256LL, grid}));
