@@ -106,7 +106,8 @@ fe_status fe_packed_read(const fe_packed_read_args* a, void* stream);
  * A row without keys gives out = 0 and lse = -infinity, and so do the rows i >= n.  ctx.N = B and own.N = B * K, or 0: none.
  *
  * Scores, the softmax's maximum and sum and the output sums are fp32.  FE_BF16: the products of the queries' bf16 values with
- * the held ones are exact, probabilities are rounded to bf16 for the product with the values.  FE_F32: queries and
+ * the held ones are exact, probabilities are rounded to bf16 for the product with the values (up to
+ * 32 rows a request and key head: to two bf16, 16 bits).  FE_F32: queries and
  * probabilities in three bf16 parts whose sum they are, the held values whole: no product is rounded; an infinite query may
  * give NaN.  A list's outputs do not depend on the own rows of other lists, NaN or not.  Results have the same
  * bits from call to call.

@@ -253,6 +253,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
   typedef Tile<DH> L;
   constexpr int WK = C::WK, GT = C::GT, ROWS = C::ROWS, UPR = C::UPR, PER = C::PER, KC = C::KC, NBUF = C::NBUF;
   constexpr int ND = C::ND, NB = C::NB, TILE = KC * DH, NS = C::NS;
+  constexpr bool FINE = WR == 1 && sizeof(T) == 2;
   static_assert(WR == 1 || (WK * 2 * KC >= 128 && WK * NBUF * 2 * TILE >= 4 * 64 * DH), "own rows by wave fit the tiles");
   static_assert(KC % (32 * NS) == 0 && (WK == 1 || W * 32 * DH * 4 <= WK * NBUF * 2 * TILE * 2), "the join fits the tiles");
   __shared__ __attribute__((aligned(16))) bf16 s_kv[WK][NBUF][2][TILE];
@@ -506,8 +507,20 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
         const Op p = F::rounded(w);
+        // bf16: one rounding of p, of about the size of out's own (out off by 2.3e-3 of its norm, 1.7e-3 without it).  Up to 32 rows
+        // what it cut is a second product: these calls wait for memory, and few outputs do not average the roundings out.
+        Op rest;
+        if constexpr (FINE) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) o[n] = mma_held(L::cols(V, kb + 32 * u + 16 * m, n, cl), p, o[n]);
+          for (int j = 0; j < 8; ++j) w[j] -= (float)p[j];
+          rest = F::rounded(w);
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const bf16x8 v = L::cols(V, kb + 32 * u + 16 * m, n, cl);
+          if constexpr (FINE) o[n] = mma_held(v, rest, o[n]);
+          o[n] = mma_held(v, p, o[n]);
+        }
       }
     }
     if (own && __builtin_amdgcn_readfirstlane(any_odd) == tag) {
