@@ -108,8 +108,8 @@ fe_status fe_packed_read(const fe_packed_read_args* a, void* stream);
  * Scores, the softmax's maximum and sum and the output sums are fp32.  FE_BF16: the products of the queries' bf16 values with
  * the held ones are exact, probabilities are rounded to bf16 for the product with the values (up to
  * 32 rows a request and key head: to two bf16, 16 bits).  FE_F32: queries and
- * probabilities in three bf16 parts whose sum they are, the held values whole: no product is rounded; an infinite query may
- * give NaN.  A list's outputs do not depend on the own rows of other lists, NaN or not.  Results have the same
+ * probabilities in three bf16 parts whose sum they are, the held values whole: no product is rounded.  A row
+ * with an infinite score is NaN.  A list's outputs do not depend on the own rows of other lists, NaN or not.  Results have the same
  * bits from call to call.
  *
  * fe_packed_weights: for every row j < len of `ctx` and of `own` and every key head g
@@ -117,7 +117,8 @@ fe_status fe_packed_read(const fe_packed_read_args* a, void* stream);
  * w, w_out [N][n_kv_heads][cols * page_rows], w_out may be w; entries past the length are left as they were.  Query rows with
  * lse = -infinity add nothing; lse is an input here.  ctx_w or own_w (with its output) may be NULL: not computed.
  *
- * Workspace: fe_packed_workspace_size(a, 0 or 1 for the weights) bytes (may be 0: then ws is not read).
+ * Workspace: fe_packed_workspace_size(a, 0 or 1 for the weights) bytes (may be 0: then ws is not read); for the weights it
+ * goes by which of ctx_w and own_w are not NULL.
  *
  * Errors: FE_EINVAL for a NULL or misaligned pointer, sizes below 1, n_heads not a multiple of n_kv_heads, ctx.N or own.N
  * other than said, strides too short or not multiples of 16 bytes, a scale that is not finite, an unknown dtype, a workspace that is

@@ -58,6 +58,15 @@ def write(pages, page, r, P, dh, k, v):
         pages[page, :, c], pages[page, :, s] = codes, scales
 
 
+def write_rows(pages, page, r, P, dh, k, v):
+    """Rows k, v [n][Hkv][dh] into rows r [n] of pages page [n]."""
+    for part, x in ((0, k), (1, v)):
+        for bytes_, width, start in zip(hold(x), (dh // 2, dh // 32), (0, P * dh)):
+            at = start + (part * P + r) * width
+            h, c = np.arange(pages.shape[1])[None, :, None], np.arange(width)[None, None]
+            pages[page[:, None, None], h, at[:, None, None] + c] = bytes_
+
+
 def read(pages, page, r, P, dh):
     """(k, v) [Hkv][dh] of a row."""
     return tuple(values(pages[page, :, place(P, dh, part, r)[0]], pages[page, :, place(P, dh, part, r)[1]]) for part in (0, 1))

@@ -272,13 +272,12 @@ class Case:
         hb = ref.head_bytes(P, dh)
         self.pages = np.full((self.n_pages, Hkv, hb), 255, np.uint8)
         nc, nq, no = self.lengths()
-        for s in range(B):
-            for j in range(nc[s]):
-                ref.write(self.pages, self.ct[s, j // P], j % P, P, dh, self.ck[s, j], self.cv[s, j])
-        for s in range(B * K):
-            for j in range(no.reshape(-1)[s]):
-                ref.write(self.pages, self.ot[s, j // P], j % P, P, dh, self.ok.reshape(B * K, -1, Hkv, dh)[s, j],
-                          self.ov.reshape(B * K, -1, Hkv, dh)[s, j])
+        ok, ov = (x.reshape(B * K, -1, Hkv, dh) for x in (self.ok, self.ov)) if self.L else ([None] * (B * K),) * 2
+        for t, n, k, v in ((self.ct, nc, self.ck, self.cv), (self.ot, no.reshape(-1), ok, ov)):
+            for s in range(len(n)):
+                if n[s]:
+                    j = np.arange(n[s])
+                    ref.write_rows(self.pages, t[s, j // P], j % P, P, dh, k[s][:n[s]], v[s][:n[s]])
         for b in range(B):
             for k in range(K):
                 self.q[b, k, nq[b, k]:] = NAN
@@ -363,6 +362,15 @@ FORWARD = [
     dict(dtype="bf16", B=1, K=2, S=150, H=3, Hkv=1, dh=128, T=20, L=150, P=48, lens="own"),
     dict(dtype="f32", B=2, K=13, S=11, H=4, Hkv=4, dh=32, T=64, L=11, P=5, causal=False, lens="own"),
     dict(dtype="bf16", B=1, K=1, S=260, H=2, Hkv=1, dh=64, T=0, L=300, P=64, lens="ragged"),
+    dict(dtype="bf16", B=1, K=1, S=50, H=1, Hkv=1, dh=128, T=70, L=80, P=16, lens="ragged"),
+    # many requests of few rows: four waves a workgroup
+    dict(dtype="bf16", B=64, K=2, S=1, H=8, Hkv=8, dh=32, T=40, L=9, P=4),
+    dict(dtype="bf16", B=70, K=3, S=1, H=8, Hkv=8, dh=64, T=33, L=9, P=7),
+    dict(dtype="bf16", B=64, K=1, S=2, H=8, Hkv=8, dh=128, T=37, L=9, P=4),
+    dict(dtype="f32", B=64, K=2, S=1, H=8, Hkv=8, dh=64, T=40, L=9, P=4),
+    dict(dtype="f32", B=66, K=2, S=1, H=8, Hkv=8, dh=32, T=40, L=9, P=4),
+    # ranges of keys in proportion to the requests' lengths
+    dict(dtype="bf16", B=8, K=34, S=1, H=4, Hkv=4, dh=32, T=16384, L=3, P=64),
     # lengths at and past their limits, rows without keys
     dict(dtype="bf16", B=6, K=5, S=3, H=4, Hkv=2, dh=32, T=40, L=9, P=4, lens="edge"),
     dict(dtype="bf16", B=6, K=5, S=9, H=4, Hkv=2, dh=64, T=140, L=70, P=10, lens="edge", causal=False),
@@ -469,21 +477,23 @@ def _sizes(c):
     return a
 
 
-@pytest.mark.parametrize("K,dh", [(5, 64), (40, 32), (70, 128)])
-def test_own_rows_of_nan_stay_in_their_list(K, dh):
+@pytest.mark.parametrize("K,S,dh,dtype", [(5, 3, 64, "bf16"), (40, 3, 32, "bf16"), (70, 3, 128, "bf16"), (15, 3, 64, "bf16"), (15, 3, 128, "f32"),
+                                          (3, 45, 32, "bf16"), (3, 70, 64, "f32"), (2, 90, 128, "bf16")])
+def test_own_rows_of_nan_stay_in_their_list(K, S, dh, dtype):
     """Blocks of NaN among one list's own keys and values: the other lists keep their bits; in that list the rows that see the
     key are NaN, in all columns for a key's block and in the block's for a value's."""
-    kw = dict(dtype="bf16", B=2, K=K, S=3, H=2, Hkv=2, dh=dh, T=40, L=9, P=4, lens="full", seed=6)
+    L = S + 6
+    kw = dict(dtype=dtype, B=2, K=K, S=S, H=2, Hkv=2, dh=dh, T=40, L=L, P=4, lens="full", seed=6)
     clean = Case(**kw).device()
     want, lse0 = clean.run()
-    for part, row in ((1, 7), (0, 7), (1, 2)):
+    for part, row in ((1, L - 2), (0, L - 2), (1, 2), (0, L // 2)):
         c = Case(**kw)
         page = c.ot[K + 1, row // 4]                                      # list 1 of request 1
         s = ref.place(4, dh, part, row % 4)[1]
         c.pages[page, 1, s.start] = 255                                   # key head 1, the first block
         got, lse = c.device().run()
         same = torch.ones_like(want, dtype=torch.bool)
-        sees = [i for i in range(3) if row <= 9 - 3 + i]
+        sees = [i for i in range(S) if row <= L - S + i]
         cols = slice(0, 32) if part else slice(0, dh)
         same[1, 1, sees, 1, cols] = False
         assert torch.equal(got[same], want[same])
@@ -523,6 +533,37 @@ def test_strided_queries_and_another_stream():
     got = plan.run(wide[..., 4:8, :], c.ctx, c.own, q_len=c.q_len, stream=side)
     side.synchronize()
     assert torch.equal(got, want) and torch.equal(plan.lse, lse)
+
+
+def test_shared_pages_and_two_pools():
+    """Requests whose tables name the same pages, and own rows in another pool with pages of another size."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()                               # noqa: E731
+    B, K, Hkv, H, dh = 3, 4, 2, 4, 64
+    pool = torch.full((9, PagedCache4.page_bytes(16, Hkv, dh)), 255, dtype=torch.uint8, device="cuda")
+    other = torch.full((B * K * 3, PagedCache4.page_bytes(5, Hkv, dh)), 255, dtype=torch.uint8, device="cuda")
+    one = PagedCache4(pool, _i32([[2, 7, 4]]), 16, Hkv, dh)
+    one.append(rnd(1, 40, Hkv, dh), rnd(1, 40, Hkv, dh))
+    ctx = PagedCache4(pool, _i32([[2, 7, 4]] * B), 16, Hkv, dh, _i32([40, 17, 33]))
+    own = PagedCache4(other, torch.randperm(B * K * 3, generator=g, device="cuda").int().view(B * K, 3), 5, Hkv, dh)
+    own.append(rnd(B * K, 13, Hkv, dh), rnd(B * K, 13, Hkv, dh))
+    q = rnd(B, K, 2, H, dh)
+    plan = PrefixAttention4(B=B, K=K, S=2, T=48, L=15, n_heads=H, n_kv_heads=Hkv, dh=dh, dtype="bf16", causal=True)
+    out = plan.run(q, ctx, own)
+    (ck, cv), (ok, ov) = ((_np(x) for x in c.read()) for c in (ctx, own))
+    want = dense.attend(_np(q), ck, cv, ok.reshape(B, K, 15, Hkv, dh), ov.reshape(B, K, 15, Hkv, dh), dtype="bf16", causal=True,
+                        ctx_len=np.array([40, 17, 33]), own_len=np.full((B, K), 13))
+    _near(out, want["out"], "out")
+    w = torch.zeros(B, Hkv, 48, device="cuda")
+    plan.weigh(q, plan.lse, ctx, own, ctx_w=w)
+    to = PagedCache4(pool, _i32([[0], [1], [3]]), 16, Hkv, dh)            # each request keeps rows of the shared pages for itself
+    kept = ctx.evict(w, to, keep=9, recent=3)
+    k, v = to.read()
+    for b, n in enumerate((40, 17, 33)):
+        for h in range(Hkv):
+            rows = ref.evict_rows(w[b, h].tolist(), n, 9, 0, 3)
+            assert kept[b, h].tolist() == rows
+            assert np.array_equal(_np(k)[b, :9, h], ck[b, rows, h]) and np.array_equal(_np(v)[b, :9, h], cv[b, rows, h])
 
 
 def test_replayed_step():

@@ -219,6 +219,10 @@ def test_reference_pages_keep_rows_apart():
         for p in (0, 1):
             for row in range(P):
                 ref.write(pages, p, row, P, dh, x[p, row, 0], x[p, row, 1])
+        many = np.zeros_like(pages)
+        for p in (0, 1):
+            ref.write_rows(many, np.full(P, p), np.arange(P), P, dh, x[p, :, 0], x[p, :, 1])
+        assert np.array_equal(many, pages)
         for p in (0, 1):
             for row in range(P):
                 k, v = ref.read(pages, p, row, P, dh)
