@@ -228,12 +228,23 @@ FE_DEV ArgsAgain args_again() {
 FE_DEV void order() { asm volatile("" ::: "memory"); }   // LDS operations of one wave stay in order
 
 // ------------------------------------------------------------------------------------------
-// Forward.  The rows of a (request, key head) are one matrix of R rows; four waves are WK groups of WR waves with 32
+// Forward.  The rows of a (request, key head) are one matrix of R rows; W waves are WK groups of WR waves with 32
 // rows each.  A group takes every WK-th chunk of KC keys (first the shared rows, then the own rows of the lists that the
 // tile touches, packed without gaps); a thread loads PER units of UE codes of the keys and of the values, the next
 // chunk's in flight behind this one's products, turns them into bf16, which holds them exactly, and puts them into LDS.
-// Scores are formed transposed (keys x rows), so that a lane holds 16 keys of one row in the operand layout of the
-// product with the values.  With WK > 1 the groups' sums are joined in LDS at the end.
+// Scores are formed transposed (keys x rows, 32 x 32 x 16 products, at twice the rate of 16 x 16 x 32 ones), so that a lane
+// holds 16 keys of one row in the operand layout of the product with the values.  With WK > 1 the groups' sums are joined in LDS
+// at the end.
+//
+// 128 rows a workgroup above 64, so that a key is turned into bf16 once for 128; 64 above 32; up to 32 the groups have a wave
+// each, which meet no barrier.  Own rows of short lists are seen by few of a tile's rows: staged by every wave for itself (4
+// x 32 lists over 32768 rows, heads of 128: 105 us -> 97; 64 x 50 slates of 11: 34 -> 27).  Two blocks of keys at a time, at one
+// or two waves fewer a SIMD (115 -> 108, prompts 281 -> 261).
+// Bound: no unit alone.  2 x 2048 rows of 16 heads of 128 over 5120 keys: 223 us, 770 TFLOP/s, with the vector unit busy 42% of
+// the time, matrix cores 32%, LDS 32%, waits 31% of the waves' time; leaving out any one of staging, exponentials, either product or
+// the loads takes 8 to 15% away.  4 x 32 x 4 rows a key head over 16384 .. 32768: 96 us and the join's 10 (145 MB,
+// 52 GFLOP).  64 x 550 rows of 4 heads of 32 over 267 keys: 25 us, vector unit 60%, a third of it outside the score loop.
+// 5 rows of 181 keys: 7.7 us, a chain of dependent trips to memory.
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int WR, int UE, int W> struct Shape {
   static constexpr int WK = W / WR, GT = 64 * WR, ROWS = 32 * WR, UPR = DH / UE;
@@ -658,6 +669,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
 }
 
 // Joins the key ranges of a row in ascending order: DH / 4 threads a row.
+// Bound: the partial sums (4096 rows of 128 in about 16 ranges, 34 MB: 10 us); one trip for a few (4 us).
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
   const long long per = (long long)a.K * a.S * a.Hq, rows = a.B * per;
@@ -720,6 +732,12 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
 // without meeting the others, its operands made in registers from the codes, whose loads run a tile ahead and their pages two.
 // Which column a summed element is does not matter: lane l has the half l / 32 of its key's columns.  A lane then holds 16
 // rows' scores of its key, and their exponentials are added up in it.
+//
+// Operands of 32 keys a wave and four waves a SIMD: two operands, half the reads of LDS, leave room for two waves (32 lists
+// over 32768 rows, heads of 128: 73 us and 54).  Key ranges by the requests' lengths: 54 -> 48; 1024 workgroups: 512
+// 59 us, 768 50, 1024 51, 2048 57.
+// Bound: the vector unit, 63% (a product-sum, an exponential and a sum a score; the codes' conversion): 46 us, 561 TFLOP/s.
+// 8 x 16 lists over 1024: 7.5 us, three dependent trips to memory.
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH> struct Weigh {
   typedef Form<T> F;
@@ -921,7 +939,7 @@ __global__ __launch_bounds__(256, sizeof(T) * DH > 256 ? 2 : 4) void k_packed_we
   else W::template run<true, 1>(a, id - n_ctx, S);
 }
 
-// Adds the row ranges of every key in ascending order.
+// Adds the row ranges of every key in ascending order.  Bound: the partial sums; launch latency where they are few.
 __global__ __launch_bounds__(256) void k_packed_weigh_sum(PackedCache x, int Hkv, int splits, long long keys, const float* part,
                                                           const float* w, float* out) {
   const long long at = (long long)blockIdx.x * 256 + threadIdx.x;

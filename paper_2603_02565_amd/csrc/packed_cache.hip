@@ -82,6 +82,8 @@ constexpr int kAppendRows = 64;           // rows of a workgroup
 // One workgroup takes `rows` (a power of two) consecutive new rows of one sequence: sines and cosines of a row are
 // formed once, in LDS, for all its heads; then every thread takes units of 8 columns, 4 lanes a block, consecutive
 // units along a row, then rows, then heads, as the pages hold them.
+// Bound: the vector unit (73%), fp64 among it, beside HBM: 24 x 1000 rows of 24 heads of 128, bf16, 246 MB: 71 us, 3.5 TB/s.  128
+// rows of 24 heads of 64: 4.4 us, launch latency and two trips to memory.
 template <typename T>
 __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, PackedCache c, int log_rows, int blocks) {
   typedef typename Vec8<T>::type V8;
@@ -212,7 +214,8 @@ FE_DEV void put8(float* p, bf16x8 v) {
   *reinterpret_cast<f32x8*>(p) = w;
 }
 
-// A thread takes 8 columns of a row's head, of keys and of values.
+// A thread takes 8 columns of a row's head, of keys and of values: 4 bytes of codes each in, 16 or 32 bytes out, both in
+// order.  Bound: HBM (4 x 8192 rows of 8 heads of 128, 170 MB: 28.5 us, 6.0 TB/s, partly from cache).
 template <typename T>
 __global__ __launch_bounds__(256) void k_packed_read(fe_packed_read_args a, PackedCache c, int blocks) {
   const int s = blockIdx.x / blocks, blk = blockIdx.x % blocks;
@@ -286,7 +289,8 @@ FE_DEV void move_block(const PackedCache& from, const PackedCache& to, int s, in
 }
 
 // Short sequences (64 E rows at most): one wave selects, all four move.  The m-th greatest order is found bit by bit: a ballot
-// counts the candidates at or above a trial.
+// counts the candidates at or above a trial.  Bound: three trips to memory (1024 heads of 64 rows, 9 MB: 5.1 us; with the
+// histograms below and a launch of its own for the move 48).
 template <int E>
 __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args a, PackedCache from, PackedCache to) {
   __shared__ int s_kept[64 * E];
@@ -350,6 +354,8 @@ __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args
 // a histogram in LDS, in 32 copies by lane so that equal digits, the rule among weights, do not meet in one word.  Then
 // every wave walks its rows in order and numbers what is kept.  The orders of 1024 E rows stay in registers where they are
 // all.  What is no candidate has order 0, below all of them, and is counted with them to no effect.
+// Bound: instructions of the one compute unit that a head has (32 heads of 32768 rows: 26 us, of which the loads take 4, a
+// pass 3, the numbering 8).
 template <int E>
 __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
   constexpr int NW = 16, NT = NW * 64, SEG = NT * E;
@@ -477,7 +483,8 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
   }
 }
 
-// The kept rows: a thread takes one block, of keys and of values, the first of a row its weight as well.
+// The kept rows: a thread takes one block, of keys and of values, the first of a row its weight as well.  Bound: HBM at 64
+// contiguous bytes a row (4 x 8192 rows of 8 heads of 128, 71 MB: 19 us, 3.7 TB/s).
 __global__ __launch_bounds__(256) void k_packed_move(fe_packed_evict_args a, PackedCache from, PackedCache to, int blocks) {
   const int sh = blockIdx.x / blocks, blk = blockIdx.x % blocks, s = sh / a.n_kv_heads, h = sh - s * a.n_kv_heads;
   const int log_blocks = a.dh == 32 ? 0 : a.dh == 64 ? 1 : 2;
