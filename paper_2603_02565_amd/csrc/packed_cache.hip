@@ -29,10 +29,6 @@ FE_DEV float to_odd(double x) {
   if (back != a) b |= 1;
   return copysignf(__uint_as_float(b), (float)x);
 }
-template <typename T> FE_DEV T rounded(double x);
-template <> FE_DEV float rounded<float>(double x) { return (float)x; }
-template <> FE_DEV bf16 rounded<bf16>(double x) { return (bf16)to_odd(x); }
-
 // Eight codes of a block that the lanes of a quad share (lane i: columns 8 i ..), and the block's scale.  The magnitudes'
 // leading bits as integers order as they do; 1.5 * 2^(E - bias) is the largest whose scale is 2 below its exponent.
 FE_DEV unsigned codes8(const float (&f)[8], float unit) {
@@ -88,6 +84,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, PackedCache c, int log_rows, int blocks) {
   typedef typename Vec8<T>::type V8;
   __shared__ double s_cos[kTurns], s_sin[kTurns];
+  __shared__ float s_cos32[kTurns], s_sin32[kTurns];
   __shared__ long long s_page[kAppendRows];
   __shared__ int s_row[kAppendRows];
   const int tid = threadIdx.x, s = blockIdx.x / blocks, blk = blockIdx.x % blocks, rows = 1 << log_rows;
@@ -111,7 +108,12 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
   }
   for (int e = tid; e < m * np; e += 256) {
     const int r = e / np;
-    sincos((double)(pos0 + i0 + r) * a.freq[e - r * np], &s_sin[e], &s_cos[e]);
+    double sn, cs;
+    sincos((double)(pos0 + i0 + r) * a.freq[e - r * np], &sn, &cs);
+    s_sin[e] = sn;
+    s_cos[e] = cs;
+    s_sin32[e] = (float)sn;
+    s_cos32[e] = (float)cs;
   }
   if (blk == 0 && a.status) {              // uniform over the workgroup: the pages of all n rows
     int bad = (long long)len + n > c.cap && n > 0;
@@ -143,11 +145,34 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
     const V8 own = *reinterpret_cast<const V8*>(src + 8 * x);
     unsigned w;
     unsigned char scale;
-    if (is_v || a.rot == 0) {
-      if (is_q) {
-        *reinterpret_cast<V8*>(static_cast<T*>(a.q_out) + row * a.q_out_ld + h * a.dh + 8 * x) = own;
-        continue;
+    const bool turned = !is_v && 8 * x < a.rot, apart = turned && !a.neighbours;   // apart: the pair's columns lie rot / 2 apart
+    const bool second = 8 * x >= np;
+    const int c0 = !apart ? 4 * x : second ? 8 * x - np : 8 * x;       // the unit's first pair
+    V8 other{};
+    if (apart) other = *reinterpret_cast<const V8*>(src + (second ? c0 : c0 + np));
+    if (is_q) {                            // in fp32: nothing but a rounding follows
+      V8 out = own;
+      if (turned) {
+        const float *cs = s_cos32 + r * np + c0, *sn = s_sin32 + r * np + c0;
+        if (apart) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float u = to_f32((T)own[i]), v = to_f32((T)other[i]);
+            out[i] = from_f32<T>(fmaf(u, cs[i], second ? v * sn[i] : -v * sn[i]));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float u = to_f32((T)own[2 * i]), v = to_f32((T)own[2 * i + 1]);
+            out[2 * i] = from_f32<T>(fmaf(u, cs[i], -v * sn[i]));
+            out[2 * i + 1] = from_f32<T>(fmaf(v, cs[i], u * sn[i]));
+          }
+        }
       }
+      *reinterpret_cast<V8*>(static_cast<T*>(a.q_out) + row * a.q_out_ld + h * a.dh + 8 * x) = out;
+      continue;
+    }
+    if (is_v || a.rot == 0) {
       float f[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = to_f32((T)own[i]);
@@ -156,32 +181,22 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
       double y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = (double)to_f32((T)own[i]);
-      if (8 * x < a.rot) {
-        const double *cs = s_cos + r * np, *sn = s_sin + r * np;
-        if (a.neighbours) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const double u = y[2 * i], v = y[2 * i + 1], p = cs[4 * x + i], q = sn[4 * x + i];
-            y[2 * i] = u * p - v * q;
-            y[2 * i + 1] = v * p + u * q;
-          }
-        } else {                           // the pair's other columns lie rot / 2 apart
-          const bool second = 8 * x >= np;
-          const int c0 = second ? 8 * x - np : 8 * x;
-          const V8 other = *reinterpret_cast<const V8*>(src + (second ? c0 : c0 + np));
+      if (turned) {
+        const double *cs = s_cos + r * np + c0, *sn = s_sin + r * np + c0;
+        if (apart) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const double o = (double)to_f32((T)other[i]), q = sn[c0 + i];
-            y[i] = y[i] * cs[c0 + i] + (second ? o * q : -o * q);
+            const double o = (double)to_f32((T)other[i]);
+            y[i] = y[i] * cs[i] + (second ? o * sn[i] : -o * sn[i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const double u = y[2 * i], v = y[2 * i + 1];
+            y[2 * i] = u * cs[i] - v * sn[i];
+            y[2 * i + 1] = v * cs[i] + u * sn[i];
           }
         }
-      }
-      if (is_q) {
-        V8 out;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = rounded<T>(y[i]);
-        *reinterpret_cast<V8*>(static_cast<T*>(a.q_out) + row * a.q_out_ld + h * a.dh + 8 * x) = out;
-        continue;
       }
       w = held(y, &scale);
     }

@@ -103,9 +103,9 @@ def test_append_holds_the_nearest(kw):
     assert (cache.status.cpu().numpy() == 0).all()
     assert np.array_equal(cache.len.cpu().numpy(), c["len"] + c["new"])
     if kw["H"]:
-        half = dense.HALF_STEP[kw["dtype"]]
-        # one rounding; the fp64 products before it, 2^-50 of the pair's size
-        assert (np.abs(_np(q_got) - q_want) <= half * np.abs(q_want) + 2.0 ** -48 * np.abs(q_want).max()).all()
+        # fp32 products of sines good to 2^-24, one rounding to the type
+        bound = dense.turned_bound(c["q"], c["freq"], kw["near"], kw["dtype"])
+        assert (np.abs(_np(q_got) - q_want) <= bound).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -177,7 +177,7 @@ def test_append_rows_without_a_page(S):
     want, q_want = _append_want(c, pages=empty.copy(), q_out=q0.copy(), **kw)
     got, q_got, cache = _append_run(c, pages=empty, q_out=q0, **kw)
     assert np.array_equal(got.cpu().numpy(), want)
-    assert (np.abs(_np(q_got) - q_want) <= 2.0 ** -8 * np.abs(q_want) + 1e-9).all()
+    assert (np.abs(_np(q_got) - q_want) <= dense.turned_bound(c["q"], c["freq"], False, "bf16")).all()
     bad = [4, 4 if S > 1 else 0, 4, 4, 0, 0]
     assert cache.status.cpu().tolist() == bad
     assert cache.len.cpu().tolist() == [S, 23 + S, 24 + S, 5 + S, min(2, S), 1000]
