@@ -94,6 +94,23 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
   const int32_t* tab = c.table + (long long)s * c.cols;
   const int i0 = blk * rows, m = min(rows, n - i0), np = a.rot / 2;
 
+  const int hq = a.q ? a.n_heads : 0, heads = hq + 2 * a.n_kv_heads;
+  const int log_units = a.dh == 32 ? 2 : a.dh == 64 ? 3 : 4, units = 1 << log_units;
+  // A unit and its pairs' other columns where they lie rot / 2 apart: requested one ahead, the first before the sines.
+  V8 own{}, other{};
+  auto fetch = [&](int e) __attribute__((always_inline)) {
+    const int x = e & (units - 1), r = e >> log_units & (rows - 1), hh = e >> (log_rows + log_units);
+    if (r >= m || hh >= heads) return;
+    const long long row = (long long)s * a.S + i0 + r;
+    const bool is_q = hh < hq, is_v = hh >= hq + a.n_kv_heads;
+    const T* src = is_q ? static_cast<const T*>(a.q) + row * a.q_ld : is_v ? static_cast<const T*>(a.v) + row * a.v_ld
+                                                                          : static_cast<const T*>(a.k) + row * a.k_ld;
+    src += (is_q ? hh : is_v ? hh - hq - a.n_kv_heads : hh - hq) * a.dh;
+    own = *reinterpret_cast<const V8*>(src + 8 * x);
+    if (!is_v && 8 * x < a.rot && !a.neighbours) other = *reinterpret_cast<const V8*>(src + (8 * x >= np ? 8 * x - np : 8 * x + np));
+  };
+  fetch(tid);
+
   if (tid < m) {
     const long long j = (long long)len + i0 + tid;
     long long at = -1;
@@ -129,41 +146,35 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
     a.len_out[s] = (int)min((long long)len + n, 0x7fffffffLL);
   if (m <= 0) return;
 
-  const int hq = a.q ? a.n_heads : 0, heads = hq + 2 * a.n_kv_heads;
-  const int log_units = a.dh == 32 ? 2 : a.dh == 64 ? 3 : 4, units = 1 << log_units;
   for (int e = tid; e < heads << (log_rows + log_units); e += 256) {
     const int x = e & (units - 1), r = e >> log_units & (rows - 1), hh = e >> (log_rows + log_units);
+    const V8 mine = own, pair = other;
+    fetch(e + 256);
     if (r >= m) continue;
     const long long row = (long long)s * a.S + i0 + r;
     const bool is_q = hh < hq, is_v = hh >= hq + a.n_kv_heads;
     const int h = is_q ? hh : is_v ? hh - hq - a.n_kv_heads : hh - hq;
     const long long page = s_page[r];
     if (!is_q && page < 0) continue;       // the same in a quad
-    const T* src = is_q ? static_cast<const T*>(a.q) + row * a.q_ld : is_v ? static_cast<const T*>(a.v) + row * a.v_ld
-                                                                          : static_cast<const T*>(a.k) + row * a.k_ld;
-    src += h * a.dh;
-    const V8 own = *reinterpret_cast<const V8*>(src + 8 * x);
     unsigned w;
     unsigned char scale;
     const bool turned = !is_v && 8 * x < a.rot, apart = turned && !a.neighbours;   // apart: the pair's columns lie rot / 2 apart
     const bool second = 8 * x >= np;
     const int c0 = !apart ? 4 * x : second ? 8 * x - np : 8 * x;       // the unit's first pair
-    V8 other{};
-    if (apart) other = *reinterpret_cast<const V8*>(src + (second ? c0 : c0 + np));
     if (is_q) {                            // in fp32: nothing but a rounding follows
-      V8 out = own;
+      V8 out = mine;
       if (turned) {
         const float *cs = s_cos32 + r * np + c0, *sn = s_sin32 + r * np + c0;
         if (apart) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float u = to_f32((T)own[i]), v = to_f32((T)other[i]);
+            const float u = to_f32((T)mine[i]), v = to_f32((T)pair[i]);
             out[i] = from_f32<T>(fmaf(u, cs[i], second ? v * sn[i] : -v * sn[i]));
           }
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float u = to_f32((T)own[2 * i]), v = to_f32((T)own[2 * i + 1]);
+            const float u = to_f32((T)mine[2 * i]), v = to_f32((T)mine[2 * i + 1]);
             out[2 * i] = from_f32<T>(fmaf(u, cs[i], -v * sn[i]));
             out[2 * i + 1] = from_f32<T>(fmaf(v, cs[i], u * sn[i]));
           }
@@ -175,18 +186,18 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
     if (is_v || a.rot == 0) {
       float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = to_f32((T)own[i]);
+      for (int i = 0; i < 8; ++i) f[i] = to_f32((T)mine[i]);
       w = held(f, &scale);
     } else {
       double y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = (double)to_f32((T)own[i]);
+      for (int i = 0; i < 8; ++i) y[i] = (double)to_f32((T)mine[i]);
       if (turned) {
         const double *cs = s_cos + r * np + c0, *sn = s_sin + r * np + c0;
         if (apart) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const double o = (double)to_f32((T)other[i]);
+            const double o = (double)to_f32((T)pair[i]);
             y[i] = y[i] * cs[i] + (second ? o * sn[i] : -o * sn[i]);
           }
         } else {
