@@ -78,8 +78,9 @@ constexpr int kAppendRows = 64;           // rows of a workgroup
 // One workgroup takes `rows` (a power of two) consecutive new rows of one sequence: sines and cosines of a row are
 // formed once, in LDS, for all its heads; then every thread takes units of 8 columns, 4 lanes a block, consecutive
 // units along a row, then rows, then heads, as the pages hold them.
-// Bound: the vector unit (73%), fp64 among it, beside HBM: 24 x 1000 rows of 24 heads of 128, bf16, 246 MB: 71 us, 3.5 TB/s.  128
-// rows of 24 heads of 64: 4.4 us, launch latency and two trips to memory.
+// Bound: HBM beside the vector unit (71%), the keys' fp64 and the sines: 24 x 1000 rows of 24 heads of 128, bf16, 246 MB: 60 us,
+// 4.1 TB/s (units requested when they are needed 70; the queries in fp64 as well 71).  128 rows of 24 heads of 64: 4.6 us,
+// launch latency and a trip to memory.
 template <typename T>
 __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, PackedCache c, int log_rows, int blocks) {
   typedef typename Vec8<T>::type V8;
