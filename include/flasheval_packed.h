@@ -13,7 +13,8 @@
  * Conventions are those of flasheval_prefix.h: device pointers owned by the caller, nothing allocated and
  * nothing waited for, asynchronous on `stream`, host-side validation before any launch, no state between
  * calls, lengths on the device and clamped to their range, rows outside them never used.  One workspace is not used by
- * two streams, or two captured graphs that may run at once, at a time.
+ * two streams, or two captured graphs that may run at once, at a time.  No output may overlap an input or another output, but
+ * where that is said below.
  *
  * What 4 bits stand for.  The columns of a head are held in blocks of 32: 4-bit floats (from the top bit: sign, two
  * exponent bits, one mantissa bit; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(e - 127) with one byte e a block.
@@ -62,7 +63,7 @@ fe_status fe_packed_page_bytes(int32_t page_rows, int32_t n_kv_heads, int32_t dh
  * the nearest to the turned key itself.
  * A row whose index reaches the capacity, or whose table entry names no page, is not written (its q_out row is);
  * status[s] is FE_DEV_BAD_PAGE then and 0 otherwise.  Other rows of the pages and rows i >= n(s) of q_out are left as they
- * were.  Two new rows must not share a cache row.  No output may overlap an input, but for len_out.
+ * were.  Two new rows must not share a cache row.
  *
  * Errors: as fe_cache_append's, and FE_EINVAL for q_out = q.
  */
@@ -158,8 +159,8 @@ fe_status fe_packed_weights(const fe_packed_args* a, void* stream);
  * none, 0 otherwise.  Entries of weight_out past m are left as they were.
  *
  * Errors: FE_EINVAL for a NULL or misaligned pointer, sizes below 1, first or recent below 0, keep above to's
- * capacity, to.N other than from.N, the same table or lengths on both sides; FE_EUNSUPPORTED for dh outside {32, 64, 128}, a capacity above 4194304
- * or more than 16777215 workgroups.
+ * capacity, to.N other than from.N, the same table or lengths on both sides, a weight_out that overlaps weight;
+ * FE_EUNSUPPORTED for dh outside {32, 64, 128}, a capacity above 4194304 or more than 16777215 workgroups.
  */
 typedef struct {
   fe_packed_cache from, to;

@@ -258,6 +258,12 @@ fe_status fe_packed_evict(const fe_packed_evict_args* a, void* stream) {
   if (!a->weight || !a->kept) return pfail(FE_EINVAL, "weight or kept is NULL");
   if (!aligned(a->weight, 4) || !aligned(a->weight_out, 4) || !aligned(a->kept, 4) || !aligned(a->status, 4))
     return pfail(FE_EINVAL, "weights, kept and status must be 4-byte aligned");
+  if (a->weight_out) {                     // rows move while others are read
+    const auto from = reinterpret_cast<uintptr_t>(a->weight), to = reinterpret_cast<uintptr_t>(a->weight_out);
+    const uintptr_t heads = 4ull * a->from.N * a->n_kv_heads;
+    if (from < to + heads * a->to.cols * a->to.page_rows && to < from + heads * a->from.cols * a->from.page_rows)
+      return pfail(FE_EINVAL, "weight_out overlaps weight");
+  }
   const double rows = std::ceil((double)a->keep * (a->dh / 32) / 256);
   if ((double)a->from.N * a->n_kv_heads * rows > kMaxGrid || (double)a->from.N * a->n_kv_heads * 1024 > 4294967295.)
     return pfail(FE_EUNSUPPORTED, "batch too large: more than %lld workgroups", kMaxGrid);

@@ -1041,9 +1041,9 @@ class PagedCache4:
         """Fill `to`, a cache of as many sequences in pages that none of this one's sequences use, with the `keep` rows of
         every sequence and key head that matter: the `first` and the `recent` ones, and of the others those of
         greatest weights [N][n_kv_heads][capacity] (fp32; of equal ones the lower index).  Sets to.len; rows keep their
-        order and their bits.  Their weights go to weights_out [N][n_kv_heads][to.capacity] when given, their indices
-        here to kept [N][n_kv_heads][keep] int32 (-1 where there are fewer), which is returned.  `status` holds
-        FE_DEV_BAD_PAGE for a sequence with rows of no page."""
+        order and their bits.  Their weights go to weights_out [N][n_kv_heads][to.capacity] when given, no
+        part of weights; their indices here to kept [N][n_kv_heads][keep] int32 (-1 where there are fewer), which is
+        returned.  `status` holds FE_DEV_BAD_PAGE for a sequence with rows of no page."""
         import torch
         a = self.evict_args
         if (to.N, to.n_kv_heads, to.dh) != (self.N, self.n_kv_heads, self.dh):
@@ -1071,7 +1071,8 @@ class PrefixAttention4:
     `run` takes q [B][K][S][n_heads][dh], `ctx`, a PagedCache4 of B sequences with a capacity of T rows, and `own`, one of
     B * K sequences with a capacity of L rows (T = 0 or L = 0: None); their lengths are the rows in use, q_len [B][K]
     int32 the query rows in use, with `causal` the last own rows.  out and lse [B][K][S][n_heads] belong to this
-    object and are overwritten by its next call, as is its workspace: one object per stream."""
+    object and are overwritten by its next call, as is its workspace: one object per stream.  For answering: autograd
+    records nothing here."""
 
     def __init__(self, B: int, K: int, S: int, T: int, L: int, n_heads: int, n_kv_heads: int, dh: int, dtype: str,
                  causal: bool = False, scale: Optional[float] = None):

@@ -43,7 +43,7 @@ def _attend(**kw):
 
 def _evict(**kw):
     return _fill(fe.fe_packed_evict_args(), dict(from_=_cache(), to=_cache(table=2 * A16, len=2 * A16), n_kv_heads=2, dh=64, keep=8, first=1,
-                                                 recent=2, weight=A16, weight_out=A16, kept=A16, status=A16), kw)
+                                                 recent=2, weight=A16, weight_out=2 * A16, kept=A16, status=A16), kw)
 
 
 CACHE = [  # what every call checks of a cache
@@ -129,6 +129,8 @@ def test_attention_or_weights_are_checked(call, kw, word):
     (dict(first=-1), "first", fe.FE_EINVAL), (dict(recent=-1), "recent", fe.FE_EINVAL), (dict(weight=None), "NULL", fe.FE_EINVAL),
     (dict(kept=None), "NULL", fe.FE_EINVAL), (dict(weight=A16 + 2), "aligned", fe.FE_EINVAL), (dict(dh=20), "width", fe.FE_EUNSUPPORTED),
     (dict(to=_cache(pages=None, table=2 * A16, len=2 * A16)), "NULL", fe.FE_EINVAL),
+    (dict(weight_out=A16), "overlaps", fe.FE_EINVAL), (dict(weight_out=A16 + 2 * 2 * 48 * 4 - 4), "overlaps", fe.FE_EINVAL),
+    (dict(weight=A16 + 2 * 2 * 16 * 4 - 4, weight_out=A16, to=_cache(cols=1, table=2 * A16, len=2 * A16)), "overlaps", fe.FE_EINVAL),
 ])
 def test_evict_is_checked(kw, word, status):
     lib = fe.load_library()
