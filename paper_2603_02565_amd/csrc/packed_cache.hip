@@ -270,7 +270,8 @@ __global__ __launch_bounds__(256) void k_packed_read(fe_packed_read_args a, Pack
   if (a.v) put8(static_cast<T*>(a.v) + row * a.v_ld + h * a.dh + 8 * x, v);
 }
 
-// The order of weights as that of integers; NaN (1) below every number, both zeros equal.  0 is left for what is no candidate.
+// The order of weights as that of integers; NaN (1) below every number, both zeros equal.  0 is left for what is no candidate,
+// the greatest for what is certain.
 FE_DEV unsigned order_of(float w) {
   if (w != w) return 1;
   const unsigned b = __float_as_uint(w == 0.f ? 0.f : w);
@@ -380,9 +381,10 @@ __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args
 // Selects a (sequence, key head)'s rows.  Four passes over 8 bits each find the m-th greatest order among the candidates:
 // a histogram in LDS, in 32 copies by lane so that equal digits, the rule among weights, do not meet in one word.  Then
 // every wave walks its rows in order and numbers what is kept.  The orders of 1024 E rows stay in registers where they are
-// all.  What is no candidate has order 0, below all of them, and is counted with them to no effect.
+// all.  Rows that are kept in any case have the highest order, which no weight has, and what is no row the order 0.
 // Bound: instructions of the one compute unit that a head has (32 heads of 32768 rows: 26 us, of which the loads take 4, a
 // pass 3, the numbering 8).
+constexpr unsigned kCertain = 0xffffffffu;
 template <int E>
 __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
   constexpr int NW = 16, NT = NW * 64, SEG = NT * E;
@@ -392,14 +394,14 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
   const int s = blockIdx.x / a.n_kv_heads, h = blockIdx.x % a.n_kv_heads;
   const int n = packed_len(from, s), m = min(a.keep, n);
   const int first = min(a.first, m), recent = min(a.recent, m - first);
-  const int lo = first, hi = n - recent, segments = (n + SEG - 1) / SEG;
+  const bool all = m == n;                 // uniform
+  const int lo = first, hi = all ? 0 : n - recent, segments = (n + SEG - 1) / SEG;
   const float* w = a.weight + (long long)blockIdx.x * from.cap;
   int32_t* kept = a.kept + (long long)blockIdx.x * a.keep;
 
   if (h == 0) evict_state<NW>(a, from, to, s, n, m);
   for (int i = m + tid; i < a.keep; i += NT) kept[i] = -1;
 
-  const bool all = m == n;                 // uniform
   unsigned o[E];
   auto index = [&](int seg, int e) { return seg * SEG + (wave * E + e) * 64 + lane; };
   auto load = [&](int seg) __attribute__((always_inline)) {
@@ -409,14 +411,15 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int i = index(seg, e);
-      o[e] = i >= lo && i < hi ? order_of(v[e]) : 0;
+      o[e] = i >= lo && i < hi ? order_of(v[e]) : i < n ? kCertain : 0;
     }
   };
-  unsigned cut = 0xffffffffu;              // orders above it are kept, and `left` of those equal to it; none is as great
-  int left = m - first - recent;
+  unsigned cut = kCertain - 1;             // orders above it are kept, and the first `left` of those equal to it
+  int left = 0;
   if (segments == 1) load(0);
-  if (!all && left > 0) {
+  if (!all && m > first + recent) {
     cut = 0;
+    left = m;
 #pragma unroll 1
     for (int shift = 24; shift >= 0; shift -= 8) {
       for (int i = tid; i < 256 * 32; i += NT) s_hist[i] = 0;
@@ -465,17 +468,15 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
     }
   }
 
-  // certain: rows outside the candidates, and candidates above the cut; all of them where nothing is left out
-  const int sure_lo = all ? n : lo, sure_hi = all ? 0 : hi;
   int kept_before = 0, equal_before = 0;   // in the segments before
   for (int seg = 0; seg < segments; ++seg) {
     if (segments > 1) load(seg);
-    int n_kept = 0, n_equal = 0;           // the wave's: certain ones, and candidates equal to the cut
+    int n_kept = 0, n_equal = 0;           // the wave's rows above the cut, and equal to it
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int i = index(seg, e);
-      n_kept += __popcll(__ballot((i < sure_lo || i >= sure_hi) && i < n) | __ballot(o[e] > cut));
+      n_kept += __popcll(__ballot(o[e] > cut));
       n_equal += __popcll(__ballot(o[e] == cut));
+      asm volatile("" : "+s"(n_kept), "+s"(n_equal));    // one row's ballots after the other's: all at once they would not fit
     }
     if (lane == 0) {
       s_kept[wave] = n_kept;
@@ -491,15 +492,14 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
     int at = k0 + min(e0, left);           // of the equal ones the first `left` are kept
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      int i = index(seg, e);
-      asm volatile("" : "+v"(o[e]), "+v"(i));            // ballots are made again: kept, they would not fit the scalar registers
+      asm volatile("" : "+v"(o[e]));       // ballots are made again: kept, they would not fit the scalar registers
       const unsigned long long eq = __ballot(o[e] == cut);
-      unsigned long long got = __ballot((i < sure_lo || i >= sure_hi) && i < n) | __ballot(o[e] > cut);
+      unsigned long long got = __ballot(o[e] > cut);
       if (eq)                              // uniform
         got |= __ballot((eq >> lane & 1) && e0 + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(eq >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)eq, 0)) < left);
       if (got >> lane & 1) {
         const int d = at + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(got >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)got, 0));
-        kept[d] = i;
+        kept[d] = index(seg, e);
       }
       at += __popcll(got);
       e0 += __popcll(eq);
