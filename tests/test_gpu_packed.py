@@ -717,6 +717,28 @@ def test_evict(kw, kind):
     assert frm.len.cpu().tolist() == length.tolist()
 
 
+@pytest.mark.parametrize("keep,first,recent", [(300, 200, 150), (300, 200, 100), (300, 0, 0), (301, 10, 20), (2999, 1, 1), (1, 0, 0)])
+@pytest.mark.parametrize("T", [3000, 9001, 40000])
+def test_evict_where_digits_end(T, keep, first, recent):
+    """Weights of which exactly as many as are kept, one more or one fewer share their upper digits; NaN and -infinity at the cut."""
+    _say("evict, digits", T, keep, first, recent)
+    r = np.random.default_rng(T + keep)
+    w = np.full((1, 8, T), 1e-30, np.float32)
+    for h, (high, low) in enumerate([(1e30, 1e-30), (1.0, 1.0 + 2.0 ** -23), (1.5, 1.25), (0.0, NAN), (-INF, NAN), (NAN, NAN), (INF, -INF),
+                                     (1.0 + 2.0 ** -15, 1.0)]):
+        w[0, h] = low
+        w[0, h, r.permutation(T)[:max(keep - first - recent, 0) + h % 3 - 1]] = high
+    pool = torch.zeros(1, PagedCache4.page_bytes(64, 8, 32), dtype=torch.uint8, device="cuda")
+    cols, to_cols = -(-T // 64), -(-keep // 64)
+    full = np.zeros((1, 8, cols * 64), np.float32)
+    full[:, :, :T] = w
+    frm = PagedCache4(pool, torch.zeros(1, cols, dtype=torch.int32, device="cuda"), 64, 8, 32, _i32([T]))
+    to = PagedCache4(torch.zeros_like(pool), torch.zeros(1, to_cols, dtype=torch.int32, device="cuda"), 64, 8, 32)
+    kept = frm.evict(torch.tensor(full).cuda(), to, keep=keep, first=first, recent=recent).cpu().numpy()
+    for h in range(8):
+        assert kept[0, h].tolist() == ref.evict_rows(w[0, h], T, keep, first, recent), h
+
+
 def test_evict_rows_without_a_page():
     P, Hkv, dh = 4, 1, 32
     r = np.random.default_rng(0)
