@@ -382,7 +382,7 @@ __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args
 // a histogram in LDS, in 32 copies by lane so that equal digits, the rule among weights, do not meet in one word.  Then
 // every wave walks its rows in order and numbers what is kept.  The orders of 1024 E rows stay in registers where they are
 // all.  Rows that are kept in any case have the highest order, which no weight has, and what is no row the order 0.
-// Bound: instructions of the one compute unit that a head has (32 heads of 32768 rows: 20.8 us, of which the loads take 4 and
+// Bound: instructions of the one compute unit that a head has (32 heads of 32768 rows: 20.1 us, of which the loads take 4 and
 // a pass 3; the last pass is left out where the third one ends on a digit that is kept whole, as among weights that
 // hardly repeat it does; with it 21.9).
 constexpr unsigned kCertain = 0xffffffffu;
