@@ -7,6 +7,7 @@
  *   fe_packed_read            rows of every sequence as dense tensors
  *   fe_packed_attention       attention over shared rows and the list's own rows, both in such caches
  *   fe_packed_weights         adds to every cached row's weight what the query rows gave it
+ *   fe_packed_weights_strided the same with log sums of any strides
  *   fe_packed_evict           keeps the rows of greatest weight, in other pages
  *   fe_packed_workspace_size  workspace bytes of fe_packed_attention or fe_packed_weights
  *
@@ -118,14 +119,17 @@ fe_status fe_packed_read(const fe_packed_read_args* a, void* stream);
  *   w_out[s][g][j] = w[s][g][j] + sum over the query rows and heads of g that see it of exp(scale * q.k - lse)
  * w, w_out [N][n_kv_heads][cols * page_rows], w_out may be w; entries past the length are left as they were.  Query rows with
  * lse = -infinity add nothing; lse is an input here.  ctx_w or own_w (with its output) may be NULL: not computed.
+ * fe_packed_weights_strided reads the log sum of (b, k, i, h) at lse + b lse_ld[0] + k lse_ld[1] + i lse_ld[2] + h lse_ld[3]
+ * (elements; lse_ld in host memory, read during the call; a stride of 0 shares log sums).
  *
  * Workspace: fe_packed_workspace_size(a, 0 or 1 for the weights) bytes (may be 0: then ws is not read); for the weights it
  * goes by which of ctx_w and own_w are not NULL.
  *
  * Errors: FE_EINVAL for a NULL or misaligned pointer, sizes below 1, n_heads not a multiple of n_kv_heads, ctx.N or own.N
  * other than said, strides too short or not multiples of 16 bytes, a scale that is not finite, an unknown dtype, a workspace that is
- * too small; FE_EUNSUPPORTED for dh outside {32, 64, 128}, a capacity above 4194304, B*K*S*n_heads or N*capacity above
- * 1073741823, or more than 16777215 workgroups.
+ * too small, a negative stride of the log sums; FE_EUNSUPPORTED for dh outside {32, 64, 128}, a capacity above 4194304,
+ * B*K*S*n_heads or N*capacity above 1073741823, more than 16777215 workgroups, or log sums that lie more than 2147483647
+ * elements apart in one request or 10^15 from the first request to the last.
  */
 typedef struct {
   fe_packed_cache ctx, own;
@@ -145,6 +149,7 @@ typedef struct {
 fe_status fe_packed_workspace_size(const fe_packed_args* a, int weights, size_t* bytes); /* reads sizes only */
 fe_status fe_packed_attention(const fe_packed_args* a, void* stream);
 fe_status fe_packed_weights(const fe_packed_args* a, void* stream);
+fe_status fe_packed_weights_strided(const fe_packed_args* a, const int64_t lse_ld[4], void* stream);
 
 /*
  * fe_packed_evict: for every sequence s (n = from.len[s] rows) and key head g, m = min(keep, n) rows are kept: the

@@ -130,6 +130,43 @@ fe_status check_rows(const fe_packed_cache& c, int dtype, int S, int n_kv_heads,
   return FE_OK;
 }
 
+// lse_ld: strides of the log sums, nullptr: dense.
+fe_status weigh(const fe_packed_args* a, const int64_t* lse_ld, void* stream) {
+  const fe_status st = check_call(a);
+  if (st != FE_OK) return st;
+  if (!a->lse) return pfail(FE_EINVAL, "lse is NULL");
+  if ((a->ctx_w == nullptr) != (a->ctx_w_out == nullptr) || (a->own_w == nullptr) != (a->own_w_out == nullptr))
+    return pfail(FE_EINVAL, "weights and their output go together");
+  if ((a->ctx_w && !a->ctx.N) || (a->own_w && !a->own.N)) return pfail(FE_EINVAL, "weights without their cache");
+  if (!aligned(a->ctx_w, 4) || !aligned(a->own_w, 4) || !aligned(a->ctx_w_out, 4) || !aligned(a->own_w_out, 4))
+    return pfail(FE_EINVAL, "weights must be 4-byte aligned");
+  const int64_t n[4] = {a->B, a->K, a->S, a->n_heads}, dense[4] = {n[1] * n[2] * n[3], n[2] * n[3], n[3], 1};
+  int64_t ld[4];                           // of an axis of one element: 0
+  double span = 0;
+  for (int i = 0; i < 4; ++i) {
+    ld[i] = n[i] == 1 ? 0 : lse_ld ? lse_ld[i] : dense[i];
+    if (ld[i] < 0) return pfail(FE_EINVAL, "a stride of lse is negative");
+    if (i) span += (double)ld[i] * (n[i] - 1);
+  }
+  if (span > (double)kInt32 || (double)ld[0] * (n[0] - 1) > 1e15)
+    return pfail(FE_EUNSUPPORTED, "log sums of a request lie more than %lld elements apart, or the requests' out of reach", kInt32);
+  const PackedWeighPlan p = packed_weigh_plan(*a);
+  if (check_weigh_grid(p) != FE_OK) return FE_EUNSUPPORTED;
+  const size_t need = up256(p.ctx_bytes) + up256(p.own_bytes);
+  if (need && (!a->ws || a->ws_bytes < need))
+    return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);
+  PackedArgs k = kernel_args(*a);
+  k.lse_b = ld[0];
+  k.lse_k = (unsigned)ld[1]; k.lse_s = (unsigned)ld[2]; k.lse_h = (unsigned)ld[3];
+  k.ctx_keys = p.ctx_keys; k.own_keys = p.own_keys;
+  k.ctx_splits = p.ctx_splits; k.own_splits = p.own_splits;
+  k.keys_by_length = p.keys_by_length;
+  k.part_ctx = static_cast<float*>(a->ws);
+  k.part_own = reinterpret_cast<float*>(static_cast<char*>(a->ws) + up256(p.ctx_bytes));
+  const hipError_t e = launch_packed_weights(k, a->dh, a->dtype == FE_BF16, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? FE_OK : pfail(FE_EHIP, "attention weights launch failed: %s", hipGetErrorString(e));
+}
+
 }  // namespace
 
 extern "C" {
@@ -219,28 +256,11 @@ fe_status fe_packed_attention(const fe_packed_args* a, void* stream) {
   return e == hipSuccess ? FE_OK : pfail(FE_EHIP, "4-bit attention launch failed: %s", hipGetErrorString(e));
 }
 
-fe_status fe_packed_weights(const fe_packed_args* a, void* stream) {
-  const fe_status st = check_call(a);
-  if (st != FE_OK) return st;
-  if (!a->lse) return pfail(FE_EINVAL, "lse is NULL");
-  if ((a->ctx_w == nullptr) != (a->ctx_w_out == nullptr) || (a->own_w == nullptr) != (a->own_w_out == nullptr))
-    return pfail(FE_EINVAL, "weights and their output go together");
-  if ((a->ctx_w && !a->ctx.N) || (a->own_w && !a->own.N)) return pfail(FE_EINVAL, "weights without their cache");
-  if (!aligned(a->ctx_w, 4) || !aligned(a->own_w, 4) || !aligned(a->ctx_w_out, 4) || !aligned(a->own_w_out, 4))
-    return pfail(FE_EINVAL, "weights must be 4-byte aligned");
-  const PackedWeighPlan p = packed_weigh_plan(*a);
-  if (check_weigh_grid(p) != FE_OK) return FE_EUNSUPPORTED;
-  const size_t need = up256(p.ctx_bytes) + up256(p.own_bytes);
-  if (need && (!a->ws || a->ws_bytes < need))
-    return pfail(FE_EINVAL, "workspace of %zu bytes < %zu needed", a->ws ? a->ws_bytes : 0, need);
-  PackedArgs k = kernel_args(*a);
-  k.ctx_keys = p.ctx_keys; k.own_keys = p.own_keys;
-  k.ctx_splits = p.ctx_splits; k.own_splits = p.own_splits;
-  k.keys_by_length = p.keys_by_length;
-  k.part_ctx = static_cast<float*>(a->ws);
-  k.part_own = reinterpret_cast<float*>(static_cast<char*>(a->ws) + up256(p.ctx_bytes));
-  const hipError_t e = launch_packed_weights(k, a->dh, a->dtype == FE_BF16, static_cast<hipStream_t>(stream));
-  return e == hipSuccess ? FE_OK : pfail(FE_EHIP, "attention weights launch failed: %s", hipGetErrorString(e));
+fe_status fe_packed_weights(const fe_packed_args* a, void* stream) { return weigh(a, nullptr, stream); }
+
+fe_status fe_packed_weights_strided(const fe_packed_args* a, const int64_t lse_ld[4], void* stream) {
+  if (!lse_ld) return pfail(FE_EINVAL, "lse_ld is NULL");
+  return weigh(a, lse_ld, stream);
 }
 
 fe_status fe_packed_evict(const fe_packed_evict_args* a, void* stream) {

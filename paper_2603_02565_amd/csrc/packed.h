@@ -44,6 +44,8 @@ struct PackedArgs {
   // rows taken as own_chunks chunks of 64
   int by_length, own_chunks;
   float *part_o, *part_ml;               // splits > 1: [B * splits][K S Hq][dh] sums, [..][2] maximum and sum
+  long long lse_b;                       // the weights' log sum of (b, k, s, h): lse + b lse_b + k lse_k + s lse_s + h lse_h
+  unsigned lse_k, lse_s, lse_h;          // a request's less than 2^31 apart
   const float *ctx_w, *own_w;            // weights
   float *ctx_w_out, *own_w_out;
   int ctx_keys, own_keys, ctx_splits, own_splits;     // key ranges, and row ranges, per (sequence, key head)

@@ -829,7 +829,7 @@ template <typename T, int DH> struct Weigh {
           if (u >= units) break;
           const Row q = row_of(a, b, g, first + rc + min(r, here - 1));
           v[i] = ldv<typename F::V>(static_cast<const T*>(a.q) + q.at * a.q_ld + q.h * DH + u % (DH / 8) * 8);
-          lse[i] = a.lse[q.at * a.Hq + q.h];
+          lse[i] = a.lse[b * a.lse_b + (q.k * a.lse_k + q.s * a.lse_s + q.h * a.lse_h)];
           sees[i] = r < here && q.live ? (a.causal ? n - nq + q.s + 1 : n) : -0x7fffffff;
         }
       };

@@ -30,7 +30,7 @@ EXPORTED = ("fe_param_count", "fe_model_create", "fe_model_destroy", "fe_workspa
             "fe_executor_create", "fe_executor_submit", "fe_executor_join", "fe_executor_destroy",
             "fe_cache_append", "fe_prefix_workspace_size", "fe_prefix_attention", "fe_prefix_attention_grad",
             "fe_packed_page_bytes", "fe_packed_append", "fe_packed_read", "fe_packed_attention", "fe_packed_weights",
-            "fe_packed_evict", "fe_packed_workspace_size")
+            "fe_packed_weights_strided", "fe_packed_evict", "fe_packed_workspace_size")
 FE_EXECUTOR_MAX_STREAMS = 8
 FE_TRACE_FAMILIES = 12
 
@@ -152,6 +152,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "fe_packed_workspace_size": (S, [ctypes.POINTER(fe_packed_args), I, ctypes.POINTER(Z)]),
         "fe_packed_attention": (S, [ctypes.POINTER(fe_packed_args), P]),
         "fe_packed_weights": (S, [ctypes.POINTER(fe_packed_args), P]),
+        "fe_packed_weights_strided": (S, [ctypes.POINTER(fe_packed_args), ctypes.POINTER(ctypes.c_int64), P]),
         "fe_packed_evict": (S, [ctypes.POINTER(fe_packed_evict_args), P]),
     }
     for name, (res, args) in sig.items():
@@ -441,6 +442,13 @@ def fe_packed_weights(args: fe_packed_args, stream=None) -> None:
     st = load_library().fe_packed_weights(args, _stream(stream))
     if st != FE_OK:
         _check(st, "fe_packed_weights")
+
+
+def fe_packed_weights_strided(args: fe_packed_args, lse_ld, stream=None) -> None:
+    """lse_ld: elements from one request, list, row and head to the next."""
+    st = load_library().fe_packed_weights_strided(args, (ctypes.c_int64 * 4)(*lse_ld), _stream(stream))
+    if st != FE_OK:
+        _check(st, "fe_packed_weights_strided")
 
 
 def fe_packed_evict(args: fe_packed_evict_args, stream=None) -> None:
@@ -1144,18 +1152,22 @@ class PrefixAttention4:
 
     def weigh(self, q, lse, ctx: Optional[PagedCache4], own: Optional[PagedCache4], ctx_w=None, own_w=None, q_len=None,
               ctx_w_out=None, own_w_out=None, stream=None):
-        """Add the attention weight that every cached row received from the query rows (lse: `run`'s) to ctx_w
-        [B][n_kv_heads][T] and own_w [B * K][n_kv_heads][L] fp32 (either may be None), in place or into the outputs.
-        Returns the two tensors written."""
+        """Add the attention weight that every cached row received from the query rows (lse: `run`'s, or such log sums with
+        any strides) to ctx_w [B][n_kv_heads][T] and own_w [B * K][n_kv_heads][L] fp32 (either may be None), in place or into
+        the outputs.  Returns the two tensors written."""
         import torch
         a, Hkv = self.args, self.heads[0]
         ctx_w_out, own_w_out = (w if o is None else o for w, o in ((ctx_w, ctx_w_out), (own_w, own_w_out)))
         for t, name, n in ((ctx_w, "ctx_w", self.B * self.T), (ctx_w_out, "ctx_w_out", self.B * self.T),
                            (own_w, "own_w", self.B * self.K * self.L), (own_w_out, "own_w_out", self.B * self.K * self.L)):
             _need(t, name, torch.float32, n * Hkv)
-        _need(lse, "lse", torch.float32, self.B * self.K * self.q_shape[2] * self.q_shape[3])
+        if lse.dtype != torch.float32 or lse.shape != self.q_shape[:-1]:
+            _need(lse, "lse", torch.float32, self.B * self.K * self.q_shape[2] * self.q_shape[3])
         handle = self._take(stream, q, ctx, own, q_len, lse, ctx_w, own_w, ctx_w_out, own_w_out)
         a.lse = lse.data_ptr()
         a.ctx_w, a.own_w, a.ctx_w_out, a.own_w_out = _addr(ctx_w), _addr(own_w), _addr(ctx_w_out), _addr(own_w_out)
-        fe_packed_weights(a, handle)
+        if lse.is_contiguous():
+            fe_packed_weights(a, handle)
+        else:
+            fe_packed_weights_strided(a, lse.stride(), handle)
         return ctx_w_out, own_w_out

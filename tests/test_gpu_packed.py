@@ -858,3 +858,51 @@ def test_refusals():
     with pytest.raises(ValueError, match="count"):
         c.own.read(x, x, count=torch.zeros(2, device="cuda"))
     assert math.isfinite(float(plan.run(c.qd, c.ctx, c.own).float().sum()))
+
+
+# ---------------------------------------------------------------------------------------------
+# Log sums of any strides
+# ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype="bf16", B=8, K=16, S=1, H=8, Hkv=8, dh=64, T=100, L=20),
+    dict(dtype="bf16", B=2, K=5, S=3, H=4, Hkv=2, dh=128, T=70, L=20, P=7),
+    dict(dtype="f32", B=3, K=4, S=6, H=4, Hkv=2, dh=32, T=50, L=16, P=5),
+    dict(dtype="bf16", B=1, K=60, S=30, H=4, Hkv=1, dh=32, T=70, L=30),
+    dict(dtype="f32", B=1, K=1, S=1, H=1, Hkv=1, dh=32, T=9, L=0),
+], ids=IDS)
+def test_weights_of_strided_log_sums(kw):
+    """Log sums head by head, row by row, in a wider tensor and shared along an axis: the weights of the dense ones."""
+    _say("strided log sums", kw)
+    c = Case(**kw, seed=12).device()
+    plan = c.plan()
+    _, lse = c.run(plan)
+    lse = lse.clone()
+
+    def weights(lse):
+        w = torch.zeros(c.B, c.Hkv, c.T, device="cuda"), torch.zeros(c.B * c.K, c.Hkv, c.L, device="cuda")
+        plan.weigh(c.qd, lse, c.ctx, c.own, w[0] if c.T else None, w[1] if c.L else None, q_len=c.q_len)
+        return w
+
+    def wide(x):
+        y = torch.full([2 * n + 1 for n in x.shape], NAN, device="cuda")[:x.shape[0], 1:1 + x.shape[1], -x.shape[2]:, :x.shape[3]]
+        return y.copy_(x)
+
+    want = weights(lse)
+    by_head = lse.view(c.B, c.K, c.S, c.Hkv, -1).permute(0, 3, 1, 2, 4).contiguous()
+    for got in (weights(by_head.permute(0, 2, 3, 1, 4).flatten(3, 4)), weights(lse.permute(3, 2, 1, 0).contiguous().permute(3, 2, 1, 0)),
+                weights(wide(lse))):
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    one = lse[:, :1].expand(lse.shape)
+    for a, b in zip(weights(one), weights(one.contiguous())):
+        assert torch.equal(a, b)
+
+
+def test_refusals_of_log_sums():
+    c = Case("bf16", B=2, K=2, S=1, H=2, Hkv=1, dh=32, T=8, L=4, P=4, lens="full").device()
+    plan = c.plan()
+    w = torch.zeros(2, 1, 8, device="cuda")
+    for lse in (torch.zeros(2, 2, 1, 2, device="cuda").double(), torch.zeros(2, 2, 1, 3, device="cuda")[..., :1], torch.zeros(7, device="cuda"),
+                torch.zeros(2, 2, 2, 1, device="cuda").transpose(0, 2)[:, :, :, :1].expand(2, 2, 2, 2)):
+        with pytest.raises(ValueError, match="lse"):
+            plan.weigh(c.qd, lse, c.ctx, c.own, ctx_w=w)

@@ -259,3 +259,33 @@ def test_held_values_are_exact_in_bf16():
     x = np.random.default_rng(3).standard_normal((7, 64))
     v = ref.held_values(x)
     assert np.array_equal(torch.tensor(v).bfloat16().double().numpy(), v)
+
+
+# ---------------------------------------------------------------------------------------------
+# Log sums of any strides
+# ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("ld,word,status", [
+    ((24, 8, 4, -1), "negative", fe.FE_EINVAL), ((-24, 8, 4, 1), "negative", fe.FE_EINVAL),
+    ((1, 1 << 30, 4, 1), "apart", fe.FE_EUNSUPPORTED), ((1, 8, 1 << 31, 1), "apart", fe.FE_EUNSUPPORTED),
+    ((1 << 50, 8, 4, 1), "apart", fe.FE_EUNSUPPORTED), ((1, 1 << 62, 1 << 62, 1 << 62), "apart", fe.FE_EUNSUPPORTED),
+])
+def test_strides_of_log_sums_are_checked(ld, word, status):
+    lib = fe.load_library()
+    st = lib.fe_packed_weights_strided(ctypes.byref(_attend()), (ctypes.c_int64 * 4)(*ld), None)
+    assert st == status and word in lib.fe_last_error().decode()
+
+
+def test_strided_weights_check_what_the_dense_ones_do():
+    lib, ld = fe.load_library(), (ctypes.c_int64 * 4)(24, 8, 4, 1)
+    assert lib.fe_packed_weights_strided(ctypes.byref(_attend()), None, None) == fe.FE_EINVAL
+    assert lib.fe_packed_weights_strided(None, ld, None) == fe.FE_EINVAL
+    for kw, word in ((dict(lse=None), "lse"), (dict(ctx_w=None), "together"), (dict(n_heads=3), "multiple")):
+        assert lib.fe_packed_weights_strided(ctypes.byref(_attend(**kw)), ld, None) == fe.FE_EINVAL
+        assert word in lib.fe_last_error().decode()
+    # the axes of one element: their stride is not looked at, and the workspace is the next thing that is missing
+    many = _attend(K=3000, S=40, own=_cache(N=6000), ws=None)
+    for n in (dict(), dict(B=1, ctx=_cache(N=1), own=_cache(N=3000))):
+        a = _fill(many, {}, n)
+        st = lib.fe_packed_weights_strided(ctypes.byref(a), (ctypes.c_int64 * 4)(-5 if n else 1, 1, 0, 7), None)
+        assert st == fe.FE_EINVAL and "workspace" in lib.fe_last_error().decode()
