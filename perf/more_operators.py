@@ -264,7 +264,7 @@ def prepare(case, seed):
               q_len=ints(q)[pair].contiguous() if case["ragged"] else None)
     if kind == "weigh":
         had = 8 * S * (H // Hkv) / (T + L)                  # about what a few such calls before gave a row of one list
-        st.update(lse=_plain_attend(st)["lse"].contiguous(),
+        st.update(lse=_plain_attend(st)["lse"],
                   ctx_w=torch.rand(B, Hkv, st["ctx_table"].shape[1] * P, generator=g, device=DEV) * had * K,
                   own_w=torch.rand(B * K, Hkv, st["own_table"].shape[1] * P, generator=g, device=DEV) * had)
         st.update(ctx_w_out=torch.zeros_like(st["ctx_w"]), own_w_out=torch.zeros_like(st["own_w"]))
