@@ -112,7 +112,8 @@ fe_status fe_packed_read(const fe_packed_read_args* a, void* stream);
  * the held ones are exact, probabilities are rounded to bf16 for the product with the values (up to
  * 32 rows a request and key head: to two bf16, 16 bits).  FE_F32: queries and
  * probabilities in three bf16 parts whose sum they are, the held values whole: no product is rounded.  A row
- * with an infinite score is NaN.  A list's outputs do not depend on the own rows of other lists, NaN or not.  Results have the same
+ * with a score of +infinity or NaN is NaN, and so is one whose scores are all -infinity; beside finite ones a score of
+ * -infinity weighs nothing.  (Scores are fp32: infinite from 2^128 on.)  A list's outputs do not depend on the own rows of other lists, NaN or not.  Results have the same
  * bits from call to call.
  *
  * fe_packed_weights: for every row j < len of `ctx` and of `own` and every key head g

@@ -74,6 +74,19 @@ FE_DEV int q_rows(const PackedArgs& a, int bk) { return a.q_len ? min(max(a.q_le
 FE_DEV int own_rows(const PackedArgs& a, int bk) { return a.own.cap ? packed_len(a.own, bk) : 0; }
 FE_DEV int ctx_rows(const PackedArgs& a, int b) { return a.ctx.cap ? packed_len(a.ctx, b) : 0; }
 
+// Whether one of the first `n` rows of sequence s has a page in the pool.
+FE_DEV bool any_key(const PackedCache& x, long long s, int n) {
+  for (int j = 0, p = 0; j < n; j += x.page_rows, ++p)
+    if ((unsigned)x.table[s * x.cols + p] < (unsigned)x.n_pages) return true;
+  return false;
+}
+// Whether row `at` = (b K + k) S + s, one in use, sees a key at all.  Asked where a sum is 0 alone: of rows without keys, and of
+// rows whose scores are all -infinity, which are NaN.
+FE_DEV bool any_key(const PackedArgs& a, long long at) {
+  const int bk = (int)(at / a.S), s = (int)(at % a.S), b = bk / a.K, n = q_rows(a, bk), m = own_rows(a, bk);
+  return any_key(a.ctx, b, ctx_rows(a, b)) || any_key(a.own, bk, a.causal ? min(max(m - n + s + 1, 0), m) : m);
+}
+
 // log2(e) |scale|; positive, so that masked scores stay -infinity when scale is 0.
 FE_DEV float score_unit(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-37f); }
 
@@ -608,8 +621,14 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
   const float l_all = halves_sum(l_run);
   const bool in = r0 + wr * 32 + c32 < a.R;
   const long long ro = row.at * a.Hq + row.h;
+  // No key; a NaN score leaves a NaN sum, and 0 for all keys, where each is -infinity, NaN as 0 times 1 / 0.
+  auto none_of = [&](float l) __attribute__((always_inline)) {
+    if (!row.live || l != 0.f) return !row.live;
+    const PackedArgs& again = *(const PackedArgs*)args_again();
+    return again.splits == 1 && !any_key(again, row.at);
+  };
   // Slice i of a lane: columns 8 i + 4 half .. + 3, v its sums against reference m (in units of 1 / sl2).
-  auto store = [&](int i, f32x4 v, float m, float l) __attribute__((always_inline)) {
+  auto store = [&](int i, f32x4 v, float m, float l, bool none) __attribute__((always_inline)) {
     const float m2 = m * sl2;
     if (a.splits > 1) {
       const long long at = ro + (long long)(range - b) * a.K * a.S * a.Hq;   // [range][row of the request]
@@ -617,14 +636,13 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
       if (i == 0 && half == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = float2{m2, l};
       return;
     }
-    const bool none = !row.live || l == 0.f;   // no key; a NaN score leaves a NaN sum
     const float inv = none ? 0.f : 1.f / l;
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 w;
 #pragma unroll
     for (int x = 0; x < 4; ++x) w[x] = from_f32<T>(none ? 0.f : v[x] * inv);
     *reinterpret_cast<T4*>(static_cast<T*>(a.out) + row.at * a.out_ld + row.h * DH + 8 * i + 4 * half) = w;
-    if (a.lse && i == 0 && half == 0) a.lse[ro] = none ? -INFINITY : (m2 + log2f(l)) * kLn2;
+    if (a.lse && i == 0 && half == 0) a.lse[ro] = none ? -INFINITY : l == 0.f ? NAN : (m2 + log2f(l)) * kLn2;
   };
   auto slice = [&](int i) __attribute__((always_inline)) {
     const f32x16 v = o[i >> 2];
@@ -632,8 +650,9 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
   };
   if constexpr (WK == 1) {
     if (!in) return;
+    const bool none = none_of(l_all);
 #pragma unroll
-    for (int i = 0; i < 4 * NB; ++i) store(i, slice(i), m_run, l_all);
+    for (int i = 0; i < 4 * NB; ++i) store(i, slice(i), m_run, l_all, none);
   } else {                                 // joins the groups in their order, every group some of the slices
     __syncthreads();
     float* X = reinterpret_cast<float*>(s_kv);
@@ -654,6 +673,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
       f[w] = __builtin_amdgcn_exp2f((s_ml[w * WR + wr][c32][0] - ref) * sl2);
       l = fmaf(s_ml[w * WR + wr][c32][1], f[w], l);
     }
+    const bool none = none_of(l);
 #pragma unroll 1
     for (int i = grp; i < 4 * NB; i += WK) {
       f32x4 v{};
@@ -663,7 +683,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
 #pragma unroll
         for (int y = 0; y < 4; ++y) v[y] = fmaf(x[y], f[w], v[y]);
       }
-      store(i, v, top, l);
+      store(i, v, top, l, none);
     }
   }
 }
@@ -716,14 +736,14 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
   }
   const long long at = ro / a.Hq;
   const int h = (int)(ro % a.Hq), bk = (int)(at / a.S), s = (int)(at % a.S);
-  const bool none = s >= q_rows(a, bk) || l == 0.f;
+  const bool none = s >= q_rows(a, bk) || (l == 0.f && !any_key(a, at));
   const float inv = none ? 0.f : 1.f / l;
   typedef T T4 __attribute__((ext_vector_type(4)));
   T4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(none ? 0.f : o[i] * inv);
   *reinterpret_cast<T4*>(static_cast<T*>(a.out) + at * a.out_ld + h * DH + d0) = v;
-  if (a.lse && d0 == 0) a.lse[ro] = none ? -INFINITY : (top + log2f(l)) * kLn2;
+  if (a.lse && d0 == 0) a.lse[ro] = none ? -INFINITY : l == 0.f ? NAN : (top + log2f(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------------------

@@ -906,3 +906,99 @@ def test_refusals_of_log_sums():
                 torch.zeros(2, 2, 2, 1, device="cuda").transpose(0, 2)[:, :, :, :1].expand(2, 2, 2, 2)):
         with pytest.raises(ValueError, match="lse"):
             plan.weigh(c.qd, lse, c.ctx, c.own, ctx_w=w)
+
+
+# ---------------------------------------------------------------------------------------------
+# Infinite scores
+# ---------------------------------------------------------------------------------------------
+
+INFINITE = [
+    dict(dtype="bf16", B=1, K=1, S=1, H=1, Hkv=1, dh=32, T=1, L=0, P=1, lens="full"),
+    dict(dtype="bf16", B=2, K=5, S=1, H=4, Hkv=4, dh=32, T=181, L=12),
+    dict(dtype="bf16", B=64, K=1, S=2, H=8, Hkv=8, dh=128, T=37, L=9, P=4),
+    dict(dtype="bf16", B=1, K=45, S=1, H=2, Hkv=2, dh=32, T=150, L=20, P=48),
+    dict(dtype="bf16", B=1, K=1, S=50, H=1, Hkv=1, dh=128, T=70, L=80, P=16),
+    dict(dtype="bf16", B=1, K=140, S=1, H=1, Hkv=1, dh=128, T=700, L=9, P=64),
+    dict(dtype="bf16", B=1, K=2, S=150, H=3, Hkv=1, dh=128, T=20, L=150, P=48, lens="own"),
+    dict(dtype="bf16", B=1, K=3, S=1, H=4, Hkv=1, dh=64, T=3000, L=100, P=64),
+    dict(dtype="f32", B=1, K=2, S=2, H=2, Hkv=1, dh=64, T=4500, L=10, P=48),
+    dict(dtype="f32", B=2, K=13, S=11, H=4, Hkv=4, dh=32, T=64, L=11, P=5, causal=False, lens="own"),
+    # rows without keys, pages outside the pool
+    dict(dtype="bf16", B=6, K=5, S=3, H=4, Hkv=2, dh=32, T=40, L=9, P=4, lens="edge"),
+    dict(dtype="bf16", B=6, K=5, S=9, H=4, Hkv=2, dh=64, T=140, L=70, P=10, lens="edge", causal=False),
+    dict(dtype="f32", B=6, K=7, S=4, H=2, Hkv=1, dh=32, T=33, L=20, P=3, lens="edge"),
+    dict(dtype="bf16", B=3, K=4, S=2, H=4, Hkv=2, dh=64, T=10, L=10, P=5, holes=16),
+    dict(dtype="f32", B=2, K=50, S=1, H=4, Hkv=2, dh=128, T=16, L=16, P=8, holes=70),
+]
+
+
+def _first_column(c, code):
+    """Column 0 of every cached key is the 4-bit float `code` of its block's scale."""
+    for r in range(c.P):
+        at = ref.place(c.P, c.dh, 0, r)[0].start
+        c.pages[:, :, at] = c.pages[:, :, at] & 0xF0 | code
+    return c
+
+
+def _sees(c):
+    """[B][K][S] rows that see a key."""
+    nc, nq, no = c.lengths()
+    ctx, own = c.seen(c.ct), c.seen(c.ot).reshape(c.B, c.K, c.L)
+    some = np.zeros((c.B, c.K, c.S), bool)
+    for b in range(c.B):
+        for k in range(c.K):
+            for i in range(nq[b, k]):
+                m = no[b, k]
+                to = min(max(m - nq[b, k] + i + 1, 0), m) if c.causal else m
+                some[b, k, i] = ctx[b, :nc[b]].any() or own[b, k, :to].any()
+    return some
+
+
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+@pytest.mark.parametrize("kw", INFINITE, ids=IDS)
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(kw, scale):
+    """Queries with an infinity over keys whose column has the other sign: NaN, as softmax of such scores is, and not the zeros
+    of a row that sees no key."""
+    _say("all -infinity", kw, scale)
+    c = _first_column(Case(**kw, scale=scale, seed=21), 2)
+    live = ~np.isnan(c.q[..., 0])
+    c.q[..., 0] = np.where(live, -INF if scale > 0 else INF, NAN)
+    out, lse = c.device().run()
+    some = torch.tensor(_sees(c)).cuda()
+    assert torch.isnan(out[some]).all() and torch.isnan(lse[some]).all()
+    assert (out[~some] == 0).all() and torch.isneginf(lse[~some]).all()
+
+
+@pytest.mark.parametrize("kw", [k for k in INFINITE if k.get("lens") != "edge"], ids=IDS)
+def test_rows_beside_one_with_infinite_scores_keep_their_bits(kw):
+    c = _first_column(Case(**kw, seed=22), 2).device()
+    out, lse = (t.clone() for t in c.run())
+    row = (c.B - 1, c.K // 2, 0, c.H - 1)
+    for value in (-INF, INF, NAN):
+        c.qd[row][0] = value
+        got, lse2 = c.run()
+        other = torch.ones_like(lse, dtype=torch.bool)
+        other[row] = False
+        assert torch.equal(got[other], out[other]) and torch.equal(lse2[other], lse[other])
+        if _sees(c)[row[:3]]:
+            assert torch.isnan(got[row]).all() and torch.isnan(lse2[row])
+
+
+@pytest.mark.parametrize("kw", [INFINITE[1], INFINITE[4], INFINITE[5], INFINITE[7], INFINITE[8]], ids=IDS)
+def test_a_score_of_minus_infinity_beside_finite_ones_weighs_nothing(kw):
+    """Products that overflow for some keys: the row is the softmax over the others, the bits that they give without these."""
+    c = Case(**{**kw, "lens": "full"}, seed=23)
+    nc, _, no = c.lengths()
+    c.q[..., 0] = -2.0 ** 127
+    _first_column(c, 0)                                                  # a 0 there: finite
+    far = [(c.ct, b, j) for b in range(c.B) for j in range(0, nc[b], 3)] + \
+          [(c.ot, s, j) for s in range(c.B * c.K) for j in range(0, no.reshape(-1)[s], 2)] if c.L else []
+    for t, s, j in far:
+        at, by = ref.place(c.P, c.dh, 0, j % c.P)
+        c.pages[t[s, j // c.P], :, at.start] |= 7                        # 6 times a scale of 1: beyond fp32
+        c.pages[t[s, j // c.P], :, by.start] = 127
+    got, lse = c.device().run()
+    # the same keys far below the others, by a finite query
+    c.q[..., 0] = -2.0 ** 90
+    want, lse2 = c.device().run()
+    assert torch.isfinite(got).all() and torch.equal(got, want) and torch.equal(lse, lse2)
