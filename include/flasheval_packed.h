@@ -60,8 +60,7 @@ fe_status fe_packed_page_bytes(int32_t page_rows, int32_t n_kv_heads, int32_t dh
  *   values of that row = held(v[s][i])
  *   q_out[s][i]        = rotate(q[s][i], pos0[s] + j), rounded to its type     (when q is given)
  *   len_out[s]         = len[s] + n(s)                                         (when len_out is given; may be len)
- * with rotate as in fe_cache_append, the angle and its sine and cosine in fp64, of the keys the products as well: what is held is
- * the nearest to the turned key itself.
+ * with rotate as in fe_cache_append, in fp64 throughout: what is held, and what q_out gets, is the nearest to the turned row itself.
  * A row whose index reaches the capacity, or whose table entry names no page, is not written (its q_out row is);
  * status[s] is FE_DEV_BAD_PAGE then and 0 otherwise.  Other rows of the pages and rows i >= n(s) of q_out are left as they
  * were.  Two new rows must not share a cache row.

@@ -29,6 +29,10 @@ FE_DEV float to_odd(double x) {
   if (back != a) b |= 1;
   return copysignf(__uint_as_float(b), (float)x);
 }
+template <typename T> FE_DEV T rounded(double x);
+template <> FE_DEV float rounded<float>(double x) { return (float)x; }
+template <> FE_DEV bf16 rounded<bf16>(double x) { return (bf16)to_odd(x); }
+
 // Eight codes of a block that the lanes of a quad share (lane i: columns 8 i ..), and the block's scale.  The magnitudes'
 // leading bits as integers order as they do; 1.5 * 2^(E - bias) is the largest whose scale is 2 below its exponent.
 FE_DEV unsigned codes8(const float (&f)[8], float unit) {
@@ -78,14 +82,13 @@ constexpr int kAppendRows = 64;           // rows of a workgroup
 // One workgroup takes `rows` (a power of two) consecutive new rows of one sequence: sines and cosines of a row are
 // formed once, in LDS, for all its heads; then every thread takes units of 8 columns, 4 lanes a block, consecutive
 // units along a row, then rows, then heads, as the pages hold them.
-// Bound: HBM beside the vector unit (71%), the keys' fp64 and the sines: 24 x 1000 rows of 24 heads of 128, bf16, 246 MB: 60 us,
-// 4.1 TB/s (units requested when they are needed 70; the queries in fp64 as well 71).  128 rows of 24 heads of 64: 4.6 us,
+// Bound: the vector unit (fp64 and the sines) beside HBM: 24 x 1000 rows of 24 heads of 128, bf16, 246 MB: 68 us, 3.6 TB/s.  The
+// queries in fp32 60 us, but then a turned query may go to the number that is not the nearest.  128 rows of 24 heads of 64: 4.6 us,
 // launch latency and a trip to memory.
 template <typename T>
 __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, PackedCache c, int log_rows, int blocks) {
   typedef typename Vec8<T>::type V8;
   __shared__ double s_cos[kTurns], s_sin[kTurns];
-  __shared__ float s_cos32[kTurns], s_sin32[kTurns];
   __shared__ long long s_page[kAppendRows];
   __shared__ int s_row[kAppendRows];
   const int tid = threadIdx.x, s = blockIdx.x / blocks, blk = blockIdx.x % blocks, rows = 1 << log_rows;
@@ -126,12 +129,7 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
   }
   for (int e = tid; e < m * np; e += 256) {
     const int r = e / np;
-    double sn, cs;
-    sincos((double)(pos0 + i0 + r) * a.freq[e - r * np], &sn, &cs);
-    s_sin[e] = sn;
-    s_cos[e] = cs;
-    s_sin32[e] = (float)sn;
-    s_cos32[e] = (float)cs;
+    sincos((double)(pos0 + i0 + r) * a.freq[e - r * np], &s_sin[e], &s_cos[e]);
   }
   if (blk == 0 && a.status) {              // uniform over the workgroup: the pages of all n rows
     int bad = (long long)len + n > c.cap && n > 0;
@@ -162,26 +160,9 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
     const bool turned = !is_v && 8 * x < a.rot, apart = turned && !a.neighbours;   // apart: the pair's columns lie rot / 2 apart
     const bool second = 8 * x >= np;
     const int c0 = !apart ? 4 * x : second ? 8 * x - np : 8 * x;       // the unit's first pair
-    if (is_q) {                            // in fp32: nothing but a rounding follows
-      V8 out = mine;
-      if (turned) {
-        const float *cs = s_cos32 + r * np + c0, *sn = s_sin32 + r * np + c0;
-        if (apart) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float u = to_f32((T)mine[i]), v = to_f32((T)pair[i]);
-            out[i] = from_f32<T>(fmaf(u, cs[i], second ? v * sn[i] : -v * sn[i]));
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float u = to_f32((T)mine[2 * i]), v = to_f32((T)mine[2 * i + 1]);
-            out[2 * i] = from_f32<T>(fmaf(u, cs[i], -v * sn[i]));
-            out[2 * i + 1] = from_f32<T>(fmaf(v, cs[i], u * sn[i]));
-          }
-        }
-      }
-      *reinterpret_cast<V8*>(static_cast<T*>(a.q_out) + row * a.q_out_ld + h * a.dh + 8 * x) = out;
+    T* q_out = static_cast<T*>(a.q_out) + row * a.q_out_ld + h * a.dh + 8 * x;
+    if (is_q && !turned) {
+      *reinterpret_cast<V8*>(q_out) = mine;
       continue;
     }
     if (is_v || a.rot == 0) {
@@ -209,6 +190,13 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
             y[2 * i + 1] = v * cs[i] + u * sn[i];
           }
         }
+      }
+      if (is_q) {
+        V8 out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = rounded<T>(y[i]);
+        *reinterpret_cast<V8*>(q_out) = out;
+        continue;
       }
       w = held(y, &scale);
     }

@@ -1002,3 +1002,41 @@ def test_a_score_of_minus_infinity_beside_finite_ones_weighs_nothing(kw):
     c.q[..., 0] = -2.0 ** 90
     want, lse2 = c.device().run()
     assert torch.isfinite(got).all() and torch.equal(got, want) and torch.equal(lse, lse2)
+
+
+# ---------------------------------------------------------------------------------------------
+# Turned queries
+# ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [k for k in APPEND if k["H"]], ids=lambda k: f"{k['dtype']}-N{k['N']}-S{k['S']}-dh{k['dh']}-rot{k['rot']}-P{k['P']}")
+def test_append_turns_queries_to_the_nearest(kw):
+    """q_out is the turned query rounded once: off by half a step of its own size, and by the fp64 products of sines good to
+    2^-52, 2^-50 (|a| + |b|) in all."""
+    c = _append_case(**kw, seed=31)
+    empty = np.zeros((c["n_pages"], kw["Hkv"], ref.head_bytes(kw["P"], kw["dh"])), np.uint8)
+    q0 = np.full((kw["N"], kw["S"], kw["H"], kw["dh"]), 7.0)
+    _, want = _append_want(c, pages=empty.copy(), q_out=q0.copy(), **kw)
+    _, got, _ = _append_run(c, pages=empty, q_out=q0, **kw)
+    pair = dense.turned_bound(c["q"], c["freq"], kw["near"], kw["dtype"]) / (dense.HALF_STEP[kw["dtype"]] + 2.0 ** -21)
+    assert (np.abs(_np(got) - want) <= dense.HALF_STEP[kw["dtype"]] * np.abs(want) + 2.0 ** -50 * pair).all()
+
+
+def test_append_turns_queries_next_to_a_border():
+    """Turned queries down to 2^-22 from the border between two bf16 numbers, on both sides, go to the nearer one."""
+    r = np.random.default_rng(7)
+    N, angle = 4000, 0.7
+    b = torch.tensor(r.uniform(1, 2, (N, 16))).bfloat16().double().numpy()
+    a = torch.tensor(r.uniform(1, 2, (N, 16))).bfloat16().double().numpy()
+    c = dict(q=np.concatenate((a, b), -1)[:, None, None], k=np.zeros((N, 1, 1, 32)), v=np.zeros((N, 1, 1, 32)), new=np.ones(N, int),
+             len=np.zeros(N, int), pos0=np.ones(N, int), freq=np.full(16, angle), table=np.arange(N)[:, None])
+    kw = dict(dtype="bf16", Hkv=1, dh=32, rot=32, P=1, near=False)
+    empty, q0 = np.zeros((N, 1, ref.head_bytes(1, 32)), np.uint8), np.zeros((N, 1, 1, 32))
+    _, want = _append_want(c, N=N, pages=empty.copy(), q_out=q0.copy(), **kw)
+    _, got, _ = _append_run(c, pages=empty, q_out=q0, **kw)
+    # the smallest are about 2^-14, so fp64 products of size 2 are off by 2^-36 of them at most, 2^16 units of 2^-52: less than
+    # any one's distance from a border, and the nearest bf16 number is the same by every fp64 way to it
+    bits = want.view(np.int64)
+    rest = (bits & ((1 << 45) - 1)) - (1 << 44)                          # to the border, in units of 2^-52 of the exponent
+    assert np.abs(want).min() > 2.0 ** -15 and 1 << 24 < np.abs(rest).min() < 1 << 30
+    nearest = ((bits + (1 << 44)) & ~((1 << 45) - 1)).view(np.float64)
+    assert np.array_equal(_np(got), nearest)
