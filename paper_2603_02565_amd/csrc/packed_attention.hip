@@ -87,8 +87,8 @@ FE_DEV bool any_key(const PackedArgs& a, long long at) {
   return any_key(a.ctx, b, ctx_rows(a, b)) || any_key(a.own, bk, a.causal ? min(max(m - n + s + 1, 0), m) : m);
 }
 
-// log2(e) |scale|; positive, so that masked scores stay -infinity when scale is 0.
-FE_DEV float score_unit(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-37f); }
+// log2(e) |scale|; positive, so that masked scores stay -infinity: with a scale of 0 the queries are 0 in its place.
+FE_DEV float score_unit(float scale) { return scale == 0.f ? 1.f : fabsf(scale) * kLog2e; }
 
 // The two halves of a wave hold the same rows.
 FE_DEV float halves_max(float v) {
@@ -401,11 +401,15 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
   const bool by_wave = WR > 1 && 2 * a.S * a.G <= ROWS;
   const int cown = by_wave ? 0 : (nown + KC - 1) / KC, ob = share(cown, z, splits), nq = nc + share(cown, z + 1, splits) - ob;
 
+  if (a.scale <= 0) {                      // uniform
+#pragma unroll
+    for (int c = 0; c < ND; ++c)           // negative: exact, and the largest score is then the largest product; 0: 0, of infinities NaN
+      qreg[c] = a.scale < 0 ? -qreg[c] : qreg[c] - qreg[c];
+  }
   Op qf[ND];
 #pragma unroll
   for (int c = 0; c < ND; ++c) {
     if (!row.live) qreg[c] = typename F::V{};
-    if (a.scale < 0) qreg[c] = -qreg[c];   // exact; the largest score is then the largest product
     qf[c] = F::of(qreg[c]);
   }
   const float sl2 = score_unit(a.scale), lag = fminf(8.f / sl2, 1e30f);

@@ -1040,3 +1040,52 @@ def test_append_turns_queries_next_to_a_border():
     assert np.abs(want).min() > 2.0 ** -15 and 1 << 24 < np.abs(rest).min() < 1 << 30
     nearest = ((bits + (1 << 44)) & ~((1 << 45) - 1)).view(np.float64)
     assert np.array_equal(_np(got), nearest)
+
+
+# ---------------------------------------------------------------------------------------------
+# Scales of 0 and next to it
+# ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 2.0 ** -124, -2.0 ** -126, 2.0 ** -128])
+@pytest.mark.parametrize("kw", [dict(dtype="bf16", B=2, K=3, S=2, H=2, Hkv=2, dh=32, T=60, L=12, P=4),
+                                dict(dtype="f32", B=2, K=3, S=2, H=2, Hkv=2, dh=32, T=60, L=12, P=4),
+                                dict(dtype="bf16", B=1, K=40, S=2, H=2, Hkv=1, dh=64, T=70, L=12, P=4),
+                                dict(dtype="bf16", B=1, K=2, S=2, H=2, Hkv=1, dh=128, T=1500, L=12, P=16)], ids=IDS)
+def test_scales_next_to_zero_over_large_products(kw, scale):
+    """Products of queries and keys up to 2^127: a scale of 0 gives every key the same weight, one of 2^-126 the weights of that."""
+    class Large(Case):
+        def __init__(self, **kw):
+            super().__init__(**kw)
+            self.q *= 2.0 ** 98
+            self.ck *= 2.0 ** 24
+            self.ok *= 2.0 ** 24
+            for r in range(self.P):                                       # the scale bytes of the keys
+                at = ref.place(self.P, self.dh, 0, r)[1]
+                self.pages[:, :, at] = np.where(self.pages[:, :, at] == 255, 255, np.minimum(self.pages[:, :, at], 230) + 24)
+
+    c = Large(**kw, scale=scale, seed=41).device()
+    want = c.reference()
+    out, lse = c.run()
+    _near(out, want["out"], "out")
+    _near(lse, want["lse"], "lse")
+    nc, nq, no = c.lengths()
+    cw, ow = np.zeros((c.B, c.Hkv, c.T), np.float32), np.zeros((c.B, c.K, c.Hkv, c.L), np.float32)
+    at = lse.cpu().numpy()
+    weights = ref.weigh(c.q, c.ck, c.ok, at, causal=c.causal, scale=c.scale, ctx_len=nc, q_len=nq, own_len=no, ctx_w=cw, own_w=ow)
+    cd, od = torch.tensor(cw).cuda(), torch.tensor(ow).cuda()
+    c.plan().weigh(c.qd, lse, c.ctx, c.own, cd, od, q_len=c.q_len)
+    _near(cd, weights["ctx_w"], "ctx_w")
+    _near(od, weights["own_w"], "own_w")
+
+
+def test_a_scale_of_zero_over_what_is_no_number():
+    """0 times an infinity is no number: the row is NaN, whatever the infinity's sign; the others keep their bits."""
+    c = _first_column(Case("bf16", B=2, K=3, S=2, H=2, Hkv=2, dh=64, T=60, L=12, P=4, scale=0.0, lens="full", seed=42), 2).device()
+    out, lse = (t.clone() for t in c.run())
+    for value in (INF, -INF, NAN):
+        c.qd[1, 1, 0, 1, 0] = value
+        got, lse2 = c.run()
+        other = torch.ones_like(lse, dtype=torch.bool)
+        other[1, 1, 0, 1] = False
+        assert torch.isnan(got[1, 1, 0, 1]).all() and torch.isnan(lse2[1, 1, 0, 1])
+        assert torch.equal(got[other], out[other]) and torch.equal(lse2[other], lse[other])
