@@ -677,7 +677,7 @@ class _Layouts:
         if got is None:
             got = check(*tensors)
             if len(self.known) >= self.MOST:
-                del self.known[next(iter(self.known))]
+                self.known.pop(list(self.known)[0], None)        # the oldest; another thread may have been here
             self.known[key] = got
         return got
 
@@ -725,11 +725,12 @@ class _Kept:
         if handle in self.known:
             return
         import torch
-        if not torch.cuda.is_current_stream_capturing():
-            self.known.add(handle)
-        elif torch.cuda.current_stream().cuda_stream != self.home.cuda_stream:
+        capturing = torch.cuda.is_current_stream_capturing()
+        if capturing and torch.cuda.current_stream().cuda_stream != self.home.cuda_stream:
             return                           # a capture cannot wait for work outside it; it begins after that
         _allocated_for(handle, *self.tensors, home=self.home)
+        if not capturing:
+            self.known.add(handle)           # last: another thread that finds it there need not wait
 
 
 def _addr(t) -> Optional[int]:
@@ -931,7 +932,8 @@ class PagedCache4:
     pages [n_pages][page_bytes(page_rows, n_kv_heads, dh)] uint8 and table [N][cols] int32 are the caller's:
     table[s][c] names the page that holds rows c * page_rows .. of sequence s.  len [N] int32 counts the rows
     of every sequence; `append` advances it, `evict` sets that of the cache it fills.  A shared context is such a cache of B
-    sequences, the lists' own rows one of B * K; both may use one pool."""
+    sequences, the lists' own rows one of B * K; both may use one pool.  Several threads may call one cache: every call has
+    arguments of its own.  `status` is that of the last append or eviction."""
 
     def __init__(self, pages, table, page_rows: int, n_kv_heads: int, dh: int, length=None):
         import torch
@@ -997,7 +999,7 @@ class PagedCache4:
         [rot / 2]) keys and q [N][S][n_heads][dh] are turned by their positions pos0[s] + row.  q_out defaults to a new
         tensor and may not be q; it is returned.  The lengths advance in place, or into len_out when that is given.
         `status` [N] holds FE_DEV_BAD_PAGE for a sequence with a row that found no page."""
-        a = self.args
+        a = fe_packed_append_args.from_buffer_copy(self.args)
         if (q is None) != (q_out is None):
             if q is None:
                 raise ValueError("q_out without q")
@@ -1032,7 +1034,7 @@ class PagedCache4:
         rows of k and v are left as they were.  Without k and v: new bf16 tensors of the cache's capacity, zeros past the
         length.  Returns (k, v)."""
         import torch
-        a = self.read_args
+        a = fe_packed_read_args.from_buffer_copy(self.read_args)
         if k is None and v is None:
             k, v = (torch.zeros((self.N, self.capacity, self.n_kv_heads, self.dh), dtype=torch.bfloat16,
                                 device=self.pages.device) for _ in range(2))
@@ -1053,7 +1055,7 @@ class PagedCache4:
         part of weights; their indices here to kept [N][n_kv_heads][keep] int32 (-1 where there are fewer), which is
         returned.  `status` holds FE_DEV_BAD_PAGE for a sequence with rows of no page."""
         import torch
-        a = self.evict_args
+        a = fe_packed_evict_args.from_buffer_copy(self.evict_args)
         if (to.N, to.n_kv_heads, to.dh) != (self.N, self.n_kv_heads, self.dh):
             raise ValueError(f"to: expected {self.N} sequences of {self.n_kv_heads} heads of {self.dh}, got "
                              f"{(to.N, to.n_kv_heads, to.dh)}")

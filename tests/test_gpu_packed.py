@@ -1089,3 +1089,85 @@ def test_a_scale_of_zero_over_what_is_no_number():
         other[1, 1, 0, 1] = False
         assert torch.isnan(got[1, 1, 0, 1]).all() and torch.isnan(lse2[1, 1, 0, 1])
         assert torch.equal(got[other], out[other]) and torch.equal(lse2[other], lse[other])
+
+
+# ---------------------------------------------------------------------------------------------
+# Two threads
+# ---------------------------------------------------------------------------------------------
+
+def _during(monkeypatch, name, other):
+    """The binding's call `name` runs `other` once just before it enters the library, as another thread may."""
+    real, calls = getattr(fe, name), []
+
+    def call(args, stream=None):
+        if not calls:
+            calls.append(1)
+            other()
+        real(args, stream)
+
+    monkeypatch.setattr(fe, name, call)
+
+
+def test_reads_and_evictions_of_one_cache_from_two_threads(monkeypatch):
+    """A call's arguments are its own: another thread's call on the same cache in between does not change them."""
+    P, Hkv, dh, N = 8, 2, 64, 3
+    g = torch.Generator(device="cuda").manual_seed(9)
+    width = PagedCache4.page_bytes(P, Hkv, dh)
+    pages = lambda n: torch.zeros(n, width, dtype=torch.uint8, device="cuda")                             # noqa: E731
+    cache = PagedCache4(pages(N * 4), torch.arange(N * 4, device="cuda").int().view(N, 4), P, Hkv, dh)
+    cache.append(*(torch.randn(N, 30, Hkv, dh, generator=g, device="cuda").bfloat16() for _ in range(2)))
+    want = [t.clone() for t in cache.read()]
+    new = lambda n, dt: [torch.full((N, n, Hkv, dh), 3.0, dtype=dt, device="cuda") for _ in range(2)]     # noqa: E731
+    one, two = new(32, torch.bfloat16), new(7, torch.float32)
+    start = _i32([5, 0, 20])
+    with monkeypatch.context() as m:
+        _during(m, "fe_packed_read", lambda: cache.read(*two, start=start))
+        cache.read(*one)
+    for a, b, w in zip(one, two, want):
+        assert torch.equal(a[:, :30], w[:, :30]) and (a[:, 30:] == 3).all()
+        for s, f in enumerate((5, 0, 20)):
+            assert torch.equal(b[s], w[s, f:f + 7].float())
+    to = [PagedCache4(pages(N * 2), torch.arange(N * 2, device="cuda").int().view(N, 2), P, Hkv, dh) for _ in range(2)]
+    w = [torch.rand(N, Hkv, 32, generator=g, device="cuda") for _ in range(2)]
+    got = []
+    with monkeypatch.context() as m:
+        _during(m, "fe_packed_evict", lambda: got.append(cache.evict(w[1], to[1], keep=5, recent=2)))
+        got.insert(0, cache.evict(w[0], to[0], keep=16, first=1))
+    for i, (keep, first, recent) in enumerate(((16, 1, 0), (5, 0, 2))):
+        assert to[i].len.tolist() == [keep] * N
+        k, _ = to[i].read()
+        for s in range(N):
+            for h in range(Hkv):
+                rows = ref.evict_rows(w[i][s, h].tolist(), 30, keep, first, recent)
+                assert got[i][s, h].tolist() == rows and torch.equal(k[s, :keep, h], want[0][s, rows, h])
+
+
+def test_many_threads_read_one_cache():
+    """Eight threads, each with a layout, a stream and outputs of its own."""
+    import threading
+    P, Hkv, dh, N = 8, 2, 32, 2
+    cache = PagedCache4(torch.zeros(N * 8, PagedCache4.page_bytes(P, Hkv, dh), dtype=torch.uint8, device="cuda"),
+                        torch.arange(N * 8, device="cuda").int().view(N, 8), P, Hkv, dh)
+    cache.append(*(torch.randn(N, 64, Hkv, dh, device="cuda").bfloat16() for _ in range(2)))
+    want = [t.clone() for t in cache.read()]
+    torch.cuda.synchronize()
+    bad = []
+
+    def reads(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for n in range(1, 40):                                    # n + i stays below 64
+                    k, v = (torch.zeros(N, n + i, Hkv, dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+                    cache.read(k, v)
+                    if not (torch.equal(k, want[0][:, :n + i]) and torch.equal(v, want[1][:, :n + i])):
+                        bad.append((i, n))
+        except Exception as e:                                            # noqa: BLE001
+            bad.append(repr(e))
+
+    threads = [threading.Thread(target=reads, args=(i,)) for i in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad, bad[:5]
