@@ -131,6 +131,11 @@ __global__ void k_advance(int32_t* len, const int32_t* new_len, int N, int S) {
 
 }  // namespace
 
+hipError_t launch_advance(int32_t* len, const int32_t* new_len, int N, int S, hipStream_t s) {
+  hipLaunchKernelGGL(k_advance, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, len, new_len, N, S);
+  return hipGetLastError();
+}
+
 hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s) {
   // rows per workgroup: about 512 units of 16 columns, two a thread (ragged prompts, 37 x 129 rows: 256 units 11.7 us,
   // 512 11.2, 1024 12.6, 2048 13.8; 16 x 2048 rows: 18.6, 18.8, 19.3, 20.2), and no more sines than the LDS tables hold
@@ -145,8 +150,7 @@ hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s) {
     hipLaunchKernelGGL(k_cache_append<float>, grid, dim3(256), 0, s, a, rows, blocks);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.len_out == a.len && blocks > 1) {
-    hipLaunchKernelGGL(k_advance, dim3((unsigned)((a.N + 255) / 256)), dim3(256), 0, s, a.len_out, a.new_len, a.N, a.S);
-    e = hipGetLastError();
+    e = launch_advance(a.len_out, a.new_len, a.N, a.S, s);
   }
   return e;
 }

@@ -4,6 +4,9 @@
 #include "fe_common.h"
 #include "flasheval_packed.h"
 
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kPackedMaxRows = 1 << 22;  // a sequence's capacity
 
 // Division by a number that a launch does not change, as a multiplication: n magic >> shift, exact for 0 <= n < 2^31.
@@ -27,6 +30,14 @@ PackedCache packed_cache(const fe_packed_cache& c, int dh);
 
 FE_DEV int packed_page(const PackedCache& c, int j) { return quotient(c.by_rows, j); }
 FE_DEV int packed_len(const PackedCache& c, int s) { return min(max(c.len[s], 0), c.cap); }
+
+// Eight columns from four bytes of codes and the block's power of two.
+FE_DEV bf16x8 values8(unsigned w, float unit) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+FE_DEV float unit_of(unsigned scale) { return __uint_as_float(scale << 23); }   // 255: NaN from the conversion
 
 // The attention's and the weights' arguments.  The query rows of a (request, key head) are numbered r = (k S + s) G + hg < R
 // with G = Hq / Hkv: rows that share keys are adjacent.

@@ -9,9 +9,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 FE_DEV f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
 // The side of a product that is not held in 4 bits: eight bf16 values, or eight floats in three bf16 parts whose sum they are
@@ -62,13 +59,6 @@ FE_DEV f32x16 mma_held_right(const Parts& x, bf16x8 held, f32x16 c) {
 
 template <typename V, typename T> FE_DEV V ldv(const T* p) { return *reinterpret_cast<const V*>(p); }
 
-// Eight columns from four bytes of codes and the block's power of two.
-FE_DEV bf16x8 values8(unsigned w, float unit) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-FE_DEV float unit_of(unsigned scale) { return __uint_as_float(scale << 23); }   // 255: NaN from the conversion
 
 FE_DEV int q_rows(const PackedArgs& a, int bk) { return a.q_len ? min(max(a.q_len[bk], 0), a.S) : a.S; }
 FE_DEV int own_rows(const PackedArgs& a, int bk) { return a.own.cap ? packed_len(a.own, bk) : 0; }
@@ -752,7 +742,7 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
 
 // ------------------------------------------------------------------------------------------
 // Weights.  A workgroup takes a range of a sequence's keys of one head, and a range of the query rows that see them: every
-// list's for shared keys, the list's for own keys.  The rows lie in LDS, as many as fit; each wave walks tiles of 32 NK keys
+// list's for shared keys, the list's for own keys.  The rows lie in LDS, as many as fit; each wave walks tiles of 32 keys
 // without meeting the others, its operands made in registers from the codes, whose loads run a tile ahead and their pages two.
 // Which column a summed element is does not matter: lane l has the half l / 32 of its key's columns.  A lane then holds 16
 // rows' scores of its key, and their exponentials are added up in it.
@@ -775,7 +765,7 @@ template <typename T, int DH> struct Weigh {
     int any;
   };
 
-  template <bool OWN, int NK> static FE_DEV void run(const PackedArgs& a, int id, Lds& S) {
+  template <bool OWN> static FE_DEV void run(const PackedArgs& a, int id, Lds& S) {
     constexpr int WORDS = DH / 16, SCALES = DH == 128 ? 2 : 1;         // of a lane: half a key's codes, and their blocks' scales
     const PackedCache& x = OWN ? a.own : a.ctx;
     const int key_splits = OWN ? a.own_keys : a.ctx_keys, row_splits = OWN ? a.own_splits : a.ctx_splits;
@@ -787,42 +777,36 @@ template <typename T, int DH> struct Weigh {
     int sq = id / key_splits, zk = id % key_splits, ranges = key_splits;
     if (!OWN && a.keys_by_length && !range_of(a, id, 0, sq, zk, ranges)) return;   // uniform over the workgroup
     const int b = OWN ? sq / a.K : sq;
-    const int n = packed_len(x, sq), tiles = (n + 32 * NK - 1) / (32 * NK);
+    const int n = packed_len(x, sq), tiles = (n + 31) / 32;
     const int tb = share(tiles, zk, ranges), te = share(tiles, zk + 1, ranges);
     if (tb == te) return;                  // uniform over the workgroup
     const int nq = OWN ? q_rows(a, sq) : 0, rows = OWN ? nq * a.G : a.R, first = OWN ? (sq - b * a.K) * a.S * a.G : 0;
     const int rb = share(rows, z, row_splits), re = share(rows, z + 1, row_splits);
 
-    int page[NK], row[NK];                 // of the tile after the next: row -1 past the length
-    unsigned code[NK][WORDS], scale[NK][SCALES];
-    bool counts[NK];                       // of the tile whose codes are under way
+    int page, row;                         // of the tile after the next: row -1 past the length
+    unsigned code[WORDS], scale[SCALES];
+    bool counts;                           // of the tile whose codes are under way
     const int32_t* table = x.table + (long long)sq * x.cols;
     auto find = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-      for (int u = 0; u < NK; ++u) {
-        const int j = (t * NK + u) * 32 + (lane & 31);
-        row[u] = -1;
-        if (t < te && j < n) {
-          const int p = packed_page(x, j);
-          row[u] = j - p * x.page_rows;
-          page[u] = table[(unsigned)p];
-        }
+      const int j = t * 32 + (lane & 31);
+      row = -1;
+      if (t < te && j < n) {
+        const int p = packed_page(x, j);
+        row = j - p * x.page_rows;
+        page = table[(unsigned)p];
       }
     };
     auto load = [&]() __attribute__((always_inline)) {
+      counts = row >= 0 && (unsigned)page < (unsigned)x.n_pages;
+      const unsigned r = counts ? row : 0;                             // what does not count reads row 0 of page 0
+      const char* head = x.pages + (unsigned long long)(counts ? (unsigned)page : 0u) * (unsigned)x.page_ld;
+      const unsigned at = (unsigned)g * x.head_bytes;
+      const unsigned* w = reinterpret_cast<const unsigned*>(head + (at + r * (DH / 2) + half * (DH / 4)));
+      const unsigned char* s = reinterpret_cast<const unsigned char*>(head + (at + (unsigned)x.page_rows * DH + r * (DH / 32)));
 #pragma unroll
-      for (int u = 0; u < NK; ++u) {
-        counts[u] = row[u] >= 0 && (unsigned)page[u] < (unsigned)x.n_pages;
-        const unsigned r = counts[u] ? row[u] : 0;                     // what does not count reads row 0 of page 0
-        const char* head = x.pages + (unsigned long long)(counts[u] ? (unsigned)page[u] : 0u) * (unsigned)x.page_ld;
-        const unsigned at = (unsigned)g * x.head_bytes;
-        const unsigned* w = reinterpret_cast<const unsigned*>(head + (at + r * (DH / 2) + half * (DH / 4)));
-        const unsigned char* s = reinterpret_cast<const unsigned char*>(head + (at + (unsigned)x.page_rows * DH + r * (DH / 32)));
+      for (int i = 0; i < WORDS; ++i) code[i] = w[i];
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) code[u][i] = w[i];
-#pragma unroll
-        for (int i = 0; i < SCALES; ++i) scale[u][i] = s[DH == 32 ? 0 : half * SCALES + i];
-      }
+      for (int i = 0; i < SCALES; ++i) scale[i] = s[DH == 32 ? 0 : half * SCALES + i];
     };
     const int t0 = tb + wave;
     find(t0);
@@ -840,7 +824,7 @@ template <typename T, int DH> struct Weigh {
         find(t0);
         __syncthreads();                   // the rows before are no longer read
       }
-      // the rows' loads four units of a thread at a time, the first ones' and the keys' together
+      // the rows' loads two units of a thread at a time, the first ones' and the keys' together
       constexpr int BATCH = 2;
       const int units = (here + 31) / 32 * 32 * (DH / 8);
       typename F::V v[BATCH];
@@ -890,34 +874,26 @@ template <typename T, int DH> struct Weigh {
       __syncthreads();
       const bool any = S.any;              // a row that counts: those that do not may have met NaN
       for (int t = t0; t < te; t += 4) {
-        bf16x8 k[NK][ND];
-        bool got[NK];
+        bf16x8 k[ND];
+        const bool got = counts;
 #pragma unroll
-        for (int u = 0; u < NK; ++u) {
-          got[u] = counts[u];
-#pragma unroll
-          for (int c = 0; c < ND; ++c) k[u][c] = values8(code[u][c], unit_of(scale[u][c * SCALES / ND]));
-        }
+        for (int c = 0; c < ND; ++c) k[c] = values8(code[c], unit_of(scale[c * SCALES / ND]));
         if (t + 4 < te) {                  // uniform
           load();
           find(t + 8);
         }
-        float sum[NK];
-#pragma unroll
-        for (int u = 0; u < NK; ++u) sum[u] = 0.f;
+        float sum = 0.f;
+        const int j = t * 32 + (lane & 31);
 #pragma unroll 1
         for (int r = 0; r < here; r += 32) {
-          f32x16 s[NK];
-#pragma unroll
-          for (int u = 0; u < NK; ++u) s[u] = f32x16{};
+          f32x16 s{};
 #pragma unroll
           for (int c = 0; c < ND; ++c) {
             const int at = r * DH + (from ^ c << 3);
             typename F::Op q;
             if constexpr (PARTS == 1) q = ldv<bf16x8>(S.q[0] + at);
             else q = Parts{{ldv<bf16x8>(S.q[0] + at), ldv<bf16x8>(S.q[1] + at), ldv<bf16x8>(S.q[2] + at)}};
-#pragma unroll
-            for (int u = 0; u < NK; ++u) s[u] = mma_held_right(q, k[u][c], s[u]);
+            s = mma_held_right(q, k[c], s);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {    // rows 8 e + 4 half + 0 .. 3
@@ -925,30 +901,22 @@ template <typename T, int DH> struct Weigh {
             const f32x4 ls = ldv<f32x4>(S.lse + r + 8 * e + 4 * half);
             int4 seen;
             if (OWN) seen = ldv<int4>(S.seen + r + 8 * e + 4 * half);
+            float p[4];
 #pragma unroll
-            for (int u = 0; u < NK; ++u) {
-              float p[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][4 * e + i], sl2, -ls[i]));
-              if (OWN) {
-                const int j = (t * NK + u) * 32 + (lane & 31);
-                p[0] = j < seen.x ? p[0] : 0.f;
-                p[1] = j < seen.y ? p[1] : 0.f;
-                p[2] = j < seen.z ? p[2] : 0.f;
-                p[3] = j < seen.w ? p[3] : 0.f;
-              }
-              sum[u] += (p[0] + p[1]) + (p[2] + p[3]);
+            for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[4 * e + i], sl2, -ls[i]));
+            if (OWN) {
+              p[0] = j < seen.x ? p[0] : 0.f;
+              p[1] = j < seen.y ? p[1] : 0.f;
+              p[2] = j < seen.z ? p[2] : 0.f;
+              p[3] = j < seen.w ? p[3] : 0.f;
             }
+            sum += (p[0] + p[1]) + (p[2] + p[3]);
           }
         }
-#pragma unroll
-        for (int u = 0; u < NK; ++u) {
-          const float total = halves_sum(sum[u]), add = got[u] && any ? total : 0.f;
-          const int j = (t * NK + u) * 32 + (lane & 31);
-          if (j >= n || half) continue;
-          const float had = rc > rb ? out[base + j] : row_splits > 1 ? 0.f : w_in[base + j];
-          out[base + j] = had + add;
-        }
+        const float total = halves_sum(sum), add = got && any ? total : 0.f;
+        if (j >= n || half) continue;
+        const float had = rc > rb ? out[base + j] : row_splits > 1 ? 0.f : w_in[base + j];
+        out[base + j] = had + add;
       }
     }
   }
@@ -959,8 +927,8 @@ __global__ __launch_bounds__(256, sizeof(T) * DH > 256 ? 2 : 4) void k_packed_we
   typedef Weigh<T, DH> W;
   __shared__ typename W::Lds S;
   const int id = blockIdx.x, n_ctx = a.ctx_w ? a.B * a.Hkv * a.ctx_splits * a.ctx_keys : 0;
-  if (id < n_ctx) W::template run<false, 1>(a, xcd_tile(id, n_ctx), S);   // uniform
-  else W::template run<true, 1>(a, id - n_ctx, S);
+  if (id < n_ctx) W::template run<false>(a, xcd_tile(id, n_ctx), S);   // uniform
+  else W::template run<true>(a, id - n_ctx, S);
 }
 
 // Adds the row ranges of every key in ascending order.  Bound: the partial sums; launch latency where they are few.
@@ -977,7 +945,8 @@ __global__ __launch_bounds__(256) void k_packed_weigh_sum(PackedCache x, int Hkv
 
 template <typename T, int DH>
 hipError_t fwd(const PackedArgs& a, const PackedPlan& p, hipStream_t s) {
-  constexpr int UE = DH == 128 ? 32 : 16, U1 = DH == 32 ? 16 : 32, W1 = DH == 128 || sizeof(T) == 4 ? 8 : 16;
+  // waves of the wide form, which heads of 128 in fp32 do not have
+  constexpr int UE = DH == 128 ? 32 : 16, U1 = DH == 32 ? 16 : 32, W1 = sizeof(T) == 4 ? (DH == 128 ? 4 : 8) : DH == 128 ? 8 : 16;
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.splits * a.tiles));
   if (p.waves == 1 && p.wide) hipLaunchKernelGGL((k_packed_fwd<T, DH, 1, U1, W1>), grid, dim3(64 * W1), 0, s, a);
   else if (p.waves == 1) hipLaunchKernelGGL((k_packed_fwd<T, DH, 1, U1, 4>), grid, dim3(256), 0, s, a);
@@ -1046,14 +1015,14 @@ PackedWeighPlan packed_weigh_plan(const fe_packed_args& a) {
   const long long bg = (long long)a.B * a.n_kv_heads, most = (1 << 24) - 1;
   // Workgroups: key ranges until there are some for every compute unit, each of a tile a wave at least; then row ranges, of 128
   // rows at least.
-  auto ranges = [&](long long sequences, long long keys, int tile, long long rows, int* by_key, int* by_row) {
+  auto ranges = [&](long long sequences, long long keys, long long rows, int* by_key, int* by_row) {
     const long long want = (1024 + sequences - 1) / sequences;
-    *by_key = (int)std::max(1LL, std::min({want, (keys + 4 * tile - 1) / (4 * tile), most / std::max(1LL, sequences)}));
+    *by_key = (int)std::max(1LL, std::min({want, (keys + 127) / 128, most / std::max(1LL, sequences)}));
     *by_row = (int)std::max(1LL, std::min({want / *by_key, rows / 128, 64LL, most / std::max(1LL, sequences * *by_key)}));
   };
   p.ctx_keys = p.ctx_splits = p.own_keys = p.own_splits = 1;
-  if (T) ranges(bg, T, 32, R, &p.ctx_keys, &p.ctx_splits);
-  if (L) ranges(bg * a.K, L, 32, sg, &p.own_keys, &p.own_splits);
+  if (T) ranges(bg, T, R, &p.ctx_keys, &p.ctx_splits);
+  if (L) ranges(bg * a.K, L, sg, &p.own_keys, &p.own_splits);
   p.keys_by_length = p.ctx_keys >= 8 && a.B > 1 && a.B <= 64 && T >= 512 * p.ctx_keys;
   p.ctx_bytes = p.ctx_splits > 1 ? (size_t)p.ctx_splits * bg * T * sizeof(float) : 0;
   p.own_bytes = p.own_splits > 1 ? (size_t)p.own_splits * bg * a.K * L * sizeof(float) : 0;

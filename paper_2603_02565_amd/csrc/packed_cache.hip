@@ -2,11 +2,10 @@
 #include <algorithm>
 
 #include "packed.h"
+#include "prefix.h"
 
 namespace {
 
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> { typedef bf16x8 type; };
 template <> struct Vec8<float> { typedef f32x8 type; };
@@ -208,19 +207,6 @@ __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, 
   }
 }
 
-__global__ void k_packed_advance(int32_t* len, const int32_t* new_len, int N, int S) {
-  const int s = blockIdx.x * 256 + threadIdx.x;
-  if (s >= N) return;
-  const int n = new_len ? min(max(new_len[s], 0), S) : S;
-  len[s] = (int)min((long long)max(len[s], 0) + n, 0x7fffffffLL);
-}
-
-// Eight columns of a row from four bytes of codes.
-FE_DEV bf16x8 values8(unsigned w, float unit) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 FE_DEV void put8(bf16* p, bf16x8 v) { *reinterpret_cast<bf16x8*>(p) = v; }
 FE_DEV void put8(float* p, bf16x8 v) {
   f32x8 w;
@@ -250,8 +236,8 @@ __global__ __launch_bounds__(256) void k_packed_read(fe_packed_read_args a, Pack
       const unsigned char* scale =
           reinterpret_cast<const unsigned char*>(head) + 2 * all + ((long long)r << (log_units - 2)) + (x >> 2);
       const unsigned kw = *reinterpret_cast<const unsigned*>(head + at), vw = *reinterpret_cast<const unsigned*>(head + all + at);
-      k = values8(kw, __uint_as_float((unsigned)scale[0] << 23));
-      v = values8(vw, __uint_as_float((unsigned)scale[(long long)c.page_rows << (log_units - 2)] << 23));
+      k = values8(kw, unit_of(scale[0]));
+      v = values8(vw, unit_of(scale[(long long)c.page_rows << (log_units - 2)]));
     }
   }
   if (a.k) put8(static_cast<T*>(a.k) + row * a.k_ld + h * a.dh + 8 * x, k);
@@ -378,7 +364,7 @@ template <int E>
 __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
   constexpr int NW = 16, NT = NW * 64, SEG = NT * E;
   __shared__ int s_hist[256 * 32];
-  __shared__ int s_sum[256], s_kept[NW + 1], s_equal[NW + 1], s_digit, s_left, s_whole;
+  __shared__ int s_sum[256], s_kept[NW], s_equal[NW], s_digit, s_left, s_whole;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int s = blockIdx.x / a.n_kv_heads, h = blockIdx.x % a.n_kv_heads;
   const int n = packed_len(from, s), m = min(a.keep, n);
@@ -552,11 +538,7 @@ hipError_t launch_packed_append(const fe_packed_append_args& a, hipStream_t s) {
   else
     hipLaunchKernelGGL(k_packed_append<float>, grid, dim3(256), 0, s, a, c, log_rows, blocks);
   hipError_t e = hipGetLastError();
-  if (e == hipSuccess && a.len_out == a.cache.len && a.len_out && blocks > 1) {
-    hipLaunchKernelGGL(k_packed_advance, dim3((unsigned)((a.cache.N + 255) / 256)), dim3(256), 0, s, a.len_out, a.new_len,
-                       a.cache.N, a.S);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && a.len_out == a.cache.len && a.len_out && blocks > 1) e = launch_advance(a.len_out, a.new_len, a.cache.N, a.S, s);
   return e;
 }
 

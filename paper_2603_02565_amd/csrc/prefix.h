@@ -48,4 +48,5 @@ struct PrefixGradPlan {
 };
 PrefixGradPlan prefix_grad_plan(const fe_prefix_args& a);
 hipError_t launch_prefix_grad(const PrefixGradArgs& a, int dh, bool bf16_rows, const PrefixGradPlan& p, hipStream_t s);
+hipError_t launch_advance(int32_t* len, const int32_t* new_len, int N, int S, hipStream_t s);   // lengths in place, after an append
 hipError_t launch_cache_append(const fe_append_args& a, hipStream_t s);
