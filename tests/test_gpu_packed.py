@@ -1171,3 +1171,55 @@ def test_many_threads_read_one_cache():
     for t in threads:
         t.join()
     assert not bad, bad[:5]
+
+
+# ---------------------------------------------------------------------------------------------
+# Parts of prompts over long documents: own rows in the common loop, ranges of keys that are joined
+# ---------------------------------------------------------------------------------------------
+
+PARTS = [
+    dict(dtype="bf16", B=1, K=1, S=200, H=4, Hkv=2, dh=128, T=1500, L=400),
+    dict(dtype="bf16", B=1, K=1, S=200, H=4, Hkv=2, dh=128, T=1500, L=400, lens="full"),
+    dict(dtype="bf16", B=2, K=3, S=70, H=2, Hkv=2, dh=64, T=900, L=150, P=7),
+    dict(dtype="bf16", B=1, K=1, S=60, H=2, Hkv=2, dh=32, T=2000, L=300, P=48),
+    dict(dtype="bf16", B=1, K=3, S=70, H=2, Hkv=2, dh=32, T=1000, L=90, P=5, causal=False),
+    dict(dtype="f32", B=1, K=1, S=150, H=2, Hkv=1, dh=64, T=1100, L=320),
+    dict(dtype="f32", B=1, K=1, S=130, H=1, Hkv=1, dh=128, T=800, L=200, P=48),
+    dict(dtype="f32", B=1, K=2, S=70, H=2, Hkv=2, dh=32, T=700, L=130, P=7),
+    dict(dtype="bf16", B=2, K=2, S=90, H=2, Hkv=1, dh=64, T=1200, L=200, holes=20),
+    # ... in proportion to the requests' lengths
+    dict(dtype="bf16", B=4, K=1, S=130, H=4, Hkv=4, dh=32, T=16384, L=200, P=64),
+    dict(dtype="bf16", B=2, K=2, S=66, H=8, Hkv=8, dh=64, T=16384, L=100, P=64),
+]
+
+
+@pytest.mark.parametrize("kw", PARTS, ids=IDS)
+def test_attention_of_prompt_parts(kw):
+    c = Case(**kw, seed=1)
+    size = fe.fe_packed_workspace_size(_sizes(c))
+    assert size > 0                                                       # several ranges of keys
+    test_attention(kw)
+
+
+@pytest.mark.parametrize("kw", PARTS[:9], ids=IDS)
+def test_weights_of_prompt_parts(kw):
+    test_weights(kw)
+
+
+@pytest.mark.parametrize("kw", [dict(dtype="bf16", B=2, K=9, S=4, H=4, Hkv=2, dh=64, T=50, L=24, P=4),
+                                dict(dtype="bf16", B=1, K=3, S=70, H=2, Hkv=2, dh=32, T=1000, L=90, P=5),
+                                dict(dtype="f32", B=2, K=13, S=3, H=2, Hkv=1, dh=64, T=300, L=30, P=16)], ids=IDS)
+def test_a_list_beside_lists_of_other_lengths(kw):
+    """Other lengths of the other lists move a list's keys to other places, so that its sums may have another order, and no more."""
+    c = Case(**kw, lens="full", seed=14)
+    own = c.K // 2
+    for others in (0, 1, 3):
+        d = Case(**kw, lens="full", seed=14)
+        d.nq, d.no = np.full((c.B, c.K), min(others, c.S)), np.full((c.B, c.K), others)
+        d.nq[:, own], d.no[:, own] = c.S, c.no[:, own]
+        d.device()
+        want = d.reference()
+        out, lse = d.run()
+        _near(out, want["out"], "out")
+        _near(lse, want["lse"], "lse")
+        assert torch.isfinite(out[:, own]).all()

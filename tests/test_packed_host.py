@@ -289,3 +289,24 @@ def test_strided_weights_check_what_the_dense_ones_do():
         a = _fill(many, {}, n)
         st = lib.fe_packed_weights_strided(ctypes.byref(a), (ctypes.c_int64 * 4)(-5 if n else 1, 1, 0, 7), None)
         assert st == fe.FE_EINVAL and "workspace" in lib.fe_last_error().decode()
+
+
+def test_reference_weights_keep_to_the_mask():
+    """The last own key is seen by the last query row alone, the first by all; without the mask by all of them."""
+    from tests import prefix_reference as dense
+    r = np.random.default_rng(4)
+    q, ck, ok = r.standard_normal((1, 2, 3, 4, 32)), r.standard_normal((1, 9, 2, 32)), r.standard_normal((1, 2, 5, 2, 32))
+    kw = dict(scale=0.2, ctx_len=np.array([7]), q_len=np.array([[3, 2]]), own_len=np.array([[5, 4]]))
+    zero = dict(ctx_w=np.zeros((1, 2, 9)), own_w=np.zeros((1, 2, 2, 5)))
+    for causal in (True, False):
+        lse = dense.attend(q, ck, ck, ok, ok, dtype="f32", causal=causal, **kw)["lse"][0]
+        w = ref.weigh(q, ck, ok, lse, causal=causal, **kw, **zero)
+        for k, (n, m) in enumerate(((3, 5), (2, 4))):
+            for g in range(2):
+                for j in range(m):
+                    rows = [i for i in range(n) if not causal or j <= m - n + i]
+                    want = sum(np.exp(0.2 * (q[0, k, i, h] @ ok[0, k, j, g]) - lse[0, k, i, h]) for i in rows for h in (2 * g, 2 * g + 1))
+                    assert abs(w["own_w"][0][0, k, g, j] - want) < 1e-13
+        lse[0, 0, 2] = -np.inf                                            # the last row of list 0 gives nothing
+        w = ref.weigh(q, ck, ok, lse, causal=causal, **kw, **zero)
+        assert ((w["own_w"][0][0, 0, :, 4] == 0) == causal).all() and (w["own_w"][0][0, 0, :, 3] > 0).all()
