@@ -108,12 +108,13 @@ fe_status fe_packed_read(const fe_packed_read_args* a, void* stream);
  * A row without keys gives out = 0 and lse = -infinity, and so do the rows i >= n.  ctx.N = B and own.N = B * K, or 0: none.
  *
  * Scores, the softmax's maximum and sum and the output sums are fp32.  FE_BF16: the products of the queries' bf16 values with
- * the held ones are exact, probabilities are rounded to bf16 for the product with the values (up to
- * 32 rows a request and key head: to two bf16, 16 bits).  FE_F32: queries and
- * probabilities in three bf16 parts whose sum they are, the held values whole: no product is rounded.  A row
- * with a score of +infinity or NaN is NaN, and so is one whose scores are all -infinity; beside finite ones a score of
- * -infinity weighs nothing.  (Scores are fp32: infinite from 2^128 on.)  A list's outputs do not depend on the own rows of other lists, NaN or not.  Results have the same
- * bits from call to call.
+ * the held ones are exact, probabilities are rounded to bf16 for the product with the values (where K * S * n_heads /
+ * n_kv_heads, the rows of a request and key head, are at most 32: to two bf16, 16 bits).  FE_F32: queries and
+ * probabilities in three bf16 parts whose sum they are, the held values whole: no product is rounded.
+ * A row with a score of +infinity or NaN is NaN, and so is one whose scores are all -infinity; beside finite ones a score of
+ * -infinity weighs nothing.  Scores are fp32 (infinite from 2^128 on).
+ * What the own rows of other lists hold, NaN or not, changes no bit of a list's outputs; how many rows the other lists and
+ * requests have may change the order of its sums.  The same call has the same bits each time.
  *
  * fe_packed_weights: for every row j < len of `ctx` and of `own` and every key head g
  *   w_out[s][g][j] = w[s][g][j] + sum over the query rows and heads of g that see it of exp(scale * q.k - lse)

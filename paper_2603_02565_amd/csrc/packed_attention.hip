@@ -243,11 +243,11 @@ FE_DEV void order() { asm volatile("" ::: "memory"); }   // LDS operations of on
 // each, which meet no barrier.  Own rows of short lists are seen by few of a tile's rows: staged by every wave for itself (4
 // x 32 lists over 32768 rows, heads of 128: 105 us -> 97; 64 x 50 slates of 11: 34 -> 27).  Two blocks of keys at a time, at one
 // or two waves fewer a SIMD (115 -> 108, prompts 281 -> 261).
-// Bound: no unit alone.  2 x 2048 rows of 16 heads of 128 over 5120 keys: 223 us, 770 TFLOP/s, with the vector unit busy 42% of
-// the time, matrix cores 32%, LDS 32%, waits 31% of the waves' time; leaving out any one of staging, exponentials, either product or
-// the loads takes 8 to 15% away.  4 x 32 x 4 rows a key head over 16384 .. 32768: 96 us and the join's 10 (145 MB,
-// 52 GFLOP).  64 x 550 rows of 4 heads of 32 over 267 keys: 25 us, vector unit 60%, a third of it outside the score loop.
-// 5 rows of 181 keys: 7.7 us, a chain of dependent trips to memory.
+// Bound: no unit alone.  2 x 2048 rows of 16 heads of 128 over 5120 keys: 225 us, 763 TFLOP/s, with the vector unit busy 42% of
+// the time, matrix cores 32%, LDS 33%, waits 30% of the waves' time; leaving out any one of staging, exponentials, either product or
+// the loads takes 8 to 15% away.  4 x 32 x 4 rows a key head over 16384 .. 32768: 97 us and the join's 10 (145 MB,
+// 52 GFLOP).  64 x 550 rows of 4 heads of 32 over 267 keys: 24.4 us, vector unit 60%, a third of it outside the score loop.
+// 5 rows of 181 keys: 7.6 us, a chain of dependent trips to memory.
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH, int WR, int UE, int W> struct Shape {
   static constexpr int WK = W / WR, GT = 64 * WR, ROWS = 32 * WR, UPR = DH / UE;
@@ -526,7 +526,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : fwd_waves(sizeof(T), DH, WR
         for (int j = 0; j < 8; ++j) w[j] = s[u][8 * m + j];
         const Op p = F::rounded(w);
         // bf16: one rounding of p, of about the size of out's own (out off by 2.3e-3 of its norm, 1.7e-3 without it).  Up to 32 rows
-        // what it cut is a second product: these calls wait for memory, and few outputs do not average the roundings out.
+        // what it cut is a second product, since these calls wait for memory (4 x 16 rows a key head: 15.7 us either way).  For more
+        // rows it would take 32 lists over 32768 rows from 106 to 119 us, slates from 24.8 to 29.5 and prompts from 224 to 283.
         Op rest;
         if constexpr (FINE) {
 #pragma unroll
@@ -750,8 +751,8 @@ __global__ __launch_bounds__(256) void k_packed_join(PackedArgs a) {
 // Operands of 32 keys a wave and four waves a SIMD: two operands, half the reads of LDS, leave room for two waves (32 lists
 // over 32768 rows, heads of 128: 73 us and 54).  Key ranges by the requests' lengths: 54 -> 48; 1024 workgroups: 512
 // 59 us, 768 50, 1024 51, 2048 57.
-// Bound: the vector unit, 63% (a product-sum, an exponential and a sum a score; the codes' conversion): 46 us, 561 TFLOP/s.
-// 8 x 16 lists over 1024: 7.5 us, three dependent trips to memory.
+// Bound: the vector unit, 63% (a product-sum, an exponential and a sum a score; the codes' conversion): 45 us, 575 TFLOP/s,
+// with three registers spilled while the rows are put into LDS.  8 x 16 lists over 1024: 7.7 us, three dependent trips to memory.
 // ------------------------------------------------------------------------------------------
 template <typename T, int DH> struct Weigh {
   typedef Form<T> F;
@@ -997,7 +998,8 @@ PackedPlan packed_plan(const fe_packed_args& a) {
   // and 16 chunks 16.1, 15.7; fp32, 6 x 399 rows of 777 in 2 and 4 chunks 18.1, 20.9.
   long long want = ((p.wide ? 256 : 512) + wgs - 1) / wgs;
   want = std::min(want, std::max(1LL, items / (p.wide ? 16 : a.dtype == FE_F32 ? 2 : 4)));
-  if (a.dtype == FE_F32) want = std::max(want, (items + 31) / 32);   // fp32 sums over at most 2048 keys
+  // fp32 sums over at most 2048 keys, up to 524288 of them; above, over a 256th (more on grids past their limit)
+  if (a.dtype == FE_F32) want = std::max(want, (items + 31) / 32);
   const long long grid = ((1 << 24) - 1) / std::max(1LL, wgs);
   p.splits = (int)std::max(1LL, std::min({want, 256LL, grid}));
   p.by_length = a.dtype == FE_BF16 && p.splits >= 8 && a.B > 1 && a.B <= 64 && T >= 1024 * p.splits;

@@ -82,7 +82,7 @@ constexpr int kAppendRows = 64;           // rows of a workgroup
 // formed once, in LDS, for all its heads; then every thread takes units of 8 columns, 4 lanes a block, consecutive
 // units along a row, then rows, then heads, as the pages hold them.
 // Bound: the vector unit (fp64 and the sines) beside HBM: 24 x 1000 rows of 24 heads of 128, bf16, 246 MB: 68 us, 3.6 TB/s.  The
-// queries in fp32 60 us, but then a turned query may go to the number that is not the nearest.  128 rows of 24 heads of 64: 4.6 us,
+// queries in fp32 60 us, but then a turned query may go to the number that is not the nearest.  128 rows of 24 heads of 64: 4.8 us,
 // launch latency and a trip to memory.
 template <typename T>
 __global__ __launch_bounds__(256) void k_packed_append(fe_packed_append_args a, PackedCache c, int log_rows, int blocks) {
@@ -356,9 +356,10 @@ __global__ __launch_bounds__(256) void k_packed_evict_short(fe_packed_evict_args
 // a histogram in LDS, in 32 copies by lane so that equal digits, the rule among weights, do not meet in one word.  Then
 // every wave walks its rows in order and numbers what is kept.  The orders of 1024 E rows stay in registers where they are
 // all.  Rows that are kept in any case have the highest order, which no weight has, and what is no row the order 0.
-// Bound: instructions of the one compute unit that a head has (32 heads of 32768 rows: 20.1 us, of which the loads take 4 and
+// Bound: instructions of the one compute unit that a head has (32 heads of 32768 rows: 21.6 us, of which the loads take 4 and
 // a pass 3; the last pass is left out where the third one ends on a digit that is kept whole, as among weights that
-// hardly repeat it does; with it 21.9).
+// hardly repeat it does; with it 1.8 more).  Above 32768 rows the weights are read again in every pass: 131072 rows, with the move of
+// 32768, 205 us, where 32768 rows and 8192 take 37.
 constexpr unsigned kCertain = 0xffffffffu;
 template <int E>
 __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, PackedCache from, PackedCache to) {
@@ -492,7 +493,7 @@ __global__ __launch_bounds__(1024) void k_packed_select(fe_packed_evict_args a, 
 }
 
 // The kept rows: a thread takes one block, of keys and of values, the first of a row its weight as well.  Bound: HBM at 64
-// contiguous bytes a row (4 x 8192 rows of 8 heads of 128, 71 MB: 19 us, 3.7 TB/s).
+// contiguous bytes a row (4 x 8192 rows of 8 heads of 128, 71 MB: 24 us, 3.0 TB/s).
 __global__ __launch_bounds__(256) void k_packed_move(fe_packed_evict_args a, PackedCache from, PackedCache to, int blocks) {
   const int sh = blockIdx.x / blocks, blk = blockIdx.x % blocks, s = sh / a.n_kv_heads, h = sh - s * a.n_kv_heads;
   const int log_blocks = a.dh == 32 ? 0 : a.dh == 64 ? 1 : 2;
